@@ -438,6 +438,163 @@ int viscache_kv4_dequantize(const vc_batch* batch, const vc_params* p, const uin
                             void* K_hat, void* V_hat, void* stream);
 
 /*
+ * viscache_mrope -- rotary positions with several axes (time, height, width
+ * of a visual token; text tokens carry the same position on every axis),
+ * applied to a step's query and key rows.  The paper's models rotate before
+ * the cache is written; this is that step, forward and inverse.
+ *
+ * Of each head's d values the first 2 * half are turned, half = sum of the
+ * sections: pair i (i < half) by the angle
+ *     w_i = positions[axis(i)][row] * theta^(-i / half),
+ *     a' = a cos w - b sin w,   b' = b cos w + a sin w,
+ * the rest is copied.  With inverse != 0 the angle is -w: it takes a rotation
+ * off again, and is the gradient of the forward call.  The angle is reduced
+ * in integers, so it is exact for every int32 position; products and sums in
+ * fp32, one rounding to the type.
+ *   order     VC_ROPE_SECTIONED: axis 0 has the first sections[0]
+ *             frequencies, axis 1 the next sections[1], ...;
+ *             VC_ROPE_INTERLEAVED: frequency i belongs to axis i % n_axes if
+ *             i < n_axes * sections[that axis], and to axis 0 otherwise (so an
+ *             axis whose turns run past half has those that fit)
+ *   pairing   VC_ROPE_HALVES: pair i is values (i, half + i);
+ *             VC_ROPE_ADJACENT: values (2i, 2i + 1)
+ *   positions device int32 [n_axes][n_rows]
+ *   q, k      device rows: row r, head j at element r * stride + j * d;
+ *             strides are multiples of 16 bytes, at least heads * d.  Hq or Hkv
+ *             may be 0 (then its pointers may be NULL)
+ *   q_out, k_out  the same with their own strides; an output may be its input
+ *             (same pointer and stride) and may not overlap it otherwise
+ * d in {64, 128}; half a multiple of 8, at most d / 2; n_axes 1..4; theta >= 1.
+ * n_rows = 0 does nothing.  No workspace; asynchronous on `stream`.
+ * Errors: VC_ERR_INVALID_ARG, VC_ERR_CUDA.
+ */
+#define VC_ROPE_SECTIONED   0
+#define VC_ROPE_INTERLEAVED 1
+#define VC_ROPE_HALVES      0
+#define VC_ROPE_ADJACENT    1
+typedef struct {
+    int32_t n_axes;
+    int32_t sections[4];
+    int32_t order;            /* VC_ROPE_SECTIONED or VC_ROPE_INTERLEAVED */
+    int32_t pairing;          /* VC_ROPE_HALVES or VC_ROPE_ADJACENT */
+    double theta;
+} vc_rope;
+int viscache_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int64_t n_rows, int32_t Hq,
+                   int32_t Hkv, int32_t d, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                   int inverse, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                   void* stream);
+
+/*
+ * viscache_kv8_* -- a layer's KV cache in 8-bit floating point, in pages, for
+ * serving: what the pass kept and what arrives after it (text, new frames)
+ * go into the same pages as they come, and every step attends over them.
+ *
+ * A page holds `page` tokens of every KV head as e4m3 codes (1 sign, 4
+ * exponent, 3 mantissa bits, largest value 448, no infinity) and one scale
+ * per KV head for the keys and one for the values:
+ *     x_hat = code * scale,   scale = 2^e or 0.
+ * A power of two costs e4m3 nothing (its spacing is relative) and makes the
+ * codes exact to rescale.  With amax the largest finite |x| written to a page
+ * and head, e is the least integer, at least -126, with amax <= 448 * 2^e; the
+ * scale is 0 where amax is 0.  x / scale is rounded to nearest even; an x that
+ * is not finite is stored as NaN and does not count for amax.
+ *
+ * vc_kv8       one layer's pool: codes device uint8 [n_pages][Hkv][page][d],
+ *              scales device fp32 [n_pages][Hkv]; 16-byte aligned.  page is 16,
+ *              32, 64 or 128; d 64 or 128; n_pages * Hkv * page < 2^31
+ * vc_kv8_step  the requests of one call, the same for every layer of a step:
+ *              token t of request r is slot t % page of page
+ *              block_table[r][t / page].  Request r has the packed rows
+ *              row_start[r] .. row_start[r + 1] - 1, which are its LAST tokens:
+ *              with m rows and seq_lens[r] tokens (the rows included), row i is
+ *              token seq_lens[r] - m + i.  All three arrays are on the device,
+ *              so that a captured graph can be replayed with new lengths;
+ *              n_req is 1..1024, n_rows (the rows the row arrays hold) at most
+ *              2^24, max_pages the block table's row length.  m may be 0; m may
+ *              exceed the length (the surplus first rows are then no tokens:
+ *              they are not written, and attend to nothing).
+ * The device arrays are checked as they are used: a length outside
+ * [0, max_pages * page], a request whose rows do not lie in [0, n_rows] in
+ * order, or a page outside [0, n_pages) sets VC_ERR_DEVICE_INDEX
+ * (prunekv_get_status) and is clamped or skipped; nothing out of range is
+ * read or written.  What the pages hold beyond seq_lens is never used.
+ *
+ * Workspace for every call: viscache_kv8_workspace_size(n_rows, Hq, Hkv, d)
+ * bytes (Hq = Hkv for append and read), 256-byte aligned; calls that may
+ * overlap need their own.  No device memory is allocated; calls are
+ * asynchronous on `stream`.  Errors: VC_ERR_INVALID_ARG, VC_ERR_WORKSPACE,
+ * VC_ERR_CUDA.
+ */
+typedef struct {
+    void* K_codes;
+    void* V_codes;
+    float* K_scale;
+    float* V_scale;
+    int32_t n_pages, Hkv, page, d;
+} vc_kv8;
+typedef struct {
+    int32_t n_req;
+    int32_t max_pages;
+    const int32_t* block_table;   /* device [n_req][max_pages] */
+    const int32_t* seq_lens;      /* device [n_req] */
+    const int32_t* row_start;     /* device [n_req + 1] */
+    int32_t n_rows;
+} vc_kv8_step;
+size_t viscache_kv8_workspace_size(int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t d);
+
+/*
+ * viscache_kv8_append -- write the step's key and value rows into the cache.
+ * Where a page already holds tokens of the request, its scale only grows:
+ * the older codes are then re-encoded (code * old / new, to nearest even),
+ * exact but for values that fall below e4m3's smallest normal number.  A
+ * page's scale is taken from the request's tokens alone: what a page held
+ * before the request's first token in it does not count.  Writing the same
+ * rows again gives the same cache.
+ *   K, V      device rows of `dtype` (VC_BF16 or VC_F32): row i, head g at
+ *             element i * row stride + g * head stride, strides multiples of
+ *             16 bytes (so a fused projection's slice, or prunekv_compress's
+ *             [Hkv][B][d] block, is read in place)
+ */
+int viscache_kv8_append(const vc_kv8* cache, const vc_kv8_step* step, int dtype, const void* K,
+                        int64_t k_row_stride, int64_t k_head_stride, const void* V, int64_t v_row_stride,
+                        int64_t v_head_stride, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * viscache_kv8_read -- the step's rows (tokens seq_lens - m .. seq_lens - 1 of
+ * each request) back from the cache, x_hat rounded once to `dtype`:
+ * K_hat, V_hat device [n_rows][Hkv][d].  With row_start the running sum of
+ * seq_lens it reads whole requests.  Rows that are no tokens, or whose page is
+ * out of range, are left as they were.
+ */
+int viscache_kv8_read(const vc_kv8* cache, const vc_kv8_step* step, int dtype, void* K_hat, void* V_hat,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * viscache_kv8_attention -- the step's query rows over their requests' pages:
+ *     out[i][j] = softmax_t(scale * q[i][j] . K_hat[t][g]) V_hat[t][g],
+ * g = j / (Hq / Hkv), t over the tokens 0 .. seq_lens - 1, with causal != 0
+ * only those up to the row's own (0 .. seq_lens - m + i).  The rows of a step
+ * are appended first.  One row a request is a decode step, many are a chunk
+ * of a prompt; both in one call are fine.
+ *   q       device rows of `dtype`: row i, head j at element i * q_stride + j * d
+ *           (q_stride a multiple of 16 bytes)
+ *   scale   0 selects 1/sqrt(d)
+ *   out     device [n_rows][Hq][d] of `dtype`; a row that sees no token gets zeros
+ *   lse     device fp32 [n_rows][Hq] (nullable): natural log of the softmax's
+ *           normaliser, -inf for a row that sees no token
+ * Arithmetic: e4m3 values and query rows enter the products as fp16 numbers
+ * times powers of two, bf16 rows without rounding but for values more than
+ * 2^14 below their row's largest, fp32 rows and fp32 calls' probabilities as
+ * sums of two such numbers; probabilities of bf16 calls are rounded to fp16
+ * (11 bits); sums, maxima and the softmax's normaliser in fp32.  The result
+ * does not depend on what else is in the batch but for the order of sums, and
+ * is the same for the same call.
+ */
+int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dtype, int32_t Hq, const void* q,
+                           int64_t q_stride, float scale, int causal, void* out, float* lse, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/*
  * Kernel path selection (process-wide, default VC_PATH_AUTO): AUTO runs the
  * score (Eq. token_score) and the fusion (Eq. redistribution, weight_fusion)
  * of bf16, d = 128 problems on the tcgen05 tensor cores and everything else

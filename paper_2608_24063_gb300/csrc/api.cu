@@ -10,6 +10,7 @@
 #include <atomic>
 #include <vector>
 
+#include "api_util.h"
 #include "kernels.h"
 #include "vc_common.cuh"
 
@@ -25,24 +26,10 @@ std::atomic<int> g_dependent_launch{1};
 
 namespace {
 
-constexpr size_t kAlign = 256;
-
 // Kernel path: VC_PATH_AUTO uses the tcgen05 score kernels for bf16, d = 128.
 std::atomic<int> g_path{VC_PATH_AUTO};
 // Test support: kernels whose next launches add one wait that must give up.
 std::atomic<int> g_test_wait{0};
-
-inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-
-// Sequential carving of the caller workspace into 256-byte aligned regions.
-struct Arena {
-  size_t off = 0;
-  size_t take(size_t bytes) {
-    const size_t o = off;
-    off = align_up(off + bytes);
-    return o;
-  }
-};
 
 struct RequestPlan {
   int32_t n = 0, W = 0, Nq = 0, h = 0;
@@ -342,20 +329,11 @@ cudaError_t launch_fuse(int dtype, const void* K, const void* V, const Layout& l
   return launch_fuse_simt(dtype, V, sh, tb, keep, drop, mu, tau, V_out, lay.units_fuse, st);
 }
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 bool valid_model(int dtype, int L, int Hq, int Hkv, int d) {
   if (dtype != VC_BF16 && dtype != VC_F32) return false;
   if (L < 1 || L > 256 || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0) return false;
   return d == 64 || d == 128;
 }
-
-int check_ws(const void* ws, size_t ws_bytes, size_t need) {
-  if (!ws || (reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0) return VC_ERR_WORKSPACE;
-  return ws_bytes < need ? VC_ERR_WORKSPACE : VC_OK;
-}
-
-inline int cuda_status(cudaError_t e) { return e == cudaSuccess ? VC_OK : VC_ERR_CUDA; }
 
 // Budgets B (host) must satisfy 0 <= B_l <= Nq <= n.
 bool valid_budgets(const int32_t* B, int L, int Nq, int n) {

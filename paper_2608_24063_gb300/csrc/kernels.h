@@ -148,4 +148,49 @@ cudaError_t launch_kv4(const QuantTable& tb, int units, int dtype, int d, bool q
                        const void* K, const void* V, uint8_t* Kc, uint8_t* Vc, float* Kp, float* Vp,
                        void* Kh, void* Vh, cudaStream_t st);
 
+// Rotary positions with several axes (rope.cu).
+constexpr int kRopeMaxHalf = 64;
+struct RopeArgs {
+  const int32_t* positions;            // [axes][n_rows]
+  int64_t n_rows;
+  int64_t q_stride, k_stride;          // elements between rows
+  int64_t q_out_stride, k_out_stride;
+  int32_t Hq, Hkv, half, inverse;
+  uint64_t freq[kRopeMaxHalf];         // theta^(-i / half) / 2pi in units of 2^-64 turn
+  uint8_t axis[kRopeMaxHalf];
+};
+cudaError_t launch_mrope(const RopeArgs& a, int dtype, int d, bool adjacent, const void* q, void* q_out,
+                         const void* k, void* k_out, cudaStream_t st);
+
+// 8-bit paged cache (kv8.cu, kv8_attn.cu).  The device arrays of vc_kv8 and
+// vc_kv8_step are checked as they are read: lengths are clamped to the block
+// table, requests whose rows lie outside [0, n_rows] and pages outside
+// [0, n_pages) are skipped, and the status word gets VC_ERR_DEVICE_INDEX.
+struct Kv8Rows {                       // rows of append's inputs and read's outputs
+  void* K;
+  void* V;
+  int64_t k_row, k_head, v_row, v_head;   // elements between rows / heads
+};
+cudaError_t launch_kv8_append(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8Rows& rows,
+                              int32_t* status, cudaStream_t st);
+cudaError_t launch_kv8_read(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8Rows& rows,
+                            int32_t* status, cudaStream_t st);
+
+struct Kv8AttnArgs {
+  const void* q;
+  int64_t q_stride;                    // elements between query rows
+  void* out;                           // [n_rows][Hq][d]
+  float* lse;                          // [n_rows][Hq] or NULL
+  int32_t Hq, causal;
+  float scale_log2;                    // logit scale * log2(e)
+  int32_t* status;
+  int32_t* arrivals;                   // [kKv8MaxCtas], zeroed before the launch
+  float2* part_ml;                     // [2 kKv8MaxCtas][rows a tile]: (max, sum), log2 units
+  float* part_o;                       // [2 kKv8MaxCtas][rows a tile][d]
+};
+constexpr int kKv8MaxCtas = 160;       // blocks of an attention launch at most (152 SMs, rounded up)
+int kv8_attn_rows_mma();               // rows a tile of the two attention kernels
+cudaError_t launch_kv8_attn_mma(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8AttnArgs& a,
+                                cudaStream_t st);
+
 }  // namespace vc

@@ -1,0 +1,333 @@
+// The 8-bit paged cache written (viscache_kv8_append) and read back
+// (viscache_kv8_read).
+//
+// Both are one pass over the step's rows: 2 or 4 bytes a value on one side, one
+// on the other, bound by memory.  A unit is one (page touched by the step, KV
+// head, K or V): the page's rows of that head are one contiguous block of
+// codes with one scale.  A block of threads takes one unit: it loads the rows
+// it has to write into registers (16 values a vector), reduces their largest
+// magnitude, and writes the codes.  Where the page held tokens of the request
+// before, their codes are re-encoded by the same block if the scale grew, so
+// no block waits for another and nothing is written twice.
+#include "kernels.h"
+#include "kv8.cuh"
+#include "profile.h"
+
+namespace vc {
+namespace {
+
+using namespace kv8;
+
+// The u-th page touched by the step's rows, requests in order.
+struct Touch {
+  int r, j;              // request, page within the request
+  int row0, first;       // packed row of token `first`, the request's first written token
+  int len;               // tokens of the request
+};
+
+// Called by one whole warp; false where the step touches fewer pages.  Each
+// lane counts the pages of four consecutive requests at a time, so the loads
+// of 128 requests are in flight together.
+template <int PAGE>
+__device__ __forceinline__ bool find_touch(const vc_kv8_step& s, int u, int32_t* status, Touch& out) {
+  const int lane = threadIdx.x & 31;
+  int base = 0;
+  for (int r0 = 0; r0 < s.n_req; r0 += 128) {
+    Req8 q[4];
+    int cnt[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + 4 * lane + i;
+      q[i] = r < s.n_req ? load_req(s, PAGE, r, status) : Req8{0, 0, 0};
+      const int lo = max(q[i].len - q[i].m, 0);
+      cnt[i] = q[i].len > lo ? (q[i].len - 1) / PAGE - lo / PAGE + 1 : 0;
+      sum += cnt[i];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    const int total = __shfl_sync(0xffffffffu, incl, 31);
+    if (u < base + total) {
+      const int src = __ffs(__ballot_sync(0xffffffffu, u < base + incl)) - 1;
+      Touch t = {};
+      int at = base + incl - sum;                       // pages before this lane's requests
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (u >= at && u < at + cnt[i]) {
+          const int old = q[i].len - q[i].m, lo = max(old, 0);
+          t.r = r0 + 4 * lane + i;
+          t.j = lo / PAGE + (u - at);
+          t.first = lo;
+          t.row0 = q[i].row0 + (lo - old);
+          t.len = q[i].len;
+        }
+        at += cnt[i];
+      }
+      out.r = __shfl_sync(0xffffffffu, t.r, src);
+      out.j = __shfl_sync(0xffffffffu, t.j, src);
+      out.row0 = __shfl_sync(0xffffffffu, t.row0, src);
+      out.first = __shfl_sync(0xffffffffu, t.first, src);
+      out.len = __shfl_sync(0xffffffffu, t.len, src);
+      return true;
+    }
+    base += total;
+  }
+  return false;
+}
+
+template <int D, int PAGE>
+struct UnitCfg {
+  static constexpr int VECS = PAGE * D / 16;            // 16-value vectors of a unit
+  static constexpr int THREADS = VECS / 2 < 64 ? 64 : VECS / 2 > 256 ? 256 : VECS / 2;
+  static constexpr int NV = VECS / THREADS;             // vectors of a thread
+  static constexpr int VPR = D / 16;                    // vectors of a row
+  static_assert(NV * THREADS == VECS, "whole vectors");
+};
+
+__device__ __forceinline__ void load16(const __nv_bfloat16* p, float (&v)[16]) {
+  const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 8);
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load16(const float* p, float (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 x = *reinterpret_cast<const float4*>(p + 4 * i);
+    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+  }
+}
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&v)[16]) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+}
+__device__ __forceinline__ void store16(float* p, const float (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+
+// Sixteen values times `inv` as codes; what is not finite becomes NaN.
+__device__ __forceinline__ uint4 encode16(const float (&v)[16], float inv) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float y = v[4 * i + k];
+      x[k] = finite(y) ? y * inv : __uint_as_float(0x7fffffffu);
+    }
+    w[i] = f32x2_to_e4m3x2(x[0], x[1]) | f32x2_to_e4m3x2(x[2], x[3]) << 16;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ void decode16(const uint4& c, float (&v)[16]) {
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t h = e4m3x2_to_f16x2(w[i >> 1] >> (16 * (i & 1)));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    v[2 * i] = f.x;
+    v[2 * i + 1] = f.y;
+  }
+}
+
+template <typename T, int D, int PAGE>
+__global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_append_kernel(
+    const __grid_constant__ vc_kv8 c, const __grid_constant__ vc_kv8_step s, const __grid_constant__ Kv8Rows rows,
+    int32_t* status) {
+  using C = UnitCfg<D, PAGE>;
+  __shared__ Touch touch;
+  __shared__ int found, page_id;
+  __shared__ float red[C::THREADS / 32];
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = blockIdx.y;
+  if (warp == 0) {
+    Touch x;
+    const bool ok = find_touch<PAGE>(s, (int)blockIdx.x, status, x);
+    if (lane == 0) {
+      found = ok;
+      if (ok) {
+        touch = x;
+        page_id = load_page(s, c.n_pages, x.r, x.j, status);
+      }
+    }
+  }
+  __syncthreads();
+  if (!found) return;
+  const Touch x = touch;
+  const int p = page_id;
+  if (p < 0) return;
+  // new tokens of the page: slots [a, b); slots [0, a) hold older ones
+  const int a = max(x.first - x.j * PAGE, 0), b = min(x.len - x.j * PAGE, PAGE);
+  const bool isv = blockIdx.z != 0;
+  const int64_t rstep = isv ? rows.v_row : rows.k_row;
+  const T* src = static_cast<const T*>(isv ? rows.V : rows.K) + (int64_t)g * (isv ? rows.v_head : rows.k_head) +
+                 ((int64_t)x.row0 + (x.j * PAGE - x.first)) * rstep;        // row of slot 0
+  float* scale = (isv ? c.V_scale : c.K_scale) + (int64_t)p * c.Hkv + g;
+  uint8_t* codes = static_cast<uint8_t*>(isv ? c.V_codes : c.K_codes) + ((int64_t)p * c.Hkv + g) * (PAGE * D);
+  const float old = a > 0 ? *scale : 0.f;
+  float v[C::NV][16];
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < C::NV; ++i) {
+    const int vec = t + i * C::THREADS, slot = vec / C::VPR, part = vec % C::VPR;
+    if (slot >= a && slot < b) {
+      load16(src + (int64_t)slot * rstep + part * 16, v[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < C::NV; ++i) {
+    const int slot = (t + i * C::THREADS) / C::VPR;
+    if (slot >= a && slot < b) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (finite(v[i][k])) amax = fmaxf(amax, fabsf(v[i][k]));
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+  if (lane == 0) red[warp] = amax;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < C::THREADS / 32; ++w) amax = fmaxf(amax, red[w]);
+  const float now = fmaxf(old, pow2_scale(amax));
+  const float inv = pow2_inverse(now);
+#pragma unroll
+  for (int i = 0; i < C::NV; ++i) {
+    const int vec = t + i * C::THREADS, slot = vec / C::VPR;
+    if (slot >= a && slot < b) *reinterpret_cast<uint4*>(codes + (size_t)vec * 16) = encode16(v[i], inv);
+  }
+  if (now > old) {
+    // older codes under the larger scale: value * old is exact (e4m3 has four
+    // bits above 2^-135), the division by a power of two as well
+    for (int vec = t; vec < a * C::VPR; vec += C::THREADS) {
+      uint4* w = reinterpret_cast<uint4*>(codes + (size_t)vec * 16);
+      float y[16];
+      decode16(*w, y);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) y[k] *= old;
+      *w = encode16(y, inv);
+    }
+  }
+  if (t == 0) *scale = now;
+}
+
+template <typename T, int D, int PAGE>
+__global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_read_kernel(
+    const __grid_constant__ vc_kv8 c, const __grid_constant__ vc_kv8_step s, const __grid_constant__ Kv8Rows rows,
+    int32_t* status) {
+  using C = UnitCfg<D, PAGE>;
+  __shared__ Touch touch;
+  __shared__ int found, page_id;
+  const int t = threadIdx.x, g = blockIdx.y;
+  if (t < 32) {
+    Touch x;
+    const bool ok = find_touch<PAGE>(s, (int)blockIdx.x, status, x);
+    if (t == 0) {
+      found = ok;
+      if (ok) {
+        touch = x;
+        page_id = load_page(s, c.n_pages, x.r, x.j, status);
+      }
+    }
+  }
+  __syncthreads();
+  if (!found) return;
+  const Touch x = touch;
+  const int p = page_id;
+  if (p < 0) return;
+  const int a = max(x.first - x.j * PAGE, 0), b = min(x.len - x.j * PAGE, PAGE);
+  const bool isv = blockIdx.z != 0;
+  const int64_t rstep = isv ? rows.v_row : rows.k_row;
+  T* dst = static_cast<T*>(isv ? rows.V : rows.K) + (int64_t)g * (isv ? rows.v_head : rows.k_head) +
+           ((int64_t)x.row0 + (x.j * PAGE - x.first)) * rstep;
+  const float scale = (isv ? c.V_scale : c.K_scale)[(int64_t)p * c.Hkv + g];
+  const uint8_t* codes =
+      static_cast<const uint8_t*>(isv ? c.V_codes : c.K_codes) + ((int64_t)p * c.Hkv + g) * (PAGE * D);
+  uint4 w[C::NV];
+#pragma unroll
+  for (int i = 0; i < C::NV; ++i) {
+    const int vec = t + i * C::THREADS, slot = vec / C::VPR;
+    if (slot >= a && slot < b) w[i] = *reinterpret_cast<const uint4*>(codes + (size_t)vec * 16);
+  }
+#pragma unroll
+  for (int i = 0; i < C::NV; ++i) {
+    const int vec = t + i * C::THREADS, slot = vec / C::VPR, part = vec % C::VPR;
+    if (slot >= a && slot < b) {
+      float v[16];
+      decode16(w[i], v);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] *= scale;
+      store16(dst + (int64_t)slot * rstep + part * 16, v);
+    }
+  }
+}
+
+// Pages the step may touch: a request with m > 0 rows touches at most
+// ceil(m / page) + 1.
+template <int PAGE>
+int64_t most_pages(const vc_kv8_step& s) {
+  return s.n_rows / PAGE + 2 * (int64_t)(s.n_req < s.n_rows ? s.n_req : s.n_rows);
+}
+
+template <typename T, int D, int PAGE>
+cudaError_t launch_t(bool append, const vc_kv8& c, const vc_kv8_step& s, const Kv8Rows& rows, int32_t* status,
+                     cudaStream_t st) {
+  ProfileScope ps(append ? "kv8_append" : "kv8_read", st);
+  const dim3 grid((unsigned)most_pages<PAGE>(s), (unsigned)c.Hkv, 2);
+  if (append) kv8_append_kernel<T, D, PAGE><<<grid, UnitCfg<D, PAGE>::THREADS, 0, st>>>(c, s, rows, status);
+  else kv8_read_kernel<T, D, PAGE><<<grid, UnitCfg<D, PAGE>::THREADS, 0, st>>>(c, s, rows, status);
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch_p(bool append, const vc_kv8& c, const vc_kv8_step& s, const Kv8Rows& rows, int32_t* status,
+                     cudaStream_t st) {
+  switch (c.page) {
+    case 16: return launch_t<T, D, 16>(append, c, s, rows, status, st);
+    case 32: return launch_t<T, D, 32>(append, c, s, rows, status, st);
+    case 64: return launch_t<T, D, 64>(append, c, s, rows, status, st);
+    default: return launch_t<T, D, 128>(append, c, s, rows, status, st);
+  }
+}
+
+cudaError_t launch(bool append, const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8Rows& rows,
+                   int32_t* status, cudaStream_t st) {
+  cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int32_t), st);
+  if (e != cudaSuccess || s.n_rows == 0) return e;
+  if (dtype == VC_BF16)
+    return c.d == 128 ? launch_p<__nv_bfloat16, 128>(append, c, s, rows, status, st)
+                      : launch_p<__nv_bfloat16, 64>(append, c, s, rows, status, st);
+  return c.d == 128 ? launch_p<float, 128>(append, c, s, rows, status, st)
+                    : launch_p<float, 64>(append, c, s, rows, status, st);
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_append(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8Rows& rows,
+                              int32_t* status, cudaStream_t st) {
+  return launch(true, c, s, dtype, rows, status, st);
+}
+
+cudaError_t launch_kv8_read(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8Rows& rows,
+                            int32_t* status, cudaStream_t st) {
+  return launch(false, c, s, dtype, rows, status, st);
+}
+
+}  // namespace vc

@@ -1,0 +1,147 @@
+// How the attention kernels over the 8-bit cache share out their work.
+//
+// A unit is (request, row tile, KV head): MT consecutive packed rows of a
+// request's group of query heads (row rho = i * G + j is query head j of the
+// group at the request's row i) over the tiles of KT keys that any of them
+// sees, at least one tile.  The units' tiles, in order of request, row tile,
+// KV head, form one line of T tiles; block i of N takes tiles
+// [i T / N, (i + 1) T / N) of it.  So every block has the same number of
+// tiles whatever the lengths are, a long unit is split over blocks, and a
+// block's piece of a unit is a "segment".  A segment that is not a whole unit
+// leaves its partial sums in the workspace (at most two a block: the end of
+// the unit before, the start of the one after); the block that finishes a
+// unit's last segment adds them up in order.  Lengths are read on the device.
+#pragma once
+
+#include "kernels.h"
+#include "kv8.cuh"
+
+namespace vc {
+namespace kv8 {
+
+// Place in the line: a unit and the request's numbers.
+struct Unit {
+  int r, rt, g;          // request, row tile, KV head
+  Req8 q;
+  int tiles;             // key tiles of the unit
+  int kend;              // keys its rows see (0 .. q.len)
+};
+
+template <int MT, int KT>
+struct Line {
+  int Hkv, G, page, causal;
+
+  __device__ __forceinline__ int row_tiles(const Req8& q) const { return (q.m * G + MT - 1) / MT; }
+  // keys that the rows of row tile rt see together
+  __device__ __forceinline__ int keys(const Req8& q, int rt) const {
+    if (!causal) return q.len;
+    const int last = min(q.m - 1, ((rt + 1) * MT - 1) / G);
+    return min(q.len, max(0, q.len - q.m + last + 1));
+  }
+  __device__ __forceinline__ int tiles(int kend) const { return max(1, (kend + KT - 1) / KT); }
+  // tiles of a request's units for one KV head
+  __device__ __forceinline__ int64_t request_tiles(const Req8& q) const {
+    const int n = row_tiles(q);
+    if (!causal) return (int64_t)n * tiles(q.len);
+    int64_t sum = 0;
+    for (int rt = 0; rt < n; ++rt) sum += tiles(keys(q, rt));
+    return sum;
+  }
+  __device__ __forceinline__ void set(Unit& u) const {
+    u.kend = keys(u.q, u.rt);
+    u.tiles = tiles(u.kend);
+  }
+  // the next unit (there is one)
+  __device__ __forceinline__ void next(const vc_kv8_step& s, Unit& u, int32_t* status) const {
+    if (++u.g < Hkv) return;
+    u.g = 0;
+    if (++u.rt >= row_tiles(u.q)) {
+      u.rt = 0;
+      do {
+        ++u.r;
+        u.q = load_req(s, page, u.r, status);
+      } while (u.q.m == 0 && u.r + 1 < s.n_req);
+    }
+    set(u);
+  }
+};
+
+// A block's share of the line.
+struct Share {
+  int64_t T, begin, end;   // tiles of the line, the block's range
+  int N;                   // blocks with a share (every one has at least a tile)
+  int64_t tile0;           // the first unit's first tile on the line
+  Unit u;                  // the first unit
+};
+
+// Blocks of the line that hold its tile x.
+__device__ __forceinline__ int block_of(int64_t x, int64_t T, int N) { return (int)(((x + 1) * N - 1) / T); }
+
+// Computes the block's share with all of the block's NT threads; `sh` and
+// `scan` (one word a warp) are in shared memory.  Each thread counts the
+// tiles of consecutive requests, a scan places them on the line, and the
+// thread whose requests hold the first tile of the share looks it up.
+template <int NT, int MT, int KT>
+__device__ __forceinline__ void find_share(const Line<MT, KT>& line, const vc_kv8_step& s, int32_t* status,
+                                           Share& sh, int64_t* scan) {
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int per = (s.n_req + NT - 1) / NT;
+  const int ra = min(t * per, s.n_req), rb = min(ra + per, s.n_req);
+  int64_t sum = 0;
+  for (int r = ra; r < rb; ++r) {
+    const Req8 q = load_req(s, line.page, r, status);
+    sum += line.Hkv * line.request_tiles(q);
+  }
+  int64_t incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) scan[warp] = incl;
+  __syncthreads();
+  int64_t T = 0, before = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) {
+    if (w < warp) before += scan[w];
+    T += scan[w];
+  }
+  const int N = (int)(T < (int64_t)gridDim.x ? T : (int64_t)gridDim.x);
+  const int64_t begin = N > 0 && (int)blockIdx.x < N ? blockIdx.x * T / N : 0;
+  const int64_t end = N > 0 && (int)blockIdx.x < N ? (blockIdx.x + 1) * T / N : 0;
+  int64_t at = before + incl - sum;
+  if (begin < end && begin >= at && begin < at + sum) {
+    for (int r = ra; r < rb; ++r) {
+      const Req8 q = load_req(s, line.page, r, status);
+      const int64_t w = line.Hkv * line.request_tiles(q);
+      if (begin >= at + w) {
+        at += w;
+        continue;
+      }
+      Unit u;
+      u.r = r;
+      u.rt = 0;
+      u.q = q;
+      for (;; ++u.rt) {
+        line.set(u);
+        const int64_t row = (int64_t)line.Hkv * u.tiles;
+        if (begin < at + row) break;
+        at += row;
+      }
+      u.g = (int)((begin - at) / u.tiles);
+      sh.tile0 = at + (int64_t)u.g * u.tiles;
+      sh.u = u;
+      break;
+    }
+  }
+  if (t == 0) {
+    sh.T = T;
+    sh.begin = begin;
+    sh.end = end;
+    sh.N = N;
+  }
+  __syncthreads();
+}
+
+}  // namespace kv8
+}  // namespace vc

@@ -29,6 +29,8 @@ VC_RANK_SHARED, VC_RANK_PER_LAYER = 0, 1
 VC_SCHED_PARABOLA, VC_SCHED_FIXED, VC_SCHED_ARITHMETIC, VC_SCHED_GEOMETRIC = 0, 1, 2, 3
 VC_DROP_SURVIVORS, VC_DROP_ALL = 0, 1
 VC_PATH_AUTO, VC_PATH_SIMT = 0, 1
+VC_ROPE_SECTIONED, VC_ROPE_INTERLEAVED = 0, 1
+VC_ROPE_HALVES, VC_ROPE_ADJACENT = 0, 1
 VC_TEST_WAIT_SCORE_LSE, VC_TEST_WAIT_SCORE_COLSUM, VC_TEST_WAIT_FUSE = 1, 2, 4
 
 _ERR_NAMES = {1: "VC_ERR_INVALID_ARG", 2: "VC_ERR_INFEASIBLE", 3: "VC_ERR_WORKSPACE",
@@ -45,7 +47,8 @@ EXPORTED = ("viscache_plan_budgets", "viscache_plan_budgets_ex", "prunekv_score_
             "viscache_device_accessible", "viscache_scout_workspace_size", "viscache_scout_sizes", "viscache_scout_mmr",
             "viscache_decode_workspace_size", "viscache_decode_attention",
             "viscache_kv4_sizes", "viscache_kv4_quantize", "viscache_kv4_dequantize",
-            "viscache_decode_attention_kv4")
+            "viscache_decode_attention_kv4", "viscache_mrope", "viscache_kv8_workspace_size",
+            "viscache_kv8_append", "viscache_kv8_read", "viscache_kv8_attention")
 
 
 class VisCacheError(RuntimeError):
@@ -66,6 +69,22 @@ class vc_params(ctypes.Structure):
                 ("m_num", ctypes.c_uint32), ("m_den", ctypes.c_uint32), ("mu", ctypes.c_float),
                 ("tau", ctypes.c_float), ("scale", ctypes.c_float), ("rank_mode", ctypes.c_int32),
                 ("schedule", ctypes.c_int32), ("drop_mode", ctypes.c_int32)]
+
+
+class vc_rope(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4), ("order", ctypes.c_int32),
+                ("pairing", ctypes.c_int32), ("theta", ctypes.c_double)]
+
+
+class vc_kv8(ctypes.Structure):
+    _fields_ = [("K_codes", ctypes.c_void_p), ("V_codes", ctypes.c_void_p), ("K_scale", ctypes.c_void_p),
+                ("V_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("d", ctypes.c_int32)]
+
+
+class vc_kv8_step(ctypes.Structure):
+    _fields_ = [("n_req", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("seq_lens", ctypes.c_void_p), ("row_start", ctypes.c_void_p), ("n_rows", ctypes.c_int32)]
 
 
 _lib = None
@@ -99,6 +118,15 @@ def lib() -> ctypes.CDLL:
         L.viscache_decode_workspace_size.restype = sz
         L.viscache_decode_attention.argtypes = [ctypes.POINTER(vc_batch), ctypes.POINTER(vc_params), i32,
                                                 vp, vp, vp, vp, vp, pi32, vp, vp, sz, vp]
+        i64 = ctypes.c_int64
+        L.viscache_mrope.argtypes = [ctypes.POINTER(vc_rope), vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, i32,
+                                     vp, i64, vp, i64, vp]
+        L.viscache_kv8_workspace_size.argtypes = [i32, i32, i32, i32]
+        L.viscache_kv8_workspace_size.restype = sz
+        pc8, ps8 = ctypes.POINTER(vc_kv8), ctypes.POINTER(vc_kv8_step)
+        L.viscache_kv8_append.argtypes = [pc8, ps8, i32, vp, i64, i64, vp, i64, i64, vp, sz, vp]
+        L.viscache_kv8_read.argtypes = [pc8, ps8, i32, vp, vp, vp, sz, vp]
+        L.viscache_kv8_attention.argtypes = [pc8, ps8, i32, i32, vp, i64, f32, i32, vp, vp, vp, sz, vp]
         L.prunekv_score_workspace_size.argtypes = [i32, i32, i32]
         L.prunekv_score_workspace_size.restype = sz
         L.prunekv_score.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, vp,
@@ -482,6 +510,194 @@ def viscache_kv4_dequantize(batch: Batch, params: vc_params, K_codes: torch.Tens
         ctypes.byref(batch.c), ctypes.byref(params), _ptr(K_codes), _ptr(V_codes), _ptr(K_params),
         _ptr(V_params), _ptr(kh), _ptr(vh), _stream(stream)))
     return kh[:rows], vh[:rows]
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions with several axes and the 8-bit paged cache
+
+def make_rope(sections: Sequence[int], theta: float = 10000.0, interleaved: bool = False,
+              adjacent: bool = False) -> vc_rope:
+    """Rotary description: frequencies of each axis, their order and how values are paired."""
+    if not 1 <= len(sections) <= 4:
+        raise VisCacheError("make_rope", VC_ERR_INVALID_ARG)
+    return vc_rope(len(sections), (ctypes.c_int32 * 4)(*sections),
+                   VC_ROPE_INTERLEAVED if interleaved else VC_ROPE_SECTIONED,
+                   VC_ROPE_ADJACENT if adjacent else VC_ROPE_HALVES, theta)
+
+
+def _rows3(fn: str, t: torch.Tensor, rows: int, d: int, head: Optional[int] = None) -> torch.Tensor:
+    # [rows][heads][d] with dense d; `head` the head stride the entry point wants, if it wants one
+    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != d or t.stride(2) != 1 or \
+            (head is not None and t.shape[1] > 1 and t.stride(1) != head):
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    return t
+
+
+def _on(fn: str, *tensors) -> None:
+    # one device, and the current one: the launch goes to the current device's stream
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    # a single row's stride means nothing (torch may report any): its dense length
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1) * max(t.stride(1) if t.shape[1] > 1 else 0,
+                                                                      t.shape[2])
+
+
+def viscache_mrope(rope: vc_rope, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None,
+                   inverse: bool = False, q_out: Optional[torch.Tensor] = None,
+                   k_out: Optional[torch.Tensor] = None, stream=None):
+    """Rotary positions with several axes: q [rows][Hq][d], k [rows][Hkv][d] -> (q_out, k_out).
+
+    positions: device int32 [n_axes][rows].  Rows may be strided (a slice of a
+    fused projection); ``q_out``/``k_out`` may be ``q``/``k`` themselves.
+    """
+    fn = "viscache_mrope"
+    rows, Hq, d = q.shape
+    _rows3(fn, q, rows, d, d)
+    if q_out is None:
+        q_out = torch.empty((rows, Hq, d), dtype=q.dtype, device=q.device)
+    Hkv, ks, kos = 0, 0, 0
+    if k is not None:
+        Hkv = k.shape[1]
+        _rows3(fn, k, rows, d, d)
+        if k_out is None:
+            k_out = torch.empty((rows, Hkv, d), dtype=k.dtype, device=k.device)
+        _rows3(fn, k_out, rows, d, d)
+        ks, kos = _row_stride(k), _row_stride(k_out)
+        if k.dtype != q.dtype or k_out.dtype != q.dtype or k_out.shape != k.shape:
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    _rows3(fn, q_out, rows, d, d)
+    if q_out.dtype != q.dtype or q_out.shape != q.shape or positions.dtype != torch.int32 or \
+            positions.shape != (rope.n_axes, rows) or not positions.is_contiguous():
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    _on(fn, q, k, q_out, k_out if k is not None else None, positions)
+    _check(fn, lib().viscache_mrope(
+        rope, positions.data_ptr(), _dtype_code(q), rows, Hq, Hkv, d, q.data_ptr(), _row_stride(q),
+        None if k is None else k.data_ptr(), ks, 1 if inverse else 0, q_out.data_ptr(), _row_stride(q_out),
+        None if k is None else k_out.data_ptr(), kos, _stream(stream)))
+    return q_out, (k_out if k is not None else None)
+
+
+class Kv8Cache:
+    """One layer's 8-bit pool (vc_kv8) kept alive with its tensors: codes uint8 (or
+    float8_e4m3fn) [n_pages][Hkv][page][d], scales fp32 [n_pages][Hkv]."""
+
+    def __init__(self, K_codes: torch.Tensor, V_codes: torch.Tensor, K_scale: torch.Tensor, V_scale: torch.Tensor):
+        n, Hkv, page, d = K_codes.shape
+        for t in (K_codes, V_codes):
+            if t.dtype not in (torch.uint8, torch.float8_e4m3fn) or t.shape != (n, Hkv, page, d) or \
+                    not t.is_contiguous():
+                raise VisCacheError("Kv8Cache", VC_ERR_INVALID_ARG)
+        for t in (K_scale, V_scale):
+            if t.dtype != torch.float32 or t.shape != (n, Hkv) or not t.is_contiguous():
+                raise VisCacheError("Kv8Cache", VC_ERR_INVALID_ARG)
+        if len({t.device for t in (K_codes, V_codes, K_scale, V_scale)}) != 1:
+            raise VisCacheError("Kv8Cache", VC_ERR_INVALID_ARG)
+        self.tensors = (K_codes, V_codes, K_scale, V_scale)
+        self.n_pages, self.Hkv, self.page, self.d, self.device = n, Hkv, page, d, K_codes.device
+        self.c = vc_kv8(K_codes.data_ptr(), V_codes.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr(), n, Hkv,
+                        page, d)
+
+    @classmethod
+    def empty(cls, n_pages: int, Hkv: int, page: int, d: int, device="cuda") -> "Kv8Cache":
+        """A pool with nothing in it (what unwritten slots hold is never used)."""
+        return cls(torch.empty((n_pages, Hkv, page, d), dtype=torch.uint8, device=device),
+                   torch.empty((n_pages, Hkv, page, d), dtype=torch.uint8, device=device),
+                   torch.empty((n_pages, Hkv), dtype=torch.float32, device=device),
+                   torch.empty((n_pages, Hkv), dtype=torch.float32, device=device))
+
+
+class Kv8Step:
+    """The requests of one step (vc_kv8_step) kept alive with their device arrays: block_table int32
+    [n_req][max_pages], seq_lens int32 [n_req], row_start int32 [n_req + 1], and the packed rows."""
+
+    def __init__(self, block_table: torch.Tensor, seq_lens: torch.Tensor, row_start: torch.Tensor, n_rows: int):
+        n = seq_lens.shape[0]
+        for t, shape in ((block_table, (n, block_table.shape[-1])), (seq_lens, (n,)), (row_start, (n + 1,))):
+            if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != seq_lens.device:
+                raise VisCacheError("Kv8Step", VC_ERR_INVALID_ARG)
+        self.tensors = (block_table, seq_lens, row_start)
+        self.n_rows, self.device = int(n_rows), seq_lens.device
+        self.c = vc_kv8_step(n, block_table.shape[1], block_table.data_ptr(), seq_lens.data_ptr(),
+                             row_start.data_ptr(), self.n_rows)
+
+
+def viscache_kv8_workspace_size(n_rows: int, Hq: int, Hkv: int, d: int) -> int:
+    return lib().viscache_kv8_workspace_size(n_rows, Hq, Hkv, d)
+
+
+def _kv8_ws(fn: str, cache: Kv8Cache, step: Kv8Step, Hq: int, ws: Optional[torch.Tensor]) -> torch.Tensor:
+    if cache.device != step.device:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    if ws is None:
+        need = viscache_kv8_workspace_size(step.n_rows, Hq, cache.Hkv, cache.d)
+        if need == 0:
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+        ws = _workspace(need, cache.device, None)
+    _on(fn, ws, cache.tensors[0])
+    return ws
+
+
+def viscache_kv8_append(cache: Kv8Cache, step: Kv8Step, K: torch.Tensor, V: torch.Tensor,
+                        ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Write the step's rows K, V [rows][Hkv][d] (any row and head strides) into the cache."""
+    fn = "viscache_kv8_append"
+    ws = _kv8_ws(fn, cache, step, cache.Hkv, ws)
+    for t in (K, V):
+        _rows3(fn, t, step.n_rows, cache.d)
+        if t.shape[1] != cache.Hkv or t.dtype != K.dtype:
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    _on(fn, K, V)
+    _check(fn, lib().viscache_kv8_append(
+        cache.c, step.c, _dtype_code(K), K.data_ptr(), _row_stride(K), K.stride(1) if cache.Hkv > 1 else cache.d,
+        V.data_ptr(), _row_stride(V), V.stride(1) if cache.Hkv > 1 else cache.d, ws.data_ptr(), ws.numel(),
+        _stream(stream)))
+
+
+def viscache_kv8_read(cache: Kv8Cache, step: Kv8Step, dtype=torch.bfloat16, out=None,
+                      ws: Optional[torch.Tensor] = None, stream=None):
+    """The step's rows back from the cache: (K_hat, V_hat) [rows][Hkv][d] in `dtype` (or `out`'s)."""
+    fn = "viscache_kv8_read"
+    ws = _kv8_ws(fn, cache, step, cache.Hkv, ws)
+    shape = (step.n_rows, cache.Hkv, cache.d)
+    if out is None:
+        out = (torch.empty(shape, dtype=dtype, device=cache.device),
+               torch.empty(shape, dtype=dtype, device=cache.device))
+    kh, vh = out
+    for t in (kh, vh):
+        if t.shape != shape or t.dtype != kh.dtype or not t.is_contiguous():
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    _on(fn, kh, vh)
+    _check(fn, lib().viscache_kv8_read(cache.c, step.c, _dtype_code(kh), kh.data_ptr(), vh.data_ptr(),
+                                       ws.data_ptr(), ws.numel(), _stream(stream)))
+    return kh, vh
+
+
+def viscache_kv8_attention(cache: Kv8Cache, step: Kv8Step, q: torch.Tensor, scale: float = 0.0,
+                           causal: bool = True, out: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                           stream=None) -> torch.Tensor:
+    """The step's query rows q [rows][Hq][d] over their requests' pages: out [rows][Hq][d]; ``lse`` fp32
+    [rows][Hq] takes the log of each softmax's normaliser."""
+    fn = "viscache_kv8_attention"
+    rows, Hq, d = q.shape
+    _rows3(fn, q, step.n_rows, cache.d, cache.d)
+    ws = _kv8_ws(fn, cache, step, Hq, ws)
+    if out is None:
+        out = torch.empty((rows, Hq, d), dtype=q.dtype, device=q.device)
+    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous() or \
+            (lse is not None and (lse.shape != (rows, Hq) or lse.dtype != torch.float32 or
+                                  not lse.is_contiguous())):
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    _on(fn, q, out, lse)
+    _check(fn, lib().viscache_kv8_attention(
+        cache.c, step.c, _dtype_code(q), Hq, q.data_ptr(), _row_stride(q), float(scale), 1 if causal else 0,
+        out.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
 
 
 def viscache_set_kernel_path(path: int) -> None:
