@@ -184,13 +184,17 @@ struct Kv8AttnArgs {
   int32_t Hq, causal;
   float scale_log2;                    // logit scale * log2(e)
   int32_t* status;
-  int32_t* arrivals;                   // [kKv8MaxCtas], zeroed before the launch
+  int32_t* arrivals;                   // [2 kKv8MaxCtas], zeroed before the launch
   float2* part_ml;                     // [2 kKv8MaxCtas][rows a tile]: (max, sum), log2 units
   float* part_o;                       // [2 kKv8MaxCtas][rows a tile][d]
 };
 constexpr int kKv8MaxCtas = 160;       // blocks of an attention launch at most (152 SMs, rounded up)
+int kv8_sm_count();                    // SMs of the current device, at most kKv8MaxCtas
 int kv8_attn_rows_mma();               // rows a tile of the two attention kernels
+int kv8_attn_rows_tc();
 cudaError_t launch_kv8_attn_mma(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8AttnArgs& a,
                                 cudaStream_t st);
+// the same on tcgen05: bf16 rows, many of them
+cudaError_t launch_kv8_attn_tc(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st);
 
 }  // namespace vc

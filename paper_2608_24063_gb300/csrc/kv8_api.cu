@@ -37,16 +37,23 @@ bool valid_stride(int64_t stride, int64_t least, int dtype) {
 struct Kv8Ws {
   size_t o_arr = 0, o_ml = 0, o_o = 0, total = 0;
 };
-Kv8Ws kv8_ws(int d) {
+Kv8Ws kv8_ws(bool tc, int d) {
   Arena a;
   Kv8Ws w;
   a.take(kAlign);
-  const size_t rows = (size_t)2 * kKv8MaxCtas * kv8_attn_rows_mma();
-  w.o_arr = a.take(sizeof(int32_t) * kKv8MaxCtas);
+  const size_t rows = (size_t)2 * kKv8MaxCtas * (tc ? kv8_attn_rows_tc() : kv8_attn_rows_mma());
+  w.o_arr = a.take(sizeof(int32_t) * 2 * kKv8MaxCtas);
   w.o_ml = a.take(sizeof(float2) * rows);
   w.o_o = a.take(sizeof(float) * rows * d);
   w.total = a.off;
   return w;
+}
+
+// Whether a call runs on tcgen05: bf16 rows, at least kTcRows packed rows of a
+// KV head per request on average.
+constexpr int64_t kTcRows = 64;
+bool many_rows(int64_t n_rows, int64_t n_req, int32_t Hq, int32_t Hkv) {
+  return n_rows * (Hq / Hkv) >= kTcRows * n_req;
 }
 
 bool valid_heads(int32_t Hq, int32_t Hkv) { return Hkv >= 1 && Hq >= Hkv && Hq <= 4096 && Hq % Hkv == 0; }
@@ -133,7 +140,7 @@ int viscache_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int
 
 size_t viscache_kv8_workspace_size(int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t d) {
   if (n_rows < 0 || n_rows > (1 << 24) || !valid_heads(Hq, Hkv) || (d != 64 && d != 128)) return 0;
-  return kv8_ws(d).total;
+  return kv8_ws(many_rows(n_rows, 1, Hq, Hkv), d).total;
 }
 
 int viscache_kv8_append(const vc_kv8* cache, const vc_kv8_step* step, int dtype, const void* K,
@@ -162,7 +169,12 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
                            !valid_stride(q_stride, (int64_t)Hq * cache->d, dtype)))
     return VC_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return VC_ERR_INVALID_ARG;
-  const Kv8Ws w = kv8_ws(cache->d);
+  // the attention's line of key tiles: a block's share is counted in 31 bits
+  const int64_t row_tiles = (int64_t)step->n_rows * (Hq / cache->Hkv) / kv8_attn_rows_mma() + step->n_req;
+  if (row_tiles * cache->Hkv > ((int64_t)1 << 37) / (((int64_t)step->max_pages * cache->page + 127) / 128))
+    return VC_ERR_UNSUPPORTED;
+  const bool tc = dtype == VC_BF16 && many_rows(step->n_rows, step->n_req, Hq, cache->Hkv);
+  const Kv8Ws w = kv8_ws(tc, cache->d);
   const int wc = check_ws(ws, ws_bytes, w.total);
   if (wc != VC_OK) return wc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -182,7 +194,8 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
   a.arrivals = reinterpret_cast<int32_t*>(base + w.o_arr);
   a.part_ml = reinterpret_cast<float2*>(base + w.o_ml);
   a.part_o = reinterpret_cast<float*>(base + w.o_o);
-  return cuda_status(launch_kv8_attn_mma(*cache, *step, dtype, a, st));
+  return cuda_status(tc ? launch_kv8_attn_tc(*cache, *step, a, st)
+                        : launch_kv8_attn_mma(*cache, *step, dtype, a, st));
 }
 
 }  // extern "C"

@@ -55,8 +55,6 @@ template <int D>
 struct Cfg {
   static constexpr int STAGE = kKT * D;                     // bytes of K, and of V
   static constexpr int NST = D == 128 ? 5 : 10;
-  static constexpr size_t RING = (size_t)NST * 2 * STAGE;
-  static constexpr size_t MERGE = (size_t)4 * kMT * D * 4;  // partial outputs of four warps
 };
 
 template <int D>
@@ -175,8 +173,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
   const Share& sh = sm.share;
   if (sh.begin >= sh.end) return;
   volatile int* abort = &sm.abort;
-  Unit u = sh.u;
-  int64_t pos = sh.begin, tile0 = sh.tile0;
+  Walk wk;
+  wk.start(sh);
+  const Unit& u = wk.u;
+  const int &t0 = wk.t0, &t1 = wk.t1;           // the segment's tiles of its unit
   int fill = 0;                                 // tiles so far (ring position)
 
   if (warp == kWarps) {
@@ -188,9 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
     tc::prefetch_tmap(&tmK);
     tc::prefetch_tmap(&tmV);
     bool ok = true;
-    while (ok && pos < sh.end) {
-      const int t0 = (int)(pos - tile0);
-      const int t1 = (int)(sh.end - tile0 < u.tiles ? sh.end - tile0 : u.tiles);
+    do {
       auto look = [&](int first, int& pid, float& ks, float& vs, bool& live) {
         const int tile = first + bt, j = tile * ppt + bp;
         live = tile < t1 && j * c.page < u.kend;
@@ -233,12 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
         vs = nvs;
         live = nlive;
       }
-      pos = tile0 + t1;
-      if (pos < sh.end) {
-        tile0 += u.tiles;
-        line.next(s, u, a.status);
-      }
-    }
+    } while (ok && wk.next(line, s, a.status));
     // every copy has landed before the block may end
     __syncwarp();
     if (lane == 0)
@@ -250,9 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
   const int gid = lane >> 2, tig = lane & 3;
   const int wpage = 16 * warp / c.page;         // the page of the tile they lie in
   bool ok = true;
-  while (pos < sh.end) {
-    const int t0 = (int)(pos - tile0);
-    const int t1 = (int)(sh.end - tile0 < u.tiles ? sh.end - tile0 : u.tiles);
+  do {
     uint32_t qf[NP][KS][4];
     float qs[2];
     load_q<T, D, NP>(static_cast<const T*>(a.q), a.q_stride, u, G, a.Hq, qf, qs);
@@ -460,9 +451,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
       y[e] = v.x; y[e + 1] = v.y; y[e + 2] = v.z; y[e + 3] = v.w;
     }
     bool write = real;
-    if (t0 != 0 || t1 != u.tiles) {
+    if (!wk.whole()) {
       // a piece of a unit: to the workspace; the unit's last piece to arrive adds them up
-      const int first = block_of(tile0, sh.T, sh.N), final = block_of(tile0 + u.tiles - 1, sh.T, sh.N);
+      const int first = wk.first_block(sh), final = wk.last_block(sh);
       const int64_t mine = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
       float* po = a.part_o + (mine * kMT + row) * D + part * EPT;
 #pragma unroll
@@ -520,12 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
       }
       if (a.lse && part == 0) a.lse[at] = L == 0.f ? -INFINITY : fmaf(M, 0.6931471805599453f, logf(L));
     }
-    pos = tile0 + t1;
-    if (pos < sh.end) {
-      tile0 += u.tiles;
-      line.next(s, u, a.status);
-    }
-  }
+  } while (wk.next(line, s, a.status));
   if (!ok && lane == 0) set_status(a.status, VC_ERR_DEVICE_TIMEOUT);
 }
 
@@ -555,18 +541,6 @@ bool pool_map(CUtensorMap* m, const void* base, const vc_kv8& c) {
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int sm_count() {
-  static std::atomic<int> cached[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 1;
-  int n = cached[dev].load(std::memory_order_relaxed);
-  if (n > 0) return n;
-  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 1;
-  if (n > kKv8MaxCtas) n = kKv8MaxCtas;
-  cached[dev].store(n, std::memory_order_relaxed);
-  return n;
-}
-
 template <typename T, int D>
 cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
   constexpr size_t smem = sizeof(Smem<D>) + 1024;
@@ -583,13 +557,25 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
   const int64_t G = a.Hq / c.Hkv;
   const int64_t units = ((int64_t)s.n_rows * G / kMT + (s.n_req < s.n_rows ? s.n_req : s.n_rows)) * c.Hkv;
   const int64_t tiles = units * (((int64_t)s.max_pages * c.page + kKT - 1) / kKT);
-  const int64_t sms = sm_count();
+  const int64_t sms = kv8_sm_count();
   ProfileScope ps("kv8_attn", st);
   kv8_attn_kernel<T, D><<<(unsigned)(tiles < sms ? tiles : sms), kThreads, smem, st>>>(mk, mv, c, s, a);
   return cudaGetLastError();
 }
 
 }  // namespace
+
+int kv8_sm_count() {
+  static std::atomic<int> cached[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 1;
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 1;
+  if (n > kKv8MaxCtas) n = kKv8MaxCtas;
+  cached[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
 
 int kv8_attn_rows_mma() { return kMT; }
 

@@ -77,6 +77,40 @@ struct Share {
 // Blocks of the line that hold its tile x.
 __device__ __forceinline__ int block_of(int64_t x, int64_t T, int N) { return (int)(((x + 1) * N - 1) / T); }
 
+// A role's walk over the block's segments.  Positions are relative to the
+// share's begin (a share is below 2^31 tiles: the host refuses longer lines).
+struct Walk {
+  Unit u;                // the segment's unit
+  int t0, t1;            // its tiles of the unit
+  int left;              // tiles of the share from t0 on
+  int rel;               // the unit's first tile, from the share's begin
+
+  __device__ __forceinline__ void start(const Share& sh) {
+    u = sh.u;
+    left = (int)(sh.end - sh.begin);
+    rel = (int)(sh.tile0 - sh.begin);
+    t0 = -rel;
+    t1 = left < u.tiles - t0 ? t0 + left : u.tiles;
+  }
+  __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == u.tiles; }
+  // the next segment; false at the share's end
+  template <typename L>
+  __device__ __forceinline__ bool next(const L& line, const vc_kv8_step& s, int32_t* status) {
+    left -= t1 - t0;
+    if (left <= 0) return false;
+    rel += u.tiles;
+    line.next(s, u, status);
+    t0 = 0;
+    t1 = left < u.tiles ? left : u.tiles;
+    return true;
+  }
+  // the blocks that hold the unit's first and last tile
+  __device__ __forceinline__ int first_block(const Share& sh) const { return block_of(sh.begin + rel, sh.T, sh.N); }
+  __device__ __forceinline__ int last_block(const Share& sh) const {
+    return block_of(sh.begin + rel + u.tiles - 1, sh.T, sh.N);
+  }
+};
+
 // Computes the block's share with all of the block's NT threads; `sh` and
 // `scan` (one word a warp) are in shared memory.  Each thread counts the
 // tiles of consecutive requests, a scan places them on the line, and the

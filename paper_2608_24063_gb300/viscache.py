@@ -525,26 +525,32 @@ def make_rope(sections: Sequence[int], theta: float = 10000.0, interleaved: bool
                    VC_ROPE_ADJACENT if adjacent else VC_ROPE_HALVES, theta)
 
 
-def _rows3(fn: str, t: torch.Tensor, rows: int, d: int, head: Optional[int] = None) -> torch.Tensor:
-    # [rows][heads][d] with dense d; `head` the head stride the entry point wants, if it wants one
-    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != d or t.stride(2) != 1 or \
-            (head is not None and t.shape[1] > 1 and t.stride(1) != head):
+_current_device = torch._C._cuda_getDevice
+_TYPE = {torch.bfloat16: VC_BF16, torch.float32: VC_F32}
+
+
+def _rows(fn: str, t: torch.Tensor, dtype, dev: int, rows: int, heads: int, d: int) -> Tuple[int, int]:
+    """Row and head stride of [rows][heads][d] rows with dense d on the current device (a step's calls
+    are a few microseconds, so the checks read each attribute once)."""
+    if t.dtype != dtype or t.get_device() != dev or t.shape != (rows, heads, d):
         raise VisCacheError(fn, VC_ERR_INVALID_ARG)
-    return t
+    r, h, e = t.stride()
+    if heads == 1:
+        h = d                    # a stride along a single entry means nothing
+    if rows == 1:
+        r = max(heads * h, heads * d)
+    if e != 1 and d != 1:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    return r, h
 
 
-def _on(fn: str, *tensors) -> None:
-    # one device, and the current one: the launch goes to the current device's stream
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+def _type(t: torch.Tensor) -> int:
+    code = _TYPE.get(t.dtype)
+    return _dtype_code(t) if code is None else code       # raises TypeError
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    # a single row's stride means nothing (torch may report any): its dense length
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1) * max(t.stride(1) if t.shape[1] > 1 else 0,
-                                                                      t.shape[2])
+def _raw_stream(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def viscache_mrope(rope: vc_rope, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None,
@@ -556,30 +562,32 @@ def viscache_mrope(rope: vc_rope, positions: torch.Tensor, q: torch.Tensor, k: O
     fused projection); ``q_out``/``k_out`` may be ``q``/``k`` themselves.
     """
     fn = "viscache_mrope"
+    code, dt, dev = _type(q), q.dtype, _current_device()
+    if q.dim() != 3:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
     rows, Hq, d = q.shape
-    _rows3(fn, q, rows, d, d)
     if q_out is None:
-        q_out = torch.empty((rows, Hq, d), dtype=q.dtype, device=q.device)
-    Hkv, ks, kos = 0, 0, 0
+        q_out = torch.empty((rows, Hq, d), dtype=dt, device=q.device)
+    qs, qh = _rows(fn, q, dt, dev, rows, Hq, d)
+    qos, qoh = _rows(fn, q_out, dt, dev, rows, Hq, d)
+    Hkv, ks, kos, kp, kop, kh, koh = 0, 0, 0, None, None, d, d
     if k is not None:
         Hkv = k.shape[1]
-        _rows3(fn, k, rows, d, d)
         if k_out is None:
-            k_out = torch.empty((rows, Hkv, d), dtype=k.dtype, device=k.device)
-        _rows3(fn, k_out, rows, d, d)
-        ks, kos = _row_stride(k), _row_stride(k_out)
-        if k.dtype != q.dtype or k_out.dtype != q.dtype or k_out.shape != k.shape:
-            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
-    _rows3(fn, q_out, rows, d, d)
-    if q_out.dtype != q.dtype or q_out.shape != q.shape or positions.dtype != torch.int32 or \
-            positions.shape != (rope.n_axes, rows) or not positions.is_contiguous():
+            k_out = torch.empty((rows, Hkv, d), dtype=dt, device=q.device)
+        ks, kh = _rows(fn, k, dt, dev, rows, Hkv, d)
+        kos, koh = _rows(fn, k_out, dt, dev, rows, Hkv, d)
+        kp, kop = k.data_ptr(), k_out.data_ptr()
+    else:
+        k_out = None
+    if qh != d or qoh != d or kh != d or koh != d or positions.dtype != torch.int32 or \
+            positions.shape != (rope.n_axes, rows) or not positions.is_contiguous() or positions.get_device() != dev:
         raise VisCacheError(fn, VC_ERR_INVALID_ARG)
-    _on(fn, q, k, q_out, k_out if k is not None else None, positions)
-    _check(fn, lib().viscache_mrope(
-        rope, positions.data_ptr(), _dtype_code(q), rows, Hq, Hkv, d, q.data_ptr(), _row_stride(q),
-        None if k is None else k.data_ptr(), ks, 1 if inverse else 0, q_out.data_ptr(), _row_stride(q_out),
-        None if k is None else k_out.data_ptr(), kos, _stream(stream)))
-    return q_out, (k_out if k is not None else None)
+    rc = lib().viscache_mrope(rope, positions.data_ptr(), code, rows, Hq, Hkv, d, q.data_ptr(), qs, kp, ks,
+                              1 if inverse else 0, q_out.data_ptr(), qos, kop, kos, _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
+    return q_out, k_out
 
 
 class Kv8Cache:
@@ -598,7 +606,8 @@ class Kv8Cache:
         if len({t.device for t in (K_codes, V_codes, K_scale, V_scale)}) != 1:
             raise VisCacheError("Kv8Cache", VC_ERR_INVALID_ARG)
         self.tensors = (K_codes, V_codes, K_scale, V_scale)
-        self.n_pages, self.Hkv, self.page, self.d, self.device = n, Hkv, page, d, K_codes.device
+        self.n_pages, self.Hkv, self.page, self.d = n, Hkv, page, d
+        self.device, self.index = K_codes.device, K_codes.get_device()
         self.c = vc_kv8(K_codes.data_ptr(), V_codes.data_ptr(), K_scale.data_ptr(), V_scale.data_ptr(), n, Hkv,
                         page, d)
 
@@ -621,7 +630,7 @@ class Kv8Step:
             if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != seq_lens.device:
                 raise VisCacheError("Kv8Step", VC_ERR_INVALID_ARG)
         self.tensors = (block_table, seq_lens, row_start)
-        self.n_rows, self.device = int(n_rows), seq_lens.device
+        self.n_rows, self.device, self.index = int(n_rows), seq_lens.device, seq_lens.get_device()
         self.c = vc_kv8_step(n, block_table.shape[1], block_table.data_ptr(), seq_lens.data_ptr(),
                              row_start.data_ptr(), self.n_rows)
 
@@ -630,50 +639,54 @@ def viscache_kv8_workspace_size(n_rows: int, Hq: int, Hkv: int, d: int) -> int:
     return lib().viscache_kv8_workspace_size(n_rows, Hq, Hkv, d)
 
 
-def _kv8_ws(fn: str, cache: Kv8Cache, step: Kv8Step, Hq: int, ws: Optional[torch.Tensor]) -> torch.Tensor:
-    if cache.device != step.device:
+def _kv8_ws(fn: str, cache: Kv8Cache, step: Kv8Step, Hq: int, ws: Optional[torch.Tensor]):
+    # the device of the call, and the workspace on it
+    dev = _current_device()
+    if cache.index != dev or step.index != dev:
         raise VisCacheError(fn, VC_ERR_INVALID_ARG)
     if ws is None:
         need = viscache_kv8_workspace_size(step.n_rows, Hq, cache.Hkv, cache.d)
         if need == 0:
             raise VisCacheError(fn, VC_ERR_INVALID_ARG)
         ws = _workspace(need, cache.device, None)
-    _on(fn, ws, cache.tensors[0])
-    return ws
+    elif ws.get_device() != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    return dev, ws
 
 
 def viscache_kv8_append(cache: Kv8Cache, step: Kv8Step, K: torch.Tensor, V: torch.Tensor,
                         ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """Write the step's rows K, V [rows][Hkv][d] (any row and head strides) into the cache."""
     fn = "viscache_kv8_append"
-    ws = _kv8_ws(fn, cache, step, cache.Hkv, ws)
-    for t in (K, V):
-        _rows3(fn, t, step.n_rows, cache.d)
-        if t.shape[1] != cache.Hkv or t.dtype != K.dtype:
-            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
-    _on(fn, K, V)
-    _check(fn, lib().viscache_kv8_append(
-        cache.c, step.c, _dtype_code(K), K.data_ptr(), _row_stride(K), K.stride(1) if cache.Hkv > 1 else cache.d,
-        V.data_ptr(), _row_stride(V), V.stride(1) if cache.Hkv > 1 else cache.d, ws.data_ptr(), ws.numel(),
-        _stream(stream)))
+    dev, ws = _kv8_ws(fn, cache, step, cache.Hkv, ws)
+    code, dt = _type(K), K.dtype
+    kr, kh = _rows(fn, K, dt, dev, step.n_rows, cache.Hkv, cache.d)
+    vr, vh = _rows(fn, V, dt, dev, step.n_rows, cache.Hkv, cache.d)
+    rc = lib().viscache_kv8_append(cache.c, step.c, code, K.data_ptr(), kr, kh, V.data_ptr(), vr, vh, ws.data_ptr(),
+                                   ws.numel(), _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
 
 
 def viscache_kv8_read(cache: Kv8Cache, step: Kv8Step, dtype=torch.bfloat16, out=None,
                       ws: Optional[torch.Tensor] = None, stream=None):
     """The step's rows back from the cache: (K_hat, V_hat) [rows][Hkv][d] in `dtype` (or `out`'s)."""
     fn = "viscache_kv8_read"
-    ws = _kv8_ws(fn, cache, step, cache.Hkv, ws)
-    shape = (step.n_rows, cache.Hkv, cache.d)
+    dev, ws = _kv8_ws(fn, cache, step, cache.Hkv, ws)
     if out is None:
+        shape = (step.n_rows, cache.Hkv, cache.d)
         out = (torch.empty(shape, dtype=dtype, device=cache.device),
                torch.empty(shape, dtype=dtype, device=cache.device))
     kh, vh = out
-    for t in (kh, vh):
-        if t.shape != shape or t.dtype != kh.dtype or not t.is_contiguous():
+    code = _type(kh)
+    for t in out:
+        _rows(fn, t, kh.dtype, dev, step.n_rows, cache.Hkv, cache.d)
+        if not t.is_contiguous():
             raise VisCacheError(fn, VC_ERR_INVALID_ARG)
-    _on(fn, kh, vh)
-    _check(fn, lib().viscache_kv8_read(cache.c, step.c, _dtype_code(kh), kh.data_ptr(), vh.data_ptr(),
-                                       ws.data_ptr(), ws.numel(), _stream(stream)))
+    rc = lib().viscache_kv8_read(cache.c, step.c, code, kh.data_ptr(), vh.data_ptr(), ws.data_ptr(), ws.numel(),
+                                 _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
     return kh, vh
 
 
@@ -684,19 +697,26 @@ def viscache_kv8_attention(cache: Kv8Cache, step: Kv8Step, q: torch.Tensor, scal
     """The step's query rows q [rows][Hq][d] over their requests' pages: out [rows][Hq][d]; ``lse`` fp32
     [rows][Hq] takes the log of each softmax's normaliser."""
     fn = "viscache_kv8_attention"
-    rows, Hq, d = q.shape
-    _rows3(fn, q, step.n_rows, cache.d, cache.d)
-    ws = _kv8_ws(fn, cache, step, Hq, ws)
-    if out is None:
-        out = torch.empty((rows, Hq, d), dtype=q.dtype, device=q.device)
-    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous() or \
-            (lse is not None and (lse.shape != (rows, Hq) or lse.dtype != torch.float32 or
-                                  not lse.is_contiguous())):
+    code, dt = _type(q), q.dtype
+    if q.dim() != 3:
         raise VisCacheError(fn, VC_ERR_INVALID_ARG)
-    _on(fn, q, out, lse)
-    _check(fn, lib().viscache_kv8_attention(
-        cache.c, step.c, _dtype_code(q), Hq, q.data_ptr(), _row_stride(q), float(scale), 1 if causal else 0,
-        out.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    rows, Hq, d = step.n_rows, q.shape[1], cache.d
+    dev, ws = _kv8_ws(fn, cache, step, Hq, ws)
+    qs, qh = _rows(fn, q, dt, dev, rows, Hq, d)
+    if out is None:
+        out = torch.empty((rows, Hq, d), dtype=dt, device=q.device)
+    _rows(fn, out, dt, dev, rows, Hq, d)
+    lp = None
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.shape != (rows, Hq) or not lse.is_contiguous() or lse.get_device() != dev:
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+        lp = lse.data_ptr()
+    if qh != d or not out.is_contiguous():
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    rc = lib().viscache_kv8_attention(cache.c, step.c, code, Hq, q.data_ptr(), qs, scale, 1 if causal else 0,
+                                      out.data_ptr(), lp, ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
     return out
 
 

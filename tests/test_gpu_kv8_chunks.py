@@ -1,0 +1,134 @@
+"""GPU parity of attention over the 8-bit paged cache with many query rows a request (the
+tensor-core path for 16-bit rows), against the float64 oracle on sampled rows, and against
+the few-rows path on the same inputs."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8
+from paper_2608_24063_gb300 import viscache as vc
+from tests.test_gpu_kv8 import BF, DEV, Pool, _filled, _rand
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(pool, step, q, causal, scale=0.0):
+    total, Hq, d = q.shape
+    lse = torch.full((total, Hq), float("nan"), device=DEV)
+    out = torch.full((total, Hq, d), float("nan"), dtype=q.dtype, device=DEV)
+    ws = torch.empty(vc.viscache_kv8_workspace_size(total, Hq, pool.Hkv, d), dtype=torch.uint8, device=DEV)
+    ws.fill_(0xA5)
+    vc.viscache_kv8_attention(pool.cache, step, q, scale, causal, out, lse, ws)
+    assert vc.prunekv_get_status(ws) == vc.VC_OK
+    return out, lse
+
+
+def check(pool, lens, rows, Hq, causal, scale=0.0, qscale=1.5, sample=7, seed=60):
+    """Rows of the call against the oracle: a few of each request, the first, the last and those
+    at row-tile ends among them."""
+    Hkv, d, G = pool.Hkv, pool.d, Hq // pool.Hkv
+    q = _rand((sum(rows), Hq + Hkv, d), seed, BF, qscale)
+    out, lse = _run(pool, pool.step(lens, rows), q.to(DEV)[:, :Hq], causal, scale)
+    got, z = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    sc = scale if scale > 0 else 1.0 / np.sqrt(d)
+    q64 = q[:, :Hq].double().numpy()
+    rng = np.random.default_rng(seed)
+    at = 0
+    for r, (n, m) in enumerate(zip(lens, rows)):
+        pick = sorted({0, m - 1, 128 // G, 256 // G} | set(rng.integers(0, m, sample).tolist())) if m else []
+        pick = [i for i in pick if i < m]
+        for g in range(Hkv if pick else 0):
+            K = kv8.gather(pool.codes[0], pool.scale[0], pool.table[r], n, g)
+            V = kv8.gather(pool.codes[1], pool.scale[1], pool.table[r], n, g)
+            vmax = np.abs(V).max(initial=0.0)
+            for j in range(g * G, (g + 1) * G):
+                for i in pick:
+                    k = n if not causal else min(n, max(0, n - m + i + 1))
+                    qq = q64[at + i:at + i + 1, j]
+                    ref, lref, absv = kv8.attention(qq, K[:k], V[:k], None, sc)
+                    # scores: d / 16 fp32 sums of products, scalings; probabilities to fp16
+                    # (2^-11), those below 2^-17 of the reference to 2^-28 of it; sums over k / 16
+                    # product steps; the output's rounding
+                    size = (np.abs(qq) @ np.abs(K[:k]).T * sc).max(initial=0.0)
+                    E = size * (d / 16 + 6) * 2.0 ** -23 + 2.0 ** -21
+                    rel = 2 * E + 2.0 ** -11 + (k / 16 + 40) * 2.0 ** -23
+                    tol = rel * absv + (1 + rel) * 2.0 ** -8 * np.abs(ref) + k * 2.0 ** -28 * vmax
+                    err = np.abs(got[at + i, j] - ref[0])
+                    assert (err <= tol[0]).all(), (r, i, j, float((err - tol[0]).max()), float(err.max()))
+                    if k == 0:
+                        assert np.isneginf(z[at + i, j])
+                    else:
+                        ltol = E + (k / 128 + 40) * 2.0 ** -23 + 2.0 ** -22 * abs(lref[0])
+                        assert abs(z[at + i, j] - lref[0]) <= ltol
+        at += m
+    return out, lse
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,d,page", [(28, 4, 128, 64), (8, 4, 64, 16), (16, 1, 64, 128), (2, 2, 128, 32),
+                                           (24, 1, 128, 16)])
+def test_chunks_match_oracle(Hq, Hkv, d, page, causal):
+    # one and two row tiles of a unit, units that end inside them, requests without rows, all of
+    # whose tokens are rows, with more rows than tokens
+    lens, rows = [700, 40, 300, 60, 0, 513], [129, 0, 300, 77, 65, 400]
+    check(_filled(lens, Hkv, page, d), lens, rows, Hq, causal)
+
+
+def test_units_split_over_blocks():
+    # few units and long contexts: every unit's tiles lie on many blocks
+    lens, rows = [20000, 3001], [40, 17]
+    check(_filled(lens, 1, 64, 128), lens, rows, 4, True)
+    lens, rows = [9000], [300]
+    check(_filled(lens, 1, 16, 64), lens, rows, 2, True, sample=3)
+
+
+def test_more_units_than_blocks():
+    rng = np.random.default_rng(8)
+    rows = rng.integers(1, 150, 40).tolist()
+    lens = [m + int(x) for m, x in zip(rows, rng.integers(0, 300, 40))]
+    check(_filled(lens, 4, 32, 128), lens, rows, 8, True, sample=2)
+
+
+def test_rising_maxima_and_scales():
+    # scores that rise by hundreds along the tokens and V pages of growing size: O is rescaled
+    # again and again; then the other way round
+    n = 1200
+    for flip in (False, True):
+        pool = Pool([n], 1, 16, 128)
+        K, V = _rand((n, 1, 128), 1, torch.float32), _rand((n, 1, 128), 2, torch.float32)
+        size = torch.linspace(0.2, 6.0, n)[:, None, None]
+        grow = 2.0 ** torch.div(torch.arange(n), 100, rounding_mode="floor")[:, None, None]
+        K, V = K * (size.flip(0) if flip else size), V * (grow.flip(0) if flip else grow)
+        pool.append([n], [n], K, V)
+        check(pool, [n], [90], 4, True, scale=0.5)
+        check(pool, [n], [90], 4, True, qscale=1e-20)
+
+
+def test_zero_pages_and_zero_rows():
+    pool = Pool([400], 2, 16, 64)
+    K, V = _rand((400, 2, 64), 1, torch.float32), _rand((400, 2, 64), 2, torch.float32)
+    K[0:160] = 0
+    V[128:272] = 0
+    K[320:] = 0
+    pool.append([400], [400], K, V)
+    check(pool, [400], [100], 4, True)
+    check(pool, [400], [100], 4, True, qscale=0.0)
+
+
+def test_paths_agree_and_calls_repeat():
+    # the same rows through the many-rows path (one call) and the few-rows path (fp32 rows)
+    lens, rows = [900, 333], [200, 150]
+    pool = _filled(lens, 2, 64, 128)
+    q = _rand((350, 8, 128), 5, BF).to(DEV)
+    a, la = _run(pool, pool.step(lens, rows), q, True)
+    b, lb = _run(pool, pool.step(lens, rows), q, True)
+    assert torch.equal(a, b) and torch.equal(la, lb)
+    f, lf = _run(pool, pool.step(lens, rows), q.float(), True)
+    # within the output's rounding and the fp16 probabilities' (2^-11 of sum p |V| <= max |V|),
+    # and the scores' error: sums of up to size = sum |q| |k| * scale, as in check()
+    K, V = (np.abs(kv8.VALUE[c]) * x[..., None, None] for c, x in zip(pool.codes, pool.scale))
+    vmax, kmax = np.nanmax(V[V < 1e6]), np.nanmax(K[K < 1e6])
+    E = float(q.float().abs().sum(-1).max()) * kmax / 128 ** 0.5 * 14 * 2.0 ** -23
+    assert ((a.float() - f).abs() <= 2.0 ** -8 * f.abs() + (2.0 ** -10 + 4 * E) * vmax).all()
+    assert ((la - lf).abs() <= 2 * E + 1e-5).all()
