@@ -7,11 +7,12 @@
 // them.  Persistent blocks, one per SM, share out the line of key tiles
 // (kv8_sched.cuh).  Warps (512 threads, register shares set per warpgroup):
 //   0-3, 4-7  softmax of row tile A, B: one thread a row
-//   8-11      converters: 16-byte loads of a tile's codes (the next tile's are
-//             in flight while this one's are expanded), e4m3 -> fp16, 128-byte
-//             swizzled K and V tiles in shared memory, two stages each; the
-//             unit's query rows too
+//   8-11      converters: a tile's codes from the staging buffer, e4m3 -> fp16,
+//             into 128-byte-swizzled K and V tiles, two stages each; the unit's
+//             query rows too
 //   12        one thread issues the MMAs
+//   13        loader: page numbers, scales, and a bulk copy per page into the
+//             staging buffer (one tile of K and one of V)
 // Tensor memory: S_A, S_B (128 columns each; P over the first 64 as fp16
 // pairs), O_A, O_B (d columns each).  Order of issue per tile t:
 //   PV_A(t) S_A(t+1) PV_B(t) S_B(t+1)
@@ -40,20 +41,24 @@ using namespace tc;
 
 constexpr int kTcThreads = 512;
 constexpr int kTcMT = 256, kTcKT = 128;
-constexpr int kConvWarp0 = 8, kConvWarps = 4, kIssueWarp = 12;
+constexpr int kConvWarp0 = 8, kConvWarps = 4, kIssueWarp = 12, kLoadWarp = 13;
 constexpr float kTcSlack = 10.f;                // log2 units
 constexpr int kTcPExp = 4;
 constexpr uint32_t kBlk = 128 * 128;            // 128 rows x 128 bytes (64 fp16 columns)
 constexpr uint32_t kSCol = 0, kOCol = 256;
+constexpr int kRefs = 8;                        // tiles whose scales are kept (the loader is at most 4 ahead)
 
 template <int D>
 struct TcSmem {
   uint8_t q[2][D / 64][kBlk];                   // query rows of the unit, [row tile][64-column block]
   uint8_t k[2][D / 64][kBlk];                   // [stage][block]
   uint8_t v[2][D / 64][kBlk];
+  uint8_t code[2][kTcKT * D];                   // a tile's codes as they are in the cache, [K, V]
   float qs[kTcMT];                              // power of two of each query row
-  float kref[4], vref[4];                       // largest page scales of tile t, at t % 4
-  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], ref_full[4];
+  float ref[kRefs][2];                          // largest page scales of tile t, at t % kRefs, [K, V]
+  float part[kRefs][2][8];                      // each 16-token group's share of them
+  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], ref_full[kRefs];
+  uint64_t code_full[2], code_empty[2];
   uint64_t s_full[2], p_full[2], o_full[2], done;
   int64_t scan[kTcThreads / 32];
   Share share;
@@ -127,7 +132,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       mbar_init(&sm.p_full[i], 4);
       mbar_init(&sm.o_full[i], 1);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&sm.ref_full[i], 1);
+    for (int i = 0; i < kRefs; ++i) mbar_init(&sm.ref_full[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.code_full[i], 1);
+      mbar_init(&sm.code_empty[i], kConvWarps);
+    }
     mbar_init(&sm.done, 1);
     sm.abort = 0;
     fence_mbar_init();
@@ -151,8 +160,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
   auto rows_of = [&]() { return min(kTcMT, w.u.q.m * G - w.u.rt * kTcMT); };
 
   if (warp >= kConvWarp0 + kConvWarps) {
-    // registers a thread: 128 at launch; 168 + 168 + 120 + 56 = 4 * 128
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // registers a thread: 128 at launch; 184 + 184 + 72 + 72 = 4 * 128
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == kIssueWarp && lane == 0) {
       // ---- MMA issuer
       constexpr uint32_t id_s = idesc_f16(128, kTcKT, false), id_o = idesc_f16(128, D, true);
@@ -226,46 +235,90 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       mma_commit(&sm.done);
       drain_wait(&sm.done, 0);
     }
+    if (warp == kLoadWarp) {
+      // ---- loader: lane -> (tile, page) of a batch of 32 pages; page numbers and
+      // scales of the next batch load while this one's copies are issued
+      const int ppt = kTcKT / c.page, tpb = 32 / ppt;
+      const int bt = lane / ppt, bp = lane % ppt;
+      const uint32_t page_bytes = (uint32_t)c.page * D;
+      bool ok = true;
+      int copied[2] = {0, 0};                   // tiles of K and of V under way or landed
+      do {
+        auto look = [&](int first, int& pid, float& ks, float& vs, bool& live) {
+          const int tile = first + bt, j = tile * ppt + bp;
+          live = tile < w.t1 && j * c.page < w.u.kend;
+          pid = live ? load_page(s, c.n_pages, w.u.r, j, a.status) : -1;
+          const int64_t at = (int64_t)max(pid, 0) * c.Hkv + w.u.g;
+          ks = pid >= 0 ? __ldg(c.K_scale + at) : 0.f;
+          vs = pid >= 0 ? __ldg(c.V_scale + at) : 0.f;
+        };
+        int pid, npid = -1;
+        float ks, vs, nks = 0.f, nvs = 0.f;
+        bool live, nlive = false;
+        look(w.t0, pid, ks, vs, live);
+        for (int tb = w.t0; ok && tb < w.t1; tb += tpb) {
+          if (tb + tpb < w.t1) look(tb + tpb, npid, nks, nvs, nlive);
+          // each tile's largest scales
+          float kref = ks, vref = vs;
+          for (int o = 1; o < ppt; o <<= 1) {
+            kref = fmaxf(kref, __shfl_xor_sync(0xffffffffu, kref, o));
+            vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, o));
+          }
+          const float kf = ks * pow2_inverse(kref), vf = vs * pow2_inverse(vref);
+          const int nt = min(tpb, w.t1 - tb);
+          for (int i = 0; i < nt; ++i, ++t) {
+            const bool mine = bt == i;
+            const int rt = t % kRefs;
+            const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine && live)) * page_bytes;
+            const int64_t at = ((int64_t)max(pid, 0) * c.Hkv + w.u.g) * (int64_t)page_bytes;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (!warp_wait(&sm.code_empty[h], (t & 1) ^ 1, abort)) {
+                ok = false;
+                break;
+              }
+              if (h == 0 && mine) {
+                if (bp == 0) {
+                  sm.ref[rt][0] = kref;
+                  sm.ref[rt][1] = vref;
+                }
+                for (int e = 0; e < c.page / 16; ++e) {
+                  sm.part[rt][0][bp * (c.page / 16) + e] = kf;
+                  sm.part[rt][1][bp * (c.page / 16) + e] = vf;
+                }
+              }
+              __syncwarp();
+              if (lane == 0) {
+                if (h == 0) mbar_arrive(&sm.ref_full[rt]);
+                mbar_arrive_expect_tx(&sm.code_full[h], bytes);
+              }
+              ++copied[h];
+              __syncwarp();
+              // (a page that does not exist has scale 0: page 0 stands in)
+              if (mine && live)
+                bulk_load(sm.code[h] + bp * page_bytes, static_cast<const uint8_t*>(h ? c.V_codes : c.K_codes) + at,
+                          page_bytes, &sm.code_full[h]);
+            }
+            if (!ok) break;
+          }
+          pid = npid;
+          ks = nks;
+          vs = nvs;
+          live = nlive;
+        }
+      } while (ok && w.next(line, s, a.status));
+      // every copy has landed before the block may end
+      __syncwarp();
+      if (lane == 0)
+        for (int h = 0; h < 2; ++h)
+          if (copied[h] > 0) drain_wait(&sm.code_full[h], (copied[h] - 1) & 1);
+    }
   } else if (warp >= kConvWarp0) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // ---- converters
-    constexpr int LPR = D / 16;                 // lanes of a row (16 codes each)
-    constexpr int RP = 128 / LPR, NJ = 128 / RP;
     const int i = threadIdx.x - 32 * kConvWarp0;
-    const int key_in = i / LPR, ch = i % LPR;
     bool ok = true;
     do {
-      // lane l < 8: the page of token group l (16 tokens) of a tile, or -1
-      auto page_of = [&](int tile) -> int {
-        const int key = tile * kTcKT + 16 * (lane & 7);
-        if (tile >= w.t1 || key >= w.u.kend) return -1;
-        return load_page(s, c.n_pages, w.u.r, key / c.page, a.status);
-      };
-      auto scales_of = [&](int pid, float& ks, float& vs) {
-        const int64_t at = (int64_t)max(pid, 0) * c.Hkv + w.u.g;
-        ks = pid >= 0 ? __ldg(c.K_scale + at) : 0.f;
-        vs = pid >= 0 ? __ldg(c.V_scale + at) : 0.f;
-      };
-      uint4 kr[NJ], vr[NJ];
-      auto load = [&](const void* pool, int tile, int pid, uint4 (&y)[NJ]) {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const int key = key_in + RP * j;
-          const int p = __shfl_sync(0xffffffffu, pid, key >> 4);
-          const int tok = tile * kTcKT + key;
-          y[j] = make_uint4(0u, 0u, 0u, 0u);
-          if (p >= 0 && tok < w.u.kend)
-            y[j] = __ldg(reinterpret_cast<const uint4*>(
-                static_cast<const uint8_t*>(pool) +
-                (((int64_t)p * c.Hkv + w.u.g) * c.page + (tok & (c.page - 1))) * D + ch * 16));
-        }
-      };
-      int pid = page_of(w.t0);
-      float ks, vs;
-      scales_of(pid, ks, vs);
-      load(c.K_codes, w.t0, pid, kr);
-      load(c.V_codes, w.t0, pid, vr);
-      int pid1 = page_of(w.t0 + 1);
       // the unit's query rows, once the last S of the segment before is done
       if (!warp_wait(&sm.q_empty, (seg & 1) ^ 1, abort)) break;
       {
@@ -304,54 +357,38 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full);
-      for (int j = w.t0; j < w.t1; ++j, ++t) {
+      for (int j = w.t0; ok && j < w.t1; ++j, ++t) {
         const int st = t & 1;
-        float ks1, vs1;
-        scales_of(pid1, ks1, vs1);
-        const int pid2 = page_of(j + 2);
-        // the tile's largest scales, and each group's share of them
-        float kref = ks, vref = vs;
+        const int left = w.u.kend - j * kTcKT;  // tokens of the tile
 #pragma unroll
-        for (int o = 4; o > 0; o >>= 1) {
-          kref = fmaxf(kref, __shfl_xor_sync(0xffffffffu, kref, o));
-          vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, o));
-        }
-        const float kf = ks * pow2_inverse(kref), vf = vs * pow2_inverse(vref);
-        ok = warp_wait(&sm.k_empty[st], ((t >> 1) & 1) ^ 1, abort);
-        if (!ok) break;
-        if (i == 0) {
-          sm.kref[t & 3] = kref;
-          sm.vref[t & 3] = vref;
-          mbar_arrive(&sm.ref_full[t & 3]);
-        }
+        for (int h = 0; h < 2; ++h) {
+          // K, then V: the codes have landed, the stage is free
+          ok = warp_wait(&sm.code_full[h], t & 1, abort) &&
+               warp_wait(h ? &sm.v_empty[st] : &sm.k_empty[st], ((t >> 1) & 1) ^ 1, abort);
+          if (!ok) break;
+          constexpr int LPR = D / 16, RP = 128 / LPR;   // lanes of a row (16 codes each), rows at once
+          const int key0 = i / LPR, ch = i % LPR;
+          uint8_t* tile = h ? sm.v[st][0] : sm.k[st][0];
+          const float* part = sm.part[t % kRefs][h];
 #pragma unroll
-        for (int n = 0; n < NJ; ++n) {
-          const int key = key_in + RP * n;
-          expand16(sm.k[st][0], key, ch, kr[n], __shfl_sync(0xffffffffu, kf, key >> 4));
+          for (int n = 0; n < 128 / RP; ++n) {
+            const int key = key0 + RP * n;
+            uint4 y = *reinterpret_cast<const uint4*>(sm.code[h] + key * D + ch * 16);
+            if (key >= left) y = make_uint4(0u, 0u, 0u, 0u);    // not a token: whatever was there
+            expand16(tile, key, ch, y, part[key >> 4]);
+          }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&sm.code_empty[h]);
+            mbar_arrive(h ? &sm.v_full[st] : &sm.k_full[st]);
+          }
         }
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.k_full[st]);
-        load(c.K_codes, j + 1, pid1, kr);
-        ok = warp_wait(&sm.v_empty[st], ((t >> 1) & 1) ^ 1, abort);
-        if (!ok) break;
-#pragma unroll
-        for (int n = 0; n < NJ; ++n) {
-          const int key = key_in + RP * n;
-          expand16(sm.v[st][0], key, ch, vr[n], __shfl_sync(0xffffffffu, vf, key >> 4));
-        }
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.v_full[st]);
-        load(c.V_codes, j + 1, pid1, vr);
-        ks = ks1;
-        vs = vs1;
-        pid1 = pid2;
       }
       ++seg;
     } while (ok && w.next(line, s, a.status));
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     // ---- softmax of row tile X, one row a thread
     const int X = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane_off = (uint32_t)((warp & 3) << 5) << 16;
@@ -371,13 +408,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       if (a.causal) lim = min(lim, w.u.q.len - w.u.q.m + 1 + qi);
       float m = -INFINITY, l = 0.f, cs = 0.f, vmax = 0.f;
       for (int j = w.t0; j < w.t1; ++j, ++t) {
-        ok = ok && warp_wait(&sm.ref_full[t & 3], (t >> 2) & 1, abort) && warp_wait(&sm.s_full[X], ns & 1, abort);
+        ok = ok && warp_wait(&sm.ref_full[t % kRefs], (t / kRefs) & 1, abort) && warp_wait(&sm.s_full[X], ns & 1, abort);
         if (!ok) continue;
         ++ns;
         tc_fence_after();
         if (j == w.t0) cs = a.scale_log2 * sm.qs[X * 128 + row];
         // (f > 0, so that a masked score stays -inf: scores below 1e-37 are 0)
-        const float f = fmaxf(cs * sm.kref[t & 3], 1e-37f), vr = sm.vref[t & 3];
+        const float f = fmaxf(cs * sm.ref[t % kRefs][0], 1e-37f), vr = sm.ref[t % kRefs][1];
         float x[8][16];
         {
           uint32_t v[8][16];
