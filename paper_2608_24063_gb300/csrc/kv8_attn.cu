@@ -131,7 +131,8 @@ __device__ __forceinline__ void load_q(const T* q, int64_t q_stride, const Unit&
     }
     amax = max_quad(amax);
     const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
-    qs[h] = ex == 0u || ex >= 0x7f000000u ? 1.f : __uint_as_float(ex);   // zero, tiny, huge or not finite: as it is
+    // zero, tiny or not finite rows as they are; 2^126 at most, whose inverse is normal
+    qs[h] = ex == 0u || ex == 0x7f800000u ? 1.f : __uint_as_float(min(ex, 253u << 23));
     const float inv = pow2_inverse(qs[h]);
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
@@ -528,8 +529,10 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
+}  // namespace
+
 // The pool as rows of d codes; a box is a page's rows of one head.
-bool pool_map(CUtensorMap* m, const void* base, const vc_kv8& c) {
+bool kv8_pool_map(CUtensorMap* m, const void* base, const vc_kv8& c) {
   PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
   if (!enc) return false;
   cuuint64_t dims[2] = {(cuuint64_t)c.d, (cuuint64_t)c.n_pages * c.Hkv * c.page};
@@ -540,6 +543,8 @@ bool pool_map(CUtensorMap* m, const void* base, const vc_kv8& c) {
              CU_TENSOR_MAP_INTERLEAVE_NONE, c.d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+namespace {
 
 template <typename T, int D>
 cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
@@ -552,7 +557,7 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
     attr.store(true, std::memory_order_relaxed);
   }
   CUtensorMap mk, mv;
-  if (!pool_map(&mk, c.K_codes, c) || !pool_map(&mv, c.V_codes, c)) return cudaErrorInvalidValue;
+  if (!kv8_pool_map(&mk, c.K_codes, c) || !kv8_pool_map(&mv, c.V_codes, c)) return cudaErrorInvalidValue;
   // no more blocks than the line can have tiles
   const int64_t G = a.Hq / c.Hkv;
   const int64_t units = ((int64_t)s.n_rows * G / kMT + (s.n_req < s.n_rows ? s.n_req : s.n_rows)) * c.Hkv;

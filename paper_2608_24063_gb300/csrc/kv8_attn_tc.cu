@@ -5,14 +5,23 @@
 // over tiles of 128 tokens: 4 * 256 * 128 * d flops a tile, so it is bound by
 // the tensor cores once the softmax and the expansion of the codes run beside
 // them.  Persistent blocks, one per SM, share out the line of key tiles
-// (kv8_sched.cuh).  Warps (512 threads, register shares set per warpgroup):
+// (kv8_sched.cuh).
+//
+// S = Q K^T runs on the codes as they are (kind::f8f6f4): a bf16 number has 8
+// significant bits and an e4m3 number 4, so a query value is exactly the sum
+// of two e4m3 numbers, its rounding and the rest (values below 2^-10 of their
+// row's largest keep 2^-18 of it).  Two products at twice the rate cost what
+// one fp16 product does, and K needs no expansion: TMA writes its tiles.
+// O = P V runs in fp16: P needs more than e4m3's range, so V is expanded,
+// once for both row tiles.
+//
+// Warps (512 threads, register shares set per warpgroup):
 //   0-3, 4-7  softmax of row tile A, B: one thread a row
-//   8-11      converters: a tile's codes from the staging buffer, e4m3 -> fp16,
-//             into 128-byte-swizzled K and V tiles, two stages each; the unit's
-//             query rows too
+//   8-11      converters: V codes from the staging buffer, e4m3 -> fp16, into
+//             128-byte-swizzled tiles, two stages; the unit's query rows too
 //   12        one thread issues the MMAs
-//   13        loader: page numbers, scales, and a bulk copy per page into the
-//             staging buffer (one tile of K and one of V)
+//   13        loader: page numbers, scales, a TMA box per page of K, a bulk
+//             copy per page of V
 // Tensor memory: S_A, S_B (128 columns each; P over the first 64 as fp16
 // pairs), O_A, O_B (d columns each).  Order of issue per tile t:
 //   PV_A(t) S_A(t+1) PV_B(t) S_B(t+1)
@@ -20,12 +29,13 @@
 // thread execute in order, so S_A(t+1) may overwrite the P_A(t) that PV_A(t)
 // reads, and s_full of tile t + 1 says that PV(t) is done too.
 //
-// Numbers: query rows are divided by the power of two below their largest
-// magnitude, codes multiplied by their page's scale over the tile's largest
-// one, so both are fp16 without rounding (but for pages 2^-14 of their tile).
-// A row's maximum may be passed by 2^10 before O is rescaled; P = 2^(x - m + 4)
-// times (V scale of the tile / the largest so far), at most 2^14, keeps 11
-// bits down to 2^-18 of its reference.  Row sums are fp32, of unrounded terms.
+// Numbers: query rows are scaled by a power of two to a largest magnitude in
+// [128, 256).  Scores are scaled by their page's K scale in fp32.  V codes are
+// multiplied by their page's scale over the tile's largest one (exact but for
+// pages 2^-14 of their tile).  A row's maximum may be passed by 2^10 before O
+// is rescaled; P = 2^(x - m + 4) times (V scale of the tile / the largest so
+// far), at most 2^14, keeps 11 bits down to 2^-18 of its reference.  Row sums
+// are fp32, of unrounded terms.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_sched.cuh"
@@ -46,19 +56,21 @@ constexpr float kTcSlack = 10.f;                // log2 units
 constexpr int kTcPExp = 4;
 constexpr uint32_t kBlk = 128 * 128;            // 128 rows x 128 bytes (64 fp16 columns)
 constexpr uint32_t kSCol = 0, kOCol = 256;
+constexpr int kKStages = 3, kVStages = 2, kCodeStages = 2;
 constexpr int kRefs = 8;                        // tiles whose scales are kept (the loader is at most 4 ahead)
 
 template <int D>
 struct TcSmem {
-  uint8_t q[2][D / 64][kBlk];                   // query rows of the unit, [row tile][64-column block]
-  uint8_t k[2][D / 64][kBlk];                   // [stage][block]
-  uint8_t v[2][D / 64][kBlk];
-  uint8_t code[2][kTcKT * D];                   // a tile's codes as they are in the cache, [K, V]
+  uint8_t v[kVStages][D / 64][kBlk];            // V as fp16, [stage][64-column block]
+  uint8_t q[2][2][128 * D];                     // query rows of the unit, [row tile][rounding, rest]
+  uint8_t k[kKStages][kTcKT * D];               // K codes
+  uint8_t code[kCodeStages][kTcKT * D];         // V codes as they are in the cache
   float qs[kTcMT];                              // power of two of each query row
-  float ref[kRefs][2];                          // largest page scales of tile t, at t % kRefs, [K, V]
-  float part[kRefs][2][8];                      // each 16-token group's share of them
-  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], ref_full[kRefs];
-  uint64_t code_full[2], code_empty[2];
+  float kscale[kRefs][8];                       // K scale of each 16-token group of tile t, at t % kRefs
+  float vshare[kRefs][8];                       // V scale of each group over the tile's largest
+  float vref[kRefs];                            // the tile's largest V scale
+  uint64_t q_full, q_empty, k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
+  uint64_t code_full[kCodeStages], code_empty[kCodeStages], ref_full[kRefs];
   uint64_t s_full[2], p_full[2], o_full[2], done;
   int64_t scan[kTcThreads / 32];
   Share share;
@@ -66,19 +78,59 @@ struct TcSmem {
   int abort, last[2];
 };
 
-// Instruction descriptor, kind::f16: A, B fp16, D fp32; B K-major, or MN-major.
-__host__ __device__ constexpr uint32_t idesc_f16(uint32_t M, uint32_t N, bool b_mn) {
-  return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((N >> 3) << 17) | ((M >> 4) << 24);
+// Instruction descriptors, D fp32: kind::f16 with A, B fp16 and B MN-major;
+// kind::f8f6f4 with A, B e4m3, both K-major.
+__host__ __device__ constexpr uint32_t idesc_f16_bmn(uint32_t M, uint32_t N) {
+  return (1u << 4) | (1u << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+__host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N) {
+  return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24);
 }
 
-// D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
-__device__ __forceinline__ void mma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                           uint32_t accumulate) {
+// Descriptor of a K-major tile of 8-bit rows of D bytes: 128-byte swizzle
+// (8-row groups 1024 bytes apart) or, at D = 64, 64-byte swizzle (512).
+template <int D>
+__device__ __forceinline__ uint64_t desc_codes(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)1 << 16;
+  d |= (uint64_t)((8 * D) >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)(D == 128 ? 2 : 4) << 61;
+  return d;
+}
+// Byte offset of 8-byte piece c of row r in such a tile.
+template <int D>
+__device__ __forceinline__ uint32_t code_piece(int r, int c) {
+  const int ch = D == 128 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
+  return (uint32_t)(r * D + ch * 16 + (c & 1) * 8);
+}
+
+// Shared-memory descriptors are 64 bits of which only the low word, with the
+// address in units of 16 bytes, changes: the halves are joined at the MMA, so
+// the issuing thread keeps a few registers instead of a descriptor per operand.
+//
+// D[tmem] (+)= A[smem] * B[smem]^T, issued by one thread.
+__device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi,
+                                            uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+      "mov.b64 a, {%1, %3};\n\t"
+      "mov.b64 b, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi,
+                                           uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+      "mov.b64 b, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 
@@ -112,7 +164,8 @@ __device__ __forceinline__ void expand16(uint8_t* tile, int row, int c, const ui
 }
 
 template <int D>
-__global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid_constant__ vc_kv8 c,
+__global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK,
+                                                                    const __grid_constant__ vc_kv8 c,
                                                                     const __grid_constant__ vc_kv8_step s,
                                                                     const __grid_constant__ Kv8AttnArgs a) {
   extern __shared__ uint8_t smem_raw[];
@@ -123,20 +176,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
   if (threadIdx.x == 0) {
     mbar_init(&sm.q_full, kConvWarps);
     mbar_init(&sm.q_empty, 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&sm.k_full[i], kConvWarps);
+    for (int i = 0; i < kKStages; ++i) {
+      mbar_init(&sm.k_full[i], 1);
       mbar_init(&sm.k_empty[i], 1);
+    }
+    for (int i = 0; i < kVStages; ++i) {
       mbar_init(&sm.v_full[i], kConvWarps);
       mbar_init(&sm.v_empty[i], 1);
+    }
+    for (int i = 0; i < kCodeStages; ++i) {
+      mbar_init(&sm.code_full[i], 1);
+      mbar_init(&sm.code_empty[i], kConvWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&sm.s_full[i], 1);
       mbar_init(&sm.p_full[i], 4);
       mbar_init(&sm.o_full[i], 1);
     }
     for (int i = 0; i < kRefs; ++i) mbar_init(&sm.ref_full[i], 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&sm.code_full[i], 1);
-      mbar_init(&sm.code_empty[i], kConvWarps);
-    }
     mbar_init(&sm.done, 1);
     sm.abort = 0;
     fence_mbar_init();
@@ -164,56 +221,60 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == kIssueWarp && lane == 0) {
       // ---- MMA issuer
-      constexpr uint32_t id_s = idesc_f16(128, kTcKT, false), id_o = idesc_f16(128, D, true);
+      constexpr uint32_t id_s = idesc_e4m3(128, kTcKT), id_o = idesc_f16_bmn(128, D);
       bool ok = true;
       int np[2] = {0, 0};                       // P tiles consumed per row tile
-      // descriptors hold addresses in units of 16 bytes: offsets are added to them
-      const uint64_t qd = desc_sw128(smem_u32(sm.q)), kd = desc_sw128(smem_u32(sm.k));
+      const uint64_t qd = desc_codes<D>(smem_u32(sm.q)), kd = desc_codes<D>(smem_u32(sm.k));
       const uint64_t vd = desc_sw128_mn(smem_u32(sm.v), kBlk);
-      constexpr uint32_t kRows16 = sizeof(sm.q[0]) / 16;      // a row tile, a stage
+      const uint32_t hi = (uint32_t)(qd >> 32), v_hi = (uint32_t)(vd >> 32);
+      constexpr uint32_t kV16 = sizeof(sm.v[0]) / 16, kK16 = sizeof(sm.k[0]) / 16;
+      constexpr uint32_t kQ16 = sizeof(sm.q[0]) / 16, kQPart16 = sizeof(sm.q[0][0]) / 16;
       auto issue_s = [&](int x, int st) {
-        const uint64_t ad = qd + (uint32_t)x * kRows16, bd = kd + (uint32_t)st * kRows16;
+        uint32_t ad = (uint32_t)qd + (uint32_t)x * kQ16, bd = (uint32_t)kd + (uint32_t)st * kK16;
+        asm volatile("" : "+r"(ad), "+r"(bd));                // sums stay where they are used
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = ((kk >> 2) * kBlk + (kk & 3) * 32) / 16;
-          mma_bf16(tbase + kSCol + x * kTcKT, ad + off, bd + off, id_s, kk ? 1u : 0u);
-        }
+        for (int kk = 0; kk < 2 * (D / 32); ++kk)             // 32 columns: 2 x 16 bytes
+          mma_e4m3_ss(tbase + kSCol + x * kTcKT, ad + (kk & 1) * kQPart16 + (kk >> 1) * 2, bd + (kk >> 1) * 2, hi,
+                      id_s, kk ? 1u : 0u);
         mma_commit(&sm.s_full[x]);
       };
       auto issue_pv = [&](int x, int st, bool first) -> bool {
         if (!mbar_wait(&sm.p_full[x], np[x] & 1, abort)) return false;
         ++np[x];
         tc_fence_after();
-        const uint64_t bd = vd + (uint32_t)st * kRows16;
+        uint32_t bd = (uint32_t)vd + (uint32_t)st * kV16;
+        asm volatile("" : "+r"(bd));
 #pragma unroll
         for (int kk = 0; kk < kTcKT / 16; ++kk)
-          mma_f16_ta(tbase + kOCol + x * D, tbase + kSCol + x * kTcKT + kk * 8, bd + kk * 2048 / 16, id_o,
+          mma_f16_ts(tbase + kOCol + x * D, tbase + kSCol + x * kTcKT + kk * 8, bd + kk * 2048 / 16, v_hi, id_o,
                      (!first || kk) ? 1u : 0u);
         return true;
       };
       do {
         const bool two = rows_of() > 128;
-        ok = mbar_wait(&sm.q_full, seg & 1, abort) && mbar_wait(&sm.k_full[t & 1], (t >> 1) & 1, abort);
+        int ks = t % kKStages;
+        ok = mbar_wait(&sm.q_full, seg & 1, abort) && mbar_wait(&sm.k_full[ks], (t / kKStages) & 1, abort);
         if (!ok) break;
         tc_fence_after();
-        issue_s(0, t & 1);
-        if (two) issue_s(1, t & 1);
-        mma_commit(&sm.k_empty[t & 1]);
+        issue_s(0, ks);
+        if (two) issue_s(1, ks);
+        mma_commit(&sm.k_empty[ks]);
         for (int j = w.t0; ok && j < w.t1; ++j, ++t) {
-          const int st = t & 1, sn = (t + 1) & 1;
+          const int st = t % kVStages;
           const bool more = j + 1 < w.t1;
-          if (!mbar_wait(&sm.v_full[st], (t >> 1) & 1, abort) || !issue_pv(0, st, j == w.t0)) {
+          ks = (t + 1) % kKStages;
+          if (!mbar_wait(&sm.v_full[st], (t / kVStages) & 1, abort) || !issue_pv(0, st, j == w.t0)) {
             ok = false;
             break;
           }
           if (!more) mma_commit(&sm.o_full[0]);
           if (more) {
-            if (!mbar_wait(&sm.k_full[sn], ((t + 1) >> 1) & 1, abort)) {
+            if (!mbar_wait(&sm.k_full[ks], ((t + 1) / kKStages) & 1, abort)) {
               ok = false;
               break;
             }
             tc_fence_after();
-            issue_s(0, sn);
+            issue_s(0, ks);
           }
           if (two) {
             if (!issue_pv(1, st, j == w.t0)) {
@@ -224,8 +285,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
           }
           mma_commit(&sm.v_empty[st]);
           if (more) {
-            if (two) issue_s(1, sn);
-            mma_commit(&sm.k_empty[sn]);
+            if (two) issue_s(1, ks);
+            mma_commit(&sm.k_empty[ks]);
           }
         }
         if (ok) mma_commit(&sm.q_empty);
@@ -242,7 +303,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       const int bt = lane / ppt, bp = lane % ppt;
       const uint32_t page_bytes = (uint32_t)c.page * D;
       bool ok = true;
-      int copied[2] = {0, 0};                   // tiles of K and of V under way or landed
+      int nk = 0;                               // K tiles under way or landed (t counts V tiles)
+      prefetch_tmap(&tmK);
       do {
         auto look = [&](int first, int& pid, float& ks, float& vs, bool& live) {
           const int tile = first + bt, j = tile * ppt + bp;
@@ -258,48 +320,40 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
         look(w.t0, pid, ks, vs, live);
         for (int tb = w.t0; ok && tb < w.t1; tb += tpb) {
           if (tb + tpb < w.t1) look(tb + tpb, npid, nks, nvs, nlive);
-          // each tile's largest scales
-          float kref = ks, vref = vs;
-          for (int o = 1; o < ppt; o <<= 1) {
-            kref = fmaxf(kref, __shfl_xor_sync(0xffffffffu, kref, o));
-            vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, o));
-          }
-          const float kf = ks * pow2_inverse(kref), vf = vs * pow2_inverse(vref);
+          float vref = vs;                      // each tile's largest V scale
+          for (int o = 1; o < ppt; o <<= 1) vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, o));
+          const float vshare = vs * pow2_inverse(vref);
           const int nt = min(tpb, w.t1 - tb);
+          // (a page that does not exist has scale 0: page 0 stands in)
+          const int row = (max(pid, 0) * c.Hkv + w.u.g) * c.page;
           for (int i = 0; i < nt; ++i, ++t) {
             const bool mine = bt == i;
-            const int rt = t % kRefs;
+            const int rt = t % kRefs, kst = t % kKStages, cst = t % kCodeStages;
             const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine && live)) * page_bytes;
-            const int64_t at = ((int64_t)max(pid, 0) * c.Hkv + w.u.g) * (int64_t)page_bytes;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (!warp_wait(&sm.code_empty[h], (t & 1) ^ 1, abort)) {
-                ok = false;
-                break;
-              }
-              if (h == 0 && mine) {
-                if (bp == 0) {
-                  sm.ref[rt][0] = kref;
-                  sm.ref[rt][1] = vref;
-                }
-                for (int e = 0; e < c.page / 16; ++e) {
-                  sm.part[rt][0][bp * (c.page / 16) + e] = kf;
-                  sm.part[rt][1][bp * (c.page / 16) + e] = vf;
-                }
-              }
-              __syncwarp();
-              if (lane == 0) {
-                if (h == 0) mbar_arrive(&sm.ref_full[rt]);
-                mbar_arrive_expect_tx(&sm.code_full[h], bytes);
-              }
-              ++copied[h];
-              __syncwarp();
-              // (a page that does not exist has scale 0: page 0 stands in)
-              if (mine && live)
-                bulk_load(sm.code[h] + bp * page_bytes, static_cast<const uint8_t*>(h ? c.V_codes : c.K_codes) + at,
-                          page_bytes, &sm.code_full[h]);
-            }
+            ok = warp_wait(&sm.k_empty[kst], ((t / kKStages) & 1) ^ 1, abort);
             if (!ok) break;
+            if (mine) {
+              if (bp == 0) sm.vref[rt] = vref;
+              for (int e = 0; e < c.page / 16; ++e) {
+                sm.kscale[rt][bp * (c.page / 16) + e] = ks;
+                sm.vshare[rt][bp * (c.page / 16) + e] = vshare;
+              }
+            }
+            __syncwarp();
+            if (lane == 0) {
+              mbar_arrive(&sm.ref_full[rt]);
+              mbar_arrive_expect_tx(&sm.k_full[kst], bytes);
+            }
+            ++nk;
+            __syncwarp();
+            if (mine && live) tma_load_2d(sm.k[kst] + bp * page_bytes, &tmK, 0, row, &sm.k_full[kst]);
+            ok = warp_wait(&sm.code_empty[cst], ((t / kCodeStages) & 1) ^ 1, abort);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_expect_tx(&sm.code_full[cst], bytes);
+            __syncwarp();
+            if (mine && live)
+              bulk_load(sm.code[cst] + bp * page_bytes, static_cast<const uint8_t*>(c.V_codes) + (int64_t)row * D,
+                        page_bytes, &sm.code_full[cst]);
           }
           pid = npid;
           ks = nks;
@@ -309,9 +363,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       } while (ok && w.next(line, s, a.status));
       // every copy has landed before the block may end
       __syncwarp();
-      if (lane == 0)
-        for (int h = 0; h < 2; ++h)
-          if (copied[h] > 0) drain_wait(&sm.code_full[h], (copied[h] - 1) & 1);
+      if (lane == 0) {
+        for (int i = max(0, nk - kKStages); i < nk; ++i) drain_wait(&sm.k_full[i % kKStages], (i / kKStages) & 1);
+        for (int i = max(0, t - kCodeStages); i < t; ++i)
+          drain_wait(&sm.code_full[i % kCodeStages], (i / kCodeStages) & 1);
+      }
     }
   } else if (warp >= kConvWarp0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -344,45 +400,58 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
           }
 #pragma unroll
           for (int o = QL / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+          // largest magnitude to [128, 256); zero, tiny or not finite rows as they are
           const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
-          const float qs = ex == 0u || ex >= 0x7f000000u ? 1.f : __uint_as_float(ex);
+          const float qs = ex <= (7u << 23) || ex == 0x7f800000u ? 1.f : __uint_as_float(ex - (7u << 23));
           const float inv = pow2_inverse(qs);
-          uint8_t* dst = sm.q[r >> 7][qc >> 3] + (r & 127) * 128 + (((qc & 7) ^ (r & 7)) << 4);
-          *reinterpret_cast<uint4*>(dst) =
-              make_uint4(half2_bits(x[0] * inv, x[1] * inv), half2_bits(x[2] * inv, x[3] * inv),
-                         half2_bits(x[4] * inv, x[5] * inv), half2_bits(x[6] * inv, x[7] * inv));
+          uint32_t top[2], rest[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float z[4], r4[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              z[k] = x[4 * e + k] * inv;
+              if (!(fabsf(z[k]) <= 448.f)) z[k] = __uint_as_float(0x7fffffffu);      // NaN, infinite
+            }
+            const uint32_t p0 = f32x2_to_e4m3x2(z[0], z[1]), p1 = f32x2_to_e4m3x2(z[2], z[3]);
+            const uint32_t h0 = e4m3x2_to_f16x2(p0), h1 = e4m3x2_to_f16x2(p1);
+            const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0));
+            const float2 f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+            r4[0] = z[0] - f0.x; r4[1] = z[1] - f0.y; r4[2] = z[2] - f1.x; r4[3] = z[3] - f1.y;
+            top[e] = p0 | p1 << 16;
+            rest[e] = f32x2_to_e4m3x2(r4[0], r4[1]) | f32x2_to_e4m3x2(r4[2], r4[3]) << 16;
+          }
+          const uint32_t off = code_piece<D>(r & 127, qc);
+          *reinterpret_cast<uint2*>(sm.q[r >> 7][0] + off) = make_uint2(top[0], top[1]);
+          *reinterpret_cast<uint2*>(sm.q[r >> 7][1] + off) = make_uint2(rest[0], rest[1]);
           if (qc == 0) sm.qs[r] = qs;
         }
       }
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full);
-      for (int j = w.t0; ok && j < w.t1; ++j, ++t) {
-        const int st = t & 1;
+      for (int j = w.t0; j < w.t1; ++j, ++t) {
+        const int st = t % kVStages, cst = t % kCodeStages;
         const int left = w.u.kend - j * kTcKT;  // tokens of the tile
+        // the codes have landed, the stage is free
+        ok = warp_wait(&sm.code_full[cst], (t / kCodeStages) & 1, abort) &&
+             warp_wait(&sm.v_empty[st], ((t / kVStages) & 1) ^ 1, abort);
+        if (!ok) break;
+        constexpr int LPR = D / 16, RP = 128 / LPR;     // lanes of a row (16 codes each), rows at once
+        const int key0 = i / LPR, ch = i % LPR;
+        const float* share = sm.vshare[t % kRefs];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          // K, then V: the codes have landed, the stage is free
-          ok = warp_wait(&sm.code_full[h], t & 1, abort) &&
-               warp_wait(h ? &sm.v_empty[st] : &sm.k_empty[st], ((t >> 1) & 1) ^ 1, abort);
-          if (!ok) break;
-          constexpr int LPR = D / 16, RP = 128 / LPR;   // lanes of a row (16 codes each), rows at once
-          const int key0 = i / LPR, ch = i % LPR;
-          uint8_t* tile = h ? sm.v[st][0] : sm.k[st][0];
-          const float* part = sm.part[t % kRefs][h];
-#pragma unroll
-          for (int n = 0; n < 128 / RP; ++n) {
-            const int key = key0 + RP * n;
-            uint4 y = *reinterpret_cast<const uint4*>(sm.code[h] + key * D + ch * 16);
-            if (key >= left) y = make_uint4(0u, 0u, 0u, 0u);    // not a token: whatever was there
-            expand16(tile, key, ch, y, part[key >> 4]);
-          }
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(&sm.code_empty[h]);
-            mbar_arrive(h ? &sm.v_full[st] : &sm.k_full[st]);
-          }
+        for (int n = 0; n < 128 / RP; ++n) {
+          const int key = key0 + RP * n;
+          uint4 y = *reinterpret_cast<const uint4*>(sm.code[cst] + key * D + ch * 16);
+          if (key >= left) y = make_uint4(0u, 0u, 0u, 0u);      // not a token: whatever was there
+          expand16(sm.v[st][0], key, ch, y, share[key >> 4]);
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&sm.code_empty[cst]);
+          mbar_arrive(&sm.v_full[st]);
         }
       }
       ++seg;
@@ -413,8 +482,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
         ++ns;
         tc_fence_after();
         if (j == w.t0) cs = a.scale_log2 * sm.qs[X * 128 + row];
-        // (f > 0, so that a masked score stays -inf: scores below 1e-37 are 0)
-        const float f = fmaxf(cs * sm.ref[t % kRefs][0], 1e-37f), vr = sm.ref[t % kRefs][1];
+        // factor of each 16 scores (above 0, so that a masked one stays -inf)
+        const float vr = sm.vref[t % kRefs];
+        float f[8];
+        {
+          const float4 k0 = *reinterpret_cast<const float4*>(&sm.kscale[t % kRefs][0]);
+          const float4 k1 = *reinterpret_cast<const float4*>(&sm.kscale[t % kRefs][4]);
+          f[0] = k0.x; f[1] = k0.y; f[2] = k0.z; f[3] = k0.w;
+          f[4] = k1.x; f[5] = k1.y; f[6] = k1.z; f[7] = k1.w;
+#pragma unroll
+          for (int p = 0; p < 8; ++p) f[p] = fmaxf(cs * f[p], 1e-37f);
+        }
         float x[8][16];
         {
           uint32_t v[8][16];
@@ -436,14 +514,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
             for (int q = 0; q < 16; ++q)
               if (p * 16 + q >= valid) x[p][q] = -INFINITY;
         }
-        float b[4];
+        float b[8];
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          b[p] = fmaxf(x[2 * p][0], x[2 * p + 1][0]);
+        for (int p = 0; p < 8; ++p) {
+          b[p] = fmaxf(x[p][0], x[p][1]);
 #pragma unroll
-          for (int q = 1; q < 16; ++q) b[p] = fmax3(b[p], x[2 * p][q], x[2 * p + 1][q]);
+          for (int q = 2; q < 16; q += 2) b[p] = fmax3(b[p], x[p][q], x[p][q + 1]);
+          b[p] *= f[p];
         }
-        const float tm = fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])) * f;
+        const float tm = fmax3(fmax3(b[0], b[1], b[2]), fmax3(b[3], b[4], b[5]), fmaxf(b[6], b[7]));
         const bool raise = tm > m + kTcSlack, vraise = vr > vmax;
         float g = 1.f;
         if (raise) {
@@ -472,7 +551,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
         // exponent of P's factor: 2^4 times the tile's share of vmax, not below 2^-26
         const int lc = vr > 0.f ? max(-30, (int)(__float_as_uint(vr) >> 23) - (int)(__float_as_uint(vmax) >> 23)) : -30;
         const float mm = (m == -INFINITY ? 0.f : m) - (float)(lc + kTcPExp);
-        const float2 sc = make_float2(f, f), nm = make_float2(-mm, -mm);
+        const float2 nm = make_float2(-mm, -mm);
         float2 l0 = make_float2(0.f, 0.f), l1 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -480,7 +559,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
 #pragma unroll
           for (int q = 0; q < 16; ++q) {
             const int k = 32 * h + 2 * q;
-            const float2 y = __ffma2_rn(make_float2(x[k >> 4][k & 15], x[k >> 4][(k & 15) + 1]), sc, nm);
+            const float2 y = __ffma2_rn(make_float2(x[k >> 4][k & 15], x[k >> 4][(k & 15) + 1]),
+                                        make_float2(f[k >> 4], f[k >> 4]), nm);
             const float2 e = make_float2(ex2(y.x), ex2(y.y));
             if (q & 1) l1 = __fadd2_rn(l1, e);
             else l0 = __fadd2_rn(l0, e);
@@ -607,12 +687,14 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
     if (e != cudaSuccess) return e;
     attr.store(true, std::memory_order_relaxed);
   }
+  CUtensorMap mk;
+  if (!kv8_pool_map(&mk, c.K_codes, c)) return cudaErrorInvalidValue;
   const int64_t G = a.Hq / c.Hkv;
   const int64_t units = ((int64_t)s.n_rows * G / kTcMT + (s.n_req < s.n_rows ? s.n_req : s.n_rows)) * c.Hkv;
   const int64_t tiles = units * (((int64_t)s.max_pages * c.page + kTcKT - 1) / kTcKT);
   const int64_t sms = kv8_sm_count();
   ProfileScope ps("kv8_attn_tc", st);
-  kv8_attn_tc_kernel<D><<<(unsigned)(tiles < sms ? tiles : sms), kTcThreads, smem, st>>>(c, s, a);
+  kv8_attn_tc_kernel<D><<<(unsigned)(tiles < sms ? tiles : sms), kTcThreads, smem, st>>>(mk, c, s, a);
   return cudaGetLastError();
 }
 

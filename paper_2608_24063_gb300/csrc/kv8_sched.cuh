@@ -13,10 +13,17 @@
 // unit's last segment adds them up in order.  Lengths are read on the device.
 #pragma once
 
+#include <cuda.h>
+
 #include "kernels.h"
 #include "kv8.cuh"
 
 namespace vc {
+
+// Tensor map of a pool's codes: rows of d bytes, a box is a page's rows of one
+// head, swizzled over whole rows (128 bytes at d = 128, 64 at d = 64).
+bool kv8_pool_map(CUtensorMap* m, const void* base, const vc_kv8& c);
+
 namespace kv8 {
 
 // Place in the line: a unit and the request's numbers.
