@@ -4,11 +4,13 @@
 // Both are one pass over the step's rows: 2 or 4 bytes a value on one side, one
 // on the other, bound by memory.  A unit is one (page touched by the step, KV
 // head, K or V): the page's rows of that head are one contiguous block of
-// codes with one scale.  A block of threads takes one unit: it loads the rows
-// it has to write into registers (16 values a vector), reduces their largest
-// magnitude, and writes the codes.  Where the page held tokens of the request
-// before, their codes are re-encoded by the same block if the scale grew, so
-// no block waits for another and nothing is written twice.
+// codes with one scale.  A block looks its page up once and takes a share of
+// the page's units in turn, the next unit's values in flight while it works on
+// the current one: it reduces the largest magnitude of the rows it has to write
+// (held in registers, 16 values a vector) and writes the codes.  Where the page
+// held tokens of the request before, their codes are re-encoded by the same
+// block if the scale grew, so no block waits for another and nothing is
+// written twice.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "profile.h"
@@ -17,6 +19,8 @@ namespace vc {
 namespace {
 
 using namespace kv8;
+
+constexpr int64_t kFill = 152 * 8;              // blocks that fill the device
 
 // The u-th page touched by the step's rows, requests in order.
 struct Touch {
@@ -87,22 +91,34 @@ struct UnitCfg {
   static_assert(NV * THREADS == VECS, "whole vectors");
 };
 
-__device__ __forceinline__ void load16(const __nv_bfloat16* p, float (&v)[16]) {
-  const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 8);
-  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+// Sixteen values as they lie in memory.
+template <typename T>
+struct Raw16 {
+  uint4 w[sizeof(T)];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < (int)sizeof(T); ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
   }
-}
-__device__ __forceinline__ void load16(const float* p, float (&v)[16]) {
+  __device__ __forceinline__ void get(float (&v)[16]) const {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 x = *reinterpret_cast<const float4*>(p + 4 * i);
-    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          v[8 * i + 2 * k] = __uint_as_float(x[k] << 16);
+          v[8 * i + 2 * k + 1] = __uint_as_float(x[k] & 0xffff0000u);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[4 * i] = __uint_as_float(w[i].x); v[4 * i + 1] = __uint_as_float(w[i].y);
+        v[4 * i + 2] = __uint_as_float(w[i].z); v[4 * i + 3] = __uint_as_float(w[i].w);
+      }
+    }
   }
-}
+};
 __device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&v)[16]) {
   uint32_t w[8];
 #pragma unroll
@@ -148,84 +164,109 @@ __device__ __forceinline__ void decode16(const uint4& c, float (&v)[16]) {
   }
 }
 
+// A block's page: the touch, the page and the slots [a, b) of the step's tokens;
+// false where there is nothing to do.  All threads of the block call it.
+struct PageJob {
+  int64_t row;           // packed row of slot 0 (it may lie before the first)
+  int p, a, b;
+};
+template <int PAGE>
+__device__ __forceinline__ bool find_job(const vc_kv8& c, const vc_kv8_step& s, int32_t* status, PageJob& job) {
+  __shared__ PageJob sj;
+  if (threadIdx.x < 32) {
+    Touch x = {};
+    const bool ok = find_touch<PAGE>(s, (int)blockIdx.x, status, x);
+    if (threadIdx.x == 0) {
+      sj.p = ok ? load_page(s, c.n_pages, x.r, x.j, status) : -1;
+      sj.a = max(x.first - x.j * PAGE, 0);
+      sj.b = min(x.len - x.j * PAGE, PAGE);
+      sj.row = (int64_t)x.row0 + (x.j * PAGE - x.first);
+    }
+  }
+  __syncthreads();
+  job = sj;
+  return job.p >= 0;
+}
+
+// Unit u of a page: KV head u % Hkv of K (u < Hkv) or of V.
 template <typename T, int D, int PAGE>
 __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_append_kernel(
     const __grid_constant__ vc_kv8 c, const __grid_constant__ vc_kv8_step s, const __grid_constant__ Kv8Rows rows,
     int32_t* status) {
   using C = UnitCfg<D, PAGE>;
-  __shared__ Touch touch;
-  __shared__ int found, page_id;
-  __shared__ float red[C::THREADS / 32];
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = blockIdx.y;
-  if (warp == 0) {
-    Touch x;
-    const bool ok = find_touch<PAGE>(s, (int)blockIdx.x, status, x);
-    if (lane == 0) {
-      found = ok;
-      if (ok) {
-        touch = x;
-        page_id = load_page(s, c.n_pages, x.r, x.j, status);
+  __shared__ float red[2][C::THREADS / 32];
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  PageJob job;
+  if (!find_job<PAGE>(c, s, status, job)) return;
+  const int a = job.a, b = job.b;                       // slots [0, a) hold older tokens
+  Raw16<T> next[C::NV];
+  auto load = [&](int u) {
+    const bool isv = u >= c.Hkv;
+    const int g = isv ? u - c.Hkv : u;
+    const int64_t rstep = isv ? rows.v_row : rows.k_row;
+    const T* src = static_cast<const T*>(isv ? rows.V : rows.K) + (int64_t)g * (isv ? rows.v_head : rows.k_head) +
+                   job.row * rstep;
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) {
+      const int vec = t + i * C::THREADS, slot = vec / C::VPR, part = vec % C::VPR;
+      if (slot >= a && slot < b) next[i].load(src + (int64_t)slot * rstep + part * 16);
+    }
+  };
+  int u = blockIdx.y;
+  load(u);
+  for (int turn = 0; u < 2 * c.Hkv; u += gridDim.y, turn ^= 1) {
+    const bool isv = u >= c.Hkv;
+    const int g = isv ? u - c.Hkv : u;
+    float* scale = (isv ? c.V_scale : c.K_scale) + (int64_t)job.p * c.Hkv + g;
+    uint8_t* codes = static_cast<uint8_t*>(isv ? c.V_codes : c.K_codes) + ((int64_t)job.p * c.Hkv + g) * (PAGE * D);
+    const float old = a > 0 ? *scale : 0.f;
+    Raw16<T> cur[C::NV];
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) cur[i] = next[i];
+    if (u + (int)gridDim.y < 2 * c.Hkv) load(u + gridDim.y);
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) {
+      const int slot = (t + i * C::THREADS) / C::VPR;
+      if (slot >= a && slot < b) {
+        float v[16];
+        cur[i].get(v);
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (finite(v[k])) amax = fmaxf(amax, fabsf(v[k]));
       }
     }
-  }
-  __syncthreads();
-  if (!found) return;
-  const Touch x = touch;
-  const int p = page_id;
-  if (p < 0) return;
-  // new tokens of the page: slots [a, b); slots [0, a) hold older ones
-  const int a = max(x.first - x.j * PAGE, 0), b = min(x.len - x.j * PAGE, PAGE);
-  const bool isv = blockIdx.z != 0;
-  const int64_t rstep = isv ? rows.v_row : rows.k_row;
-  const T* src = static_cast<const T*>(isv ? rows.V : rows.K) + (int64_t)g * (isv ? rows.v_head : rows.k_head) +
-                 ((int64_t)x.row0 + (x.j * PAGE - x.first)) * rstep;        // row of slot 0
-  float* scale = (isv ? c.V_scale : c.K_scale) + (int64_t)p * c.Hkv + g;
-  uint8_t* codes = static_cast<uint8_t*>(isv ? c.V_codes : c.K_codes) + ((int64_t)p * c.Hkv + g) * (PAGE * D);
-  const float old = a > 0 ? *scale : 0.f;
-  float v[C::NV][16];
-  float amax = 0.f;
+    // (non-negative numbers order like their bits)
+    amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+    if (lane == 0) red[turn][warp] = amax;
+    __syncthreads();                            // the other turn's row is read before the next barrier
 #pragma unroll
-  for (int i = 0; i < C::NV; ++i) {
-    const int vec = t + i * C::THREADS, slot = vec / C::VPR, part = vec % C::VPR;
-    if (slot >= a && slot < b) {
-      load16(src + (int64_t)slot * rstep + part * 16, v[i]);
+    for (int w = 0; w < C::THREADS / 32; ++w) amax = fmaxf(amax, red[turn][w]);
+    const float now = fmaxf(old, pow2_scale(amax));
+    const float inv = pow2_inverse(now);
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) {
+      const int vec = t + i * C::THREADS, slot = vec / C::VPR;
+      if (slot >= a && slot < b) {
+        float v[16];
+        cur[i].get(v);
+        *reinterpret_cast<uint4*>(codes + (size_t)vec * 16) = encode16(v, inv);
+      }
     }
-  }
+    if (now > old) {
+      // older codes under the larger scale: value * old is exact (e4m3 has four
+      // bits above 2^-135), the division by a power of two as well
+      for (int vec = t; vec < a * C::VPR; vec += C::THREADS) {
+        uint4* w = reinterpret_cast<uint4*>(codes + (size_t)vec * 16);
+        float y[16];
+        decode16(*w, y);
 #pragma unroll
-  for (int i = 0; i < C::NV; ++i) {
-    const int slot = (t + i * C::THREADS) / C::VPR;
-    if (slot >= a && slot < b) {
-#pragma unroll
-      for (int k = 0; k < 16; ++k)
-        if (finite(v[i][k])) amax = fmaxf(amax, fabsf(v[i][k]));
+        for (int k = 0; k < 16; ++k) y[k] *= old;
+        *w = encode16(y, inv);
+      }
     }
+    if (t == 0) *scale = now;
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-  if (lane == 0) red[warp] = amax;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < C::THREADS / 32; ++w) amax = fmaxf(amax, red[w]);
-  const float now = fmaxf(old, pow2_scale(amax));
-  const float inv = pow2_inverse(now);
-#pragma unroll
-  for (int i = 0; i < C::NV; ++i) {
-    const int vec = t + i * C::THREADS, slot = vec / C::VPR;
-    if (slot >= a && slot < b) *reinterpret_cast<uint4*>(codes + (size_t)vec * 16) = encode16(v[i], inv);
-  }
-  if (now > old) {
-    // older codes under the larger scale: value * old is exact (e4m3 has four
-    // bits above 2^-135), the division by a power of two as well
-    for (int vec = t; vec < a * C::VPR; vec += C::THREADS) {
-      uint4* w = reinterpret_cast<uint4*>(codes + (size_t)vec * 16);
-      float y[16];
-      decode16(*w, y);
-#pragma unroll
-      for (int k = 0; k < 16; ++k) y[k] *= old;
-      *w = encode16(y, inv);
-    }
-  }
-  if (t == 0) *scale = now;
 }
 
 template <typename T, int D, int PAGE>
@@ -233,48 +274,46 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_read_kernel(
     const __grid_constant__ vc_kv8 c, const __grid_constant__ vc_kv8_step s, const __grid_constant__ Kv8Rows rows,
     int32_t* status) {
   using C = UnitCfg<D, PAGE>;
-  __shared__ Touch touch;
-  __shared__ int found, page_id;
-  const int t = threadIdx.x, g = blockIdx.y;
-  if (t < 32) {
-    Touch x;
-    const bool ok = find_touch<PAGE>(s, (int)blockIdx.x, status, x);
-    if (t == 0) {
-      found = ok;
-      if (ok) {
-        touch = x;
-        page_id = load_page(s, c.n_pages, x.r, x.j, status);
-      }
+  const int t = threadIdx.x;
+  PageJob job;
+  if (!find_job<PAGE>(c, s, status, job)) return;
+  const int a = job.a, b = job.b;
+  uint4 next[C::NV];
+  float nscale = 0.f;
+  auto load = [&](int u) {
+    const bool isv = u >= c.Hkv;
+    const int64_t unit = (int64_t)job.p * c.Hkv + (isv ? u - c.Hkv : u);
+    nscale = __ldg((isv ? c.V_scale : c.K_scale) + unit);
+    const uint8_t* codes = static_cast<const uint8_t*>(isv ? c.V_codes : c.K_codes) + unit * (PAGE * D);
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) {
+      const int vec = t + i * C::THREADS, slot = vec / C::VPR;
+      if (slot >= a && slot < b) next[i] = __ldg(reinterpret_cast<const uint4*>(codes + (size_t)vec * 16));
     }
-  }
-  __syncthreads();
-  if (!found) return;
-  const Touch x = touch;
-  const int p = page_id;
-  if (p < 0) return;
-  const int a = max(x.first - x.j * PAGE, 0), b = min(x.len - x.j * PAGE, PAGE);
-  const bool isv = blockIdx.z != 0;
-  const int64_t rstep = isv ? rows.v_row : rows.k_row;
-  T* dst = static_cast<T*>(isv ? rows.V : rows.K) + (int64_t)g * (isv ? rows.v_head : rows.k_head) +
-           ((int64_t)x.row0 + (x.j * PAGE - x.first)) * rstep;
-  const float scale = (isv ? c.V_scale : c.K_scale)[(int64_t)p * c.Hkv + g];
-  const uint8_t* codes =
-      static_cast<const uint8_t*>(isv ? c.V_codes : c.K_codes) + ((int64_t)p * c.Hkv + g) * (PAGE * D);
-  uint4 w[C::NV];
+  };
+  int u = blockIdx.y;
+  load(u);
+  for (; u < 2 * c.Hkv; u += gridDim.y) {
+    const bool isv = u >= c.Hkv;
+    const int g = isv ? u - c.Hkv : u;
+    const int64_t rstep = isv ? rows.v_row : rows.k_row;
+    T* dst = static_cast<T*>(isv ? rows.V : rows.K) + (int64_t)g * (isv ? rows.v_head : rows.k_head) +
+             job.row * rstep;
+    const float scale = nscale;
+    uint4 cur[C::NV];
 #pragma unroll
-  for (int i = 0; i < C::NV; ++i) {
-    const int vec = t + i * C::THREADS, slot = vec / C::VPR;
-    if (slot >= a && slot < b) w[i] = *reinterpret_cast<const uint4*>(codes + (size_t)vec * 16);
-  }
+    for (int i = 0; i < C::NV; ++i) cur[i] = next[i];
+    if (u + (int)gridDim.y < 2 * c.Hkv) load(u + gridDim.y);
 #pragma unroll
-  for (int i = 0; i < C::NV; ++i) {
-    const int vec = t + i * C::THREADS, slot = vec / C::VPR, part = vec % C::VPR;
-    if (slot >= a && slot < b) {
-      float v[16];
-      decode16(w[i], v);
+    for (int i = 0; i < C::NV; ++i) {
+      const int vec = t + i * C::THREADS, slot = vec / C::VPR, part = vec % C::VPR;
+      if (slot >= a && slot < b) {
+        float v[16];
+        decode16(cur[i], v);
 #pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] *= scale;
-      store16(dst + (int64_t)slot * rstep + part * 16, v);
+        for (int k = 0; k < 16; ++k) v[k] *= scale;
+        store16(dst + (int64_t)slot * rstep + part * 16, v);
+      }
     }
   }
 }
@@ -290,7 +329,12 @@ template <typename T, int D, int PAGE>
 cudaError_t launch_t(bool append, const vc_kv8& c, const vc_kv8_step& s, const Kv8Rows& rows, int32_t* status,
                      cudaStream_t st) {
   ProfileScope ps(append ? "kv8_append" : "kv8_read", st);
-  const dim3 grid((unsigned)most_pages<PAGE>(s), (unsigned)c.Hkv, 2);
+  // blocks a page: enough blocks in all to fill the device, else as few as
+  // possible (a block looks its page up once)
+  const int64_t pages = most_pages<PAGE>(s);
+  int64_t split = (kFill + pages - 1) / pages;
+  if (split > 2 * c.Hkv) split = 2 * c.Hkv;
+  const dim3 grid((unsigned)pages, (unsigned)split);
   if (append) kv8_append_kernel<T, D, PAGE><<<grid, UnitCfg<D, PAGE>::THREADS, 0, st>>>(c, s, rows, status);
   else kv8_read_kernel<T, D, PAGE><<<grid, UnitCfg<D, PAGE>::THREADS, 0, st>>>(c, s, rows, status);
   return cudaGetLastError();

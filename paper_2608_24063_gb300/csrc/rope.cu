@@ -29,14 +29,31 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeHeadLanes = 8;     // heads a block works on at once
 constexpr int kRopeBatch = 3;         // heads a thread has in flight
 
-__device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// Eight values as they lie in memory.
+template <typename T>
+struct Raw8 {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
   }
-}
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t x[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(x[i] << 16);
+        v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        v[4 * i] = __uint_as_float(w[i].x); v[4 * i + 1] = __uint_as_float(w[i].y);
+        v[4 * i + 2] = __uint_as_float(w[i].z); v[4 * i + 3] = __uint_as_float(w[i].w);
+      }
+    }
+  }
+};
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -45,14 +62,6 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
   return make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
 }
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
-  unpack8(*reinterpret_cast<const uint4*>(p), v);
-}
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
-  v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-  v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-}
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
   *reinterpret_cast<uint4*>(p) = pack8(v);
 }
@@ -76,11 +85,33 @@ __global__ void __launch_bounds__(kRopeThreads) mrope_kernel(const __grid_consta
   __shared__ float2 cs[RT][HALF];
   const int t = threadIdx.x;
   const int64_t r0 = (int64_t)blockIdx.x * RT;
+  const int slot = t % SLOTS, hl = t / SLOTS % kRopeHeadLanes, lr = t / (SLOTS * kRopeHeadLanes);
+  const int64_t row = r0 + lr;
+  const bool turns = slot < a.half / 8;
+  // element offsets of the slot's two 8-value runs within a head
+  const int o0 = turns && !ADJ ? slot * 8 : slot * 16;
+  const int o1 = turns && !ADJ ? a.half + slot * 8 : slot * 16 + 8;
+  const int H = row < a.n_rows ? a.Hq + a.Hkv : 0, step = gridDim.y * kRopeHeadLanes;
+  Raw8<T> x[kRopeBatch], y[kRopeBatch];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int n = 0; n < kRopeBatch; ++n) {
+      const int h = h0 + n * step;
+      if (h < H) {
+        const T* src = (h < a.Hq ? q + row * a.q_stride + (int64_t)h * D
+                                 : k + row * a.k_stride + (int64_t)(h - a.Hq) * D);
+        x[n].load(src + o0);
+        y[n].load(src + o1);
+      }
+    }
+  };
+  int h0 = blockIdx.y * kRopeHeadLanes + hl;
+  load(h0);                                         // in flight while the angles are computed
   {
     const int i = t % HALF;
-    const int64_t row = r0 + t / HALF;
-    if (i < a.half && row < a.n_rows) {
-      const int32_t pos = __ldg(a.positions + (int64_t)a.axis[i] * a.n_rows + row);
+    const int64_t ar = r0 + t / HALF;
+    if (i < a.half && ar < a.n_rows) {
+      const int32_t pos = __ldg(a.positions + (int64_t)a.axis[i] * a.n_rows + ar);
       const uint64_t phase = (uint64_t)(int64_t)pos * a.freq[i];
       const float turn = (float)(int32_t)(phase >> 32) * 0x1p-31f;    // half turns in [-1, 1)
       float s, c;
@@ -89,10 +120,6 @@ __global__ void __launch_bounds__(kRopeThreads) mrope_kernel(const __grid_consta
     }
   }
   __syncthreads();
-  const int slot = t % SLOTS, hl = t / SLOTS % kRopeHeadLanes, lr = t / (SLOTS * kRopeHeadLanes);
-  const int64_t row = r0 + lr;
-  if (row >= a.n_rows) return;
-  const bool turns = slot < a.half / 8;
   float c[8], s[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -100,55 +127,43 @@ __global__ void __launch_bounds__(kRopeThreads) mrope_kernel(const __grid_consta
     c[i] = v.x;
     s[i] = v.y;
   }
-  // element offsets of the slot's two 8-value runs within a head
-  const int o0 = turns && !ADJ ? slot * 8 : slot * 16;
-  const int o1 = turns && !ADJ ? a.half + slot * 8 : slot * 16 + 8;
   // kBatch heads at a time, all loads before the first store: the output may
   // be the input, so the compiler would not move a load over a store by itself
-  const int H = a.Hq + a.Hkv, step = gridDim.y * kRopeHeadLanes;
-  for (int h0 = blockIdx.y * kRopeHeadLanes + hl; h0 < H; h0 += kRopeBatch * step) {
-    float x[kRopeBatch][8], y[kRopeBatch][8];
-    T* dst[kRopeBatch];
+  for (; h0 < H; h0 += kRopeBatch * step) {
+    if (h0 != (int)(blockIdx.y * kRopeHeadLanes) + hl) load(h0);
 #pragma unroll
     for (int n = 0; n < kRopeBatch; ++n) {
       const int h = h0 + n * step;
-      if (h < H) {
-        const bool isq = h < a.Hq;
-        const T* src = isq ? q + row * a.q_stride + (int64_t)h * D : k + row * a.k_stride + (int64_t)(h - a.Hq) * D;
-        dst[n] = isq ? q_out + row * a.q_out_stride + (int64_t)h * D
-                     : k_out + row * a.k_out_stride + (int64_t)(h - a.Hq) * D;
-        load8(src + o0, x[n]);
-        load8(src + o1, y[n]);
-      }
-    }
-#pragma unroll
-    for (int n = 0; n < kRopeBatch; ++n) {
-      if (h0 + n * step >= H) break;
-      float u[8], v[8];
+      if (h >= H) break;
+      T* dst = h < a.Hq ? q_out + row * a.q_out_stride + (int64_t)h * D
+                        : k_out + row * a.k_out_stride + (int64_t)(h - a.Hq) * D;
+      float xa[8], ya[8], u[8], v[8];
+      x[n].get(xa);
+      y[n].get(ya);
       if (!turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          u[i] = x[n][i];
-          v[i] = y[n][i];
+          u[i] = xa[i];
+          v[i] = ya[i];
         }
       } else if (ADJ) {
         // pairs (2i, 2i + 1): x holds pairs 0..3 of the slot, y pairs 4..7
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          u[2 * i] = x[n][2 * i] * c[i] - x[n][2 * i + 1] * s[i];
-          u[2 * i + 1] = x[n][2 * i + 1] * c[i] + x[n][2 * i] * s[i];
-          v[2 * i] = y[n][2 * i] * c[4 + i] - y[n][2 * i + 1] * s[4 + i];
-          v[2 * i + 1] = y[n][2 * i + 1] * c[4 + i] + y[n][2 * i] * s[4 + i];
+          u[2 * i] = xa[2 * i] * c[i] - xa[2 * i + 1] * s[i];
+          u[2 * i + 1] = xa[2 * i + 1] * c[i] + xa[2 * i] * s[i];
+          v[2 * i] = ya[2 * i] * c[4 + i] - ya[2 * i + 1] * s[4 + i];
+          v[2 * i + 1] = ya[2 * i + 1] * c[4 + i] + ya[2 * i] * s[4 + i];
         }
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          u[i] = x[n][i] * c[i] - y[n][i] * s[i];
-          v[i] = y[n][i] * c[i] + x[n][i] * s[i];
+          u[i] = xa[i] * c[i] - ya[i] * s[i];
+          v[i] = ya[i] * c[i] + xa[i] * s[i];
         }
       }
-      store8(dst[n] + o0, u);
-      store8(dst[n] + o1, v);
+      store8(dst + o0, u);
+      store8(dst + o1, v);
     }
   }
 }
