@@ -91,6 +91,8 @@ struct UnitCfg {
   static_assert(NV * THREADS == VECS, "whole vectors");
 };
 
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+
 // Sixteen values as they lie in memory.
 template <typename T>
 struct Raw16 {
@@ -118,6 +120,38 @@ struct Raw16 {
       }
     }
   }
+  // the largest magnitude as the bits of an fp32 number; at least infinity's
+  // where a value is infinite or NaN
+  __device__ __forceinline__ uint32_t largest() const {
+    if constexpr (sizeof(T) == 2) {
+      __nv_bfloat162 m = __float2bfloat162_rn(0.f);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&x[k])));
+      }
+      const uint32_t b = *reinterpret_cast<const uint32_t*>(&m);
+      return max(b << 16, b & 0xffff0000u);
+    } else {
+      uint32_t m = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        m = max(m, max(w[i].x & 0x7fffffffu, w[i].y & 0x7fffffffu));
+        m = max(m, max(w[i].z & 0x7fffffffu, w[i].w & 0x7fffffffu));
+      }
+      return m;
+    }
+  }
+  // the same over the finite values alone
+  __device__ __forceinline__ uint32_t largest_finite() const {
+    float v[16], m = 0.f;
+    get(v);
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (finite(v[k])) m = fmaxf(m, fabsf(v[k]));
+    return __float_as_uint(m);
+  }
 };
 __device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&v)[16]) {
   uint32_t w[8];
@@ -135,9 +169,8 @@ __device__ __forceinline__ void store16(float* p, const float (&v)[16]) {
     *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
 }
 
-__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
-
-// Sixteen values times `inv` as codes; what is not finite becomes NaN.
+// Sixteen values times `inv` as codes; with CHECK what is not finite becomes NaN.
+template <bool CHECK>
 __device__ __forceinline__ uint4 encode16(const float (&v)[16], float inv) {
   uint32_t w[4];
 #pragma unroll
@@ -146,7 +179,7 @@ __device__ __forceinline__ uint4 encode16(const float (&v)[16], float inv) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float y = v[4 * i + k];
-      x[k] = finite(y) ? y * inv : __uint_as_float(0x7fffffffu);
+      x[k] = !CHECK || finite(y) ? y * inv : __uint_as_float(0x7fffffffu);
     }
     w[i] = f32x2_to_e4m3x2(x[0], x[1]) | f32x2_to_e4m3x2(x[2], x[3]) << 16;
   }
@@ -194,7 +227,7 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_append_kernel(
     const __grid_constant__ vc_kv8 c, const __grid_constant__ vc_kv8_step s, const __grid_constant__ Kv8Rows rows,
     int32_t* status) {
   using C = UnitCfg<D, PAGE>;
-  __shared__ float red[2][C::THREADS / 32];
+  __shared__ uint32_t red[2][C::THREADS / 32];
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   PageJob job;
   if (!find_job<PAGE>(c, s, status, job)) return;
@@ -212,9 +245,9 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_append_kernel(
       if (slot >= a && slot < b) next[i].load(src + (int64_t)slot * rstep + part * 16);
     }
   };
-  int u = blockIdx.y;
+  int u = blockIdx.y, turn = 0;
   load(u);
-  for (int turn = 0; u < 2 * c.Hkv; u += gridDim.y, turn ^= 1) {
+  for (; u < 2 * c.Hkv; u += gridDim.y) {
     const bool isv = u >= c.Hkv;
     const int g = isv ? u - c.Hkv : u;
     float* scale = (isv ? c.V_scale : c.K_scale) + (int64_t)job.p * c.Hkv + g;
@@ -224,24 +257,35 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_append_kernel(
 #pragma unroll
     for (int i = 0; i < C::NV; ++i) cur[i] = next[i];
     if (u + (int)gridDim.y < 2 * c.Hkv) load(u + gridDim.y);
-    float amax = 0.f;
+    // the block's largest magnitude; with a value that is not finite among them,
+    // once more over the finite ones
+    auto block_max = [&](uint32_t m) {
+      m = __reduce_max_sync(0xffffffffu, m);
+      if (lane == 0) red[turn][warp] = m;
+      turn ^= 1;
+      __syncthreads();                          // (the other row is read before the next barrier)
+#pragma unroll
+      for (int k = 0; k < C::THREADS / 32; ++k) m = max(m, red[turn ^ 1][k]);
+      return m;
+    };
+    uint32_t m = 0u;
 #pragma unroll
     for (int i = 0; i < C::NV; ++i) {
       const int slot = (t + i * C::THREADS) / C::VPR;
-      if (slot >= a && slot < b) {
-        float v[16];
-        cur[i].get(v);
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-          if (finite(v[k])) amax = fmaxf(amax, fabsf(v[k]));
-      }
+      if (slot >= a && slot < b) m = max(m, cur[i].largest());
     }
-    // (non-negative numbers order like their bits)
-    amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
-    if (lane == 0) red[turn][warp] = amax;
-    __syncthreads();                            // the other turn's row is read before the next barrier
+    m = block_max(m);
+    const bool all_finite = m < 0x7f800000u;
+    if (!all_finite) {
+      m = 0u;
 #pragma unroll
-    for (int w = 0; w < C::THREADS / 32; ++w) amax = fmaxf(amax, red[turn][w]);
+      for (int i = 0; i < C::NV; ++i) {
+        const int slot = (t + i * C::THREADS) / C::VPR;
+        if (slot >= a && slot < b) m = max(m, cur[i].largest_finite());
+      }
+      m = block_max(m);
+    }
+    const float amax = __uint_as_float(m);
     const float now = fmaxf(old, pow2_scale(amax));
     const float inv = pow2_inverse(now);
 #pragma unroll
@@ -250,7 +294,8 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_append_kernel(
       if (slot >= a && slot < b) {
         float v[16];
         cur[i].get(v);
-        *reinterpret_cast<uint4*>(codes + (size_t)vec * 16) = encode16(v, inv);
+        *reinterpret_cast<uint4*>(codes + (size_t)vec * 16) =
+            all_finite ? encode16<false>(v, inv) : encode16<true>(v, inv);
       }
     }
     if (now > old) {
@@ -262,7 +307,7 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS) kv8_append_kernel(
         decode16(*w, y);
 #pragma unroll
         for (int k = 0; k < 16; ++k) y[k] *= old;
-        *w = encode16(y, inv);
+        *w = encode16<true>(y, inv);
       }
     }
     if (t == 0) *scale = now;

@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeHeadLanes = 8;     // heads a block works on at once
-constexpr int kRopeBatch = 3;         // heads a thread has in flight
+constexpr int kRopeBatch = 2;         // heads a thread has in flight
 
 // Eight values as they lie in memory.
 template <typename T>
