@@ -190,7 +190,7 @@ struct Kv8AttnArgs {
 };
 constexpr int kKv8MaxCtas = 160;       // blocks of an attention launch at most (152 SMs, rounded up)
 int kv8_sm_count();                    // SMs of the current device, at most kKv8MaxCtas
-int kv8_attn_rows_mma();               // rows a tile of the two attention kernels
+int kv8_attn_rows_mma();               // most rows a unit of the two attention kernels
 int kv8_attn_rows_tc();
 cudaError_t launch_kv8_attn_mma(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8AttnArgs& a,
                                 cudaStream_t st);

@@ -169,8 +169,9 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
                            !valid_stride(q_stride, (int64_t)Hq * cache->d, dtype)))
     return VC_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return VC_ERR_INVALID_ARG;
-  // the attention's line of key tiles: a block's share is counted in 31 bits
-  const int64_t row_tiles = (int64_t)step->n_rows * (Hq / cache->Hkv) / kv8_attn_rows_mma() + step->n_req;
+  // the attention's line of key tiles (units of 8 rows at least): a block's
+  // share is counted in 31 bits
+  const int64_t row_tiles = (int64_t)step->n_rows * (Hq / cache->Hkv) / 8 + step->n_req;
   if (row_tiles * cache->Hkv > ((int64_t)1 << 37) / (((int64_t)step->max_pages * cache->page + 127) / 128))
     return VC_ERR_UNSUPPORTED;
   const bool tc = dtype == VC_BF16 && many_rows(step->n_rows, step->n_req, Hq, cache->Hkv);

@@ -3,21 +3,23 @@
 //     out[rho] = sum_t p_t V[t] / sum_t p_t,  p_t = 2^(c q[rho] . K[t] - m),
 // c = scale * log2(e), over the pages of one request and KV head.
 //
-// Reads d bytes of K and of V a token for at most 16 query rows: bound by the
+// Reads d bytes of K and of V a token for 8 or 16 query rows: bound by the
 // codes' bytes as long as expanding them stays cheap.  One persistent block
 // per SM takes an equal share of the line of key tiles (kv8_sched.cuh); a
 // producer warp brings 128-token tiles into a shared-memory ring by TMA (one
-// box a page: the page's rows of one head are contiguous), eight warps take
-// 16 tokens of a tile each.
+// box a page: the page's rows of one head are contiguous); the other warps
+// take the tiles' 16-token chunks in turn, each with its own running maximum,
+// sum and output, added up at a segment's end.
 //
-// Products are m16n8k16 with the query rows as M, fp16 operands and fp32 sums:
-// an e4m3 code is exactly an fp16 number, so codes are expanded to fp16 in
-// registers (two a conversion) and never written anywhere.  The order of the
-// contracted index is free, so a thread's 16-byte read of a K row serves four
-// k-steps of QK: thread column tig holds dimensions tig * D/4 ... of its row.
-// For PV the columns (output dimensions) are permuted the same way: a thread
-// reads 16 bytes of the rows of its four tokens, pairs them with byte
-// permutations and converts.  Accumulators of QK are the A operand of PV.
+// Products are m16n8k16 with 16 tokens (QK) or 16 output dimensions (PV) as M
+// and 8 query rows as N, fp16 operands and fp32 sums: an e4m3 code is exactly an
+// fp16 number, so codes are expanded to fp16 in registers (two a conversion) and
+// never written anywhere.  The order of the contracted index is free, so a
+// thread's 16-byte read of a K row serves four k-steps of QK: thread column tig
+// holds dimensions tig * D/4 ... of its row.  For PV the order of the output
+// dimensions is free: a thread reads 16 bytes of the rows of its four tokens,
+// pairs them with byte permutations and converts.  QK leaves probabilities as
+// (token, query); movmatrix turns them into PV's (query, token).
 //
 // Numbers: a query row is divided by the power of two below its largest
 // magnitude, which makes fp16 hold bf16 values exactly (down to 2^-14 of that
@@ -44,27 +46,35 @@ namespace {
 
 using namespace kv8;
 
-constexpr int kWarps = 8;                       // consumer warps
-constexpr int kThreads = 32 * (kWarps + 1);     // and the producer
-constexpr int kKT = 128;                        // tokens of a tile, 16 a warp
-constexpr int kMT = 16;                         // query rows of a unit
+constexpr int kKT = 128;                        // tokens of a tile
+constexpr int kChunks = kKT / 16;
 constexpr float kSlack = 2.f;
 constexpr float kPScale = 4096.f;               // 2^12
 
-template <int D>
+// T: query type, D: head dimension, NQ: groups of 8 query rows of a unit.
+// Warps: registers are granted to four warps at a time, so the consumers and
+// the producer fill 8, 12 or 16 warps of 255, 168 or 128 registers.
+template <typename T, int D, int NQ>
 struct Cfg {
+  static constexpr int NP = sizeof(T) == 4 ? 2 : 1;         // fp16 parts of a query value
+  static constexpr int MT = 8 * NQ;                         // query rows of a unit
+  static constexpr int REGS = D / 4 * NQ * (1 + 0.5 * NP);  // accumulators and query fragments
+  static constexpr int WARPS = REGS <= 64 ? 15 : REGS <= 96 ? 11 : 7;
+  static constexpr int THREADS = 32 * (WARPS + 1);
   static constexpr int STAGE = kKT * D;                     // bytes of K, and of V
   static constexpr int NST = D == 128 ? 5 : 10;
+  static constexpr int SLOTS = 32768 / (MT * D * 4);        // outputs that the merge buffer holds
 };
 
-template <int D>
+template <typename T, int D, int NQ>
 struct Smem {
-  uint8_t ring[Cfg<D>::NST][2][Cfg<D>::STAGE];              // [K, V]
-  float merge[4][kMT][D];
-  float scale[Cfg<D>::NST][2][kKT / 16];                    // [K, V][page of the tile]
-  float wm[kWarps][kMT], wl[kWarps][kMT], wv[kWarps];       // a segment's warp states
-  uint64_t full[Cfg<D>::NST], empty[Cfg<D>::NST];
-  int64_t scan[kThreads / 32];
+  using C = Cfg<T, D, NQ>;
+  uint8_t ring[C::NST][2][C::STAGE];                        // [K, V]
+  float merge[C::SLOTS][C::MT][D];
+  float scale[C::NST][2][kChunks];                          // [K, V][page of the tile]
+  float wm[C::WARPS][C::MT], wl[C::WARPS][C::MT];           // a segment's warp states
+  uint64_t full[C::NST], empty[C::NST];
+  int64_t scan[C::WARPS + 1];
   Share share;
   int abort, last;
 };
@@ -74,6 +84,12 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 8 x 8 transpose of 16-bit values: lane (gid, tig) gives row gid, columns 2 tig, + 1
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -94,25 +110,28 @@ __device__ __forceinline__ uint32_t piece(int r, int c) {
                   : (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
 }
 
-__device__ __forceinline__ float max_quad(float x) {
-  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-  return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+// over the eight lanes of a thread column (the tokens of a query)
+__device__ __forceinline__ float max_column(float x) {
+  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+  return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
 }
-__device__ __forceinline__ float sum_quad(float x) {
-  x += __shfl_xor_sync(0xffffffffu, x, 1);
-  return x + __shfl_xor_sync(0xffffffffu, x, 2);
+__device__ __forceinline__ float sum_column(float x) {
+  x += __shfl_xor_sync(0xffffffffu, x, 4);
+  x += __shfl_xor_sync(0xffffffffu, x, 8);
+  return x + __shfl_xor_sync(0xffffffffu, x, 16);
 }
 
-// The warp's query fragments (row gid and gid + 8 of the unit), normalised,
-// and each row's power of two.
-template <typename T, int D, int NP>
-__device__ __forceinline__ void load_q(const T* q, int64_t q_stride, const Unit& u, int G, int Hq,
-                                       uint32_t (&f)[NP][D / 16][4], float (&qs)[2]) {
+// The warp's query fragments, normalised (lane (gid, tig): row 8 n + gid of the
+// unit, dimensions tig * D/4 ...), and the power of two of rows 8 n + 2 tig, + 1.
+template <typename T, int D, int NQ, int NP>
+__device__ __forceinline__ void load_q(const T* q, int64_t q_stride, const Unit& u, int G,
+                                       uint32_t (&f)[NP][NQ][D / 16][2], float (&qs)[NQ][2]) {
   constexpr int DPT = D / 4;                    // dimensions of a thread
-  const int gid = (threadIdx.x & 31) >> 2, tig = threadIdx.x & 3;
+  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int rho = u.rt * kMT + gid + 8 * h;
+  for (int n = 0; n < NQ; ++n) {
+    const int rho = u.rt * 8 * NQ + 8 * n + gid;
     float x[DPT];
     float amax = 0.f;
     if (rho < u.q.m * G) {
@@ -129,48 +148,49 @@ __device__ __forceinline__ void load_q(const T* q, int64_t q_stride, const Unit&
 #pragma unroll
       for (int e = 0; e < DPT; ++e) x[e] = 0.f;
     }
-    amax = max_quad(amax);
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
     // zero, tiny or not finite rows as they are; 2^126 at most, whose inverse is normal
-    qs[h] = ex == 0u || ex == 0x7f800000u ? 1.f : __uint_as_float(min(ex, 253u << 23));
-    const float inv = pow2_inverse(qs[h]);
+    const float p2 = ex == 0u || ex == 0x7f800000u ? 1.f : __uint_as_float(min(ex, 253u << 23));
+    const float inv = pow2_inverse(p2);
+    qs[n][0] = __shfl_sync(0xffffffffu, p2, 8 * tig);
+    qs[n][1] = __shfl_sync(0xffffffffu, p2, 8 * tig + 4);
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      const float a0 = x[4 * s] * inv, a1 = x[4 * s + 1] * inv, a2 = x[4 * s + 2] * inv, a3 = x[4 * s + 3] * inv;
-      f[0][s][h] = pack_f16(a0, a1);            // k = 2 tig, + 1
-      f[0][s][2 + h] = pack_f16(a2, a3);        // k = 2 tig + 8, + 9
-      if (NP == 2) {
-        f[NP - 1][s][h] = pack_rest(a0, a1, f[0][s][h]);
-        f[NP - 1][s][2 + h] = pack_rest(a2, a3, f[0][s][2 + h]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {             // k = 2 tig, + 1 and 2 tig + 8, + 9
+        const float a0 = x[4 * s + 2 * h] * inv, a1 = x[4 * s + 2 * h + 1] * inv;
+        f[0][n][s][h] = pack_f16(a0, a1);
+        if (NP == 2) f[NP - 1][n][s][h] = pack_rest(a0, a1, f[0][n][s][h]);
       }
     }
   }
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK,
-                                                               const __grid_constant__ CUtensorMap tmV,
-                                                               const __grid_constant__ vc_kv8 c,
-                                                               const __grid_constant__ vc_kv8_step s,
-                                                               const __grid_constant__ Kv8AttnArgs a) {
-  using C = Cfg<D>;
-  constexpr int NP = sizeof(T) == 4 ? 2 : 1;    // fp16 parts of a query value and of a probability
+template <typename T, int D, int NQ>
+__global__ void __launch_bounds__(Cfg<T, D, NQ>::THREADS, 1)
+kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                const __grid_constant__ vc_kv8 c, const __grid_constant__ vc_kv8_step s,
+                const __grid_constant__ Kv8AttnArgs a) {
+  using C = Cfg<T, D, NQ>;
+  constexpr int NP = C::NP, MT = C::MT, NW = C::WARPS;
   constexpr int KS = D / 16;                    // k-steps of QK
-  constexpr int NT = D / 8;                     // output column tiles of PV
+  constexpr int NM = D / 16;                    // dimension tiles of PV
   extern __shared__ uint8_t smem_raw[];
-  Smem<D>& sm = *reinterpret_cast<Smem<D>*>(tc::align1024(smem_raw));
+  Smem<T, D, NQ>& sm = *reinterpret_cast<Smem<T, D, NQ>*>(tc::align1024(smem_raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = a.Hq / c.Hkv;
-  const Line<kMT, kKT> line{c.Hkv, G, c.page, a.causal};
+  const Line<MT, kKT> line{c.Hkv, G, c.page, a.causal};
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NST; ++i) {
-      tc::mbar_init(&sm.full[i], 1);
-      tc::mbar_init(&sm.empty[i], kWarps);
+      tc::mbar_init(&sm.full[i], 2);            // the copies' bytes, and the scales
+      tc::mbar_init(&sm.empty[i], kChunks);
     }
     sm.abort = 0;
     tc::fence_mbar_init();
   }
-  find_share<kThreads>(line, s, a.status, sm.share, sm.scan);     // ends with a barrier
+  find_share<C::THREADS>(line, s, a.status, sm.share, sm.scan);   // ends with a barrier
   const Share& sh = sm.share;
   if (sh.begin >= sh.end) return;
   volatile int* abort = &sm.abort;
@@ -180,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
   const int &t0 = wk.t0, &t1 = wk.t1;           // the segment's tiles of its unit
   int fill = 0;                                 // tiles so far (ring position)
 
-  if (warp == kWarps) {
+  if (warp == NW) {
     // ---- producer: lane -> (tile, page) of a batch of 32 pages; page numbers
     // and scales of the next batch load while this one's boxes are issued
     const int ppt = kKT / c.page, tpb = 32 / ppt;
@@ -212,12 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
             break;
           }
           const bool mine = bt == i;
-          if (mine) {
-            sm.scale[st][0][bp] = ks;
-            sm.scale[st][1][bp] = vs;
-          }
           const int pages = __popc(__ballot_sync(0xffffffffu, mine && live));
-          __syncwarp();
           if (lane == 0) tc::mbar_arrive_expect_tx(&sm.full[st], (uint32_t)pages * 2 * page_bytes);
           __syncwarp();
           if (mine && live) {
@@ -226,6 +241,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
             tc::tma_load_2d(sm.ring[st][0] + bp * page_bytes, &tmK, 0, row, &sm.full[st]);
             tc::tma_load_2d(sm.ring[st][1] + bp * page_bytes, &tmV, 0, row, &sm.full[st]);
           }
+          if (mine) {
+            sm.scale[st][0][bp] = ks;
+            sm.scale[st][1][bp] = vs;
+          }
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&sm.full[st]);
         }
         pid = npid;
         ks = nks;
@@ -240,110 +261,69 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
     return;
   }
 
-  // ---- consumers: warp w has tokens 16 w .. 16 w + 15 of every tile
+  // ---- consumers: chunk k of the share's tiles (16 tokens each) goes to warp k % NW
   const int gid = lane >> 2, tig = lane & 3;
-  const int wpage = 16 * warp / c.page;         // the page of the tile they lie in
+  int next = warp;                              // the warp's next chunk
   bool ok = true;
   do {
-    uint32_t qf[NP][KS][4];
-    float qs[2];
-    load_q<T, D, NP>(static_cast<const T*>(a.q), a.q_stride, u, G, a.Hq, qf, qs);
-    const float cs0 = a.scale_log2 * qs[0], cs1 = a.scale_log2 * qs[1];
-    // keys each row sees, and the fewest that any row of the unit sees
-    int lim0 = u.q.len, lim1 = u.q.len, lim_min = u.kend;
-    if (a.causal) {
-      const int base = u.q.len - u.q.m + 1, r0 = u.rt * kMT;
-      lim0 = base + (r0 + gid) / G;
-      lim1 = base + (r0 + gid + 8) / G;
-      lim_min = base + r0 / G;
-    }
-    lim0 = min(lim0, u.kend);
-    lim1 = min(lim1, u.kend);
-    float o[NT][4];
+    uint32_t qf[NP][NQ][KS][2];
+    float cs[NQ][2];
+    load_q<T, D, NQ, NP>(static_cast<const T*>(a.q), a.q_stride, u, G, qf, cs);
+    // keys that rows 8 n + 2 tig, + 1 see, and the fewest that any row of the unit sees
+    int lim[NQ][2], lim_min = u.kend;
+    const int base = u.q.len - u.q.m + 1, r0 = u.rt * MT;
+    if (a.causal) lim_min = base + r0 / G;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f, vref = 0.f;
-    for (int tile = t0; tile < t1; ++tile, ++fill) {
-      const int st = fill % C::NST;
-      ok = ok && tc::warp_wait(&sm.full[st], (fill / C::NST) & 1, abort);
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        cs[n][h] *= a.scale_log2;
+        lim[n][h] = a.causal ? min(u.kend, base + (r0 + 8 * n + 2 * tig + h) / G) : u.kend;
+      }
+    float o[NQ][NM][4];
+    float m[NQ][2], l[NQ][2], vref = 0.f;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+      for (int i = 0; i < NM; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+    }
+    for (const int stop = (fill + t1 - t0) * kChunks; next < stop; next += NW) {
+      const int f = next / kChunks, ck = next % kChunks, st = f % C::NST;
+      const int key0 = (t0 + f - fill) * kKT + 16 * ck;
+      ok = ok && tc::warp_wait(&sm.full[st], (f / C::NST) & 1, abort);
       if (!ok) continue;
-      const int key0 = tile * kKT + 16 * warp;
       if (key0 < u.kend) {
         const uint8_t* kt = sm.ring[st][0];
         const uint8_t* vt = sm.ring[st][1];
-        const float ksc = sm.scale[st][0][wpage], vsc = sm.scale[st][1][wpage];
-        // scores of keys key0 + gid (n = gid of tile 0) and + 8
-        float x[2][4];
+        const int pg = 16 * ck / c.page;
+        const float ksc = sm.scale[st][0][pg], vsc = sm.scale[st][1][pg];
+        // scores of tokens gid (x[.][0], [1]) and gid + 8, queries 2 tig and 2 tig + 1
+        float x[NQ][4];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const int row = 16 * warp + 8 * n + gid;
-          x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
+        for (int n = 0; n < NQ; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
 #pragma unroll
-          for (int h = 0; h < D / 64; ++h) {
-            const uint4 w = *reinterpret_cast<const uint4*>(kt + piece<D>(row, tig * (D / 64) + h));
-            const uint32_t b[4] = {w.x, w.y, w.z, w.w};
+        for (int h = 0; h < D / 64; ++h) {
+          const uint4 w0 = *reinterpret_cast<const uint4*>(kt + piece<D>(16 * ck + gid, tig * (D / 64) + h));
+          const uint4 w1 = *reinterpret_cast<const uint4*>(kt + piece<D>(16 * ck + gid + 8, tig * (D / 64) + h));
+          const uint32_t b0[4] = {w0.x, w0.y, w0.z, w0.w}, b1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t b0 = e4m3x2_to_f16x2(b[k]), b1 = e4m3x2_to_f16x2(b[k] >> 16);
-              mma_f16(x[n], qf[0][4 * h + k], b0, b1);
-              if (NP == 2) mma_f16(x[n], qf[NP - 1][4 * h + k], b0, b1);
-            }
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t ka[4] = {e4m3x2_to_f16x2(b0[k]), e4m3x2_to_f16x2(b1[k]), e4m3x2_to_f16x2(b0[k] >> 16),
+                                    e4m3x2_to_f16x2(b1[k] >> 16)};
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+              for (int p = 0; p < NP; ++p) mma_f16(x[n], ka, qf[p][n][4 * h + k][0], qf[p][n][4 * h + k][1]);
           }
         }
-        const float f0 = cs0 * ksc, f1 = cs1 * ksc;
-        const bool edge = key0 + 16 > lim_min;
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          x[n][0] *= f0; x[n][1] *= f0; x[n][2] *= f1; x[n][3] *= f1;
-          if (edge) {
-            const int key = key0 + 8 * n + 2 * tig;
-            if (key >= lim0) x[n][0] = -INFINITY;
-            if (key + 1 >= lim0) x[n][1] = -INFINITY;
-            if (key >= lim1) x[n][2] = -INFINITY;
-            if (key + 1 >= lim1) x[n][3] = -INFINITY;
-          }
-        }
-        const float t0m = max_quad(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1])));
-        const float t1m = max_quad(fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3])));
-        const bool up0 = t0m > m0 + kSlack, up1 = t1m > m1 + kSlack, upv = vsc > vref;
-        if (__any_sync(0xffffffffu, up0 || up1) || upv) {
-          // the references rise: what was summed is scaled down (0 stays 0)
-          float g0 = up0 ? tc::ex2(m0 - t0m) : 1.f, g1 = up1 ? tc::ex2(m1 - t1m) : 1.f;
-          if (up0) m0 = t0m;
-          if (up1) m1 = t1m;
-          l0 *= g0;
-          l1 *= g1;
-          if (upv) {
-            const float gv = vref * pow2_inverse(vsc);
-            vref = vsc;
-            g0 *= gv;
-            g1 *= gv;
-          }
-#pragma unroll
-          for (int i = 0; i < NT; ++i) { o[i][0] *= g0; o[i][1] *= g0; o[i][2] *= g1; o[i][3] *= g1; }
-        }
-        const float r0 = m0 == -INFINITY ? 0.f : m0, r1 = m1 == -INFINITY ? 0.f : m1;
-        const float pc = vsc * pow2_inverse(vref) * kPScale;
-        uint32_t pf[NP][4];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const float p0 = tc::ex2(x[n][0] - r0), p1 = tc::ex2(x[n][1] - r0);
-          const float p2 = tc::ex2(x[n][2] - r1), p3 = tc::ex2(x[n][3] - r1);
-          l0 += p0 + p1;
-          l1 += p2 + p3;
-          pf[0][2 * n] = pack_f16(p0 * pc, p1 * pc);
-          pf[0][2 * n + 1] = pack_f16(p2 * pc, p3 * pc);
-          if (NP == 2) {
-            pf[NP - 1][2 * n] = pack_rest(p0 * pc, p1 * pc, pf[0][2 * n]);
-            pf[NP - 1][2 * n + 1] = pack_rest(p2 * pc, p3 * pc, pf[0][2 * n + 1]);
-          }
-        }
-        // PV: tokens 2 tig, + 1 (b0) and 2 tig + 8, + 9 (b1), dimensions gid * D/8 ...
+        // the V rows of tokens 2 tig, + 1, 2 tig + 8, + 9 (their latency under the softmax)
         constexpr int WPT = D / 32;             // 4-byte words of a thread's row piece
         uint32_t w[4][WPT];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int row = 16 * warp + 2 * tig + (k & 1) + 8 * (k >> 1);
+          const int row = 16 * ck + 2 * tig + (k & 1) + 8 * (k >> 1);
           if constexpr (D == 128) {
             const uint4 y = *reinterpret_cast<const uint4*>(vt + piece<D>(row, gid));
             w[k][0] = y.x; w[k][1] = y.y; w[k][2] = y.z; w[k][3] = y.w;
@@ -351,166 +331,255 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(const __grid_cons
             const uint2 y = *reinterpret_cast<const uint2*>(vt + piece<D>(row, gid >> 1) + 8 * (gid & 1));
             w[k][0] = y.x; w[k][1] = y.y;
           }
-          if (edge && key0 - 16 * warp + row >= u.kend) {   // beyond the unit's keys: whatever is there
+        }
+        const bool edge = key0 + 16 > lim_min;
+        if (edge) {
 #pragma unroll
-            for (int e = 0; e < WPT; ++e) w[k][e] = 0u;
+          for (int k = 0; k < 4; ++k)
+            if (key0 + 2 * tig + (k & 1) + 8 * (k >> 1) >= u.kend) {   // beyond the unit's keys: whatever is there
+#pragma unroll
+              for (int e = 0; e < WPT; ++e) w[k][e] = 0u;
+            }
+        }
+        float top[NQ][2];
+        bool up = vsc > vref;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float fac = cs[n][h] * ksc;
+            x[n][h] *= fac;
+            x[n][2 + h] *= fac;
+            if (edge) {
+              if (key0 + gid >= lim[n][h]) x[n][h] = -INFINITY;
+              if (key0 + gid + 8 >= lim[n][h]) x[n][2 + h] = -INFINITY;
+            }
+            top[n][h] = max_column(fmaxf(x[n][h], x[n][2 + h]));
+            up = up || top[n][h] > m[n][h] + kSlack;
+          }
+        if (__any_sync(0xffffffffu, up)) {
+          // the references rise: what was summed is scaled down (0 stays 0)
+          const float gv = vsc > vref ? vref * pow2_inverse(vsc) : 1.f;
+          vref = fmaxf(vref, vsc);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) {
+            float g[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              g[h] = 1.f;
+              if (top[n][h] > m[n][h] + kSlack) {
+                g[h] = tc::ex2(m[n][h] - top[n][h]);
+                m[n][h] = top[n][h];
+                l[n][h] *= g[h];
+              }
+              g[h] *= gv;
+            }
+#pragma unroll
+            for (int i = 0; i < NM; ++i) {
+              o[n][i][0] *= g[0]; o[n][i][1] *= g[1]; o[n][i][2] *= g[0]; o[n][i][3] *= g[1];
+            }
           }
         }
+        const float pc = vsc * pow2_inverse(vref) * kPScale;
+        uint32_t pf[NP][NQ][2];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          const float r0m = m[n][0] == -INFINITY ? 0.f : m[n][0], r1m = m[n][1] == -INFINITY ? 0.f : m[n][1];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {         // token gid, gid + 8
+            const float p0 = tc::ex2(x[n][2 * h] - r0m), p1 = tc::ex2(x[n][2 * h + 1] - r1m);
+            l[n][0] += p0;
+            l[n][1] += p1;
+            const uint32_t hi = pack_f16(p0 * pc, p1 * pc);
+            pf[0][n][h] = transpose8(hi);
+            if (NP == 2) pf[NP - 1][n][h] = transpose8(pack_rest(p0 * pc, p1 * pc, hi));
+          }
+        }
+        // PV: dimensions gid * D/8 + 4 e + 2 k (row gid of the tile) and + 1 (row gid + 8)
 #pragma unroll
         for (int e = 0; e < WPT; ++e) {
-          const uint32_t lo0 = __byte_perm(w[0][e], w[1][e], 0x5140), hi0 = __byte_perm(w[0][e], w[1][e], 0x7362);
-          const uint32_t lo1 = __byte_perm(w[2][e], w[3][e], 0x5140), hi1 = __byte_perm(w[2][e], w[3][e], 0x7362);
+          const uint32_t lo[2] = {__byte_perm(w[0][e], w[1][e], 0x5140), __byte_perm(w[0][e], w[1][e], 0x7362)};
+          const uint32_t hi[2] = {__byte_perm(w[2][e], w[3][e], 0x5140), __byte_perm(w[2][e], w[3][e], 0x7362)};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t b0 = e4m3x2_to_f16x2((k < 2 ? lo0 : hi0) >> (16 * (k & 1)));
-            const uint32_t b1 = e4m3x2_to_f16x2((k < 2 ? lo1 : hi1) >> (16 * (k & 1)));
-            mma_f16(o[4 * e + k], pf[0], b0, b1);
-            if (NP == 2) mma_f16(o[4 * e + k], pf[NP - 1], b0, b1);
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t va[4] = {e4m3x2_to_f16x2(lo[k]), e4m3x2_to_f16x2(lo[k] >> 16), e4m3x2_to_f16x2(hi[k]),
+                                    e4m3x2_to_f16x2(hi[k] >> 16)};
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+              for (int p = 0; p < NP; ++p) mma_f16(o[n][2 * e + k], va, pf[p][n][0], pf[p][n][1]);
           }
         }
       }
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&sm.empty[st]);
     }
+    fill += t1 - t0;
     // ---- the segment's end: the warps' states are added up
-    l0 = sum_quad(l0);
-    l1 = sum_quad(l1);
-    if (tig == 0) {
-      sm.wm[warp][gid] = m0;
-      sm.wm[warp][gid + 8] = m1;
-      sm.wl[warp][gid] = l0;
-      sm.wl[warp][gid + 8] = l1;
-    }
-    if (tc::named_sync_any(1, 32 * kWarps, !ok)) break;     // some warp gave up: all stop
-    // as the last step has them: thread: row t / 16, dimensions (t % 16) * D/16 ...
-    // (read here, before the next barrier: a fast warp may overwrite them in
-    // the next segment).  A state without a maximum holds 0, or NaN.
-    const int row = threadIdx.x >> 4, part = threadIdx.x & 15;
-    float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm.wm[w][row]);
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float x = sm.wm[w][row];
-      L = fmaf(sm.wl[w][row], x == -INFINITY ? 1.f : tc::ex2(x - M), L);
-    }
-    float M0 = -INFINITY, M1 = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      M0 = fmaxf(M0, sm.wm[w][gid]);
-      M1 = fmaxf(M1, sm.wm[w][gid + 8]);
-    }
-    {
-      const float g0 = m0 == -INFINITY ? 0.f : tc::ex2(m0 - M0) * (vref / kPScale);
-      const float g1 = m1 == -INFINITY ? 0.f : tc::ex2(m1 - M1) * (vref / kPScale);
-#pragma unroll
-      for (int i = 0; i < NT; ++i) { o[i][0] *= g0; o[i][1] *= g0; o[i][2] *= g1; o[i][3] *= g1; }
-    }
-    // a thread's columns: dimensions tig * D/4 + (0 .. NT-1) from the even
-    // accumulator columns, + NT ... from the odd ones; 16-byte chunks XOR-permuted
-    constexpr int CPT = D / 16;                 // chunks of a thread and row
-    auto chunk = [](int row, int ch) { return ch ^ (ch / CPT * 2 + (row & 1)); };
-    float4* slot = reinterpret_cast<float4*>(&sm.merge[warp & 3][0][0]);
-    auto put = [&](bool add) {
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int row = gid + 8 * h;
-#pragma unroll
-        for (int e = 0; e < CPT; ++e) {
-          const int odd = e >= CPT / 2, i = 4 * (e - (odd ? CPT / 2 : 0));
-          float4* at = slot + row * (D / 4) + chunk(row, CPT * tig + e);
-          const int k = 2 * h + odd;
-          if (add) {
-            const float4 y = *at;
-            o[i][k] += y.x; o[i + 1][k] += y.y; o[i + 2][k] += y.z; o[i + 3][k] += y.w;
-          } else {
-            *at = make_float4(o[i][k], o[i + 1][k], o[i + 2][k], o[i + 3][k]);
-          }
+        l[n][h] = sum_column(l[n][h]);
+        if (gid == 0) {
+          sm.wm[warp][8 * n + 2 * tig + h] = m[n][h];
+          sm.wl[warp][8 * n + 2 * tig + h] = l[n][h];
         }
       }
-    };
-    if (warp >= 4) put(false);
-    tc::named_sync(1, 32 * kWarps);
-    if (warp < 4) {
-      put(true);
-      put(false);
-    }
-    tc::named_sync(1, 32 * kWarps);
-    const int rho = u.rt * kMT + row;
-    const bool real = rho < u.q.m * G;
-    constexpr int EPT = D / 16;
-    float y[EPT];
+    if (tc::named_sync_any(1, 32 * NW, !ok)) break;         // some warp gave up: all stop
+    // outputs in true units of the unit's largest maximum
 #pragma unroll
-    for (int e = 0; e < EPT; e += 4) {
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int n = 0; n < NQ; ++n) {
+      float g[2];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float4 z =
-            reinterpret_cast<const float4*>(&sm.merge[k][0][0])[row * (D / 4) + chunk(row, (part * EPT + e) / 4)];
-        v.x += z.x; v.y += z.y; v.z += z.z; v.w += z.w;
+      for (int h = 0; h < 2; ++h) {
+        float mm = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < NW; ++k) mm = fmaxf(mm, sm.wm[k][8 * n + 2 * tig + h]);
+        g[h] = m[n][h] == -INFINITY ? 0.f : tc::ex2(m[n][h] - mm) * (vref / kPScale);
       }
-      y[e] = v.x; y[e + 1] = v.y; y[e + 2] = v.z; y[e + 3] = v.w;
-    }
-    bool write = real;
-    if (!wk.whole()) {
-      // a piece of a unit: to the workspace; the unit's last piece to arrive adds them up
-      const int first = wk.first_block(sh), final = wk.last_block(sh);
-      const int64_t mine = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
-      float* po = a.part_o + (mine * kMT + row) * D + part * EPT;
 #pragma unroll
-      for (int e = 0; e < EPT; e += 4)
-        *reinterpret_cast<float4*>(po + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
-      if (part == 0) a.part_ml[mine * kMT + row] = make_float2(M, L);
+      for (int i = 0; i < NM; ++i) {
+        o[n][i][0] *= g[0]; o[n][i][1] *= g[1]; o[n][i][2] *= g[0]; o[n][i][3] *= g[1];
+      }
+    }
+    // A thread holds dimensions gid * D/8 ... of rows 8 n + 2 tig, + 1, as D/32
+    // 16-byte pieces each; pieces are XOR-permuted by the row.
+    auto spot = [](int row, int pc4) { return row * (D / 4) + (pc4 ^ ((row >> 1) & 3) * (D / 64)); };
+    auto put = [&](bool add) {
+      float4* slot = reinterpret_cast<float4*>(&sm.merge[warp % C::SLOTS][0][0]);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < D / 32; ++e) {
+            float4* at = slot + spot(8 * n + 2 * tig + h, gid * (D / 32) + e);
+            float (&y)[4] = o[n][2 * e], (&z)[4] = o[n][2 * e + 1];
+            if (add) {
+              const float4 v = *at;
+              y[h] += v.x; y[2 + h] += v.y; z[h] += v.z; z[2 + h] += v.w;
+            } else {
+              *at = make_float4(y[h], y[2 + h], z[h], z[2 + h]);
+            }
+          }
+    };
+    // groups of SLOTS warps, the last first: each adds the group after it
+    constexpr int GROUPS = (NW + C::SLOTS - 1) / C::SLOTS;
+#pragma unroll
+    for (int gi = GROUPS - 1; gi >= 0; --gi) {
+      if (warp / C::SLOTS == gi) {
+        if (gi < GROUPS - 1 && warp + C::SLOTS < NW) put(true);
+        put(false);
+      }
+      tc::named_sync(1, 32 * NW);
+    }
+    // items of four dimensions of a row; M and L of the row are read from the
+    // warps' states before the segment's last barrier lets them be overwritten
+    constexpr int ITEMS = MT * D / 4, IPT = (ITEMS + 32 * NW - 1) / (32 * NW);
+    float M[IPT], L[IPT];
+    float4 y[IPT];
+#pragma unroll
+    for (int k = 0; k < IPT; ++k) {
+      const int it = threadIdx.x + k * 32 * NW;
+      if (it >= ITEMS) break;
+      const int row = it / (D / 4);
+      M[k] = -INFINITY;
+      L[k] = 0.f;
+#pragma unroll
+      for (int w2 = 0; w2 < NW; ++w2) M[k] = fmaxf(M[k], sm.wm[w2][row]);
+      // (a state without a maximum holds 0, or NaN)
+#pragma unroll
+      for (int w2 = 0; w2 < NW; ++w2) {
+        const float z = sm.wm[w2][row];
+        L[k] = fmaf(sm.wl[w2][row], z == -INFINITY ? 1.f : tc::ex2(z - M[k]), L[k]);
+      }
+      y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int b = 0; b < (NW < C::SLOTS ? NW : C::SLOTS); ++b) {
+        const float4 z = reinterpret_cast<const float4*>(&sm.merge[b][0][0])[spot(row, it % (D / 4))];
+        y[k].x += z.x; y[k].y += z.y; y[k].z += z.z; y[k].w += z.w;
+      }
+    }
+    const bool whole = wk.whole();
+    bool write = true;
+    int first = 0, final = 0;
+    if (!whole) {
+      // a piece of a unit: to the workspace; the unit's last piece to arrive adds them up
+      first = wk.first_block(sh);
+      final = wk.last_block(sh);
+      const int64_t mine = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
+#pragma unroll
+      for (int k = 0; k < IPT; ++k) {
+        const int it = threadIdx.x + k * 32 * NW;
+        if (it >= ITEMS) break;
+        reinterpret_cast<float4*>(a.part_o + mine * MT * D)[it] = y[k];
+        if (it % (D / 4) == 0) a.part_ml[mine * MT + it / (D / 4)] = make_float2(M[k], L[k]);
+      }
       __threadfence();
-      tc::named_sync(1, 32 * kWarps);
+      tc::named_sync(1, 32 * NW);
       if (threadIdx.x == 0) {
         sm.last = atomicAdd(&a.arrivals[first], 1) == final - first;
         __threadfence();
       }
-      tc::named_sync(1, 32 * kWarps);
-      write = real && sm.last;
-      if (write) {
-        M = -INFINITY;
-        for (int b = first; b <= final; ++b)
-          M = fmaxf(M, __ldcg(&a.part_ml[(2 * (int64_t)b + (b == first ? 1 : 0)) * kMT + row]).x);
-        L = 0.f;
+    }
+    tc::named_sync(1, 32 * NW);                 // states and merge buffer are read: the next segment may write
+    if (!whole) write = sm.last;
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) y[e] = 0.f;
-#pragma unroll 4
-        for (int b = first; b <= final; ++b) {
-          const int64_t at = (2 * (int64_t)b + (b == first ? 1 : 0)) * kMT + row;
-          const float2 ml = __ldcg(&a.part_ml[at]);
-          const float w = ml.x == -INFINITY ? 1.f : tc::ex2(ml.x - M);
-          L = fmaf(ml.y, w, L);
+    for (int k = 0; k < IPT; ++k) {
+      const int it = threadIdx.x + k * 32 * NW;
+      if (it >= ITEMS) break;
+      const int row = it / (D / 4), rho = u.rt * MT + row;
+      if (!write || rho >= u.q.m * G) continue;
+      if (!whole) {
+        auto slot = [&](int b) { return 2 * (int64_t)b + (b == first ? 1 : 0); };
+        float mx = -INFINITY, lx = 0.f;
+        float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+        // four pieces' loads at a time; what was summed is scaled to a new maximum
+        for (int b0 = first; b0 <= final; b0 += 4) {
+          float2 ml[4];
+          float4 v[4];
 #pragma unroll
-          for (int e = 0; e < EPT; e += 4) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * D + part * EPT + e));
-            y[e] = fmaf(v.x, w, y[e]);
-            y[e + 1] = fmaf(v.y, w, y[e + 1]);
-            y[e + 2] = fmaf(v.z, w, y[e + 2]);
-            y[e + 3] = fmaf(v.w, w, y[e + 3]);
+          for (int b = 0; b < 4; ++b) {
+            ml[b] = make_float2(-INFINITY, 0.f);
+            v[b] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (b0 + b <= final) {
+              ml[b] = __ldcg(&a.part_ml[slot(b0 + b) * MT + row]);
+              v[b] = __ldcg(reinterpret_cast<const float4*>(a.part_o + slot(b0 + b) * MT * D) + it);
+            }
+          }
+          const float nm = fmaxf(mx, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+          const float g = mx == -INFINITY ? 1.f : tc::ex2(mx - nm);
+          mx = nm;
+          lx *= g;
+          z.x *= g; z.y *= g; z.z *= g; z.w *= g;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const float wt = ml[b].x == -INFINITY ? 1.f : tc::ex2(ml[b].x - nm);
+            lx = fmaf(ml[b].y, wt, lx);
+            z.x = fmaf(v[b].x, wt, z.x);
+            z.y = fmaf(v[b].y, wt, z.y);
+            z.z = fmaf(v[b].z, wt, z.z);
+            z.w = fmaf(v[b].w, wt, z.w);
           }
         }
+        M[k] = mx;
+        L[k] = lx;
+        y[k] = z;
       }
-    }
-    if (write) {
-      const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);      // no token: zeros; NaN stays
+      const float inv = L[k] > 0.f ? 1.f / L[k] : (L[k] == L[k] ? 0.f : L[k]);    // no token: zeros; NaN stays
       const int i = rho / G, j = rho - i * G;
       const int64_t at = (int64_t)(u.q.row0 + i) * a.Hq + u.g * G + j;
-      T* dst = static_cast<T*>(a.out) + at * D + part * EPT;
-#pragma unroll
-      for (int e = 0; e < EPT; e += 4) {
-        if constexpr (sizeof(T) == 4) {
-          *reinterpret_cast<float4*>(dst + e) =
-              make_float4(y[e] * inv, y[e + 1] * inv, y[e + 2] * inv, y[e + 3] * inv);
-        } else {
-          const __nv_bfloat162 b0 = __floats2bfloat162_rn(y[e] * inv, y[e + 1] * inv);
-          const __nv_bfloat162 b1 = __floats2bfloat162_rn(y[e + 2] * inv, y[e + 3] * inv);
-          *reinterpret_cast<uint2*>(dst + e) = make_uint2(*reinterpret_cast<const uint32_t*>(&b0),
-                                                          *reinterpret_cast<const uint32_t*>(&b1));
-        }
+      T* dst = static_cast<T*>(a.out) + at * D + it % (D / 4) * 4;
+      if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(dst) = make_float4(y[k].x * inv, y[k].y * inv, y[k].z * inv, y[k].w * inv);
+      } else {
+        const __nv_bfloat162 b0 = __floats2bfloat162_rn(y[k].x * inv, y[k].y * inv);
+        const __nv_bfloat162 b1 = __floats2bfloat162_rn(y[k].z * inv, y[k].w * inv);
+        *reinterpret_cast<uint2*>(dst) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
       }
-      if (a.lse && part == 0) a.lse[at] = L == 0.f ? -INFINITY : fmaf(M, 0.6931471805599453f, logf(L));
+      if (a.lse && it % (D / 4) == 0) a.lse[at] = L[k] == 0.f ? -INFINITY : fmaf(M[k], 0.6931471805599453f, logf(L[k]));
     }
   } while (wk.next(line, s, a.status));
   if (!ok && lane == 0) set_status(a.status, VC_ERR_DEVICE_TIMEOUT);
@@ -546,13 +615,15 @@ bool kv8_pool_map(CUtensorMap* m, const void* base, const vc_kv8& c) {
 
 namespace {
 
-template <typename T, int D>
+template <typename T, int D, int NQ>
 cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
-  constexpr size_t smem = sizeof(Smem<D>) + 1024;
+  using C = Cfg<T, D, NQ>;
+  constexpr size_t smem = sizeof(Smem<T, D, NQ>) + 1024;
+  static_assert(smem <= 232448, "shared memory of a block");
   static std::atomic<bool> attr{false};
   if (!attr.load(std::memory_order_relaxed)) {
-    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_kernel<T, D, NQ>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     attr.store(true, std::memory_order_relaxed);
   }
@@ -560,12 +631,20 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
   if (!kv8_pool_map(&mk, c.K_codes, c) || !kv8_pool_map(&mv, c.V_codes, c)) return cudaErrorInvalidValue;
   // no more blocks than the line can have tiles
   const int64_t G = a.Hq / c.Hkv;
-  const int64_t units = ((int64_t)s.n_rows * G / kMT + (s.n_req < s.n_rows ? s.n_req : s.n_rows)) * c.Hkv;
+  const int64_t units = ((int64_t)s.n_rows * G / C::MT + (s.n_req < s.n_rows ? s.n_req : s.n_rows)) * c.Hkv;
   const int64_t tiles = units * (((int64_t)s.max_pages * c.page + kKT - 1) / kKT);
   const int64_t sms = kv8_sm_count();
   ProfileScope ps("kv8_attn", st);
-  kv8_attn_kernel<T, D><<<(unsigned)(tiles < sms ? tiles : sms), kThreads, smem, st>>>(mk, mv, c, s, a);
+  kv8_attn_kernel<T, D, NQ><<<(unsigned)(tiles < sms ? tiles : sms), C::THREADS, smem, st>>>(mk, mv, c, s, a);
   return cudaGetLastError();
+}
+
+// Units of 8 query rows where the requests have no more on average (a decode
+// step of up to 8 query heads a KV head), else of 16.
+template <typename T, int D>
+cudaError_t launch_q(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
+  const int64_t rows = (int64_t)s.n_rows * (a.Hq / c.Hkv);
+  return rows <= 8 * (int64_t)s.n_req ? launch_t<T, D, 1>(c, s, a, st) : launch_t<T, D, 2>(c, s, a, st);
 }
 
 }  // namespace
@@ -582,13 +661,13 @@ int kv8_sm_count() {
   return n;
 }
 
-int kv8_attn_rows_mma() { return kMT; }
+int kv8_attn_rows_mma() { return 16; }
 
 cudaError_t launch_kv8_attn_mma(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8AttnArgs& a,
                                 cudaStream_t st) {
   if (dtype == VC_BF16)
-    return c.d == 128 ? launch_t<__nv_bfloat16, 128>(c, s, a, st) : launch_t<__nv_bfloat16, 64>(c, s, a, st);
-  return c.d == 128 ? launch_t<float, 128>(c, s, a, st) : launch_t<float, 64>(c, s, a, st);
+    return c.d == 128 ? launch_q<__nv_bfloat16, 128>(c, s, a, st) : launch_q<__nv_bfloat16, 64>(c, s, a, st);
+  return c.d == 128 ? launch_q<float, 128>(c, s, a, st) : launch_q<float, 64>(c, s, a, st);
 }
 
 }  // namespace vc
