@@ -72,7 +72,9 @@ struct Smem {
   uint8_t ring[C::NST][2][C::STAGE];                        // [K, V]
   float merge[C::SLOTS][C::MT][D];
   float scale[C::NST][2][kChunks];                          // [K, V][page of the tile]
-  float wm[C::WARPS][C::MT], wl[C::WARPS][C::MT];           // a segment's warp states
+  float wm[C::WARPS][C::MT], wl[C::WARPS][C::MT];           // a segment's warp states: maxima, sums
+  float wf[C::WARPS][C::MT];                                // and their factors
+  float2 ml[C::MT];                                         // the segment's maximum and sum of each row
   uint64_t full[C::NST], empty[C::NST];
   int64_t scan[C::WARPS + 1];
   Share share;
@@ -427,20 +429,31 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         }
       }
     if (tc::named_sync_any(1, 32 * NW, !ok)) break;         // some warp gave up: all stop
-    // outputs in true units of the unit's largest maximum
+    // row r's states are put together by warp r (and r + NW): lane k has warp k's
+    for (int row = warp; row < MT; row += NW) {
+      const float x = lane < NW ? sm.wm[lane][row] : -INFINITY;
+      const float y = lane < NW ? sm.wl[lane][row] : 0.f;
+      float mx = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      mx = max_column(mx);
+      // (a state without a maximum holds 0, or NaN)
+      const float f = x == -INFINITY ? 1.f : tc::ex2(x - mx);
+      float sum = y * f;
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      sum = sum_column(sum);
+      if (lane < NW) sm.wf[lane][row] = f;
+      if (lane == 0) sm.ml[row] = make_float2(mx, sum);
+    }
+    tc::named_sync(1, 32 * NW);
+    // outputs in true units of the row's maximum
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      float g[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float mm = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < NW; ++k) mm = fmaxf(mm, sm.wm[k][8 * n + 2 * tig + h]);
-        g[h] = m[n][h] == -INFINITY ? 0.f : tc::ex2(m[n][h] - mm) * (vref / kPScale);
-      }
+      const float2 f = *reinterpret_cast<const float2*>(&sm.wf[warp][8 * n + 2 * tig]);
+      const float g0 = f.x * (vref / kPScale), g1 = f.y * (vref / kPScale);
 #pragma unroll
       for (int i = 0; i < NM; ++i) {
-        o[n][i][0] *= g[0]; o[n][i][1] *= g[1]; o[n][i][2] *= g[0]; o[n][i][3] *= g[1];
+        o[n][i][0] *= g0; o[n][i][1] *= g1; o[n][i][2] *= g0; o[n][i][3] *= g1;
       }
     }
     // A thread holds dimensions gid * D/8 ... of rows 8 n + 2 tig, + 1, as D/32
@@ -474,8 +487,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       }
       tc::named_sync(1, 32 * NW);
     }
-    // items of four dimensions of a row; M and L of the row are read from the
-    // warps' states before the segment's last barrier lets them be overwritten
+    // items of four dimensions of a row
     constexpr int ITEMS = MT * D / 4, IPT = (ITEMS + 32 * NW - 1) / (32 * NW);
     float M[IPT], L[IPT];
     float4 y[IPT];
@@ -484,16 +496,8 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       const int it = threadIdx.x + k * 32 * NW;
       if (it >= ITEMS) break;
       const int row = it / (D / 4);
-      M[k] = -INFINITY;
-      L[k] = 0.f;
-#pragma unroll
-      for (int w2 = 0; w2 < NW; ++w2) M[k] = fmaxf(M[k], sm.wm[w2][row]);
-      // (a state without a maximum holds 0, or NaN)
-#pragma unroll
-      for (int w2 = 0; w2 < NW; ++w2) {
-        const float z = sm.wm[w2][row];
-        L[k] = fmaf(sm.wl[w2][row], z == -INFINITY ? 1.f : tc::ex2(z - M[k]), L[k]);
-      }
+      M[k] = sm.ml[row].x;
+      L[k] = sm.ml[row].y;
       y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int b = 0; b < (NW < C::SLOTS ? NW : C::SLOTS); ++b) {
@@ -516,9 +520,10 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         reinterpret_cast<float4*>(a.part_o + mine * MT * D)[it] = y[k];
         if (it % (D / 4) == 0) a.part_ml[mine * MT + it / (D / 4)] = make_float2(M[k], L[k]);
       }
-      __threadfence();
+      // thread 0's fence after the barrier covers the whole block's stores
       tc::named_sync(1, 32 * NW);
       if (threadIdx.x == 0) {
+        __threadfence();
         sm.last = atomicAdd(&a.arrivals[first], 1) == final - first;
         __threadfence();
       }
@@ -536,6 +541,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         float mx = -INFINITY, lx = 0.f;
         float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
         // four pieces' loads at a time; what was summed is scaled to a new maximum
+#pragma unroll 1
         for (int b0 = first; b0 <= final; b0 += 4) {
           float2 ml[4];
           float4 v[4];

@@ -624,9 +624,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       } else {
         a.part_ml[(mine * 2 + X) * 128 + row] = make_float2(m, l);
         const int first = w.first_block(sh), final = w.last_block(sh);
-        __threadfence();
+        // one thread's fence after the barrier covers the warpgroup's stores
         named_sync(1 + X, 128);
         if (row == 0) {
+          __threadfence();
           sm.last[X] = atomicAdd(&a.arrivals[2 * first + X], 1) == final - first;
           __threadfence();
         }

@@ -5,8 +5,8 @@
 // group at the request's row i) over the tiles of KT keys that any of them
 // sees, at least one tile.  The units' tiles, in order of request, row tile,
 // KV head, form one line of T tiles; block i of N takes tiles
-// [i T / N, (i + 1) T / N) of it.  So every block has the same number of
-// tiles whatever the lengths are, a long unit is split over blocks, and a
+// of it in turn, T / N of them and one more for the first T % N blocks.  So every
+// block has the same number of tiles whatever the lengths are, a long unit is split over blocks, and a
 // block's piece of a unit is a "segment".  A segment that is not a whole unit
 // leaves its partial sums in the workspace (at most two a block: the end of
 // the unit before, the start of the one after); the block that finishes a
@@ -73,16 +73,26 @@ struct Line {
   }
 };
 
+// a / b, in 32 bits where that holds it (the division of a few microseconds'
+// call is felt)
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // A block's share of the line.
 struct Share {
-  int64_t T, begin, end;   // tiles of the line, the block's range
-  int N;                   // blocks with a share (every one has at least a tile)
+  int64_t begin, end;      // the block's range of the line
+  int64_t per;             // tiles of a block, T / N
+  int more;                // the first T % N blocks have one more
   int64_t tile0;           // the first unit's first tile on the line
   Unit u;                  // the first unit
-};
 
-// Blocks of the line that hold its tile x.
-__device__ __forceinline__ int block_of(int64_t x, int64_t T, int N) { return (int)(((x + 1) * N - 1) / T); }
+  // the block that holds tile x of the line
+  __device__ __forceinline__ int block_of(int64_t x) const {
+    const int64_t y = x - more * (per + 1);
+    return y < 0 ? (int)divide(x, per + 1) : more + (int)divide(y, per);
+  }
+};
 
 // A role's walk over the block's segments.  Positions are relative to the
 // share's begin (a share is below 2^31 tiles: the host refuses longer lines).
@@ -112,74 +122,109 @@ struct Walk {
     return true;
   }
   // the blocks that hold the unit's first and last tile
-  __device__ __forceinline__ int first_block(const Share& sh) const { return block_of(sh.begin + rel, sh.T, sh.N); }
+  __device__ __forceinline__ int first_block(const Share& sh) const { return sh.block_of(sh.begin + rel); }
   __device__ __forceinline__ int last_block(const Share& sh) const {
-    return block_of(sh.begin + rel + u.tiles - 1, sh.T, sh.N);
+    return sh.block_of(sh.begin + rel + u.tiles - 1);
   }
 };
 
+__device__ __forceinline__ int64_t scan_warp(int64_t x) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if ((int)(threadIdx.x & 31) >= o) x += y;
+  }
+  return x;
+}
+
+// The block's range of a line of T tiles.
+__device__ __forceinline__ void set_range(Share& sh, int64_t T) {
+  const int N = (int)(T < (int64_t)gridDim.x ? T : (int64_t)gridDim.x);
+  const int i = blockIdx.x;
+  sh.per = N > 0 ? divide(T, N) : 0;
+  sh.more = (int)(T - sh.per * N);
+  sh.begin = i < N ? i * sh.per + min(i, sh.more) : 0;
+  sh.end = i < N ? sh.begin + sh.per + (i < sh.more ? 1 : 0) : 0;
+}
+
+// Finds the tile `begin` within request r, whose first tile is `at`.
+template <int MT, int KT>
+__device__ __forceinline__ void set_first(const Line<MT, KT>& line, Share& sh, int64_t begin, int64_t at, int r,
+                                          const Req8& q) {
+  Unit u;
+  u.r = r;
+  u.rt = 0;
+  u.q = q;
+  for (;; ++u.rt) {
+    line.set(u);
+    const int64_t row = (int64_t)line.Hkv * u.tiles;
+    if (begin < at + row) break;
+    at += row;
+  }
+  u.g = (int)divide(begin - at, u.tiles);
+  sh.tile0 = at + (int64_t)u.g * u.tiles;
+  sh.u = u;
+}
+
 // Computes the block's share with all of the block's NT threads; `sh` and
-// `scan` (one word a warp) are in shared memory.  Each thread counts the
-// tiles of consecutive requests, a scan places them on the line, and the
-// thread whose requests hold the first tile of the share looks it up.
+// `scan` (one word a warp) are in shared memory.  Up to 32 requests: one warp,
+// a request a lane.  More: each thread counts the tiles of consecutive
+// requests, and a scan over the block places them on the line.  The thread
+// whose requests hold the first tile of the share looks it up.  Ends with a
+// barrier.
 template <int NT, int MT, int KT>
 __device__ __forceinline__ void find_share(const Line<MT, KT>& line, const vc_kv8_step& s, int32_t* status,
                                            Share& sh, int64_t* scan) {
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  if (s.n_req <= 32) {
+    if (warp == 0) {
+      const Req8 q = lane < s.n_req ? load_req(s, line.page, lane, status) : Req8{0, 0, 0};
+      const int64_t w = line.Hkv * line.request_tiles(q);
+      const int64_t upto = scan_warp(w);
+      Share x;
+      set_range(x, __shfl_sync(0xffffffffu, upto, 31));
+      if (lane == 0) {
+        sh.begin = x.begin;
+        sh.end = x.end;
+        sh.per = x.per;
+        sh.more = x.more;
+      }
+      if (x.begin < x.end && x.begin >= upto - w && x.begin < upto) set_first(line, sh, x.begin, upto - w, lane, q);
+    }
+    __syncthreads();
+    return;
+  }
   const int per = (s.n_req + NT - 1) / NT;
   const int ra = min(t * per, s.n_req), rb = min(ra + per, s.n_req);
   int64_t sum = 0;
-  for (int r = ra; r < rb; ++r) {
-    const Req8 q = load_req(s, line.page, r, status);
-    sum += line.Hkv * line.request_tiles(q);
-  }
-  int64_t incl = sum;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += x;
-  }
-  if (lane == 31) scan[warp] = incl;
+  for (int r = ra; r < rb; ++r) sum += line.Hkv * line.request_tiles(load_req(s, line.page, r, status));
+  const int64_t upto = scan_warp(sum);
+  if (lane == 31) scan[warp] = upto;
   __syncthreads();
   int64_t T = 0, before = 0;
-#pragma unroll
   for (int w = 0; w < NT / 32; ++w) {
     if (w < warp) before += scan[w];
     T += scan[w];
   }
-  const int N = (int)(T < (int64_t)gridDim.x ? T : (int64_t)gridDim.x);
-  const int64_t begin = N > 0 && (int)blockIdx.x < N ? blockIdx.x * T / N : 0;
-  const int64_t end = N > 0 && (int)blockIdx.x < N ? (blockIdx.x + 1) * T / N : 0;
-  int64_t at = before + incl - sum;
-  if (begin < end && begin >= at && begin < at + sum) {
+  Share x;
+  set_range(x, T);
+  if (t == 0) {
+    sh.begin = x.begin;
+    sh.end = x.end;
+    sh.per = x.per;
+    sh.more = x.more;
+  }
+  int64_t at = before + upto - sum;
+  if (x.begin < x.end && x.begin >= at && x.begin < at + sum) {
     for (int r = ra; r < rb; ++r) {
       const Req8 q = load_req(s, line.page, r, status);
       const int64_t w = line.Hkv * line.request_tiles(q);
-      if (begin >= at + w) {
-        at += w;
-        continue;
+      if (x.begin < at + w) {
+        set_first(line, sh, x.begin, at, r, q);
+        break;
       }
-      Unit u;
-      u.r = r;
-      u.rt = 0;
-      u.q = q;
-      for (;; ++u.rt) {
-        line.set(u);
-        const int64_t row = (int64_t)line.Hkv * u.tiles;
-        if (begin < at + row) break;
-        at += row;
-      }
-      u.g = (int)((begin - at) / u.tiles);
-      sh.tile0 = at + (int64_t)u.g * u.tiles;
-      sh.u = u;
-      break;
+      at += w;
     }
-  }
-  if (t == 0) {
-    sh.T = T;
-    sh.begin = begin;
-    sh.end = end;
-    sh.N = N;
   }
   __syncthreads();
 }
