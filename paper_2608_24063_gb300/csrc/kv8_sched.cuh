@@ -11,6 +11,11 @@
 // leaves its partial sums in the workspace (at most two a block: the end of
 // the unit before, the start of the one after); the block that finishes a
 // unit's last segment adds them up in order.  Lengths are read on the device.
+//
+// Where the units are no more than the blocks (few requests), a segment's end
+// costs as much as several tiles, so no block takes two: every unit gets whole
+// blocks, ceil(tiles / per) of them with the least `per` that the blocks allow
+// (24 units of 6 to 25 tiles on 152 blocks: 20.8 -> 15.2 us against the line).
 #pragma once
 
 #include <cuda.h>
@@ -86,6 +91,7 @@ struct Share {
   int more;                // the first T % N blocks have one more
   int64_t tile0;           // the first unit's first tile on the line
   Unit u;                  // the first unit
+  int pieces, piece;       // above 0: the block has this piece of that unit and no more
 
   // the block that holds tile x of the line
   __device__ __forceinline__ int block_of(int64_t x) const {
@@ -104,6 +110,13 @@ struct Walk {
 
   __device__ __forceinline__ void start(const Share& sh) {
     u = sh.u;
+    if (sh.pieces > 0) {
+      rel = 0;
+      t0 = u.tiles * sh.piece / sh.pieces;
+      t1 = u.tiles * (sh.piece + 1) / sh.pieces;
+      left = t1 - t0;
+      return;
+    }
     left = (int)(sh.end - sh.begin);
     rel = (int)(sh.tile0 - sh.begin);
     t0 = -rel;
@@ -122,16 +135,19 @@ struct Walk {
     return true;
   }
   // the blocks that hold the unit's first and last tile
-  __device__ __forceinline__ int first_block(const Share& sh) const { return sh.block_of(sh.begin + rel); }
+  __device__ __forceinline__ int first_block(const Share& sh) const {
+    return sh.pieces > 0 ? (int)blockIdx.x - sh.piece : sh.block_of(sh.begin + rel);
+  }
   __device__ __forceinline__ int last_block(const Share& sh) const {
-    return sh.block_of(sh.begin + rel + u.tiles - 1);
+    return sh.pieces > 0 ? (int)blockIdx.x - sh.piece + sh.pieces - 1 : sh.block_of(sh.begin + rel + u.tiles - 1);
   }
 };
 
-__device__ __forceinline__ int64_t scan_warp(int64_t x) {
+template <typename Int>
+__device__ __forceinline__ Int scan_warp(Int x) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+    const Int y = __shfl_up_sync(0xffffffffu, x, o);
     if ((int)(threadIdx.x & 31) >= o) x += y;
   }
   return x;
@@ -179,17 +195,57 @@ __device__ __forceinline__ void find_share(const Line<MT, KT>& line, const vc_kv
   if (s.n_req <= 32) {
     if (warp == 0) {
       const Req8 q = lane < s.n_req ? load_req(s, line.page, lane, status) : Req8{0, 0, 0};
-      const int64_t w = line.Hkv * line.request_tiles(q);
-      const int64_t upto = scan_warp(w);
-      Share x;
-      set_range(x, __shfl_sync(0xffffffffu, upto, 31));
-      if (lane == 0) {
-        sh.begin = x.begin;
-        sh.end = x.end;
-        sh.per = x.per;
-        sh.more = x.more;
+      const int N = gridDim.x, rts = line.row_tiles(q);
+      // (at most 32 (N + 1) if none is over N: no overflow)
+      const int units = __reduce_add_sync(0xffffffffu, min(rts, N + 1) * min(line.Hkv, N + 1));
+      if (units <= N) {
+        // pieces of at most `per` tiles; a unit has at most 2^23 tiles, N units fewer than 2^31
+        int w = 0;
+        for (int rt = 0; rt < rts; ++rt) w += line.Hkv * line.tiles(line.keys(q, rt));
+        int per = (__reduce_add_sync(0xffffffffu, w) + N - 1) / N, mine, before;
+        for (;;) {
+          mine = 0;
+          for (int rt = 0; rt < rts; ++rt) mine += line.Hkv * ((line.tiles(line.keys(q, rt)) + per - 1) / per);
+          before = scan_warp(mine) - mine;
+          if (__shfl_sync(0xffffffffu, before + mine, 31) <= N) break;
+          per += per / 8 + 1;
+        }
+        const int i = blockIdx.x;
+        if (lane == 31) {
+          sh.begin = 0;
+          sh.end = i < before + mine ? 1 : 0;   // whether there is anything to do
+        }
+        if (i >= before && i < before + mine) {
+          Unit u;
+          u.r = lane;
+          u.rt = 0;
+          u.q = q;
+          int at = i - before, k;               // the place among the request's blocks
+          for (;; ++u.rt) {
+            line.set(u);
+            k = (u.tiles + per - 1) / per;
+            if (at < line.Hkv * k) break;
+            at -= line.Hkv * k;
+          }
+          u.g = at / k;
+          sh.u = u;
+          sh.pieces = k;
+          sh.piece = at - u.g * k;
+        }
+      } else {
+        const int64_t w = line.Hkv * line.request_tiles(q);
+        const int64_t upto = scan_warp(w);
+        Share x;
+        set_range(x, __shfl_sync(0xffffffffu, upto, 31));
+        if (lane == 0) {
+          sh.begin = x.begin;
+          sh.end = x.end;
+          sh.per = x.per;
+          sh.more = x.more;
+          sh.pieces = 0;
+        }
+        if (x.begin < x.end && x.begin >= upto - w && x.begin < upto) set_first(line, sh, x.begin, upto - w, lane, q);
       }
-      if (x.begin < x.end && x.begin >= upto - w && x.begin < upto) set_first(line, sh, x.begin, upto - w, lane, q);
     }
     __syncthreads();
     return;
@@ -213,6 +269,7 @@ __device__ __forceinline__ void find_share(const Line<MT, KT>& line, const vc_kv
     sh.end = x.end;
     sh.per = x.per;
     sh.more = x.more;
+    sh.pieces = 0;
   }
   int64_t at = before + upto - sum;
   if (x.begin < x.end && x.begin >= at && x.begin < at + sum) {
