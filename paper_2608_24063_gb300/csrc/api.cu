@@ -701,6 +701,18 @@ int prunekv_get_status(const void* ws, void* stream) {
   if (cudaMemcpyAsync(&s, ws, sizeof(s), cudaMemcpyDeviceToHost, st) != cudaSuccess)
     return VC_ERR_CUDA;
   if (cudaStreamSynchronize(st) != cudaSuccess) return VC_ERR_CUDA;
+  if (s == kStatusPerBlock) {
+    // the call's blocks stored their own words: the first that is not VC_OK
+    int32_t n = 0, blocks[kKv8MaxCtas];
+    const uint8_t* w = static_cast<const uint8_t*>(ws);
+    if (cudaMemcpyAsync(&n, w + sizeof(s), sizeof(n), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaMemcpyAsync(blocks, w + kAlign, sizeof(blocks), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess)
+      return VC_ERR_CUDA;
+    for (int i = 0; i < n && i < kKv8MaxCtas; ++i)
+      if (blocks[i] != VC_OK) return blocks[i];
+    return VC_OK;
+  }
   return s;
 }
 

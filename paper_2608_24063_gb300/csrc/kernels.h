@@ -162,10 +162,16 @@ struct RopeArgs {
 cudaError_t launch_mrope(const RopeArgs& a, int dtype, int d, bool adjacent, const void* q, void* q_out,
                          const void* k, void* k_out, cudaStream_t st);
 
-// 8-bit paged cache (kv8.cu, kv8_attn.cu).  The device arrays of vc_kv8 and
-// vc_kv8_step are checked as they are read: lengths are clamped to the block
-// table, requests whose rows lie outside [0, n_rows] and pages outside
-// [0, n_pages) are skipped, and the status word gets VC_ERR_DEVICE_INDEX.
+// 8-bit paged cache (kv8.cu, kv8_attn.cu, kv8_attn_tc.cu).  The device arrays
+// of vc_kv8 and vc_kv8_step are checked as they are read: lengths are clamped to
+// the block table, requests whose rows lie outside [0, n_rows] and pages outside
+// [0, n_pages) are skipped, and the call's status becomes VC_ERR_DEVICE_INDEX.
+//
+// A call's status is not cleared beforehand (a memset costs a call of a few
+// microseconds 4 us).  Append and read: their block 0 checks all that the call
+// reads and stores the status.  Attention: every block stores its own, and the
+// status word says so (kStatusPerBlock); prunekv_get_status looks at them all.
+constexpr int32_t kStatusPerBlock = 0x4b385042;   // word 1: how many blocks, words at byte 256: theirs
 struct Kv8Rows {                       // rows of append's inputs and read's outputs
   void* K;
   void* V;
@@ -183,8 +189,10 @@ struct Kv8AttnArgs {
   float* lse;                          // [n_rows][Hq] or NULL
   int32_t Hq, causal;
   float scale_log2;                    // logit scale * log2(e)
-  int32_t* status;
-  int32_t* arrivals;                   // [2 kKv8MaxCtas], zeroed before the launch
+  int32_t* status;                     // status word, block count
+  int32_t* block_status;               // [kKv8MaxCtas]
+  uint64_t token;                      // the call's own number: a flag that equals it is set
+  uint64_t* flags;                     // [2 kKv8MaxCtas][row tiles]: the piece is in the workspace
   float2* part_ml;                     // [2 kKv8MaxCtas][rows a tile]: (max, sum), log2 units
   float* part_o;                       // [2 kKv8MaxCtas][rows a tile][d]
 };

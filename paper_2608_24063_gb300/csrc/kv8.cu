@@ -201,6 +201,36 @@ __device__ __forceinline__ void decode16(const uint4& c, float (&v)[16]) {
   }
 }
 
+// Block 0 checks every request and every page that the step touches, and stores
+// the call's status; the other blocks skip what is wrong silently.  A thread
+// takes a request; those that touch more than two pages are then looked at by
+// the whole warp.
+template <int PAGE>
+__device__ __forceinline__ void check_step(const vc_kv8& c, const vc_kv8_step& s, int32_t* status) {
+  __shared__ int32_t err;
+  if (threadIdx.x == 0) err = VC_OK;
+  __syncthreads();
+  const int lane = threadIdx.x & 31;
+  for (int r0 = (int)threadIdx.x - lane; r0 < s.n_req; r0 += blockDim.x) {
+    const int r = r0 + lane;
+    int j0 = 0, cnt = 0;
+    if (r < s.n_req) {
+      const Req8 q = load_req(s, PAGE, r, &err);
+      const int lo = max(q.len - q.m, 0);
+      j0 = lo / PAGE;
+      cnt = q.len > lo ? (q.len - 1) / PAGE - j0 + 1 : 0;
+      for (int k = 0; k < min(cnt, 2); ++k) load_page(s, c.n_pages, r, j0 + k, &err);
+    }
+    for (uint32_t many = __ballot_sync(0xffffffffu, cnt > 2); many; many &= many - 1) {
+      const int src = __ffs(many) - 1;
+      const int first = __shfl_sync(0xffffffffu, j0, src), n = __shfl_sync(0xffffffffu, cnt, src);
+      for (int k = 2 + lane; k < n; k += 32) load_page(s, c.n_pages, r0 + src, first + k, &err);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) *status = err;
+}
+
 // A block's page: the touch, the page and the slots [a, b) of the step's tokens;
 // false where there is nothing to do.  All threads of the block call it.
 struct PageJob {
@@ -209,12 +239,16 @@ struct PageJob {
 };
 template <int PAGE>
 __device__ __forceinline__ bool find_job(const vc_kv8& c, const vc_kv8_step& s, int32_t* status, PageJob& job) {
+  if (blockIdx.x == 0) {
+    if (blockIdx.y == 0) check_step<PAGE>(c, s, status);
+    return false;
+  }
   __shared__ PageJob sj;
   if (threadIdx.x < 32) {
     Touch x = {};
-    const bool ok = find_touch<PAGE>(s, (int)blockIdx.x, status, x);
+    const bool ok = find_touch<PAGE>(s, (int)blockIdx.x - 1, nullptr, x);
     if (threadIdx.x == 0) {
-      sj.p = ok ? load_page(s, c.n_pages, x.r, x.j, status) : -1;
+      sj.p = ok ? load_page(s, c.n_pages, x.r, x.j, nullptr) : -1;
       sj.a = max(x.first - x.j * PAGE, 0);
       sj.b = min(x.len - x.j * PAGE, PAGE);
       sj.row = (int64_t)x.row0 + (x.j * PAGE - x.first);
@@ -383,7 +417,7 @@ cudaError_t launch_t(bool append, const vc_kv8& c, const vc_kv8_step& s, const K
   const int64_t pages = most_pages<PAGE>(s);
   int64_t split = (kFill + pages - 1) / pages;
   if (split > 2 * c.Hkv) split = 2 * c.Hkv;
-  const dim3 grid((unsigned)pages, (unsigned)split);
+  const dim3 grid((unsigned)pages + 1, (unsigned)split);
   if (append) kv8_append_kernel<T, D, PAGE><<<grid, UnitCfg<D, PAGE>::THREADS, 0, st>>>(c, s, rows, status);
   else kv8_read_kernel<T, D, PAGE><<<grid, UnitCfg<D, PAGE>::THREADS, 0, st>>>(c, s, rows, status);
   return cudaGetLastError();
@@ -402,8 +436,7 @@ cudaError_t launch_p(bool append, const vc_kv8& c, const vc_kv8_step& s, const K
 
 cudaError_t launch(bool append, const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8Rows& rows,
                    int32_t* status, cudaStream_t st) {
-  cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int32_t), st);
-  if (e != cudaSuccess || s.n_rows == 0) return e;
+  if (s.n_rows == 0) return cudaMemsetAsync(status, 0, sizeof(int32_t), st);
   if (dtype == VC_BF16)
     return c.d == 128 ? launch_p<__nv_bfloat16, 128>(append, c, s, rows, status, st)
                       : launch_p<__nv_bfloat16, 64>(append, c, s, rows, status, st);

@@ -16,6 +16,7 @@ struct Req8 {
 
 // Reads and checks request r.  A length outside the block table is clamped, a
 // request whose rows do not lie in order in [0, n_rows] counts as empty.
+// `status` is any word (here as below; NULL: what is wrong is skipped silently).
 __device__ __forceinline__ Req8 load_req(const vc_kv8_step& s, int page, int r, int32_t* status) {
   Req8 q;
   q.row0 = __ldg(s.row_start + r);
@@ -23,12 +24,12 @@ __device__ __forceinline__ Req8 load_req(const vc_kv8_step& s, int page, int r, 
   q.len = __ldg(s.seq_lens + r);
   q.m = next - q.row0;
   if (q.row0 < 0 || next < q.row0 || next > s.n_rows) {
-    set_status(status, VC_ERR_DEVICE_INDEX);
+    if (status) set_status(status, VC_ERR_DEVICE_INDEX);
     q.row0 = q.m = 0;
   }
   const int cap = s.max_pages * page;
   if (q.len < 0 || q.len > cap) {
-    set_status(status, VC_ERR_DEVICE_INDEX);
+    if (status) set_status(status, VC_ERR_DEVICE_INDEX);
     q.len = min(max(q.len, 0), cap);
   }
   return q;
@@ -38,7 +39,7 @@ __device__ __forceinline__ Req8 load_req(const vc_kv8_step& s, int page, int r, 
 __device__ __forceinline__ int load_page(const vc_kv8_step& s, int n_pages, int r, int j, int32_t* status) {
   const int p = __ldg(s.block_table + (int64_t)r * s.max_pages + j);
   if (p >= 0 && p < n_pages) return p;
-  set_status(status, VC_ERR_DEVICE_INDEX);
+  if (status) set_status(status, VC_ERR_DEVICE_INDEX);
   return -1;
 }
 

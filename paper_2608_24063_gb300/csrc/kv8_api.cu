@@ -2,6 +2,9 @@
 // (include/viscache.h): argument checks, workspace layout, launches.
 #include <math.h>
 
+#include <atomic>
+#include <chrono>
+
 #include "api_util.h"
 #include "kernels.h"
 
@@ -32,21 +35,35 @@ bool valid_stride(int64_t stride, int64_t least, int dtype) {
   return stride >= least && stride % (dtype == VC_BF16 ? 8 : 4) == 0 && stride < (int64_t)1 << 40;
 }
 
-// Workspace: status word (256 bytes), arrival counters, partial (max, sum)
-// and outputs of the attention's split units.
+// Workspace: status word and block count (256 bytes), the blocks' status
+// words, flags, (max, sum) and outputs of the attention's split units.
 struct Kv8Ws {
-  size_t o_arr = 0, o_ml = 0, o_o = 0, total = 0;
+  size_t o_blocks = 0, o_flags = 0, o_ml = 0, o_o = 0, total = 0;
 };
 Kv8Ws kv8_ws(bool tc, int d) {
   Arena a;
   Kv8Ws w;
   a.take(kAlign);
   const size_t rows = (size_t)2 * kKv8MaxCtas * (tc ? kv8_attn_rows_tc() : kv8_attn_rows_mma());
-  w.o_arr = a.take(sizeof(int32_t) * 2 * kKv8MaxCtas);
+  w.o_blocks = a.take(sizeof(int32_t) * kKv8MaxCtas);      // at byte 256: prunekv_get_status reads it there
+  w.o_flags = a.take(sizeof(uint64_t) * 2 * kKv8MaxCtas * 2);
   w.o_ml = a.take(sizeof(float2) * rows);
   w.o_o = a.take(sizeof(float) * rows * d);
   w.total = a.off;
   return w;
+}
+
+// A number of its own for every call, spread over 64 bits so that what happens
+// to be in a workspace is none of them: a counter from a point that differs
+// between processes, through the SplitMix64 finaliser.
+uint64_t next_token() {
+  static std::atomic<uint64_t> count{(uint64_t)std::chrono::steady_clock::now().time_since_epoch().count() ^
+                                     (uint64_t)std::chrono::system_clock::now().time_since_epoch().count() << 20};
+  uint64_t z = count.fetch_add(0x9E3779B97F4A7C15ull, std::memory_order_relaxed);
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  z ^= z >> 31;
+  return z ? z : 1;
 }
 
 // Whether a call runs on tcgen05: bf16 rows, at least kTcRows packed rows of a
@@ -180,9 +197,7 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
   if (wc != VC_OK) return wc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   uint8_t* base = static_cast<uint8_t*>(ws);
-  // status word and arrival counters
-  if (cudaMemsetAsync(base, 0, w.o_ml, st) != cudaSuccess) return VC_ERR_CUDA;
-  if (step->n_rows == 0) return VC_OK;
+  if (step->n_rows == 0) return cuda_status(cudaMemsetAsync(base, 0, sizeof(int32_t), st));
   Kv8AttnArgs a = {};
   a.q = q;
   a.q_stride = q_stride;
@@ -192,7 +207,9 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
   a.causal = causal != 0;
   a.scale_log2 = (scale == 0.f ? 1.0f / sqrtf((float)cache->d) : scale) * kLog2e;
   a.status = reinterpret_cast<int32_t*>(base);
-  a.arrivals = reinterpret_cast<int32_t*>(base + w.o_arr);
+  a.block_status = reinterpret_cast<int32_t*>(base + w.o_blocks);
+  a.token = next_token();
+  a.flags = reinterpret_cast<uint64_t*>(base + w.o_flags);
   a.part_ml = reinterpret_cast<float2*>(base + w.o_ml);
   a.part_o = reinterpret_cast<float*>(base + w.o_o);
   return cuda_status(tc ? launch_kv8_attn_tc(*cache, *step, a, st)

@@ -79,6 +79,7 @@ struct Smem {
   int64_t scan[C::WARPS + 1];
   Share share;
   int abort, last;
+  int32_t err;                                              // the block's status
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -190,11 +191,17 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       tc::mbar_init(&sm.empty[i], kChunks);
     }
     sm.abort = 0;
+    sm.err = VC_OK;
     tc::fence_mbar_init();
   }
-  find_share<C::THREADS>(line, s, a.status, sm.share, sm.scan);   // ends with a barrier
+  __syncthreads();
+  int32_t* const err = &sm.err;
+  find_share<C::THREADS>(line, s, err, sm.share, sm.scan);        // ends with a barrier
   const Share& sh = sm.share;
-  if (sh.begin >= sh.end) return;
+  if (sh.begin >= sh.end) {
+    if (threadIdx.x == 0) store_status(a, sm.err);
+    return;
+  }
   volatile int* abort = &sm.abort;
   Walk wk;
   wk.start(sh);
@@ -215,7 +222,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       auto look = [&](int first, int& pid, float& ks, float& vs, bool& live) {
         const int tile = first + bt, j = tile * ppt + bp;
         live = tile < t1 && j * c.page < u.kend;
-        pid = live ? load_page(s, c.n_pages, u.r, j, a.status) : -1;
+        pid = live ? load_page(s, c.n_pages, u.r, j, err) : -1;
         const int64_t at = (int64_t)max(pid, 0) * c.Hkv + u.g;
         ks = pid >= 0 ? __ldg(c.K_scale + at) : 0.f;
         vs = pid >= 0 ? __ldg(c.V_scale + at) : 0.f;
@@ -255,14 +262,12 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         vs = nvs;
         live = nlive;
       }
-    } while (ok && wk.next(line, s, a.status));
+    } while (ok && wk.next(line, s, err));
     // every copy has landed before the block may end
     __syncwarp();
     if (lane == 0)
       for (int i = max(0, fill - C::NST); i < fill; ++i) tc::drain_wait(&sm.full[i % C::NST], (i / C::NST) & 1);
-    return;
-  }
-
+  } else {
   // ---- consumers: chunk k of the share's tiles (16 tokens each) goes to warp k % NW
   const int gid = lane >> 2, tig = lane & 3;
   int next = warp;                              // the warp's next chunk
@@ -520,12 +525,10 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         reinterpret_cast<float4*>(a.part_o + mine * MT * D)[it] = y[k];
         if (it % (D / 4) == 0) a.part_ml[mine * MT + it / (D / 4)] = make_float2(M[k], L[k]);
       }
-      // thread 0's fence after the barrier covers the whole block's stores
       tc::named_sync(1, 32 * NW);
-      if (threadIdx.x == 0) {
-        __threadfence();
-        sm.last = atomicAdd(&a.arrivals[first], 1) == final - first;
-        __threadfence();
+      if (warp == 0) {
+        const bool all = piece_done(a.flags, 1, a.token, first, final);
+        if (lane == 0) sm.last = all;
       }
     }
     tc::named_sync(1, 32 * NW);                 // states and merge buffer are read: the next segment may write
@@ -587,8 +590,11 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       }
       if (a.lse && it % (D / 4) == 0) a.lse[at] = L[k] == 0.f ? -INFINITY : fmaf(M[k], 0.6931471805599453f, logf(L[k]));
     }
-  } while (wk.next(line, s, a.status));
-  if (!ok && lane == 0) set_status(a.status, VC_ERR_DEVICE_TIMEOUT);
+  } while (wk.next(line, s, err));
+  if (!ok && lane == 0) set_status(err, VC_ERR_DEVICE_TIMEOUT);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) store_status(a, sm.err);
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {

@@ -76,6 +76,7 @@ struct TcSmem {
   Share share;
   uint32_t tmem_base;
   int abort, last[2];
+  int32_t err;                                  // the block's status
 };
 
 // Instruction descriptors, D fp32: kind::f16 with A, B fp16 and B MN-major;
@@ -196,11 +197,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
     for (int i = 0; i < kRefs; ++i) mbar_init(&sm.ref_full[i], 1);
     mbar_init(&sm.done, 1);
     sm.abort = 0;
+    sm.err = VC_OK;
     fence_mbar_init();
   }
-  find_share<kTcThreads>(line, s, a.status, sm.share, sm.scan);   // ends with a barrier
+  __syncthreads();
+  int32_t* const err = &sm.err;
+  find_share<kTcThreads>(line, s, err, sm.share, sm.scan);        // ends with a barrier
   const Share& sh = sm.share;
-  if (sh.begin >= sh.end) return;
+  if (sh.begin >= sh.end) {
+    if (threadIdx.x == 0) store_status(a, sm.err);
+    return;
+  }
   if (warp == kIssueWarp) {
     tmem_alloc(&sm.tmem_base, 512);
     tmem_relinquish();
@@ -291,7 +298,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
         }
         if (ok) mma_commit(&sm.q_empty);
         ++seg;
-      } while (ok && w.next(line, s, a.status));
+      } while (ok && w.next(line, s, err));
       // every MMA is done before the block frees its tensor memory
       mma_commit(&sm.done);
       drain_wait(&sm.done, 0);
@@ -309,7 +316,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
         auto look = [&](int first, int& pid, float& ks, float& vs, bool& live) {
           const int tile = first + bt, j = tile * ppt + bp;
           live = tile < w.t1 && j * c.page < w.u.kend;
-          pid = live ? load_page(s, c.n_pages, w.u.r, j, a.status) : -1;
+          pid = live ? load_page(s, c.n_pages, w.u.r, j, err) : -1;
           const int64_t at = (int64_t)max(pid, 0) * c.Hkv + w.u.g;
           ks = pid >= 0 ? __ldg(c.K_scale + at) : 0.f;
           vs = pid >= 0 ? __ldg(c.V_scale + at) : 0.f;
@@ -360,7 +367,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
           vs = nvs;
           live = nlive;
         }
-      } while (ok && w.next(line, s, a.status));
+      } while (ok && w.next(line, s, err));
       // every copy has landed before the block may end
       __syncwarp();
       if (lane == 0) {
@@ -455,7 +462,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
         }
       }
       ++seg;
-    } while (ok && w.next(line, s, a.status));
+    } while (ok && w.next(line, s, err));
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     // ---- softmax of row tile X, one row a thread
@@ -624,12 +631,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       } else {
         a.part_ml[(mine * 2 + X) * 128 + row] = make_float2(m, l);
         const int first = w.first_block(sh), final = w.last_block(sh);
-        // one thread's fence after the barrier covers the warpgroup's stores
         named_sync(1 + X, 128);
-        if (row == 0) {
-          __threadfence();
-          sm.last[X] = atomicAdd(&a.arrivals[2 * first + X], 1) == final - first;
-          __threadfence();
+        if ((warp & 3) == 0) {
+          const bool all = piece_done(a.flags + X, 2, a.token, first, final);
+          if (lane == 0) sm.last[X] = all;
         }
         named_sync(1 + X, 128);
         if (sm.last[X] && real) {
@@ -665,8 +670,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
           put_lse(M, L);
         }
       }
-    } while (w.next(line, s, a.status));
-    if (!ok && lane == 0) set_status(a.status, VC_ERR_DEVICE_TIMEOUT);
+    } while (w.next(line, s, err));
+    if (!ok && lane == 0) set_status(err, VC_ERR_DEVICE_TIMEOUT);
   }
   __syncwarp();
   tc_fence_before();
@@ -675,7 +680,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
     tc_fence_after();
     tmem_dealloc(tbase, 512);
   }
-  if (threadIdx.x == 0 && sm.abort) set_status(a.status, VC_ERR_DEVICE_TIMEOUT);
+  if (threadIdx.x == 0) store_status(a, sm.abort ? VC_ERR_DEVICE_TIMEOUT : sm.err);
 }
 
 template <int D>

@@ -100,6 +100,40 @@ struct Share {
   }
 };
 
+// A split unit's pieces meet in the workspace without counters that would have
+// to be cleared: a block that has stored its piece sets the piece's flag to the
+// call's token, and then looks at the flags of all of the unit's pieces.  With a
+// sequentially consistent fence between the two, the last block to set one sees
+// them all; a block that sees them all adds the pieces up (two may: they write
+// the same values) and clears the flags, so that a replayed graph, whose token
+// is the same, finds them clear.  One warp calls it, after a barrier behind the
+// block's stores.
+__device__ __forceinline__ bool piece_done(uint64_t* flags, int step, uint64_t token, int first, int final) {
+  const int lane = threadIdx.x & 31, n = final - first + 1;
+  // block b's piece is its second (the unit's first) for b == first, else its first
+  auto flag = [&](int k) -> volatile uint64_t* { return flags + (2 * (first + k) + (k == 0 ? 1 : 0)) * step; };
+  __threadfence();
+  if (lane == 0) *flag((int)blockIdx.x - first) = token;
+  __threadfence();
+  __syncwarp();
+  bool all = true;
+  for (int k = lane; k < n; k += 32) all = all && *flag(k) == token;
+  all = __all_sync(0xffffffffu, all);
+  if (all)
+    for (int k = lane; k < n; k += 32) *flag(k) = 0;
+  __threadfence();
+  return all;
+}
+
+// The block's status, and that the status is the blocks'.
+__device__ __forceinline__ void store_status(const Kv8AttnArgs& a, int32_t err) {
+  a.block_status[blockIdx.x] = err;
+  if (blockIdx.x == 0) {
+    a.status[0] = kStatusPerBlock;
+    a.status[1] = (int32_t)gridDim.x;
+  }
+}
+
 // A role's walk over the block's segments.  Positions are relative to the
 // share's begin (a share is below 2^31 tiles: the host refuses longer lines).
 struct Walk {
