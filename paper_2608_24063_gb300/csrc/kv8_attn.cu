@@ -188,7 +188,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NST; ++i) {
       tc::mbar_init(&sm.full[i], 2);            // the copies' bytes, and the scales
-      tc::mbar_init(&sm.empty[i], kChunks);
+      tc::mbar_init(&sm.empty[i], NW);
     }
     sm.abort = 0;
     sm.err = VC_OK;
@@ -268,9 +268,12 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
     if (lane == 0)
       for (int i = max(0, fill - C::NST); i < fill; ++i) tc::drain_wait(&sm.full[i % C::NST], (i / C::NST) & 1);
   } else {
-  // ---- consumers: chunk k of the share's tiles (16 tokens each) goes to warp k % NW
+  // ---- consumers: chunk k of the share's tiles (16 tokens each) goes to warp k % NW.
+  // Every warp waits for every tile and frees it, whether it has a chunk of it
+  // or not: a warp that passed over a tile could find the tile's barrier a phase
+  // behind or two ahead of the one it waits for, and parities do not tell.
   const int gid = lane >> 2, tig = lane & 3;
-  int next = warp;                              // the warp's next chunk
+  int off = warp;                               // the warp's first chunk of the next tile (or past it)
   bool ok = true;
   do {
     uint32_t qf[NP][NQ][KS][2];
@@ -296,12 +299,14 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       m[n][0] = m[n][1] = -INFINITY;
       l[n][0] = l[n][1] = 0.f;
     }
-    for (const int stop = (fill + t1 - t0) * kChunks; next < stop; next += NW) {
-      const int f = next / kChunks, ck = next % kChunks, st = f % C::NST;
-      const int key0 = (t0 + f - fill) * kKT + 16 * ck;
-      ok = ok && tc::warp_wait(&sm.full[st], (f / C::NST) & 1, abort);
+    for (int tile = t0; tile < t1; ++tile, ++fill) {
+      const int st = fill % C::NST;
+      ok = ok && tc::warp_wait(&sm.full[st], (fill / C::NST) & 1, abort);
       if (!ok) continue;
-      if (key0 < u.kend) {
+      int ck = off;
+      for (; ck < kChunks; ck += NW) {
+        const int key0 = tile * kKT + 16 * ck;
+        if (key0 >= u.kend) continue;
         const uint8_t* kt = sm.ring[st][0];
         const uint8_t* vt = sm.ring[st][1];
         const int pg = 16 * ck / c.page;
@@ -387,6 +392,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             }
           }
         }
+        __syncwarp();                           // (the products take whole warps)
         const float pc = vsc * pow2_inverse(vref) * kPScale;
         uint32_t pf[NP][NQ][2];
 #pragma unroll
@@ -418,10 +424,10 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
           }
         }
       }
+      off = ck - kChunks;
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&sm.empty[st]);
     }
-    fill += t1 - t0;
     // ---- the segment's end: the warps' states are added up
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
@@ -433,6 +439,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
           sm.wl[warp][8 * n + 2 * tig + h] = l[n][h];
         }
       }
+    __syncwarp();                               // (the named barriers take whole warps)
     if (tc::named_sync_any(1, 32 * NW, !ok)) break;         // some warp gave up: all stop
     // row r's states are put together by warp r (and r + NW): lane k has warp k's
     for (int row = warp; row < MT; row += NW) {
@@ -450,6 +457,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       if (lane < NW) sm.wf[lane][row] = f;
       if (lane == 0) sm.ml[row] = make_float2(mx, sum);
     }
+    __syncwarp();
     tc::named_sync(1, 32 * NW);
     // outputs in true units of the row's maximum
 #pragma unroll
@@ -525,10 +533,12 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         reinterpret_cast<float4*>(a.part_o + mine * MT * D)[it] = y[k];
         if (it % (D / 4) == 0) a.part_ml[mine * MT + it / (D / 4)] = make_float2(M[k], L[k]);
       }
+      __syncwarp();
       tc::named_sync(1, 32 * NW);
       if (warp == 0) {
         const bool all = piece_done(a.flags, 1, a.token, first, final);
         if (lane == 0) sm.last = all;
+        __syncwarp();
       }
     }
     tc::named_sync(1, 32 * NW);                 // states and merge buffer are read: the next segment may write

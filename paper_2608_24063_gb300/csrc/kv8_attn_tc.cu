@@ -475,6 +475,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
     do {
       if (X == 1 && rows_of() <= 128) {         // no rows in this half
         t += w.t1 - w.t0;
+        ++seg;
         continue;
       }
       const int rho = w.u.rt * kTcMT + X * 128 + row;
@@ -484,7 +485,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       if (a.causal) lim = min(lim, w.u.q.len - w.u.q.m + 1 + qi);
       float m = -INFINITY, l = 0.f, cs = 0.f, vmax = 0.f;
       for (int j = w.t0; j < w.t1; ++j, ++t) {
-        ok = ok && warp_wait(&sm.ref_full[t % kRefs], (t / kRefs) & 1, abort) && warp_wait(&sm.s_full[X], ns & 1, abort);
+        // S first: then the scales' (and the query rows') barriers are at the phase
+        // asked for, also where this row tile sat out the segments before
+        ok = ok && warp_wait(&sm.s_full[X], ns & 1, abort) &&
+             warp_wait(&sm.ref_full[t % kRefs], (t / kRefs) & 1, abort) &&
+             (j > w.t0 || warp_wait(&sm.q_full, seg & 1, abort));
         if (!ok) continue;
         ++ns;
         tc_fence_after();
@@ -555,6 +560,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
             tmem_st16(o_col + p * 16, v);
           }
         }
+        __syncwarp();                           // (whole warps store P)
         // exponent of P's factor: 2^4 times the tile's share of vmax, not below 2^-26
         const int lc = vr > 0.f ? max(-30, (int)(__float_as_uint(vr) >> 23) - (int)(__float_as_uint(vmax) >> 23)) : -30;
         const float mm = (m == -INFINITY ? 0.f : m) - (float)(lc + kTcPExp);
@@ -584,6 +590,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       }
       ok = ok && warp_wait(&sm.o_full[X], no & 1, abort);
       ++no;
+      ++seg;
       if (named_sync_any(1 + X, 128, !ok)) break;
       tc_fence_after();
       // O in units of vmax * 2^-4
@@ -610,6 +617,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
 #pragma unroll 1
       for (int p = 0; p < D / 16; ++p) {
         uint32_t v[16];
+        __syncwarp();                           // (whole warps read tensor memory)
         tmem_ld16(o_col + p * 16, v);
         tmem_wait(v);
         float y[16];
@@ -631,10 +639,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       } else {
         a.part_ml[(mine * 2 + X) * 128 + row] = make_float2(m, l);
         const int first = w.first_block(sh), final = w.last_block(sh);
+        __syncwarp();                           // (the named barriers take whole warps)
         named_sync(1 + X, 128);
         if ((warp & 3) == 0) {
           const bool all = piece_done(a.flags + X, 2, a.token, first, final);
           if (lane == 0) sm.last[X] = all;
+          __syncwarp();
         }
         named_sync(1 + X, 128);
         if (sm.last[X] && real) {
