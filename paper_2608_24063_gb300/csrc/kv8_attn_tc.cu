@@ -19,7 +19,7 @@
 //   0-3, 4-7  softmax of row tile A, B: one thread a row
 //   8-11      converters: V codes from the staging buffer, e4m3 -> fp16, into
 //             128-byte-swizzled tiles, two stages; the unit's query rows too
-//   12        one thread issues the MMAs
+//   12        MMA issuer
 //   13        loader: page numbers, scales, a TMA box per page of K, a bulk
 //             copy per page of V
 // Tensor memory: S_A, S_B (128 columns each; P over the first 64 as fp16
@@ -107,31 +107,39 @@ __device__ __forceinline__ uint32_t code_piece(int r, int c) {
   return (uint32_t)(r * D + ch * 16 + (c & 1) * 8);
 }
 
-// Shared-memory descriptors are 64 bits of which only the low word, with the
-// address in units of 16 bytes, changes: the halves are joined at the MMA, so
-// the issuing thread keeps a few registers instead of a descriptor per operand.
+// The issuing warp runs as a whole and each instruction elects its lane: then
+// descriptors and addresses are warp-uniform values, and an MMA is issued every 7
+// to 15 clocks.  Issued from a branch of one thread, each takes 50 to 60 (and a
+// lone one is seen done after 274 clocks instead of 130): as long as it runs.
 //
-// D[tmem] (+)= A[smem] * B[smem]^T, issued by one thread.
-__device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi,
-                                            uint32_t idesc, uint32_t accumulate) {
+// D[tmem] (+)= A[smem] * B[smem]^T.
+__device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                            uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
-      "mov.b64 a, {%1, %3};\n\t"
-      "mov.b64 b, {%2, %3};\n\t"
-      "setp.ne.b32 p, %5, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %4, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
-__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi,
-                                           uint32_t idesc, uint32_t accumulate) {
+// D[tmem] (+)= A[tmem] * B[smem].
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                           uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
-      "mov.b64 b, {%2, %3};\n\t"
-      "setp.ne.b32 p, %5, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Arrive on bar once every MMA issued so far has completed (the same elected lane).
+__device__ __forceinline__ void mma_commit_elected(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
       : "memory");
 }
 
@@ -171,7 +179,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
                                                                     const __grid_constant__ Kv8AttnArgs a) {
   extern __shared__ uint8_t smem_raw[];
   TcSmem<D>& sm = *reinterpret_cast<TcSmem<D>*>(align1024(smem_raw));
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (warp: uniform)
   const int G = a.Hq / c.Hkv;
   const Line<kTcMT, kTcKT> line{c.Hkv, G, c.page, a.causal};
   if (threadIdx.x == 0) {
@@ -226,57 +234,57 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
   if (warp >= kConvWarp0 + kConvWarps) {
     // registers a thread: 128 at launch; 184 + 184 + 72 + 72 = 4 * 128
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == kIssueWarp && lane == 0) {
+    if (warp == kIssueWarp) {
       // ---- MMA issuer
       constexpr uint32_t id_s = idesc_e4m3(128, kTcKT), id_o = idesc_f16_bmn(128, D);
       bool ok = true;
       int np[2] = {0, 0};                       // P tiles consumed per row tile
       const uint64_t qd = desc_codes<D>(smem_u32(sm.q)), kd = desc_codes<D>(smem_u32(sm.k));
       const uint64_t vd = desc_sw128_mn(smem_u32(sm.v), kBlk);
-      const uint32_t hi = (uint32_t)(qd >> 32), v_hi = (uint32_t)(vd >> 32);
+      // descriptors hold addresses in units of 16 bytes
       constexpr uint32_t kV16 = sizeof(sm.v[0]) / 16, kK16 = sizeof(sm.k[0]) / 16;
       constexpr uint32_t kQ16 = sizeof(sm.q[0]) / 16, kQPart16 = sizeof(sm.q[0][0]) / 16;
       auto issue_s = [&](int x, int st) {
-        uint32_t ad = (uint32_t)qd + (uint32_t)x * kQ16, bd = (uint32_t)kd + (uint32_t)st * kK16;
-        asm volatile("" : "+r"(ad), "+r"(bd));                // sums stay where they are used
+        const uint64_t ad = qd + (uint32_t)x * kQ16, bd = kd + (uint32_t)st * kK16;
+        __syncwarp();
 #pragma unroll
         for (int kk = 0; kk < 2 * (D / 32); ++kk)             // 32 columns: 2 x 16 bytes
-          mma_e4m3_ss(tbase + kSCol + x * kTcKT, ad + (kk & 1) * kQPart16 + (kk >> 1) * 2, bd + (kk >> 1) * 2, hi,
-                      id_s, kk ? 1u : 0u);
-        mma_commit(&sm.s_full[x]);
+          mma_e4m3_ss(tbase + kSCol + x * kTcKT, ad + (kk & 1) * kQPart16 + (kk >> 1) * 2, bd + (kk >> 1) * 2, id_s,
+                      kk ? 1u : 0u);
+        mma_commit_elected(&sm.s_full[x]);
       };
       auto issue_pv = [&](int x, int st, bool first) -> bool {
-        if (!mbar_wait(&sm.p_full[x], np[x] & 1, abort)) return false;
+        if (!warp_wait(&sm.p_full[x], np[x] & 1, abort)) return false;
         ++np[x];
         tc_fence_after();
-        uint32_t bd = (uint32_t)vd + (uint32_t)st * kV16;
-        asm volatile("" : "+r"(bd));
+        const uint64_t bd = vd + (uint32_t)st * kV16;
+        __syncwarp();
 #pragma unroll
         for (int kk = 0; kk < kTcKT / 16; ++kk)
-          mma_f16_ts(tbase + kOCol + x * D, tbase + kSCol + x * kTcKT + kk * 8, bd + kk * 2048 / 16, v_hi, id_o,
+          mma_f16_ts(tbase + kOCol + x * D, tbase + kSCol + x * kTcKT + kk * 8, bd + kk * 2048 / 16, id_o,
                      (!first || kk) ? 1u : 0u);
         return true;
       };
       do {
         const bool two = rows_of() > 128;
         int ks = t % kKStages;
-        ok = mbar_wait(&sm.q_full, seg & 1, abort) && mbar_wait(&sm.k_full[ks], (t / kKStages) & 1, abort);
+        ok = warp_wait(&sm.q_full, seg & 1, abort) && warp_wait(&sm.k_full[ks], (t / kKStages) & 1, abort);
         if (!ok) break;
         tc_fence_after();
         issue_s(0, ks);
         if (two) issue_s(1, ks);
-        mma_commit(&sm.k_empty[ks]);
+        mma_commit_elected(&sm.k_empty[ks]);
         for (int j = w.t0; ok && j < w.t1; ++j, ++t) {
           const int st = t % kVStages;
           const bool more = j + 1 < w.t1;
           ks = (t + 1) % kKStages;
-          if (!mbar_wait(&sm.v_full[st], (t / kVStages) & 1, abort) || !issue_pv(0, st, j == w.t0)) {
+          if (!warp_wait(&sm.v_full[st], (t / kVStages) & 1, abort) || !issue_pv(0, st, j == w.t0)) {
             ok = false;
             break;
           }
-          if (!more) mma_commit(&sm.o_full[0]);
+          if (!more) mma_commit_elected(&sm.o_full[0]);
           if (more) {
-            if (!mbar_wait(&sm.k_full[ks], ((t + 1) / kKStages) & 1, abort)) {
+            if (!warp_wait(&sm.k_full[ks], ((t + 1) / kKStages) & 1, abort)) {
               ok = false;
               break;
             }
@@ -288,19 +296,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
               ok = false;
               break;
             }
-            if (!more) mma_commit(&sm.o_full[1]);
+            if (!more) mma_commit_elected(&sm.o_full[1]);
           }
-          mma_commit(&sm.v_empty[st]);
+          mma_commit_elected(&sm.v_empty[st]);
           if (more) {
             if (two) issue_s(1, ks);
-            mma_commit(&sm.k_empty[ks]);
+            mma_commit_elected(&sm.k_empty[ks]);
           }
         }
-        if (ok) mma_commit(&sm.q_empty);
+        if (ok) mma_commit_elected(&sm.q_empty);
         ++seg;
       } while (ok && w.next(line, s, err));
       // every MMA is done before the block frees its tensor memory
-      mma_commit(&sm.done);
+      __syncwarp();
+      mma_commit_elected(&sm.done);
       drain_wait(&sm.done, 0);
     }
     if (warp == kLoadWarp) {
