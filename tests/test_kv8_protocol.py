@@ -153,9 +153,10 @@ def run_chunks(segments, seed, mistake=None):
     mk = lambda n: [Bar() for _ in range(n)]
     k_full, k_empty, v_full, v_empty = mk(K_STAGES), mk(K_STAGES), mk(V_STAGES), mk(V_STAGES)
     code_full, code_empty, ref_full = mk(CODE_STAGES), mk(CODE_STAGES), mk(REFS)
-    s_full, p_full, o_full, (q_full, q_empty) = mk(2), mk(2), mk(2), mk(2)
+    s_full, p_half, p_full, o_full, (q_full, q_empty) = mk(2), mk(2), mk(2), mk(2), mk(2)
     K, V, code, ref, q = [None] * K_STAGES, [None] * V_STAGES, [None] * CODE_STAGES, [None] * REFS, [None]
-    S, P, sums = [None, None], [None, None], [[], []]       # sums: tiles added to O of a row tile
+    S, sums = [None, None], [[], []]                        # sums: tiles added to O of a row tile
+    P = [[None, None], [None, None]]                        # P of a row tile, in halves
     flying, pipe, read_o = [], [], [0, 0]
 
     def w(name, bar, phase):
@@ -206,9 +207,11 @@ def run_chunks(segments, seed, mistake=None):
                 st, more = t % V_STAGES, j + 1 < n
                 yield w("v_full", v_full[st], t // V_STAGES)
                 for x in xs:
+                    yield w("p_half", p_half[x], np[x])
+                    pipe.append(("PV", x, t, 0, j == 0))
                     yield w("p_full", p_full[x], np[x])
                     np[x] += 1
-                    pipe.append(("PV", x, t, j == 0))
+                    pipe.append(("PV", x, t, 1, j == 0))
                     if not more:
                         pipe.append(("commit", o_full[x]))
                     if x == xs[-1]:
@@ -244,7 +247,11 @@ def run_chunks(segments, seed, mistake=None):
                     need(sums[x] == list(range(t - j, t)), "O rescaled under a product")
                     yield None
                     need(sums[x] == list(range(t - j, t)), "O rescaled under a product")
-                S[x], P[x] = None, t
+                S[x], P[x] = None, [t, None]
+                yield None
+                p_half[x].arrive()
+                yield None
+                P[x][1] = t
                 yield None
                 p_full[x].arrive()
                 t += 1
@@ -279,10 +286,11 @@ def run_chunks(segments, seed, mistake=None):
             need(S[x] is None, "S written before it was read")
             S[x] = t
         else:
-            _, x, t, first = b
-            need(P[x] == t and V[t % V_STAGES] == t, "PV of another tile")
-            P[x] = None
-            sums[x] = [t] if first else sums[x] + [t]
+            _, x, t, h, first = b
+            need(P[x][h] == t and V[t % V_STAGES] == t, "PV of another tile")
+            P[x][h] = None
+            if h:
+                sums[x] = [t] if first else sums[x] + [t]
         pipe.pop(0)
         return True
 
@@ -300,7 +308,7 @@ def test_chunk_protocol_holds():
 
 
 @pytest.mark.parametrize("mistake", ["k_empty", "code_empty", "code_full", "v_empty", "q_empty", "q_full", "k_full",
-                                     "v_full", "p_full", "s_full", "o_full", "scales first"])
+                                     "v_full", "p_half", "p_full", "s_full", "o_full", "scales first"])
 def test_chunk_protocol_mistakes_are_caught(mistake):
     caught = 0
     for seed in range(150):
