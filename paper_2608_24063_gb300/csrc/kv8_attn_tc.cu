@@ -623,7 +623,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       const float ou = vmax * __uint_as_float((uint32_t)(127 - kTcPExp) << 23);
       const bool whole = w.whole();
       const int64_t at = (int64_t)(w.u.q.row0 + qi) * a.Hq + w.u.g * G + qj;
-      auto put_out = [&](int col, const float (&y)[16], float inv) {
+      auto put_out = [&](int64_t at, int col, const float (&y)[16], float inv) {
         __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + at * D + col;
         uint32_t b8[8];
 #pragma unroll
@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
         *reinterpret_cast<uint4*>(dst) = make_uint4(b8[0], b8[1], b8[2], b8[3]);
         *reinterpret_cast<uint4*>(dst + 8) = make_uint4(b8[4], b8[5], b8[6], b8[7]);
       };
-      auto put_lse = [&](float M, float L) {
+      auto put_lse = [&](int64_t at, float M, float L) {
         if (a.lse) a.lse[at] = L == 0.f ? -INFINITY : fmaf(M, 0.6931471805599453f, logf(L));
       };
       auto inverse_of = [](float L) { return L > 0.f ? 1.f / L : (L == L ? 0.f : L); };
@@ -650,20 +650,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
 #pragma unroll
         for (int q = 0; q < 16; ++q) y[q] = __uint_as_float(v[q]);
         if (whole) {
-          if (real) put_out(p * 16, y, inv);
+          if (real) put_out(at, p * 16, y, inv);
         } else {
-          float* po = a.part_o + ((mine * 2 + X) * 128 + row) * D + p * 16;
+          // (four columns of the row tile's rows side by side)
+          float4* po = reinterpret_cast<float4*>(a.part_o + (mine * 2 + X) * 128 * D) + p * 4 * 128 + row;
 #pragma unroll
-          for (int q = 0; q < 16; q += 4)
-            *reinterpret_cast<float4*>(po + q) =
-                make_float4(y[q] * inv, y[q + 1] * inv, y[q + 2] * inv, y[q + 3] * inv);
+          for (int q = 0; q < 4; ++q)
+            if (real) po[q * 128] = make_float4(y[4 * q] * inv, y[4 * q + 1] * inv, y[4 * q + 2] * inv, y[4 * q + 3] * inv);
         }
       }
       tc_fence_before();
       if (whole) {
-        if (real) put_lse(m, l);
+        if (real) put_lse(at, m, l);
       } else {
-        a.part_ml[(mine * 2 + X) * 128 + row] = make_float2(m, l);
+        if (real) a.part_ml[(mine * 2 + X) * 128 + row] = make_float2(m, l);
         const int first = w.first_block(sh), final = w.last_block(sh);
         __syncwarp();                           // (the named barriers take whole warps)
         named_sync(1 + X, 128);
@@ -673,37 +673,73 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
           __syncwarp();
         }
         named_sync(1 + X, 128);
-        if (sm.last[X] && real) {
-          auto slot = [&](int b) { return ((2 * (int64_t)b + (b == first ? 1 : 0)) * 2 + X) * 128 + row; };
-          float M = -INFINITY, L = 0.f;
-          for (int b = first; b <= final; ++b) M = fmaxf(M, __ldcg(&a.part_ml[slot(b)]).x);
-          for (int b = first; b <= final; ++b) {
-            const float2 ml = __ldcg(&a.part_ml[slot(b)]);
-            L = fmaf(ml.y, ml.x == -INFINITY ? 1.f : ex2(ml.x - M), L);
-          }
-          const float il = inverse_of(L);
-#pragma unroll 1
-          for (int p = 0; p < D / 16; ++p) {
-            float y[16];
+        if (sm.last[X]) {
+          // A warp takes a quarter of the columns of 32 rows, a lane a row, and
+          // has the values of kJoin pieces in flight at once (8 KV heads over 8192
+          // tokens, 19 pieces a unit: 256 rows 156 -> 53 us, 64 rows 65 -> 32 us
+          // against a row a thread and a piece at a time).
+          constexpr int kJoin = 3, kCols = D / 16;          // kCols: float4 a row of a warp
+          const int rows = min(128, w.u.q.m * G - w.u.rt * kTcMT - X * 128);
+          for (int r0 = 0; r0 < rows; r0 += 32) {
+            const int jr = r0 + lane;
+            const bool live = jr < rows;
+            float4 y[kCols];
 #pragma unroll
-            for (int q = 0; q < 16; ++q) y[q] = 0.f;
-            for (int b = first; b <= final; ++b) {
-              const int64_t k = slot(b);
-              const float mx = __ldcg(&a.part_ml[k]).x;
-              const float wt = mx == -INFINITY ? 1.f : ex2(mx - M);
-              const float4* src = reinterpret_cast<const float4*>(a.part_o + k * D + p * 16);
+            for (int q = 0; q < kCols; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            float M = -INFINITY, L = 0.f;
+            for (int b0 = first; b0 <= final; b0 += kJoin) {
+              float2 ml[kJoin];
+              float4 z[kJoin][kCols];
 #pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const float4 z = __ldcg(src + q);
-                y[4 * q] = fmaf(z.x, wt, y[4 * q]);
-                y[4 * q + 1] = fmaf(z.y, wt, y[4 * q + 1]);
-                y[4 * q + 2] = fmaf(z.z, wt, y[4 * q + 2]);
-                y[4 * q + 3] = fmaf(z.w, wt, y[4 * q + 3]);
+              for (int n = 0; n < kJoin; ++n) {
+                const int b = b0 + n;
+                const int64_t tile = (2 * (int64_t)b + (b == first ? 1 : 0)) * 2 + X;
+                const bool on = live && b <= final;
+                ml[n] = on ? __ldcg(&a.part_ml[tile * 128 + jr]) : make_float2(-INFINITY, 0.f);
+                const float4* src =
+                    reinterpret_cast<const float4*>(a.part_o + tile * 128 * D) + (warp & 3) * kCols * 128 + jr;
+#pragma unroll
+                for (int q = 0; q < kCols; ++q) z[n][q] = on ? __ldcg(src + q * 128) : make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+              float top = M;
+#pragma unroll
+              for (int n = 0; n < kJoin; ++n) top = fmaxf(top, ml[n].x);
+              const float g = M == -INFINITY ? 1.f : ex2(M - top);
+              M = top;
+              L *= g;
+#pragma unroll
+              for (int q = 0; q < kCols; ++q) {
+                y[q].x *= g; y[q].y *= g; y[q].z *= g; y[q].w *= g;
+              }
+#pragma unroll
+              for (int n = 0; n < kJoin; ++n) {
+                const float wt = ml[n].x == -INFINITY ? 1.f : ex2(ml[n].x - M);
+                L = fmaf(ml[n].y, wt, L);
+#pragma unroll
+                for (int q = 0; q < kCols; ++q) {
+                  y[q].x = fmaf(z[n][q].x, wt, y[q].x);
+                  y[q].y = fmaf(z[n][q].y, wt, y[q].y);
+                  y[q].z = fmaf(z[n][q].z, wt, y[q].z);
+                  y[q].w = fmaf(z[n][q].w, wt, y[q].w);
+                }
               }
             }
-            put_out(p * 16, y, il);
+            if (!live) continue;
+            const int jrho = w.u.rt * kTcMT + X * 128 + jr, ji = jrho / G;
+            const int64_t jat = (int64_t)(w.u.q.row0 + ji) * a.Hq + w.u.g * G + (jrho - ji * G);
+            const float il = inverse_of(L);
+#pragma unroll
+            for (int p = 0; p < kCols / 4; ++p) {
+              float o[16];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                o[4 * q] = y[4 * p + q].x; o[4 * q + 1] = y[4 * p + q].y;
+                o[4 * q + 2] = y[4 * p + q].z; o[4 * q + 3] = y[4 * p + q].w;
+              }
+              put_out(jat, (warp & 3) * kCols * 4 + p * 16, o, il);
+            }
+            if ((warp & 3) == 0) put_lse(jat, M, L);
           }
-          put_lse(M, L);
         }
       }
     } while (w.next(line, s, err));
