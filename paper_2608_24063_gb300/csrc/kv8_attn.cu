@@ -53,13 +53,17 @@ constexpr float kPScale = 4096.f;               // 2^12
 
 // T: query type, D: head dimension, NQ: groups of 8 query rows of a unit.
 // Warps: registers are granted to four warps at a time, so the consumers and
-// the producer fill 8, 12 or 16 warps of 255, 168 or 128 registers.
+// the producer fill 8, 12 or 16 warps of 255, 168 or 128 registers, chosen by
+// what the accumulators and the query fragments take.  64 requests of 8192
+// tokens, 8 KV heads, us with 7 / 11 / 15 consumers: d = 64, 8 rows 145 / 126 /
+// 121; d = 128, 8 rows 179 / 170 / 171 (fp32 rows 215 / 192 / 201); d = 128, 16
+// rows 230 / 242 / 407.
 template <typename T, int D, int NQ>
 struct Cfg {
   static constexpr int NP = sizeof(T) == 4 ? 2 : 1;         // fp16 parts of a query value
   static constexpr int MT = 8 * NQ;                         // query rows of a unit
   static constexpr int REGS = D / 4 * NQ * (1 + 0.5 * NP);  // accumulators and query fragments
-  static constexpr int WARPS = REGS <= 64 ? 15 : REGS <= 96 ? 11 : 7;
+  static constexpr int WARPS = REGS <= 32 ? 15 : REGS <= 64 ? 11 : 7;
   static constexpr int THREADS = 32 * (WARPS + 1);
   static constexpr int STAGE = kKT * D;                     // bytes of K, and of V
   static constexpr int NST = D == 128 ? 5 : 10;
@@ -662,7 +666,10 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
 }
 
 // Units of 8 query rows where the requests have no more on average (a decode
-// step of up to 8 query heads a KV head), else of 16.
+// step of up to 8 query heads a KV head), else of 16.  Us with units of 8 / of
+// 16, d = 128, 8 KV heads: 64 requests of 8192 tokens, 8 rows 171 / 234, 16 rows
+// 324 / 242; one request, 8 rows 13.3 / 16.5, 16 rows 15.5 / 19.4 (twice the
+// units keep more SMs busy there, which a length on the device does not tell).
 template <typename T, int D>
 cudaError_t launch_q(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
   const int64_t rows = (int64_t)s.n_rows * (a.Hq / c.Hkv);
