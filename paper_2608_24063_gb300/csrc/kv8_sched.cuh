@@ -15,7 +15,7 @@
 // Where the units are no more than the blocks (few requests), a segment's end
 // costs as much as several tiles, so no block takes two: every unit gets whole
 // blocks, ceil(tiles / per) of them with the least `per` that the blocks allow
-// (24 units of 6 to 25 tiles on 152 blocks: 20.8 -> 15.2 us against the line).
+// (24 units of 6 to 25 tiles on 152 blocks: 20.8 -> 16.5 us against the line).
 #pragma once
 
 #include <cuda.h>
