@@ -66,11 +66,26 @@ uint64_t next_token() {
   return z ? z : 1;
 }
 
-// Whether a call runs on tcgen05: bf16 rows, at least kTcRows packed rows of a
-// KV head per request on average.
-constexpr int64_t kTcRows = 64;
-bool many_rows(int64_t n_rows, int64_t n_req, int32_t Hq, int32_t Hkv) {
-  return n_rows * (Hq / Hkv) >= kTcRows * n_req;
+// Whether a call's rows (bf16) run on tcgen05: more than kTcRows packed rows of
+// a KV head per request on average, so more than two 16-row units of the other
+// kernel, and enough of those units that they do not get a few blocks each.
+// That kernel's time goes with units * tiles, this one's begins at 20 us (one
+// block's chain of a tile, and pieces to add up) and then goes with the tiles.
+// d = 128, 8 KV heads, us on mma.sync / on tcgen05:
+//   64 requests of 4096 tokens, 32 rows 248 / 217, 48 rows 364 / 226, 256 rows 1848 / 329
+//   8 of 600 tokens, 32 rows 13.4 / 21.8, 48 rows 30 / 23
+//   one of 32768 tokens, 36 rows 52 / 48, 64 rows 70 / 48
+//   one of 2000 tokens, 48 rows 16.6 / 25.1, 256 rows 25.9 / 49.1
+// Lengths are on the device, so the block table's width stands for them.
+constexpr int64_t kTcRows = 32, kTcShare = 16;
+bool may_have_many_rows(int64_t n_rows, int64_t n_req, int32_t Hq, int32_t Hkv) {
+  return n_rows * (Hq / Hkv) > kTcRows * n_req;
+}
+bool many_rows(const vc_kv8& c, const vc_kv8_step& s, int32_t Hq) {
+  if (!may_have_many_rows(s.n_rows, s.n_req, Hq, c.Hkv)) return false;
+  const int64_t units = (int64_t)s.n_rows * Hq / 16, sms = kv8_sm_count();
+  const int64_t tiles = ((int64_t)s.max_pages * c.page + 127) / 128;
+  return units > sms || units * tiles > kTcShare * sms;
 }
 
 bool valid_heads(int32_t Hq, int32_t Hkv) { return Hkv >= 1 && Hq >= Hkv && Hq <= 4096 && Hq % Hkv == 0; }
@@ -157,7 +172,7 @@ int viscache_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int
 
 size_t viscache_kv8_workspace_size(int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t d) {
   if (n_rows < 0 || n_rows > (1 << 24) || !valid_heads(Hq, Hkv) || (d != 64 && d != 128)) return 0;
-  return kv8_ws(many_rows(n_rows, 1, Hq, Hkv), d).total;
+  return kv8_ws(may_have_many_rows(n_rows, 1, Hq, Hkv), d).total;
 }
 
 int viscache_kv8_append(const vc_kv8* cache, const vc_kv8_step* step, int dtype, const void* K,
@@ -191,7 +206,7 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
   const int64_t row_tiles = (int64_t)step->n_rows * (Hq / cache->Hkv) / 8 + step->n_req;
   if (row_tiles * cache->Hkv > ((int64_t)1 << 37) / (((int64_t)step->max_pages * cache->page + 127) / 128))
     return VC_ERR_UNSUPPORTED;
-  const bool tc = dtype == VC_BF16 && many_rows(step->n_rows, step->n_req, Hq, cache->Hkv);
+  const bool tc = dtype == VC_BF16 && many_rows(*cache, *step, Hq);
   const Kv8Ws w = kv8_ws(tc, cache->d);
   const int wc = check_ws(ws, ws_bytes, w.total);
   if (wc != VC_OK) return wc;

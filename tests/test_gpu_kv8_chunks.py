@@ -1,6 +1,7 @@
-"""GPU parity of attention over the 8-bit paged cache with many query rows a request (the
-tensor-core path for 16-bit rows), against the float64 oracle on sampled rows, and against
-the few-rows path on the same inputs."""
+"""GPU parity of attention over the 8-bit paged cache with many query rows a request, against
+the float64 oracle on sampled rows, and against fp32 rows of the same values.  The block
+table's width stands for the lengths where a call chooses between its two kernels, so every
+case runs on both: with the table as wide as its pages, and much wider."""
 import numpy as np
 import pytest
 import torch
@@ -10,6 +11,34 @@ from paper_2608_24063_gb300 import viscache as vc
 from tests.test_gpu_kv8 import BF, DEV, Pool, _filled, _rand
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(params=[False, True], ids=["narrow", "wide"])
+def wide(request):
+    return request.param
+
+
+def _step(pool, lens, rows, wide):
+    step = pool.step(lens, rows)
+    if not wide:
+        return step
+    # entries past a request's pages are not read: no page has this number
+    table = torch.full((len(lens), 400000 // pool.page), -7, dtype=torch.int32, device=DEV)
+    table[:, :pool.table.shape[1]] = step.tensors[0]
+    return vc.Kv8Step(table, step.tensors[1], step.tensors[2], step.n_rows)
+
+
+def test_both_kernels_run():
+    lens, rows = [300, 40], [20, 20]
+    pool = _filled(lens, 1, 64, 128)
+    q = _rand((40, 4, 128), 1, BF).to(DEV)
+    for is_wide, name in ((False, "kv8_attn"), (True, "kv8_attn_tc")):
+        vc.viscache_profile_enable(True)
+        try:
+            _run(pool, _step(pool, lens, rows, is_wide), q, True)
+            assert list(vc.viscache_profile_read()) == [name]
+        finally:
+            vc.viscache_profile_enable(False)
 
 
 def _run(pool, step, q, causal, scale=0.0):
@@ -23,12 +52,12 @@ def _run(pool, step, q, causal, scale=0.0):
     return out, lse
 
 
-def check(pool, lens, rows, Hq, causal, scale=0.0, qscale=1.5, sample=7, seed=60):
+def check(pool, lens, rows, Hq, causal, wide, scale=0.0, qscale=1.5, sample=7, seed=60):
     """Rows of the call against the oracle: a few of each request, the first, the last and those
     at row-tile ends among them."""
     Hkv, d, G = pool.Hkv, pool.d, Hq // pool.Hkv
     q = _rand((sum(rows), Hq + Hkv, d), seed, BF, qscale)
-    out, lse = _run(pool, pool.step(lens, rows), q.to(DEV)[:, :Hq], causal, scale)
+    out, lse = _run(pool, _step(pool, lens, rows, wide), q.to(DEV)[:, :Hq], causal, scale)
     got, z = out.double().cpu().numpy(), lse.double().cpu().numpy()
     assert np.isfinite(got).all()
     sc = scale if scale > 0 else 1.0 / np.sqrt(d)
@@ -68,29 +97,29 @@ def check(pool, lens, rows, Hq, causal, scale=0.0, qscale=1.5, sample=7, seed=60
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("Hq,Hkv,d,page", [(28, 4, 128, 64), (8, 4, 64, 16), (16, 1, 64, 128), (2, 2, 128, 32),
                                            (24, 1, 128, 16)])
-def test_chunks_match_oracle(Hq, Hkv, d, page, causal):
+def test_chunks_match_oracle(Hq, Hkv, d, page, causal, wide):
     # one and two row tiles of a unit, units that end inside them, requests without rows, all of
     # whose tokens are rows, with more rows than tokens
     lens, rows = [700, 40, 300, 60, 0, 513], [129, 0, 300, 77, 65, 400]
-    check(_filled(lens, Hkv, page, d), lens, rows, Hq, causal)
+    check(_filled(lens, Hkv, page, d), lens, rows, Hq, causal, wide)
 
 
-def test_units_split_over_blocks():
+def test_units_split_over_blocks(wide):
     # few units and long contexts: every unit's tiles lie on many blocks
     lens, rows = [20000, 3001], [40, 17]
-    check(_filled(lens, 1, 64, 128), lens, rows, 4, True)
+    check(_filled(lens, 1, 64, 128), lens, rows, 4, True, wide)
     lens, rows = [9000], [300]
-    check(_filled(lens, 1, 16, 64), lens, rows, 2, True, sample=3)
+    check(_filled(lens, 1, 16, 64), lens, rows, 2, True, wide, sample=3)
 
 
-def test_more_units_than_blocks():
+def test_more_units_than_blocks(wide):
     rng = np.random.default_rng(8)
     rows = rng.integers(1, 150, 40).tolist()
     lens = [m + int(x) for m, x in zip(rows, rng.integers(0, 300, 40))]
-    check(_filled(lens, 4, 32, 128), lens, rows, 8, True, sample=2)
+    check(_filled(lens, 4, 32, 128), lens, rows, 8, True, wide, sample=2)
 
 
-def test_rising_maxima_and_scales():
+def test_rising_maxima_and_scales(wide):
     # scores that rise by hundreds along the tokens and V pages of growing size: O is rescaled
     # again and again; then the other way round
     n = 1200
@@ -101,30 +130,30 @@ def test_rising_maxima_and_scales():
         grow = 2.0 ** torch.div(torch.arange(n), 100, rounding_mode="floor")[:, None, None]
         K, V = K * (size.flip(0) if flip else size), V * (grow.flip(0) if flip else grow)
         pool.append([n], [n], K, V)
-        check(pool, [n], [90], 4, True, scale=0.5)
-        check(pool, [n], [90], 4, True, qscale=1e-20)
+        check(pool, [n], [90], 4, True, wide, scale=0.5)
+        check(pool, [n], [90], 4, True, wide, qscale=1e-20)
 
 
-def test_zero_pages_and_zero_rows():
+def test_zero_pages_and_zero_rows(wide):
     pool = Pool([400], 2, 16, 64)
     K, V = _rand((400, 2, 64), 1, torch.float32), _rand((400, 2, 64), 2, torch.float32)
     K[0:160] = 0
     V[128:272] = 0
     K[320:] = 0
     pool.append([400], [400], K, V)
-    check(pool, [400], [100], 4, True)
-    check(pool, [400], [100], 4, True, qscale=0.0)
+    check(pool, [400], [100], 4, True, wide)
+    check(pool, [400], [100], 4, True, wide, qscale=0.0)
 
 
-def test_paths_agree_and_calls_repeat():
+def test_paths_agree_and_calls_repeat(wide):
     # the same rows through the many-rows path (one call) and the few-rows path (fp32 rows)
     lens, rows = [900, 333], [200, 150]
     pool = _filled(lens, 2, 64, 128)
     q = _rand((350, 8, 128), 5, BF).to(DEV)
-    a, la = _run(pool, pool.step(lens, rows), q, True)
-    b, lb = _run(pool, pool.step(lens, rows), q, True)
+    a, la = _run(pool, _step(pool, lens, rows, wide), q, True)
+    b, lb = _run(pool, _step(pool, lens, rows, wide), q, True)
     assert torch.equal(a, b) and torch.equal(la, lb)
-    f, lf = _run(pool, pool.step(lens, rows), q.float(), True)
+    f, lf = _run(pool, _step(pool, lens, rows, wide), q.float(), True)
     # within the output's rounding and the fp16 probabilities' (2^-11 of sum p |V| <= max |V|),
     # and the scores' error: sums of up to size = sum |q| |k| * scale, as in check()
     K, V = (np.abs(kv8.VALUE[c]) * x[..., None, None] for c, x in zip(pool.codes, pool.scale))
