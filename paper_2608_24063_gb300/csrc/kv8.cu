@@ -20,8 +20,6 @@ namespace {
 
 using namespace kv8;
 
-constexpr int64_t kFill = 152 * 8;              // blocks that fill the device
-
 // The u-th page touched by the step's rows, requests in order.
 struct Touch {
   int r, j;              // request, page within the request
@@ -412,13 +410,19 @@ template <typename T, int D, int PAGE>
 cudaError_t launch_t(bool append, const vc_kv8& c, const vc_kv8_step& s, const Kv8Rows& rows, int32_t* status,
                      cudaStream_t st) {
   ProfileScope ps(append ? "kv8_append" : "kv8_read", st);
-  // blocks a page: enough blocks in all to fill the device, else as few as
-  // possible (a block looks its page up once).  8 KV heads of 128, pages of 64,
-  // us with one / 8 / 32 blocks an SM: append of 64 requests' next tokens 8.1 /
-  // 5.6 / 6.6, of 2048 rows 6.6 / 4.6 / 4.6, of 16384 rows 21.6 / 17.9 / 21.5;
-  // read of 2048 rows 7.0 / 5.4 / 5.6, of 16384 rows 19.2 / 22.0 / 20.1
+  // blocks a page: as many as make the device full at 1280 threads an SM, since
+  // a step of few rows is as long as one block's turn; three (two with
+  // fp32 rows or four vectors a thread) where there are pages enough, so that
+  // the last blocks to start are short.  Us with 152 * 8 blocks in all and no least number / so:
+  //   64 requests' next tokens, 8 KV heads of 128, pages of 64: append 6.0 / 5.4, read 4.9 / 3.7
+  //   32 of 4096 tokens, 8 of 128, pages of 64: append 121.8 / 120.4, read 141.6 / 134.5
+  //   32 of 4096 tokens, 8 of 128, pages of 16: append 165.1 / 140.7, read 189.7 / 147.5
+  //   32 of 4096 tokens, 4 of 64, pages of 16: append 92.4 / 61.9, read 101.7 / 63.3
   const int64_t pages = most_pages<PAGE>(s);
-  int64_t split = (kFill + pages - 1) / pages;
+  constexpr int threads = UnitCfg<D, PAGE>::THREADS;
+  int64_t split = (152 * (1280 / threads) + pages - 1) / pages;
+  constexpr int least = UnitCfg<D, PAGE>::blocks(sizeof(T)) > 1 ? 3 : 2;
+  if (split < least) split = least;
   if (split > 2 * c.Hkv) split = 2 * c.Hkv;
   const dim3 grid((unsigned)pages + 1, (unsigned)split);
   if (append) kv8_append_kernel<T, D, PAGE><<<grid, UnitCfg<D, PAGE>::THREADS, 0, st>>>(c, s, rows, status);
