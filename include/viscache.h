@@ -523,7 +523,8 @@ int viscache_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int
  * bytes (Hq = Hkv for append and read), 256-byte aligned; calls that may
  * overlap need their own.  No device memory is allocated; calls are
  * asynchronous on `stream`.  Errors: VC_ERR_INVALID_ARG, VC_ERR_WORKSPACE,
- * VC_ERR_CUDA.
+ * VC_ERR_CUDA, and VC_ERR_UNSUPPORTED from the attention where the rows times
+ * max_pages are past 2^37 tiles.
  */
 typedef struct {
     void* K_codes;
@@ -582,13 +583,19 @@ int viscache_kv8_read(const vc_kv8* cache, const vc_kv8_step* step, int dtype, v
  *   out     device [n_rows][Hq][d] of `dtype`; a row that sees no token gets zeros
  *   lse     device fp32 [n_rows][Hq] (nullable): natural log of the softmax's
  *           normaliser, -inf for a row that sees no token
- * Arithmetic: e4m3 values and query rows enter the products as fp16 numbers
- * times powers of two, bf16 rows without rounding but for values more than
- * 2^14 below their row's largest, fp32 rows and fp32 calls' probabilities as
- * sums of two such numbers; probabilities of bf16 calls are rounded to fp16
- * (11 bits); sums, maxima and the softmax's normaliser in fp32.  The result
- * does not depend on what else is in the batch but for the order of sums, and
+ * Arithmetic: e4m3 values and query rows enter the products as numbers of few
+ * bits times powers of two.  fp32 rows and fp32 calls' probabilities are sums
+ * of two fp16 numbers (22 bits).  bf16 rows are fp16 numbers, exact for values
+ * down to 2^-14 of their row's largest; in calls of many rows (more than 32 rows
+ * of a KV head per request and work for every SM, judged by n_rows, n_req and
+ * max_pages) they are sums of two e4m3 numbers, exact down to 2^-9 of the row's
+ * largest and within 2^-17 of it below.  Probabilities of bf16 calls are rounded
+ * to fp16 (11 bits, down to 2^-17 of the largest; 2^-28 of it below).  Sums,
+ * maxima and the softmax's normaliser are fp32.  The result does not depend on
+ * what else is in the batch but for that choice and for the order of sums, and
  * is the same for the same call.
+ * After VC_ERR_DEVICE_TIMEOUT (prunekv_get_status) clear the workspace before a
+ * captured call is replayed with it.
  */
 int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dtype, int32_t Hq, const void* q,
                            int64_t q_stride, float scale, int causal, void* out, float* lse, void* ws,

@@ -9,8 +9,9 @@
 //
 // S = Q K^T runs on the codes as they are (kind::f8f6f4): a bf16 number has 8
 // significant bits and an e4m3 number 4, so a query value is exactly the sum
-// of two e4m3 numbers, its rounding and the rest (values below 2^-10 of their
-// row's largest keep 2^-18 of it).  Two products at twice the rate cost what
+// of two e4m3 numbers, its rounding and the rest (values below 2^-9 of their
+// row's largest are off by up to 2^-17 of it: the largest lies in [128, 256) and
+// e4m3 ends at steps of 2^-9).  Two products at twice the rate cost what
 // one fp16 product does, and K needs no expansion: TMA writes its tiles.
 // O = P V runs in fp16: P needs more than e4m3's range, so V is expanded,
 // once for both row tiles.
