@@ -204,5 +204,7 @@ cudaError_t launch_kv8_attn_mma(const vc_kv8& c, const vc_kv8_step& s, int dtype
                                 cudaStream_t st);
 // the same on tcgen05: bf16 rows, many of them
 cudaError_t launch_kv8_attn_tc(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st);
+// fp32 rows, many of them
+cudaError_t launch_kv8_attn_tc32(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st);
 
 }  // namespace vc

@@ -206,7 +206,7 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
   const int64_t row_tiles = (int64_t)step->n_rows * (Hq / cache->Hkv) / 8 + step->n_req;
   if (row_tiles * cache->Hkv > ((int64_t)1 << 37) / (((int64_t)step->max_pages * cache->page + 127) / 128))
     return VC_ERR_UNSUPPORTED;
-  const bool tc = dtype == VC_BF16 && many_rows(*cache, *step, Hq);
+  const bool tc = many_rows(*cache, *step, Hq);
   const Kv8Ws w = kv8_ws(tc, cache->d);
   const int wc = check_ws(ws, ws_bytes, w.total);
   if (wc != VC_OK) return wc;
@@ -227,8 +227,9 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
   a.flags = reinterpret_cast<uint64_t*>(base + w.o_flags);
   a.part_ml = reinterpret_cast<float2*>(base + w.o_ml);
   a.part_o = reinterpret_cast<float*>(base + w.o_o);
-  return cuda_status(tc ? launch_kv8_attn_tc(*cache, *step, a, st)
-                        : launch_kv8_attn_mma(*cache, *step, dtype, a, st));
+  if (!tc) return cuda_status(launch_kv8_attn_mma(*cache, *step, dtype, a, st));
+  return cuda_status(dtype == VC_BF16 ? launch_kv8_attn_tc(*cache, *step, a, st)
+                                      : launch_kv8_attn_tc32(*cache, *step, a, st));
 }
 
 }  // extern "C"

@@ -42,6 +42,7 @@
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_sched.cuh"
+#include "kv8_tc.cuh"
 #include "profile.h"
 #include "tc_common.cuh"
 #include "vc_common.cuh"
@@ -57,7 +58,6 @@ constexpr int kTcMT = 256, kTcKT = 128;
 constexpr int kConvWarp0 = 8, kConvWarps = 4, kIssueWarp = 12, kLoadWarp = 13;
 constexpr float kTcSlack = 10.f;                // log2 units
 constexpr int kTcPExp = 4;
-constexpr uint32_t kBlk = 128 * 128;            // 128 rows x 128 bytes (64 fp16 columns)
 constexpr uint32_t kSCol = 0, kOCol = 256;
 constexpr int kKStages = 3, kVStages = 2, kCodeStages = 2;
 constexpr int kRefs = 8;                        // tiles whose scales are kept (the loader is at most 4 ahead)
@@ -81,99 +81,6 @@ struct TcSmem {
   int abort, last[2];
   int32_t err;                                  // the block's status
 };
-
-// Instruction descriptors, D fp32: kind::f16 with A, B fp16 and B MN-major;
-// kind::f8f6f4 with A, B e4m3, both K-major.
-__host__ __device__ constexpr uint32_t idesc_f16_bmn(uint32_t M, uint32_t N) {
-  return (1u << 4) | (1u << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
-}
-__host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N) {
-  return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24);
-}
-
-// Descriptor of a K-major tile of 8-bit rows of D bytes: 128-byte swizzle
-// (8-row groups 1024 bytes apart) or, at D = 64, 64-byte swizzle (512).
-template <int D>
-__device__ __forceinline__ uint64_t desc_codes(uint32_t smem_addr) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)1 << 16;
-  d |= (uint64_t)((8 * D) >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)(D == 128 ? 2 : 4) << 61;
-  return d;
-}
-// Byte offset of 8-byte piece c of row r in such a tile.
-template <int D>
-__device__ __forceinline__ uint32_t code_piece(int r, int c) {
-  const int ch = D == 128 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
-  return (uint32_t)(r * D + ch * 16 + (c & 1) * 8);
-}
-
-// The issuing warp runs as a whole and each instruction elects its lane: then
-// descriptors and addresses are warp-uniform values, and an MMA is issued every 7
-// to 15 clocks.  Issued from a branch of one thread, each takes 50 to 60 (and a
-// lone one is seen done after 274 clocks instead of 130): as long as it runs.
-//
-// D[tmem] (+)= A[smem] * B[smem]^T.
-__device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                            uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, e;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// D[tmem] (+)= A[tmem] * B[smem].
-__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                           uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, e;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// Arrive on bar once every MMA issued so far has completed (the same elected lane).
-__device__ __forceinline__ void mma_commit_elected(uint64_t* bar) {
-  asm volatile(
-      "{\n\t.reg .pred e;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
-      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
-      : "memory");
-}
-
-__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t hmul2_bits(uint32_t a, __half2 f) {
-  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), f);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-// Sixteen codes times a power of two, as 32 bytes of row `row`, column chunk c
-// (16 columns) of a tile: the two 16-byte pieces are written in an order that
-// keeps the eight lanes of a row on different banks.
-__device__ __forceinline__ void expand16(uint8_t* tile, int row, int c, const uint4& w, float factor) {
-  const __half2 f = __float2half2_rn(factor);
-  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-  uint32_t y[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[2 * i] = hmul2_bits(e4m3x2_to_f16x2(x[i]), f);
-    y[2 * i + 1] = hmul2_bits(e4m3x2_to_f16x2(x[i] >> 16), f);
-  }
-  uint8_t* base = tile + (c >> 2) * kBlk + row * 128;
-  const int ch = 2 * (c & 3), r7 = row & 7;
-  const uint4 lo = make_uint4(y[0], y[1], y[2], y[3]), hi = make_uint4(y[4], y[5], y[6], y[7]);
-  const bool swap = (c & 4) != 0;
-  *reinterpret_cast<uint4*>(base + (((ch + swap) ^ r7) << 4)) = swap ? hi : lo;
-  *reinterpret_cast<uint4*>(base + (((ch + !swap) ^ r7) << 4)) = swap ? lo : hi;
-}
 
 template <int D>
 __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK,
@@ -638,7 +545,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
       auto put_lse = [&](int64_t at, float M, float L) {
         if (a.lse) a.lse[at] = L == 0.f ? -INFINITY : fmaf(M, 0.6931471805599453f, logf(L));
       };
-      auto inverse_of = [](float L) { return L > 0.f ? 1.f / L : (L == L ? 0.f : L); };
       const int64_t mine = 2 * (int64_t)blockIdx.x + (w.t0 == 0 ? 1 : 0);
       const float inv = whole ? inverse_of(l) * ou : ou;
 #pragma unroll 1
@@ -675,72 +581,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid
         }
         named_sync(1 + X, 128);
         if (sm.last[X]) {
-          // A warp takes a quarter of the columns of 32 rows, a lane a row, and
-          // has the values of kJoin pieces in flight at once (8 KV heads over 8192
-          // tokens, 19 pieces a unit: 256 rows 156 -> 53 us, 64 rows 65 -> 32 us
-          // against a row a thread and a piece at a time).
-          constexpr int kJoin = 3, kCols = D / 16;          // kCols: float4 a row of a warp
           const int rows = min(128, w.u.q.m * G - w.u.rt * kTcMT - X * 128);
-          for (int r0 = 0; r0 < rows; r0 += 32) {
-            const int jr = r0 + lane;
-            const bool live = jr < rows;
-            float4 y[kCols];
-#pragma unroll
-            for (int q = 0; q < kCols; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-            float M = -INFINITY, L = 0.f;
-            for (int b0 = first; b0 <= final; b0 += kJoin) {
-              float2 ml[kJoin];
-              float4 z[kJoin][kCols];
-#pragma unroll
-              for (int n = 0; n < kJoin; ++n) {
-                const int b = b0 + n;
-                const int64_t tile = (2 * (int64_t)b + (b == first ? 1 : 0)) * 2 + X;
-                const bool on = live && b <= final;
-                ml[n] = on ? __ldcg(&a.part_ml[tile * 128 + jr]) : make_float2(-INFINITY, 0.f);
-                const float4* src =
-                    reinterpret_cast<const float4*>(a.part_o + tile * 128 * D) + (warp & 3) * kCols * 128 + jr;
-#pragma unroll
-                for (int q = 0; q < kCols; ++q) z[n][q] = on ? __ldcg(src + q * 128) : make_float4(0.f, 0.f, 0.f, 0.f);
-              }
-              float top = M;
-#pragma unroll
-              for (int n = 0; n < kJoin; ++n) top = fmaxf(top, ml[n].x);
-              const float g = M == -INFINITY ? 1.f : ex2(M - top);
-              M = top;
-              L *= g;
-#pragma unroll
-              for (int q = 0; q < kCols; ++q) {
-                y[q].x *= g; y[q].y *= g; y[q].z *= g; y[q].w *= g;
-              }
-#pragma unroll
-              for (int n = 0; n < kJoin; ++n) {
-                const float wt = ml[n].x == -INFINITY ? 1.f : ex2(ml[n].x - M);
-                L = fmaf(ml[n].y, wt, L);
-#pragma unroll
-                for (int q = 0; q < kCols; ++q) {
-                  y[q].x = fmaf(z[n][q].x, wt, y[q].x);
-                  y[q].y = fmaf(z[n][q].y, wt, y[q].y);
-                  y[q].z = fmaf(z[n][q].z, wt, y[q].z);
-                  y[q].w = fmaf(z[n][q].w, wt, y[q].w);
-                }
-              }
-            }
-            if (!live) continue;
+          join_pieces<D>(a, first, final, 2, X, rows, [&](int jr, int col, const float (&y)[16], float M, float L) {
             const int jrho = w.u.rt * kTcMT + X * 128 + jr, ji = jrho / G;
             const int64_t jat = (int64_t)(w.u.q.row0 + ji) * a.Hq + w.u.g * G + (jrho - ji * G);
-            const float il = inverse_of(L);
-#pragma unroll
-            for (int p = 0; p < kCols / 4; ++p) {
-              float o[16];
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                o[4 * q] = y[4 * p + q].x; o[4 * q + 1] = y[4 * p + q].y;
-                o[4 * q + 2] = y[4 * p + q].z; o[4 * q + 3] = y[4 * p + q].w;
-              }
-              put_out(jat, (warp & 3) * kCols * 4 + p * 16, o, il);
-            }
-            if ((warp & 3) == 0) put_lse(jat, M, L);
-          }
+            put_out(jat, col, y, inverse_of(L));
+            if (col == 0) put_lse(jat, M, L);
+          });
         }
       }
     } while (w.next(line, s, err));

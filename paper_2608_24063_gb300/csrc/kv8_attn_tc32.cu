@@ -1,0 +1,604 @@
+// Attention over the 8-bit paged cache, many query rows a request, fp32 rows
+// (viscache_kv8_attention on tcgen05).
+//
+// fp32 rows and probabilities enter the products as sums of two fp16 numbers (22
+// bits), so a tile costs twice what it does with 16-bit rows, and both K and V are
+// expanded to fp16 (exact).  A unit has 128 packed query rows (one TMEM lane a
+// row) over tiles of 128 tokens: 8 * 128 * 128 * d flops a tile, bound by the
+// tensor cores.  Two parts of 256 rows would not fit beside the expanded tiles;
+// with one row tile the softmax of a tile runs while the next tile's S does, from
+// the other of two S buffers.  Persistent blocks, one per SM, share out the line
+// of key tiles (kv8_sched.cuh).
+//
+// Warps (512 threads, register shares set per warpgroup):
+//   0-3    softmax, one thread a row
+//   4-11   converters: K and V codes from the staging ring, e4m3 -> fp16, into
+//          128-byte-swizzled tiles; the unit's query rows too
+//   12     MMA issuer
+//   13     loader: page numbers, scales, a bulk copy per page
+// Tensor memory: S_0, S_1 (128 columns each; P over them, its larger parts in the
+// first 64 columns and the rest in the others), O.  Order of issue:
+//   S(0) S(1) PV(0) S(2) PV(1) ...
+// and the codes come in the same order (K one tile ahead of V).  MMAs of one
+// thread execute in order, so S(t+2) may overwrite the P(t) that PV(t) reads.  P
+// arrives in two halves.
+//
+// Numbers: query rows are scaled by a power of two to a largest magnitude in
+// [2^14, 2^15), so their parts keep 2^-39 of it.  Scores are scaled by their page's
+// K scale in fp32.  V codes are multiplied by their page's scale over the tile's
+// largest one (exact but for pages 2^-15 of their tile).  A row's maximum may be
+// passed by 2^2 before O is rescaled; P = 2^(x - m + 12) times (V scale of the tile
+// / the largest so far), at most 2^14, keeps 22 bits down to 2^-25 of its
+// reference.  Row sums are fp32, of unrounded terms.
+#include "kernels.h"
+#include "kv8.cuh"
+#include "kv8_sched.cuh"
+#include "kv8_tc.cuh"
+#include "profile.h"
+#include "tc_common.cuh"
+#include "vc_common.cuh"
+
+namespace vc {
+namespace {
+
+using namespace kv8;
+using namespace tc;
+
+constexpr int kTcThreads = 512;
+constexpr int kTcMT = 128, kTcKT = 128;
+constexpr int kConvWarp0 = 4, kConvWarps = 8, kIssueWarp = 12, kLoadWarp = 13;
+constexpr float kTcSlack = 2.f;                 // log2 units
+constexpr int kTcPExp = 12;
+constexpr uint32_t kSCol = 0, kOCol = 256;
+constexpr int kKStages = 2, kCodeStages = 4;
+constexpr int kRefs = 8;                        // tiles whose scales are kept (the loader is at most 5 ahead)
+
+template <int D>
+struct Tc32Smem {
+  uint8_t q[2][D / 64][kBlk];                   // query rows of the unit, [larger part, rest][64-column block]
+  uint8_t k[kKStages][D / 64][kBlk];            // K as fp16
+  uint8_t v[D / 64][kBlk];                      // V as fp16
+  uint8_t code[kCodeStages][kTcKT * D];         // codes as they are in the cache: K, K, V, K, V, ...
+  float qs[kTcMT];                              // power of two of each query row
+  float kscale[kRefs][8];                       // K scale of each 16-token group of tile t, at t % kRefs
+  float vshare[kRefs][8];                       // V scale of each group over the tile's largest
+  float vref[kRefs];                            // the tile's largest V scale
+  uint64_t q_full, q_empty, k_full[kKStages], k_empty[kKStages], v_full, pv_done;
+  uint64_t code_full[kCodeStages], code_empty[kCodeStages], ref_full[kRefs];
+  uint64_t s_full[2], p_half[2], p_full, done;
+  int64_t scan[kTcThreads / 32];
+  Share share;
+  uint32_t tmem_base;
+  int abort, last;
+  int32_t err;                                  // the block's status
+};
+
+template <int D>
+__global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __grid_constant__ vc_kv8 c,
+                                                                      const __grid_constant__ vc_kv8_step s,
+                                                                      const __grid_constant__ Kv8AttnArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  Tc32Smem<D>& sm = *reinterpret_cast<Tc32Smem<D>*>(align1024(smem_raw));
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (warp: uniform)
+  const int G = a.Hq / c.Hkv;
+  const Line<kTcMT, kTcKT> line{c.Hkv, G, c.page, a.causal};
+  if (threadIdx.x == 0) {
+    mbar_init(&sm.q_full, kConvWarps);
+    mbar_init(&sm.q_empty, 1);
+    for (int i = 0; i < kKStages; ++i) {
+      mbar_init(&sm.k_full[i], kConvWarps);
+      mbar_init(&sm.k_empty[i], 1);
+    }
+    mbar_init(&sm.v_full, kConvWarps);
+    mbar_init(&sm.pv_done, 1);
+    for (int i = 0; i < kCodeStages; ++i) {
+      mbar_init(&sm.code_full[i], 1);
+      mbar_init(&sm.code_empty[i], kConvWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.s_full[i], 1);
+      mbar_init(&sm.p_half[i], 4);              // (sent before the tile before's is looked for)
+    }
+    mbar_init(&sm.p_full, 4);
+    for (int i = 0; i < kRefs; ++i) mbar_init(&sm.ref_full[i], 1);
+    mbar_init(&sm.done, 1);
+    sm.abort = 0;
+    sm.err = VC_OK;
+    fence_mbar_init();
+  }
+  __syncthreads();
+  int32_t* const err = &sm.err;
+  find_share<kTcThreads>(line, s, err, sm.share, sm.scan);        // ends with a barrier
+  const Share& sh = sm.share;
+  if (sh.begin >= sh.end) {
+    if (threadIdx.x == 0) store_status(a, sm.err);
+    return;
+  }
+  if (warp == kIssueWarp) {
+    tmem_alloc(&sm.tmem_base, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tbase = sm.tmem_base;
+  volatile int* abort = &sm.abort;
+  Walk w;
+  w.start(sh);
+  int seg = 0;                                  // segments so far
+  int t = 0;                                    // tiles so far
+
+  if (warp >= kConvWarp0 + kConvWarps) {
+    // registers a thread: 128 at launch; 216 + 104 + 104 + 88 = 4 * 128
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kIssueWarp) {
+      // ---- MMA issuer
+      constexpr uint32_t id_s = idesc_f16(128, kTcKT), id_o = idesc_f16_bmn(128, D);
+      bool ok = true;
+      const uint64_t qd = desc_sw128(smem_u32(sm.q)), kd = desc_sw128(smem_u32(sm.k));
+      const uint64_t vd = desc_sw128_mn(smem_u32(sm.v), kBlk);
+      // descriptors hold addresses in units of 16 bytes
+      constexpr uint32_t kTile16 = sizeof(sm.v) / 16, kBlk16 = kBlk / 16;
+      auto issue_pv = [&](uint32_t s_col, int kk0, bool first) {
+        tc_fence_after();
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < kTcKT / 32; ++k) {
+          const int kk = kk0 + k;
+          mma_f16_ts(tbase + kOCol, s_col + kk * 8, vd + kk * 2048 / 16, id_o, (!first || k) ? 1u : 0u);
+          mma_f16_ts(tbase + kOCol, s_col + 64 + kk * 8, vd + kk * 2048 / 16, id_o, 1u);
+        }
+      };
+      do {
+        ok = warp_wait(&sm.q_full, seg & 1, abort);
+        for (int j = w.t0; ok && j <= w.t1; ++j) {
+          if (j < w.t1) {
+            const int tk = t + j - w.t0, ks = tk % kKStages;
+            ok = warp_wait(&sm.k_full[ks], (tk / kKStages) & 1, abort);
+            if (!ok) break;
+            tc_fence_after();
+            __syncwarp();
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t at = (kk >> 2) * kBlk16 + (kk & 3) * 2;
+                mma_f16_ss(tbase + kSCol + (tk & 1) * kTcKT, qd + part * kTile16 + at, kd + (uint32_t)ks * kTile16 + at,
+                           id_s, (part || kk) ? 1u : 0u);
+              }
+            mma_commit_elected(&sm.s_full[tk & 1]);
+            mma_commit_elected(&sm.k_empty[ks]);
+          }
+          if (j > w.t0) {
+            const int tv = t + j - 1 - w.t0;
+            const uint32_t s_col = tbase + kSCol + (tv & 1) * kTcKT;
+            ok = warp_wait(&sm.v_full, tv & 1, abort) && warp_wait(&sm.p_half[tv & 1], (tv >> 1) & 1, abort);
+            if (!ok) break;
+            issue_pv(s_col, 0, j - 1 == w.t0);
+            ok = warp_wait(&sm.p_full, tv & 1, abort);
+            if (!ok) break;
+            issue_pv(s_col, kTcKT / 32, false);
+            mma_commit_elected(&sm.pv_done);
+          }
+        }
+        // (after the last PV: the softmax has read the rows' powers of two)
+        if (ok) mma_commit_elected(&sm.q_empty);
+        t += w.t1 - w.t0;
+        ++seg;
+      } while (ok && w.next(line, s, err));
+      // every MMA is done before the block frees its tensor memory
+      __syncwarp();
+      mma_commit_elected(&sm.done);
+      drain_wait(&sm.done, 0);
+    }
+    if (warp == kLoadWarp) {
+      // ---- loader: lane -> (tile, page) of a batch of 32 pages; page numbers and
+      // scales of the next batch load while this one's copies are issued
+      const int ppt = kTcKT / c.page, tpb = 32 / ppt;
+      const int bt = lane / ppt, bp = lane % ppt;
+      const uint32_t page_bytes = (uint32_t)c.page * D;
+      bool ok = true;
+      int item = 0;                             // code tiles under way or landed
+      // the code tile of the pages that the lanes with `mine` hold
+      auto put = [&](const void* codes, bool mine, int pid) {
+        const int st = item % kCodeStages;
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * page_bytes;
+        ok = warp_wait(&sm.code_empty[st], ((item / kCodeStages) & 1) ^ 1, abort);
+        if (!ok) return;
+        if (lane == 0) mbar_arrive_expect_tx(&sm.code_full[st], bytes);
+        __syncwarp();
+        // (a page that does not exist has scale 0: page 0 stands in)
+        if (mine)
+          bulk_load(sm.code[st] + bp * page_bytes,
+                    static_cast<const uint8_t*>(codes) + ((int64_t)max(pid, 0) * c.Hkv + w.u.g) * page_bytes,
+                    page_bytes, &sm.code_full[st]);
+        ++item;
+      };
+      do {
+        auto look = [&](int first, int& pid, float& ks, float& vs, bool& live) {
+          const int tile = first + bt, j = tile * ppt + bp;
+          live = tile < w.t1 && j * c.page < w.u.kend;
+          pid = live ? load_page(s, c.n_pages, w.u.r, j, err) : -1;
+          const int64_t at = (int64_t)max(pid, 0) * c.Hkv + w.u.g;
+          ks = pid >= 0 ? __ldg(c.K_scale + at) : 0.f;
+          vs = pid >= 0 ? __ldg(c.V_scale + at) : 0.f;
+        };
+        int pid, npid = -1, ppid = -1;          // this batch's pages, the next one's, the one's before
+        float ks, vs, nks = 0.f, nvs = 0.f;
+        bool live, nlive = false, plive = false;
+        look(w.t0, pid, ks, vs, live);
+        for (int tb = w.t0; ok && tb < w.t1; tb += tpb) {
+          if (tb + tpb < w.t1) look(tb + tpb, npid, nks, nvs, nlive);
+          float vref = vs;                      // each tile's largest V scale
+          for (int o = 1; o < ppt; o <<= 1) vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, o));
+          const float vshare = vs * pow2_inverse(vref);
+          const int nt = min(tpb, w.t1 - tb);
+          for (int i = 0; i < nt; ++i, ++t) {
+            const int rt = t % kRefs;
+            // (what reads this place's scales is done: the codes of the tile 2 before are expanded
+            // once the PV of the one 5 before is)
+            ok = warp_wait(&sm.code_empty[item % kCodeStages], ((item / kCodeStages) & 1) ^ 1, abort);
+            if (!ok) break;
+            if (bt == i) {
+              if (bp == 0) sm.vref[rt] = vref;
+              for (int e = 0; e < c.page / 16; ++e) {
+                sm.kscale[rt][bp * (c.page / 16) + e] = ks;
+                sm.vshare[rt][bp * (c.page / 16) + e] = vshare;
+              }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.ref_full[rt]);
+            put(c.K_codes, bt == i && live, pid);
+            if (ok && tb + i > w.t0) {
+              if (i > 0) put(c.V_codes, bt == i - 1 && live, pid);
+              else put(c.V_codes, bt == tpb - 1 && plive, ppid);
+            }
+            if (!ok) break;
+          }
+          if (ok && tb + nt == w.t1) put(c.V_codes, bt == nt - 1 && live, pid);
+          ppid = pid;
+          plive = live;
+          pid = npid;
+          ks = nks;
+          vs = nvs;
+          live = nlive;
+        }
+      } while (ok && w.next(line, s, err));
+      // every copy has landed before the block may end
+      __syncwarp();
+      if (lane == 0)
+        for (int i = max(0, item - kCodeStages); i < item; ++i)
+          drain_wait(&sm.code_full[i % kCodeStages], (i / kCodeStages) & 1);
+    }
+  } else if (warp >= kConvWarp0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    // ---- converters
+    const int i = threadIdx.x - 32 * kConvWarp0;
+    bool ok = true;
+    int item = 0;
+    constexpr int LPR = D / 16, RP = 32 * kConvWarps / LPR;       // lanes of a row (16 codes each), rows at once
+    const int key0 = i / LPR, ch = i % LPR;
+    do {
+      // the unit's query rows, once the segment before is done
+      if (!warp_wait(&sm.q_empty, (seg & 1) ^ 1, abort)) break;
+      {
+        const int rows = min(kTcMT, w.u.q.m * G - w.u.rt * kTcMT);
+        constexpr int QL = D / 8;               // lanes of a query row
+#pragma unroll 2
+        for (int r = i / QL; r < kTcMT; r += 32 * kConvWarps / QL) {
+          const int qc = i % QL;
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = 0.f;
+          if (r < rows) {
+            const int rho = w.u.rt * kTcMT + r, qi = rho / G, qj = rho - qi * G;
+            const float4* src =
+                reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (int64_t)(w.u.q.row0 + qi) * a.q_stride +
+                                                (int64_t)(w.u.g * G + qj) * D + qc * 8);
+            const float4 x0 = __ldg(src), x1 = __ldg(src + 1);
+            x[0] = x0.x; x[1] = x0.y; x[2] = x0.z; x[3] = x0.w;
+            x[4] = x1.x; x[5] = x1.y; x[6] = x1.z; x[7] = x1.w;
+          }
+          float amax = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
+#pragma unroll
+          for (int o = QL / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+          // largest magnitude to [2^14, 2^15); zero, tiny or not finite rows as they are
+          const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
+          const float qs = ex <= (14u << 23) || ex == 0x7f800000u ? 1.f : __uint_as_float(ex - (14u << 23));
+          const float inv = pow2_inverse(qs);
+          uint32_t top[4], rest[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float z0 = x[2 * e] * inv, z1 = x[2 * e + 1] * inv;
+            top[e] = half2_bits(z0, z1);
+            rest[e] = half2_rest(z0, z1, top[e]);
+          }
+          const uint32_t off = (uint32_t)((qc >> 3) * kBlk + r * 128 + (((qc & 7) ^ (r & 7)) << 4));
+          *reinterpret_cast<uint4*>(sm.q[0][0] + off) = make_uint4(top[0], top[1], top[2], top[3]);
+          *reinterpret_cast<uint4*>(sm.q[1][0] + off) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+          if (qc == 0) sm.qs[r] = qs;
+        }
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.q_full);
+      for (int j = w.t0; ok && j <= w.t1; ++j) {
+        if (j < w.t1) {                         // K of tile j
+          const int tk = t + j - w.t0, ks = tk % kKStages, st = item % kCodeStages;
+          ok = warp_wait(&sm.code_full[st], (item / kCodeStages) & 1, abort) &&
+               warp_wait(&sm.k_empty[ks], ((tk / kKStages) & 1) ^ 1, abort);
+          if (!ok) break;
+#pragma unroll
+          for (int n = 0; n < 128 / RP; ++n) {
+            const int key = key0 + RP * n;
+            expand16(sm.k[ks][0], key, ch, *reinterpret_cast<const uint4*>(sm.code[st] + key * D + ch * 16), 1.f);
+          }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&sm.code_empty[st]);
+            mbar_arrive(&sm.k_full[ks]);
+          }
+          ++item;
+        }
+        if (j > w.t0) {                         // V of tile j - 1
+          const int tv = t + j - 1 - w.t0, st = item % kCodeStages;
+          const int left = w.u.kend - (j - 1) * kTcKT;            // tokens of the tile
+          ok = warp_wait(&sm.code_full[st], (item / kCodeStages) & 1, abort) &&
+               warp_wait(&sm.pv_done, (tv & 1) ^ 1, abort);
+          if (!ok) break;
+          const float* share = sm.vshare[tv % kRefs];
+#pragma unroll
+          for (int n = 0; n < 128 / RP; ++n) {
+            const int key = key0 + RP * n;
+            uint4 y = *reinterpret_cast<const uint4*>(sm.code[st] + key * D + ch * 16);
+            if (key >= left) y = make_uint4(0u, 0u, 0u, 0u);      // not a token: whatever was there
+            expand16(sm.v[0], key, ch, y, share[key >> 4]);
+          }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&sm.code_empty[st]);
+            mbar_arrive(&sm.v_full);
+          }
+          ++item;
+        }
+      }
+      t += w.t1 - w.t0;
+      ++seg;
+    } while (ok && w.next(line, s, err));
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    // ---- softmax, one row a thread
+    const int row = threadIdx.x;
+    const uint32_t lane_off = (uint32_t)(warp << 5) << 16;
+    const uint32_t o_col = tbase + lane_off + kOCol;
+    bool ok = true;
+    do {
+      const int rho = w.u.rt * kTcMT + row;
+      const bool real = rho < w.u.q.m * G;
+      const int qi = rho / G, qj = rho - qi * G;
+      int lim = w.u.kend;
+      if (a.causal) lim = min(lim, w.u.q.len - w.u.q.m + 1 + qi);
+      float m = -INFINITY, l = 0.f, cs = 0.f, vmax = 0.f;
+      for (int j = w.t0; j < w.t1; ++j, ++t) {
+        ok = ok && warp_wait(&sm.s_full[t & 1], (t >> 1) & 1, abort) &&
+             warp_wait(&sm.ref_full[t % kRefs], (t / kRefs) & 1, abort) &&
+             (j > w.t0 || warp_wait(&sm.q_full, seg & 1, abort));
+        if (!ok) continue;
+        tc_fence_after();
+        const uint32_t s_col = tbase + lane_off + kSCol + (t & 1) * kTcKT;
+        if (j == w.t0) cs = a.scale_log2 * sm.qs[row];
+        // factor of each 16 scores (above 0, so that a masked one stays -inf)
+        const float vr = sm.vref[t % kRefs];
+        float f[8];
+        {
+          const float4 k0 = *reinterpret_cast<const float4*>(&sm.kscale[t % kRefs][0]);
+          const float4 k1 = *reinterpret_cast<const float4*>(&sm.kscale[t % kRefs][4]);
+          f[0] = k0.x; f[1] = k0.y; f[2] = k0.z; f[3] = k0.w;
+          f[4] = k1.x; f[5] = k1.y; f[6] = k1.z; f[7] = k1.w;
+#pragma unroll
+          for (int p = 0; p < 8; ++p) f[p] = fmaxf(cs * f[p], 1e-37f);
+        }
+        float x[8][16];
+        {
+          uint32_t v[8][16];
+#pragma unroll
+          for (int p = 0; p < 8; ++p) tmem_ld16(s_col + p * 16, v[p]);
+          tmem_wait_only();
+#pragma unroll
+          for (int p = 0; p < 8; ++p) {
+            reg_fence(v[p]);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) x[p][q] = __uint_as_float(v[p][q]);
+          }
+        }
+        const int valid = lim - j * kTcKT;
+        if (__any_sync(0xffffffffu, valid < kTcKT)) {
+#pragma unroll
+          for (int p = 0; p < 8; ++p)
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+              if (p * 16 + q >= valid) x[p][q] = -INFINITY;
+        }
+        float b[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) {
+          b[p] = fmaxf(x[p][0], x[p][1]);
+#pragma unroll
+          for (int q = 2; q < 16; q += 2) b[p] = fmax3(b[p], x[p][q], x[p][q + 1]);
+          b[p] *= f[p];
+        }
+        const float tm = fmax3(fmax3(b[0], b[1], b[2]), fmax3(b[3], b[4], b[5]), fmaxf(b[6], b[7]));
+        const bool raise = tm > m + kTcSlack, vraise = vr > vmax;
+        float g = 1.f;
+        if (raise) {
+          g = ex2(m - tm);                      // 0 on the first
+          l *= g;
+          m = tm;
+        }
+        if (vraise) {
+          // one step above, so that a tile with a page of the next size fits
+          const float up = vr * 2.f;
+          g *= vmax * pow2_inverse(up);
+          vmax = up;
+        }
+        if (j > w.t0 && __any_sync(0xffffffffu, raise || vraise)) {
+          // the PV of the tile before is done, the next waits for this P
+          ok = warp_wait(&sm.pv_done, (t & 1) ^ 1, abort);
+          if (!ok) continue;
+          tc_fence_after();
+#pragma unroll 1
+          for (int p = 0; p < D / 16; ++p) {
+            uint32_t v[16];
+            tmem_ld16(o_col + p * 16, v);
+            tmem_wait(v);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * g);
+            tmem_st16(o_col + p * 16, v);
+          }
+        }
+        __syncwarp();                           // (whole warps store P)
+        // exponent of P's factor: 2^12 times the tile's share of vmax, not below 2^-18
+        const int lc = vr > 0.f ? max(-30, (int)(__float_as_uint(vr) >> 23) - (int)(__float_as_uint(vmax) >> 23)) : -30;
+        const float mm = (m == -INFINITY ? 0.f : m) - (float)(lc + kTcPExp);
+        const float2 nm = make_float2(-mm, -mm);
+        float2 l0 = make_float2(0.f, 0.f), l1 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          uint32_t top[16], rest[16];
+#pragma unroll
+          for (int q = 0; q < 16; ++q) {
+            const int k = 32 * h + 2 * q;
+            const float2 y = __ffma2_rn(make_float2(x[k >> 4][k & 15], x[k >> 4][(k & 15) + 1]),
+                                        make_float2(f[k >> 4], f[k >> 4]), nm);
+            const float2 e = make_float2(ex2(y.x), ex2(y.y));
+            if (q & 1) l1 = __fadd2_rn(l1, e);
+            else l0 = __fadd2_rn(l0, e);
+            top[q] = half2_bits(e.x, e.y);
+            rest[q] = half2_rest(e.x, e.y, top[q]);
+          }
+          tmem_st16(s_col + h * 16, top);
+          tmem_st16(s_col + 64 + h * 16, rest);
+          if (h == 1) {                         // the first half may be multiplied
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.p_half[t & 1]);
+          }
+        }
+        const float2 ls = __fadd2_rn(l0, l1);
+        l += (ls.x + ls.y) * __uint_as_float((uint32_t)(127 - lc - kTcPExp) << 23);
+        // the PV of the tile before in turn, so that no wait for one is two phases behind
+        ok = warp_wait(&sm.pv_done, (t & 1) ^ 1, abort);
+        if (!ok) continue;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.p_full);
+      }
+      ok = ok && warp_wait(&sm.pv_done, (t & 1) ^ 1, abort);
+      ++seg;
+      if (named_sync_any(1, 128, !ok)) break;
+      tc_fence_after();
+      // O in units of vmax * 2^-12
+      const float ou = vmax * __uint_as_float((uint32_t)(127 - kTcPExp) << 23);
+      const bool whole = w.whole();
+      const int64_t at = (int64_t)(w.u.q.row0 + qi) * a.Hq + w.u.g * G + qj;
+      auto put_out = [&](int64_t at, int col, const float (&y)[16], float inv) {
+        float4* dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at * D + col);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          dst[q] = make_float4(y[4 * q] * inv, y[4 * q + 1] * inv, y[4 * q + 2] * inv, y[4 * q + 3] * inv);
+      };
+      auto put_lse = [&](int64_t at, float M, float L) {
+        if (a.lse) a.lse[at] = L == 0.f ? -INFINITY : fmaf(M, 0.6931471805599453f, logf(L));
+      };
+      const int64_t mine = 2 * (int64_t)blockIdx.x + (w.t0 == 0 ? 1 : 0);
+      const float inv = whole ? inverse_of(l) * ou : ou;
+#pragma unroll 1
+      for (int p = 0; p < D / 16; ++p) {
+        uint32_t v[16];
+        __syncwarp();                           // (whole warps read tensor memory)
+        tmem_ld16(o_col + p * 16, v);
+        tmem_wait(v);
+        float y[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) y[q] = __uint_as_float(v[q]);
+        if (whole) {
+          if (real) put_out(at, p * 16, y, inv);
+        } else {
+          // (four columns of the row tile's rows side by side)
+          float4* po = reinterpret_cast<float4*>(a.part_o + mine * 128 * D) + p * 4 * 128 + row;
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (real)
+              po[q * 128] = make_float4(y[4 * q] * inv, y[4 * q + 1] * inv, y[4 * q + 2] * inv, y[4 * q + 3] * inv);
+        }
+      }
+      tc_fence_before();
+      if (whole) {
+        if (real) put_lse(at, m, l);
+      } else {
+        if (real) a.part_ml[mine * 128 + row] = make_float2(m, l);
+        const int first = w.first_block(sh), final = w.last_block(sh);
+        __syncwarp();                           // (the named barriers take whole warps)
+        named_sync(1, 128);
+        if (warp == 0) {
+          const bool all = piece_done(a.flags, 1, a.token, first, final);
+          if (lane == 0) sm.last = all;
+          __syncwarp();
+        }
+        named_sync(1, 128);
+        if (sm.last) {
+          const int rows = min(kTcMT, w.u.q.m * G - w.u.rt * kTcMT);
+          join_pieces<D>(a, first, final, 1, 0, rows, [&](int jr, int col, const float (&y)[16], float M, float L) {
+            const int jrho = w.u.rt * kTcMT + jr, ji = jrho / G;
+            const int64_t jat = (int64_t)(w.u.q.row0 + ji) * a.Hq + w.u.g * G + (jrho - ji * G);
+            put_out(jat, col, y, inverse_of(L));
+            if (col == 0) put_lse(jat, M, L);
+          });
+        }
+      }
+    } while (w.next(line, s, err));
+    if (!ok && lane == 0) set_status(err, VC_ERR_DEVICE_TIMEOUT);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kIssueWarp) {
+    tc_fence_after();
+    tmem_dealloc(tbase, 512);
+  }
+  if (threadIdx.x == 0) store_status(a, sm.abort ? VC_ERR_DEVICE_TIMEOUT : sm.err);
+}
+
+template <int D>
+cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
+  constexpr size_t smem = sizeof(Tc32Smem<D>) + 1024;
+  static_assert(smem <= 232448, "shared memory of a block");
+  static std::atomic<bool> attr{false};
+  if (!attr.load(std::memory_order_relaxed)) {
+    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_tc32_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)smem);
+    if (e != cudaSuccess) return e;
+    attr.store(true, std::memory_order_relaxed);
+  }
+  const int64_t G = a.Hq / c.Hkv;
+  const int64_t units = ((int64_t)s.n_rows * G / kTcMT + (s.n_req < s.n_rows ? s.n_req : s.n_rows)) * c.Hkv;
+  const int64_t tiles = units * (((int64_t)s.max_pages * c.page + kTcKT - 1) / kTcKT);
+  const int64_t sms = kv8_sm_count();
+  ProfileScope ps("kv8_attn_tc32", st);
+  kv8_attn_tc32_kernel<D><<<(unsigned)(tiles < sms ? tiles : sms), kTcThreads, smem, st>>>(c, s, a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_attn_tc32(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
+  return c.d == 128 ? launch_t<128>(c, s, a, st) : launch_t<64>(c, s, a, st);
+}
+
+}  // namespace vc

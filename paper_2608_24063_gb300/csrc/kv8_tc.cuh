@@ -1,0 +1,201 @@
+// What the tcgen05 attention kernels over the 8-bit cache share: descriptors, MMAs
+// issued by a whole warp, codes expanded to fp16 tiles, and the join of a split
+// unit's pieces.
+#pragma once
+
+#include "kernels.h"
+#include "kv8.cuh"
+#include "tc_common.cuh"
+
+namespace vc {
+namespace kv8 {
+
+using namespace tc;
+
+constexpr uint32_t kBlk = 128 * 128;            // 128 rows x 128 bytes (64 fp16 columns)
+
+// Instruction descriptors, D fp32: kind::f16 with A, B fp16, both K-major or B
+// MN-major; kind::f8f6f4 with A, B e4m3, both K-major.
+__host__ __device__ constexpr uint32_t idesc_f16(uint32_t M, uint32_t N) {
+  return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+__host__ __device__ constexpr uint32_t idesc_f16_bmn(uint32_t M, uint32_t N) {
+  return (1u << 4) | (1u << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+__host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N) {
+  return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+
+// Descriptor of a K-major tile of 8-bit rows of D bytes: 128-byte swizzle
+// (8-row groups 1024 bytes apart) or, at D = 64, 64-byte swizzle (512).
+template <int D>
+__device__ __forceinline__ uint64_t desc_codes(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)1 << 16;
+  d |= (uint64_t)((8 * D) >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)(D == 128 ? 2 : 4) << 61;
+  return d;
+}
+// Byte offset of 8-byte piece c of row r in such a tile.
+template <int D>
+__device__ __forceinline__ uint32_t code_piece(int r, int c) {
+  const int ch = D == 128 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
+  return (uint32_t)(r * D + ch * 16 + (c & 1) * 8);
+}
+
+// The issuing warp runs as a whole and each instruction elects its lane: then
+// descriptors and addresses are warp-uniform values, and an MMA is issued every 7
+// to 15 clocks.  Issued from a branch of one thread, each takes 50 to 60 (and a
+// lone one is seen done after 274 clocks instead of 130): as long as it runs.
+//
+// D[tmem] (+)= A[smem] * B[smem]^T.
+__device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_f16_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem].
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Arrive on bar once every MMA issued so far has completed (the same elected lane).
+__device__ __forceinline__ void mma_commit_elected(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
+      : "memory");
+}
+
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// what half2_bits(lo, hi) lost, as fp16 numbers again
+__device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t bits) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&bits));
+  return half2_bits(lo - f.x, hi - f.y);
+}
+__device__ __forceinline__ uint32_t hmul2_bits(uint32_t a, __half2 f) {
+  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), f);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Sixteen codes times a power of two, as 32 bytes of row `row`, column chunk c
+// (16 columns) of a tile: the two 16-byte pieces are written in an order that
+// keeps the eight lanes of a row on different banks.
+__device__ __forceinline__ void expand16(uint8_t* tile, int row, int c, const uint4& w, float factor) {
+  const __half2 f = __float2half2_rn(factor);
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  uint32_t y[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = hmul2_bits(e4m3x2_to_f16x2(x[i]), f);
+    y[2 * i + 1] = hmul2_bits(e4m3x2_to_f16x2(x[i] >> 16), f);
+  }
+  uint8_t* base = tile + (c >> 2) * kBlk + row * 128;
+  const int ch = 2 * (c & 3), r7 = row & 7;
+  const uint4 lo = make_uint4(y[0], y[1], y[2], y[3]), hi = make_uint4(y[4], y[5], y[6], y[7]);
+  const bool swap = (c & 4) != 0;
+  *reinterpret_cast<uint4*>(base + (((ch + swap) ^ r7) << 4)) = swap ? hi : lo;
+  *reinterpret_cast<uint4*>(base + (((ch + !swap) ^ r7) << 4)) = swap ? lo : hi;
+}
+
+// 1 / a row's sum; 0 where it saw no token, NaN stays.
+__device__ __forceinline__ float inverse_of(float L) { return L > 0.f ? 1.f / L : (L == L ? 0.f : L); }
+
+// Adds up the pieces of a split unit's 128-row tile `x` of `tiles`, called by
+// four warps: a warp takes a quarter of the columns of 32 rows, a lane a row, and
+// has the values of kJoin pieces in flight at once (8 KV heads over 8192 tokens,
+// 19 pieces a unit: 256 rows 156 -> 53 us, 64 rows 65 -> 32 us against a row a
+// thread and a piece at a time).  Pieces lie as [block, end of it][tile]: (max,
+// sum) of its rows, and outputs [four columns][row].  put(row, column, 16
+// unscaled outputs, max, sum).
+template <int D, typename Put>
+__device__ __forceinline__ void join_pieces(const Kv8AttnArgs& a, int first, int final, int tiles, int x, int rows,
+                                            Put put) {
+  constexpr int kJoin = 3, kCols = D / 16;      // kCols: float4 a row of a warp
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
+  for (int r0 = 0; r0 < rows; r0 += 32) {
+    const int row = r0 + lane;
+    const bool live = row < rows;
+    float4 y[kCols];
+#pragma unroll
+    for (int q = 0; q < kCols; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float M = -INFINITY, L = 0.f;
+    for (int b0 = first; b0 <= final; b0 += kJoin) {
+      float2 ml[kJoin];
+      float4 z[kJoin][kCols];
+#pragma unroll
+      for (int n = 0; n < kJoin; ++n) {
+        const int b = b0 + n;
+        const int64_t tile = (2 * (int64_t)b + (b == first ? 1 : 0)) * tiles + x;
+        const bool on = live && b <= final;
+        ml[n] = on ? __ldcg(&a.part_ml[tile * 128 + row]) : make_float2(-INFINITY, 0.f);
+        const float4* src = reinterpret_cast<const float4*>(a.part_o + tile * 128 * D) + warp * kCols * 128 + row;
+#pragma unroll
+        for (int q = 0; q < kCols; ++q) z[n][q] = on ? __ldcg(src + q * 128) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      float top = M;
+#pragma unroll
+      for (int n = 0; n < kJoin; ++n) top = fmaxf(top, ml[n].x);
+      const float g = M == -INFINITY ? 1.f : ex2(M - top);
+      M = top;
+      L *= g;
+#pragma unroll
+      for (int q = 0; q < kCols; ++q) {
+        y[q].x *= g; y[q].y *= g; y[q].z *= g; y[q].w *= g;
+      }
+#pragma unroll
+      for (int n = 0; n < kJoin; ++n) {
+        const float wt = ml[n].x == -INFINITY ? 1.f : ex2(ml[n].x - M);
+        L = fmaf(ml[n].y, wt, L);
+#pragma unroll
+        for (int q = 0; q < kCols; ++q) {
+          y[q].x = fmaf(z[n][q].x, wt, y[q].x);
+          y[q].y = fmaf(z[n][q].y, wt, y[q].y);
+          y[q].z = fmaf(z[n][q].z, wt, y[q].z);
+          y[q].w = fmaf(z[n][q].w, wt, y[q].w);
+        }
+      }
+    }
+    if (!live) continue;
+#pragma unroll
+    for (int p = 0; p < kCols / 4; ++p) {
+      float o[16];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        o[4 * q] = y[4 * p + q].x; o[4 * q + 1] = y[4 * p + q].y;
+        o[4 * q + 2] = y[4 * p + q].z; o[4 * q + 3] = y[4 * p + q].w;
+      }
+      put(row, warp * kCols * 4 + p * 16, o, M, L);
+    }
+  }
+}
+
+}  // namespace kv8
+}  // namespace vc

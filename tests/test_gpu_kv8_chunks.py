@@ -1,6 +1,6 @@
 """GPU parity of attention over the 8-bit paged cache with many query rows a request, against
 the float64 oracle on sampled rows, and against fp32 rows of the same values.  The block
-table's width stands for the lengths where a call chooses between its two kernels, so every
+table's width stands for the lengths where a call chooses between its kernels, so every
 case runs on both: with the table as wide as its pages, and much wider."""
 import numpy as np
 import pytest
@@ -28,11 +28,12 @@ def _step(pool, lens, rows, wide):
     return vc.Kv8Step(table, step.tensors[1], step.tensors[2], step.n_rows)
 
 
-def test_both_kernels_run():
+def test_every_kernel_runs():
     lens, rows = [300, 40], [20, 20]
     pool = _filled(lens, 1, 64, 128)
     q = _rand((40, 4, 128), 1, BF).to(DEV)
-    for is_wide, name in ((False, "kv8_attn"), (True, "kv8_attn_tc")):
+    for is_wide, name, q in ((False, "kv8_attn", q), (True, "kv8_attn_tc", q), (False, "kv8_attn", q.float()),
+                             (True, "kv8_attn_tc32", q.float())):
         vc.viscache_profile_enable(True)
         try:
             _run(pool, _step(pool, lens, rows, is_wide), q, True)
@@ -52,11 +53,11 @@ def _run(pool, step, q, causal, scale=0.0):
     return out, lse
 
 
-def check(pool, lens, rows, Hq, causal, wide, scale=0.0, qscale=1.5, sample=7, seed=60):
+def check(pool, lens, rows, Hq, causal, wide, scale=0.0, qscale=1.5, sample=7, seed=60, dtype=BF):
     """Rows of the call against the oracle: a few of each request, the first, the last and those
     at row-tile ends among them."""
     Hkv, d, G = pool.Hkv, pool.d, Hq // pool.Hkv
-    q = _rand((sum(rows), Hq + Hkv, d), seed, BF, qscale)
+    q = _rand((sum(rows), Hq + Hkv, d), seed, dtype, qscale)
     out, lse = _run(pool, _step(pool, lens, rows, wide), q.to(DEV)[:, :Hq], causal, scale)
     got, z = out.double().cpu().numpy(), lse.double().cpu().numpy()
     assert np.isfinite(got).all()
@@ -80,9 +81,18 @@ def check(pool, lens, rows, Hq, causal, wide, scale=0.0, qscale=1.5, sample=7, s
                     # (2^-11), those below 2^-17 of the reference to 2^-28 of it; sums over k / 16
                     # product steps; the output's rounding
                     size = (np.abs(qq) @ np.abs(K[:k]).T * sc).max(initial=0.0)
-                    E = size * (d / 16 + 6) * 2.0 ** -23 + 2.0 ** -21
-                    rel = 2 * E + 2.0 ** -11 + (k / 16 + 40) * 2.0 ** -23
-                    tol = rel * absv + (1 + rel) * 2.0 ** -8 * np.abs(ref) + k * 2.0 ** -28 * vmax
+                    if dtype == BF:
+                        E = size * (d / 16 + 6) * 2.0 ** -23 + 2.0 ** -21
+                        rel = 2 * E + 2.0 ** -11 + (k / 16 + 40) * 2.0 ** -23
+                        tol = rel * absv + (1 + rel) * 2.0 ** -8 * np.abs(ref) + k * 2.0 ** -28 * vmax
+                    else:
+                        # fp32 rows: two fp16 parts of rows and probabilities (2^-22 each), so
+                        # twice the product steps; a probability's second part ends at 2^-25 of
+                        # 2^12 (2^-37 a key), a value's fp16 number at 2^-25 of its tile's scale
+                        # (under 2^-32 of the largest value)
+                        E = size * (d / 8 + 8) * 2.0 ** -23 + 2.0 ** -21
+                        rel = 2 * E + 2.0 ** -21 + (k / 8 + 40) * 2.0 ** -23
+                        tol = rel * absv + (1 + rel) * 2.0 ** -24 * np.abs(ref) + (k * 2.0 ** -36 + 2.0 ** -32) * vmax
                     err = np.abs(got[at + i, j] - ref[0])
                     assert (err <= tol[0]).all(), (r, i, j, float((err - tol[0]).max()), float(err.max()))
                     if k == 0:
@@ -94,32 +104,36 @@ def check(pool, lens, rows, Hq, causal, wide, scale=0.0, qscale=1.5, sample=7, s
     return out, lse
 
 
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("Hq,Hkv,d,page", [(28, 4, 128, 64), (8, 4, 64, 16), (16, 1, 64, 128), (2, 2, 128, 32),
                                            (24, 1, 128, 16)])
-def test_chunks_match_oracle(Hq, Hkv, d, page, causal, wide):
+def test_chunks_match_oracle(Hq, Hkv, d, page, causal, wide, dtype):
     # one and two row tiles of a unit, units that end inside them, requests without rows, all of
     # whose tokens are rows, with more rows than tokens
     lens, rows = [700, 40, 300, 60, 0, 513], [129, 0, 300, 77, 65, 400]
-    check(_filled(lens, Hkv, page, d), lens, rows, Hq, causal, wide)
+    check(_filled(lens, Hkv, page, d), lens, rows, Hq, causal, wide, dtype=dtype)
 
 
-def test_units_split_over_blocks(wide):
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
+def test_units_split_over_blocks(wide, dtype):
     # few units and long contexts: every unit's tiles lie on many blocks
     lens, rows = [20000, 3001], [40, 17]
-    check(_filled(lens, 1, 64, 128), lens, rows, 4, True, wide)
+    check(_filled(lens, 1, 64, 128), lens, rows, 4, True, wide, dtype=dtype)
     lens, rows = [9000], [300]
-    check(_filled(lens, 1, 16, 64), lens, rows, 2, True, wide, sample=3)
+    check(_filled(lens, 1, 16, 64), lens, rows, 2, True, wide, sample=3, dtype=dtype)
 
 
-def test_more_units_than_blocks(wide):
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
+def test_more_units_than_blocks(wide, dtype):
     rng = np.random.default_rng(8)
     rows = rng.integers(1, 150, 40).tolist()
     lens = [m + int(x) for m, x in zip(rows, rng.integers(0, 300, 40))]
-    check(_filled(lens, 4, 32, 128), lens, rows, 8, True, wide, sample=2)
+    check(_filled(lens, 4, 32, 128), lens, rows, 8, True, wide, sample=2, dtype=dtype)
 
 
-def test_rising_maxima_and_scales(wide):
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
+def test_rising_maxima_and_scales(wide, dtype):
     # scores that rise by hundreds along the tokens and V pages of growing size: O is rescaled
     # again and again; then the other way round
     n = 1200
@@ -130,19 +144,20 @@ def test_rising_maxima_and_scales(wide):
         grow = 2.0 ** torch.div(torch.arange(n), 100, rounding_mode="floor")[:, None, None]
         K, V = K * (size.flip(0) if flip else size), V * (grow.flip(0) if flip else grow)
         pool.append([n], [n], K, V)
-        check(pool, [n], [90], 4, True, wide, scale=0.5)
-        check(pool, [n], [90], 4, True, wide, qscale=1e-20)
+        check(pool, [n], [90], 4, True, wide, scale=0.5, dtype=dtype)
+        check(pool, [n], [90], 4, True, wide, qscale=1e-20, dtype=dtype)
 
 
-def test_zero_pages_and_zero_rows(wide):
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
+def test_zero_pages_and_zero_rows(wide, dtype):
     pool = Pool([400], 2, 16, 64)
     K, V = _rand((400, 2, 64), 1, torch.float32), _rand((400, 2, 64), 2, torch.float32)
     K[0:160] = 0
     V[128:272] = 0
     K[320:] = 0
     pool.append([400], [400], K, V)
-    check(pool, [400], [100], 4, True, wide)
-    check(pool, [400], [100], 4, True, wide, qscale=0.0)
+    check(pool, [400], [100], 4, True, wide, dtype=dtype)
+    check(pool, [400], [100], 4, True, wide, qscale=0.0, dtype=dtype)
 
 
 def test_paths_agree_and_calls_repeat(wide):

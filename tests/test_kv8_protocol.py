@@ -1,5 +1,5 @@
-"""Host models of the barrier protocols of the two attention kernels over the 8-bit cache
-(csrc/kv8_attn.cu, csrc/kv8_attn_tc.cu).
+"""Host models of the barrier protocols of the attention kernels over the 8-bit cache
+(csrc/kv8_attn.cu, csrc/kv8_attn_tc.cu, csrc/kv8_attn_tc32.cu).
 
 Each role of a kernel (producer or loader, consumers, converters, MMA issuer, softmax of a
 row tile) is a coroutine that makes the kernel's waits and arrivals in the kernel's order;
@@ -317,3 +317,183 @@ def test_chunk_protocol_mistakes_are_caught(mistake):
         except ProtocolError:
             caught += 1
     assert caught > 0, mistake
+
+
+# ---------------------------------------------------------------------------------------
+# the many-rows kernel of fp32 rows: one row tile, two S buffers, K expanded a tile ahead of V
+
+def run_chunks32(segments, seed, mistake=None):
+    """segments: tiles of each."""
+    rnd = random.Random(seed)
+    mk = lambda n, count=1: [Bar(count) for _ in range(n)]
+    ring, stages = 4, 2
+    k_full, k_empty, v_full, pv_done = mk(stages), mk(stages), Bar(), Bar()
+    code_full, code_empty, ref_full = mk(ring), mk(ring), mk(REFS)
+    s_full, p_half, p_full, q_full, q_empty = mk(2), mk(2), Bar(), Bar(), Bar()
+    K, V, code, ref, q, qs = [None] * stages, [None], [None] * ring, [None] * REFS, [None], [None]
+    S, P, added = [None, None], [[None, None], [None, None]], []
+    flying, pipe = [], []
+
+    def w(name, bar, phase):
+        return None if mistake == name else (bar, phase)
+
+    def items(n, t):
+        # the order of the codes of a segment whose first tile is t
+        for j in range(n + 1):
+            if j < n:
+                yield "K", t + j
+            if j > 0:
+                yield "V", t + j - 1
+
+    def loader():
+        t, item = 0, 0
+        for n in segments:
+            for kind, x in items(n, t):
+                yield w("code_empty", code_empty[item % ring], item // ring - 1)
+                if kind == "K":
+                    ref[x % REFS] = x
+                    ref_full[x % REFS].arrive()
+                flying.append((kind, x, item))
+                item += 1
+            t += n
+
+    def converters():
+        t, item = 0, 0
+        for seg, n in enumerate(segments):
+            yield w("q_empty", q_empty, seg - 1)
+            need(not any(b[0] == "S" for b in pipe), "query rows written under an S that reads them")
+            q[0], qs[0] = seg, seg
+            yield None
+            q_full.arrive()
+            for kind, x in items(n, t):
+                yield w("code_full", code_full[item % ring], item // ring)
+                if kind == "K":
+                    yield w("k_empty", k_empty[x % stages], x // stages - 1)
+                    need(not any(b[0] == "S" and b[1] % stages == x % stages for b in pipe), "K written under its product")
+                    K[x % stages] = x
+                else:
+                    yield w("pv_done", pv_done, x - 1)
+                    need(not any(b[0] == "PV" for b in pipe), "V written under its product")
+                    need(ref[x % REFS] == x, "scales of another tile")
+                    V[0] = x
+                need(code[item % ring] == (kind, x), "codes of another tile expanded")
+                yield None
+                code_empty[item % ring].arrive()
+                (k_full[x % stages] if kind == "K" else v_full).arrive()
+                item += 1
+            t += n
+
+    def issuer():
+        t = 0
+        for seg, n in enumerate(segments):
+            yield w("q_full", q_full, seg)
+            for kind, x in items(n, t):
+                if kind == "K":
+                    yield w("k_full", k_full[x % stages], x // stages)
+                    pipe.append(("S", x, seg))
+                    pipe.append(("commit", s_full[x & 1]))
+                    pipe.append(("commit", k_empty[x % stages]))
+                    if mistake == "rows early" and x == t + n - 1:
+                        pipe.append(("commit", q_empty))
+                else:
+                    yield w("v_full", v_full, x)
+                    yield w("p_half", p_half[x & 1], x >> 1)
+                    pipe.append(("PV", x, 0, x == t))
+                    yield w("p_full", p_full, x)
+                    pipe.append(("PV", x, 1, x == t))
+                    pipe.append(("commit", pv_done))
+            if mistake != "rows early":
+                pipe.append(("commit", q_empty))
+            t += n
+
+    def softmax():
+        t = 0
+        for seg, n in enumerate(segments):
+            for j in range(n):
+                yield w("s_full", s_full[t & 1], t >> 1)
+                yield ref_full[t % REFS], t // REFS
+                if j == 0:
+                    yield q_full, seg
+                    need(qs[0] == seg, "powers of two of other rows")
+                need(S[t & 1] == t, "scores of another tile")
+                need(ref[t % REFS] == t, "scales of another tile")
+                if j and rnd.random() < 0.3:        # O is rescaled
+                    yield w("rescale", pv_done, t - 1)
+                    need(added == list(range(t - j, t)), "O rescaled under a product")
+                    yield None
+                    need(added == list(range(t - j, t)), "O rescaled under a product")
+                S[t & 1], P[t & 1] = None, [t, None]
+                yield None
+                p_half[t & 1].arrive()
+                yield None
+                P[t & 1][1] = t
+                if mistake != "in turn":
+                    yield pv_done, t - 1
+                p_full.arrive()
+                t += 1
+            yield w("last", pv_done, t - 1)
+            need(added == list(range(t - n, t)), "O read before its last product")
+            yield None
+            need(added == list(range(t - n, t)), "O overwritten while it is read")
+
+    def land(_):
+        if not flying:
+            return False
+        kind, x, item = flying.pop(rnd.randrange(len(flying)))
+        code[item % ring] = (kind, x)
+        code_full[item % ring].arrive()
+        return True
+
+    late = []                                       # commits whose batches are done: they arrive in any order
+
+    def batch(_):
+        if late and (not pipe or rnd.random() < 0.6):
+            late.pop(rnd.randrange(len(late))).arrive()
+            return True
+        if not pipe:
+            return False
+        b = pipe.pop(0)
+        if b[0] == "commit":
+            late.append(b[1])
+        elif b[0] == "S":
+            _, x, seg = b
+            need(K[x % stages] == x and q[0] == seg, "S of other keys or rows")
+            need(S[x & 1] is None and P[x & 1] == [None, None], "S written before it was read, or over a P")
+            S[x & 1] = x
+        else:
+            _, x, h, first = b
+            need(P[x & 1][h] == x and V[0] == x, "PV of another tile")
+            P[x & 1][h] = None
+            if h:
+                added[:] = [x] if first else added + [x]
+        return True
+
+    schedule(rnd, [loader(), converters(), issuer(), softmax()], [land, batch])
+
+
+def _tiles(seed):
+    r = random.Random(2000 + seed)
+    return [r.choice([1, 1, 1, 2, 2, 3, 5, 12, 30]) for _ in range(r.randrange(1, 8))]
+
+
+def test_fp32_chunk_protocol_holds():
+    for seed in range(250):
+        run_chunks32(_tiles(seed), seed)
+
+
+@pytest.mark.parametrize("mistake", ["code_empty", "code_full", "k_empty", "k_full", "pv_done", "v_full", "q_empty",
+                                     "s_full", "p_half", "p_full", "rescale", "in turn", "last", "rows early"])
+def test_fp32_chunk_protocol_mistakes_are_caught(mistake):
+    caught = 0
+    for seed in range(300):
+        try:
+            run_chunks32(_tiles(seed), seed, mistake)
+        except ProtocolError:
+            caught += 1
+    assert caught > 0, mistake
+
+
+def test_fp32_issuers_wait_for_query_rows_is_implied():
+    # the converters write a segment's rows before its first K
+    for seed in range(200):
+        run_chunks32(_tiles(seed), seed, "q_full")
