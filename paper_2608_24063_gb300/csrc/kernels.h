@@ -162,7 +162,7 @@ struct RopeArgs {
 cudaError_t launch_mrope(const RopeArgs& a, int dtype, int d, bool adjacent, const void* q, void* q_out,
                          const void* k, void* k_out, cudaStream_t st);
 
-// 8-bit paged cache (kv8.cu, kv8_attn.cu, kv8_attn_tc.cu).  The device arrays
+// 8-bit paged cache (kv8.cu, kv8_attn.cu, kv8_attn_tc1.cu, kv8_attn_tc2.cu).  The device arrays
 // of vc_kv8 and vc_kv8_step are checked as they are read: lengths are clamped to
 // the block table, requests whose rows lie outside [0, n_rows] and pages outside
 // [0, n_pages) are skipped, and the call's status becomes VC_ERR_DEVICE_INDEX.
@@ -198,13 +198,13 @@ struct Kv8AttnArgs {
 };
 constexpr int kKv8MaxCtas = 160;       // blocks of an attention launch at most (152 SMs, rounded up)
 int kv8_sm_count();                    // SMs of the current device, at most kKv8MaxCtas
-int kv8_attn_rows_mma();               // most rows a unit of the two attention kernels
-int kv8_attn_rows_tc();
+int kv8_attn_rows_mma();               // most rows a unit of the attention kernels
+int kv8_attn_rows_tc2();
 cudaError_t launch_kv8_attn_mma(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8AttnArgs& a,
                                 cudaStream_t st);
-// the same on tcgen05: bf16 rows, many of them
-cudaError_t launch_kv8_attn_tc(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st);
-// fp32 rows, many of them
-cudaError_t launch_kv8_attn_tc32(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st);
+// the same on tcgen05: 128 rows a unit, or 256 of bf16
+cudaError_t launch_kv8_attn_tc1(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8AttnArgs& a,
+                                cudaStream_t st);
+cudaError_t launch_kv8_attn_tc2(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st);
 
 }  // namespace vc

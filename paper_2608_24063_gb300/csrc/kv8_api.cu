@@ -44,7 +44,7 @@ Kv8Ws kv8_ws(bool tc, int d) {
   Arena a;
   Kv8Ws w;
   a.take(kAlign);
-  const size_t rows = (size_t)2 * kKv8MaxCtas * (tc ? kv8_attn_rows_tc() : kv8_attn_rows_mma());
+  const size_t rows = (size_t)2 * kKv8MaxCtas * (tc ? kv8_attn_rows_tc2() : kv8_attn_rows_mma());
   w.o_blocks = a.take(sizeof(int32_t) * kKv8MaxCtas);      // at byte 256: prunekv_get_status reads it there
   w.o_flags = a.take(sizeof(uint64_t) * 2 * kKv8MaxCtas * 2);
   w.o_ml = a.take(sizeof(float2) * rows);
@@ -66,26 +66,35 @@ uint64_t next_token() {
   return z ? z : 1;
 }
 
-// Whether a call's rows (bf16) run on tcgen05: more than kTcRows packed rows of
-// a KV head per request on average, so more than two 16-row units of the other
-// kernel, and enough of those units that they do not get a few blocks each.
-// That kernel's time goes with units * tiles, this one's begins at 20 us (one
-// block's chain of a tile, and pieces to add up) and then goes with the tiles.
-// d = 128, 8 KV heads, us on mma.sync / on tcgen05:
-//   64 requests of 4096 tokens, 32 rows 248 / 217, 48 rows 364 / 226, 256 rows 1848 / 329
-//   8 of 600 tokens, 32 rows 13.4 / 21.8, 48 rows 30 / 23
-//   one of 32768 tokens, 36 rows 52 / 48, 64 rows 70 / 48
-//   one of 2000 tokens, 48 rows 16.6 / 25.1, 256 rows 25.9 / 49.1
-// Lengths are on the device, so the block table's width stands for them.
-constexpr int64_t kTcRows = 32, kTcShare = 16;
+// The kernel of a call.  On tcgen05 (tc1): more than kTcRows packed rows of a KV
+// head per request on average, so at least two 16-row units of the mma.sync kernel,
+// and more of those units than SMs, or of their tiles than kTcShare an SM: below
+// that every unit there gets blocks of its own.  With 256-row units (tc2): bf16, at
+// least kTc2Rows such rows, kTc2Tiles tiles and more than kTc2Share tiles of those
+// units an SM: its segments cost more at their ends.  Lengths are on the device, so
+// the block table's width stands for them.
+// d = 128, 8 KV heads, us on mma.sync / tc1:
+//   64 requests of 4096 tokens, 16 rows 135 / 147, 20 rows 246 / 149, 128 rows 933 / 178
+//   8 of 600 tokens, 24 rows 13.2 / 15.8, 48 rows 29.6 / 17.0
+//   one of 8192 tokens, 20 rows 20.3 / 19.6, 128 rows 42.4 / 34.4
+//   fp32: one of 2000 tokens, 128 rows 24.7 / 35.3; 8 of 4096, 24 rows 47.9 / 43.9, 256 rows 308 / 81
+// on tc1 / tc2:
+//   one of 32768 tokens, 320 rows 71 / 92, 512 rows 93.7 / 92.5, 8192 rows 988 / 739
+//   one of 8192 tokens, 1024 rows 54.4 / 58.1, 2048 rows 85.7 / 80.8
+//   one of 4096 tokens, 8192 rows 148 / 156; 64 of 1000, 1024 rows 499 / 611
+constexpr int64_t kTcRows = 16, kTcShare = 8, kTc2Rows = 512, kTc2Tiles = 64, kTc2Share = 16;
+enum class Kernel { kMma, kTc1, kTc2 };
 bool may_have_many_rows(int64_t n_rows, int64_t n_req, int32_t Hq, int32_t Hkv) {
   return n_rows * (Hq / Hkv) > kTcRows * n_req;
 }
-bool many_rows(const vc_kv8& c, const vc_kv8_step& s, int32_t Hq) {
-  if (!may_have_many_rows(s.n_rows, s.n_req, Hq, c.Hkv)) return false;
-  const int64_t units = (int64_t)s.n_rows * Hq / 16, sms = kv8_sm_count();
+Kernel kernel_of(const vc_kv8& c, const vc_kv8_step& s, int dtype, int32_t Hq) {
+  if (!may_have_many_rows(s.n_rows, s.n_req, Hq, c.Hkv)) return Kernel::kMma;
+  const int64_t rows = (int64_t)s.n_rows * Hq, sms = kv8_sm_count();
   const int64_t tiles = ((int64_t)s.max_pages * c.page + 127) / 128;
-  return units > sms || units * tiles > kTcShare * sms;
+  if (rows / 16 <= sms && rows / 16 * tiles <= kTcShare * sms) return Kernel::kMma;
+  const bool two = dtype == VC_BF16 && rows / c.Hkv >= kTc2Rows * s.n_req && tiles >= kTc2Tiles &&
+                   rows / 256 * tiles > kTc2Share * sms;
+  return two ? Kernel::kTc2 : Kernel::kTc1;
 }
 
 bool valid_heads(int32_t Hq, int32_t Hkv) { return Hkv >= 1 && Hq >= Hkv && Hq <= 4096 && Hq % Hkv == 0; }
@@ -206,8 +215,8 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
   const int64_t row_tiles = (int64_t)step->n_rows * (Hq / cache->Hkv) / 8 + step->n_req;
   if (row_tiles * cache->Hkv > ((int64_t)1 << 37) / (((int64_t)step->max_pages * cache->page + 127) / 128))
     return VC_ERR_UNSUPPORTED;
-  const bool tc = many_rows(*cache, *step, Hq);
-  const Kv8Ws w = kv8_ws(tc, cache->d);
+  const Kernel kernel = kernel_of(*cache, *step, dtype, Hq);
+  const Kv8Ws w = kv8_ws(kernel != Kernel::kMma, cache->d);
   const int wc = check_ws(ws, ws_bytes, w.total);
   if (wc != VC_OK) return wc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -227,9 +236,9 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
   a.flags = reinterpret_cast<uint64_t*>(base + w.o_flags);
   a.part_ml = reinterpret_cast<float2*>(base + w.o_ml);
   a.part_o = reinterpret_cast<float*>(base + w.o_o);
-  if (!tc) return cuda_status(launch_kv8_attn_mma(*cache, *step, dtype, a, st));
-  return cuda_status(dtype == VC_BF16 ? launch_kv8_attn_tc(*cache, *step, a, st)
-                                      : launch_kv8_attn_tc32(*cache, *step, a, st));
+  return cuda_status(kernel == Kernel::kMma   ? launch_kv8_attn_mma(*cache, *step, dtype, a, st)
+                     : kernel == Kernel::kTc1 ? launch_kv8_attn_tc1(*cache, *step, dtype, a, st)
+                                              : launch_kv8_attn_tc2(*cache, *step, a, st));
 }
 
 }  // extern "C"

@@ -1,35 +1,47 @@
-// Attention over the 8-bit paged cache, many query rows a request, fp32 rows
-// (viscache_kv8_attention on tcgen05).
+// Attention over the 8-bit paged cache, many query rows a request
+// (viscache_kv8_attention on tcgen05): 128 rows a unit, bf16 or fp32.
 //
-// fp32 rows and probabilities enter the products as sums of two fp16 numbers (22
-// bits), so a tile costs twice what it does with 16-bit rows, and both K and V are
-// expanded to fp16 (exact).  A unit has 128 packed query rows (one TMEM lane a
-// row) over tiles of 128 tokens: 8 * 128 * 128 * d flops a tile, bound by the
-// tensor cores.  Two parts of 256 rows would not fit beside the expanded tiles;
-// with one row tile the softmax of a tile runs while the next tile's S does, from
-// the other of two S buffers.  Persistent blocks, one per SM, share out the line
-// of key tiles (kv8_sched.cuh).
+// A unit has 128 packed query rows (one TMEM lane a row) over tiles of 128 tokens.
+// A tile's scores come from one of two S buffers, so its softmax runs while the
+// next tile's products do.  Persistent blocks, one per SM, share out the line of
+// key tiles (kv8_sched.cuh).
+//
+// bf16 rows.  S = Q K^T runs on the codes as they are (kind::f8f6f4): a bf16
+// number has 8 significant bits and an e4m3 number 4, so a query value is exactly
+// the sum of two e4m3 numbers, its rounding and the rest (values below 2^-9 of
+// their row's largest are off by up to 2^-17 of it: the largest lies in [128, 256)
+// and e4m3 ends at steps of 2^-9).  Two products at twice the rate cost what one
+// fp16 product does, and K needs no expansion: TMA writes its tiles.  O = P V runs
+// in fp16: P needs more than e4m3's range, so V is expanded.
+// fp32 rows.  Rows and probabilities are sums of two fp16 numbers (22 bits), and K
+// and V are both expanded to fp16 (exact), K a tile ahead of V.
 //
 // Warps (512 threads, register shares set per warpgroup):
 //   0-3    softmax, one thread a row
-//   4-11   converters: K and V codes from the staging ring, e4m3 -> fp16, into
+//   4-11   converters: codes from the staging ring, e4m3 -> fp16, into
 //          128-byte-swizzled tiles; the unit's query rows too
 //   12     MMA issuer
-//   13     loader: page numbers, scales, a bulk copy per page
-// Tensor memory: S_0, S_1 (128 columns each; P over them, its larger parts in the
-// first 64 columns and the rest in the others), O.  Order of issue:
+//   13     loader: page numbers, scales, a TMA box (K, bf16 rows) or a bulk copy
+//          per page
+// Tensor memory: S_0, S_1 (128 columns each; P over them: fp16 pairs in the first
+// 64 columns, of fp32 calls the rest of each in the others), O.  Order of issue:
 //   S(0) S(1) PV(0) S(2) PV(1) ...
-// and the codes come in the same order (K one tile ahead of V).  MMAs of one
-// thread execute in order, so S(t+2) may overwrite the P(t) that PV(t) reads.  P
-// arrives in two halves.
+// MMAs of one thread execute in order, so S(t+2) may overwrite the P(t) that PV(t)
+// reads.  P arrives in two halves: the first half's products run while the second's
+// exponentials do.
 //
 // Numbers: query rows are scaled by a power of two to a largest magnitude in
-// [2^14, 2^15), so their parts keep 2^-39 of it.  Scores are scaled by their page's
-// K scale in fp32.  V codes are multiplied by their page's scale over the tile's
-// largest one (exact but for pages 2^-15 of their tile).  A row's maximum may be
-// passed by 2^2 before O is rescaled; P = 2^(x - m + 12) times (V scale of the tile
-// / the largest so far), at most 2^14, keeps 22 bits down to 2^-25 of its
-// reference.  Row sums are fp32, of unrounded terms.
+// [128, 256), of fp32 calls in [2^14, 2^15) (their parts keep 2^-39 of it).  Scores
+// are scaled by their page's K scale in fp32.  V codes are multiplied by their
+// page's scale over the tile's largest one (exact but for pages 2^-15 of their
+// tile).  A row's maximum may be passed by 2^10 (fp32: 2^2) before O is rescaled;
+// P = 2^(x - m + 4) (fp32: + 12) times (V scale of the tile / the largest so far),
+// at most 2^14, keeps 11 bits down to 2^-18 of its reference (fp32: 22 bits down
+// to 2^-25).  Row sums are fp32, of unrounded terms.
+//
+// Bound by the softmax's chain: one tile takes about 2200 clocks (its products
+// 1024).  64 requests of 128 rows over 4096 tokens, 8 KV heads of 128: 177 us, 3.0
+// TB/s of codes; fp32 315 us.  Long chunks: kv8_attn_tc2.cu.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_sched.cuh"
@@ -47,24 +59,31 @@ using namespace tc;
 constexpr int kTcThreads = 512;
 constexpr int kTcMT = 128, kTcKT = 128;
 constexpr int kConvWarp0 = 4, kConvWarps = 8, kIssueWarp = 12, kLoadWarp = 13;
-constexpr float kTcSlack = 2.f;                 // log2 units
-constexpr int kTcPExp = 12;
 constexpr uint32_t kSCol = 0, kOCol = 256;
-constexpr int kKStages = 2, kCodeStages = 4;
 constexpr int kRefs = 8;                        // tiles whose scales are kept (the loader is at most 5 ahead)
 
-template <int D>
-struct Tc32Smem {
-  uint8_t q[2][D / 64][kBlk];                   // query rows of the unit, [larger part, rest][64-column block]
-  uint8_t k[kKStages][D / 64][kBlk];            // K as fp16
-  uint8_t v[D / 64][kBlk];                      // V as fp16
-  uint8_t code[kCodeStages][kTcKT * D];         // codes as they are in the cache: K, K, V, K, V, ...
+template <typename T, int D>
+struct Cfg {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr float SLACK = F32 ? 2.f : 10.f;          // log2 units
+  static constexpr int PEXP = F32 ? 12 : 4;
+  static constexpr int QPART = F32 ? kTcMT * D * 2 : kTcMT * D, KTILE = F32 ? kTcKT * D * 2 : kTcKT * D;
+  static constexpr int KS = F32 ? 2 : 3, VS = F32 ? 1 : 2, CS = F32 ? 4 : 3;
+};
+
+template <typename T, int D>
+struct Tc1Smem {
+  using C = Cfg<T, D>;
+  uint8_t q[2][C::QPART];                       // query rows of the unit, [larger part, rest]: fp16 or e4m3
+  uint8_t k[C::KS][C::KTILE];                   // K as fp16, or its codes
+  uint8_t v[C::VS][D / 64][kBlk];               // V as fp16, [stage][64-column block]
+  uint8_t code[C::CS][kTcKT * D];               // codes as they are in the cache: K, K, V, K, V, ..., or V
   float qs[kTcMT];                              // power of two of each query row
   float kscale[kRefs][8];                       // K scale of each 16-token group of tile t, at t % kRefs
   float vshare[kRefs][8];                       // V scale of each group over the tile's largest
   float vref[kRefs];                            // the tile's largest V scale
-  uint64_t q_full, q_empty, k_full[kKStages], k_empty[kKStages], v_full, pv_done;
-  uint64_t code_full[kCodeStages], code_empty[kCodeStages], ref_full[kRefs];
+  uint64_t q_full, q_empty, k_full[C::KS], k_empty[C::KS], v_full[C::VS], v_empty[C::VS], pv_done;
+  uint64_t code_full[C::CS], code_empty[C::CS], ref_full[kRefs];
   uint64_t s_full[2], p_half[2], p_full, done;
   int64_t scan[kTcThreads / 32];
   Share share;
@@ -73,12 +92,34 @@ struct Tc32Smem {
   int32_t err;                                  // the block's status
 };
 
-template <int D>
-__global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __grid_constant__ vc_kv8 c,
+// Eight values of a query row.
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const float4 x0 = __ldg(reinterpret_cast<const float4*>(p)), x1 = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  x[0] = x0.x; x[1] = x0.y; x[2] = x0.z; x[3] = x0.w;
+  x[4] = x1.x; x[5] = x1.y; x[6] = x1.z; x[7] = x1.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
+  const uint4 y = __ldg(reinterpret_cast<const uint4*>(p));
+  const uint32_t b[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(b[e] << 16);
+    x[2 * e + 1] = __uint_as_float(b[e] & 0xffff0000u);
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __grid_constant__ CUtensorMap tmK,
+                                                                      const __grid_constant__ vc_kv8 c,
                                                                       const __grid_constant__ vc_kv8_step s,
                                                                       const __grid_constant__ Kv8AttnArgs a) {
+  using C = Cfg<T, D>;
+  constexpr bool F32 = C::F32;
+  constexpr int kKStages = C::KS, kVStages = C::VS, kCodeStages = C::CS;
+  constexpr float kTcSlack = C::SLACK;
+  constexpr int kTcPExp = C::PEXP;
   extern __shared__ uint8_t smem_raw[];
-  Tc32Smem<D>& sm = *reinterpret_cast<Tc32Smem<D>*>(align1024(smem_raw));
+  Tc1Smem<T, D>& sm = *reinterpret_cast<Tc1Smem<T, D>*>(align1024(smem_raw));
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (warp: uniform)
   const int G = a.Hq / c.Hkv;
   const Line<kTcMT, kTcKT> line{c.Hkv, G, c.page, a.causal};
@@ -86,10 +127,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
     mbar_init(&sm.q_full, kConvWarps);
     mbar_init(&sm.q_empty, 1);
     for (int i = 0; i < kKStages; ++i) {
-      mbar_init(&sm.k_full[i], kConvWarps);
+      mbar_init(&sm.k_full[i], F32 ? kConvWarps : 1);
       mbar_init(&sm.k_empty[i], 1);
     }
-    mbar_init(&sm.v_full, kConvWarps);
+    for (int i = 0; i < kVStages; ++i) {
+      mbar_init(&sm.v_full[i], kConvWarps);
+      mbar_init(&sm.v_empty[i], 1);
+    }
     mbar_init(&sm.pv_done, 1);
     for (int i = 0; i < kCodeStages; ++i) {
       mbar_init(&sm.code_full[i], 1);
@@ -133,20 +177,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == kIssueWarp) {
       // ---- MMA issuer
-      constexpr uint32_t id_s = idesc_f16(128, kTcKT), id_o = idesc_f16_bmn(128, D);
+      constexpr uint32_t id_s = F32 ? idesc_f16(128, kTcKT) : idesc_e4m3(128, kTcKT), id_o = idesc_f16_bmn(128, D);
       bool ok = true;
-      const uint64_t qd = desc_sw128(smem_u32(sm.q)), kd = desc_sw128(smem_u32(sm.k));
+      const uint64_t qd = F32 ? desc_sw128(smem_u32(sm.q)) : desc_codes<D>(smem_u32(sm.q));
+      const uint64_t kd = F32 ? desc_sw128(smem_u32(sm.k)) : desc_codes<D>(smem_u32(sm.k));
       const uint64_t vd = desc_sw128_mn(smem_u32(sm.v), kBlk);
       // descriptors hold addresses in units of 16 bytes
-      constexpr uint32_t kTile16 = sizeof(sm.v) / 16, kBlk16 = kBlk / 16;
-      auto issue_pv = [&](uint32_t s_col, int kk0, bool first) {
+      constexpr uint32_t kV16 = sizeof(sm.v[0]) / 16, kK16 = C::KTILE / 16, kQ16 = C::QPART / 16, kBlk16 = kBlk / 16;
+      auto issue_pv = [&](uint32_t s_col, uint64_t bd, int kk0, bool first) {
         tc_fence_after();
         __syncwarp();
 #pragma unroll
         for (int k = 0; k < kTcKT / 32; ++k) {
           const int kk = kk0 + k;
-          mma_f16_ts(tbase + kOCol, s_col + kk * 8, vd + kk * 2048 / 16, id_o, (!first || k) ? 1u : 0u);
-          mma_f16_ts(tbase + kOCol, s_col + 64 + kk * 8, vd + kk * 2048 / 16, id_o, 1u);
+          mma_f16_ts(tbase + kOCol, s_col + kk * 8, bd + kk * 2048 / 16, id_o, (!first || k) ? 1u : 0u);
+          if (F32) mma_f16_ts(tbase + kOCol, s_col + 64 + kk * 8, bd + kk * 2048 / 16, id_o, 1u);
         }
       };
       do {
@@ -158,27 +203,37 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
             if (!ok) break;
             tc_fence_after();
             __syncwarp();
+            const uint32_t d = tbase + kSCol + (tk & 1) * kTcKT;
+            const uint64_t bd = kd + (uint32_t)ks * kK16;
+            if constexpr (F32) {
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+              for (int part = 0; part < 2; ++part)
 #pragma unroll
-              for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t at = (kk >> 2) * kBlk16 + (kk & 3) * 2;
-                mma_f16_ss(tbase + kSCol + (tk & 1) * kTcKT, qd + part * kTile16 + at, kd + (uint32_t)ks * kTile16 + at,
-                           id_s, (part || kk) ? 1u : 0u);
-              }
+                for (int kk = 0; kk < D / 16; ++kk) {
+                  const uint32_t at = (kk >> 2) * kBlk16 + (kk & 3) * 2;
+                  mma_f16_ss(d, qd + part * kQ16 + at, bd + at, id_s, (part || kk) ? 1u : 0u);
+                }
+            } else {
+#pragma unroll
+              for (int kk = 0; kk < 2 * (D / 32); ++kk)
+                mma_e4m3_ss(d, qd + (kk & 1) * kQ16 + (kk >> 1) * 2, bd + (kk >> 1) * 2, id_s, kk ? 1u : 0u);
+            }
             mma_commit_elected(&sm.s_full[tk & 1]);
             mma_commit_elected(&sm.k_empty[ks]);
           }
           if (j > w.t0) {
             const int tv = t + j - 1 - w.t0;
             const uint32_t s_col = tbase + kSCol + (tv & 1) * kTcKT;
-            ok = warp_wait(&sm.v_full, tv & 1, abort) && warp_wait(&sm.p_half[tv & 1], (tv >> 1) & 1, abort);
+            const int vs = tv % kVStages;
+            const uint64_t bd = vd + (uint32_t)vs * kV16;
+            ok = warp_wait(&sm.v_full[vs], (tv / kVStages) & 1, abort) && warp_wait(&sm.p_half[tv & 1], (tv >> 1) & 1, abort);
             if (!ok) break;
-            issue_pv(s_col, 0, j - 1 == w.t0);
+            issue_pv(s_col, bd, 0, j - 1 == w.t0);
             ok = warp_wait(&sm.p_full, tv & 1, abort);
             if (!ok) break;
-            issue_pv(s_col, kTcKT / 32, false);
+            issue_pv(s_col, bd, kTcKT / 32, false);
             mma_commit_elected(&sm.pv_done);
+            mma_commit_elected(&sm.v_empty[vs]);
           }
         }
         // (after the last PV: the softmax has read the rows' powers of two)
@@ -198,7 +253,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
       const int bt = lane / ppt, bp = lane % ppt;
       const uint32_t page_bytes = (uint32_t)c.page * D;
       bool ok = true;
-      int item = 0;                             // code tiles under way or landed
+      int item = 0, nk = 0;                     // code tiles (and K tiles) under way or landed
+      if (!F32) prefetch_tmap(&tmK);
       // the code tile of the pages that the lanes with `mine` hold
       auto put = [&](const void* codes, bool mine, int pid) {
         const int st = item % kCodeStages;
@@ -237,7 +293,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
             const int rt = t % kRefs;
             // (what reads this place's scales is done: the codes of the tile 2 before are expanded
             // once the PV of the one 5 before is)
-            ok = warp_wait(&sm.code_empty[item % kCodeStages], ((item / kCodeStages) & 1) ^ 1, abort);
+            ok = F32 ? warp_wait(&sm.code_empty[item % kCodeStages], ((item / kCodeStages) & 1) ^ 1, abort)
+                     : warp_wait(&sm.k_empty[t % kKStages], ((t / kKStages) & 1) ^ 1, abort);
             if (!ok) break;
             if (bt == i) {
               if (bp == 0) sm.vref[rt] = vref;
@@ -248,14 +305,26 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm.ref_full[rt]);
-            put(c.K_codes, bt == i && live, pid);
-            if (ok && tb + i > w.t0) {
-              if (i > 0) put(c.V_codes, bt == i - 1 && live, pid);
-              else put(c.V_codes, bt == tpb - 1 && plive, ppid);
+            if constexpr (F32) {
+              put(c.K_codes, bt == i && live, pid);
+              if (ok && tb + i > w.t0) {
+                if (i > 0) put(c.V_codes, bt == i - 1 && live, pid);
+                else put(c.V_codes, bt == tpb - 1 && plive, ppid);
+              }
+            } else {
+              const int kst = t % kKStages;
+              const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, bt == i && live)) * page_bytes;
+              if (lane == 0) mbar_arrive_expect_tx(&sm.k_full[kst], bytes);
+              ++nk;
+              __syncwarp();
+              if (bt == i && live)
+                tma_load_2d(sm.k[kst] + bp * page_bytes, &tmK, 0, (max(pid, 0) * c.Hkv + w.u.g) * c.page,
+                            &sm.k_full[kst]);
+              put(c.V_codes, bt == i && live, pid);
             }
             if (!ok) break;
           }
-          if (ok && tb + nt == w.t1) put(c.V_codes, bt == nt - 1 && live, pid);
+          if (F32 && ok && tb + nt == w.t1) put(c.V_codes, bt == nt - 1 && live, pid);
           ppid = pid;
           plive = live;
           pid = npid;
@@ -266,9 +335,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
       } while (ok && w.next(line, s, err));
       // every copy has landed before the block may end
       __syncwarp();
-      if (lane == 0)
+      if (lane == 0) {
+        for (int i = max(0, nk - kKStages); i < nk; ++i) drain_wait(&sm.k_full[i % kKStages], (i / kKStages) & 1);
         for (int i = max(0, item - kCodeStages); i < item; ++i)
           drain_wait(&sm.code_full[i % kCodeStages], (i / kCodeStages) & 1);
+      }
     }
   } else if (warp >= kConvWarp0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
@@ -292,32 +363,52 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
           for (int e = 0; e < 8; ++e) x[e] = 0.f;
           if (r < rows) {
             const int rho = w.u.rt * kTcMT + r, qi = rho / G, qj = rho - qi * G;
-            const float4* src =
-                reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (int64_t)(w.u.q.row0 + qi) * a.q_stride +
-                                                (int64_t)(w.u.g * G + qj) * D + qc * 8);
-            const float4 x0 = __ldg(src), x1 = __ldg(src + 1);
-            x[0] = x0.x; x[1] = x0.y; x[2] = x0.z; x[3] = x0.w;
-            x[4] = x1.x; x[5] = x1.y; x[6] = x1.z; x[7] = x1.w;
+            load8(static_cast<const T*>(a.q) + (int64_t)(w.u.q.row0 + qi) * a.q_stride +
+                      (int64_t)(w.u.g * G + qj) * D + qc * 8, x);
           }
           float amax = 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
 #pragma unroll
           for (int o = QL / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-          // largest magnitude to [2^14, 2^15); zero, tiny or not finite rows as they are
+          // largest magnitude to [2^14, 2^15) or [2^7, 2^8); zero, tiny or not finite rows as they are
+          constexpr uint32_t kUp = (F32 ? 14u : 7u) << 23;
           const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
-          const float qs = ex <= (14u << 23) || ex == 0x7f800000u ? 1.f : __uint_as_float(ex - (14u << 23));
+          const float qs = ex <= kUp || ex == 0x7f800000u ? 1.f : __uint_as_float(ex - kUp);
           const float inv = pow2_inverse(qs);
-          uint32_t top[4], rest[4];
+          if constexpr (F32) {
+            uint32_t top[4], rest[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float z0 = x[2 * e] * inv, z1 = x[2 * e + 1] * inv;
-            top[e] = half2_bits(z0, z1);
-            rest[e] = half2_rest(z0, z1, top[e]);
+            for (int e = 0; e < 4; ++e) {
+              const float z0 = x[2 * e] * inv, z1 = x[2 * e + 1] * inv;
+              top[e] = half2_bits(z0, z1);
+              rest[e] = half2_rest(z0, z1, top[e]);
+            }
+            const uint32_t off = (uint32_t)((qc >> 3) * kBlk + r * 128 + (((qc & 7) ^ (r & 7)) << 4));
+            *reinterpret_cast<uint4*>(sm.q[0] + off) = make_uint4(top[0], top[1], top[2], top[3]);
+            *reinterpret_cast<uint4*>(sm.q[1] + off) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+          } else {
+            uint32_t top[2], rest[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float z[4], r4[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                z[k] = x[4 * e + k] * inv;
+                if (!(fabsf(z[k]) <= 448.f)) z[k] = __uint_as_float(0x7fffffffu);      // NaN, infinite
+              }
+              const uint32_t p0 = f32x2_to_e4m3x2(z[0], z[1]), p1 = f32x2_to_e4m3x2(z[2], z[3]);
+              const uint32_t h0 = e4m3x2_to_f16x2(p0), h1 = e4m3x2_to_f16x2(p1);
+              const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0));
+              const float2 f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+              r4[0] = z[0] - f0.x; r4[1] = z[1] - f0.y; r4[2] = z[2] - f1.x; r4[3] = z[3] - f1.y;
+              top[e] = p0 | p1 << 16;
+              rest[e] = f32x2_to_e4m3x2(r4[0], r4[1]) | f32x2_to_e4m3x2(r4[2], r4[3]) << 16;
+            }
+            const uint32_t off = code_piece<D>(r, qc);
+            *reinterpret_cast<uint2*>(sm.q[0] + off) = make_uint2(top[0], top[1]);
+            *reinterpret_cast<uint2*>(sm.q[1] + off) = make_uint2(rest[0], rest[1]);
           }
-          const uint32_t off = (uint32_t)((qc >> 3) * kBlk + r * 128 + (((qc & 7) ^ (r & 7)) << 4));
-          *reinterpret_cast<uint4*>(sm.q[0][0] + off) = make_uint4(top[0], top[1], top[2], top[3]);
-          *reinterpret_cast<uint4*>(sm.q[1][0] + off) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
           if (qc == 0) sm.qs[r] = qs;
         }
       }
@@ -325,7 +416,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full);
       for (int j = w.t0; ok && j <= w.t1; ++j) {
-        if (j < w.t1) {                         // K of tile j
+        if (F32 && j < w.t1) {                  // K of tile j
           const int tk = t + j - w.t0, ks = tk % kKStages, st = item % kCodeStages;
           ok = warp_wait(&sm.code_full[st], (item / kCodeStages) & 1, abort) &&
                warp_wait(&sm.k_empty[ks], ((tk / kKStages) & 1) ^ 1, abort);
@@ -333,7 +424,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
 #pragma unroll
           for (int n = 0; n < 128 / RP; ++n) {
             const int key = key0 + RP * n;
-            expand16(sm.k[ks][0], key, ch, *reinterpret_cast<const uint4*>(sm.code[st] + key * D + ch * 16), 1.f);
+            expand16(sm.k[ks], key, ch, *reinterpret_cast<const uint4*>(sm.code[st] + key * D + ch * 16), 1.f);
           }
           fence_proxy_async();
           __syncwarp();
@@ -344,10 +435,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
           ++item;
         }
         if (j > w.t0) {                         // V of tile j - 1
-          const int tv = t + j - 1 - w.t0, st = item % kCodeStages;
+          const int tv = t + j - 1 - w.t0, vs = tv % kVStages, st = item % kCodeStages;
           const int left = w.u.kend - (j - 1) * kTcKT;            // tokens of the tile
           ok = warp_wait(&sm.code_full[st], (item / kCodeStages) & 1, abort) &&
-               warp_wait(&sm.pv_done, (tv & 1) ^ 1, abort);
+               warp_wait(&sm.v_empty[vs], ((tv / kVStages) & 1) ^ 1, abort);
           if (!ok) break;
           const float* share = sm.vshare[tv % kRefs];
 #pragma unroll
@@ -355,13 +446,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
             const int key = key0 + RP * n;
             uint4 y = *reinterpret_cast<const uint4*>(sm.code[st] + key * D + ch * 16);
             if (key >= left) y = make_uint4(0u, 0u, 0u, 0u);      // not a token: whatever was there
-            expand16(sm.v[0], key, ch, y, share[key >> 4]);
+            expand16(sm.v[vs][0], key, ch, y, share[key >> 4]);
           }
           fence_proxy_async();
           __syncwarp();
           if (lane == 0) {
             mbar_arrive(&sm.code_empty[st]);
-            mbar_arrive(&sm.v_full);
+            mbar_arrive(&sm.v_full[vs]);
           }
           ++item;
         }
@@ -478,10 +569,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
             if (q & 1) l1 = __fadd2_rn(l1, e);
             else l0 = __fadd2_rn(l0, e);
             top[q] = half2_bits(e.x, e.y);
-            rest[q] = half2_rest(e.x, e.y, top[q]);
+            if (F32) rest[q] = half2_rest(e.x, e.y, top[q]);
           }
           tmem_st16(s_col + h * 16, top);
-          tmem_st16(s_col + 64 + h * 16, rest);
+          if (F32) tmem_st16(s_col + 64 + h * 16, rest);
           if (h == 1) {                         // the first half may be multiplied
             tmem_wait_st();
             tc_fence_before();
@@ -508,10 +599,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
       const bool whole = w.whole();
       const int64_t at = (int64_t)(w.u.q.row0 + qi) * a.Hq + w.u.g * G + qj;
       auto put_out = [&](int64_t at, int col, const float (&y)[16], float inv) {
-        float4* dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at * D + col);
+        T* dst = static_cast<T*>(a.out) + at * D + col;
+        if constexpr (F32) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          dst[q] = make_float4(y[4 * q] * inv, y[4 * q + 1] * inv, y[4 * q + 2] * inv, y[4 * q + 3] * inv);
+          for (int q = 0; q < 16; q += 4)
+            *reinterpret_cast<float4*>(dst + q) =
+                make_float4(y[q] * inv, y[q + 1] * inv, y[q + 2] * inv, y[q + 3] * inv);
+        } else {
+          uint32_t b8[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const __nv_bfloat162 b2 = __floats2bfloat162_rn(y[2 * q] * inv, y[2 * q + 1] * inv);
+            b8[q] = *reinterpret_cast<const uint32_t*>(&b2);
+          }
+          *reinterpret_cast<uint4*>(dst) = make_uint4(b8[0], b8[1], b8[2], b8[3]);
+          *reinterpret_cast<uint4*>(dst + 8) = make_uint4(b8[4], b8[5], b8[6], b8[7]);
+        }
       };
       auto put_lse = [&](int64_t at, float M, float L) {
         if (a.lse) a.lse[at] = L == 0.f ? -INFINITY : fmaf(M, 0.6931471805599453f, logf(L));
@@ -575,30 +678,35 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc32_kernel(const __gr
   if (threadIdx.x == 0) store_status(a, sm.abort ? VC_ERR_DEVICE_TIMEOUT : sm.err);
 }
 
-template <int D>
+template <typename T, int D>
 cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
-  constexpr size_t smem = sizeof(Tc32Smem<D>) + 1024;
+  constexpr size_t smem = sizeof(Tc1Smem<T, D>) + 1024;
   static_assert(smem <= 232448, "shared memory of a block");
   static std::atomic<bool> attr{false};
   if (!attr.load(std::memory_order_relaxed)) {
-    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_tc32_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_tc1_kernel<T, D>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     attr.store(true, std::memory_order_relaxed);
   }
+  CUtensorMap mk = {};
+  if (!Cfg<T, D>::F32 && !kv8_pool_map(&mk, c.K_codes, c)) return cudaErrorInvalidValue;
   const int64_t G = a.Hq / c.Hkv;
   const int64_t units = ((int64_t)s.n_rows * G / kTcMT + (s.n_req < s.n_rows ? s.n_req : s.n_rows)) * c.Hkv;
   const int64_t tiles = units * (((int64_t)s.max_pages * c.page + kTcKT - 1) / kTcKT);
   const int64_t sms = kv8_sm_count();
-  ProfileScope ps("kv8_attn_tc32", st);
-  kv8_attn_tc32_kernel<D><<<(unsigned)(tiles < sms ? tiles : sms), kTcThreads, smem, st>>>(c, s, a);
+  ProfileScope ps("kv8_attn_tc1", st);
+  kv8_attn_tc1_kernel<T, D><<<(unsigned)(tiles < sms ? tiles : sms), kTcThreads, smem, st>>>(mk, c, s, a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_kv8_attn_tc32(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
-  return c.d == 128 ? launch_t<128>(c, s, a, st) : launch_t<64>(c, s, a, st);
+cudaError_t launch_kv8_attn_tc1(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8AttnArgs& a,
+                                cudaStream_t st) {
+  if (dtype == VC_BF16)
+    return c.d == 128 ? launch_t<__nv_bfloat16, 128>(c, s, a, st) : launch_t<__nv_bfloat16, 64>(c, s, a, st);
+  return c.d == 128 ? launch_t<float, 128>(c, s, a, st) : launch_t<float, 64>(c, s, a, st);
 }
 
 }  // namespace vc

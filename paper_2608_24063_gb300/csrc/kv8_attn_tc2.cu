@@ -1,5 +1,12 @@
-// Attention over the 8-bit paged cache, many query rows a request, bf16 rows
-// (viscache_kv8_attention on tcgen05).
+// Attention over the 8-bit paged cache, long chunks of bf16 query rows
+// (viscache_kv8_attention on tcgen05): 256 rows a unit.
+//
+// Where there is work for every SM, two row tiles share a tile's expansion and each
+// other's waits: a chunk of 2048 rows over 32768 tokens (64 query heads, 8 KV heads
+// of 128) takes 1430 us, 1.49 PFLOP/s, against 1914 us with one row tile; 512 rows tie.  Bound by
+// a row tile's chain (scores, softmax, products) and the tensor cores about equally:
+// without exponentials, maxima and expansion it would take 1255 us, the products
+// alone 1111.
 //
 // A unit has 256 packed query rows (two tiles of 128 rows, one TMEM lane a row)
 // over tiles of 128 tokens: 4 * 256 * 128 * d flops a tile, so it is bound by
@@ -83,7 +90,7 @@ struct TcSmem {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK,
+__global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __grid_constant__ CUtensorMap tmK,
                                                                     const __grid_constant__ vc_kv8 c,
                                                                     const __grid_constant__ vc_kv8_step s,
                                                                     const __grid_constant__ Kv8AttnArgs a) {
@@ -608,7 +615,7 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
   constexpr size_t smem = sizeof(TcSmem<D>) + 1024;
   static std::atomic<bool> attr{false};
   if (!attr.load(std::memory_order_relaxed)) {
-    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_tc2_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                (int)smem);
     if (e != cudaSuccess) return e;
     attr.store(true, std::memory_order_relaxed);
@@ -619,16 +626,16 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
   const int64_t units = ((int64_t)s.n_rows * G / kTcMT + (s.n_req < s.n_rows ? s.n_req : s.n_rows)) * c.Hkv;
   const int64_t tiles = units * (((int64_t)s.max_pages * c.page + kTcKT - 1) / kTcKT);
   const int64_t sms = kv8_sm_count();
-  ProfileScope ps("kv8_attn_tc", st);
-  kv8_attn_tc_kernel<D><<<(unsigned)(tiles < sms ? tiles : sms), kTcThreads, smem, st>>>(mk, c, s, a);
+  ProfileScope ps("kv8_attn_tc2", st);
+  kv8_attn_tc2_kernel<D><<<(unsigned)(tiles < sms ? tiles : sms), kTcThreads, smem, st>>>(mk, c, s, a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-int kv8_attn_rows_tc() { return kTcMT; }
+int kv8_attn_rows_tc2() { return kTcMT; }
 
-cudaError_t launch_kv8_attn_tc(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
+cudaError_t launch_kv8_attn_tc2(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
   return c.d == 128 ? launch_t<128>(c, s, a, st) : launch_t<64>(c, s, a, st);
 }
 

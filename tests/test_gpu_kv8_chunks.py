@@ -29,14 +29,18 @@ def _step(pool, lens, rows, wide):
 
 
 def test_every_kernel_runs():
-    lens, rows = [300, 40], [20, 20]
-    pool = _filled(lens, 1, 64, 128)
+    pool = _filled([300, 40], 1, 64, 128)
     q = _rand((40, 4, 128), 1, BF).to(DEV)
-    for is_wide, name, q in ((False, "kv8_attn", q), (True, "kv8_attn_tc", q), (False, "kv8_attn", q.float()),
-                             (True, "kv8_attn_tc32", q.float())):
+    big = _rand((600, 8, 128), 1, BF).to(DEV)
+    pools = (pool, [300, 40], [20, 20]), (_filled([700], 1, 64, 128), [700], [600])
+    for (p, lens, rows), x, is_wide, name in ((pools[0], q, False, "kv8_attn"), (pools[0], q, True, "kv8_attn_tc1"),
+                                              (pools[0], q.float(), False, "kv8_attn"),
+                                              (pools[0], q.float(), True, "kv8_attn_tc1"),
+                                              (pools[1], big, True, "kv8_attn_tc2"),
+                                              (pools[1], big.float(), True, "kv8_attn_tc1")):
         vc.viscache_profile_enable(True)
         try:
-            _run(pool, _step(pool, lens, rows, is_wide), q, True)
+            _run(p, _step(p, lens, rows, is_wide), x, True)
             assert list(vc.viscache_profile_read()) == [name]
         finally:
             vc.viscache_profile_enable(False)
@@ -116,6 +120,16 @@ def test_chunks_match_oracle(Hq, Hkv, d, page, causal, wide, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
+def test_long_chunks_match_oracle(wide, dtype):
+    # at least 512 packed rows a request on average: units of 256 rows in the wide case, whole and
+    # partial ones, a request without rows, rows without tokens
+    lens, rows = [1500, 40, 700, 513], [300, 0, 259, 700]
+    check(_filled(lens, 2, 64, 128), lens, rows, 8, True, wide, sample=4, dtype=dtype)
+    lens, rows = [2900, 3], [330, 3]
+    check(_filled(lens, 1, 16, 64), lens, rows, 16, False, wide, sample=4, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
 def test_units_split_over_blocks(wide, dtype):
     # few units and long contexts: every unit's tiles lie on many blocks
     lens, rows = [20000, 3001], [40, 17]
@@ -144,8 +158,9 @@ def test_rising_maxima_and_scales(wide, dtype):
         grow = 2.0 ** torch.div(torch.arange(n), 100, rounding_mode="floor")[:, None, None]
         K, V = K * (size.flip(0) if flip else size), V * (grow.flip(0) if flip else grow)
         pool.append([n], [n], K, V)
-        check(pool, [n], [90], 4, True, wide, scale=0.5, dtype=dtype)
-        check(pool, [n], [90], 4, True, wide, qscale=1e-20, dtype=dtype)
+        for rows in (90, 130):                  # 360 and 520 rows of the KV head
+            check(pool, [n], [rows], 4, True, wide, scale=0.5, dtype=dtype)
+            check(pool, [n], [rows], 4, True, wide, qscale=1e-20, dtype=dtype)
 
 
 @pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
@@ -156,8 +171,9 @@ def test_zero_pages_and_zero_rows(wide, dtype):
     V[128:272] = 0
     K[320:] = 0
     pool.append([400], [400], K, V)
-    check(pool, [400], [100], 4, True, wide, dtype=dtype)
-    check(pool, [400], [100], 4, True, wide, qscale=0.0, dtype=dtype)
+    for rows in (100, 260):                     # 200 and 520 rows of a KV head
+        check(pool, [400], [rows], 4, True, wide, dtype=dtype)
+        check(pool, [400], [rows], 4, True, wide, qscale=0.0, dtype=dtype)
 
 
 def test_paths_agree_and_calls_repeat(wide):

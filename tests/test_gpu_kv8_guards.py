@@ -81,7 +81,7 @@ def test_many_rows_call_stays_in_its_buffers():
         vc.viscache_kv8_attention(pool.cache, pool.step(lens, rows), q, out=out.view(total, Hq, d),
                                   lse=lse.view(total, Hq), ws=ws.body)
         torch.cuda.synchronize()
-        assert list(vc.viscache_profile_read()) == ["kv8_attn_tc"]
+        assert list(vc.viscache_profile_read()) == ["kv8_attn_tc1"]
     finally:
         vc.viscache_profile_enable(False)
     for g in (out, lse, ws):

@@ -1,5 +1,5 @@
 """Host models of the barrier protocols of the attention kernels over the 8-bit cache
-(csrc/kv8_attn.cu, csrc/kv8_attn_tc.cu, csrc/kv8_attn_tc32.cu).
+(csrc/kv8_attn.cu, csrc/kv8_attn_tc2.cu, csrc/kv8_attn_tc1.cu).
 
 Each role of a kernel (producer or loader, consumers, converters, MMA issuer, softmax of a
 row tile) is a coroutine that makes the kernel's waits and arrivals in the kernel's order;
@@ -320,41 +320,49 @@ def test_chunk_protocol_mistakes_are_caught(mistake):
 
 
 # ---------------------------------------------------------------------------------------
-# the many-rows kernel of fp32 rows: one row tile, two S buffers, K expanded a tile ahead of V
+# one row tile, two S buffers; fp32 rows: K expanded a tile ahead of V; 16-bit rows: K by TMA
 
-def run_chunks32(segments, seed, mistake=None):
+def run_rows(segments, seed, f32, mistake=None):
     """segments: tiles of each."""
     rnd = random.Random(seed)
-    mk = lambda n, count=1: [Bar(count) for _ in range(n)]
-    ring, stages = 4, 2
-    k_full, k_empty, v_full, pv_done = mk(stages), mk(stages), Bar(), Bar()
+    mk = lambda n: [Bar() for _ in range(n)]
+    ks, vs, ring = (2, 1, 4) if f32 else (3, 2, 3)
+    k_full, k_empty, v_full, v_empty, pv_done = mk(ks), mk(ks), mk(vs), mk(vs), Bar()
     code_full, code_empty, ref_full = mk(ring), mk(ring), mk(REFS)
     s_full, p_half, p_full, q_full, q_empty = mk(2), mk(2), Bar(), Bar(), Bar()
-    K, V, code, ref, q, qs = [None] * stages, [None], [None] * ring, [None] * REFS, [None], [None]
+    K, V, code, ref, q, qs = [None] * ks, [None] * vs, [None] * ring, [None] * REFS, [None], [None]
     S, P, added = [None, None], [[None, None], [None, None]], []
-    flying, pipe = [], []
+    flying, pipe, late = [], [], []     # late: commits whose batches are done; they arrive in any order
 
     def w(name, bar, phase):
         return None if mistake == name else (bar, phase)
 
-    def items(n, t):
-        # the order of the codes of a segment whose first tile is t
+    def items(n, t, ahead):
+        # the order of a segment whose first tile is t: K, K, V, K, V, ... or K, V, K, V, ...
         for j in range(n + 1):
             if j < n:
                 yield "K", t + j
-            if j > 0:
+            if ahead and j > 0:
                 yield "V", t + j - 1
+            elif not ahead and j < n:
+                yield "V", t + j
+
+    def k_free(x):
+        need(not any(b[0] == "S" and b[1] % ks == x % ks for b in pipe), "K written under its product")
 
     def loader():
         t, item = 0, 0
         for n in segments:
-            for kind, x in items(n, t):
-                yield w("code_empty", code_empty[item % ring], item // ring - 1)
+            for kind, x in items(n, t, f32):
+                if kind == "K" and not f32:
+                    yield w("k_empty", k_empty[x % ks], x // ks - 1)
+                else:
+                    yield w("code_empty", code_empty[item % ring], item // ring - 1)
                 if kind == "K":
                     ref[x % REFS] = x
                     ref_full[x % REFS].arrive()
                 flying.append((kind, x, item))
-                item += 1
+                item += kind == "V" or f32
             t += n
 
     def converters():
@@ -365,21 +373,23 @@ def run_chunks32(segments, seed, mistake=None):
             q[0], qs[0] = seg, seg
             yield None
             q_full.arrive()
-            for kind, x in items(n, t):
+            for kind, x in items(n, t, f32):
+                if kind == "K" and not f32:
+                    continue
                 yield w("code_full", code_full[item % ring], item // ring)
                 if kind == "K":
-                    yield w("k_empty", k_empty[x % stages], x // stages - 1)
-                    need(not any(b[0] == "S" and b[1] % stages == x % stages for b in pipe), "K written under its product")
-                    K[x % stages] = x
+                    yield w("k_empty", k_empty[x % ks], x // ks - 1)
+                    k_free(x)
+                    K[x % ks] = x
                 else:
-                    yield w("pv_done", pv_done, x - 1)
-                    need(not any(b[0] == "PV" for b in pipe), "V written under its product")
+                    yield w("v_empty", v_empty[x % vs], x // vs - 1)
+                    need(not any(b[0] == "PV" and b[1] % vs == x % vs for b in pipe), "V written under its product")
                     need(ref[x % REFS] == x, "scales of another tile")
-                    V[0] = x
+                    V[x % vs] = x
                 need(code[item % ring] == (kind, x), "codes of another tile expanded")
                 yield None
                 code_empty[item % ring].arrive()
-                (k_full[x % stages] if kind == "K" else v_full).arrive()
+                (k_full[x % ks] if kind == "K" else v_full[x % vs]).arrive()
                 item += 1
             t += n
 
@@ -387,21 +397,22 @@ def run_chunks32(segments, seed, mistake=None):
         t = 0
         for seg, n in enumerate(segments):
             yield w("q_full", q_full, seg)
-            for kind, x in items(n, t):
+            for kind, x in items(n, t, True):
                 if kind == "K":
-                    yield w("k_full", k_full[x % stages], x // stages)
+                    yield w("k_full", k_full[x % ks], x // ks)
                     pipe.append(("S", x, seg))
                     pipe.append(("commit", s_full[x & 1]))
-                    pipe.append(("commit", k_empty[x % stages]))
+                    pipe.append(("commit", k_empty[x % ks]))
                     if mistake == "rows early" and x == t + n - 1:
                         pipe.append(("commit", q_empty))
                 else:
-                    yield w("v_full", v_full, x)
+                    yield w("v_full", v_full[x % vs], x // vs)
                     yield w("p_half", p_half[x & 1], x >> 1)
                     pipe.append(("PV", x, 0, x == t))
                     yield w("p_full", p_full, x)
                     pipe.append(("PV", x, 1, x == t))
                     pipe.append(("commit", pv_done))
+                    pipe.append(("commit", v_empty[x % vs]))
             if mistake != "rows early":
                 pipe.append(("commit", q_empty))
             t += n
@@ -440,11 +451,14 @@ def run_chunks32(segments, seed, mistake=None):
         if not flying:
             return False
         kind, x, item = flying.pop(rnd.randrange(len(flying)))
-        code[item % ring] = (kind, x)
-        code_full[item % ring].arrive()
+        if kind == "K" and not f32:
+            k_free(x)
+            K[x % ks] = x
+            k_full[x % ks].arrive()
+        else:
+            code[item % ring] = (kind, x)
+            code_full[item % ring].arrive()
         return True
-
-    late = []                                       # commits whose batches are done: they arrive in any order
 
     def batch(_):
         if late and (not pipe or rnd.random() < 0.6):
@@ -457,12 +471,12 @@ def run_chunks32(segments, seed, mistake=None):
             late.append(b[1])
         elif b[0] == "S":
             _, x, seg = b
-            need(K[x % stages] == x and q[0] == seg, "S of other keys or rows")
+            need(K[x % ks] == x and q[0] == seg, "S of other keys or rows")
             need(S[x & 1] is None and P[x & 1] == [None, None], "S written before it was read, or over a P")
             S[x & 1] = x
         else:
             _, x, h, first = b
-            need(P[x & 1][h] == x and V[0] == x, "PV of another tile")
+            need(P[x & 1][h] == x and V[x % vs] == x, "PV of another tile")
             P[x & 1][h] = None
             if h:
                 added[:] = [x] if first else added + [x]
@@ -476,24 +490,29 @@ def _tiles(seed):
     return [r.choice([1, 1, 1, 2, 2, 3, 5, 12, 30]) for _ in range(r.randrange(1, 8))]
 
 
-def test_fp32_chunk_protocol_holds():
+@pytest.mark.parametrize("f32", [False, True])
+def test_row_tile_protocol_holds(f32):
     for seed in range(250):
-        run_chunks32(_tiles(seed), seed)
+        run_rows(_tiles(seed), seed, f32)
 
 
-@pytest.mark.parametrize("mistake", ["code_empty", "code_full", "k_empty", "k_full", "pv_done", "v_full", "q_empty",
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("mistake", ["code_empty", "code_full", "k_empty", "k_full", "v_empty", "v_full", "q_empty",
                                      "s_full", "p_half", "p_full", "rescale", "in turn", "last", "rows early"])
-def test_fp32_chunk_protocol_mistakes_are_caught(mistake):
+def test_row_tile_protocol_mistakes_are_caught(mistake, f32):
     caught = 0
     for seed in range(300):
         try:
-            run_chunks32(_tiles(seed), seed, mistake)
+            run_rows(_tiles(seed), seed, f32, mistake)
         except ProtocolError:
             caught += 1
     assert caught > 0, mistake
 
 
-def test_fp32_issuers_wait_for_query_rows_is_implied():
-    # the converters write a segment's rows before its first K
+def test_issuers_wait_for_query_rows():
+    # needed where K comes by TMA; where K is expanded it is implied (a segment's rows come before its first K)
     for seed in range(200):
-        run_chunks32(_tiles(seed), seed, "q_full")
+        run_rows(_tiles(seed), seed, True, "q_full")
+    with pytest.raises(ProtocolError):
+        for seed in range(200):
+            run_rows(_tiles(seed), seed, False, "q_full")
