@@ -67,7 +67,8 @@ uint64_t next_token() {
 }
 
 // The kernel of a call.  On tcgen05 (tc1): more than kTcRows packed rows of a KV
-// head per request on average, so at least two 16-row units of the mma.sync kernel,
+// head per request on average, so at least two 16-row units of the mma.sync kernel
+// (fp32, whose tiles take twice as long: three),
 // and more of those units than SMs, or of their tiles than kTcShare an SM: below
 // that every unit there gets blocks of its own.  With 256-row units (tc2): bf16, at
 // least kTc2Rows such rows, kTc2Tiles tiles and more than kTc2Share tiles of those
@@ -77,7 +78,7 @@ uint64_t next_token() {
 //   64 requests of 4096 tokens, 16 rows 135 / 147, 20 rows 246 / 149, 128 rows 933 / 178
 //   8 of 600 tokens, 24 rows 13.2 / 15.8, 48 rows 29.6 / 17.0
 //   one of 8192 tokens, 20 rows 20.3 / 19.6, 128 rows 42.4 / 34.4
-//   fp32: one of 2000 tokens, 128 rows 24.7 / 35.3; 8 of 4096, 24 rows 47.9 / 43.9, 256 rows 308 / 81
+//   fp32, twice the rows: 8 of 4096, 24 rows 47.9 / 51.1, 36 rows 73 / 52, 256 rows 308 / 98
 // on tc1 / tc2:
 //   one of 32768 tokens, 320 rows 71 / 92, 512 rows 93.7 / 92.5, 8192 rows 988 / 739
 //   one of 8192 tokens, 1024 rows 54.4 / 58.1, 2048 rows 85.7 / 80.8
@@ -88,8 +89,8 @@ bool may_have_many_rows(int64_t n_rows, int64_t n_req, int32_t Hq, int32_t Hkv) 
   return n_rows * (Hq / Hkv) > kTcRows * n_req;
 }
 Kernel kernel_of(const vc_kv8& c, const vc_kv8_step& s, int dtype, int32_t Hq) {
-  if (!may_have_many_rows(s.n_rows, s.n_req, Hq, c.Hkv)) return Kernel::kMma;
   const int64_t rows = (int64_t)s.n_rows * Hq, sms = kv8_sm_count();
+  if (rows / c.Hkv <= (dtype == VC_F32 ? 2 : 1) * kTcRows * s.n_req) return Kernel::kMma;
   const int64_t tiles = ((int64_t)s.max_pages * c.page + 127) / 128;
   if (rows / 16 <= sms && rows / 16 * tiles <= kTcShare * sms) return Kernel::kMma;
   const bool two = dtype == VC_BF16 && rows / c.Hkv >= kTc2Rows * s.n_req && tiles >= kTc2Tiles &&

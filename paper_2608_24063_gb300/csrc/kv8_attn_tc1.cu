@@ -24,7 +24,8 @@
 //   13     loader: page numbers, scales, a TMA box (K, bf16 rows) or a bulk copy
 //          per page
 // Tensor memory: S_0, S_1 (128 columns each; P over them: fp16 pairs in the first
-// 64 columns, of fp32 calls the rest of each in the others), O.  Order of issue:
+// 64 columns, of fp32 calls the rest of each in the others), O, and in fp32 calls
+// the sum of earlier O.  Order of issue:
 //   S(0) S(1) PV(0) S(2) PV(1) ...
 // MMAs of one thread execute in order, so S(t+2) may overwrite the P(t) that PV(t)
 // reads.  P arrives in two halves: the first half's products run while the second's
@@ -37,11 +38,15 @@
 // tile).  A row's maximum may be passed by 2^10 (fp32: 2^2) before O is rescaled;
 // P = 2^(x - m + 4) (fp32: + 12) times (V scale of the tile / the largest so far),
 // at most 2^14, keeps 11 bits down to 2^-18 of its reference (fp32: 22 bits down
-// to 2^-25).  Row sums are fp32, of unrounded terms.
+// to 2^-25).  Row sums are fp32, of unrounded terms.  The tensor cores' fp32 sums
+// cut off, so in fp32 calls the smaller parts are added first and O goes into a
+// sum beside it every four tiles: the error over 29000 tokens falls from 2.5e-5
+// of the output to 1.3e-6 and the time rises by a tenth, with the exponentials'
+// factor taken out of their exponents (3e-7 of each) included.
 //
 // Bound by the softmax's chain: one tile takes about 2200 clocks (its products
 // 1024).  64 requests of 128 rows over 4096 tokens, 8 KV heads of 128: 177 us, 3.0
-// TB/s of codes; fp32 315 us.  Long chunks: kv8_attn_tc2.cu.
+// TB/s of codes; fp32 rows 362 us.  Long chunks: kv8_attn_tc2.cu.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_sched.cuh"
@@ -59,7 +64,7 @@ using namespace tc;
 constexpr int kTcThreads = 512;
 constexpr int kTcMT = 128, kTcKT = 128;
 constexpr int kConvWarp0 = 4, kConvWarps = 8, kIssueWarp = 12, kLoadWarp = 13;
-constexpr uint32_t kSCol = 0, kOCol = 256;
+constexpr uint32_t kSCol = 0, kOCol = 256, kSumCol = 384;
 constexpr int kRefs = 8;                        // tiles whose scales are kept (the loader is at most 5 ahead)
 
 template <typename T, int D>
@@ -67,6 +72,10 @@ struct Cfg {
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr float SLACK = F32 ? 2.f : 10.f;          // log2 units
   static constexpr int PEXP = F32 ? 12 : 4;
+  // Tiles whose products O takes before it is added to the sum beside it (fp32: the
+  // tensor core's sums lose about 2^-26 of O a step, a context of 29000 tokens 2.5e-5).
+  static constexpr int FOLD = F32 ? 4 : 1 << 30;
+  static __device__ __forceinline__ bool fresh(int i) { return i % FOLD == 0; }     // tile i begins O anew
   static constexpr int QPART = F32 ? kTcMT * D * 2 : kTcMT * D, KTILE = F32 ? kTcKT * D * 2 : kTcKT * D;
   static constexpr int KS = F32 ? 2 : 3, VS = F32 ? 1 : 2, CS = F32 ? 4 : 3;
 };
@@ -190,8 +199,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
 #pragma unroll
         for (int k = 0; k < kTcKT / 32; ++k) {
           const int kk = kk0 + k;
-          mma_f16_ts(tbase + kOCol, s_col + kk * 8, bd + kk * 2048 / 16, id_o, (!first || k) ? 1u : 0u);
-          if (F32) mma_f16_ts(tbase + kOCol, s_col + 64 + kk * 8, bd + kk * 2048 / 16, id_o, 1u);
+          if (F32) mma_f16_ts(tbase + kOCol, s_col + 64 + kk * 8, bd + kk * 2048 / 16, id_o, (!first || k) ? 1u : 0u);
+          mma_f16_ts(tbase + kOCol, s_col + kk * 8, bd + kk * 2048 / 16, id_o, (F32 || !first || k) ? 1u : 0u);
         }
       };
       do {
@@ -211,7 +220,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                   const uint32_t at = (kk >> 2) * kBlk16 + (kk & 3) * 2;
-                  mma_f16_ss(d, qd + part * kQ16 + at, bd + at, id_s, (part || kk) ? 1u : 0u);
+                  // (the rest first: the sum is large only while the larger parts are added)
+                  mma_f16_ss(d, qd + (1 - part) * kQ16 + at, bd + at, id_s, (part || kk) ? 1u : 0u);
                 }
             } else {
 #pragma unroll
@@ -228,7 +238,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             const uint64_t bd = vd + (uint32_t)vs * kV16;
             ok = warp_wait(&sm.v_full[vs], (tv / kVStages) & 1, abort) && warp_wait(&sm.p_half[tv & 1], (tv >> 1) & 1, abort);
             if (!ok) break;
-            issue_pv(s_col, bd, 0, j - 1 == w.t0);
+            issue_pv(s_col, bd, 0, C::fresh(j - 1 - w.t0));
             ok = warp_wait(&sm.p_full, tv & 1, abort);
             if (!ok) break;
             issue_pv(s_col, bd, kTcKT / 32, false);
@@ -465,7 +475,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
     // ---- softmax, one row a thread
     const int row = threadIdx.x;
     const uint32_t lane_off = (uint32_t)(warp << 5) << 16;
-    const uint32_t o_col = tbase + lane_off + kOCol;
+    const uint32_t o_col = tbase + lane_off + kOCol, sum_col = tbase + lane_off + kSumCol;
     bool ok = true;
     do {
       const int rho = w.u.rt * kTcMT + row;
@@ -536,26 +546,39 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
           g *= vmax * pow2_inverse(up);
           vmax = up;
         }
-        if (j > w.t0 && __any_sync(0xffffffffu, raise || vraise)) {
+        const bool fold = j > w.t0 && C::fresh(j - w.t0);
+        if (j > w.t0 && (fold || __any_sync(0xffffffffu, raise || vraise))) {
           // the PV of the tile before is done, the next waits for this P
           ok = warp_wait(&sm.pv_done, (t & 1) ^ 1, abort);
           if (!ok) continue;
           tc_fence_after();
+          const bool sums = j - w.t0 > C::FOLD;             // O was added to the sum before
 #pragma unroll 1
           for (int p = 0; p < D / 16; ++p) {
-            uint32_t v[16];
+            uint32_t v[16], u[16];
             tmem_ld16(o_col + p * 16, v);
-            tmem_wait(v);
+            if (F32 && sums) tmem_ld16(sum_col + p * 16, u);
+            tmem_wait_only();
+            reg_fence(v);
 #pragma unroll
             for (int q = 0; q < 16; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * g);
-            tmem_st16(o_col + p * 16, v);
+            if (!fold) tmem_st16(o_col + p * 16, v);
+            if (F32 && sums) {
+              reg_fence(u);
+#pragma unroll
+              for (int q = 0; q < 16; ++q)
+                v[q] = __float_as_uint(fmaf(__uint_as_float(u[q]), g, fold ? __uint_as_float(v[q]) : 0.f));
+            }
+            if (F32 && (fold || sums)) tmem_st16(sum_col + p * 16, v);
           }
         }
         __syncwarp();                           // (whole warps store P)
         // exponent of P's factor: 2^12 times the tile's share of vmax, not below 2^-18
         const int lc = vr > 0.f ? max(-30, (int)(__float_as_uint(vr) >> 23) - (int)(__float_as_uint(vmax) >> 23)) : -30;
-        const float mm = (m == -INFINITY ? 0.f : m) - (float)(lc + kTcPExp);
+        // (fp32: the factor after the exponential, so that the largest terms' exponents are small numbers)
+        const float mm = (m == -INFINITY ? 0.f : m) - (F32 ? 0.f : (float)(lc + kTcPExp));
         const float2 nm = make_float2(-mm, -mm);
+        const float pf = __uint_as_float((uint32_t)(127 + lc + kTcPExp) << 23);
         float2 l0 = make_float2(0.f, 0.f), l1 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -568,8 +591,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             const float2 e = make_float2(ex2(y.x), ex2(y.y));
             if (q & 1) l1 = __fadd2_rn(l1, e);
             else l0 = __fadd2_rn(l0, e);
-            top[q] = half2_bits(e.x, e.y);
-            if (F32) rest[q] = half2_rest(e.x, e.y, top[q]);
+            if constexpr (F32) {
+              const float2 pe = __fmul2_rn(e, make_float2(pf, pf));
+              top[q] = half2_bits(pe.x, pe.y);
+              rest[q] = half2_rest(pe.x, pe.y, top[q]);
+            } else {
+              top[q] = half2_bits(e.x, e.y);
+            }
           }
           tmem_st16(s_col + h * 16, top);
           if (F32) tmem_st16(s_col + 64 + h * 16, rest);
@@ -581,7 +609,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
           }
         }
         const float2 ls = __fadd2_rn(l0, l1);
-        l += (ls.x + ls.y) * __uint_as_float((uint32_t)(127 - lc - kTcPExp) << 23);
+        l += F32 ? ls.x + ls.y : (ls.x + ls.y) * __uint_as_float((uint32_t)(127 - lc - kTcPExp) << 23);
         // the PV of the tile before in turn, so that no wait for one is two phases behind
         ok = warp_wait(&sm.pv_done, (t & 1) ^ 1, abort);
         if (!ok) continue;
@@ -630,6 +658,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
         float y[16];
 #pragma unroll
         for (int q = 0; q < 16; ++q) y[q] = __uint_as_float(v[q]);
+        if constexpr (F32) {
+          if (w.t1 - w.t0 > C::FOLD) {
+            tmem_ld16(sum_col + p * 16, v);
+            tmem_wait(v);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) y[q] += __uint_as_float(v[q]);
+          }
+        }
         if (whole) {
           if (real) put_out(at, p * 16, y, inv);
         } else {
