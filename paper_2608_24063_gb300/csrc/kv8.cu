@@ -10,7 +10,11 @@
 // (held in registers, 16 values a vector) and writes the codes.  Where the page
 // held tokens of the request before, their codes are re-encoded by the same
 // block if the scale grew, so no block waits for another and nothing is
-// written twice.
+// written twice.  At 128 dimensions in bf16: append of 32768 rows of 8 heads (201
+// MB) 35 us, 5.7 TB/s; read of 16 caches of up to 12544 tokens, 4 heads (389 MB) 70
+// us, 5.5 TB/s (84% of a plain copy's rate: what is left is the start and the last
+// blocks of 70 us, and a look-up before each block's first load); append of 64
+// requests' next tokens 4.0 us, three memory round trips after the launch.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "profile.h"

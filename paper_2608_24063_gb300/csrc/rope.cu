@@ -9,7 +9,9 @@
 // angles depend on the row alone, so a block takes a few rows and computes
 // each (row, frequency)'s cosine and sine once, into shared memory; a thread
 // then keeps the eight pairs of its (row, slot) in registers and walks over
-// the heads, 16 values (two or four 16-byte loads) at a time.
+// the heads, 16 values (two or four 16-byte loads) at a time.  32768 rows of 72
+// heads of 128 in bf16 (1.21 GB): 198 us, 6.1 TB/s, 90% of a plain copy's rate.  16
+// rows of 32 heads: 2.3 us, a launch.
 //
 // The phase is an integer: F_i = theta^(-i/half) / 2pi in units of 2^-64 turn,
 // so pos * F_i modulo 2^64 is the reduced angle without any range reduction,

@@ -192,3 +192,18 @@ def test_paths_agree_and_calls_repeat(wide):
     E = float(q.float().abs().sum(-1).max()) * kmax / 128 ** 0.5 * 14 * 2.0 ** -23
     assert ((a.float() - f).abs() <= 2.0 ** -8 * f.abs() + (2.0 ** -10 + 4 * E) * vmax).all()
     assert ((la - lf).abs() <= 2 * E + 1e-5).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp32_rows_keep_their_precision_over_long_contexts(wide, d):
+    # as a whole: exponentials within 2^-22, their exponents (up to 2^4) within 2^-21, scores of
+    # size 2^3 summed within 2^-22 of them, the sum of a few tiles cut off at 2^-26 a step
+    # (2^-20 for 64), fp32 sums of the rest: under 2^-18 of the output's norm together
+    n, m = 20000, 40
+    pool = _filled([n], 1, 64, d)
+    q = _rand((m, 4, d), 9, torch.float32)
+    out, _ = _run(pool, _step(pool, [n], [m], wide), q.to(DEV), False)
+    K, V = (kv8.gather(c, s, pool.table[0], n, 0) for c, s in zip(pool.codes, pool.scale))
+    ref = kv8.attention(q.double().numpy().reshape(m * 4, d), K, V, None, d ** -0.5)[0].reshape(m, 4, d)
+    err = np.linalg.norm(out.double().cpu().numpy() - ref) / np.linalg.norm(ref)
+    assert err <= 2.0 ** -18, err

@@ -327,6 +327,7 @@ def run_rows(segments, seed, f32, mistake=None):
     rnd = random.Random(seed)
     mk = lambda n: [Bar() for _ in range(n)]
     ks, vs, ring = (2, 1, 4) if f32 else (3, 2, 3)
+    fold = 4 if f32 else 1 << 30        # tiles whose products O takes before it goes into the sum
     k_full, k_empty, v_full, v_empty, pv_done = mk(ks), mk(ks), mk(vs), mk(vs), Bar()
     code_full, code_empty, ref_full = mk(ring), mk(ring), mk(REFS)
     s_full, p_half, p_full, q_full, q_empty = mk(2), mk(2), Bar(), Bar(), Bar()
@@ -408,9 +409,9 @@ def run_rows(segments, seed, f32, mistake=None):
                 else:
                     yield w("v_full", v_full[x % vs], x // vs)
                     yield w("p_half", p_half[x & 1], x >> 1)
-                    pipe.append(("PV", x, 0, x == t))
+                    pipe.append(("PV", x, 0, (x - t) % fold == 0))
                     yield w("p_full", p_full, x)
-                    pipe.append(("PV", x, 1, x == t))
+                    pipe.append(("PV", x, 1, (x - t) % fold == 0))
                     pipe.append(("commit", pv_done))
                     pipe.append(("commit", v_empty[x % vs]))
             if mistake != "rows early":
@@ -428,11 +429,15 @@ def run_rows(segments, seed, f32, mistake=None):
                     need(qs[0] == seg, "powers of two of other rows")
                 need(S[t & 1] == t, "scores of another tile")
                 need(ref[t % REFS] == t, "scales of another tile")
-                if j and rnd.random() < 0.3:        # O is rescaled
+                if j == 0:
+                    summed = []
+                if j and (j % fold == 0 or rnd.random() < 0.3):     # O is rescaled, or added to the sum
                     yield w("rescale", pv_done, t - 1)
-                    need(added == list(range(t - j, t)), "O rescaled under a product")
+                    need(summed + added == list(range(t - j, t)), "O rescaled under a product")
                     yield None
-                    need(added == list(range(t - j, t)), "O rescaled under a product")
+                    need(summed + added == list(range(t - j, t)), "O rescaled under a product")
+                    if j % fold == 0:
+                        summed = summed + added
                 S[t & 1], P[t & 1] = None, [t, None]
                 yield None
                 p_half[t & 1].arrive()
@@ -443,9 +448,9 @@ def run_rows(segments, seed, f32, mistake=None):
                 p_full.arrive()
                 t += 1
             yield w("last", pv_done, t - 1)
-            need(added == list(range(t - n, t)), "O read before its last product")
+            need(summed + added == list(range(t - n, t)), "O read before its last product")
             yield None
-            need(added == list(range(t - n, t)), "O overwritten while it is read")
+            need(summed + added == list(range(t - n, t)), "O overwritten while it is read")
 
     def land(_):
         if not flying:
