@@ -131,3 +131,56 @@ def test_a_workspace_serves_calls_of_other_shapes_between_replays():
         graph.replay()
         assert torch.equal(out, wa)
         assert torch.equal(vc.viscache_kv8_attention(pool_b.cache, sb, qb, ws=ws), wb)
+
+
+def test_pool_past_four_gigabytes():
+    # pages on both sides of byte 2^32 of the pools hold the same tokens: the same codes, rows and outputs
+    Hkv, page, d, n_pages = 8, 128, 128, 33200          # 4.35 GB of codes each for K and V
+    cache = vc.Kv8Cache.empty(n_pages, Hkv, page, d, DEV)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    n, m = 700, 40
+    low, high = i32([[5, 1, 9, 0, 3, 7]]), i32([[33199, 32800, 32766, 32768, 33000, 32767]])
+    K, V = (_rand((n, Hkv, d), k, F32, 3.0).to(DEV) for k in (1, 2))
+    got = []
+    for table in (low, high):
+        step = lambda rows: vc.Kv8Step(table, i32([n]), i32([0, rows]), rows)
+        vc.viscache_kv8_append(cache, step(n), K, V)
+        out = list(vc.viscache_kv8_read(cache, step(n), F32))
+        wide = torch.full((1, 3200), -7, dtype=torch.int32, device=DEV)
+        wide[:, :6] = table
+        for dtype in (BF, F32):
+            out.append(vc.viscache_kv8_attention(cache, step(1), _rand((1, 16, d), 3, dtype).to(DEV)))
+            q = _rand((m, 64, d), 4, dtype).to(DEV)
+            for rows in (m, 4):                         # 512-row and 32-row units of a KV head and fewer
+                out.append(vc.viscache_kv8_attention(cache, vc.Kv8Step(wide, i32([n]), i32([0, rows]), rows), q[:rows]))
+            q = _rand((80, 64, d), 5, dtype).to(DEV)
+            out.append(vc.viscache_kv8_attention(cache, vc.Kv8Step(wide, i32([n]), i32([0, 80]), 80), q))
+        got.append(out)
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+def test_rows_past_four_gigabytes():
+    # rows 2.5 GB apart
+    d, H, stride = 128, 3, (5 << 28)
+    buf = torch.zeros(2 * stride + H * d, dtype=BF, device=DEV)
+    x = _rand((3, H, d), 1, BF).to(DEV)
+    far = buf.as_strided((3, H, d), (stride, d, 1))
+    far.copy_(x)
+    pos = torch.tensor([[5, 70, 900]] * 3, dtype=torch.int32, device=DEV)
+    rope = vc.make_rope((16, 24, 24))
+    near, _ = vc.viscache_mrope(rope, pos, x)
+    out, _ = vc.viscache_mrope(rope, pos, far)
+    assert torch.equal(out, near)
+    vc.viscache_mrope(rope, pos, far, q_out=far)
+    assert torch.equal(far, near)
+    caches = [vc.Kv8Cache.empty(1, H, 16, d, DEV) for _ in range(2)]
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)
+    step = vc.Kv8Step(i32([[0]]), i32([3]), i32([0, 3]), 3)
+    rows, outs = [], []
+    for cache, k in zip(caches, (near, far)):
+        vc.viscache_kv8_append(cache, step, k, k)
+        rows += vc.viscache_kv8_read(cache, step)
+        outs.append(vc.viscache_kv8_attention(cache, step, k))
+    assert torch.equal(rows[0], rows[2]) and torch.equal(rows[1], rows[3]) and torch.equal(*outs)
