@@ -594,9 +594,9 @@ int viscache_kv8_read(const vc_kv8* cache, const vc_kv8_step* step, int dtype, v
  * maxima and the softmax's normaliser are fp32.  The result does not depend on
  * what else is in the batch but for that choice and for the order of sums, and
  * is the same for the same call.
- * A key that is not finite makes every row that sees it NaN; a value that is
- * not finite also those rows of the same call and request that stand before it
- * (their weight of it is 0, and 0 * NaN is NaN).
+ * A key that is not finite makes every row that sees it NaN, a value that is
+ * not finite its dimension of them; rows that do not see it are what they would
+ * be without it.
  * After VC_ERR_DEVICE_TIMEOUT (prunekv_get_status) clear the workspace before a
  * captured call is replayed with it.
  */

@@ -73,5 +73,33 @@ __device__ __forceinline__ float pow2_inverse(float s) {
   return s == 0.f ? 1.f : __uint_as_float((254u << 23) - __float_as_uint(s));
 }
 
+// A value that is NaN spoils the sums of rows that see it and no others.  A product
+// takes 0 * NaN for a row that does not, so where a tile has tokens that some of the
+// unit's rows do not see, NaN codes of V count as 0 and the first such token is
+// noted; at the segment's end the rows that see it look their dimensions up.
+constexpr int kNoNan = 0x7fffffff;
+// 0xff in each byte that is a NaN code
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu); }
+// Which of the N dimensions from `col` on (a multiple of 4) are NaN in V of any of
+// the request's tokens [from, to): bit i for dimension col + i.
+template <int N>
+__device__ __forceinline__ uint32_t nan_dims(const vc_kv8& c, const vc_kv8_step& s, int r, int g, int from, int to,
+                                          int col) {
+  uint32_t found = 0;
+#pragma unroll 1
+  for (int t = from; t < to; ++t) {
+    const int p = load_page(s, c.n_pages, r, t / c.page, nullptr);
+    if (p < 0) continue;
+    const uint32_t* codes = reinterpret_cast<const uint32_t*>(
+        static_cast<const uint8_t*>(c.V_codes) + (((int64_t)p * c.Hkv + g) * c.page + t % c.page) * c.d + col);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const uint32_t m = nan_codes(__ldg(codes + i));
+      found |= ((m & 1u) | (m >> 7 & 2u) | (m >> 14 & 4u) | (m >> 21 & 8u)) << (4 * i);
+    }
+  }
+  return found;
+}
+
 }  // namespace kv8
 }  // namespace vc

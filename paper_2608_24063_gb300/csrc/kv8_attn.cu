@@ -88,6 +88,7 @@ struct Smem {
   int64_t scan[C::WARPS + 1];
   Share share;
   int abort, last;
+  int nan_token[2];                                         // first token whose V has a NaN in an edge chunk: [segment & 1]
   int32_t err;                                              // the block's status
 };
 
@@ -200,6 +201,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       tc::mbar_init(&sm.empty[i], NW);
     }
     sm.abort = 0;
+    sm.nan_token[0] = sm.nan_token[1] = kNoNan;
     sm.err = VC_OK;
     tc::fence_mbar_init();
   }
@@ -284,6 +286,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
   const int gid = lane >> 2, tig = lane & 3;
   int off = warp;                               // the warp's first chunk of the next tile (or past it)
   bool ok = true;
+  int seg = 0;                                  // segments so far
   do {
     uint32_t qf[NP][NQ][KS][2];
     float cs[NQ][2];
@@ -357,10 +360,17 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         if (edge) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (key0 + 2 * tig + (k & 1) + 8 * (k >> 1) >= u.kend) {   // beyond the unit's keys: whatever is there
+          {
+            const int key = key0 + 2 * tig + (k & 1) + 8 * (k >> 1);
+            uint32_t bad = 0;
 #pragma unroll
-              for (int e = 0; e < WPT; ++e) w[k][e] = 0u;
+            for (int e = 0; e < WPT; ++e) {
+              const uint32_t n = key >= u.kend ? 0xffffffffu : nan_codes(w[k][e]);   // beyond the unit's keys: whatever is there
+              w[k][e] &= ~n;
+              bad |= n;
             }
+            if (bad && key < u.kend) atomicMin(&sm.nan_token[seg & 1], key);
+          }
         }
         float top[NQ][2];
         bool up = vsc > vref;
@@ -450,6 +460,9 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       }
     __syncwarp();                               // (the named barriers take whole warps)
     if (tc::named_sync_any(1, 32 * NW, !ok)) break;         // some warp gave up: all stop
+    const int nan_from = sm.nan_token[seg & 1];
+    ++seg;
+    if (threadIdx.x == 0) sm.nan_token[seg & 1] = kNoNan;   // (noted from the next segment on)
     // row r's states are put together by warp r (and r + NW): lane k has warp k's
     for (int row = warp; row < MT; row += NW) {
       const float x = lane < NW ? sm.wm[lane][row] : -INFINITY;
@@ -525,6 +538,15 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       for (int b = 0; b < (NW < C::SLOTS ? NW : C::SLOTS); ++b) {
         const float4 z = reinterpret_cast<const float4*>(&sm.merge[b][0][0])[spot(row, it % (D / 4))];
         y[k].x += z.x; y[k].y += z.y; y[k].z += z.z; y[k].w += z.w;
+      }
+      const int rho = r0 + row, nan_to = min(t1 * kKT, a.causal ? min(u.kend, base + rho / G) : u.kend);
+      if (nan_from < nan_to && rho < u.q.m * G) {
+        const uint32_t bad = nan_dims<4>(c, s, u.r, u.g, nan_from, nan_to, it % (D / 4) * 4);
+        const float nan = __uint_as_float(0x7fffffffu);
+        if (bad & 1u) y[k].x = nan;
+        if (bad & 2u) y[k].y = nan;
+        if (bad & 4u) y[k].z = nan;
+        if (bad & 8u) y[k].w = nan;
       }
     }
     const bool whole = wk.whole();

@@ -45,8 +45,8 @@
 // factor taken out of their exponents (3e-7 of each) included.
 //
 // Bound by the softmax's chain: one tile takes about 2200 clocks (its products
-// 1024).  64 requests of 128 rows over 4096 tokens, 8 KV heads of 128: 177 us, 3.0
-// TB/s of codes; fp32 rows 362 us.  Long chunks: kv8_attn_tc2.cu.
+// 1024).  64 requests of 128 rows over 4096 tokens, 8 KV heads of 128: 188 us, 2.9
+// TB/s of codes; fp32 rows 375 us.  Long chunks: kv8_attn_tc2.cu.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_sched.cuh"
@@ -98,6 +98,7 @@ struct Tc1Smem {
   Share share;
   uint32_t tmem_base;
   int abort, last;
+  int nan_token[2][4];                          // first token whose V has a NaN in a mixed tile: [segment & 1][warp]
   int32_t err;                                  // the block's status
 };
 
@@ -155,6 +156,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
     mbar_init(&sm.p_full, 4);
     for (int i = 0; i < kRefs; ++i) mbar_init(&sm.ref_full[i], 1);
     mbar_init(&sm.done, 1);
+    for (int i = 0; i < 8; ++i) sm.nan_token[i >> 2][i & 3] = kNoNan;
     sm.abort = 0;
     sm.err = VC_OK;
     fence_mbar_init();
@@ -425,6 +427,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full);
+      // keys that every row of the unit sees
+      const int lim_min = a.causal ? w.u.q.len - w.u.q.m + 1 + w.u.rt * kTcMT / G : w.u.kend;
       for (int j = w.t0; ok && j <= w.t1; ++j) {
         if (F32 && j < w.t1) {                  // K of tile j
           const int tk = t + j - w.t0, ks = tk % kKStages, st = item % kCodeStages;
@@ -451,6 +455,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
                warp_wait(&sm.v_empty[vs], ((tv / kVStages) & 1) ^ 1, abort);
           if (!ok) break;
           const float* share = sm.vshare[tv % kRefs];
+          const bool mixed = j * kTcKT > lim_min;               // some rows do not see all of it
+          if (mixed) {                          // (a pass of its own: within the loop below it costs every tile)
+#pragma unroll 1
+            for (int key = key0; key < min(left, 128); key += RP) {
+              uint4* at = reinterpret_cast<uint4*>(sm.code[st] + key * D + ch * 16);
+              uint4 y = *at;
+              if (drop_nan(y)) {
+                *at = y;
+                for (int k = 0; k < 4; ++k) atomicMin(&sm.nan_token[seg & 1][k], (j - 1) * kTcKT + key);
+              }
+            }
+          }
 #pragma unroll
           for (int n = 0; n < 128 / RP; ++n) {
             const int key = key0 + RP * n;
@@ -648,6 +664,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
         if (a.lse) a.lse[at] = L == 0.f ? -INFINITY : fmaf(M, 0.6931471805599453f, logf(L));
       };
       const int64_t mine = 2 * (int64_t)blockIdx.x + (w.t0 == 0 ? 1 : 0);
+      const int nan_from = sm.nan_token[(seg - 1) & 1][warp], nan_to = min(lim, w.t1 * kTcKT);
+      __syncwarp();
+      if (lane == 0) sm.nan_token[(seg - 1) & 1][warp] = kNoNan;
       const float inv = whole ? inverse_of(l) * ou : ou;
 #pragma unroll 1
       for (int p = 0; p < D / 16; ++p) {
@@ -665,6 +684,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
 #pragma unroll
             for (int q = 0; q < 16; ++q) y[q] += __uint_as_float(v[q]);
           }
+        }
+        if (nan_from < nan_to && real) {
+          const uint32_t bad = nan_dims<16>(c, s, w.u.r, w.u.g, nan_from, nan_to, p * 16);
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (bad >> q & 1u) y[q] = __uint_as_float(0x7fffffffu);
         }
         if (whole) {
           if (real) put_out(at, p * 16, y, inv);

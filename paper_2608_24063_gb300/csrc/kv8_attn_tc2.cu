@@ -3,7 +3,7 @@
 //
 // Where there is work for every SM, two row tiles share a tile's expansion and each
 // other's waits: a chunk of 2048 rows over 32768 tokens (64 query heads, 8 KV heads
-// of 128) takes 1430 us, 1.49 PFLOP/s, against 1914 us with one row tile; 512 rows tie.  Bound by
+// of 128) takes 1447 us, 1.47 PFLOP/s, against 1914 us with one row tile; 512 rows tie.  Bound by
 // a row tile's chain (scores, softmax, products) and the tensor cores about equally:
 // without exponentials, maxima and expansion it would take 1255 us, the products
 // alone 1111.
@@ -86,6 +86,7 @@ struct TcSmem {
   Share share;
   uint32_t tmem_base;
   int abort, last[2];
+  int nan_token[2][2][4];                       // first token whose V has a NaN in a mixed tile: [row tile][its segment & 1][warp]
   int32_t err;                                  // the block's status
 };
 
@@ -122,6 +123,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
     }
     for (int i = 0; i < kRefs; ++i) mbar_init(&sm.ref_full[i], 1);
     mbar_init(&sm.done, 1);
+    for (int i = 0; i < 16; ++i) sm.nan_token[i >> 3][i >> 2 & 1][i & 3] = kNoNan;
     sm.abort = 0;
     sm.err = VC_OK;
     fence_mbar_init();
@@ -316,6 +318,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
     // ---- converters
     const int i = threadIdx.x - 32 * kConvWarp0;
     bool ok = true;
+    int seg1 = 0;                               // segments in which row tile B had rows
     do {
       // the unit's query rows, once the last S of the segment before is done
       if (!warp_wait(&sm.q_empty, (seg & 1) ^ 1, abort)) break;
@@ -372,6 +375,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full);
+      // keys that every row of the unit sees; whether row tile B has rows
+      const int lim_min = a.causal ? w.u.q.len - w.u.q.m + 1 + w.u.rt * kTcMT / G : w.u.kend;
+      const bool two = rows_of() > 128;
       for (int j = w.t0; j < w.t1; ++j, ++t) {
         const int st = t % kVStages, cst = t % kCodeStages;
         const int left = w.u.kend - j * kTcKT;  // tokens of the tile
@@ -382,6 +388,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         constexpr int LPR = D / 16, RP = 128 / LPR;     // lanes of a row (16 codes each), rows at once
         const int key0 = i / LPR, ch = i % LPR;
         const float* share = sm.vshare[t % kRefs];
+        const bool mixed = (j + 1) * kTcKT > lim_min;           // some rows do not see all of it
+        if (mixed) {                            // (a pass of its own: 4% of a long chunk within the loop below)
+#pragma unroll 1
+          for (int key = key0; key < min(left, 128); key += RP) {
+            uint4* at = reinterpret_cast<uint4*>(sm.code[cst] + key * D + ch * 16);
+            uint4 y = *at;
+            if (drop_nan(y)) {
+              *at = y;
+              for (int k = 0; k < 4; ++k) {
+                atomicMin(&sm.nan_token[0][seg & 1][k], j * kTcKT + key);
+                if (two) atomicMin(&sm.nan_token[1][seg1 & 1][k], j * kTcKT + key);
+              }
+            }
+          }
+        }
 #pragma unroll
         for (int n = 0; n < 128 / RP; ++n) {
           const int key = key0 + RP * n;
@@ -397,6 +418,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         }
       }
       ++seg;
+      seg1 += two;
     } while (ok && w.next(line, s, err));
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
@@ -553,6 +575,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         if (a.lse) a.lse[at] = L == 0.f ? -INFINITY : fmaf(M, 0.6931471805599453f, logf(L));
       };
       const int64_t mine = 2 * (int64_t)blockIdx.x + (w.t0 == 0 ? 1 : 0);
+      int& nan_token = sm.nan_token[X][(no - 1) & 1][warp & 3];
+      const int nan_from = nan_token, nan_to = min(lim, w.t1 * kTcKT);
+      __syncwarp();
+      if (lane == 0) nan_token = kNoNan;
       const float inv = whole ? inverse_of(l) * ou : ou;
 #pragma unroll 1
       for (int p = 0; p < D / 16; ++p) {
@@ -563,6 +589,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         float y[16];
 #pragma unroll
         for (int q = 0; q < 16; ++q) y[q] = __uint_as_float(v[q]);
+        if (nan_from < nan_to && real) {
+          const uint32_t bad = nan_dims<16>(c, s, w.u.r, w.u.g, nan_from, nan_to, p * 16);
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (bad >> q & 1u) y[q] = __uint_as_float(0x7fffffffu);
+        }
         if (whole) {
           if (real) put_out(at, p * 16, y, inv);
         } else {

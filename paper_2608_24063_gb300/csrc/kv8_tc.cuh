@@ -125,6 +125,13 @@ __device__ __forceinline__ void expand16(uint8_t* tile, int row, int c, const ui
   *reinterpret_cast<uint4*>(base + (((ch + !swap) ^ r7) << 4)) = swap ? lo : hi;
 }
 
+// Takes the NaN codes out of y; whether there was one.
+__device__ __forceinline__ bool drop_nan(uint4& y) {
+  const uint32_t n[4] = {nan_codes(y.x), nan_codes(y.y), nan_codes(y.z), nan_codes(y.w)};
+  y.x &= ~n[0]; y.y &= ~n[1]; y.z &= ~n[2]; y.w &= ~n[3];
+  return (n[0] | n[1] | n[2] | n[3]) != 0u;
+}
+
 // 1 / a row's sum; 0 where it saw no token, NaN stays.
 __device__ __forceinline__ float inverse_of(float L) { return L > 0.f ? 1.f / L : (L == L ? 0.f : L); }
 

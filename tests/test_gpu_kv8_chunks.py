@@ -207,3 +207,36 @@ def test_fp32_rows_keep_their_precision_over_long_contexts(wide, d):
     ref = kv8.attention(q.double().numpy().reshape(m * 4, d), K, V, None, d ** -0.5)[0].reshape(m, 4, d)
     err = np.linalg.norm(out.double().cpu().numpy() - ref) / np.linalg.norm(ref)
     assert err <= 2.0 ** -18, err
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,d,page,n,m", [(8, 2, 128, 64, 900, 300), (4, 1, 64, 16, 500, 500), (2, 2, 128, 128, 260, 5),
+                                               (32, 2, 128, 32, 700, 90), (4, 2, 64, 32, 6000, 40)])
+def test_what_a_row_does_not_see_does_not_reach_it(Hq, Hkv, d, page, n, m, dtype, wide):
+    # keys and values of tokens that are not finite: rows before them are what they would be without
+    # them, and a row that sees one is NaN: everywhere for a key, in the value's dimensions for a value
+    K, V = (_rand((n, Hkv, d), k, torch.float32, 2.0) for k in (1, 2))
+    bad = K.clone(), V.clone()
+    first_k, first_v, second_v = n - m // 2, n - m // 3 - 1, n - 2
+    bad[0][first_k, 0, 3] = float("inf")
+    bad[1][first_v, Hkv - 1, 5] = float("nan")
+    bad[1][second_v, Hkv - 1, d - 1] = float("-inf")
+    # (finite stand-ins that leave the pages' scales as they are)
+    K[first_k, 0, 3] = V[first_v, Hkv - 1, 5] = V[second_v, Hkv - 1, d - 1] = 0.0
+    q = _rand((m, Hq, d), 3, dtype).to(DEV)
+    outs = []
+    for k, v in ((K, V), bad):
+        pool = Pool([n], Hkv, page, d)
+        pool.append([n], [n], k, v)
+        pool.check()
+        outs.append(_run(pool, _step(pool, [n], [m], wide), q, True))
+    (out, lse), (got, zgot) = outs
+    G, own = Hq // Hkv, torch.arange(n - m, n, device=DEV)
+    want, zwant = out.clone(), lse.clone()
+    sees = own >= first_k
+    want[sees, :G], zwant[sees, :G] = float("nan"), float("nan")
+    want[own >= first_v, (Hkv - 1) * G:, 5] = float("nan")
+    want[own >= second_v, (Hkv - 1) * G:, d - 1] = float("nan")
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isnan(zgot), torch.isnan(zwant))
+    assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+    assert torch.equal(torch.nan_to_num(zgot), torch.nan_to_num(zwant))
