@@ -12,10 +12,12 @@
 // the unit before, the start of the one after); the block that finishes a
 // unit's last segment adds them up in order.  Lengths are read on the device.
 //
-// Where the units are no more than the blocks (few requests), a segment's end
-// costs as much as several tiles, so no block takes two: every unit gets whole
-// blocks, ceil(tiles / per) of them with the least `per` that the blocks allow
-// (24 units of 6 to 25 tiles on 152 blocks: 20.8 -> 16.5 us against the line).
+// Where the units are no more than the blocks (few requests), no block takes two:
+// every unit gets whole blocks, ceil(tiles / per) of them with the least `per` that
+// the blocks allow, if that is no more than kEndTiles above an equal share, since a
+// segment's end costs as much as several tiles.  Us on the line / in whole blocks,
+// 152 blocks: 24 units of 6 to 25 tiles 22.9 / 15.5, 144 of 8 to 32 33.4 / 29.4,
+// 128 of 16 to 64 44.9 / 47.0, 128 of 64 to 256 119 / 149.
 #pragma once
 
 #include <cuda.h>
@@ -30,6 +32,9 @@ namespace vc {
 bool kv8_pool_map(CUtensorMap* m, const void* base, const vc_kv8& c);
 
 namespace kv8 {
+
+// What a segment's end costs, in tiles.
+constexpr int kEndTiles = 16;
 
 // Place in the line: a unit and the request's numbers.
 struct Unit {
@@ -232,18 +237,23 @@ __device__ __forceinline__ void find_share(const Line<MT, KT>& line, const vc_kv
       const int N = gridDim.x, rts = line.row_tiles(q);
       // (at most 32 (N + 1) if none is over N: no overflow)
       const int units = __reduce_add_sync(0xffffffffu, min(rts, N + 1) * min(line.Hkv, N + 1));
-      if (units <= N) {
+      int per = 0, mine = 0, before = 0;
+      bool pieces = units <= N;
+      if (pieces) {
         // pieces of at most `per` tiles; a unit has at most 2^23 tiles, N units fewer than 2^31
         int w = 0;
         for (int rt = 0; rt < rts; ++rt) w += line.Hkv * line.tiles(line.keys(q, rt));
-        int per = (__reduce_add_sync(0xffffffffu, w) + N - 1) / N, mine, before;
-        for (;;) {
+        const int share = (__reduce_add_sync(0xffffffffu, w) + N - 1) / N;
+        for (per = share;;) {
           mine = 0;
           for (int rt = 0; rt < rts; ++rt) mine += line.Hkv * ((line.tiles(line.keys(q, rt)) + per - 1) / per);
           before = scan_warp(mine) - mine;
           if (__shfl_sync(0xffffffffu, before + mine, 31) <= N) break;
           per += per / 8 + 1;
         }
+        pieces = per <= share + kEndTiles;
+      }
+      if (pieces) {
         const int i = blockIdx.x;
         if (lane == 31) {
           sh.begin = 0;
