@@ -198,6 +198,9 @@ struct Kv8AttnArgs {
 };
 constexpr int kKv8MaxCtas = 160;       // blocks of an attention launch at most (152 SMs, rounded up)
 int kv8_sm_count();                    // SMs of the current device, at most kKv8MaxCtas
+// Lets a kernel use `bytes` of dynamic shared memory on the current device, once a
+// device (`done`: a bit each).
+cudaError_t kv8_allow_smem(const void* kernel, size_t bytes, std::atomic<uint64_t>& done);
 int kv8_attn_rows_mma();               // most rows a unit of the attention kernels
 int kv8_attn_rows_tc2();
 cudaError_t launch_kv8_attn_mma(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8AttnArgs& a,

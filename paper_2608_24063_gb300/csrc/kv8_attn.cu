@@ -673,13 +673,9 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
   using C = Cfg<T, D, NQ>;
   constexpr size_t smem = sizeof(Smem<T, D, NQ>) + 1024;
   static_assert(smem <= 232448, "shared memory of a block");
-  static std::atomic<bool> attr{false};
-  if (!attr.load(std::memory_order_relaxed)) {
-    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_kernel<T, D, NQ>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    attr.store(true, std::memory_order_relaxed);
-  }
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = kv8_allow_smem(reinterpret_cast<const void*>(kv8_attn_kernel<T, D, NQ>), smem, allowed);
+  if (e != cudaSuccess) return e;
   CUtensorMap mk, mv;
   if (!kv8_pool_map(&mk, c.K_codes, c) || !kv8_pool_map(&mv, c.V_codes, c)) return cudaErrorInvalidValue;
   // no more blocks than the line can have tiles
@@ -715,6 +711,17 @@ int kv8_sm_count() {
   if (n > kKv8MaxCtas) n = kKv8MaxCtas;
   cached[dev].store(n, std::memory_order_relaxed);
   return n;
+}
+
+cudaError_t kv8_allow_smem(const void* kernel, size_t bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 int kv8_attn_rows_mma() { return 16; }

@@ -743,13 +743,9 @@ template <typename T, int D>
 cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
   constexpr size_t smem = sizeof(Tc1Smem<T, D>) + 1024;
   static_assert(smem <= 232448, "shared memory of a block");
-  static std::atomic<bool> attr{false};
-  if (!attr.load(std::memory_order_relaxed)) {
-    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_tc1_kernel<T, D>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    attr.store(true, std::memory_order_relaxed);
-  }
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = kv8_allow_smem(reinterpret_cast<const void*>(kv8_attn_tc1_kernel<T, D>), smem, allowed);
+  if (e != cudaSuccess) return e;
   CUtensorMap mk = {};
   if (!Cfg<T, D>::F32 && !kv8_pool_map(&mk, c.K_codes, c)) return cudaErrorInvalidValue;
   const int64_t G = a.Hq / c.Hkv;

@@ -645,13 +645,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
 template <int D>
 cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {
   constexpr size_t smem = sizeof(TcSmem<D>) + 1024;
-  static std::atomic<bool> attr{false};
-  if (!attr.load(std::memory_order_relaxed)) {
-    const cudaError_t e = cudaFuncSetAttribute(kv8_attn_tc2_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (int)smem);
-    if (e != cudaSuccess) return e;
-    attr.store(true, std::memory_order_relaxed);
-  }
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = kv8_allow_smem(reinterpret_cast<const void*>(kv8_attn_tc2_kernel<D>), smem, allowed);
+  if (e != cudaSuccess) return e;
   CUtensorMap mk;
   if (!kv8_pool_map(&mk, c.K_codes, c)) return cudaErrorInvalidValue;
   const int64_t G = a.Hq / c.Hkv;
