@@ -364,3 +364,15 @@ def test_binding_refuses():
         vc.viscache_kv8_read(pool.cache, step, out=(kv[:1], kv))
     with pytest.raises(TypeError):
         vc.viscache_kv8_attention(pool.cache, step, q.half())
+
+
+@pytest.mark.parametrize("n,Hq,Hkv,top", [(33, 4, 1, 900), (38, 8, 4, 700), (150, 16, 1, 300), (160, 2, 1, 2000),
+                                          (161, 2, 1, 500), (64, 3, 3, 1500)])
+def test_more_requests_than_a_warps_lanes(n, Hq, Hkv, top):
+    # units around the number of SMs, some requests empty, some without rows
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, top, n).tolist()
+    rows = (rng.random(n) < 0.9).astype(int).tolist()
+    pool = _filled(lens, Hkv, 32, 64)
+    _attend_case(pool, lens, rows, Hq, BF, True)
+    _attend_case(pool, lens, [3 * m for m in rows], Hq, F32, True)
