@@ -8,6 +8,7 @@ the functions raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import List, Optional, Sequence, Tuple
@@ -183,10 +184,21 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError("unsupported dtype %s (bf16 or fp32)" % t.dtype)
 
 
-def _workspace(nbytes: int, device, ws: Optional[torch.Tensor]) -> torch.Tensor:
-    if ws is not None:
-        return ws
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+def _on(stream):
+    """Where a call allocates: its own stream.  A block of another stream's pool may still be in use
+    there, and one that the call drops on return would be handed out again before its kernels ran."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(nbytes: int, device, ws: Optional[torch.Tensor], stream) -> torch.Tensor:
+    return ws if ws is not None else _empty(max(nbytes, 256), torch.uint8, device, stream)
 
 
 def _i32(seq):
@@ -254,10 +266,10 @@ def viscache_scout_mmr(H: torch.Tensor, prompt: torch.Tensor, n_frames: Sequence
     if out is not None:
         order, keys, gains = out
     else:
-        order = torch.empty(sum(ks), dtype=torch.int32, device=dev)
-        keys = torch.empty(sum(ks), dtype=torch.int32, device=dev)
-        gains = torch.empty(sum(ks), dtype=torch.float32, device=dev) if with_gains else None
-    ws = _workspace(need, dev, ws)
+        order = _empty(sum(ks), torch.int32, dev, stream)
+        keys = _empty(sum(ks), torch.int32, dev, stream)
+        gains = _empty(sum(ks), torch.float32, dev, stream) if with_gains else None
+    ws = _workspace(need, dev, ws, stream)
     k_out = (ctypes.c_int32 * n_req)()
     if H.dtype != torch.float32 or prompt.dtype != torch.float32 or not H.is_contiguous() \
             or not prompt.is_contiguous() or prompt.shape != (n_req, D) or H.shape[0] != sum(n_frames):
@@ -282,8 +294,8 @@ def prunekv_score(Qw: torch.Tensor, K: torch.Tensor, scale: float = 0.0,
     _, Hkv, n, _ = K.shape
     if scores is None:
         shape = (Hkv, n) if rank_mode == VC_RANK_SHARED else (L, Hkv, n)
-        scores = torch.empty(shape, dtype=torch.float32, device=K.device)
-    ws = _workspace(prunekv_score_workspace_size(L, Hq, W), K.device, ws)
+        scores = _empty(shape, torch.float32, K.device, stream)
+    ws = _workspace(prunekv_score_workspace_size(L, Hq, W), K.device, ws, stream)
     _check("prunekv_score", lib().prunekv_score(
         _ptr(Qw), _ptr(K), _dtype_code(K), L, Hq, Hkv, d, n, W, float(scale), rank_mode,
         _ptr(row_lse), _ptr(scores), _ptr(ws), ws.numel(), _stream(stream)))
@@ -313,7 +325,7 @@ def prunekv_score_static(Qw: torch.Tensor, K: torch.Tensor, scale: float = 0.0,
     _, Hkv, n, _ = K.shape
     if scores is None:
         shape = (Hkv, n) if rank_mode == VC_RANK_SHARED else (L, Hkv, n)
-        scores = torch.empty(shape, dtype=torch.float32, device=K.device)
+        scores = _empty(shape, torch.float32, K.device, stream)
     _check("prunekv_score_static", lib().prunekv_score_static(
         _ptr(Qw), _ptr(K), _dtype_code(K), L, Hq, Hkv, d, n, W, float(scale), rank_mode,
         _ptr(row_lse), _ptr(scores), _stream(stream)))
@@ -334,10 +346,10 @@ def prunekv_select(scores: torch.Tensor, B: Sequence[int], Nq: int, rank_mode: i
     L = len(B)
     Hkv, n = scores.shape[-2], scores.shape[-1]
     dev = scores.device
-    rank = torch.empty(scores.shape, dtype=torch.int32, device=dev)
-    keep = torch.empty(max(1, Hkv * sum(B)), dtype=torch.int32, device=dev)
-    drop = torch.empty(max(1, drop_rows(B, Nq, Hkv)), dtype=torch.int32, device=dev)
-    ws = _workspace(prunekv_select_workspace_size(L, Hkv, n, rank_mode), dev, ws)
+    rank = _empty(scores.shape, torch.int32, dev, stream)
+    keep = _empty(max(1, Hkv * sum(B)), torch.int32, dev, stream)
+    drop = _empty(max(1, drop_rows(B, Nq, Hkv)), torch.int32, dev, stream)
+    ws = _workspace(prunekv_select_workspace_size(L, Hkv, n, rank_mode), dev, ws, stream)
     _check("prunekv_select", lib().prunekv_select(
         _ptr(scores), L, Hkv, n, _i32(B), Nq, rank_mode, _ptr(rank), _ptr(keep), _ptr(drop),
         _ptr(ws), ws.numel(), _stream(stream)))
@@ -357,12 +369,13 @@ def prunekv_fuse_compact(K: torch.Tensor, V: torch.Tensor, B: Sequence[int], Nq:
     L, Hkv, n, d = K.shape
     rows = Hkv * sum(B)
     if K_out is None:
-        K_out = torch.empty((max(rows, 1), d), dtype=K.dtype, device=K.device)
+        K_out = _empty((max(rows, 1), d), K.dtype, K.device, stream)
     if V_out is None:
-        V_out = torch.empty((max(rows, 1), d), dtype=V.dtype, device=V.device)
-    keep_idx = keep_idx if keep_idx.numel() else torch.zeros(1, dtype=torch.int32, device=K.device)
-    drop_idx = drop_idx if drop_idx.numel() else torch.zeros(1, dtype=torch.int32, device=K.device)
-    ws = _workspace(prunekv_fuse_workspace_size(B, Hkv, d, n, Nq), K.device, ws)
+        V_out = _empty((max(rows, 1), d), V.dtype, V.device, stream)
+    with _on(stream):
+        keep_idx = keep_idx if keep_idx.numel() else torch.zeros(1, dtype=torch.int32, device=K.device)
+        drop_idx = drop_idx if drop_idx.numel() else torch.zeros(1, dtype=torch.int32, device=K.device)
+    ws = _workspace(prunekv_fuse_workspace_size(B, Hkv, d, n, Nq), K.device, ws, stream)
     _check("prunekv_fuse_compact", lib().prunekv_fuse_compact(
         _ptr(K), _ptr(V), _dtype_code(K), L, Hkv, d, n, _i32(B), Nq, _ptr(keep_idx),
         _ptr(drop_idx), float(mu), float(tau), _ptr(K_out), _ptr(V_out), _ptr(ws), ws.numel(),
@@ -412,12 +425,12 @@ def prunekv_compress(batch: Batch, params: vc_params, Qw: torch.Tensor, K: torch
     rows = compressed_rows(batch, params)
     dev = K.device
     if K_out is None:
-        K_out = torch.empty((max(rows, 1), params.d), dtype=K.dtype, device=dev)
+        K_out = _empty((max(rows, 1), params.d), K.dtype, dev, stream)
     if V_out is None:
-        V_out = torch.empty((max(rows, 1), params.d), dtype=V.dtype, device=dev)
+        V_out = _empty((max(rows, 1), params.d), V.dtype, dev, stream)
     if idx_out is None:
-        idx_out = torch.empty(max(rows, 1), dtype=torch.int32, device=dev)
-    ws = _workspace(prunekv_workspace_size(batch, params), dev, ws)
+        idx_out = _empty(max(rows, 1), torch.int32, dev, stream)
+    ws = _workspace(prunekv_workspace_size(batch, params), dev, ws, stream)
     _check("prunekv_compress", lib().prunekv_compress(
         ctypes.byref(batch.c), ctypes.byref(params), _ptr(Qw), _ptr(K), _ptr(V), _ptr(K_out),
         _ptr(V_out), _ptr(idx_out), _ptr(ws), ws.numel(), _stream(stream)))
@@ -437,13 +450,14 @@ def viscache_decode_attention(batch: Batch, params: vc_params, layer: int, q: to
                               ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One decode step's attention in `layer` over the compressed cache: q [n_req][Hq][d] -> out."""
     if out is None:
-        out = torch.empty_like(q)
+        with _on(stream):
+            out = torch.empty_like(q)
     nt = _i32(n_text) if n_text is not None else None
     if ws is None:
         need = lib().viscache_decode_workspace_size(ctypes.byref(batch.c), ctypes.byref(params), nt)
         if need == 0:
             raise VisCacheError("viscache_decode_workspace_size", VC_ERR_INVALID_ARG)
-        ws = _workspace(need, q.device, None)
+        ws = _workspace(need, q.device, None, stream)
     _check("viscache_decode_attention", lib().viscache_decode_attention(
         ctypes.byref(batch.c), ctypes.byref(params), int(layer), _ptr(q), _ptr(K_out), _ptr(V_out),
         _ptr(K_text), _ptr(V_text), nt, _ptr(out), _ptr(ws), ws.numel(), _stream(stream)))
@@ -457,13 +471,14 @@ def viscache_decode_attention_kv4(batch: Batch, params: vc_params, layer: int, q
                                   stream=None) -> torch.Tensor:
     """Decode step in `layer` over the 4-bit cache kv4 = (K_codes, V_codes, K_params, V_params)."""
     if out is None:
-        out = torch.empty_like(q)
+        with _on(stream):
+            out = torch.empty_like(q)
     nt = _i32(n_text) if n_text is not None else None
     if ws is None:
         need = lib().viscache_decode_workspace_size(ctypes.byref(batch.c), ctypes.byref(params), nt)
         if need == 0:
             raise VisCacheError("viscache_decode_workspace_size", VC_ERR_INVALID_ARG)
-        ws = _workspace(need, q.device, None)
+        ws = _workspace(need, q.device, None, stream)
     kc, vc_, kp, vp_ = kv4
     _check("viscache_decode_attention_kv4", lib().viscache_decode_attention_kv4(
         ctypes.byref(batch.c), ctypes.byref(params), int(layer), _ptr(q), _ptr(kc), _ptr(vc_), _ptr(kp),
@@ -486,10 +501,10 @@ def viscache_kv4_quantize(batch: Batch, params: vc_params, K_out: torch.Tensor, 
     rows, groups = viscache_kv4_sizes(batch, params)
     d, dev = params.d, K_out.device
     if out is None:
-        out = (torch.empty((max(rows, 1), d // 2), dtype=torch.uint8, device=dev),
-               torch.empty((max(rows, 1), d // 2), dtype=torch.uint8, device=dev),
-               torch.empty((max(groups, 1), d, 2), dtype=torch.float32, device=dev),
-               torch.empty((max(rows, 1), d // 32, 2), dtype=torch.float32, device=dev))
+        out = (_empty((max(rows, 1), d // 2), torch.uint8, dev, stream),
+               _empty((max(rows, 1), d // 2), torch.uint8, dev, stream),
+               _empty((max(groups, 1), d, 2), torch.float32, dev, stream),
+               _empty((max(rows, 1), d // 32, 2), torch.float32, dev, stream))
     kc, vc_, kp, vp_ = out
     _check("viscache_kv4_quantize", lib().viscache_kv4_quantize(
         ctypes.byref(batch.c), ctypes.byref(params), _ptr(K_out), _ptr(V_out), _ptr(kc), _ptr(vc_),
@@ -503,8 +518,8 @@ def viscache_kv4_dequantize(batch: Batch, params: vc_params, K_codes: torch.Tens
     """Reconstruction (K_hat, V_hat) [rows][d] of the 4-bit cache in `dtype`."""
     rows = K_codes.shape[0]
     if out is None:
-        out = (torch.empty((max(rows, 1), params.d), dtype=dtype, device=K_codes.device),
-               torch.empty((max(rows, 1), params.d), dtype=dtype, device=K_codes.device))
+        out = (_empty((max(rows, 1), params.d), dtype, K_codes.device, stream),
+               _empty((max(rows, 1), params.d), dtype, K_codes.device, stream))
     kh, vh = out
     _check("viscache_kv4_dequantize", lib().viscache_kv4_dequantize(
         ctypes.byref(batch.c), ctypes.byref(params), _ptr(K_codes), _ptr(V_codes), _ptr(K_params),
@@ -567,14 +582,14 @@ def viscache_mrope(rope: vc_rope, positions: torch.Tensor, q: torch.Tensor, k: O
         raise VisCacheError(fn, VC_ERR_INVALID_ARG)
     rows, Hq, d = q.shape
     if q_out is None:
-        q_out = torch.empty((rows, Hq, d), dtype=dt, device=q.device)
+        q_out = _empty((rows, Hq, d), dt, q.device, stream)
     qs, qh = _rows(fn, q, dt, dev, rows, Hq, d)
     qos, qoh = _rows(fn, q_out, dt, dev, rows, Hq, d)
     Hkv, ks, kos, kp, kop, kh, koh = 0, 0, 0, None, None, d, d
     if k is not None:
         Hkv = k.shape[1]
         if k_out is None:
-            k_out = torch.empty((rows, Hkv, d), dtype=dt, device=q.device)
+            k_out = _empty((rows, Hkv, d), dt, q.device, stream)
         ks, kh = _rows(fn, k, dt, dev, rows, Hkv, d)
         kos, koh = _rows(fn, k_out, dt, dev, rows, Hkv, d)
         kp, kop = k.data_ptr(), k_out.data_ptr()
@@ -639,7 +654,7 @@ def viscache_kv8_workspace_size(n_rows: int, Hq: int, Hkv: int, d: int) -> int:
     return lib().viscache_kv8_workspace_size(n_rows, Hq, Hkv, d)
 
 
-def _kv8_ws(fn: str, cache: Kv8Cache, step: Kv8Step, Hq: int, ws: Optional[torch.Tensor]):
+def _kv8_ws(fn: str, cache: Kv8Cache, step: Kv8Step, Hq: int, ws: Optional[torch.Tensor], stream):
     # the device of the call, and the workspace on it
     dev = _current_device()
     if cache.index != dev or step.index != dev:
@@ -648,7 +663,7 @@ def _kv8_ws(fn: str, cache: Kv8Cache, step: Kv8Step, Hq: int, ws: Optional[torch
         need = viscache_kv8_workspace_size(step.n_rows, Hq, cache.Hkv, cache.d)
         if need == 0:
             raise VisCacheError(fn, VC_ERR_INVALID_ARG)
-        ws = _workspace(need, cache.device, None)
+        ws = _workspace(need, cache.device, None, stream)
     elif ws.get_device() != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
         raise VisCacheError(fn, VC_ERR_INVALID_ARG)
     return dev, ws
@@ -658,7 +673,7 @@ def viscache_kv8_append(cache: Kv8Cache, step: Kv8Step, K: torch.Tensor, V: torc
                         ws: Optional[torch.Tensor] = None, stream=None) -> None:
     """Write the step's rows K, V [rows][Hkv][d] (any row and head strides) into the cache."""
     fn = "viscache_kv8_append"
-    dev, ws = _kv8_ws(fn, cache, step, cache.Hkv, ws)
+    dev, ws = _kv8_ws(fn, cache, step, cache.Hkv, ws, stream)
     code, dt = _type(K), K.dtype
     kr, kh = _rows(fn, K, dt, dev, step.n_rows, cache.Hkv, cache.d)
     vr, vh = _rows(fn, V, dt, dev, step.n_rows, cache.Hkv, cache.d)
@@ -672,11 +687,11 @@ def viscache_kv8_read(cache: Kv8Cache, step: Kv8Step, dtype=torch.bfloat16, out=
                       ws: Optional[torch.Tensor] = None, stream=None):
     """The step's rows back from the cache: (K_hat, V_hat) [rows][Hkv][d] in `dtype` (or `out`'s)."""
     fn = "viscache_kv8_read"
-    dev, ws = _kv8_ws(fn, cache, step, cache.Hkv, ws)
+    dev, ws = _kv8_ws(fn, cache, step, cache.Hkv, ws, stream)
     if out is None:
         shape = (step.n_rows, cache.Hkv, cache.d)
-        out = (torch.empty(shape, dtype=dtype, device=cache.device),
-               torch.empty(shape, dtype=dtype, device=cache.device))
+        out = (_empty(shape, dtype, cache.device, stream),
+               _empty(shape, dtype, cache.device, stream))
     kh, vh = out
     code = _type(kh)
     for t in out:
@@ -701,10 +716,10 @@ def viscache_kv8_attention(cache: Kv8Cache, step: Kv8Step, q: torch.Tensor, scal
     if q.dim() != 3:
         raise VisCacheError(fn, VC_ERR_INVALID_ARG)
     rows, Hq, d = step.n_rows, q.shape[1], cache.d
-    dev, ws = _kv8_ws(fn, cache, step, Hq, ws)
+    dev, ws = _kv8_ws(fn, cache, step, Hq, ws, stream)
     qs, qh = _rows(fn, q, dt, dev, rows, Hq, d)
     if out is None:
-        out = torch.empty((rows, Hq, d), dtype=dt, device=q.device)
+        out = _empty((rows, Hq, d), dt, q.device, stream)
     _rows(fn, out, dt, dev, rows, Hq, d)
     lp = None
     if lse is not None:
