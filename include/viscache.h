@@ -589,9 +589,14 @@ int viscache_kv8_read(const vc_kv8* cache, const vc_kv8_step* step, int dtype, v
  * down to 2^-14 of their row's largest; in calls of many rows (more than 16 rows
  * of a KV head per request and work for every SM, judged by n_rows, n_req and
  * max_pages) they are sums of two e4m3 numbers, exact down to 2^-9 of the row's
- * largest and within 2^-17 of it below.  Probabilities of bf16 calls are rounded
- * to fp16 (11 bits, down to 2^-17 of the largest; 2^-28 of it below).  Sums,
- * maxima and the softmax's normaliser are fp32.  The result does not depend on
+ * largest and within 2^-17 of it below.  A probability times its page's V scale
+ * is rounded to fp16 in bf16 calls: 11 bits, down to 2^-18 of the row's largest such
+ * product, 2^-29 of it below (fp32 calls: 22 bits down to 2^-14, 2^-36 below; fewer
+ * where a row sees no scale above 2^-100).  Only
+ * what the row sees counts: pages that it does not see leave its bits as they are,
+ * and values without weight cost the others nothing (a token is dropped where its
+ * probability is below 2^-100 of the largest).  Sums, maxima and the softmax's
+ * normaliser are fp32.  The result does not depend on
  * what else is in the batch but for that choice and for the order of sums, and
  * is the same for the same call.
  * A key that is not finite makes every row that sees it NaN, a value that is

@@ -73,6 +73,13 @@ __device__ __forceinline__ float pow2_inverse(float s) {
   return s == 0.f ? 1.f : __uint_as_float((254u << 23) - __float_as_uint(s));
 }
 
+// log2 of a scale; of 0 (a page of zeros, whose contribution does not depend on it) the least.
+__device__ __forceinline__ float scale_log2(float s) { return fmaxf((float)(int)(__float_as_uint(s) >> 23) - 127.f, -126.f); }
+
+// 2^e, -126 <= e <= 127; and for an e in [-250, 254] as two such factors.
+__device__ __forceinline__ float pow2_bits(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+__device__ __forceinline__ float2 pow2_factors(int e) { return make_float2(pow2_bits(e >> 1), pow2_bits(e - (e >> 1))); }
+
 // A value that is NaN spoils the sums of rows that see it and no others.  A product
 // takes 0 * NaN for a row that does not, so where a tile has tokens that some of the
 // unit's rows do not see, NaN codes of V count as 0 and the first such token is

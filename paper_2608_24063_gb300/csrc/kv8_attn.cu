@@ -25,11 +25,13 @@
 // magnitude, which makes fp16 hold bf16 values exactly (down to 2^-14 of that
 // magnitude, then to 2^-24 of it); fp32 calls use a second fp16 part of the
 // row and of the probabilities.  Scores are scaled by the page's K scale in
-// fp32.  Probabilities enter as p * 2^12 * (V scale / largest V scale so far
-// of the warp): at most 2^14 in fp16, so they keep 11 bits down to 2^-26 of
-// the largest.  The row sum adds them before they are rounded.  The maximum
-// m follows the scores with a slack of 2 (log2 units), which saves most
-// rescales of the accumulators.
+// fp32.  Probabilities enter as p * 2^(12 - r) * V scale, r + m following the
+// row's largest score + log2 of its V scale: a row's fixed point is set by its
+// largest contribution, not by values that it does not see or that have no
+// weight.  At most 2^15 in fp16, the largest above 2^11, so they keep 11 bits down
+// to 2^-25 of the largest.  The row sum adds p before it is rounded.  Both
+// references are whole numbers and follow with a slack of 3 (log2 units), which
+// saves most rescales of the accumulators.
 //
 // 32 requests of up to 32768 tokens, 8 KV heads of 128, 8 query heads each (1.35
 // GB): 217 us, 6.2 TB/s, 92% of a plain copy's rate.  One request of 777 tokens, 4
@@ -53,8 +55,9 @@ using namespace kv8;
 
 constexpr int kKT = 128;                        // tokens of a tile
 constexpr int kChunks = kKT / 16;
-constexpr float kSlack = 2.f;
-constexpr float kPScale = 4096.f;               // 2^12
+constexpr float kSlack = 3.f;
+constexpr int kPExp = 12;
+constexpr float kLeastRef = -110.f;             // (2^(kPExp - r) stays a normal number; scales below 2^-100 alone: fewer bits)
 
 // T: query type, D: head dimension, NQ: groups of 8 query rows of a unit.
 // Warps: registers are granted to four warps at a time, so the consumers and
@@ -303,12 +306,15 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         lim[n][h] = a.causal ? min(u.kend, base + (r0 + 8 * n + 2 * tig + h) / G) : u.kend;
       }
     float o[NQ][NM][4];
-    float m[NQ][2], l[NQ][2], vref = 0.f;
+    // references of rows 8 n + 2 tig, + 1: m of the scores x, r + m of x + log2 of the page's V
+    // scale, and rs = 2^(kPExp - r)
+    float m[NQ][2], r[NQ][2], rs[NQ][2], l[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
 #pragma unroll
       for (int i = 0; i < NM; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
-      m[n][0] = m[n][1] = -INFINITY;
+      m[n][0] = m[n][1] = r[n][0] = r[n][1] = -INFINITY;
+      rs[n][0] = rs[n][1] = 1.f;
       l[n][0] = l[n][1] = 0.f;
     }
     for (int tile = t0; tile < t1; ++tile, ++fill) {
@@ -323,6 +329,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
         const uint8_t* vt = sm.ring[st][1];
         const int pg = 16 * ck / c.page;
         const float ksc = sm.scale[st][0][pg], vsc = sm.scale[st][1][pg];
+        const float vlog = scale_log2(vsc);     // (the producer has no time to spare with pages of 16)
         // scores of tokens gid (x[.][0], [1]) and gid + 8, queries 2 tig and 2 tig + 1
         float x[NQ][4];
 #pragma unroll
@@ -373,7 +380,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
           }
         }
         float top[NQ][2];
-        bool up = vsc > vref;
+        bool up = false;
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -386,24 +393,26 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
               if (key0 + gid + 8 >= lim[n][h]) x[n][2 + h] = -INFINITY;
             }
             top[n][h] = max_column(fmaxf(x[n][h], x[n][2 + h]));
-            up = up || top[n][h] > m[n][h] + kSlack;
+            up = up || top[n][h] - m[n][h] > fminf(kSlack, r[n][h] + kSlack - vlog);
           }
         if (__any_sync(0xffffffffu, up)) {
           // the references rise: what was summed is scaled down (0 stays 0)
-          const float gv = vsc > vref ? vref * pow2_inverse(vsc) : 1.f;
-          vref = fmaxf(vref, vsc);
 #pragma unroll
           for (int n = 0; n < NQ; ++n) {
             float g[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              g[h] = 1.f;
-              if (top[n][h] > m[n][h] + kSlack) {
-                g[h] = tc::ex2(m[n][h] - top[n][h]);
-                m[n][h] = top[n][h];
-                l[n][h] *= g[h];
+              if (top[n][h] - m[n][h] > kSlack) {
+                const float to = ceilf(top[n][h]);
+                l[n][h] *= tc::ex2(m[n][h] - to);
+                r[n][h] -= to - m[n][h];
+                m[n][h] = to;
               }
-              g[h] *= gv;
+              const float y = top[n][h] - m[n][h] + vlog;
+              const float to = fmaxf(y > r[n][h] + kSlack ? ceilf(y) : r[n][h], kLeastRef);
+              g[h] = to == r[n][h] ? 1.f : tc::ex2(r[n][h] - to);
+              r[n][h] = to;
+              rs[n][h] = pow2_bits(kPExp - (int)to);
             }
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
@@ -412,19 +421,20 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
           }
         }
         __syncwarp();                           // (the products take whole warps)
-        const float pc = vsc * pow2_inverse(vref) * kPScale;
         uint32_t pf[NP][NQ][2];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
           const float r0m = m[n][0] == -INFINITY ? 0.f : m[n][0], r1m = m[n][1] == -INFINITY ? 0.f : m[n][1];
+          // (finite, also where a row sees nothing of a page far above its reference)
+          const float c0 = fminf(vsc * rs[n][0], 0x1p127f), c1 = fminf(vsc * rs[n][1], 0x1p127f);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {         // token gid, gid + 8
             const float p0 = tc::ex2(x[n][2 * h] - r0m), p1 = tc::ex2(x[n][2 * h + 1] - r1m);
             l[n][0] += p0;
             l[n][1] += p1;
-            const uint32_t hi = pack_f16(p0 * pc, p1 * pc);
+            const uint32_t hi = pack_f16(p0 * c0, p1 * c1);
             pf[0][n][h] = transpose8(hi);
-            if (NP == 2) pf[NP - 1][n][h] = transpose8(pack_rest(p0 * pc, p1 * pc, hi));
+            if (NP == 2) pf[NP - 1][n][h] = transpose8(pack_rest(p0 * c0, p1 * c1, hi));
           }
         }
         // PV: dimensions gid * D/8 + 4 e + 2 k (row gid of the tile) and + 1 (row gid + 8)
@@ -485,7 +495,7 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       const float2 f = *reinterpret_cast<const float2*>(&sm.wf[warp][8 * n + 2 * tig]);
-      const float g0 = f.x * (vref / kPScale), g1 = f.y * (vref / kPScale);
+      const float g0 = f.x * pow2_inverse(rs[n][0]), g1 = f.y * pow2_inverse(rs[n][1]);
 #pragma unroll
       for (int i = 0; i < NM; ++i) {
         o[n][i][0] *= g0; o[n][i][1] *= g1; o[n][i][2] *= g0; o[n][i][3] *= g1;

@@ -33,12 +33,13 @@
 //
 // Numbers: query rows are scaled by a power of two to a largest magnitude in
 // [128, 256), of fp32 calls in [2^14, 2^15) (their parts keep 2^-39 of it).  Scores
-// are scaled by their page's K scale in fp32.  V codes are multiplied by their
-// page's scale over the tile's largest one (exact but for pages 2^-15 of their
-// tile).  A row's maximum may be passed by 2^10 (fp32: 2^2) before O is rescaled;
-// P = 2^(x - m + 4) (fp32: + 12) times (V scale of the tile / the largest so far),
-// at most 2^14, keeps 11 bits down to 2^-18 of its reference (fp32: 22 bits down
-// to 2^-25).  Row sums are fp32, of unrounded terms.  The tensor cores' fp32 sums
+// are scaled by their page's K scale in fp32.  V codes are fp16 numbers as they are;
+// a page's V scale enters with P (RowRefs, kv8_tc.cuh), so that a row depends on no
+// page that it does not see: P = 2^(x + log2 V scale - reference + 5) (fp32: + 13).
+// A reference may be passed by 2^10 (fp32: 2^2) before O is rescaled, so P is at most
+// 2^15 and its largest above 2^4 (2^12): it keeps 11 bits down to 2^-18 of the largest
+// (fp32: 22 bits down to 2^-15, and 2^-37 of it below).  Row sums are fp32, of unrounded
+// terms.  The tensor cores' fp32 sums
 // cut off, so in fp32 calls the smaller parts are added first and O goes into a
 // sum beside it every four tiles: the error over 29000 tokens falls from 2.5e-5
 // of the output to 1.3e-6 and the time rises by a tenth, with the exponentials'
@@ -71,7 +72,7 @@ template <typename T, int D>
 struct Cfg {
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr float SLACK = F32 ? 2.f : 10.f;          // log2 units
-  static constexpr int PEXP = F32 ? 12 : 4;
+  static constexpr int PEXP = F32 ? 13 : 5;
   // Tiles whose products O takes before it is added to the sum beside it (fp32: the
   // tensor core's sums lose about 2^-26 of O a step, a context of 29000 tokens 2.5e-5).
   static constexpr int FOLD = F32 ? 4 : 1 << 30;
@@ -89,8 +90,7 @@ struct Tc1Smem {
   uint8_t code[C::CS][kTcKT * D];               // codes as they are in the cache: K, K, V, K, V, ..., or V
   float qs[kTcMT];                              // power of two of each query row
   float kscale[kRefs][8];                       // K scale of each 16-token group of tile t, at t % kRefs
-  float vshare[kRefs][8];                       // V scale of each group over the tile's largest
-  float vref[kRefs];                            // the tile's largest V scale
+  float vlog[kRefs][8];                         // log2 of its V scale
   uint64_t q_full, q_empty, k_full[C::KS], k_empty[C::KS], v_full[C::VS], v_empty[C::VS], pv_done;
   uint64_t code_full[C::CS], code_empty[C::CS], ref_full[kRefs];
   uint64_t s_full[2], p_half[2], p_full, done;
@@ -297,9 +297,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
         look(w.t0, pid, ks, vs, live);
         for (int tb = w.t0; ok && tb < w.t1; tb += tpb) {
           if (tb + tpb < w.t1) look(tb + tpb, npid, nks, nvs, nlive);
-          float vref = vs;                      // each tile's largest V scale
-          for (int o = 1; o < ppt; o <<= 1) vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, o));
-          const float vshare = vs * pow2_inverse(vref);
+          const float vlog = scale_log2(vs);
           const int nt = min(tpb, w.t1 - tb);
           for (int i = 0; i < nt; ++i, ++t) {
             const int rt = t % kRefs;
@@ -309,10 +307,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
                      : warp_wait(&sm.k_empty[t % kKStages], ((t / kKStages) & 1) ^ 1, abort);
             if (!ok) break;
             if (bt == i) {
-              if (bp == 0) sm.vref[rt] = vref;
               for (int e = 0; e < c.page / 16; ++e) {
                 sm.kscale[rt][bp * (c.page / 16) + e] = ks;
-                sm.vshare[rt][bp * (c.page / 16) + e] = vshare;
+                sm.vlog[rt][bp * (c.page / 16) + e] = vlog;
               }
             }
             __syncwarp();
@@ -438,7 +435,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
 #pragma unroll
           for (int n = 0; n < 128 / RP; ++n) {
             const int key = key0 + RP * n;
-            expand16(sm.k[ks], key, ch, *reinterpret_cast<const uint4*>(sm.code[st] + key * D + ch * 16), 1.f);
+            expand16(sm.k[ks], key, ch, *reinterpret_cast<const uint4*>(sm.code[st] + key * D + ch * 16));
           }
           fence_proxy_async();
           __syncwarp();
@@ -454,7 +451,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
           ok = warp_wait(&sm.code_full[st], (item / kCodeStages) & 1, abort) &&
                warp_wait(&sm.v_empty[vs], ((tv / kVStages) & 1) ^ 1, abort);
           if (!ok) break;
-          const float* share = sm.vshare[tv % kRefs];
           const bool mixed = j * kTcKT > lim_min;               // some rows do not see all of it
           if (mixed) {                          // (a pass of its own: within the loop below it costs every tile)
 #pragma unroll 1
@@ -472,7 +468,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             const int key = key0 + RP * n;
             uint4 y = *reinterpret_cast<const uint4*>(sm.code[st] + key * D + ch * 16);
             if (key >= left) y = make_uint4(0u, 0u, 0u, 0u);      // not a token: whatever was there
-            expand16(sm.v[vs][0], key, ch, y, share[key >> 4]);
+            expand16(sm.v[vs][0], key, ch, y);
           }
           fence_proxy_async();
           __syncwarp();
@@ -499,7 +495,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
       const int qi = rho / G, qj = rho - qi * G;
       int lim = w.u.kend;
       if (a.causal) lim = min(lim, w.u.q.len - w.u.q.m + 1 + qi);
-      float m = -INFINITY, l = 0.f, cs = 0.f, vmax = 0.f;
+      RowRefs ref;
+      ref.clear();
+      float cs = 0.f;
       for (int j = w.t0; j < w.t1; ++j, ++t) {
         ok = ok && warp_wait(&sm.s_full[t & 1], (t >> 1) & 1, abort) &&
              warp_wait(&sm.ref_full[t % kRefs], (t / kRefs) & 1, abort) &&
@@ -509,7 +507,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
         const uint32_t s_col = tbase + lane_off + kSCol + (t & 1) * kTcKT;
         if (j == w.t0) cs = a.scale_log2 * sm.qs[row];
         // factor of each 16 scores (above 0, so that a masked one stays -inf)
-        const float vr = sm.vref[t % kRefs];
         float f[8];
         {
           const float4 k0 = *reinterpret_cast<const float4*>(&sm.kscale[t % kRefs][0]);
@@ -548,22 +545,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
           for (int q = 2; q < 16; q += 2) b[p] = fmax3(b[p], x[p][q], x[p][q + 1]);
           b[p] *= f[p];
         }
-        const float tm = fmax3(fmax3(b[0], b[1], b[2]), fmax3(b[3], b[4], b[5]), fmaxf(b[6], b[7]));
-        const bool raise = tm > m + kTcSlack, vraise = vr > vmax;
-        float g = 1.f;
-        if (raise) {
-          g = ex2(m - tm);                      // 0 on the first
-          l *= g;
-          m = tm;
-        }
-        if (vraise) {
-          // one step above, so that a tile with a page of the next size fits
-          const float up = vr * 2.f;
-          g *= vmax * pow2_inverse(up);
-          vmax = up;
-        }
+        const float* vlog = sm.vlog[t % kRefs];
+        float g;
+        const bool rise = ref.raise(b, vlog, kTcSlack, g);
         const bool fold = j > w.t0 && C::fresh(j - w.t0);
-        if (j > w.t0 && (fold || __any_sync(0xffffffffu, raise || vraise))) {
+        if (j > w.t0 && (fold || __any_sync(0xffffffffu, rise))) {
           // the PV of the tile before is done, the next waits for this P
           ok = warp_wait(&sm.pv_done, (t & 1) ^ 1, abort);
           if (!ok) continue;
@@ -589,30 +575,39 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
           }
         }
         __syncwarp();                           // (whole warps store P)
-        // exponent of P's factor: 2^12 times the tile's share of vmax, not below 2^-18
-        const int lc = vr > 0.f ? max(-30, (int)(__float_as_uint(vr) >> 23) - (int)(__float_as_uint(vmax) >> 23)) : -30;
-        // (fp32: the factor after the exponential, so that the largest terms' exponents are small numbers)
-        const float mm = (m == -INFINITY ? 0.f : m) - (F32 ? 0.f : (float)(lc + kTcPExp));
-        const float2 nm = make_float2(-mm, -mm);
-        const float pf = __uint_as_float((uint32_t)(127 + lc + kTcPExp) << 23);
-        float2 l0 = make_float2(0.f, 0.f), l1 = make_float2(0.f, 0.f);
+        const float mr = ref.base(), lift = kTcPExp - ref.value_base();
+        float2 ls = make_float2(0.f, 0.f);
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           uint32_t top[16], rest[16];
+          const float2 v2 = *reinterpret_cast<const float2*>(vlog + 2 * h);
 #pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            const int k = 32 * h + 2 * q;
-            const float2 y = __ffma2_rn(make_float2(x[k >> 4][k & 15], x[k >> 4][(k & 15) + 1]),
-                                        make_float2(f[k >> 4], f[k >> 4]), nm);
-            const float2 e = make_float2(ex2(y.x), ex2(y.y));
-            if (q & 1) l1 = __fadd2_rn(l1, e);
-            else l0 = __fadd2_rn(l0, e);
+          for (int gr = 0; gr < 2; ++gr) {      // 16 tokens: one page's
+            const int p = 2 * h + gr;
+            // exponent of the page's factor in P; what P's sum then takes for the row's
+            const float e = fmaxf((gr ? v2.y : v2.x) + lift, kLeastShare);
+            // (fp32: the factor after the exponential, so that the largest terms' exponents are small numbers)
+            const float2 nm = F32 ? make_float2(-mr, -mr) : make_float2(e - mr, e - mr);
+            const float pf = pow2_bits((int)fminf(e, 127.f));
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const float2 y = __ffma2_rn(make_float2(x[p][2 * q], x[p][2 * q + 1]), make_float2(f[p], f[p]), nm);
+              const float2 ex = make_float2(ex2(y.x), ex2(y.y));
+              sum = q ? __fadd2_rn(sum, ex) : ex;
+              if constexpr (F32) {
+                const float2 pe = __fmul2_rn(ex, make_float2(pf, pf));
+                top[8 * gr + q] = half2_bits(pe.x, pe.y);
+                rest[8 * gr + q] = half2_rest(pe.x, pe.y, top[8 * gr + q]);
+              } else {
+                top[8 * gr + q] = half2_bits(ex.x, ex.y);
+              }
+            }
             if constexpr (F32) {
-              const float2 pe = __fmul2_rn(e, make_float2(pf, pf));
-              top[q] = half2_bits(pe.x, pe.y);
-              rest[q] = half2_rest(pe.x, pe.y, top[q]);
+              ls = __fadd2_rn(ls, sum);
             } else {
-              top[q] = half2_bits(e.x, e.y);
+              const float back = ex2(-e);
+              ls = __ffma2_rn(sum, make_float2(back, back), ls);
             }
           }
           tmem_st16(s_col + h * 16, top);
@@ -624,8 +619,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             if (lane == 0) mbar_arrive(&sm.p_half[t & 1]);
           }
         }
-        const float2 ls = __fadd2_rn(l0, l1);
-        l += F32 ? ls.x + ls.y : (ls.x + ls.y) * __uint_as_float((uint32_t)(127 - lc - kTcPExp) << 23);
+        ref.l += ls.x + ls.y;
         // the PV of the tile before in turn, so that no wait for one is two phases behind
         ok = warp_wait(&sm.pv_done, (t & 1) ^ 1, abort);
         if (!ok) continue;
@@ -638,8 +632,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
       ++seg;
       if (named_sync_any(1, 128, !ok)) break;
       tc_fence_after();
-      // O in units of vmax * 2^-12
-      const float ou = vmax * __uint_as_float((uint32_t)(127 - kTcPExp) << 23);
+      // O in units of 2^(r - kTcPExp)
+      const float2 ou = pow2_factors((int)ref.value_base() - kTcPExp);
       const bool whole = w.whole();
       const int64_t at = (int64_t)(w.u.q.row0 + qi) * a.Hq + w.u.g * G + qj;
       auto put_out = [&](int64_t at, int col, const float (&y)[16], float inv) {
@@ -667,7 +661,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
       const int nan_from = sm.nan_token[(seg - 1) & 1][warp], nan_to = min(lim, w.t1 * kTcKT);
       __syncwarp();
       if (lane == 0) sm.nan_token[(seg - 1) & 1][warp] = kNoNan;
-      const float inv = whole ? inverse_of(l) * ou : ou;
+      const float inv = whole ? inverse_of(ref.l) : 1.f;
 #pragma unroll 1
       for (int p = 0; p < D / 16; ++p) {
         uint32_t v[16];
@@ -685,6 +679,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             for (int q = 0; q < 16; ++q) y[q] += __uint_as_float(v[q]);
           }
         }
+#pragma unroll
+        for (int q = 0; q < 16; ++q) y[q] = y[q] * ou.x * inv * ou.y;
         if (nan_from < nan_to && real) {
           const uint32_t bad = nan_dims<16>(c, s, w.u.r, w.u.g, nan_from, nan_to, p * 16);
 #pragma unroll
@@ -692,21 +688,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             if (bad >> q & 1u) y[q] = __uint_as_float(0x7fffffffu);
         }
         if (whole) {
-          if (real) put_out(at, p * 16, y, inv);
+          if (real) put_out(at, p * 16, y, 1.f);
         } else {
           // (four columns of the row tile's rows side by side)
           float4* po = reinterpret_cast<float4*>(a.part_o + mine * 128 * D) + p * 4 * 128 + row;
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            if (real)
-              po[q * 128] = make_float4(y[4 * q] * inv, y[4 * q + 1] * inv, y[4 * q + 2] * inv, y[4 * q + 3] * inv);
+            if (real) po[q * 128] = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
         }
       }
       tc_fence_before();
       if (whole) {
-        if (real) put_lse(at, m, l);
+        if (real) put_lse(at, ref.m, ref.l);
       } else {
-        if (real) a.part_ml[mine * 128 + row] = make_float2(m, l);
+        if (real) a.part_ml[mine * 128 + row] = make_float2(ref.m, ref.l);
         const int first = w.first_block(sh), final = w.last_block(sh);
         __syncwarp();                           // (the named barriers take whole warps)
         named_sync(1, 128);

@@ -40,11 +40,11 @@
 // reads, and s_full of tile t + 1 says that PV(t) is done too.
 //
 // Numbers: query rows are scaled by a power of two to a largest magnitude in
-// [128, 256).  Scores are scaled by their page's K scale in fp32.  V codes are
-// multiplied by their page's scale over the tile's largest one (exact but for
-// pages 2^-14 of their tile).  A row's maximum may be passed by 2^10 before O
-// is rescaled; P = 2^(x - m + 4) times (V scale of the tile / the largest so
-// far), at most 2^14, keeps 11 bits down to 2^-18 of its reference.  Row sums
+// [128, 256).  Scores are scaled by their page's K scale in fp32.  V codes are fp16
+// numbers as they are; a page's V scale enters with P (RowRefs, kv8_tc.cuh), so that
+// a row depends on no page that it does not see: P = 2^(x + log2 V scale - reference
+// + 5).  A reference may be passed by 2^10 before O is rescaled, so P is at most 2^15
+// and its largest above 2^4: it keeps 11 bits down to 2^-18 of the largest.  Row sums
 // are fp32, of unrounded terms.
 #include "kernels.h"
 #include "kv8.cuh"
@@ -64,7 +64,7 @@ constexpr int kTcThreads = 512;
 constexpr int kTcMT = 256, kTcKT = 128;
 constexpr int kConvWarp0 = 8, kConvWarps = 4, kIssueWarp = 12, kLoadWarp = 13;
 constexpr float kTcSlack = 10.f;                // log2 units
-constexpr int kTcPExp = 4;
+constexpr int kTcPExp = 5;
 constexpr uint32_t kSCol = 0, kOCol = 256;
 constexpr int kKStages = 3, kVStages = 2, kCodeStages = 2;
 constexpr int kRefs = 8;                        // tiles whose scales are kept (the loader is at most 4 ahead)
@@ -77,8 +77,7 @@ struct TcSmem {
   uint8_t code[kCodeStages][kTcKT * D];         // V codes as they are in the cache
   float qs[kTcMT];                              // power of two of each query row
   float kscale[kRefs][8];                       // K scale of each 16-token group of tile t, at t % kRefs
-  float vshare[kRefs][8];                       // V scale of each group over the tile's largest
-  float vref[kRefs];                            // the tile's largest V scale
+  float vlog[kRefs][8];                         // log2 of its V scale
   uint64_t q_full, q_empty, k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t code_full[kCodeStages], code_empty[kCodeStages], ref_full[kRefs];
   uint64_t s_full[2], p_full[2], p_half[2], o_full[2], done;
@@ -264,9 +263,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         look(w.t0, pid, ks, vs, live);
         for (int tb = w.t0; ok && tb < w.t1; tb += tpb) {
           if (tb + tpb < w.t1) look(tb + tpb, npid, nks, nvs, nlive);
-          float vref = vs;                      // each tile's largest V scale
-          for (int o = 1; o < ppt; o <<= 1) vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, o));
-          const float vshare = vs * pow2_inverse(vref);
+          const float vlog = scale_log2(vs);
           const int nt = min(tpb, w.t1 - tb);
           // (a page that does not exist has scale 0: page 0 stands in)
           const int row = (max(pid, 0) * c.Hkv + w.u.g) * c.page;
@@ -277,10 +274,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
             ok = warp_wait(&sm.k_empty[kst], ((t / kKStages) & 1) ^ 1, abort);
             if (!ok) break;
             if (mine) {
-              if (bp == 0) sm.vref[rt] = vref;
               for (int e = 0; e < c.page / 16; ++e) {
                 sm.kscale[rt][bp * (c.page / 16) + e] = ks;
-                sm.vshare[rt][bp * (c.page / 16) + e] = vshare;
+                sm.vlog[rt][bp * (c.page / 16) + e] = vlog;
               }
             }
             __syncwarp();
@@ -387,7 +383,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         if (!ok) break;
         constexpr int LPR = D / 16, RP = 128 / LPR;     // lanes of a row (16 codes each), rows at once
         const int key0 = i / LPR, ch = i % LPR;
-        const float* share = sm.vshare[t % kRefs];
         const bool mixed = (j + 1) * kTcKT > lim_min;           // some rows do not see all of it
         if (mixed) {                            // (a pass of its own: 4% of a long chunk within the loop below)
 #pragma unroll 1
@@ -408,7 +403,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
           const int key = key0 + RP * n;
           uint4 y = *reinterpret_cast<const uint4*>(sm.code[cst] + key * D + ch * 16);
           if (key >= left) y = make_uint4(0u, 0u, 0u, 0u);      // not a token: whatever was there
-          expand16(sm.v[st][0], key, ch, y, share[key >> 4]);
+          expand16(sm.v[st][0], key, ch, y);
         }
         fence_proxy_async();
         __syncwarp();
@@ -440,7 +435,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
       const int qi = rho / G, qj = rho - qi * G;
       int lim = w.u.kend;
       if (a.causal) lim = min(lim, w.u.q.len - w.u.q.m + 1 + qi);
-      float m = -INFINITY, l = 0.f, cs = 0.f, vmax = 0.f;
+      RowRefs ref;
+      ref.clear();
+      float cs = 0.f;
       for (int j = w.t0; j < w.t1; ++j, ++t) {
         // S first: then the scales' (and the query rows') barriers are at the phase
         // asked for, also where this row tile sat out the segments before
@@ -452,7 +449,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         tc_fence_after();
         if (j == w.t0) cs = a.scale_log2 * sm.qs[X * 128 + row];
         // factor of each 16 scores (above 0, so that a masked one stays -inf)
-        const float vr = sm.vref[t % kRefs];
         float f[8];
         {
           const float4 k0 = *reinterpret_cast<const float4*>(&sm.kscale[t % kRefs][0]);
@@ -491,21 +487,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
           for (int q = 2; q < 16; q += 2) b[p] = fmax3(b[p], x[p][q], x[p][q + 1]);
           b[p] *= f[p];
         }
-        const float tm = fmax3(fmax3(b[0], b[1], b[2]), fmax3(b[3], b[4], b[5]), fmaxf(b[6], b[7]));
-        const bool raise = tm > m + kTcSlack, vraise = vr > vmax;
-        float g = 1.f;
-        if (raise) {
-          g = ex2(m - tm);                      // 0 on the first
-          l *= g;
-          m = tm;
-        }
-        if (vraise) {
-          // one step above, so that a tile with a page of the next size fits
-          const float up = vr * 2.f;
-          g *= vmax * pow2_inverse(up);
-          vmax = up;
-        }
-        if (j > w.t0 && __any_sync(0xffffffffu, raise || vraise)) {
+        const float* vlog = sm.vlog[t % kRefs];
+        float g;
+        const bool rise = ref.raise(b, vlog, kTcSlack, g);
+        if (j > w.t0 && __any_sync(0xffffffffu, rise)) {
           // PV of the tile before is done (s_full) and the next waits for this P
 #pragma unroll 1
           for (int p = 0; p < D / 16; ++p) {
@@ -518,23 +503,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
           }
         }
         __syncwarp();                           // (whole warps store P)
-        // exponent of P's factor: 2^4 times the tile's share of vmax, not below 2^-26
-        const int lc = vr > 0.f ? max(-30, (int)(__float_as_uint(vr) >> 23) - (int)(__float_as_uint(vmax) >> 23)) : -30;
-        const float mm = (m == -INFINITY ? 0.f : m) - (float)(lc + kTcPExp);
-        const float2 nm = make_float2(-mm, -mm);
-        float2 l0 = make_float2(0.f, 0.f), l1 = make_float2(0.f, 0.f);
+        const float mr = ref.base(), lift = kTcPExp - ref.value_base();
+        float2 ls = make_float2(0.f, 0.f);
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           uint32_t y16[16];
+          const float2 v2 = *reinterpret_cast<const float2*>(vlog + 2 * h);
 #pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            const int k = 32 * h + 2 * q;
-            const float2 y = __ffma2_rn(make_float2(x[k >> 4][k & 15], x[k >> 4][(k & 15) + 1]),
-                                        make_float2(f[k >> 4], f[k >> 4]), nm);
-            const float2 e = make_float2(ex2(y.x), ex2(y.y));
-            if (q & 1) l1 = __fadd2_rn(l1, e);
-            else l0 = __fadd2_rn(l0, e);
-            y16[q] = half2_bits(e.x, e.y);
+          for (int gr = 0; gr < 2; ++gr) {      // 16 tokens: one page's
+            const int p = 2 * h + gr;
+            // exponent of the page's factor in P; what P's sum then takes for the row's
+            const float e = fmaxf((gr ? v2.y : v2.x) + lift, kLeastShare), back = ex2(-e);
+            const float2 nm = make_float2(e - mr, e - mr);
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const float2 y = __ffma2_rn(make_float2(x[p][2 * q], x[p][2 * q + 1]), make_float2(f[p], f[p]), nm);
+              const float2 ex = make_float2(ex2(y.x), ex2(y.y));
+              sum = q ? __fadd2_rn(sum, ex) : ex;
+              y16[8 * gr + q] = half2_bits(ex.x, ex.y);
+            }
+            ls = __ffma2_rn(sum, make_float2(back, back), ls);
           }
           tmem_st16(s_col + h * 16, y16);
           if (h == 1) {                         // the first half may be multiplied
@@ -544,8 +533,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
             if (lane == 0) mbar_arrive(&sm.p_half[X]);
           }
         }
-        const float2 ls = __fadd2_rn(l0, l1);
-        l += (ls.x + ls.y) * __uint_as_float((uint32_t)(127 - lc - kTcPExp) << 23);
+        ref.l += ls.x + ls.y;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -556,8 +544,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
       ++seg;
       if (named_sync_any(1 + X, 128, !ok)) break;
       tc_fence_after();
-      // O in units of vmax * 2^-4
-      const float ou = vmax * __uint_as_float((uint32_t)(127 - kTcPExp) << 23);
+      // O in units of 2^(r - kTcPExp)
+      const float2 ou = pow2_factors((int)ref.value_base() - kTcPExp);
       const bool whole = w.whole();
       const int64_t at = (int64_t)(w.u.q.row0 + qi) * a.Hq + w.u.g * G + qj;
       auto put_out = [&](int64_t at, int col, const float (&y)[16], float inv) {
@@ -579,7 +567,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
       const int nan_from = nan_token, nan_to = min(lim, w.t1 * kTcKT);
       __syncwarp();
       if (lane == 0) nan_token = kNoNan;
-      const float inv = whole ? inverse_of(l) * ou : ou;
+      const float inv = whole ? inverse_of(ref.l) : 1.f;
 #pragma unroll 1
       for (int p = 0; p < D / 16; ++p) {
         uint32_t v[16];
@@ -588,7 +576,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         tmem_wait(v);
         float y[16];
 #pragma unroll
-        for (int q = 0; q < 16; ++q) y[q] = __uint_as_float(v[q]);
+        for (int q = 0; q < 16; ++q) y[q] = __uint_as_float(v[q]) * ou.x * inv * ou.y;
         if (nan_from < nan_to && real) {
           const uint32_t bad = nan_dims<16>(c, s, w.u.r, w.u.g, nan_from, nan_to, p * 16);
 #pragma unroll
@@ -596,20 +584,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
             if (bad >> q & 1u) y[q] = __uint_as_float(0x7fffffffu);
         }
         if (whole) {
-          if (real) put_out(at, p * 16, y, inv);
+          if (real) put_out(at, p * 16, y, 1.f);
         } else {
           // (four columns of the row tile's rows side by side)
           float4* po = reinterpret_cast<float4*>(a.part_o + (mine * 2 + X) * 128 * D) + p * 4 * 128 + row;
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            if (real) po[q * 128] = make_float4(y[4 * q] * inv, y[4 * q + 1] * inv, y[4 * q + 2] * inv, y[4 * q + 3] * inv);
+            if (real) po[q * 128] = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
         }
       }
       tc_fence_before();
       if (whole) {
-        if (real) put_lse(at, m, l);
+        if (real) put_lse(at, ref.m, ref.l);
       } else {
-        if (real) a.part_ml[(mine * 2 + X) * 128 + row] = make_float2(m, l);
+        if (real) a.part_ml[(mine * 2 + X) * 128 + row] = make_float2(ref.m, ref.l);
         const int first = w.first_block(sh), final = w.last_block(sh);
         __syncwarp();                           // (the named barriers take whole warps)
         named_sync(1 + X, 128);

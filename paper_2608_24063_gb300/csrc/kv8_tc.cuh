@@ -12,6 +12,10 @@ namespace kv8 {
 
 using namespace tc;
 
+// Least exponent that a page's scale gives P's factor: below it P is 0 in fp16 anyway, and
+// the row's sum is still read off P.
+constexpr float kLeastShare = -80.f;
+
 constexpr uint32_t kBlk = 128 * 128;            // 128 rows x 128 bytes (64 fp16 columns)
 
 // Instruction descriptors, D fp32: kind::f16 with A, B fp16, both K-major or B
@@ -100,22 +104,17 @@ __device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t bits
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&bits));
   return half2_bits(lo - f.x, hi - f.y);
 }
-__device__ __forceinline__ uint32_t hmul2_bits(uint32_t a, __half2 f) {
-  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), f);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 
-// Sixteen codes times a power of two, as 32 bytes of row `row`, column chunk c
+// Sixteen codes as fp16 numbers (exact): 32 bytes of row `row`, column chunk c
 // (16 columns) of a tile: the two 16-byte pieces are written in an order that
 // keeps the eight lanes of a row on different banks.
-__device__ __forceinline__ void expand16(uint8_t* tile, int row, int c, const uint4& w, float factor) {
-  const __half2 f = __float2half2_rn(factor);
+__device__ __forceinline__ void expand16(uint8_t* tile, int row, int c, const uint4& w) {
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
   uint32_t y[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    y[2 * i] = hmul2_bits(e4m3x2_to_f16x2(x[i]), f);
-    y[2 * i + 1] = hmul2_bits(e4m3x2_to_f16x2(x[i] >> 16), f);
+    y[2 * i] = e4m3x2_to_f16x2(x[i]);
+    y[2 * i + 1] = e4m3x2_to_f16x2(x[i] >> 16);
   }
   uint8_t* base = tile + (c >> 2) * kBlk + row * 128;
   const int ch = 2 * (c & 3), r7 = row & 7;
@@ -131,6 +130,43 @@ __device__ __forceinline__ bool drop_nan(uint4& y) {
   y.x &= ~n[0]; y.y &= ~n[1]; y.z &= ~n[2]; y.w &= ~n[3];
   return (n[0] | n[1] | n[2] | n[3]) != 0u;
 }
+
+// The references of a row's softmax, log2 units.  x is a score, v the log2 of its page's V
+// scale.  m follows the largest x and r + m the largest x + v, both of what the row sees
+// and in whole numbers (so that differences of exponents are exact), and each may be
+// passed by `slack` before it rises.  P = 2^(x + v - m - r + const) multiplies the codes as
+// they are: a page's scale enters with its tokens' probabilities, so a row's fixed point is
+// set by its largest contribution and by nothing that it does not see or that has no weight.
+struct RowRefs {
+  float m, r, l;
+  __device__ __forceinline__ void clear() {
+    m = r = -INFINITY;
+    l = 0.f;
+  }
+  // b: largest x of each 16-token group; whether O's reference rises (O times g then)
+  __device__ __forceinline__ bool raise(const float (&b)[8], const float* vlog, float slack, float& g) {
+    const float tx = fmax3(fmax3(b[0], b[1], b[2]), fmax3(b[3], b[4], b[5]), fmaxf(b[6], b[7]));
+    if (tx > m + slack) {
+      const float up = ceilf(tx);
+      l *= ex2(m - up);                         // 0 on the first
+      r -= up - m;
+      m = up;
+    }
+    const float4 v0 = *reinterpret_cast<const float4*>(vlog), v1 = *reinterpret_cast<const float4*>(vlog + 4);
+    const float mr = base();
+    const float ty = fmax3(fmax3(b[0] - mr + v0.x, b[1] - mr + v0.y, b[2] - mr + v0.z),
+                           fmax3(b[3] - mr + v0.w, b[4] - mr + v1.x, b[5] - mr + v1.y),
+                           fmaxf(b[6] - mr + v1.z, b[7] - mr + v1.w));
+    g = 1.f;
+    if (!(ty > r + slack)) return false;
+    const float up = ceilf(ty);
+    g = ex2(r - up);
+    r = up;
+    return true;
+  }
+  __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.f : m; }
+  __device__ __forceinline__ float value_base() const { return r == -INFINITY ? 0.f : r; }
+};
 
 // 1 / a row's sum; 0 where it saw no token, NaN stays.
 __device__ __forceinline__ float inverse_of(float L) { return L > 0.f ? 1.f / L : (L == L ? 0.f : L); }
