@@ -585,8 +585,9 @@ int viscache_kv8_read(const vc_kv8* cache, const vc_kv8_step* step, int dtype, v
  *           normaliser, -inf for a row that sees no token
  * Arithmetic: e4m3 values and query rows enter the products as numbers of few
  * bits times powers of two.  fp32 rows and fp32 calls' probabilities are sums
- * of two fp16 numbers (22 bits).  bf16 rows are fp16 numbers, exact for values
- * down to 2^-14 of their row's largest; in calls of many rows (more than 16 rows
+ * of two fp16 numbers (22 bits; of a row's values down to 2^-17 of its largest, and
+ * 2^-39 of it below).  bf16 rows are fp16 numbers, exact for values
+ * down to 2^-31 of their row's largest; in calls of many rows (more than 16 rows
  * of a KV head per request and work for every SM, judged by n_rows, n_req and
  * max_pages) they are sums of two e4m3 numbers, exact down to 2^-9 of the row's
  * largest and within 2^-17 of it below.  A probability times its page's V scale

@@ -21,10 +21,10 @@
 // pairs them with byte permutations and converts.  QK leaves probabilities as
 // (token, query); movmatrix turns them into PV's (query, token).
 //
-// Numbers: a query row is divided by the power of two below its largest
-// magnitude, which makes fp16 hold bf16 values exactly (down to 2^-14 of that
-// magnitude, then to 2^-24 of it); fp32 calls use a second fp16 part of the
-// row and of the probabilities.  Scores are scaled by the page's K scale in
+// Numbers: a query row is multiplied by the power of two that brings its largest
+// magnitude to [2^14, 2^15), so that fp16 holds bf16 values exactly down to 2^-31 of
+// it; fp32 calls use a second fp16 part of the row (22 bits down to 2^-17 of the
+// largest, 2^-39 of it below) and of the probabilities.  Scores are scaled by the page's K scale in
 // fp32.  Probabilities enter as p * 2^(12 - r) * V scale, r + m following the
 // row's largest score + log2 of its V scale: a row's fixed point is set by its
 // largest contribution, not by values that it does not see or that have no
@@ -167,8 +167,8 @@ __device__ __forceinline__ void load_q(const T* q, int64_t q_stride, const Unit&
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
-    // zero, tiny or not finite rows as they are; 2^126 at most, whose inverse is normal
-    const float p2 = ex == 0u || ex == 0x7f800000u ? 1.f : __uint_as_float(min(ex, 253u << 23));
+    // 2^-126 at least, so that it and its inverse are normal; a row that is not finite as it is
+    const float p2 = ex == 0x7f800000u ? 1.f : __uint_as_float(max(ex, 15u << 23) - (14u << 23));
     const float inv = pow2_inverse(p2);
     qs[n][0] = __shfl_sync(0xffffffffu, p2, 8 * tig);
     qs[n][1] = __shfl_sync(0xffffffffu, p2, 8 * tig + 4);
