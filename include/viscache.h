@@ -589,8 +589,8 @@ int viscache_kv8_read(const vc_kv8* cache, const vc_kv8_step* step, int dtype, v
  * 2^-39 of it below).  bf16 rows are fp16 numbers, exact for values
  * down to 2^-31 of their row's largest; in calls of many rows (more than 16 rows
  * of a KV head per request and work for every SM, judged by n_rows, n_req and
- * max_pages) they are sums of two e4m3 numbers, exact down to 2^-9 of the row's
- * largest and within 2^-17 of it below.  A probability times its page's V scale
+ * max_pages) they are sums of an e4m3 and an e5m2 number, exact down to 2^-13 of the
+ * row's largest and within 2^-21 of it below.  A probability times its page's V scale
  * is rounded to fp16 in bf16 calls: 11 bits, down to 2^-18 of the row's largest such
  * product, 2^-29 of it below (fp32 calls: 22 bits down to 2^-14, 2^-36 below; fewer
  * where a row sees no scale above 2^-100).  Only

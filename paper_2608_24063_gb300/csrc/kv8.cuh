@@ -58,6 +58,13 @@ __device__ __forceinline__ uint32_t f32x2_to_e4m3x2(float x, float y) {
   return r;
 }
 
+// Two fp32 numbers of any size, or NaN, -> e5m2 pair, to nearest even.
+__device__ __forceinline__ uint32_t f32x2_to_e5m2x2(float x, float y) {
+  unsigned short r;
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y), "f"(x));
+  return r;
+}
+
 // The least power of two s = 2^e, e >= -126, with amax <= 448 s; 0 for 0.
 // 448 = 1.75 * 2^8, so e is amax's exponent minus 8, or minus 7 where its
 // mantissa is above 1.75 (below 2^-126 the clamp decides).

@@ -6,13 +6,12 @@
 // next tile's products do.  Persistent blocks, one per SM, share out the line of
 // key tiles (kv8_sched.cuh).
 //
-// bf16 rows.  S = Q K^T runs on the codes as they are (kind::f8f6f4): a bf16
-// number has 8 significant bits and an e4m3 number 4, so a query value is exactly
-// the sum of two e4m3 numbers, its rounding and the rest (values below 2^-9 of
-// their row's largest are off by up to 2^-17 of it: the largest lies in [128, 256)
-// and e4m3 ends at steps of 2^-9).  Two products at twice the rate cost what one
-// fp16 product does, and K needs no expansion: TMA writes its tiles.  O = P V runs
-// in fp16: P needs more than e4m3's range, so V is expanded.
+// bf16 rows.  S = Q K^T runs on the codes as they are (kind::f8f6f4): a query value is
+// the sum of its rounding to e4m3 and the rest in e5m2 (split8, kv8_tc.cuh), exact down
+// to 2^-13 of its row's largest, which lies in [128, 256), and within 2^-21 of it below.
+// Two products at twice the rate cost what one fp16 product does, and K needs no
+// expansion: TMA writes its tiles.  O = P V runs in fp16: P needs more than e4m3's
+// range, so V is expanded.
 // fp32 rows.  Rows and probabilities are sums of two fp16 numbers (22 bits), and K
 // and V are both expanded to fp16 (exact), K a tile ahead of V.
 //
@@ -84,7 +83,7 @@ struct Cfg {
 template <typename T, int D>
 struct Tc1Smem {
   using C = Cfg<T, D>;
-  uint8_t q[2][C::QPART];                       // query rows of the unit, [larger part, rest]: fp16 or e4m3
+  uint8_t q[2][C::QPART];                       // query rows of the unit, [larger part, rest]: fp16, or e4m3 and e5m2
   uint8_t k[C::KS][C::KTILE];                   // K as fp16, or its codes
   uint8_t v[C::VS][D / 64][kBlk];               // V as fp16, [stage][64-column block]
   uint8_t code[C::CS][kTcKT * D];               // codes as they are in the cache: K, K, V, K, V, ..., or V
@@ -189,6 +188,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
     if (warp == kIssueWarp) {
       // ---- MMA issuer
       constexpr uint32_t id_s = F32 ? idesc_f16(128, kTcKT) : idesc_e4m3(128, kTcKT), id_o = idesc_f16_bmn(128, D);
+      constexpr uint32_t id_rest = idesc_e5m2_e4m3(128, kTcKT);
       bool ok = true;
       const uint64_t qd = F32 ? desc_sw128(smem_u32(sm.q)) : desc_codes<D>(smem_u32(sm.q));
       const uint64_t kd = F32 ? desc_sw128(smem_u32(sm.k)) : desc_codes<D>(smem_u32(sm.k));
@@ -228,7 +228,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             } else {
 #pragma unroll
               for (int kk = 0; kk < 2 * (D / 32); ++kk)
-                mma_e4m3_ss(d, qd + (kk & 1) * kQ16 + (kk >> 1) * 2, bd + (kk >> 1) * 2, id_s, kk ? 1u : 0u);
+                mma_f8_ss(d, qd + (kk & 1) * kQ16 + (kk >> 1) * 2, bd + (kk >> 1) * 2, kk & 1 ? id_rest : id_s,
+                          kk ? 1u : 0u);
             }
             mma_commit_elected(&sm.s_full[tk & 1]);
             mma_commit_elected(&sm.k_empty[ks]);
@@ -397,26 +398,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             *reinterpret_cast<uint4*>(sm.q[0] + off) = make_uint4(top[0], top[1], top[2], top[3]);
             *reinterpret_cast<uint4*>(sm.q[1] + off) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
           } else {
-            uint32_t top[2], rest[2];
+            float z[8];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float z[4], r4[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                z[k] = x[4 * e + k] * inv;
-                if (!(fabsf(z[k]) <= 448.f)) z[k] = __uint_as_float(0x7fffffffu);      // NaN, infinite
-              }
-              const uint32_t p0 = f32x2_to_e4m3x2(z[0], z[1]), p1 = f32x2_to_e4m3x2(z[2], z[3]);
-              const uint32_t h0 = e4m3x2_to_f16x2(p0), h1 = e4m3x2_to_f16x2(p1);
-              const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0));
-              const float2 f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-              r4[0] = z[0] - f0.x; r4[1] = z[1] - f0.y; r4[2] = z[2] - f1.x; r4[3] = z[3] - f1.y;
-              top[e] = p0 | p1 << 16;
-              rest[e] = f32x2_to_e4m3x2(r4[0], r4[1]) | f32x2_to_e4m3x2(r4[2], r4[3]) << 16;
-            }
+            for (int e = 0; e < 8; ++e) z[e] = x[e] * inv;
+            uint2 top, rest;
+            split8(z, top, rest);
             const uint32_t off = code_piece<D>(r, qc);
-            *reinterpret_cast<uint2*>(sm.q[0] + off) = make_uint2(top[0], top[1]);
-            *reinterpret_cast<uint2*>(sm.q[1] + off) = make_uint2(rest[0], rest[1]);
+            *reinterpret_cast<uint2*>(sm.q[0] + off) = top;
+            *reinterpret_cast<uint2*>(sm.q[1] + off) = rest;
           }
           if (qc == 0) sm.qs[r] = qs;
         }

@@ -14,12 +14,11 @@
 // them.  Persistent blocks, one per SM, share out the line of key tiles
 // (kv8_sched.cuh).
 //
-// S = Q K^T runs on the codes as they are (kind::f8f6f4): a bf16 number has 8
-// significant bits and an e4m3 number 4, so a query value is exactly the sum
-// of two e4m3 numbers, its rounding and the rest (values below 2^-9 of their
-// row's largest are off by up to 2^-17 of it: the largest lies in [128, 256) and
-// e4m3 ends at steps of 2^-9).  Two products at twice the rate cost what
-// one fp16 product does, and K needs no expansion: TMA writes its tiles.
+// S = Q K^T runs on the codes as they are (kind::f8f6f4): a query value is the
+// sum of its rounding to e4m3 and the rest in e5m2 (split8, kv8_tc.cuh), exact
+// down to 2^-13 of its row's largest, which lies in [128, 256), and within 2^-21 of
+// it below.  Two products at twice the rate cost what one fp16 product does, and K
+// needs no expansion: TMA writes its tiles.
 // O = P V runs in fp16: P needs more than e4m3's range, so V is expanded,
 // once for both row tiles.
 //
@@ -155,7 +154,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == kIssueWarp) {
       // ---- MMA issuer
-      constexpr uint32_t id_s = idesc_e4m3(128, kTcKT), id_o = idesc_f16_bmn(128, D);
+      constexpr uint32_t id_s = idesc_e4m3(128, kTcKT), id_rest = idesc_e5m2_e4m3(128, kTcKT);
+      constexpr uint32_t id_o = idesc_f16_bmn(128, D);
       bool ok = true;
       int np[2] = {0, 0};                       // P tiles consumed per row tile
       const uint64_t qd = desc_codes<D>(smem_u32(sm.q)), kd = desc_codes<D>(smem_u32(sm.k));
@@ -168,8 +168,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         __syncwarp();
 #pragma unroll
         for (int kk = 0; kk < 2 * (D / 32); ++kk)             // 32 columns: 2 x 16 bytes
-          mma_e4m3_ss(tbase + kSCol + x * kTcKT, ad + (kk & 1) * kQPart16 + (kk >> 1) * 2, bd + (kk >> 1) * 2, id_s,
-                      kk ? 1u : 0u);
+          mma_f8_ss(tbase + kSCol + x * kTcKT, ad + (kk & 1) * kQPart16 + (kk >> 1) * 2, bd + (kk >> 1) * 2,
+                    kk & 1 ? id_rest : id_s, kk ? 1u : 0u);
         mma_commit_elected(&sm.s_full[x]);
       };
       // P comes in two halves
@@ -345,26 +345,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
           const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
           const float qs = ex <= (7u << 23) || ex == 0x7f800000u ? 1.f : __uint_as_float(ex - (7u << 23));
           const float inv = pow2_inverse(qs);
-          uint32_t top[2], rest[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float z[4], r4[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              z[k] = x[4 * e + k] * inv;
-              if (!(fabsf(z[k]) <= 448.f)) z[k] = __uint_as_float(0x7fffffffu);      // NaN, infinite
-            }
-            const uint32_t p0 = f32x2_to_e4m3x2(z[0], z[1]), p1 = f32x2_to_e4m3x2(z[2], z[3]);
-            const uint32_t h0 = e4m3x2_to_f16x2(p0), h1 = e4m3x2_to_f16x2(p1);
-            const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0));
-            const float2 f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-            r4[0] = z[0] - f0.x; r4[1] = z[1] - f0.y; r4[2] = z[2] - f1.x; r4[3] = z[3] - f1.y;
-            top[e] = p0 | p1 << 16;
-            rest[e] = f32x2_to_e4m3x2(r4[0], r4[1]) | f32x2_to_e4m3x2(r4[2], r4[3]) << 16;
-          }
+          for (int e = 0; e < 8; ++e) x[e] *= inv;
+          uint2 top, rest;
+          split8(x, top, rest);
           const uint32_t off = code_piece<D>(r & 127, qc);
-          *reinterpret_cast<uint2*>(sm.q[r >> 7][0] + off) = make_uint2(top[0], top[1]);
-          *reinterpret_cast<uint2*>(sm.q[r >> 7][1] + off) = make_uint2(rest[0], rest[1]);
+          *reinterpret_cast<uint2*>(sm.q[r >> 7][0] + off) = top;
+          *reinterpret_cast<uint2*>(sm.q[r >> 7][1] + off) = rest;
           if (qc == 0) sm.qs[r] = qs;
         }
       }

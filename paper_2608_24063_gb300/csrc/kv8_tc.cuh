@@ -19,7 +19,7 @@ constexpr float kLeastShare = -80.f;
 constexpr uint32_t kBlk = 128 * 128;            // 128 rows x 128 bytes (64 fp16 columns)
 
 // Instruction descriptors, D fp32: kind::f16 with A, B fp16, both K-major or B
-// MN-major; kind::f8f6f4 with A, B e4m3, both K-major.
+// MN-major; kind::f8f6f4 with A e4m3 or e5m2 and B e4m3, both K-major.
 __host__ __device__ constexpr uint32_t idesc_f16(uint32_t M, uint32_t N) {
   return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24);
 }
@@ -29,6 +29,7 @@ __host__ __device__ constexpr uint32_t idesc_f16_bmn(uint32_t M, uint32_t N) {
 __host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N) {
   return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24);
 }
+__host__ __device__ constexpr uint32_t idesc_e5m2_e4m3(uint32_t M, uint32_t N) { return idesc_e4m3(M, N) | (1u << 7); }
 
 // Descriptor of a K-major tile of 8-bit rows of D bytes: 128-byte swizzle
 // (8-row groups 1024 bytes apart) or, at D = 64, 64-byte swizzle (512).
@@ -54,8 +55,8 @@ __device__ __forceinline__ uint32_t code_piece(int r, int c) {
 // to 15 clocks.  Issued from a branch of one thread, each takes 50 to 60 (and a
 // lone one is seen done after 274 clocks instead of 130): as long as it runs.
 //
-// D[tmem] (+)= A[smem] * B[smem]^T.
-__device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+// D[tmem] (+)= A[smem] * B[smem]^T, 8-bit operands.
+__device__ __forceinline__ void mma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                             uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p, e;\n\t"
@@ -103,6 +104,29 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
 __device__ __forceinline__ uint32_t half2_rest(float lo, float hi, uint32_t bits) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&bits));
   return half2_bits(lo - f.x, hi - f.y);
+}
+
+// Eight query values (|z| < 256, or NaN for what is not finite) as the sum of an e4m3
+// and an e5m2 number each.  A bf16 number has 8 significant bits, an e4m3 number 4: its
+// rounding leaves at most 8 units of the last bit, which 3 bits hold.  So the sum is
+// exact from 2^-6 on, where e4m3 still has its 4 bits; below, a rest of at most 2^-10 is
+// off by up to 2^-14.
+__device__ __forceinline__ void split8(const float (&z)[8], uint2& top, uint2& rest) {
+  uint32_t t[2], r[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    float y[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = fabsf(z[4 * e + k]) <= 448.f ? z[4 * e + k] : __uint_as_float(0x7fffffffu);
+    const uint32_t p0 = f32x2_to_e4m3x2(y[0], y[1]), p1 = f32x2_to_e4m3x2(y[2], y[3]);
+    const uint32_t h0 = e4m3x2_to_f16x2(p0), h1 = e4m3x2_to_f16x2(p1);
+    const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0));
+    const float2 f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+    t[e] = p0 | p1 << 16;
+    r[e] = f32x2_to_e5m2x2(y[0] - f0.x, y[1] - f0.y) | f32x2_to_e5m2x2(y[2] - f1.x, y[3] - f1.y) << 16;
+  }
+  top = make_uint2(t[0], t[1]);
+  rest = make_uint2(r[0], r[1]);
 }
 
 // Sixteen codes as fp16 numbers (exact): 32 bytes of row `row`, column chunk c

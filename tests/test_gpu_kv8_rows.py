@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import kv8
-from tests.test_gpu_kv8 import DEV, F32, _rand
+from tests.test_gpu_kv8 import BF, DEV, F32, _rand
 from tests.test_gpu_kv8_values import FORMS as ALL
 from tests.test_gpu_kv8_values import _call, _pool
 
@@ -43,3 +43,13 @@ def test_fp32_rows_with_a_wide_channel(form, d):
     # and scalings as elsewhere
     err, ref, size, _ = _wide_rows(form, d, 4096.0)
     assert (err <= size * (d / 8 + 8) * 2.0 ** -23 + 2.0 ** -20 + 2.0 ** -22 * ref).all(), float(err.max())
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if f[3] == BF], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("width", [128.0, 1024.0])
+def test_bf16_rows_with_a_wide_channel(form, d, width):
+    # values down to 2^-13 of their row's largest are exact, those below within 2^-21 of it
+    err, ref, size, low = _wide_rows(form, d, width)
+    tol = size * (d / 16 + 6) * 2.0 ** -23 + 2.0 ** -20 + 2.0 ** -22 * ref + low * 2.0 ** -21 * width
+    assert (err <= tol).all(), float((err / tol).max())
