@@ -381,10 +381,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
           for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
 #pragma unroll
           for (int o = QL / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-          // largest magnitude to [2^14, 2^15) or [2^7, 2^8); zero, tiny or not finite rows as they are
+          // largest magnitude to [2^14, 2^15) or [2^7, 2^8), by 2^126 at most; rows that are not
+          // finite as they are
           constexpr uint32_t kUp = (F32 ? 14u : 7u) << 23;
           const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
-          const float qs = ex <= kUp || ex == 0x7f800000u ? 1.f : __uint_as_float(ex - kUp);
+          const float qs = ex == 0x7f800000u ? 1.f : __uint_as_float(max(ex, kUp + (1u << 23)) - kUp);
           const float inv = pow2_inverse(qs);
           if constexpr (F32) {
             uint32_t top[4], rest[4];

@@ -341,9 +341,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
           }
 #pragma unroll
           for (int o = QL / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-          // largest magnitude to [128, 256); zero, tiny or not finite rows as they are
+          // largest magnitude to [128, 256), by 2^126 at most; rows that are not finite as they are
           const uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
-          const float qs = ex <= (7u << 23) || ex == 0x7f800000u ? 1.f : __uint_as_float(ex - (7u << 23));
+          const float qs = ex == 0x7f800000u ? 1.f : __uint_as_float(max(ex, 8u << 23) - (7u << 23));
           const float inv = pow2_inverse(qs);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] *= inv;

@@ -53,3 +53,23 @@ def test_bf16_rows_with_a_wide_channel(form, d, width):
     err, ref, size, low = _wide_rows(form, d, width)
     tol = size * (d / 16 + 6) * 2.0 ** -23 + 2.0 ** -20 + 2.0 ** -22 * ref + low * 2.0 ** -21 * width
     assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("form", FORMS, ids=str)
+def test_tiny_rows_over_large_keys(form):
+    # rows of 2^-122 and keys of 2^124: ordinary scores
+    m, Hq, dtype = form[1:4]
+    n, d = 300, 64
+    K, V = _rand((n, d), 1, F32, 2.0 ** 124), _rand((n, d), 2, F32)
+    q = _rand((m, Hq, d), 3, F32, 2.0 ** -122).to(dtype)
+    pool = _pool(form, 32, d, K, V)
+    _, lse = _call(form, pool, n, q.to(DEV))
+    Kd, Vd = (kv8.gather(c, s, pool.table[0], n, 0) for c, s in zip(pool.codes, pool.scale))
+    for i in (0, m - 1):
+        k = n - m + i + 1
+        x = q[i, :1].double().numpy()
+        ref = kv8.attention(x, Kd[:k], Vd[:k], None, d ** -0.5)[1][0]
+        size = (np.abs(x) @ np.abs(Kd[:k]).T * d ** -0.5).max()
+        # sums and scalings as elsewhere; the scaling's factor, 2^-126 of a row times a page's scale,
+        # may be a number below the normal ones: within 2^-12
+        assert abs(float(lse[0, i, 0, 0]) - ref) <= size * ((d / 8 + 8) * 2.0 ** -23 + 2.0 ** -12) + 2.0 ** -20 + 2.0 ** -22 * abs(ref)
