@@ -29,7 +29,11 @@
 // row's largest score + log2 of its V scale: a row's fixed point is set by its
 // largest contribution, not by values that it does not see or that have no
 // weight.  At most 2^15 in fp16, the largest above 2^11, so they keep 11 bits down
-// to 2^-25 of the largest.  The row sum adds p before it is rounded.  Both
+// to 2^-25 of the largest.  The row sum adds p before it is rounded.  The tensor
+// core's fp32 sums cut off, so fp32 calls take a chunk's product from 0 and add it to
+// the output to nearest: over 20000 tokens, 12 rows of 128, the error falls from 5.9e-6
+// of the output to 2e-7, and 64 requests of 8192 tokens, 8 KV heads, take 211 us instead
+// of 197 (8 rows), 330 instead of 308 (16 rows).  Both
 // references are whole numbers and follow with a slack of 3 (log2 units), which
 // saves most rescales of the accumulators.
 //
@@ -447,9 +451,18 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             const uint32_t va[4] = {e4m3x2_to_f16x2(lo[k]), e4m3x2_to_f16x2(lo[k] >> 16), e4m3x2_to_f16x2(hi[k]),
                                     e4m3x2_to_f16x2(hi[k] >> 16)};
 #pragma unroll
-            for (int n = 0; n < NQ; ++n)
+            for (int n = 0; n < NQ; ++n) {
+              if constexpr (NP == 2) {
+                // the tensor core cuts its sums off, the smaller part first; added up to nearest
+                float y[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(y, va, pf[NP - 1][n][0], pf[NP - 1][n][1]);
+                mma_f16(y, va, pf[0][n][0], pf[0][n][1]);
 #pragma unroll
-              for (int p = 0; p < NP; ++p) mma_f16(o[n][2 * e + k], va, pf[p][n][0], pf[p][n][1]);
+                for (int i = 0; i < 4; ++i) o[n][2 * e + k][i] += y[i];
+              } else {
+                mma_f16(o[n][2 * e + k], va, pf[0][n][0], pf[0][n][1]);
+              }
+            }
           }
         }
       }
