@@ -496,8 +496,9 @@ int viscache_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int
  * A power of two costs e4m3 nothing (its spacing is relative) and makes the
  * codes exact to rescale.  With amax the largest finite |x| written to a page
  * and head, e is the least integer, at least -126, with amax <= 448 * 2^e; the
- * scale is 0 where amax is 0.  x / scale is rounded to nearest even; an x that
- * is not finite is stored as NaN and does not count for amax.
+ * scale is 0 where amax is 0.  x / scale is rounded to nearest even, and to 240 at
+ * most where the scale is 2^120 (256 would stand for 2^128): a finite x is read back
+ * finite.  An x that is not finite is stored as NaN and does not count for amax.
  *
  * vc_kv8       one layer's pool: codes device uint8 [n_pages][Hkv][page][d],
  *              scales device fp32 [n_pages][Hkv]; 16-byte aligned.  page is 16,

@@ -6,7 +6,8 @@ A value is an e4m3 code (sign, 4 exponent bits with bias 7, 3 mantissa bits;
 0x7F and 0xFF are NaN, no infinity, largest 448) times the scale of its page
 and KV head, 2^e or 0: e the least integer >= -126 with amax <= 448 * 2^e.
 Every step of writing is exact in float64 but the rounding to a code, which is
-to nearest, ties to the even code.
+to nearest, ties to the even code; at scale 2^120 codes end at 240, so that what
+they stand for is an fp32 number.
 """
 from __future__ import annotations
 
@@ -73,7 +74,9 @@ def append(codes: np.ndarray, scale: np.ndarray, table: np.ndarray, lens: Sequen
                 if now > old:
                     codes[p, g, :a] = encode(VALUE[codes[p, g, :a]] * old / s)
                 with np.errstate(invalid="ignore", over="ignore"):
-                    codes[p, g, a:b] = encode(y / s)
+                    # (at the largest scale a code of 256 would stand for 2^128, which is no fp32 number)
+                    top = 240.0 if s == 2.0 ** 120 else MAX
+                    codes[p, g, a:b] = encode(np.where(np.isfinite(y), np.clip(y / s, -top, top), y))
                 scale[p, g] = now
         at += m
 

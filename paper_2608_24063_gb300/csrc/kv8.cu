@@ -175,9 +175,10 @@ __device__ __forceinline__ void store16(float* p, const float (&v)[16]) {
     *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
 }
 
-// Sixteen values times `inv` as codes; with CHECK what is not finite becomes NaN.
+// Sixteen values times `inv` as codes; with CHECK what is not finite becomes NaN and
+// products stop at `top`.
 template <bool CHECK>
-__device__ __forceinline__ uint4 encode16(const float (&v)[16], float inv) {
+__device__ __forceinline__ uint4 encode16(const float (&v)[16], float inv, float top) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -185,7 +186,8 @@ __device__ __forceinline__ uint4 encode16(const float (&v)[16], float inv) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float y = v[4 * i + k];
-      x[k] = !CHECK || finite(y) ? y * inv : __uint_as_float(0x7fffffffu);
+      if constexpr (CHECK) x[k] = finite(y) ? fminf(fmaxf(y * inv, -top), top) : __uint_as_float(0x7fffffffu);
+      else x[k] = y * inv;
     }
     w[i] = f32x2_to_e4m3x2(x[0], x[1]) | f32x2_to_e4m3x2(x[2], x[3]) << 16;
   }
@@ -328,6 +330,9 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS, UnitCfg<D, PAGE>::b
     const float amax = __uint_as_float(m);
     const float now = fmaxf(old, pow2_scale(amax));
     const float inv = pow2_inverse(now);
+    // at the largest scale, 2^120, a code of 256 would stand for 2^128: no number
+    const bool largest = now >= 0x1p120f;
+    const float top = largest ? 240.f : 448.f;
 #pragma unroll
     for (int i = 0; i < C::NV; ++i) {
       const int vec = t + i * C::THREADS, slot = vec / C::VPR;
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS, UnitCfg<D, PAGE>::b
         float v[16];
         cur[i].get(v);
         *reinterpret_cast<uint4*>(codes + (size_t)vec * 16) =
-            all_finite ? encode16<false>(v, inv) : encode16<true>(v, inv);
+            all_finite && !largest ? encode16<false>(v, inv, top) : encode16<true>(v, inv, top);
       }
     }
     if (now > old) {
@@ -347,7 +352,7 @@ __global__ void __launch_bounds__(UnitCfg<D, PAGE>::THREADS, UnitCfg<D, PAGE>::b
         decode16(*w, y);
 #pragma unroll
         for (int k = 0; k < 16; ++k) y[k] *= old;
-        *w = encode16<true>(y, inv);
+        *w = encode16<true>(y, inv, top);
       }
     }
     if (t == 0) *scale = now;
