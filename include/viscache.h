@@ -448,9 +448,10 @@ int viscache_kv4_dequantize(const vc_batch* batch, const vc_params* p, const uin
  *     w_i = positions[axis(i)][row] * theta^(-i / half),
  *     a' = a cos w - b sin w,   b' = b cos w + a sin w,
  * the rest is copied.  With inverse != 0 the angle is -w: it takes a rotation
- * off again, and is the gradient of the forward call.  The angle is reduced
- * in integers, so it is exact for every int32 position; products and sums in
- * fp32, one rounding to the type.
+ * off again, and is the gradient of the forward call.  The angle is reduced in
+ * integers: for every int32 position it is within 2^-25 turn, and within 2^-45 of
+ * itself (the frequencies are fp64 products); products and sums in fp32, one
+ * rounding to the type.
  *   order     VC_ROPE_SECTIONED: axis 0 has the first sections[0]
  *             frequencies, axis 1 the next sections[1], ...;
  *             VC_ROPE_INTERLEAVED: frequency i belongs to axis i % n_axes if

@@ -162,7 +162,7 @@ int viscache_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int
       return VC_ERR_INVALID_ARG;
   }
   if (n_rows == 0 || Hq + Hkv == 0) return VC_OK;
-  // theta^(-i / half) by one power and repeated products: within 2^-47
+  // theta^(-i / half) by one power, off by an ulp, and up to 63 products: within 2^-45
   const double r = pow(rope->theta, -1.0 / (double)half);
   double f = kInv2Pi;
   for (int i = 0; i < (int)half; ++i, f *= r) a.freq[i] = (uint64_t)(f * 18446744073709551616.0);

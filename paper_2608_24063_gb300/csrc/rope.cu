@@ -16,8 +16,9 @@
 // The phase is an integer: F_i = theta^(-i/half) / 2pi in units of 2^-64 turn,
 // so pos * F_i modulo 2^64 is the reduced angle without any range reduction,
 // for every 32-bit position, negative ones too.  Its top 32 bits become the
-// argument of sincospif (error about 2^-26 turn; F_i itself is good to 47
-// bits, so the phase of position 2^20 is off by 2^-29 turn at most).
+// argument of sincospif (error about 2^-26 turn; F_i itself is good to 45 bits:
+// one fp64 power and up to 63 products, so the phase of position 2^20 is off by
+// 2^-27 turn at most, and that of 2^31 - 1 by 2^-16).
 #include <math.h>
 
 #include "kernels.h"
