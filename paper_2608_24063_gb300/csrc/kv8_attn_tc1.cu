@@ -566,16 +566,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
         }
         __syncwarp();                           // (whole warps store P)
         const float mr = ref.base(), lift = kTcPExp - ref.value_base();
+        float ev[8];                            // exponent of each 16-token group's page in P
+        {
+          const float4 v0 = *reinterpret_cast<const float4*>(vlog), v1 = *reinterpret_cast<const float4*>(vlog + 4);
+          ev[0] = v0.x; ev[1] = v0.y; ev[2] = v0.z; ev[3] = v0.w; ev[4] = v1.x; ev[5] = v1.y; ev[6] = v1.z; ev[7] = v1.w;
+#pragma unroll
+          for (int p = 0; p < 8; ++p) ev[p] = fmaxf(ev[p] + lift, kLeastShare);
+        }
         float2 ls = make_float2(0.f, 0.f);
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           uint32_t top[16], rest[16];
-          const float2 v2 = *reinterpret_cast<const float2*>(vlog + 2 * h);
 #pragma unroll
           for (int gr = 0; gr < 2; ++gr) {      // 16 tokens: one page's
             const int p = 2 * h + gr;
-            // exponent of the page's factor in P; what P's sum then takes for the row's
-            const float e = fmaxf((gr ? v2.y : v2.x) + lift, kLeastShare);
+            const float e = ev[p];
             // (fp32: the factor after the exponential, so that the largest terms' exponents are small numbers)
             const float2 nm = F32 ? make_float2(-mr, -mr) : make_float2(e - mr, e - mr);
             const float pf = pow2_bits((int)fminf(e, 127.f));
@@ -596,7 +601,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
             if constexpr (F32) {
               ls = __fadd2_rn(ls, sum);
             } else {
-              const float back = ex2(-e);
+              const float back = ex2(-e);       // (what P's sum takes for the row's)
               ls = __ffma2_rn(sum, make_float2(back, back), ls);
             }
           }

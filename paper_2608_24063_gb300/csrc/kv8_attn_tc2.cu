@@ -491,16 +491,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         }
         __syncwarp();                           // (whole warps store P)
         const float mr = ref.base(), lift = kTcPExp - ref.value_base();
+        float ev[8];                            // exponent of each 16-token group's page in P
+        {
+          const float4 v0 = *reinterpret_cast<const float4*>(vlog), v1 = *reinterpret_cast<const float4*>(vlog + 4);
+          ev[0] = v0.x; ev[1] = v0.y; ev[2] = v0.z; ev[3] = v0.w; ev[4] = v1.x; ev[5] = v1.y; ev[6] = v1.z; ev[7] = v1.w;
+#pragma unroll
+          for (int p = 0; p < 8; ++p) ev[p] = fmaxf(ev[p] + lift, kLeastShare);
+        }
         float2 ls = make_float2(0.f, 0.f);
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           uint32_t y16[16];
-          const float2 v2 = *reinterpret_cast<const float2*>(vlog + 2 * h);
 #pragma unroll
           for (int gr = 0; gr < 2; ++gr) {      // 16 tokens: one page's
             const int p = 2 * h + gr;
-            // exponent of the page's factor in P; what P's sum then takes for the row's
-            const float e = fmaxf((gr ? v2.y : v2.x) + lift, kLeastShare), back = ex2(-e);
+            const float e = ev[p], back = ex2(-e);      // (what P's sum takes for the row's)
             const float2 nm = make_float2(e - mr, e - mr);
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
