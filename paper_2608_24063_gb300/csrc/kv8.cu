@@ -429,7 +429,7 @@ cudaError_t launch_t(bool append, const vc_kv8& c, const vc_kv8_step& s, const K
   //   32 of 4096 tokens, 4 of 64, pages of 16: append 92.4 / 61.9, read 101.7 / 63.3
   const int64_t pages = most_pages<PAGE>(s);
   constexpr int threads = UnitCfg<D, PAGE>::THREADS;
-  int64_t split = (152 * (1280 / threads) + pages - 1) / pages;
+  int64_t split = ((int64_t)kv8_sm_count() * (1280 / threads) + pages - 1) / pages;
   constexpr int least = UnitCfg<D, PAGE>::blocks(sizeof(T)) > 1 ? 3 : 2;
   if (split < least) split = least;
   if (split > 2 * c.Hkv) split = 2 * c.Hkv;

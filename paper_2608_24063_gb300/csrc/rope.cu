@@ -180,7 +180,7 @@ cudaError_t launch_t(const RopeArgs& a, const void* q, void* q_out, const void* 
   // us with one share / with shares / with shares for four blocks an SM: 16 rows
   // 3.7 / 2.6 / 2.6, 256 rows 4.0 / 3.2 / 4.0, 512 rows 4.1 / 4.2 / 5.9
   const int64_t hmax = (a.Hq + a.Hkv + kRopeHeadLanes - 1) / kRopeHeadLanes;
-  const int64_t want = 152 / rb;
+  const int64_t want = kv8_sm_count() / rb;
   const unsigned hs = (unsigned)(want < 1 ? 1 : want > hmax ? hmax : want);
   ProfileScope ps("mrope", st);
   mrope_kernel<T, D, ADJ><<<dim3((unsigned)rb, hs), kRopeThreads, 0, st>>>(
