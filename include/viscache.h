@@ -552,7 +552,8 @@ size_t viscache_kv8_workspace_size(int32_t n_rows, int32_t Hq, int32_t Hkv, int3
  * exact but for values that fall below e4m3's smallest normal number.  A
  * page's scale is taken from the request's tokens alone: what a page held
  * before the request's first token in it does not count.  Writing the same
- * rows again gives the same cache.
+ * rows again gives the same cache.  A page that a call writes to belongs to one
+ * of its requests (others may share the pages that are full).
  *   K, V      device rows of `dtype` (VC_BF16 or VC_F32): row i, head g at
  *             element i * row stride + g * head stride, strides multiples of
  *             16 bytes (so a fused projection's slice, or prunekv_compress's

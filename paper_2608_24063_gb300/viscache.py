@@ -671,7 +671,8 @@ def _kv8_ws(fn: str, cache: Kv8Cache, step: Kv8Step, Hq: int, ws: Optional[torch
 
 def viscache_kv8_append(cache: Kv8Cache, step: Kv8Step, K: torch.Tensor, V: torch.Tensor,
                         ws: Optional[torch.Tensor] = None, stream=None) -> None:
-    """Write the step's rows K, V [rows][Hkv][d] (any row and head strides) into the cache."""
+    """Write the step's rows K, V [rows][Hkv][d] into the cache (row and head strides of at least d,
+    multiples of 16 bytes: slices of a fused projection and transposed blocks are read in place)."""
     fn = "viscache_kv8_append"
     dev, ws = _kv8_ws(fn, cache, step, cache.Hkv, ws, stream)
     code, dt = _type(K), K.dtype
