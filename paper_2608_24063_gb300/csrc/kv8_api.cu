@@ -75,14 +75,14 @@ uint64_t next_token() {
 // units an SM: its segments cost more at their ends.  Lengths are on the device, so
 // the block table's width stands for them.
 // d = 128, 8 KV heads, us on mma.sync / tc1:
-//   64 requests of 4096 tokens, 16 rows 135 / 147, 20 rows 246 / 149, 128 rows 933 / 178
-//   8 of 600 tokens, 24 rows 13.2 / 15.8, 48 rows 29.6 / 17.0
-//   one of 8192 tokens, 20 rows 20.3 / 19.6, 128 rows 42.4 / 34.4
-//   fp32, twice the rows: 8 of 4096, 24 rows 47.9 / 51.1, 36 rows 73 / 52, 256 rows 308 / 98
+//   64 requests of 4096 tokens, 16 rows 146 / 164, 20 rows 267 / 164, 128 rows 1012 / 192
+//   8 of 600 tokens, 24 rows 14.4 / 16.7, 48 rows 31.8 / 17.6
+//   one of 8192 tokens, 20 rows 22.3 / 20.7, 128 rows 45.6 / 35.6
+//   fp32, twice the rows: 8 of 4096, 24 rows 53.8 / 55.2, 36 rows 83 / 58, 256 rows 350 / 103
 // on tc1 / tc2:
-//   one of 32768 tokens, 320 rows 71 / 92, 512 rows 93.7 / 92.5, 8192 rows 988 / 739
-//   one of 8192 tokens, 1024 rows 54.4 / 58.1, 2048 rows 85.7 / 80.8
-//   one of 4096 tokens, 8192 rows 148 / 156; 64 of 1000, 1024 rows 499 / 611
+//   one of 32768 tokens, 320 rows 75 / 98, 512 rows 98.6 / 98.1, 8192 rows 1049 / 778
+//   one of 8192 tokens, 1024 rows 56.4 / 58.6, 2048 rows 89.5 / 82.7
+//   one of 4096 tokens, 8192 rows 162 / 156; 64 of 1000, 1024 rows 537 / 628
 constexpr int64_t kTcRows = 16, kTcShare = 8, kTc2Rows = 512, kTc2Tiles = 64, kTc2Share = 16;
 enum class Kernel { kMma, kTc1, kTc2 };
 bool may_have_many_rows(int64_t n_rows, int64_t n_req, int32_t Hq, int32_t Hkv) {

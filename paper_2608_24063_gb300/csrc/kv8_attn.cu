@@ -25,21 +25,22 @@
 // magnitude to [2^14, 2^15), so that fp16 holds bf16 values exactly down to 2^-31 of
 // it; fp32 calls use a second fp16 part of the row (22 bits down to 2^-17 of the
 // largest, 2^-39 of it below) and of the probabilities.  Scores are scaled by the page's K scale in
-// fp32.  Probabilities enter as p * 2^(12 - r) * V scale, r + m following the
+// fp32.  Probabilities enter as p * 2^(13 - r) * V scale, r + m following the
 // row's largest score + log2 of its V scale: a row's fixed point is set by its
 // largest contribution, not by values that it does not see or that have no
-// weight.  At most 2^15 in fp16, the largest above 2^11, so they keep 11 bits down
-// to 2^-25 of the largest.  The row sum adds p before it is rounded.  The tensor
+// weight.  At most 2^15 in fp16, the largest above 2^12, so they keep 11 bits down
+// to 2^-26 of the largest.  The row sum adds p before it is rounded.  The tensor
 // core's fp32 sums cut off, so fp32 calls take a chunk's product from 0 and add it to
 // the output to nearest: over 20000 tokens, 12 rows of 128, the error falls from 5.9e-6
-// of the output to 2e-7, and 64 requests of 8192 tokens, 8 KV heads, take 211 us instead
-// of 197 (8 rows), 330 instead of 308 (16 rows).  Both
-// references are whole numbers and follow with a slack of 3 (log2 units), which
-// saves most rescales of the accumulators.
+// of the output to 3e-7, and 64 requests of 8192 tokens, 8 KV heads, take 213 us instead
+// of 197 (8 rows), 337 instead of 308 (16 rows).  Both
+// references follow with a slack of 2 (log2 units), which saves most rescales of
+// the accumulators; r is a whole number and m a score, so that the probability 1
+// of a dominant token is not rounded.
 //
 // 32 requests of up to 32768 tokens, 8 KV heads of 128, 8 query heads each (1.35
-// GB): 217 us, 6.2 TB/s, 92% of a plain copy's rate.  One request of 777 tokens, 4
-// KV heads: 9.7 us, a chain of launch, lengths, page numbers, codes, products and
+// GB): 214 us, 6.3 TB/s, 93% of a plain copy's rate.  One request of 777 tokens, 4
+// KV heads: 10 us, a chain of launch, lengths, page numbers, codes, products and
 // the join of its pieces.
 #include <cudaTypedefs.h>
 
@@ -59,17 +60,17 @@ using namespace kv8;
 
 constexpr int kKT = 128;                        // tokens of a tile
 constexpr int kChunks = kKT / 16;
-constexpr float kSlack = 3.f;
-constexpr int kPExp = 12;
+constexpr float kSlack = 2.f;
+constexpr int kPExp = 13;
 constexpr float kLeastRef = -110.f;             // (2^(kPExp - r) stays a normal number; scales below 2^-100 alone: fewer bits)
 
 // T: query type, D: head dimension, NQ: groups of 8 query rows of a unit.
 // Warps: registers are granted to four warps at a time, so the consumers and
 // the producer fill 8, 12 or 16 warps of 255, 168 or 128 registers, chosen by
 // what the accumulators and the query fragments take.  64 requests of 8192
-// tokens, 8 KV heads, us with 7 / 11 / 15 consumers: d = 64, 8 rows 145 / 126 /
-// 121; d = 128, 8 rows 179 / 170 / 171 (fp32 rows 215 / 192 / 201); d = 128, 16
-// rows 230 / 242 / 407.
+// tokens, 8 KV heads, us with 7 / 11 / 15 consumers: d = 64, 8 rows 154 / 132 /
+// 127; d = 128, 8 rows 188 / 174 / 175 (fp32 rows 233 / 213 / 231); d = 128, 16
+// rows 249 / 279 / 385.
 template <typename T, int D, int NQ>
 struct Cfg {
   static constexpr int NP = sizeof(T) == 4 ? 2 : 1;         // fp16 parts of a query value
@@ -406,15 +407,15 @@ kv8_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
             float g[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+              float was = r[n][h];
               if (top[n][h] - m[n][h] > kSlack) {
-                const float to = ceilf(top[n][h]);
-                l[n][h] *= tc::ex2(m[n][h] - to);
-                r[n][h] -= to - m[n][h];
-                m[n][h] = to;
+                l[n][h] *= tc::ex2(m[n][h] - top[n][h]);
+                was -= top[n][h] - m[n][h];
+                m[n][h] = top[n][h];
               }
               const float y = top[n][h] - m[n][h] + vlog;
-              const float to = fmaxf(y > r[n][h] + kSlack ? ceilf(y) : r[n][h], kLeastRef);
-              g[h] = to == r[n][h] ? 1.f : tc::ex2(r[n][h] - to);
+              const float to = fmaxf(y > was + kSlack ? ceilf(y) : floorf(was), kLeastRef);
+              g[h] = tc::ex2(was - to);
               r[n][h] = to;
               rs[n][h] = pow2_bits(kPExp - (int)to);
             }
@@ -713,8 +714,8 @@ cudaError_t launch_t(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a
 
 // Units of 8 query rows where the requests have no more on average (a decode
 // step of up to 8 query heads a KV head), else of 16.  Us with units of 8 / of
-// 16, d = 128, 8 KV heads: 64 requests of 8192 tokens, 8 rows 171 / 234, 16 rows
-// 324 / 242; one request, 8 rows 13.3 / 16.5, 16 rows 15.5 / 19.4 (twice the
+// 16, d = 128, 8 KV heads: 64 requests of 8192 tokens, 8 rows 173 / 240, 16 rows
+// 327 / 248; one request, 8 rows 13.5 / 17.7, 16 rows 15.7 / 20.5 (twice the
 // units keep more SMs busy there, which a length on the device does not tell).
 template <typename T, int D>
 cudaError_t launch_q(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st) {

@@ -45,8 +45,8 @@
 // factor taken out of their exponents (3e-7 of each) included.
 //
 // Bound by the softmax's chain: one tile takes about 2200 clocks (its products
-// 1024).  64 requests of 128 rows over 4096 tokens, 8 KV heads of 128: 188 us, 2.9
-// TB/s of codes; fp32 rows 375 us.  Long chunks: kv8_attn_tc2.cu.
+// 1024).  64 requests of 128 rows over 4096 tokens, 8 KV heads of 128: 192 us, 2.8
+// TB/s of codes; fp32 rows 381 us.  Long chunks: kv8_attn_tc2.cu.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_sched.cuh"
@@ -537,9 +537,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc1_kernel(const __gri
         }
         const float* vlog = sm.vlog[t % kRefs];
         float g;
-        const bool rise = ref.raise(b, vlog, kTcSlack, g);
+        const bool moved = ref.raise(b, vlog, kTcSlack, g);
         const bool fold = j > w.t0 && C::fresh(j - w.t0);
-        if (j > w.t0 && (fold || __any_sync(0xffffffffu, rise))) {
+        if (j > w.t0 && (fold || __any_sync(0xffffffffu, moved))) {
           // the PV of the tile before is done, the next waits for this P
           ok = warp_wait(&sm.pv_done, (t & 1) ^ 1, abort);
           if (!ok) continue;

@@ -3,10 +3,10 @@
 //
 // Where there is work for every SM, two row tiles share a tile's expansion and each
 // other's waits: a chunk of 2048 rows over 32768 tokens (64 query heads, 8 KV heads
-// of 128) takes 1447 us, 1.47 PFLOP/s, against 1914 us with one row tile; 512 rows tie.  Bound by
-// a row tile's chain (scores, softmax, products) and the tensor cores about equally:
-// without exponentials, maxima and expansion it would take 1255 us, the products
-// alone 1111.
+// of 128) takes 1479 us, 1.44 PFLOP/s, against 2039 us with one row tile; 512 packed rows
+// tie.  Bound by a row tile's chain (scores, softmax, products) and the tensor cores
+// about equally: before the pages' exponents, which cost 3%, it would have taken 1255 us
+// without exponentials, maxima and expansion; the products alone take 1111.
 //
 // A unit has 256 packed query rows (two tiles of 128 rows, one TMEM lane a row)
 // over tiles of 128 tokens: 4 * 256 * 128 * d flops a tile, so it is bound by
@@ -476,8 +476,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_attn_tc2_kernel(const __gri
         }
         const float* vlog = sm.vlog[t % kRefs];
         float g;
-        const bool rise = ref.raise(b, vlog, kTcSlack, g);
-        if (j > w.t0 && __any_sync(0xffffffffu, rise)) {
+        const bool moved = ref.raise(b, vlog, kTcSlack, g);
+        if (j > w.t0 && __any_sync(0xffffffffu, moved)) {
           // PV of the tile before is done (s_full) and the next waits for this P
 #pragma unroll 1
           for (int p = 0; p < D / 16; ++p) {

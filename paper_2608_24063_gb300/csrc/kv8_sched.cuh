@@ -16,8 +16,8 @@
 // every unit gets whole blocks, ceil(tiles / per) of them with the least `per` that
 // the blocks allow, if that is no more than kEndTiles above an equal share, since a
 // segment's end costs as much as several tiles.  Us on the line / in whole blocks,
-// 152 blocks: 24 units of 6 to 25 tiles 22.9 / 15.5, 144 of 8 to 32 33.4 / 29.4,
-// 128 of 16 to 64 44.9 / 47.0, 128 of 64 to 256 119 / 149.
+// 152 blocks: 24 units of 6 to 25 tiles 17.5 / 12.8, 144 of 8 to 32 31.6 / 29.7,
+// 128 of 16 to 64 43.6 / 47.8, 128 of 64 to 256 116 / 152.
 #pragma once
 
 #include <cuda.h>

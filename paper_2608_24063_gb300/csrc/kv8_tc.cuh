@@ -156,9 +156,9 @@ __device__ __forceinline__ bool drop_nan(uint4& y) {
 }
 
 // The references of a row's softmax, log2 units.  x is a score, v the log2 of its page's V
-// scale.  m follows the largest x and r + m the largest x + v, both of what the row sees
-// and in whole numbers (so that differences of exponents are exact), and each may be
-// passed by `slack` before it rises.  P = 2^(x + v - m - r + const) multiplies the codes as
+// scale.  m follows the largest x and r + m the largest x + v, both of what the row sees,
+// and each may be passed by `slack` before it rises.  m is a score and r a whole number, so
+// that the probability 1 of a dominant token is not rounded.  P = 2^(x + v - m - r + const) multiplies the codes as
 // they are: a page's scale enters with its tokens' probabilities, so a row's fixed point is
 // set by its largest contribution and by nothing that it does not see or that has no weight.
 struct RowRefs {
@@ -167,26 +167,24 @@ struct RowRefs {
     m = r = -INFINITY;
     l = 0.f;
   }
-  // b: largest x of each 16-token group; whether O's reference rises (O times g then)
+  // b: largest x of each 16-token group; whether O's reference moves (O times g then)
   __device__ __forceinline__ bool raise(const float (&b)[8], const float* vlog, float slack, float& g) {
     const float tx = fmax3(fmax3(b[0], b[1], b[2]), fmax3(b[3], b[4], b[5]), fmaxf(b[6], b[7]));
+    float was = r;
     if (tx > m + slack) {
-      const float up = ceilf(tx);
-      l *= ex2(m - up);                         // 0 on the first
-      r -= up - m;
-      m = up;
+      l *= ex2(m - tx);                         // 0 on the first
+      was -= tx - m;
+      m = tx;
     }
     const float4 v0 = *reinterpret_cast<const float4*>(vlog), v1 = *reinterpret_cast<const float4*>(vlog + 4);
     const float mr = base();
     const float ty = fmax3(fmax3(b[0] - mr + v0.x, b[1] - mr + v0.y, b[2] - mr + v0.z),
                            fmax3(b[3] - mr + v0.w, b[4] - mr + v1.x, b[5] - mr + v1.y),
                            fmaxf(b[6] - mr + v1.z, b[7] - mr + v1.w));
-    g = 1.f;
-    if (!(ty > r + slack)) return false;
-    const float up = ceilf(ty);
-    g = ex2(r - up);
+    const float up = ty > was + slack ? ceilf(ty) : floorf(was);
+    g = was == up ? 1.f : ex2(was - up);
     r = up;
-    return true;
+    return up != was;
   }
   __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.f : m; }
   __device__ __forceinline__ float value_base() const { return r == -INFINITY ? 0.f : r; }
