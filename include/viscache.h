@@ -600,7 +600,8 @@ int viscache_kv8_read(const vc_kv8* cache, const vc_kv8_step* step, int dtype, v
  * what the row sees counts: pages that it does not see leave its bits as they are,
  * and values without weight cost the others nothing (a token is dropped where its
  * probability is below 2^-100 of the largest).  Sums, maxima and the softmax's
- * normaliser are fp32.  The result does not depend on
+ * normaliser are fp32.  Scores have to stay below 2^22 in magnitude: the exponents of
+ * calls of many rows are sums that fp32 holds up to there.  The result does not depend on
  * what else is in the batch but for that choice and for the order of sums, and
  * is the same for the same call.
  * A key that is not finite makes every row that sees it NaN, a value that is
