@@ -587,23 +587,26 @@ int viscache_kv8_read(const vc_kv8* cache, const vc_kv8_step* step, int dtype, v
  *   lse     device fp32 [n_rows][Hq] (nullable): natural log of the softmax's
  *           normaliser, -inf for a row that sees no token
  * Arithmetic: e4m3 values and query rows enter the products as numbers of few
- * bits times powers of two.  fp32 rows and fp32 calls' probabilities are sums
- * of two fp16 numbers (22 bits; of a row's values down to 2^-17 of its largest, and
- * 2^-39 of it below).  bf16 rows are fp16 numbers, exact for values
- * down to 2^-31 of their row's largest; in calls of many rows (more than 16 rows
- * of a KV head per request and work for every SM, judged by n_rows, n_req and
- * max_pages) they are sums of an e4m3 and an e5m2 number, exact down to 2^-13 of the
- * row's largest and within 2^-21 of it below.  A probability times its page's V scale
- * is rounded to fp16 in bf16 calls: 11 bits, down to 2^-18 of the row's largest such
- * product, 2^-29 of it below (fp32 calls: 22 bits down to 2^-14, 2^-36 below; fewer
- * where a row sees no scale above 2^-100).  Only
- * what the row sees counts: pages that it does not see leave its bits as they are,
- * and values without weight cost the others nothing (a token is dropped where its
- * probability is below 2^-100 of the largest).  Sums, maxima and the softmax's
- * normaliser are fp32.  Scores have to stay below 2^22 in magnitude: the exponents of
- * calls of many rows are sums that fp32 holds up to there.  The result does not depend on
- * what else is in the batch but for that choice and for the order of sums, and
- * is the same for the same call.
+ * bits times powers of two.
+ *   rows      of fp32 calls: two fp16 numbers (22 bits of values down to 2^-17 of
+ *             the row's largest, 2^-39 of it below).  Of bf16 calls: fp16 numbers,
+ *             exact for values down to 2^-31 of their row's largest; in calls of
+ *             many rows (more than 16 rows of a KV head per request and work for
+ *             every SM, judged by n_rows, n_req and max_pages) an e4m3 and an e5m2
+ *             number, exact down to 2^-13 of the row's largest and within 2^-21 of
+ *             it below.
+ *   weights   a probability times its page's V scale, rounded to fp16 in bf16
+ *             calls: 11 bits down to 2^-18 of the row's largest such product, 2^-29
+ *             of it below.  fp32 calls: two fp16 numbers, 22 bits down to 2^-14,
+ *             2^-36 below.  Fewer where a row sees no V scale above 2^-100.  Only
+ *             what the row sees counts: pages that it does not see leave its bits as
+ *             they are, and values without weight cost the others nothing (a token
+ *             is dropped where its probability is below 2^-100 of the largest).
+ *   sums,     maxima and the softmax's normaliser fp32.  Scores have to stay below
+ *             2^22 in magnitude: the exponents of calls of many rows are sums that
+ *             fp32 holds up to there.
+ * The result does not depend on what else is in the batch but for that choice and
+ * for the order of sums, and is the same for the same call.
  * A key that is not finite makes every row that sees it NaN, a value that is
  * not finite its dimension of them; rows that do not see it are what they would
  * be without it.

@@ -39,7 +39,7 @@
 // of a dominant token is not rounded.
 //
 // 32 requests of up to 32768 tokens, 8 KV heads of 128, 8 query heads each (1.35
-// GB): 214 us, 6.3 TB/s, 93% of a plain copy's rate.  One request of 777 tokens, 4
+// GB): 221 us, 6.1 TB/s, 90% of a plain copy's rate.  One request of 777 tokens, 4
 // KV heads: 10 us, a chain of launch, lengths, page numbers, codes, products and
 // the join of its pieces.
 #include <cudaTypedefs.h>
