@@ -187,7 +187,11 @@ def _dtype_code(t: torch.Tensor) -> int:
 def _on(stream):
     """Where a call allocates: its own stream.  A block of another stream's pool may still be in use
     there, and one that the call drops on return would be handed out again before its kernels ran."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return contextlib.nullcontext()
+    if not hasattr(stream, "device"):           # a stream of another library: its handle is enough
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    return torch.cuda.stream(stream)
 
 
 def _empty(shape, dtype, device, stream) -> torch.Tensor:

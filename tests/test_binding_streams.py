@@ -74,7 +74,7 @@ def test_every_entry_with_a_stream_is_listed():
 
 @pytest.mark.parametrize("name", CALLS)
 def test_a_call_allocates_on_its_own_stream(name, monkeypatch):
-    side, on, made = types.SimpleNamespace(cuda_stream=77), [None], []
+    side, on, made = types.SimpleNamespace(cuda_stream=77, device="cuda"), [None], []
     args, fake = CALLS[name](), _Library(vc.lib())
 
     @contextlib.contextmanager
@@ -96,3 +96,12 @@ def test_a_call_allocates_on_its_own_stream(name, monkeypatch):
         monkeypatch.setattr(torch, f, noted(getattr(torch, f)))
     getattr(vc, name)(*args, stream=side)
     assert made and all(s is side for s in made), made
+
+
+def test_a_handle_is_enough(monkeypatch):
+    # a stream object that is not torch's: what it wraps
+    entered = []
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: ("external", handle))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: entered.append(s) or contextlib.nullcontext())
+    t = vc._workspace(300, "cpu", None, types.SimpleNamespace(cuda_stream=77))
+    assert entered == [("external", 77)] and t.numel() == 300

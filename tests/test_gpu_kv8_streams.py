@@ -35,3 +35,18 @@ def test_memory_of_a_call_in_flight_is_not_handed_out():
         assert torch.equal(got, want) and torch.equal(spun, turned)
         assert all(bool((t == 0xFF).all()) for t in held)
         del b, got, spun, held
+
+
+def test_a_stream_of_another_library():
+    # an object with a handle alone, as other libraries' streams have
+    import types
+    lens, rows = [300], [2]
+    pool = _filled(lens, 1, 64, 128)
+    q = _rand((2, 4, 128), 1, BF).to(DEV)
+    step = pool.step(lens, rows)
+    want = vc.viscache_kv8_attention(pool.cache, step, q)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = vc.viscache_kv8_attention(pool.cache, step, q, stream=types.SimpleNamespace(cuda_stream=side.cuda_stream))
+    side.synchronize()
+    assert torch.equal(got, want)
