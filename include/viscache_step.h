@@ -1,0 +1,71 @@
+/*
+ * viscache_step.h -- the rest of a decode step around the 8-bit paged cache
+ * (viscache.h): query and key heads normed and rotated in one pass, with the
+ * gradient; the attention each token receives added up, and the cache held to
+ * a budget by it; the next token drawn from the logits.
+ *
+ * The conventions are those of viscache.h: int status codes, caller-owned
+ * buffers, work queued on the caller's stream, 16-byte aligned rows, no device
+ * memory allocated, nothing printed, no C++ exception.
+ */
+#ifndef VISCACHE_STEP_H_
+#define VISCACHE_STEP_H_
+
+#include "viscache.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * viscache_norm_mrope -- query and key heads normed (root mean square over the
+ * head's d values, a weight a channel) and rotated as viscache_mrope does, in
+ * the same pass:
+ *     r = 1 / sqrt(sum_c x_c^2 / d + eps),   y = R(positions) (x r w).
+ * Each head is normed by itself; w is q_weight for query heads, k_weight for
+ * key heads.  Sums, products and the rotation in fp32, one rounding to the
+ * type.  A head whose squares pass fp32's range is summed again scaled, so that
+ * finite rows of any size give what the formula says; a head with a value that
+ * is not finite gives NaN in that value's place at least.
+ *   rope, positions, q, k, q_out, k_out, strides   as in viscache_mrope (an
+ *             output may be its input, same pointer and stride)
+ *   q_weight, k_weight   device [d] of `dtype`
+ *   eps       1e-20 .. 1
+ * Hq or Hkv may be 0 (its pointers may then be NULL).  n_rows = 0 does nothing.
+ * Errors: VC_ERR_INVALID_ARG, VC_ERR_CUDA.
+ */
+int viscache_norm_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int64_t n_rows, int32_t Hq,
+                        int32_t Hkv, int32_t d, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                        const void* q_weight, const void* k_weight, float eps, void* q_out, int64_t q_out_stride,
+                        void* k_out, int64_t k_out_stride, void* stream);
+
+/*
+ * viscache_norm_mrope_grad -- its gradient.  With dy the gradient of a head's
+ * output, x its input, n = x r, g = R(positions)^T dy and h = g w:
+ *     dx = r (h - n sum_c(h n) / d),      dw = sum over rows and heads of g n.
+ *   q, k                    the forward call's inputs
+ *   q_out_grad, k_out_grad  gradients of its outputs, rows with their own strides
+ *   q_grad, k_grad          gradients of its inputs; may be the forward's input or
+ *             the output's gradient (same pointer and stride), and may not overlap
+ *             them otherwise
+ *   q_weight_grad, k_weight_grad  device fp32 [d], 16-byte aligned: written, not
+ *             added to (n_rows = 0 writes zeros).  The order of the sums depends on
+ *             the sizes alone: the same call gives the same bits.
+ * Workspace: viscache_norm_mrope_grad_workspace_size(n_rows, Hq, Hkv, d) bytes
+ * (0 for arguments that the call refuses), 256-byte aligned.
+ * Errors: VC_ERR_INVALID_ARG, VC_ERR_WORKSPACE, VC_ERR_CUDA.
+ */
+size_t viscache_norm_mrope_grad_workspace_size(int64_t n_rows, int32_t Hq, int32_t Hkv, int32_t d);
+int viscache_norm_mrope_grad(const vc_rope* rope, const int32_t* positions, int dtype, int64_t n_rows, int32_t Hq,
+                             int32_t Hkv, int32_t d, const void* q, int64_t q_stride, const void* k,
+                             int64_t k_stride, const void* q_out_grad, int64_t q_out_grad_stride,
+                             const void* k_out_grad, int64_t k_out_grad_stride, const void* q_weight,
+                             const void* k_weight, float eps, void* q_grad, int64_t q_grad_stride, void* k_grad,
+                             int64_t k_grad_stride, float* q_weight_grad, float* k_weight_grad, void* ws,
+                             size_t ws_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* VISCACHE_STEP_H_ */

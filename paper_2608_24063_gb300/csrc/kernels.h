@@ -162,6 +162,29 @@ struct RopeArgs {
 cudaError_t launch_mrope(const RopeArgs& a, int dtype, int d, bool adjacent, const void* q, void* q_out,
                          const void* k, void* k_out, cudaStream_t st);
 
+// The same heads normed first (norm_rope.cu).
+struct NormRope {
+  const void *q, *k, *q_weight, *k_weight;
+  void *q_out, *k_out;
+  float eps;
+};
+cudaError_t launch_norm_mrope(const RopeArgs& a, const NormRope& p, int dtype, int d, bool adjacent, cudaStream_t st);
+struct NormRopeGrad {
+  const void *q, *k, *q_dy, *k_dy, *q_weight, *k_weight;
+  void *q_out, *k_out;                 // gradients of q and k (their strides: RopeArgs' out strides)
+  int64_t q_dy_stride, k_dy_stride;
+  float* partial;                      // [blocks][d]
+  float eps;
+  int32_t nq;                          // blocks of query heads, the first
+};
+constexpr int kNormGradBlocks = 304;   // blocks of the gradient at most, two for each of 152 SMs
+struct NormGradGrid {
+  int nq, nk;
+};
+NormGradGrid norm_grad_grid(int64_t n_rows, int32_t Hq, int32_t Hkv);
+cudaError_t launch_norm_mrope_grad(const RopeArgs& a, NormRopeGrad& p, int dtype, int d, bool adjacent, float* dwq,
+                                   float* dwk, cudaStream_t st);
+
 // 8-bit paged cache (kv8.cu, kv8_attn.cu, kv8_attn_tc1.cu, kv8_attn_tc2.cu).  The device arrays
 // of vc_kv8 and vc_kv8_step are checked as they are read: lengths are clamped to
 // the block table, requests whose rows lie outside [0, n_rows] and pages outside

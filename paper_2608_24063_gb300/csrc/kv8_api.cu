@@ -1,5 +1,6 @@
 // C entry points of the rotary positions and of the 8-bit paged cache
-// (include/viscache.h): argument checks, workspace layout, launches.
+// (include/viscache.h) and of the step around it (include/viscache_step.h):
+// argument checks, workspace layout, launches.
 #include <math.h>
 
 #include <atomic>
@@ -7,6 +8,7 @@
 
 #include "api_util.h"
 #include "kernels.h"
+#include "viscache_step.h"
 
 namespace vc {
 namespace {
@@ -33,6 +35,51 @@ bool valid_type(int dtype) { return dtype == VC_BF16 || dtype == VC_F32; }
 // Row or head strides in elements: whole 16-byte pieces.
 bool valid_stride(int64_t stride, int64_t least, int dtype) {
   return stride >= least && stride % (dtype == VC_BF16 ? 8 : 4) == 0 && stride < (int64_t)1 << 40;
+}
+
+bool valid_rope(const vc_rope* rope, int dtype, int64_t n_rows, int32_t Hq, int32_t Hkv, int32_t d) {
+  if (!rope || !valid_type(dtype) || (d != 64 && d != 128)) return false;
+  if (n_rows < 0 || n_rows > (1 << 24) || Hq < 0 || Hkv < 0 || Hq > 4096 || Hkv > 4096) return false;
+  if (rope->n_axes < 1 || rope->n_axes > 4 || !(rope->theta >= 1.0) || !isfinite(rope->theta)) return false;
+  if ((rope->order != VC_ROPE_SECTIONED && rope->order != VC_ROPE_INTERLEAVED) ||
+      (rope->pairing != VC_ROPE_HALVES && rope->pairing != VC_ROPE_ADJACENT))
+    return false;
+  int64_t half = 0;
+  for (int a = 0; a < rope->n_axes; ++a) {
+    if (rope->sections[a] < 0 || rope->sections[a] > d / 2) return false;
+    half += rope->sections[a];
+  }
+  return half >= 8 && half % 8 == 0 && half <= d / 2;
+}
+
+// Rows of `heads` heads (none: nothing to look at).
+bool valid_rows(const void* p, int64_t stride, int32_t heads, int32_t d, int dtype) {
+  return heads == 0 || (p && aligned16(p) && valid_stride(stride, (int64_t)heads * d, dtype));
+}
+
+// Frequencies and their axes, positions and counts; strides and direction are the caller's.
+void set_rope(RopeArgs& a, const vc_rope& rope, const int32_t* positions, int64_t n_rows, int32_t Hq, int32_t Hkv) {
+  int half = 0;
+  for (int x = 0; x < rope.n_axes; ++x) half += rope.sections[x];
+  for (int i = 0; i < half; ++i) {
+    if (rope.order == VC_ROPE_INTERLEAVED) {
+      const int x = i % rope.n_axes;
+      a.axis[i] = (uint8_t)(i < rope.n_axes * rope.sections[x] ? x : 0);
+    } else {
+      int x = 0;
+      for (int upto = rope.sections[0]; i >= upto; upto += rope.sections[x]) ++x;
+      a.axis[i] = (uint8_t)x;
+    }
+  }
+  // theta^(-i / half) by one power, off by an ulp, and up to 63 products: within 2^-45
+  const double r = pow(rope.theta, -1.0 / (double)half);
+  double f = kInv2Pi;
+  for (int i = 0; i < half; ++i, f *= r) a.freq[i] = (uint64_t)(f * 18446744073709551616.0);
+  a.positions = positions;
+  a.n_rows = n_rows;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.half = half;
 }
 
 // Workspace: status word and block count (256 bytes), the blocks' status
@@ -100,6 +147,13 @@ Kernel kernel_of(const vc_kv8& c, const vc_kv8_step& s, int dtype, int32_t Hq) {
 
 bool valid_heads(int32_t Hq, int32_t Hkv) { return Hkv >= 1 && Hq >= Hkv && Hq <= 4096 && Hq % Hkv == 0; }
 
+// The attention's line of key tiles (units of 8 rows at least): a block's share is
+// counted in 31 bits.
+bool short_line(const vc_kv8& c, const vc_kv8_step& s, int32_t Hq) {
+  const int64_t row_tiles = (int64_t)s.n_rows * (Hq / c.Hkv) / 8 + s.n_req;
+  return row_tiles * c.Hkv <= ((int64_t)1 << 37) / (((int64_t)s.max_pages * c.page + 127) / 128);
+}
+
 int kv8_rows_call(bool append, const vc_kv8* cache, const vc_kv8_step* step, int dtype, const Kv8Rows& rows,
                   void* ws, size_t ws_bytes, void* stream) {
   if (!valid_cache(cache) || !valid_step(cache, step) || !valid_type(dtype)) return VC_ERR_INVALID_ARG;
@@ -126,58 +180,97 @@ int viscache_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int
                    int32_t Hkv, int32_t d, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                    int inverse, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
                    void* stream) {
-  if (!rope || !valid_type(dtype) || (d != 64 && d != 128)) return VC_ERR_INVALID_ARG;
-  if (n_rows < 0 || n_rows > (1 << 24) || Hq < 0 || Hkv < 0 || Hq > 4096 || Hkv > 4096) return VC_ERR_INVALID_ARG;
-  if (rope->n_axes < 1 || rope->n_axes > 4 || !(rope->theta >= 1.0) || !isfinite(rope->theta))
-    return VC_ERR_INVALID_ARG;
-  if ((rope->order != VC_ROPE_SECTIONED && rope->order != VC_ROPE_INTERLEAVED) ||
-      (rope->pairing != VC_ROPE_HALVES && rope->pairing != VC_ROPE_ADJACENT))
-    return VC_ERR_INVALID_ARG;
-  int64_t half = 0;
-  for (int a = 0; a < rope->n_axes; ++a) {
-    if (rope->sections[a] < 0 || rope->sections[a] > d / 2) return VC_ERR_INVALID_ARG;
-    half += rope->sections[a];
-  }
-  if (half < 8 || half % 8 != 0 || half > d / 2) return VC_ERR_INVALID_ARG;
   RopeArgs a = {};
-  for (int i = 0; i < (int)half; ++i) {
-    if (rope->order == VC_ROPE_INTERLEAVED) {
-      const int x = i % rope->n_axes;
-      a.axis[i] = (uint8_t)(i < rope->n_axes * rope->sections[x] ? x : 0);
-    } else {
-      int x = 0;
-      for (int upto = rope->sections[0]; i >= upto; upto += rope->sections[x]) ++x;
-      a.axis[i] = (uint8_t)x;
-    }
-  }
+  if (!valid_rope(rope, dtype, n_rows, Hq, Hkv, d)) return VC_ERR_INVALID_ARG;
   if (n_rows > 0) {
     if (!positions) return VC_ERR_INVALID_ARG;
-    if (Hq > 0 && (!q || !q_out || !aligned16(q) || !aligned16(q_out) ||
-                   !valid_stride(q_stride, (int64_t)Hq * d, dtype) ||
-                   !valid_stride(q_out_stride, (int64_t)Hq * d, dtype)))
-      return VC_ERR_INVALID_ARG;
-    if (Hkv > 0 && (!k || !k_out || !aligned16(k) || !aligned16(k_out) ||
-                    !valid_stride(k_stride, (int64_t)Hkv * d, dtype) ||
-                    !valid_stride(k_out_stride, (int64_t)Hkv * d, dtype)))
+    if (!valid_rows(q, q_stride, Hq, d, dtype) || !valid_rows(q_out, q_out_stride, Hq, d, dtype) ||
+        !valid_rows(k, k_stride, Hkv, d, dtype) || !valid_rows(k_out, k_out_stride, Hkv, d, dtype))
       return VC_ERR_INVALID_ARG;
   }
   if (n_rows == 0 || Hq + Hkv == 0) return VC_OK;
-  // theta^(-i / half) by one power, off by an ulp, and up to 63 products: within 2^-45
-  const double r = pow(rope->theta, -1.0 / (double)half);
-  double f = kInv2Pi;
-  for (int i = 0; i < (int)half; ++i, f *= r) a.freq[i] = (uint64_t)(f * 18446744073709551616.0);
-  a.positions = positions;
-  a.n_rows = n_rows;
+  set_rope(a, *rope, positions, n_rows, Hq, Hkv);
   a.q_stride = q_stride;
   a.k_stride = k_stride;
   a.q_out_stride = q_out_stride;
   a.k_out_stride = k_out_stride;
-  a.Hq = Hq;
-  a.Hkv = Hkv;
-  a.half = (int32_t)half;
   a.inverse = inverse != 0;
   return cuda_status(launch_mrope(a, dtype, d, rope->pairing == VC_ROPE_ADJACENT, q, q_out, k, k_out,
                                   static_cast<cudaStream_t>(stream)));
+}
+
+static bool valid_eps(float eps) { return eps >= 1e-20f && eps <= 1.f; }
+
+int viscache_norm_mrope(const vc_rope* rope, const int32_t* positions, int dtype, int64_t n_rows, int32_t Hq,
+                        int32_t Hkv, int32_t d, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                        const void* q_weight, const void* k_weight, float eps, void* q_out, int64_t q_out_stride,
+                        void* k_out, int64_t k_out_stride, void* stream) {
+  RopeArgs a = {};
+  if (!valid_rope(rope, dtype, n_rows, Hq, Hkv, d) || !valid_eps(eps)) return VC_ERR_INVALID_ARG;
+  if (n_rows > 0) {
+    if (!positions) return VC_ERR_INVALID_ARG;
+    if (!valid_rows(q, q_stride, Hq, d, dtype) || !valid_rows(q_out, q_out_stride, Hq, d, dtype) ||
+        !valid_rows(k, k_stride, Hkv, d, dtype) || !valid_rows(k_out, k_out_stride, Hkv, d, dtype) ||
+        !valid_rows(q_weight, d, Hq > 0, d, dtype) || !valid_rows(k_weight, d, Hkv > 0, d, dtype))
+      return VC_ERR_INVALID_ARG;
+  }
+  if (n_rows == 0 || Hq + Hkv == 0) return VC_OK;
+  set_rope(a, *rope, positions, n_rows, Hq, Hkv);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_out_stride = k_out_stride;
+  const NormRope p = {q, k, q_weight, k_weight, q_out, k_out, eps};
+  return cuda_status(launch_norm_mrope(a, p, dtype, d, rope->pairing == VC_ROPE_ADJACENT,
+                                       static_cast<cudaStream_t>(stream)));
+}
+
+size_t viscache_norm_mrope_grad_workspace_size(int64_t n_rows, int32_t Hq, int32_t Hkv, int32_t d) {
+  if (n_rows < 0 || n_rows > (1 << 24) || Hq < 0 || Hkv < 0 || Hq > 4096 || Hkv > 4096 || (d != 64 && d != 128))
+    return 0;
+  return align_up(sizeof(float) * kNormGradBlocks * d);
+}
+
+int viscache_norm_mrope_grad(const vc_rope* rope, const int32_t* positions, int dtype, int64_t n_rows, int32_t Hq,
+                             int32_t Hkv, int32_t d, const void* q, int64_t q_stride, const void* k,
+                             int64_t k_stride, const void* q_out_grad, int64_t q_out_grad_stride,
+                             const void* k_out_grad, int64_t k_out_grad_stride, const void* q_weight,
+                             const void* k_weight, float eps, void* q_grad, int64_t q_grad_stride, void* k_grad,
+                             int64_t k_grad_stride, float* q_weight_grad, float* k_weight_grad, void* ws,
+                             size_t ws_bytes, void* stream) {
+  RopeArgs a = {};
+  if (!valid_rope(rope, dtype, n_rows, Hq, Hkv, d) || !valid_eps(eps)) return VC_ERR_INVALID_ARG;
+  if ((Hq > 0 && (!q_weight_grad || !aligned16(q_weight_grad))) ||
+      (Hkv > 0 && (!k_weight_grad || !aligned16(k_weight_grad))))
+    return VC_ERR_INVALID_ARG;
+  if (n_rows > 0) {
+    if (!positions) return VC_ERR_INVALID_ARG;
+    if (!valid_rows(q, q_stride, Hq, d, dtype) || !valid_rows(q_out_grad, q_out_grad_stride, Hq, d, dtype) ||
+        !valid_rows(q_grad, q_grad_stride, Hq, d, dtype) || !valid_rows(k, k_stride, Hkv, d, dtype) ||
+        !valid_rows(k_out_grad, k_out_grad_stride, Hkv, d, dtype) ||
+        !valid_rows(k_grad, k_grad_stride, Hkv, d, dtype) || !valid_rows(q_weight, d, Hq > 0, d, dtype) ||
+        !valid_rows(k_weight, d, Hkv > 0, d, dtype))
+      return VC_ERR_INVALID_ARG;
+  }
+  const int wc = check_ws(ws, ws_bytes, viscache_norm_mrope_grad_workspace_size(n_rows, Hq, Hkv, d));
+  if (wc != VC_OK) return wc;
+  if (Hq + Hkv == 0) return VC_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (n_rows == 0) {
+    cudaError_t e = Hq > 0 ? cudaMemsetAsync(q_weight_grad, 0, sizeof(float) * d, st) : cudaSuccess;
+    if (e == cudaSuccess && Hkv > 0) e = cudaMemsetAsync(k_weight_grad, 0, sizeof(float) * d, st);
+    return cuda_status(e);
+  }
+  set_rope(a, *rope, positions, n_rows, Hq, Hkv);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_out_stride = q_grad_stride;
+  a.k_out_stride = k_grad_stride;
+  a.inverse = 1;
+  NormRopeGrad p = {q, k, q_out_grad, k_out_grad, q_weight, k_weight, q_grad, k_grad, q_out_grad_stride,
+                    k_out_grad_stride, static_cast<float*>(ws), eps, 0};
+  return cuda_status(launch_norm_mrope_grad(a, p, dtype, d, rope->pairing == VC_ROPE_ADJACENT,
+                                            Hq > 0 ? q_weight_grad : nullptr, Hkv > 0 ? k_weight_grad : nullptr, st));
 }
 
 size_t viscache_kv8_workspace_size(int32_t n_rows, int32_t Hq, int32_t Hkv, int32_t d) {
@@ -211,11 +304,7 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
                            !valid_stride(q_stride, (int64_t)Hq * cache->d, dtype)))
     return VC_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return VC_ERR_INVALID_ARG;
-  // the attention's line of key tiles (units of 8 rows at least): a block's
-  // share is counted in 31 bits
-  const int64_t row_tiles = (int64_t)step->n_rows * (Hq / cache->Hkv) / 8 + step->n_req;
-  if (row_tiles * cache->Hkv > ((int64_t)1 << 37) / (((int64_t)step->max_pages * cache->page + 127) / 128))
-    return VC_ERR_UNSUPPORTED;
+  if (!short_line(*cache, *step, Hq)) return VC_ERR_UNSUPPORTED;
   const Kernel kernel = kernel_of(*cache, *step, dtype, Hq);
   const Kv8Ws w = kv8_ws(kernel != Kernel::kMma, cache->d);
   const int wc = check_ws(ws, ws_bytes, w.total);

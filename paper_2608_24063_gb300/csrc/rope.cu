@@ -23,55 +23,17 @@
 
 #include "kernels.h"
 #include "profile.h"
+#include "rope.cuh"
 #include "vc_common.cuh"
 
 namespace vc {
 namespace {
 
+using namespace rope;
+
 constexpr int kRopeThreads = 256;
 constexpr int kRopeHeadLanes = 8;     // heads a block works on at once
 constexpr int kRopeBatch = 2;         // heads a thread has in flight
-
-// Eight values as they lie in memory.
-template <typename T>
-struct Raw8 {
-  uint4 w[sizeof(T) / 2];
-  __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
-  }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    if constexpr (sizeof(T) == 2) {
-      const uint32_t x[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(x[i] << 16);
-        v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        v[4 * i] = __uint_as_float(w[i].x); v[4 * i + 1] = __uint_as_float(w[i].y);
-        v[4 * i + 2] = __uint_as_float(w[i].z); v[4 * i + 3] = __uint_as_float(w[i].w);
-      }
-    }
-  }
-};
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
-  return make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
-}
-
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
-  *reinterpret_cast<uint4*>(p) = pack8(v);
-}
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
 
 // Block: rows [blockIdx.x * RT, ...) with RT = 32 / SLOTS, heads of share
 // blockIdx.y of gridDim.y.  Thread: slot t % SLOTS (16 values of a head), head
@@ -114,12 +76,7 @@ __global__ void __launch_bounds__(kRopeThreads) mrope_kernel(const __grid_consta
     const int i = t % HALF;
     const int64_t ar = r0 + t / HALF;
     if (i < a.half && ar < a.n_rows) {
-      const int32_t pos = __ldg(a.positions + (int64_t)a.axis[i] * a.n_rows + ar);
-      const uint64_t phase = (uint64_t)(int64_t)pos * a.freq[i];
-      const float turn = (float)(int32_t)(phase >> 32) * 0x1p-31f;    // half turns in [-1, 1)
-      float s, c;
-      sincospif(turn, &s, &c);
-      cs[t / HALF][i] = make_float2(c, a.inverse ? -s : s);
+      cs[t / HALF][i] = angle(a, i, ar);
     }
   }
   __syncthreads();
@@ -149,21 +106,8 @@ __global__ void __launch_bounds__(kRopeThreads) mrope_kernel(const __grid_consta
           u[i] = xa[i];
           v[i] = ya[i];
         }
-      } else if (ADJ) {
-        // pairs (2i, 2i + 1): x holds pairs 0..3 of the slot, y pairs 4..7
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          u[2 * i] = xa[2 * i] * c[i] - xa[2 * i + 1] * s[i];
-          u[2 * i + 1] = xa[2 * i + 1] * c[i] + xa[2 * i] * s[i];
-          v[2 * i] = ya[2 * i] * c[4 + i] - ya[2 * i + 1] * s[4 + i];
-          v[2 * i + 1] = ya[2 * i + 1] * c[4 + i] + ya[2 * i] * s[4 + i];
-        }
       } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          u[i] = xa[i] * c[i] - ya[i] * s[i];
-          v[i] = ya[i] * c[i] + xa[i] * s[i];
-        }
+        turn8<ADJ>(xa, ya, c, s, u, v);
       }
       store8(dst + o0, u);
       store8(dst + o1, v);

@@ -1,4 +1,4 @@
-"""Python binding of libviscache (include/viscache.h): argument marshalling only.
+"""Python binding of libviscache (include/viscache.h, include/viscache_step.h): argument marshalling only.
 
 Every function here has the name of the C entry point it calls.  torch is used
 for device memory (outputs and workspaces) and for the current CUDA stream;
@@ -50,6 +50,9 @@ EXPORTED = ("viscache_plan_budgets", "viscache_plan_budgets_ex", "prunekv_score_
             "viscache_kv4_sizes", "viscache_kv4_quantize", "viscache_kv4_dequantize",
             "viscache_decode_attention_kv4", "viscache_mrope", "viscache_kv8_workspace_size",
             "viscache_kv8_append", "viscache_kv8_read", "viscache_kv8_attention")
+
+# the entry points of include/viscache_step.h
+EXPORTED_STEP = ("viscache_norm_mrope", "viscache_norm_mrope_grad_workspace_size", "viscache_norm_mrope_grad")
 
 
 class VisCacheError(RuntimeError):
@@ -128,6 +131,13 @@ def lib() -> ctypes.CDLL:
         L.viscache_kv8_append.argtypes = [pc8, ps8, i32, vp, i64, i64, vp, i64, i64, vp, sz, vp]
         L.viscache_kv8_read.argtypes = [pc8, ps8, i32, vp, vp, vp, sz, vp]
         L.viscache_kv8_attention.argtypes = [pc8, ps8, i32, i32, vp, i64, f32, i32, vp, vp, vp, sz, vp]
+        pr = ctypes.POINTER(vc_rope)
+        L.viscache_norm_mrope.argtypes = [pr, vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp, vp, f32, vp, i64, vp,
+                                          i64, vp]
+        L.viscache_norm_mrope_grad_workspace_size.argtypes = [i64, i32, i32, i32]
+        L.viscache_norm_mrope_grad_workspace_size.restype = sz
+        L.viscache_norm_mrope_grad.argtypes = [pr, vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp,
+                                               vp, f32, vp, i64, vp, i64, vp, vp, vp, sz, vp]
         L.prunekv_score_workspace_size.argtypes = [i32, i32, i32]
         L.prunekv_score_workspace_size.restype = sz
         L.prunekv_score.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, vp,
@@ -738,6 +748,118 @@ def viscache_kv8_attention(cache: Kv8Cache, step: Kv8Step, q: torch.Tensor, scal
     if rc != VC_OK:
         raise VisCacheError(fn, rc)
     return out
+
+
+# ---------------------------------------------------------------------------
+# The rest of a decode step around the 8-bit paged cache
+
+def _flat(fn: str, t: torch.Tensor, dtype, dev: int, shape) -> int:
+    """Address of a dense tensor of that type and shape on the current device."""
+    if t.dtype != dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    return t.data_ptr()
+
+
+def _heads(fn: str, t: torch.Tensor, dtype, dev: int, rows: int, heads: int, d: int) -> int:
+    """Row stride of rows whose heads are dense."""
+    r, h = _rows(fn, t, dtype, dev, rows, heads, d)
+    if h != d:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    return r
+
+
+def viscache_norm_mrope(rope: vc_rope, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor],
+                        q_weight: torch.Tensor, k_weight: Optional[torch.Tensor], eps: float = 1e-6,
+                        q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """Heads normed by their root mean square, times q_weight / k_weight [d], and rotated as by
+    viscache_mrope: q [rows][Hq][d], k [rows][Hkv][d] (or None, with None for its weight) -> (q_out, k_out).
+
+    Rows may be strided; ``q_out``/``k_out`` may be ``q``/``k`` themselves.
+    """
+    fn = "viscache_norm_mrope"
+    code, dt, dev = _type(q), q.dtype, _current_device()
+    if q.dim() != 3:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    rows, Hq, d = q.shape
+    if q_out is None:
+        q_out = _empty((rows, Hq, d), dt, q.device, stream)
+    qs, qos = _heads(fn, q, dt, dev, rows, Hq, d), _heads(fn, q_out, dt, dev, rows, Hq, d)
+    Hkv, ks, kos, kp, kop, kw = 0, 0, 0, None, None, None
+    if k is not None:
+        if k.dim() != 3 or k_weight is None:
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+        Hkv = k.shape[1]
+        if k_out is None:
+            k_out = _empty((rows, Hkv, d), dt, q.device, stream)
+        ks, kos = _heads(fn, k, dt, dev, rows, Hkv, d), _heads(fn, k_out, dt, dev, rows, Hkv, d)
+        kp, kop, kw = k.data_ptr(), k_out.data_ptr(), _flat(fn, k_weight, dt, dev, (d,))
+    else:
+        k_out = None
+    rc = lib().viscache_norm_mrope(rope, _flat(fn, positions, torch.int32, dev, (rope.n_axes, rows)), code, rows, Hq,
+                                   Hkv, d, q.data_ptr(), qs, kp, ks, _flat(fn, q_weight, dt, dev, (d,)), kw, eps,
+                                   q_out.data_ptr(), qos, kop, kos, _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
+    return q_out, k_out
+
+
+def viscache_norm_mrope_grad_workspace_size(n_rows: int, Hq: int, Hkv: int, d: int) -> int:
+    return lib().viscache_norm_mrope_grad_workspace_size(n_rows, Hq, Hkv, d)
+
+
+def viscache_norm_mrope_grad(rope: vc_rope, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor],
+                             q_out_grad: torch.Tensor, k_out_grad: Optional[torch.Tensor], q_weight: torch.Tensor,
+                             k_weight: Optional[torch.Tensor], eps: float = 1e-6,
+                             q_grad: Optional[torch.Tensor] = None, k_grad: Optional[torch.Tensor] = None,
+                             q_weight_grad: Optional[torch.Tensor] = None,
+                             k_weight_grad: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                             stream=None):
+    """Gradient of viscache_norm_mrope: (q_grad, k_grad) rows and (q_weight_grad, k_weight_grad) fp32 [d].
+
+    q, k are the forward call's inputs, q_out_grad, k_out_grad the gradients of its outputs; the weights'
+    gradients are written, not added to.
+    """
+    fn = "viscache_norm_mrope_grad"
+    code, dt, dev = _type(q), q.dtype, _current_device()
+    if q.dim() != 3:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    rows, Hq, d = q.shape
+    if q_grad is None:
+        q_grad = _empty((rows, Hq, d), dt, q.device, stream)
+    if q_weight_grad is None:
+        q_weight_grad = _empty((d,), torch.float32, q.device, stream)
+    qs, qgs = _heads(fn, q, dt, dev, rows, Hq, d), _heads(fn, q_grad, dt, dev, rows, Hq, d)
+    qys = _heads(fn, q_out_grad, dt, dev, rows, Hq, d)
+    Hkv, ks, kys, kgs, kp, kyp, kgp, kw, kwg = 0, 0, 0, 0, None, None, None, None, None
+    if k is not None:
+        if k.dim() != 3 or k_weight is None or k_out_grad is None:
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+        Hkv = k.shape[1]
+        if k_grad is None:
+            k_grad = _empty((rows, Hkv, d), dt, q.device, stream)
+        if k_weight_grad is None:
+            k_weight_grad = _empty((d,), torch.float32, q.device, stream)
+        ks, kgs = _heads(fn, k, dt, dev, rows, Hkv, d), _heads(fn, k_grad, dt, dev, rows, Hkv, d)
+        kys = _heads(fn, k_out_grad, dt, dev, rows, Hkv, d)
+        kp, kyp, kgp = k.data_ptr(), k_out_grad.data_ptr(), k_grad.data_ptr()
+        kw, kwg = _flat(fn, k_weight, dt, dev, (d,)), _flat(fn, k_weight_grad, torch.float32, dev, (d,))
+    else:
+        k_grad = k_weight_grad = None
+    if ws is None:
+        need = viscache_norm_mrope_grad_workspace_size(rows, Hq, Hkv, d)
+        if need == 0:
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+        ws = _workspace(need, q.device, None, stream)
+    elif ws.get_device() != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    rc = lib().viscache_norm_mrope_grad(
+        rope, _flat(fn, positions, torch.int32, dev, (rope.n_axes, rows)), code, rows, Hq, Hkv, d, q.data_ptr(), qs,
+        kp, ks, q_out_grad.data_ptr(), qys, kyp, kys, _flat(fn, q_weight, dt, dev, (d,)), kw, eps, q_grad.data_ptr(),
+        qgs, kgp, kgs, _flat(fn, q_weight_grad, torch.float32, dev, (d,)), kwg, ws.data_ptr(), ws.numel(),
+        _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
+    return q_grad, k_grad, q_weight_grad, k_weight_grad
 
 
 def viscache_set_kernel_path(path: int) -> None:
