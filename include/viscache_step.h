@@ -64,6 +64,35 @@ int viscache_norm_mrope_grad(const vc_rope* rope, const int32_t* positions, int 
                              int64_t k_grad_stride, float* q_weight_grad, float* k_weight_grad, void* ws,
                              size_t ws_bytes, void* stream);
 
+/*
+ * viscache_kv8_weigh -- what attention each cached token gets from the step's
+ * query rows, added up for each KV head:
+ *     A[t][g] = sum over the rows i that see t and the query heads j of group g
+ *               of exp(scale * q[i][j] . K_hat[t][g] - lse[i][j]),
+ *     weights[t][g] <- A[t][g] + (weights[t][g] if t < seq_lens - m else 0),
+ * m the request's rows: the step's own tokens start from A.  Rows, `causal` and
+ * `scale` mean what they mean in viscache_kv8_attention, whose `lse` this call
+ * reads; it is called after the rows have been appended and attended.
+ *   lse       device fp32 [n_rows][Hq].  A row whose lse is -inf (one that sees
+ *             no token) adds nothing
+ *   weights   device fp32 [n_pages][Hkv][page], a number for every slot of the
+ *             pool; 16-byte aligned.  Slots past seq_lens are left as they were.
+ * The pages of a call's requests must be different ones (a page of two requests
+ * would be written by both): requests that share a prefix's pages are weighed
+ * in calls of their own.
+ * Scores as in viscache_kv8_attention (fp32 rows as two fp16 numbers), sums in
+ * fp32 in an order that the call's sizes, lengths and the device's SMs decide:
+ * the same call gives the same bits.  A key that is not finite makes its token's
+ * weight NaN.
+ * Workspace: viscache_kv8_workspace_size(n_rows, Hq, Hkv, d), as for the
+ * attention; device checks and prunekv_get_status too.
+ * Errors: VC_ERR_INVALID_ARG, VC_ERR_WORKSPACE, VC_ERR_CUDA, and
+ * VC_ERR_UNSUPPORTED where the rows times max_pages are past 2^37 tiles.
+ */
+int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, int32_t Hq, const void* q,
+                       int64_t q_stride, const float* lse, float scale, int causal, float* weights, void* ws,
+                       size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -233,4 +233,18 @@ cudaError_t launch_kv8_attn_tc1(const vc_kv8& c, const vc_kv8_step& s, int dtype
                                 cudaStream_t st);
 cudaError_t launch_kv8_attn_tc2(const vc_kv8& c, const vc_kv8_step& s, const Kv8AttnArgs& a, cudaStream_t st);
 
+// Attention added up for each cached token (kv8_weigh.cu).
+struct Kv8WeighArgs {
+  const void* q;
+  int64_t q_stride;                    // elements between query rows
+  const float* lse;                    // [n_rows][Hq]
+  float* weights;                      // [n_pages][Hkv][page]
+  int32_t Hq, causal;
+  float scale;
+  int32_t* status;                     // status word, block count
+  int32_t* block_status;               // [kKv8MaxCtas]
+};
+cudaError_t launch_kv8_weigh(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8WeighArgs& a,
+                             cudaStream_t st);
+
 }  // namespace vc

@@ -331,4 +331,33 @@ int viscache_kv8_attention(const vc_kv8* cache, const vc_kv8_step* step, int dty
                                               : launch_kv8_attn_tc2(*cache, *step, a, st));
 }
 
+int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, int32_t Hq, const void* q,
+                       int64_t q_stride, const float* lse, float scale, int causal, float* weights, void* ws,
+                       size_t ws_bytes, void* stream) {
+  if (!valid_cache(cache) || !valid_step(cache, step) || !valid_type(dtype)) return VC_ERR_INVALID_ARG;
+  if (!valid_heads(Hq, cache->Hkv) || (int64_t)step->n_rows * Hq >= (int64_t)1 << 31) return VC_ERR_INVALID_ARG;
+  if (!(scale >= 0.f) || !isfinite(scale) || !weights || !aligned16(weights)) return VC_ERR_INVALID_ARG;
+  if (step->n_rows > 0 && (!q || !aligned16(q) || !valid_stride(q_stride, (int64_t)Hq * cache->d, dtype) || !lse ||
+                           (reinterpret_cast<uintptr_t>(lse) & 3u) != 0))
+    return VC_ERR_INVALID_ARG;
+  if (!short_line(*cache, *step, Hq)) return VC_ERR_UNSUPPORTED;
+  const Kv8Ws w = kv8_ws(false, cache->d);
+  const int wc = check_ws(ws, ws_bytes, w.total);
+  if (wc != VC_OK) return wc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  if (step->n_rows == 0) return cuda_status(cudaMemsetAsync(base, 0, sizeof(int32_t), st));
+  Kv8WeighArgs a = {};
+  a.q = q;
+  a.q_stride = q_stride;
+  a.lse = lse;
+  a.weights = weights;
+  a.Hq = Hq;
+  a.causal = causal != 0;
+  a.scale = scale == 0.f ? 1.0f / sqrtf((float)cache->d) : scale;
+  a.status = reinterpret_cast<int32_t*>(base);
+  a.block_status = reinterpret_cast<int32_t*>(base + w.o_blocks);
+  return cuda_status(launch_kv8_weigh(*cache, *step, dtype, a, st));
+}
+
 }  // extern "C"

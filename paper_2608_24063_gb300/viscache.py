@@ -52,7 +52,8 @@ EXPORTED = ("viscache_plan_budgets", "viscache_plan_budgets_ex", "prunekv_score_
             "viscache_kv8_append", "viscache_kv8_read", "viscache_kv8_attention")
 
 # the entry points of include/viscache_step.h
-EXPORTED_STEP = ("viscache_norm_mrope", "viscache_norm_mrope_grad_workspace_size", "viscache_norm_mrope_grad")
+EXPORTED_STEP = ("viscache_norm_mrope", "viscache_norm_mrope_grad_workspace_size", "viscache_norm_mrope_grad",
+                 "viscache_kv8_weigh")
 
 
 class VisCacheError(RuntimeError):
@@ -138,6 +139,7 @@ def lib() -> ctypes.CDLL:
         L.viscache_norm_mrope_grad_workspace_size.restype = sz
         L.viscache_norm_mrope_grad.argtypes = [pr, vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp,
                                                vp, f32, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.viscache_kv8_weigh.argtypes = [pc8, ps8, i32, i32, vp, i64, vp, f32, i32, vp, vp, sz, vp]
         L.prunekv_score_workspace_size.argtypes = [i32, i32, i32]
         L.prunekv_score_workspace_size.restype = sz
         L.prunekv_score.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, vp,
@@ -860,6 +862,27 @@ def viscache_norm_mrope_grad(rope: vc_rope, positions: torch.Tensor, q: torch.Te
     if rc != VC_OK:
         raise VisCacheError(fn, rc)
     return q_grad, k_grad, q_weight_grad, k_weight_grad
+
+
+def viscache_kv8_weigh(cache: Kv8Cache, step: Kv8Step, q: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor,
+                       scale: float = 0.0, causal: bool = True, ws: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """Adds the attention that the step's rows q [rows][Hq][d] pay each cached token to `weights` fp32
+    [n_pages][Hkv][page]; ``lse`` fp32 [rows][Hq] is viscache_kv8_attention's.  Returns `weights`."""
+    fn = "viscache_kv8_weigh"
+    code, dt = _type(q), q.dtype
+    if q.dim() != 3:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    rows, Hq, d = step.n_rows, q.shape[1], cache.d
+    dev, ws = _kv8_ws(fn, cache, step, Hq, ws, stream)
+    qs = _heads(fn, q, dt, dev, rows, Hq, d)
+    rc = lib().viscache_kv8_weigh(cache.c, step.c, code, Hq, q.data_ptr(), qs,
+                                  _flat(fn, lse, torch.float32, dev, (rows, Hq)), scale, 1 if causal else 0,
+                                  _flat(fn, weights, torch.float32, dev, (cache.n_pages, cache.Hkv, cache.page)),
+                                  ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
+    return weights
 
 
 def viscache_set_kernel_path(path: int) -> None:

@@ -30,11 +30,20 @@ def test_library_exports_every_declared_symbol():
         assert hasattr(vc.lib(), name) and callable(getattr(vc, name))
 
 
+def _cache():
+    return vc.Kv8Cache(z(4, 2, 16, 64, dt=U8), z(4, 2, 16, 64, dt=U8), z(4, 2, dt=F32), z(4, 2, dt=F32))
+
+
+def _step():
+    return vc.Kv8Step(z(1, 4, dt=I32), torch.full((1,), 3, dtype=I32), torch.tensor([0, 3], dtype=I32), 3)
+
+
 # the arguments of a call that makes its own workspace and outputs
 CALLS = {
     "viscache_norm_mrope": lambda: (vc.make_rope((16, 16)), z(2, 3, dt=I32), z(3, 4, 64), z(3, 2, 64), z(64), z(64)),
     "viscache_norm_mrope_grad": lambda: (vc.make_rope((16, 16)), z(2, 3, dt=I32), z(3, 4, 64), z(3, 2, 64), z(3, 4, 64),
                                          z(3, 2, 64), z(64), z(64)),
+    "viscache_kv8_weigh": lambda: (_cache(), _step(), z(3, 4, 64), z(3, 4, dt=F32), z(4, 2, 16, dt=F32)),
 }
 
 
@@ -132,3 +141,33 @@ def test_norm_mrope_grad_refuses():
              vc.VC_ERR_WORKSPACE)
     assert size(-1, 4, 2, 64) == 0 and size(3, 4, 2, 96) == 0 and size(3, 4097, 2, 64) == 0
     assert size(1 << 24, 64, 8, 128) == size(3, 64, 8, 128)
+
+
+def _pool(**kw):
+    return vc.vc_kv8(*{**dict(K_codes=A, V_codes=A, K_scale=A, V_scale=A, n_pages=4, Hkv=2, page=16, d=64), **kw}.values())
+
+
+def _requests(**kw):
+    return vc.vc_kv8_step(*{**dict(n_req=2, max_pages=3, block_table=A, seq_lens=A, row_start=A, n_rows=5), **kw}.values())
+
+
+POOLS = [dict(cache=None)] + [dict(cache=_pool(**kw)) for kw in (
+    dict(K_codes=None), dict(V_codes=A + 4), dict(K_scale=None), dict(V_scale=A + 8), dict(n_pages=0), dict(page=48),
+    dict(d=32), dict(Hkv=0), dict(Hkv=1025), dict(n_pages=1 << 27))]
+STEPS = [dict(step=None)] + [dict(step=_requests(**kw)) for kw in (
+    dict(block_table=None), dict(seq_lens=None), dict(row_start=None), dict(n_req=0), dict(n_req=1025),
+    dict(max_pages=0), dict(max_pages=1 << 28), dict(n_rows=-1), dict(n_rows=(1 << 24) + 1))]
+
+
+def test_kv8_weigh_refuses():
+    need = vc.viscache_kv8_workspace_size(5, 4, 2, 64)
+    good = dict(cache=_pool(), step=_requests(), dtype=0, Hq=4, q=A, q_stride=256, lse=A, scale=0.0, causal=1,
+                weights=A, ws=A, ws_bytes=need, stream=None)
+    own = [dict(dtype=2), dict(Hq=3), dict(Hq=0), dict(Hq=8192), dict(q=None), dict(q=A + 8), dict(q_stride=248),
+           dict(q_stride=260), dict(lse=None), dict(lse=A + 2), dict(scale=-1.0), dict(scale=float("inf")),
+           dict(scale=float("nan")), dict(weights=None), dict(weights=A + 4)]
+    _refused("viscache_kv8_weigh", good, POOLS + STEPS + own)
+    _refused("viscache_kv8_weigh", good, [dict(ws=None), dict(ws=A + 16), dict(ws_bytes=1024)], vc.VC_ERR_WORKSPACE)
+    long = dict(cache=_pool(Hkv=1024, n_pages=1 << 10), Hq=1024, step=_requests(n_rows=1 << 20, max_pages=1 << 26),
+                q_stride=1 << 16)
+    _refused("viscache_kv8_weigh", good, [long], vc.VC_ERR_UNSUPPORTED)
