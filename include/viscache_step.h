@@ -93,6 +93,41 @@ int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, 
                        int64_t q_stride, const float* lse, float scale, int causal, float* weights, void* ws,
                        size_t ws_bytes, void* stream);
 
+/*
+ * viscache_kv8_evict -- hold requests to a budget: of each request and KV head
+ * the keep[r] tokens with the largest weights stay, in their order, and move
+ * together; the others are gone.  A request of no more than keep[r] tokens is
+ * left as it is.
+ *   weights   as in viscache_kv8_weigh; moved with their tokens
+ *   keep      device int32 [n_req], 0 .. max_keep
+ *   sink, recent   the first `sink` and the last `recent` tokens of a request
+ *             count as heavier than any weight but +inf; among equal weights the
+ *             lower token stays; NaN counts as less than any number
+ *   kept      device int32 [n_req][Hkv][max_keep]: the tokens that stayed, by
+ *             their old places, ascending; entries past the new length are left as
+ *             they were
+ *   new_lens  device int32 [n_req]: min(seq_lens, keep).  May be step->seq_lens
+ *             itself; else seq_lens is left as it was, and the caller goes on with
+ *             new_lens
+ * Each page from the one with the first gap on holds what viscache_kv8_append
+ * would write into it from the values x_hat that stayed: scales are taken anew,
+ * codes are re-encoded where the scale changed (exact but for values that fall
+ * below e4m3's smallest normal number under a larger scale).  Slots past the new
+ * length, and pages past it, hold what they held.  Of the step only n_req, the
+ * block table and seq_lens count.  The pages of the call's requests must be
+ * different ones.
+ * Workspace: viscache_kv8_evict_workspace_size(n_req, Hkv) bytes (0 for arguments
+ * that the call refuses), 256-byte aligned; prunekv_get_status(ws) reports device
+ * checks: a length or a page out of range (VC_ERR_DEVICE_INDEX), keep outside
+ * [0, max_keep].  They are clamped; a request with a page out of range is left
+ * as it was, with new_lens its (clamped) length and no `kept`.
+ * Errors: VC_ERR_INVALID_ARG, VC_ERR_WORKSPACE, VC_ERR_CUDA.
+ */
+size_t viscache_kv8_evict_workspace_size(int32_t n_req, int32_t Hkv);
+int viscache_kv8_evict(const vc_kv8* cache, const vc_kv8_step* step, float* weights, const int32_t* keep,
+                       int32_t max_keep, int32_t sink, int32_t recent, int32_t* kept, int32_t* new_lens, void* ws,
+                       size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -247,4 +247,19 @@ struct Kv8WeighArgs {
 cudaError_t launch_kv8_weigh(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8WeighArgs& a,
                              cudaStream_t st);
 
+// Eviction by weight (kv8_evict.cu).
+struct Kv8Unit {                       // a request and KV head: first gap, new length; the request's error
+  int32_t gap, len, err, pad;
+};
+struct Kv8EvictArgs {
+  float* weights;                      // [n_pages][Hkv][page]
+  const int32_t* keep;                 // [n_req]
+  int32_t max_keep, sink, recent;
+  int32_t* kept;                       // [n_req][Hkv][max_keep]
+  int32_t* new_lens;                   // [n_req]
+  int32_t* status;
+  Kv8Unit* units;                      // [n_req][Hkv]
+};
+cudaError_t launch_kv8_evict(const vc_kv8& c, const vc_kv8_step& s, const Kv8EvictArgs& a, cudaStream_t st);
+
 }  // namespace vc

@@ -360,4 +360,26 @@ int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, 
   return cuda_status(launch_kv8_weigh(*cache, *step, dtype, a, st));
 }
 
+size_t viscache_kv8_evict_workspace_size(int32_t n_req, int32_t Hkv) {
+  if (n_req < 1 || n_req > 1024 || Hkv < 1 || Hkv > 1024) return 0;
+  return kAlign + align_up(sizeof(Kv8Unit) * n_req * Hkv);
+}
+
+int viscache_kv8_evict(const vc_kv8* cache, const vc_kv8_step* step, float* weights, const int32_t* keep,
+                       int32_t max_keep, int32_t sink, int32_t recent, int32_t* kept, int32_t* new_lens, void* ws,
+                       size_t ws_bytes, void* stream) {
+  if (!valid_cache(cache) || !valid_step(cache, step)) return VC_ERR_INVALID_ARG;
+  if (!weights || !aligned16(weights) || !keep || !kept || !new_lens) return VC_ERR_INVALID_ARG;
+  if (((reinterpret_cast<uintptr_t>(keep) | reinterpret_cast<uintptr_t>(kept) |
+        reinterpret_cast<uintptr_t>(new_lens)) & 3u) != 0)
+    return VC_ERR_INVALID_ARG;
+  if (max_keep < 1 || max_keep > (1 << 30) || sink < 0 || recent < 0) return VC_ERR_INVALID_ARG;
+  const int wc = check_ws(ws, ws_bytes, viscache_kv8_evict_workspace_size(step->n_req, cache->Hkv));
+  if (wc != VC_OK) return wc;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  const Kv8EvictArgs a = {weights, keep, max_keep, sink, recent, kept, new_lens, reinterpret_cast<int32_t*>(base),
+                          reinterpret_cast<Kv8Unit*>(base + kAlign)};
+  return cuda_status(launch_kv8_evict(*cache, *step, a, static_cast<cudaStream_t>(stream)));
+}
+
 }  // extern "C"

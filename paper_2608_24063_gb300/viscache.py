@@ -53,7 +53,7 @@ EXPORTED = ("viscache_plan_budgets", "viscache_plan_budgets_ex", "prunekv_score_
 
 # the entry points of include/viscache_step.h
 EXPORTED_STEP = ("viscache_norm_mrope", "viscache_norm_mrope_grad_workspace_size", "viscache_norm_mrope_grad",
-                 "viscache_kv8_weigh")
+                 "viscache_kv8_weigh", "viscache_kv8_evict_workspace_size", "viscache_kv8_evict")
 
 
 class VisCacheError(RuntimeError):
@@ -140,6 +140,9 @@ def lib() -> ctypes.CDLL:
         L.viscache_norm_mrope_grad.argtypes = [pr, vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp,
                                                vp, f32, vp, i64, vp, i64, vp, vp, vp, sz, vp]
         L.viscache_kv8_weigh.argtypes = [pc8, ps8, i32, i32, vp, i64, vp, f32, i32, vp, vp, sz, vp]
+        L.viscache_kv8_evict_workspace_size.argtypes = [i32, i32]
+        L.viscache_kv8_evict_workspace_size.restype = sz
+        L.viscache_kv8_evict.argtypes = [pc8, ps8, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
         L.prunekv_score_workspace_size.argtypes = [i32, i32, i32]
         L.prunekv_score_workspace_size.restype = sz
         L.prunekv_score.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, vp,
@@ -883,6 +886,42 @@ def viscache_kv8_weigh(cache: Kv8Cache, step: Kv8Step, q: torch.Tensor, lse: tor
     if rc != VC_OK:
         raise VisCacheError(fn, rc)
     return weights
+
+
+def viscache_kv8_evict_workspace_size(n_req: int, Hkv: int) -> int:
+    return lib().viscache_kv8_evict_workspace_size(n_req, Hkv)
+
+
+def viscache_kv8_evict(cache: Kv8Cache, step: Kv8Step, weights: torch.Tensor, keep: torch.Tensor, max_keep: int,
+                       sink: int = 0, recent: int = 0, kept: Optional[torch.Tensor] = None,
+                       new_lens: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Holds each request to its keep[r] (int32, on the device, at most max_keep) heaviest tokens of each
+    KV head, in place: (kept int32 [n_req][Hkv][max_keep], new_lens int32 [n_req]).  ``new_lens`` may be
+    the step's seq_lens."""
+    fn = "viscache_kv8_evict"
+    dev, n = _current_device(), step.c.n_req
+    if cache.index != dev or step.index != dev:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    if kept is None:
+        kept = _empty((n, cache.Hkv, max_keep), torch.int32, cache.device, stream)
+    if new_lens is None:
+        new_lens = _empty((n,), torch.int32, cache.device, stream)
+    if ws is None:
+        need = viscache_kv8_evict_workspace_size(n, cache.Hkv)
+        if need == 0:
+            raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+        ws = _workspace(need, cache.device, None, stream)
+    elif ws.get_device() != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    rc = lib().viscache_kv8_evict(cache.c, step.c,
+                                  _flat(fn, weights, torch.float32, dev, (cache.n_pages, cache.Hkv, cache.page)),
+                                  _flat(fn, keep, torch.int32, dev, (n,)), max_keep, sink, recent,
+                                  _flat(fn, kept, torch.int32, dev, (n, cache.Hkv, max_keep)),
+                                  _flat(fn, new_lens, torch.int32, dev, (n,)), ws.data_ptr(), ws.numel(),
+                                  _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
+    return kept, new_lens
 
 
 def viscache_set_kernel_path(path: int) -> None:

@@ -44,6 +44,7 @@ CALLS = {
     "viscache_norm_mrope_grad": lambda: (vc.make_rope((16, 16)), z(2, 3, dt=I32), z(3, 4, 64), z(3, 2, 64), z(3, 4, 64),
                                          z(3, 2, 64), z(64), z(64)),
     "viscache_kv8_weigh": lambda: (_cache(), _step(), z(3, 4, 64), z(3, 4, dt=F32), z(4, 2, 16, dt=F32)),
+    "viscache_kv8_evict": lambda: (_cache(), _step(), z(4, 2, 16, dt=F32), z(1, dt=I32), 2),
 }
 
 
@@ -171,3 +172,15 @@ def test_kv8_weigh_refuses():
     long = dict(cache=_pool(Hkv=1024, n_pages=1 << 10), Hq=1024, step=_requests(n_rows=1 << 20, max_pages=1 << 26),
                 q_stride=1 << 16)
     _refused("viscache_kv8_weigh", good, [long], vc.VC_ERR_UNSUPPORTED)
+
+
+def test_kv8_evict_refuses():
+    size = vc.viscache_kv8_evict_workspace_size
+    good = dict(cache=_pool(), step=_requests(), weights=A, keep=A, max_keep=8, sink=0, recent=0, kept=A, new_lens=A,
+                ws=A, ws_bytes=size(2, 2), stream=None)
+    own = [{p: v} for p in ("weights", "keep", "kept", "new_lens") for v in (None, A + 2)] + [
+        dict(weights=A + 4), dict(max_keep=0), dict(max_keep=(1 << 30) + 1), dict(sink=-1), dict(recent=-1)]
+    _refused("viscache_kv8_evict", good, POOLS + STEPS + own)
+    _refused("viscache_kv8_evict", good, [dict(ws=None), dict(ws=A + 16), dict(ws_bytes=size(2, 2) - 1)],
+             vc.VC_ERR_WORKSPACE)
+    assert size(0, 2) == 0 and size(1025, 2) == 0 and size(2, 0) == 0 and size(2, 1025) == 0
