@@ -128,6 +128,36 @@ int viscache_kv8_evict(const vc_kv8* cache, const vc_kv8_step* step, float* weig
                        int32_t max_keep, int32_t sink, int32_t recent, int32_t* kept, int32_t* new_lens, void* ws,
                        size_t ws_bytes, void* stream);
 
+/*
+ * viscache_sample -- the next token of each row of logits, from a given random
+ * number.  With x the row, M its maximum, T its temperature:
+ *     w_i = exp((x_i - M) / T);   order: by logit descending, ties by index;
+ *     kept: the first min(top_k, n_p, n_m) tokens of the order, at least one,
+ *       n_p  the least n whose first n weights reach top_p times the weights of
+ *            the first top_k,
+ *       n_m  the number of tokens with w_i >= min_p;
+ *     token = the least i with  sum_{kept j <= i} w_j > u * sum_kept w,
+ *     logprob = log(w_token / sum_kept w).
+ * T <= 0 (or NaN) is greedy: the first of the largest logits, logprob 0.  top_k <= 0,
+ * top_p >= 1 and min_p <= 0 (or NaN) keep everything, and so does a NULL array;
+ * top_p <= 0 and min_p >= 1 keep the first, min_p >= 1 all that tie with it.
+ * u below 0 (or NaN) counts as 0, of 1 and more as the last kept token with a weight.
+ *   logits    device rows of `dtype`, row r at element r * stride; any stride of at
+ *             least vocab and any alignment of the type
+ *   u, temperature   device fp32 [n_rows]; top_k int32, top_p, min_p fp32 [n_rows]
+ *   token     device int32 [n_rows];  logprob device fp32 [n_rows] (nullable)
+ * A logit of -inf or NaN has weight 0; of +inf, weight 1 and all others 0.  A row with
+ * nothing above -inf gives token -1 and logprob NaN.
+ * Weights are whole numbers of 2^-44 (2^-45 at 131072 tokens and fewer, 2^-47 at 32768)
+ * from an exponential of about 38 bits: sums are exact and do not depend on their order,
+ * and a token differs from the formula's only where u, top_p or min_p lie within about
+ * 2^-36 of a border.  vocab 1 .. 262144; n_rows 0 .. 65535.  No workspace.
+ * Errors: VC_ERR_INVALID_ARG, VC_ERR_CUDA.
+ */
+int viscache_sample(int dtype, int64_t n_rows, int64_t vocab, const void* logits, int64_t stride, const float* u,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                    int32_t* token, float* logprob, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -107,6 +107,7 @@ def sample(x, u: float, T: float, top_k: int = 0, top_p: float = 1.0, min_p: flo
         return int(np.argmax(x)), 0.0
     with np.errstate(invalid="ignore"):
         w = np.where(x == M, 1.0, np.exp((x - M) / T))
+    w[(x == -np.inf) | ((M == np.inf) & (x != M))] = 0.0            # whatever T is
     order = np.argsort(-x, kind="stable")
     n = len(x)
     if top_k > 0:

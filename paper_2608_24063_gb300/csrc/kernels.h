@@ -262,4 +262,18 @@ struct Kv8EvictArgs {
 };
 cudaError_t launch_kv8_evict(const vc_kv8& c, const vc_kv8_step& s, const Kv8EvictArgs& a, cudaStream_t st);
 
+// The next token of each row of logits (sample.cu).
+constexpr int64_t kSampleMaxVocab = 262144;
+struct SampleArgs {
+  const void* logits;
+  int64_t stride, vocab;
+  const float *u, *temperature, *top_p, *min_p;   // [rows]; the filters may be NULL
+  const int32_t* top_k;
+  int32_t* token;
+  float* logprob;                      // or NULL
+  int32_t q;                           // a weight of 1 is 2^q: vocab of them fit 62 bits
+  int32_t C, vecs;                     // blocks of a row, 16-byte vectors of a block (set by the launcher)
+};
+cudaError_t launch_sample(const SampleArgs& a, int dtype, int64_t n_rows, cudaStream_t st);
+
 }  // namespace vc

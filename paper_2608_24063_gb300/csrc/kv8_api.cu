@@ -382,4 +382,21 @@ int viscache_kv8_evict(const vc_kv8* cache, const vc_kv8_step* step, float* weig
   return cuda_status(launch_kv8_evict(*cache, *step, a, static_cast<cudaStream_t>(stream)));
 }
 
+int viscache_sample(int dtype, int64_t n_rows, int64_t vocab, const void* logits, int64_t stride, const float* u,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                    int32_t* token, float* logprob, void* stream) {
+  if (!valid_type(dtype) || n_rows < 0 || n_rows > 65535 || vocab < 1 || vocab > kSampleMaxVocab)
+    return VC_ERR_INVALID_ARG;
+  if (stride < vocab || stride >= (int64_t)1 << 40) return VC_ERR_INVALID_ARG;
+  if (n_rows == 0) return VC_OK;
+  if (!logits || !u || !temperature || !token) return VC_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(logits) & (dtype == VC_BF16 ? 1u : 3u)) != 0) return VC_ERR_INVALID_ARG;
+  const void* words[] = {u, temperature, top_k, top_p, min_p, token, logprob};
+  for (const void* w : words)
+    if ((reinterpret_cast<uintptr_t>(w) & 3u) != 0) return VC_ERR_INVALID_ARG;
+  SampleArgs a = {logits, stride, vocab, u, temperature, top_p, min_p, top_k, token, logprob, 47, 1, 0};
+  while ((uint64_t)vocab > ((uint64_t)1 << 62) >> a.q) --a.q;
+  return cuda_status(launch_sample(a, dtype, n_rows, static_cast<cudaStream_t>(stream)));
+}
+
 }  // extern "C"

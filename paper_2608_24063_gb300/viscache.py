@@ -53,7 +53,7 @@ EXPORTED = ("viscache_plan_budgets", "viscache_plan_budgets_ex", "prunekv_score_
 
 # the entry points of include/viscache_step.h
 EXPORTED_STEP = ("viscache_norm_mrope", "viscache_norm_mrope_grad_workspace_size", "viscache_norm_mrope_grad",
-                 "viscache_kv8_weigh", "viscache_kv8_evict_workspace_size", "viscache_kv8_evict")
+                 "viscache_kv8_weigh", "viscache_kv8_evict_workspace_size", "viscache_kv8_evict", "viscache_sample")
 
 
 class VisCacheError(RuntimeError):
@@ -143,6 +143,7 @@ def lib() -> ctypes.CDLL:
         L.viscache_kv8_evict_workspace_size.argtypes = [i32, i32]
         L.viscache_kv8_evict_workspace_size.restype = sz
         L.viscache_kv8_evict.argtypes = [pc8, ps8, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.viscache_sample.argtypes = [i32, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
         L.prunekv_score_workspace_size.argtypes = [i32, i32, i32]
         L.prunekv_score_workspace_size.restype = sz
         L.prunekv_score.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, vp,
@@ -922,6 +923,35 @@ def viscache_kv8_evict(cache: Kv8Cache, step: Kv8Step, weights: torch.Tensor, ke
     if rc != VC_OK:
         raise VisCacheError(fn, rc)
     return kept, new_lens
+
+
+def viscache_sample(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor,
+                    top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                    min_p: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None,
+                    logprob: Optional[torch.Tensor] = None, stream=None):
+    """The next token of each row of logits [rows][vocab] from random numbers u [rows] in [0, 1):
+    (token int32 [rows], logprob fp32 [rows]).  temperature, top_p, min_p fp32 [rows], top_k int32 [rows];
+    a filter that is None keeps everything.  Rows of logits may be strided."""
+    fn = "viscache_sample"
+    code, dev = _type(logits), _current_device()
+    if logits.dim() != 2 or logits.get_device() != dev:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    n, vocab = logits.shape
+    stride = logits.stride(0) if n > 1 else vocab
+    if vocab > 1 and logits.stride(1) != 1:
+        raise VisCacheError(fn, VC_ERR_INVALID_ARG)
+    if token is None:
+        token = _empty((n,), torch.int32, logits.device, stream)
+    if logprob is None:
+        logprob = _empty((n,), torch.float32, logits.device, stream)
+    row = lambda t, dt: None if t is None else _flat(fn, t, dt, dev, (n,))
+    rc = lib().viscache_sample(code, n, vocab, logits.data_ptr(), stride, row(u, torch.float32),
+                               row(temperature, torch.float32), row(top_k, torch.int32), row(top_p, torch.float32),
+                               row(min_p, torch.float32), row(token, torch.int32), row(logprob, torch.float32),
+                               _raw_stream(stream, dev))
+    if rc != VC_OK:
+        raise VisCacheError(fn, rc)
+    return token, logprob
 
 
 def viscache_set_kernel_path(path: int) -> None:

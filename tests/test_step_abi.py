@@ -45,6 +45,7 @@ CALLS = {
                                          z(3, 2, 64), z(64), z(64)),
     "viscache_kv8_weigh": lambda: (_cache(), _step(), z(3, 4, 64), z(3, 4, dt=F32), z(4, 2, 16, dt=F32)),
     "viscache_kv8_evict": lambda: (_cache(), _step(), z(4, 2, 16, dt=F32), z(1, dt=I32), 2),
+    "viscache_sample": lambda: (z(3, 40), z(3, dt=F32), z(3, dt=F32)),
 }
 
 
@@ -184,3 +185,14 @@ def test_kv8_evict_refuses():
     _refused("viscache_kv8_evict", good, [dict(ws=None), dict(ws=A + 16), dict(ws_bytes=size(2, 2) - 1)],
              vc.VC_ERR_WORKSPACE)
     assert size(0, 2) == 0 and size(1025, 2) == 0 and size(2, 0) == 0 and size(2, 1025) == 0
+
+
+def test_sample_refuses():
+    good = dict(dtype=0, n_rows=3, vocab=100, logits=A, stride=100, u=A, temperature=A, top_k=A, top_p=A, min_p=A,
+                token=A, logprob=A, stream=None)
+    _refused("viscache_sample", good, [
+        dict(dtype=2), dict(n_rows=-1), dict(n_rows=65536), dict(vocab=0), dict(vocab=262145, stride=262145),
+        dict(stride=99), dict(stride=1 << 40), dict(logits=None), dict(logits=A + 1), dict(dtype=1, logits=A + 2),
+        dict(u=None), dict(temperature=None), dict(token=None)] +
+        [{p: A + 2} for p in ("u", "temperature", "top_k", "top_p", "min_p", "token", "logprob")])
+    assert vc.lib().viscache_sample(*{**good, "n_rows": 0, "logits": None}.values()) == vc.VC_OK
