@@ -240,10 +240,16 @@ struct Kv8WeighArgs {
   const float* lse;                    // [n_rows][Hq]
   float* weights;                      // [n_pages][Hkv][page]
   int32_t Hq, causal;
-  float scale;
+  float scale;                         // of the logits
+  float scale_log2, lse_log2, lse_log2_lo;   // scale * log2(e), and lse's factor in two parts (kv8_weigh_tc.cu)
   int32_t* status;                     // status word, block count
   int32_t* block_status;               // [kKv8MaxCtas]
+  uint64_t token;                      // as in Kv8AttnArgs, of kv8_weigh_tc.cu alone
+  uint64_t* flags;                     // [2 kKv8MaxCtas]
+  float* part;                         // [2 kKv8MaxCtas][tokens of a unit]
 };
+cudaError_t launch_kv8_weigh_tc(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8WeighArgs& a,
+                                cudaStream_t st);    // many query rows a request
 cudaError_t launch_kv8_weigh(const vc_kv8& c, const vc_kv8_step& s, int dtype, const Kv8WeighArgs& a,
                              cudaStream_t st);
 

@@ -145,6 +145,10 @@ Kernel kernel_of(const vc_kv8& c, const vc_kv8_step& s, int dtype, int32_t Hq) {
   return two ? Kernel::kTc2 : Kernel::kTc1;
 }
 
+// viscache_kv8_weigh on tcgen05: more packed rows of a KV head per request on average
+// than the mma.sync kernel's fragments hold.
+constexpr int64_t kWeighTcRows = 16;
+
 bool valid_heads(int32_t Hq, int32_t Hkv) { return Hkv >= 1 && Hq >= Hkv && Hq <= 4096 && Hq % Hkv == 0; }
 
 // The attention's line of key tiles (units of 8 rows at least): a block's share is
@@ -341,7 +345,7 @@ int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, 
                            (reinterpret_cast<uintptr_t>(lse) & 3u) != 0))
     return VC_ERR_INVALID_ARG;
   if (!short_line(*cache, *step, Hq)) return VC_ERR_UNSUPPORTED;
-  const Kv8Ws w = kv8_ws(false, cache->d);
+  const Kv8Ws w = kv8_ws(false, cache->d);      // (the outputs' place, 16 rows of d a piece, holds the sums of 384 tokens)
   const int wc = check_ws(ws, ws_bytes, w.total);
   if (wc != VC_OK) return wc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -354,10 +358,22 @@ int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, 
   a.weights = weights;
   a.Hq = Hq;
   a.causal = causal != 0;
-  a.scale = scale == 0.f ? 1.0f / sqrtf((float)cache->d) : scale;
+  const double exact = scale == 0.f ? 1.0 / sqrt((double)cache->d) : (double)scale;
+  a.scale = (float)exact;
+  constexpr double kLog2eExact = 1.4426950408889634074, kCut = 0.7213 * 0x1p-24;
+  a.scale_log2 = (float)(exact * kLog2eExact);
+  const double factor = exact > 0.0 ? (double)a.scale_log2 / exact * (1.0 - kCut) : kLog2eExact;
+  a.lse_log2 = (float)factor;
+  a.lse_log2_lo = (float)(factor - (double)a.lse_log2);
   a.status = reinterpret_cast<int32_t*>(base);
   a.block_status = reinterpret_cast<int32_t*>(base + w.o_blocks);
-  return cuda_status(launch_kv8_weigh(*cache, *step, dtype, a, st));
+  a.token = next_token();
+  a.flags = reinterpret_cast<uint64_t*>(base + w.o_flags);
+  a.part = reinterpret_cast<float*>(base + w.o_o);
+  // (a step there holds all heads of a group: 128 fit in both types)
+  const bool many = (int64_t)step->n_rows * (Hq / cache->Hkv) > kWeighTcRows * step->n_req && Hq / cache->Hkv <= 128;
+  return cuda_status(many ? launch_kv8_weigh_tc(*cache, *step, dtype, a, st)
+                          : launch_kv8_weigh(*cache, *step, dtype, a, st));
 }
 
 size_t viscache_kv8_evict_workspace_size(int32_t n_req, int32_t Hkv) {

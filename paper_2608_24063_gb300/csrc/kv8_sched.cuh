@@ -30,6 +30,9 @@ namespace vc {
 // Tensor map of a pool's codes: rows of d bytes, a box is a page's rows of one
 // head, swizzled over whole rows (128 bytes at d = 128, 64 at d = 64).
 bool kv8_pool_map(CUtensorMap* m, const void* base, const vc_kv8& c);
+// Tensor map of bf16 query rows [n_rows][Hq][d], `stride` elements between rows: a box is 64
+// dimensions of `heads` heads (at most 256) of `rows` rows, swizzled over 128 bytes.
+bool kv8_rows_map(CUtensorMap* m, const void* q, int64_t n_rows, int Hq, int d, int64_t stride, int heads, int rows);
 
 namespace kv8 {
 
@@ -204,8 +207,8 @@ __device__ __forceinline__ void set_range(Share& sh, int64_t T) {
 }
 
 // Finds the tile `begin` within request r, whose first tile is `at`.
-template <int MT, int KT>
-__device__ __forceinline__ void set_first(const Line<MT, KT>& line, Share& sh, int64_t begin, int64_t at, int r,
+template <typename L>
+__device__ __forceinline__ void set_first(const L& line, Share& sh, int64_t begin, int64_t at, int r,
                                           const Req8& q) {
   Unit u;
   u.r = r;
@@ -228,8 +231,8 @@ __device__ __forceinline__ void set_first(const Line<MT, KT>& line, Share& sh, i
 // requests, and a scan over the block places them on the line.  The thread
 // whose requests hold the first tile of the share looks it up.  Ends with a
 // barrier.
-template <int NT, int MT, int KT>
-__device__ __forceinline__ void find_share(const Line<MT, KT>& line, const vc_kv8_step& s, int32_t* status,
+template <int NT, typename L>
+__device__ __forceinline__ void find_share(const L& line, const vc_kv8_step& s, int32_t* status,
                                            Share& sh, int64_t* scan) {
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   if (s.n_req <= 32) {
