@@ -138,7 +138,7 @@ int viscache_kv8_evict(const vc_kv8* cache, const vc_kv8_step* step, float* weig
  *       n_m  the number of tokens with w_i >= min_p;
  *     token = the least i with  sum_{kept j <= i} w_j > u * sum_kept w,
  *     logprob = log(w_token / sum_kept w).
- * T <= 0 (or NaN) is greedy: the first of the largest logits, logprob 0.  top_k <= 0,
+ * T <= 0 (or NaN) is greedy (a positive T below 2^-127 counts as 2^-127): the first of the largest logits, logprob 0.  top_k <= 0,
  * top_p >= 1 and min_p <= 0 (or NaN) keep everything, and so does a NULL array;
  * top_p <= 0 and min_p >= 1 keep the first, min_p >= 1 all that tie with it.
  * u below 0 (or NaN) counts as 0, of 1 and more as the last kept token with a weight.

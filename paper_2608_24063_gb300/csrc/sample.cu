@@ -7,16 +7,24 @@
 // index, first pass u times their sum.
 //
 // Reads the logits once: a cluster of C blocks holds a row in shared memory, and
-// everything after works there.  Passes: (1) load, maximum; (2) weights summed, with
-// top-k or top-p into a histogram of buckets of 1/16 in z; (3) for a cut that falls
-// inside a bucket, histograms of ever finer ranges of keys until one logit is left;
-// (4) sums of the kept weights of each thread's run of tokens, a scan, and the one warp
-// that holds the token looks through its run.
-//
-// A token is a whole number: an answer off by one border is wrong, and rows have up to
-// 262144 borders, so weights are computed to about 40 bits (pairs of fp32 numbers, a table
-// of 2^(-i/64) and a polynomial of degree 4) and added as 64-bit whole numbers: exact in
-// any order, so atomics and the split over blocks do not change a result.
+// everything after works there.  A token is a whole number: an answer off by one border is
+// wrong, and rows have up to 262144 borders, so weights are computed to about 38 bits
+// (pairs of fp32 numbers, a table of 2^(-i/64) and a polynomial of degree 4) and added as
+// 64-bit whole numbers: exact in any order, so neither atomics nor the split over blocks
+// change a result.  Such a weight costs some forty instructions, and what bounds large
+// batches is that arithmetic, so it is done as rarely as the cuts allow:
+//   - without filters once for each token;
+//   - with filters, the tokens are counted by buckets of 1/16 in z first (no weight).  What
+//     top-k keeps, and where top-p's cut can lie (a bucket's weights differ by 4.4%), follows
+//     from the counts.  If that is kMostListed tokens or fewer, they are listed, one block orders
+//     them by counting and does the rest on the list; for top-p alone the sum of all
+//     weights is taken once;
+//   - a larger nucleus: the sums of all weights and of those in buckets before the cut's
+//     are taken in one pass, by runs of tokens, and the cut is narrowed by counts of ever finer
+//     ranges of keys; weights are taken again of the tokens in the cut's buckets alone;
+//   - a larger top-k goes through histograms of counts and weights.
+// Then the kept weights of each thread's run of tokens are scanned, and the one warp that
+// holds the token looks through its run.
 #include "kernels.h"
 #include "kv8_sched.cuh"
 #include "profile.h"
@@ -32,62 +40,70 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBuckets = 1024;
 constexpr float kPerZ = 16.f;                   // buckets of 1 in z: z < 64
-constexpr int kTableBits = 47;
+constexpr int kTableBits = 48;
+constexpr int kMostListed = 1024;
 
-// 2^(47 - i / 64), rounded
+// 2^(48 - i / 64), rounded
 __constant__ uint64_t kPowers[64] = {
-    0x800000000000ull, 0x7e9f06067a43ull, 0x7d41d96db915ull, 0x7be86fb98569ull, 0x7a92be8a9243ull, 0x7940bb9e2d00ull,
-    0x77f25ccdee6dull, 0x76a7980f6ccaull, 0x75606373ee92ull, 0x741cb5281e26ull, 0x72dc8373be42ull, 0x719fc4b95f45ull,
-    0x70666f76154aull, 0x6f307a412f07ull, 0x6dfddbcbed79ull, 0x6cce8ae13c58ull, 0x6ba27e656b4full, 0x6a79ad55e7f7ull,
-    0x69540ec8f895ull, 0x683199ed7796ull, 0x6712460a8fc2ull, 0x65f60a7f7939ull, 0x64dcdec33718ull, 0x63c6ba6455ddull,
-    0x62b39508aa83ull, 0x61a3666d124cull, 0x609626653338ull, 0x5f8bccdb3d3aull, 0x5e8451cfac06ull, 0x5d7fad59099full,
-    0x5c7dd7a3b17eull, 0x5b7ec8f19469ull, 0x5a827999fcefull, 0x5988e2095489ull, 0x5891fac0e956ull, 0x579dbc56b485ull,
-    0x56ac1f752151ull, 0x55bd1cdad49full, 0x54d0ad5a753eull, 0x53e6c9da74b3ull, 0x52ff6b54d8a9ull, 0x521a8ad704f3ull,
-    0x513821818625ull, 0x50582887dcb9ull, 0x4f7a993048d1ull, 0x4e9f6cd39680ull, 0x4dc69cdceaa7ull, 0x4cf022c9905cull,
-    0x4c1bf828c6dcull, 0x4b4a169b900cull, 0x4a7a77d47f7cull, 0x49ad159789f3ull, 0x48e1e9b9d589ull, 0x4818ee218a33ull,
-    0x47521cc5a2e7ull, 0x468d6fadbf2eull, 0x45cae0f1f546ull, 0x450a6abaa4b7ull, 0x444c0740496dull, 0x438fb0cb4f47ull,
-    0x42d561b3e624ull, 0x421d1461d66full, 0x4166c34c5616ull, 0x40b268f9de02ull
+    0x1000000000000ull, 0xfd3e0c0cf487ull, 0xfa83b2db722aull, 0xf7d0df730ad1ull, 0xf5257d152487ull, 0xf281773c5a00ull,
+    0xefe4b99bdcdbull, 0xed4f301ed994ull, 0xeac0c6e7dd24ull, 0xe8396a503c4cull, 0xe5b906e77c83ull, 0xe33f8972be8aull,
+    0xe0ccdeec2a95ull, 0xde60f4825e0full, 0xdbfbb797daf2ull, 0xd99d15c278b0ull, 0xd744fccad69dull, 0xd4f35aabcfeeull,
+    0xd2a81d91f12bull, 0xd06333daef2bull, 0xce248c151f85ull, 0xcbec14fef272ull, 0xc9b9bd866e2full, 0xc78d74c8abbaull,
+    0xc5672a115507ull, 0xc346ccda2497ull, 0xc12c4cca6671ull, 0xbf1799b67a73ull, 0xbd08a39f580cull, 0xbaff5ab2133eull,
+    0xb8fbaf4762fcull, 0xb6fd91e328d1ull, 0xb504f333f9deull, 0xb311c412a911ull, 0xb123f581d2acull, 0xaf3b78ad690aull,
+    0xad583eea42a1ull, 0xab7a39b5a93full, 0xa9a15ab4ea7cull, 0xa7cd93b4e965ull, 0xa5fed6a9b151ull, 0xa43515ae09e7ull,
+    0xa27043030c49ull, 0xa0b0510fb971ull, 0x9ef5326091a1ull, 0x9d3ed9a72d00ull, 0x9b8d39b9d54eull, 0x99e0459320b8ull,
+    0x9837f0518db9ull, 0x96942d372018ull, 0x94f4efa8fef7ull, 0x935a2b2f13e7ull, 0x91c3d373ab12ull, 0x9031dc431467ull,
+    0x8ea4398b45cdull, 0x8d1adf5b7e5cull, 0x8b95c1e3ea8cull, 0x8a14d575496full, 0x88980e8092dbull, 0x871f61969e8dull,
+    0x85aac367cc48ull, 0x843a28c3acdeull, 0x82cd8698ac2cull, 0x8164d1f3bc03ull
 };
+
+// A power as the larger 24 bits and the rest of 1 = 2^0, and as a whole number (minus what the magic numbers
+// below bring in).
+struct alignas(16) Power {
+  float hi, lo;
+  int64_t whole;
+};
+// 1.5 * 2^23: the low bits of a sum with it are the rounded number
+constexpr float kMagic = 12582912.f;
+constexpr int kMagicBits = 0x4b400000;
 
 // Weights of a row's logits.
 struct Weights {
   float M, ch, cl;                              // the maximum times `small`; log2(e) / (T small) = ch + cl
   float small;                                  // 1; 2^-90 where T is past 2^90: then M - x stays in range
   int q;                                        // a weight of 1 is 2^q
-  const uint64_t* table;
+  const Power* table;
 
   __device__ __forceinline__ uint64_t one() const { return (uint64_t)1 << q; }
   // z to fp32, never decreasing as x falls; infinite (or NaN, of an infinite T) for -inf
-  __device__ __forceinline__ float z_of(float x) const {
-    x *= small;
-    return x == M ? 0.f : (M - x) * ch;
-  }
+  __device__ __forceinline__ float z_of(float x) const { return (M - x * small) * ch; }
   __device__ __forceinline__ int bucket(float x) const { return (int)fminf(z_of(x) * kPerZ, (float)(kBuckets - 1)); }
   __device__ __forceinline__ uint64_t of(float x) const {
     x *= small;
-    if (x == M) return one();
-    const float d = M - x;
-    const float zh = d * ch;
-    if (!(zh < 63.f)) return 0;
+    const float d = M - x, zh = fminf(d * ch, 64.f);
     // d's rounding, and z in two parts
     const float b = d - M, de = (M - (d - b)) + (-x - b);
     const float zl = fmaf(de, ch, fmaf(d, cl, fmaf(d, ch, -zh)));
-    const float jf = rintf(zh * 64.f);
-    const float g = fmaf(jf, -1.f / 64.f, zh);  // exact, |g| <= 1/128
-    const int j = (int)jf;
-    const uint64_t ti = table[j & 63];
-    const float th = (float)(uint32_t)(ti >> 24) * 0x1p-23f, tl = (float)(uint32_t)(ti & 0xffffffu) * 0x1p-47f;
+    const float t = fmaf(zh, 64.f, kMagic);
+    const float g = fmaf(t - kMagic, -1.f / 64.f, zh);          // exact, |g| <= 1/128
+    const int j = __float_as_int(t) - kMagicBits;
+    const Power power = table[j & 63];
     // 2^-(g + zl) = e^-y, y = yh + yl
     constexpr float kLn2 = 0.693147182f, kLn2Lo = -1.904654323e-9f;
     const float yh = g * kLn2;
     const float yl = fmaf(zl, kLn2, fmaf(g, kLn2Lo, fmaf(g, kLn2, -yh)));
-    const float sq = yh * yh * fmaf(yh, fmaf(yh, 1.f / 24.f, -1.f / 6.f), 0.5f);
-    // T (1 - yh + (sq - yl)) - T, in two parts
-    const float p = th * yh;
-    const float e = sq - yl, r = fmaf(th, e, fmaf(tl, e, fmaf(-tl, yh, -fmaf(th, yh, -p))));
-    const int64_t v = (int64_t)ti - __float2ll_rn(p * 0x1p47f) + __float2ll_rn(r * 0x1p47f);
-    const int sh = (j >> 6) + kTableBits - q;
-    return sh > 60 ? 0 : sh == 0 ? (uint64_t)v : ((uint64_t)v + ((uint64_t)1 << (sh - 1))) >> sh;
+    const float e = fmaf(yh * yh, fmaf(yh, fmaf(yh, 1.f / 24.f, -1.f / 6.f), 0.5f), -yl);
+    // T (1 - yh + e) - T = r - p: whole numbers of 2^-29, and of 2^-37 of what they leave
+    const float p = power.hi * yh;
+    const float r = fmaf(power.hi, e, fmaf(power.lo, e, fmaf(-power.lo, yh, -fmaf(power.hi, yh, -p))));
+    const float t1 = fmaf(p, 0x1p29f, kMagic);
+    const float rest = r - fmaf(t1 - kMagic, -0x1p-29f, p);
+    const float t2 = fmaf(rest, 0x1p37f, kMagic);
+    const int64_t v = power.whole - (int64_t)__float_as_int(t1) * (1 << 19) + (int64_t)__float_as_int(t2) * (1 << 11);
+    // half a unit of what is left is added (q is below kTableBits); nothing is left of z above 63
+    const int sh = (j >> 6) + kTableBits - 1 - q;
+    return zh < 63.f && sh < 60 ? (((uint64_t)v >> sh) + 1) >> 1 : 0;
   }
 };
 
@@ -101,14 +117,17 @@ __device__ __forceinline__ float logit_of(uint32_t k) {
 }
 
 // What a row's blocks share.
-struct Shared {
-  uint64_t table[64];
+struct alignas(16) Shared {
+  Power table[64];
   uint64_t mass[2][kBuckets], mass_all[kBuckets];       // the block's, by turn; the cluster's
   uint32_t count[2][kBuckets], count_all[kBuckets];
   uint64_t warp_mass[kWarps];
   uint32_t warp_count[kWarps];
   uint64_t mine[8][2];                                  // what the block tells the others, by turn
   uint64_t found[4];
+  uint32_t listed;                                      // the block's tokens on the list
+  float factor[2];                                      // log2(e) / T
+  uint32_t list_key[kMostListed], list_index[kMostListed];
 };
 
 static_assert(sizeof(Shared) % 16 == 0, "the slice behind it is read in vectors");
@@ -154,24 +173,39 @@ __device__ __forceinline__ float element<__nv_bfloat16>(const uint8_t* data, int
   return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(data)[i] << 16);
 }
 
-// Calls f(x) for every element of vectors t, t + kThreads, ... of the slice.
+// Calls f(x, e) for elements e of the slice: of vectors v0, v0 + step, .. below v1.
 template <typename T, typename F>
-__device__ __forceinline__ void each(const uint8_t* data, int vecs, F f) {
+__device__ __forceinline__ void walk(const uint8_t* data, int v0, int v1, int step, F f) {
   constexpr int E = 16 / sizeof(T);
-  for (int v = threadIdx.x; v < vecs; v += kThreads) {
+  for (int v = v0; v < v1; v += step) {
     const uint4 w = reinterpret_cast<const uint4*>(data)[v];
     const uint32_t b[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      if constexpr (sizeof(T) == 4) f(__uint_as_float(b[i]));
-      else f(__uint_as_float(i & 1 ? b[i >> 1] & 0xffff0000u : b[i >> 1] << 16));
+      if constexpr (sizeof(T) == 4) f(__uint_as_float(b[i]), v * E + i);
+      else f(__uint_as_float(i & 1 ? b[i >> 1] & 0xffff0000u : b[i >> 1] << 16), v * E + i);
     }
   }
+}
+template <typename T, typename F>
+__device__ __forceinline__ void each(const uint8_t* data, int vecs, F f) {
+  walk<T>(data, threadIdx.x, vecs, kThreads, f);
 }
 
 __device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// Sum of x over the block.
+__device__ __forceinline__ uint64_t block_sum(Shared& sm, uint64_t x) {
+  x = warp_sum(x);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sm.warp_mass[threadIdx.x >> 5] = x;
+  __syncthreads();
+  x = 0;
+  for (int w = 0; w < kWarps; ++w) x += sm.warp_mass[w];
   return x;
 }
 
@@ -267,6 +301,24 @@ __device__ __forceinline__ void join_histogram(Row& row) {
   }
   __syncthreads();
 }
+// The same of histograms of counts alone.
+__device__ __forceinline__ void clear_counts(Row& row) {
+  row.turn ^= 1;
+  for (int i = threadIdx.x; i < kBuckets; i += kThreads) row.sm->count[row.turn][i] = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ void join_counts(Row& row) {
+  Shared& sm = *row.sm;
+  row.sync();
+  for (int i = threadIdx.x; i < kBuckets; i += kThreads) {
+    uint32_t n = row.C > 1 ? 0u : sm.count[row.turn][i];
+    if (row.C > 1)
+      for (int c = 0; c < row.C; ++c) n += row.read(&sm.count[row.turn][i], c);
+    sm.count_all[i] = n;
+    sm.mass_all[i] = 0;
+  }
+  __syncthreads();
+}
 // The first bucket at whose end the running count (or mass) reaches `need` (>= 1): its
 // index, and the count and mass before it; false if all together do not.
 struct Place {
@@ -324,7 +376,7 @@ __device__ __forceinline__ Cut find_cut(Row& row, const Weights& wt, const uint8
                                         uint64_t need, Place at, uint64_t& mass) {
   // the keys of the bucket
   uint64_t lo = 0, hi = 0;                      // as largest of ~key and of key
-  each<T>(data, vecs, [&](float x) {
+  each<T>(data, vecs, [&](float x, int) {
     if (x != -INFINITY && wt.bucket(x) == at.bucket) {
       const uint32_t k = key_of(x);
       hi = max(hi, (uint64_t)k);
@@ -335,11 +387,11 @@ __device__ __forceinline__ Cut find_cut(Row& row, const Weights& wt, const uint8
   mass = at.mass;
   uint64_t count = at.count;
   Shared& sm = *row.sm;
-  for (;;) {
+  for (int turn = 0; turn < 40; ++turn) {       // (each at least halves the range of 32-bit keys)
     const int bits = 32 - __clz((int)(top - low) | 1);
     const int shift = bits > 10 ? bits - 10 : 0;
     clear_histogram(row);
-    each<T>(data, vecs, [&](float x) {
+    each<T>(data, vecs, [&](float x, int) {
       const uint32_t k = key_of(x);
       if (k >= low && k <= top) {
         const uint32_t b = (top - k) >> shift;
@@ -364,6 +416,266 @@ __device__ __forceinline__ Cut find_cut(Row& row, const Weights& wt, const uint8
     const uint32_t width = (1u << shift) - 1u;
     low = top - low > width ? top - width : low;
   }
+  return Cut{low, 0xffffffffu};
+}
+
+// The row's answer: token `at` of weight w among kept weights `total`.
+__device__ __forceinline__ void write_token(const Weights& wt, uint32_t at, uint64_t w, uint64_t total, float z,
+                                            int32_t* token, float* logprob) {
+  *token = (int32_t)at;
+  if (!logprob) return;
+  const float total_f = (float)total, rest = (float)(total - w) / total_f;
+  if (rest < 0.5f) *logprob = log1pf(-rest);
+  else if (w >= (1u << 26)) *logprob = logf((float)w / total_f);
+  else *logprob = -z - logf(total_f * exp2f(-(float)wt.q));
+}
+
+// Buckets that can hold the end of the first tokens whose weights reach the share p of all,
+// from the counts of the buckets: a bucket's weights lie between 2^-(b + 1) / 16 and 2^-b / 16.
+// The share reached at a bucket's end is largest where its tokens and those before weigh
+// most and the others least.
+__device__ __forceinline__ int2 share_buckets(Row& row, float p) {
+  Shared& sm = *row.sm;
+  constexpr int per = kBuckets / kThreads;
+  constexpr float kRoom = 1e-4f;                // (more than z's and the sums' rounding)
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float lo[per], hi[per], ls = 0.f, hs = 0.f;
+#pragma unroll
+  for (int i = 0; i < per; ++i) {
+    const int b = threadIdx.x * per + i;
+    const float n = (float)sm.count_all[b];
+    lo[i] = n * tc::ex2(-(float)(b + 1) / kPerZ);
+    hi[i] = n * tc::ex2(-(float)b / kPerZ);
+    ls += lo[i];
+    hs += hi[i];
+  }
+  const float il = scan_warp(ls), ih = scan_warp(hs);
+  float2* word = reinterpret_cast<float2*>(sm.warp_mass);
+  __syncthreads();
+  if (lane == 31) word[warp] = make_float2(il, ih);
+  if (threadIdx.x == 0) sm.warp_count[0] = sm.warp_count[1] = kBuckets - 1;
+  __syncthreads();
+  float bl = il - ls, bh = ih - hs, tl = 0.f, th = 0.f;
+  for (int w = 0; w < kWarps; ++w) {
+    const float2 v = word[w];
+    if (w < warp) {
+      bl += v.x;
+      bh += v.y;
+    }
+    tl += v.x;
+    th += v.y;
+  }
+#pragma unroll
+  for (int i = 0; i < per; ++i) {
+    bl += lo[i];
+    bh += hi[i];
+    if (bh >= (p - kRoom) * (bh + fmaxf(tl - bl, 0.f))) atomicMin(&sm.warp_count[0], (uint32_t)(threadIdx.x * per + i));
+    if (bl >= (p + kRoom) * (bl + fmaxf(th - bh, 0.f))) atomicMin(&sm.warp_count[1], (uint32_t)(threadIdx.x * per + i));
+  }
+  __syncthreads();
+  const int2 b = make_int2((int)sm.warp_count[0], (int)sm.warp_count[1]);
+  __syncthreads();
+  return b;
+}
+
+// floor(x * total) of an fp32 x in [0, 1) and a total below 2^62, exactly (fp64 is slow here); `rest`: whether
+// something was cut off.
+__device__ __forceinline__ uint64_t times(float x, uint64_t total, bool& rest) {
+  const uint32_t b = __float_as_uint(x);
+  const int s = 150 - (int)(b >> 23);           // x = m 2^-s
+  const uint64_t m = (b & 0x7fffffu) | 0x800000u, lo = total * m, hi = __umul64hi(total, m);
+  rest = x > 0.f;
+  if (!(x > 0.f) || s >= 128 || s > 149) return 0;      // (below 2^-126 times 2^62)
+  if (s >= 64) {
+    rest = lo != 0 || (s > 64 && (hi & (((uint64_t)1 << (s - 64)) - 1)) != 0);
+    return hi >> (s - 64);
+  }
+  rest = (lo & (((uint64_t)1 << s) - 1)) != 0;
+  return hi << (64 - s) | lo >> s;
+}
+// Where a token is drawn: running sum > u * total.
+__device__ __forceinline__ uint64_t target_of(float u, uint64_t total) {
+  bool rest;
+  return u >= 1.f ? total - 1 : min(total - 1, times(u, total, rest));
+}
+// top_p of the weights `total`, in whole numbers, at least 1.
+__device__ __forceinline__ uint64_t share_of(float p, uint64_t total) {
+  bool rest = false;
+  const uint64_t x = times(fmaxf(p, 0.f), total, rest);
+  return min(total, max((uint64_t)1, x + (rest ? 1 : 0)));
+}
+
+// The cut where the weights of the keys in [low, top], the largest first, reach `need`.
+template <typename T>
+__device__ __forceinline__ Cut narrow(Row& row, const Weights& wt, const uint8_t* data, int vecs, uint32_t top,
+                                      uint32_t low, uint64_t need) {
+  Shared& sm = *row.sm;
+  for (int turn = 0; turn < 40; ++turn) {       // (each at least halves the range of 32-bit keys)
+    const int bits = 32 - __clz((int)(top - low) | 1);
+    const int shift = bits > 10 ? bits - 10 : 0;
+    const uint32_t width = (1u << shift) - 1u;
+    clear_counts(row);
+    each<T>(data, vecs, [&](float x, int) {
+      const uint32_t k = key_of(x);
+      if (k >= low && k <= top) atomicAdd(&sm.count[row.turn][(top - k) >> shift], 1u);
+    });
+    join_counts(row);
+    // bounds of the bins' weights (single keys: the weights themselves); find_place ends with a barrier
+    auto fill = [&](bool upper) {
+      for (int b = threadIdx.x; b < kBuckets; b += kThreads) {
+        const uint64_t n = sm.count_all[b];
+        if (n == 0) continue;
+        const uint32_t first = top - ((uint32_t)b << shift), last = first - low > width ? first - width : low;
+        const uint64_t w = wt.of(logit_of(upper ? first : last)), room = shift > 0 ? (w >> 30) + 1 : 0;
+        sm.mass_all[b] = n * (upper ? w + room : w - min(w, room));
+      }
+      __syncthreads();
+    };
+    Place p, q;
+    fill(true);
+    if (!find_place(row, true, need, p)) return Cut{low, 0xffffffffu};  // (all of them: not by the bounds)
+    if (shift == 0) {
+      Cut cut;
+      cut.key = top - (uint32_t)p.bucket;
+      const uint64_t w = wt.of(logit_of(cut.key));
+      cut.ties = (uint32_t)((need - p.mass + w - 1) / w);
+      return cut;
+    }
+    // the cut lies in bins p .. q; where that is more than one, it is looked for by the weights themselves:
+    // in bin p, in the bins up to the middle, or in the rest, so every turn at least halves the range
+    fill(false);
+    const int end = find_place(row, true, need, q) ? max(q.bucket, p.bucket) : kBuckets - 1, mid = (p.bucket + end) >> 1;
+    auto last_of = [&](int b) {
+      const uint32_t at = top - ((uint32_t)b << shift);
+      return (uint32_t)b << shift > top - low || at - low < width ? low : at - width;
+    };
+    const uint32_t p_first = top - ((uint32_t)p.bucket << shift), p_last = last_of(p.bucket), m_last = last_of(mid),
+                   e_last = last_of(end);
+    uint64_t m0 = 0, m1 = 0, m2 = 0;
+    each<T>(data, vecs, [&](float x, int) {
+      const uint32_t k = key_of(x);
+      if (k > top || k < m_last) return;
+      const uint64_t w = wt.of(x);
+      if (k > p_first) m0 += w;
+      else if (k >= p_last) m1 += w;
+      else m2 += w;
+    });
+    m0 = cluster_sum(row, m0, nullptr);
+    need = need > m0 ? need - m0 : 1;
+    top = p_first;
+    uint32_t to = p_last;
+    if (end > p.bucket) {
+      m1 = cluster_sum(row, m1, nullptr);
+      if (need > m1) {
+        need -= m1;
+        m2 = cluster_sum(row, m2, nullptr);
+        to = m_last;
+        if (mid > p.bucket && need <= m2) {
+          top = p_last - 1;
+        } else {
+          need = need > m2 ? need - m2 : 1;
+          if (m_last == low) return Cut{low, 0xffffffffu};            // (nothing is left: all of them)
+          top = m_last - 1;
+          to = e_last;
+        }
+      }
+    }
+    low = max(low, to);
+  }
+  return Cut{low, 0xffffffffu};
+}
+
+// What the filters keep of the tokens in buckets up to `upto`, on a list of rank 0, and the
+// token; `total`: the weights of which top_p is a share where there is no top_k.
+template <typename T>
+__device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uint8_t* data, int vecs, int index0,
+                                          int upto, uint32_t k, bool by_p, float p, uint64_t total, uint64_t least,
+                                          float u, int32_t* token, float* logprob) {
+  Shared& sm = *row.sm;
+  const int t = threadIdx.x;
+  if (t == 0) sm.listed = 0;
+  __syncthreads();
+  each<T>(data, vecs, [&](float x, int e) {
+    if (wt.z_of(x) * kPerZ < (float)(upto + 1)) {
+      const uint32_t at = atomicAdd(&sm.listed, 1u);
+      sm.list_key[at] = key_of(x);
+      sm.list_index[at] = (uint32_t)(index0 + e);
+    }
+  });
+  row.sync();
+  if (row.rank != 0) return;
+  uint32_t n = sm.listed;
+  for (int c = 1; c < row.C; ++c) {
+    const uint32_t m = row.read(&sm.listed, c);
+    for (uint32_t i = t; i < m; i += kThreads) {
+      sm.list_key[n + i] = row.read(&sm.list_key[i], c);
+      sm.list_index[n + i] = row.read(&sm.list_index[i], c);
+    }
+    n += m;
+  }
+  __syncthreads();
+  // in order: a token's place is the number of those before it
+  uint64_t* weight = sm.mass[0];
+  uint64_t* upto_sum = sm.mass[1];
+  uint32_t *index = sm.count[0], *key_in_order = sm.count[1];
+  constexpr int per = kMostListed / kThreads;
+  static_assert(kMostListed <= kBuckets, "the histograms' words hold the list in order");
+#pragma unroll
+  for (int i = 0; i < per; ++i) {
+    const uint32_t me = t + i * kThreads;
+    if (me >= n) break;
+    const uint32_t key = sm.list_key[me], at = sm.list_index[me];
+    uint32_t rank = 0;
+    for (uint32_t j = 0; j < n; ++j) {
+      const uint32_t o = sm.list_key[j];
+      rank += o > key || (o == key && sm.list_index[j] < at) ? 1u : 0u;
+    }
+    weight[rank] = wt.of(logit_of(key));
+    index[rank] = at;
+    key_in_order[rank] = key;
+  }
+  __syncthreads();
+  const uint32_t nk = min(n, k);
+  uint64_t mine[per], sum = 0;
+#pragma unroll
+  for (int i = 0; i < per; ++i) {
+    const uint32_t r = t * per + i;
+    mine[i] = r < nk ? weight[r] : 0;
+    sum += mine[i];
+  }
+  const uint64_t incl = scan_warp(sum);
+  if ((t & 31) == 31) sm.warp_mass[t >> 5] = incl;
+  if (t == 0) sm.found[0] = sm.found[1] = nk;
+  __syncthreads();
+  uint64_t before = incl - sum, all = 0;
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < (t >> 5)) before += sm.warp_mass[w];
+    all += sm.warp_mass[w];
+  }
+  const uint64_t need = by_p ? share_of(p, total != 0 ? total : all) : 0;
+#pragma unroll
+  for (int i = 0; i < per; ++i) {
+    const uint32_t r = t * per + i;
+    const uint64_t from = before;
+    before += mine[i];
+    if (r < nk) {
+      upto_sum[r] = before;
+      // the first to reach top_p's share, and the first below min_p (at least one stays)
+      if (by_p && from < need && need <= before) sm.found[0] = r + 1;
+      if (r > 0 && weight[r] < least && weight[r - 1] >= least) sm.found[1] = r;
+    }
+  }
+  __syncthreads();
+  const uint32_t kept = (uint32_t)min(sm.found[0], sm.found[1]);
+  const uint64_t sum_kept = upto_sum[kept - 1];
+  const uint64_t target = target_of(u, sum_kept);
+  for (uint32_t r = t; r < kept; r += kThreads) {
+    const uint32_t at = index[r];
+    uint64_t cum = 0;
+    for (uint32_t j = 0; j < kept; ++j) cum += index[j] <= at ? weight[j] : 0;
+    if (target < cum && target >= cum - weight[r])
+      write_token(wt, at, weight[r], sum_kept, wt.z_of(logit_of(key_in_order[r])) * 0.693147182f, token, logprob);
+  }
 }
 
 template <typename T>
@@ -380,7 +692,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   row.told = 0;
   row.sm = &sm;
   const int r = (int)blockIdx.x / a.C;
-  if (t < 64) sm.table[t] = kPowers[t];
+  if (t < 64) {
+    const uint64_t x = kPowers[t];
+    sm.table[t] = {(float)(uint32_t)(x >> 25) * 0x1p-23f, (float)(uint32_t)(x & 0x1ffffffu) * 0x1p-48f,
+                   (int64_t)x + ((int64_t)kMagicBits << 19) - ((int64_t)kMagicBits << 11)};
+  }
 
   // (1) the slice: vectors of 16 bytes from the row's first byte rounded down; what is not
   // the row's, and NaN, as -inf
@@ -389,162 +705,229 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   const int all_vecs = (a0 + (int)a.vocab + E - 1) / E;
   const int first = row.rank * a.vecs, vecs = max(0, min(a.vecs, all_vecs - first));
   float M = -INFINITY;
-  for (int v = t; v < vecs; v += kThreads) {
-    const int e0 = (first + v) * E - a0;        // element of the vector's start
+  auto edge = [&](int e0) {                     // a vector that is not all the row's
     uint4 w;
     uint32_t* b = reinterpret_cast<uint32_t*>(&w);
-    if (e0 >= 0 && e0 + E <= a.vocab) {
-      w = __ldg(reinterpret_cast<const uint4*>(x0 + e0));
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        b[i] = e0 + i >= 0 && e0 + i < a.vocab ? __float_as_uint((float)x0[e0 + i]) : 0xff800000u;
     } else {
-      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          b[i] = e0 + i >= 0 && e0 + i < a.vocab ? __float_as_uint((float)x0[e0 + i]) : 0xff800000u;
-      } else {
+      for (int i = 0; i < 4; ++i) {
+        uint32_t h[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t h[2];
+        for (int k = 0; k < 2; ++k) {
+          const int e = e0 + 2 * i + k;
+          h[k] = e >= 0 && e < a.vocab ? (uint32_t)reinterpret_cast<const uint16_t*>(x0)[e] : 0xff80u;
+        }
+        b[i] = h[0] | h[1] << 16;
+      }
+    }
+    return w;
+  };
+  constexpr int kLoads = 4;                     // vectors of a thread in flight
+  for (int vb = t; vb < vecs; vb += kLoads * kThreads) {
+    uint4 w[kLoads];
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int e = e0 + 2 * i + k;
-            h[k] = e >= 0 && e < a.vocab ? (uint32_t)reinterpret_cast<const uint16_t*>(x0)[e] : 0xff80u;
-          }
-          b[i] = h[0] | h[1] << 16;
+    for (int n = 0; n < kLoads; ++n) {
+      const int v = vb + n * kThreads, e0 = (first + v) * E - a0;     // element of the vector's start
+      if (v < vecs && e0 >= 0 && e0 + E <= a.vocab) w[n] = __ldg(reinterpret_cast<const uint4*>(x0 + e0));
+    }
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int v = vb + n * kThreads, e0 = (first + v) * E - a0;
+      if (v >= vecs) break;
+      if (!(e0 >= 0 && e0 + E <= a.vocab)) w[n] = edge(e0);
+      uint32_t b[4] = {w[n].x, w[n].y, w[n].z, w[n].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          if ((b[i] & 0x7fffffffu) > 0x7f800000u) b[i] = 0xff800000u;
+          M = fmaxf(M, __uint_as_float(b[i]));
+        } else {
+          if ((b[i] & 0x7fffu) > 0x7f80u) b[i] = (b[i] & 0xffff0000u) | 0xff80u;
+          if ((b[i] & 0x7fff0000u) > 0x7f800000u) b[i] = (b[i] & 0xffffu) | 0xff800000u;
+          M = fmaxf(M, fmaxf(__uint_as_float(b[i] << 16), __uint_as_float(b[i] & 0xffff0000u)));
         }
       }
+      reinterpret_cast<uint4*>(data)[v] = make_uint4(b[0], b[1], b[2], b[3]);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(T) == 4) {
-        if ((b[i] & 0x7fffffffu) > 0x7f800000u) b[i] = 0xff800000u;
-        M = fmaxf(M, __uint_as_float(b[i]));
-      } else {
-        if ((b[i] & 0x7fffu) > 0x7f80u) b[i] = (b[i] & 0xffff0000u) | 0xff80u;
-        if ((b[i] & 0x7fff0000u) > 0x7f800000u) b[i] = (b[i] & 0xffffu) | 0xff800000u;
-        M = fmaxf(M, fmaxf(__uint_as_float(b[i] << 16), __uint_as_float(b[i] & 0xffff0000u)));
-      }
-    }
-    reinterpret_cast<uint4*>(data)[v] = w;
   }
-  M = logit_of((uint32_t)cluster_max(row, key_of(M)));
   const float temp = __ldg(a.temperature + r);
   const bool greedy = !(temp > 0.f);
   Weights wt;
   wt.small = temp > 0x1p90f ? 0x1p-90f : 1.f;
+  if (t == 0) {
+    // (one thread: fp64 is slow here; the maximum's barriers come before it is read)
+    const double c = greedy ? 0.0 : 1.4426950408889634074 / ((double)temp * (double)wt.small);
+    // (a T so small that the factor is no fp32 number: 0 times it has to be 0)
+    sm.factor[0] = c < 3e38 ? (float)c : 3e38f;
+    sm.factor[1] = c < 3e38 ? (float)(c - (double)(float)c) : 0.f;
+  }
+  M = logit_of((uint32_t)cluster_max(row, key_of(M)));
+  if (M == INFINITY) {
+    // these share everything: 0 for them, nothing for the others
+    for (int v = t; v < vecs; v += kThreads) {
+      uint4 w = reinterpret_cast<uint4*>(data)[v];
+      uint32_t b[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) b[i] = b[i] == 0x7f800000u ? 0u : 0xff800000u;
+        else b[i] = ((b[i] & 0xffffu) == 0x7f80u ? 0u : 0xff80u) | (b[i] >> 16 == 0x7f80u ? 0u : 0xff800000u);
+      }
+      reinterpret_cast<uint4*>(data)[v] = make_uint4(b[0], b[1], b[2], b[3]);
+    }
+    M = 0.f;
+    __syncthreads();
+  }
   wt.M = M * wt.small;
   wt.q = a.q;
   wt.table = sm.table;
-  {
-    const double c = greedy ? 0.0 : 1.4426950408889634074 / ((double)temp * (double)wt.small);
-    wt.ch = (float)c;
-    wt.cl = isinf(wt.ch) ? 0.f : (float)(c - (double)wt.ch);
-  }
+  wt.ch = sm.factor[0];
+  wt.cl = sm.factor[1];
   const int32_t k = a.top_k ? __ldg(a.top_k + r) : 0;
   const float p = a.top_p ? __ldg(a.top_p + r) : 1.f;
   const float mp = a.min_p ? __ldg(a.min_p + r) : 0.f;
   float u = __ldg(a.u + r);
   u = u > 0.f ? u : 0.f;
 
-  // (2), (3) the cuts
-  Cut cut_k = {0u, 0xffffffffu}, cut_p = {0u, 0xffffffffu};
+  // the cuts
   uint64_t least = 1;                           // weights below it are not kept
-  if (mp > 0.f) least = max((uint64_t)1, (uint64_t)__double2ull_rn((double)fminf(mp, 1.f) * (double)wt.one()));
-  const bool by_k = !greedy && k > 0 && k < a.vocab, by_p = !greedy && p < 1.f;
+  if (mp > 0.f) least = max((uint64_t)1, (uint64_t)__float2ull_rn(fminf(mp, 1.f) * (float)wt.one()));
+  const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.f;
+  // runs of tokens: thread t has vectors [t * run, t * run + run) of the slice
+  const int run = ((a.vecs + kThreads - 1) / kThreads) | 1;       // (odd: lanes on different banks)
+  const int v0 = min(t * run, vecs), v1 = min(v0 + run, vecs), index0 = first * E - a0;
+  int32_t* const token = a.token + r;
+  float* const logprob = a.logprob ? a.logprob + r : nullptr;
   if (M == -INFINITY) {
     if (row.rank == 0 && t == 0) {
-      a.token[r] = -1;
-      if (a.logprob) a.logprob[r] = __uint_as_float(0x7fffffffu);
+      *token = -1;
+      if (logprob) *logprob = __uint_as_float(0x7fffffffu);
+    }
+  } else if (greedy) {
+    // the first of the largest
+    uint64_t best = 0;
+    walk<T>(data, v0, v1, 1, [&](float x, int e) {
+      if (x == M) best = max(best, (uint64_t)(0xffffffffull - (uint32_t)(index0 + e)));
+    });
+    best = cluster_max(row, best);
+    if (row.rank == 0 && t == 0) {
+      *token = (int32_t)(0xffffffffull - best);
+      if (logprob) *logprob = 0.f;
     }
   } else {
+    Cut cut_k = {0u, 0xffffffffu}, cut_p = {0u, 0xffffffffu};
+    bool done = false, have_sum = false;
+    uint64_t sum = 0;                           // kept weights of the run
+    uint32_t top = 0;                           // with have_sum: those of keys above it
     if (by_k || by_p) {
-      clear_histogram(row);
-      each<T>(data, vecs, [&](float x) {
-        const uint64_t w = wt.of(x);
-        if (w != 0) {
-          const int b = wt.bucket(x);
-          atomicAdd(&sm.count[row.turn][b], 1u);
-          atomicAdd(reinterpret_cast<unsigned long long*>(&sm.mass[row.turn][b]), (unsigned long long)w);
-        }
+      clear_counts(row);
+      each<T>(data, vecs, [&](float x, int) {
+        const float z = wt.z_of(x) * kPerZ;
+        if (z < (float)(kBuckets - 1)) atomicAdd(&sm.count[row.turn][(int)z], 1u);      // (beyond: no weight)
       });
-      join_histogram(row);
-      uint64_t mass = 0, part = 0;
-      // (the total: need it before the histogram is overwritten)
-      for (int i = t; i < kBuckets; i += kThreads) part += sm.mass_all[i];
-      part = warp_sum(part);
-      __syncthreads();
-      if (lane == 0) sm.warp_mass[t >> 5] = part;
-      __syncthreads();
-      for (int w = 0; w < kWarps; ++w) mass += sm.warp_mass[w];
-      __syncthreads();
-      Place pk, pp;
+      join_counts(row);
+      Place pk;
       const bool cut_by_k = by_k && find_place(row, false, (uint64_t)k, pk);
-      // top-p alone: its place on the same histogram
-      auto need_of = [&](uint64_t total) {
-        const double x = ceil((double)fmaxf(p, 0.f) * (double)total);
-        return min(total, max((uint64_t)1, (uint64_t)x));
-      };
       if (cut_by_k) {
-        // (top-p's bucket lies at top-k's or before it: the histogram is kept in registers' stead by a second look)
-        cut_k = find_cut<T>(row, wt, data, vecs, false, (uint64_t)k, pk, mass);
-        if (by_p) {
-          clear_histogram(row);
-          each<T>(data, vecs, [&](float x) {
-            if (key_of(x) >= cut_k.key) {
-              const uint64_t w = wt.of(x);
-              const int b = wt.bucket(x);
-              atomicAdd(&sm.count[row.turn][b], 1u);
-              atomicAdd(reinterpret_cast<unsigned long long*>(&sm.mass[row.turn][b]), (unsigned long long)w);
-            }
-          });
-          join_histogram(row);
+        if (pk.count + sm.count_all[pk.bucket] <= kMostListed) {
+          from_list<T>(row, wt, data, vecs, index0, pk.bucket, (uint32_t)k, by_p, p, 0, least, u, token, logprob);
+          done = true;
+        } else {
+          uint64_t mass = 0;
+          pk.mass = 0;
+          cut_k = find_cut<T>(row, wt, data, vecs, false, (uint64_t)k, pk, mass);
+          if (by_p) {
+            uint64_t kept = 0, unused, tie0;    // all that top-k keeps
+            uint32_t ties = 0;
+            walk<T>(data, v0, v1, 1, [&](float x, int) { ties += key_of(x) == cut_k.key ? 1u : 0u; });
+            cluster_sum(row, ties, &tie0);
+            walk<T>(data, v0, v1, 1, [&](float x, int) {
+              const uint32_t key = key_of(x);
+              if (key > cut_k.key || (key == cut_k.key && tie0++ < cut_k.ties)) kept += wt.of(x);
+            });
+            kept = cluster_sum(row, kept, nullptr);
+            clear_histogram(row);
+            each<T>(data, vecs, [&](float x, int) {
+              if (key_of(x) >= cut_k.key) {
+                const uint64_t w = wt.of(x);
+                const int b = wt.bucket(x);
+                atomicAdd(&sm.count[row.turn][b], 1u);
+                atomicAdd(reinterpret_cast<unsigned long long*>(&sm.mass[row.turn][b]), (unsigned long long)w);
+              }
+            });
+            join_histogram(row);
+            const uint64_t need = share_of(p, kept);
+            Place pp;
+            if (find_place(row, true, need, pp)) cut_p = find_cut<T>(row, wt, data, vecs, true, need, pp, unused);
+          }
         }
-      }
-      if (by_p) {
-        const uint64_t need = need_of(mass);
-        uint64_t unused;
-        if (find_place(row, true, need, pp)) cut_p = find_cut<T>(row, wt, data, vecs, true, need, pp, unused);
+      } else if (by_p) {
+        const int2 b = share_buckets(row, p);
+        uint64_t n = 0, total = 0, above = 0, hi = 0, lo = 0;
+        for (int i = t; i <= b.y; i += kThreads) n += sm.count_all[i];
+        n = block_sum(sm, n);
+        const bool few = n <= kMostListed;
+        // all weights, those before the cut's buckets, and the keys of those buckets
+        walk<T>(data, v0, v1, 1, [&](float x, int) {
+          const uint64_t w = wt.of(x);
+          total += w;
+          if (few || w == 0) return;
+          const float z = wt.z_of(x) * kPerZ;
+          if (z < (float)b.x) {
+            above += w;
+            sum += w >= least ? w : 0;
+          } else if (z < (float)(b.y + 1)) {
+            hi = max(hi, (uint64_t)key_of(x));
+            lo = max(lo, (uint64_t)(~key_of(x)));
+          }
+        });
+        total = cluster_sum(row, total, nullptr);
+        if (few) {
+          from_list<T>(row, wt, data, vecs, index0, b.y, 0xffffffffu, true, p, total, least, u, token, logprob);
+          done = true;
+        } else {
+          above = cluster_sum(row, above, nullptr);
+          const uint64_t need = share_of(p, total);
+          top = (uint32_t)cluster_max(row, hi);
+          cut_p = narrow<T>(row, wt, data, vecs, top, ~(uint32_t)cluster_max(row, lo), need > above ? need - above : 1);
+          have_sum = true;
+        }
       }
     }
-    // (4) runs of tokens: thread t has vectors [t * run, t * run + run) of the slice
-    const int run = ((a.vecs + kThreads - 1) / kThreads) | 1;     // (odd: lanes on different banks)
-    const int v0 = min(t * run, vecs), v1 = min(v0 + run, vecs);
-    const uint32_t ck = max(cut_k.key, cut_p.key);
-    // tokens equal to the cut's logit that stay: of the two cuts the one that keeps fewer
-    uint32_t ties = 0xffffffffu;
-    if (cut_k.key == ck) ties = min(ties, cut_k.ties);
-    if (cut_p.key == ck) ties = min(ties, cut_p.ties);
-    uint64_t tie0 = 0;                          // such tokens in front of the run
-    if (greedy) {
-      // the first of the largest
-      uint64_t best = 0;
-      for (int e = v0 * E; e < v1 * E && best == 0; ++e)
-        if (element<T>(data, e) == M) best = 0xffffffffull - (uint32_t)(first * E - a0 + e);
-      best = cluster_max(row, best);
-      if (row.rank == 0 && t == 0) {
-        a.token[r] = (int32_t)(0xffffffffull - best);
-        if (a.logprob) a.logprob[r] = 0.f;
-      }
-    } else {
+    if (!done) {
+      const uint32_t ck = max(cut_k.key, cut_p.key);
+      // tokens equal to the cut's logit that stay: of the two cuts the one that keeps fewer
+      uint32_t ties = 0xffffffffu;
+      if (cut_k.key == ck) ties = min(ties, cut_k.ties);
+      if (cut_p.key == ck) ties = min(ties, cut_p.ties);
+      uint64_t tie0 = 0;                        // such tokens in front of the run
       if (ties != 0xffffffffu) {
         uint32_t n = 0;
-        for (int e = v0 * E; e < v1 * E; ++e) n += key_of(element<T>(data, e)) == ck ? 1u : 0u;
+        walk<T>(data, v0, v1, 1, [&](float x, int) { n += key_of(x) == ck ? 1u : 0u; });
         cluster_sum(row, n, &tie0);
       }
-      auto weight = [&](int e, uint64_t& tie) -> uint64_t {
-        const float x = element<T>(data, e);
+      auto weight = [&](float x, uint64_t& tie) -> uint64_t {
         const uint32_t key = key_of(x);
         if (key < ck) return 0;
         if (key == ck && tie++ >= ties) return 0;
         const uint64_t w = wt.of(x);
         return w >= least ? w : 0;
       };
-      uint64_t sum = 0, tie = tie0;
-      for (int e = v0 * E; e < v1 * E; ++e) sum += weight(e, tie);
-      uint64_t before;
+      uint64_t tie = tie0, before;
+      if (have_sum)
+        walk<T>(data, v0, v1, 1, [&](float x, int) {
+          if (key_of(x) <= top) sum += weight(x, tie);
+        });
+      else if (ck == 0 && least == 1)
+        walk<T>(data, v0, v1, 1, [&](float x, int) { sum += wt.of(x); });
+      else
+        walk<T>(data, v0, v1, 1, [&](float x, int) { sum += weight(x, tie); });
       const uint64_t total = cluster_sum(row, sum, &before);
       // running sum > u * total, in whole numbers
-      uint64_t target = (uint64_t)((double)u * (double)total);
-      if (u >= 1.f || target >= total) target = total - 1;
+      const uint64_t target = target_of(u, total);
       const bool mine = before <= target && target < before + sum;
       const uint32_t who = __ballot_sync(0xffffffffu, mine);
       if (who) {
@@ -554,29 +937,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         uint64_t at = __shfl_sync(0xffffffffu, before, src), seen = __shfl_sync(0xffffffffu, tie0, src);
         for (int e0 = b0; e0 < b1; e0 += 32) {
           const int e = e0 + lane;
-          const bool tied = e < b1 && key_of(element<T>(data, e)) == ck;
-          const uint32_t tied_all = __ballot_sync(0xffffffffu, tied);
-          uint64_t rank = seen + __popc(tied_all & ((1u << lane) - 1u));
-          const uint64_t w = e < b1 ? weight(e, rank) : 0;
+          const float x = e < b1 ? element<T>(data, e) : -INFINITY;
+          const uint32_t tied = __ballot_sync(0xffffffffu, e < b1 && key_of(x) == ck);
+          uint64_t rank = seen + __popc(tied & ((1u << lane) - 1u));
+          const uint64_t w = e < b1 ? weight(x, rank) : 0;
           const uint64_t upto = at + scan_warp(w);
           const uint32_t hit = __ballot_sync(0xffffffffu, upto > target);
           if (hit) {
-            if (lane == __ffs(hit) - 1) {
-              a.token[r] = first * E - a0 + e;
-              if (a.logprob) {
-                const float x = element<T>(data, e);
-                const float total_f = (float)total, rest = (float)(total - w) / total_f;
-                float lp;
-                if (rest < 0.5f) lp = log1pf(-rest);
-                else if (w >= (1u << 26)) lp = logf((float)w / total_f);
-                else lp = (float)(-((double)M - (double)x) / (double)temp) - logf(total_f * exp2f(-(float)wt.q));
-                a.logprob[r] = lp;
-              }
-            }
+            if (lane == __ffs(hit) - 1)
+              write_token(wt, (uint32_t)(index0 + e), w, total, wt.z_of(x) * 0.693147182f, token, logprob);
             break;
           }
           at = __shfl_sync(0xffffffffu, upto, 31);
-          seen += __popc(tied_all);
+          seen += __popc(tied);
         }
       }
     }
@@ -592,7 +965,7 @@ cudaError_t launch_t(SampleArgs a, int64_t n_rows, cudaStream_t st) {
   // blocks of a row: so many that a slice leaves room for a second block on the SM, and
   // that few rows use the device
   int C = 1;
-  while (C < 8 && ((vecs + C - 1) / C * 16 > 64 * 1024 || (n_rows * C < kv8_sm_count() && vecs / C > 2 * kThreads))) C *= 2;
+  while (C < 8 && ((vecs + C - 1) / C * 16 > 66 * 1024 || (n_rows * C < kv8_sm_count() && vecs / C > 2 * kThreads))) C *= 2;
   a.C = C;
   a.vecs = (int)((vecs + C - 1) / C);
   const size_t smem = sizeof(Shared) + (size_t)a.vecs * 16;
