@@ -42,6 +42,7 @@ constexpr int kBuckets = 1024;
 constexpr float kPerZ = 16.f;                   // buckets of 1 in z: z < 64
 constexpr int kTableBits = 48;
 constexpr int kMostListed = 1024;
+constexpr int kMostBlocks = 8;                  // of a row
 
 // 2^(48 - i / 64), rounded
 __constant__ uint64_t kPowers[64] = {
@@ -107,12 +108,15 @@ struct Weights {
   }
 };
 
-// Orders like the logit.
+// Orders like the logit: 32 bits, or 16 of a bf16 number.
+template <typename T>
 __device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __float_as_uint(x + 0.f);
-  return b >> 31 ? ~b : b | 0x80000000u;
+  const uint32_t b = __float_as_uint(x + 0.f), k = b >> 31 ? ~b : b | 0x80000000u;
+  return sizeof(T) == 4 ? k : k >> 16;
 }
+template <typename T>
 __device__ __forceinline__ float logit_of(uint32_t k) {
+  if (sizeof(T) == 2) k = k << 16 | (k >> 15 ? 0u : 0xffffu);
   return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k);
 }
 
@@ -123,10 +127,10 @@ struct alignas(16) Shared {
   uint32_t count[2][kBuckets], count_all[kBuckets];
   uint64_t warp_mass[kWarps];
   uint32_t warp_count[kWarps];
-  uint64_t mine[8][2];                                  // what the block tells the others, by turn
+  uint64_t words[kWarps][3];
+  uint64_t mine[8][4];                                  // what the block tells the others, by turn
   uint64_t found[4];
   uint32_t listed;                                      // the block's tokens on the list
-  float factor[2];                                      // log2(e) / T
   uint32_t list_key[kMostListed], list_index[kMostListed];
 };
 
@@ -230,13 +234,10 @@ __device__ __forceinline__ uint64_t cluster_sum(Row& row, uint64_t x, uint64_t* 
     ++row.told;
     if (threadIdx.x == 0) *word = sum;
     row.sync();
-    uint64_t all = 0;
-    for (int c = 0; c < row.C; ++c) {
-      const uint64_t v = row.read(word, c);
-      if (c < row.rank) b += v;
-      all += v;
-    }
-    sum = all;
+    // (a lane a block: one latency)
+    const uint64_t v = lane < row.C ? row.read(word, lane) : 0;
+    sum = warp_sum(v);
+    b += warp_sum(lane < row.rank ? v : 0);
   }
   if (before) *before = b;
   return sum;
@@ -262,12 +263,59 @@ __device__ __forceinline__ uint64_t cluster_max(Row& row, uint64_t x) {
     ++row.told;
     if (threadIdx.x == 0) *word = x;
     row.sync();
-    for (int c = 0; c < row.C; ++c) {
-      const uint64_t y = row.read(word, c);
+    x = lane < row.C ? row.read(word, lane) : 0;
+#pragma unroll
+    for (int o = kMostBlocks / 2; o > 0; o >>= 1) {
+      const uint64_t y = __shfl_xor_sync(0xffffffffu, x, o);
       if (y > x) x = y;
     }
+    x = __shfl_sync(0xffffffffu, x, 0);
   }
   return x;
+}
+
+// Sums of a and b over the cluster, and of c; or of c's halves the largest each.
+__device__ __forceinline__ void cluster_words(Row& row, uint64_t& a, uint64_t& b, uint64_t& c, bool halves) {
+  Shared& sm = *row.sm;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto join = [&](uint64_t x, uint64_t y) {
+    if (!halves) return x + y;
+    const uint32_t hi = max((uint32_t)(x >> 32), (uint32_t)(y >> 32)), lo = max((uint32_t)x, (uint32_t)y);
+    return (uint64_t)hi << 32 | lo;
+  };
+  a = warp_sum(a);
+  b = warp_sum(b);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) c = join(c, __shfl_xor_sync(0xffffffffu, c, o));
+  uint64_t(*words)[3] = sm.words;
+  __syncthreads();
+  if (lane == 0) {
+    words[warp][0] = a;
+    words[warp][1] = b;
+    words[warp][2] = c;
+  }
+  __syncthreads();
+  a = b = c = 0;
+  for (int w = 0; w < kWarps; ++w) {
+    a += words[w][0];
+    b += words[w][1];
+    c = join(c, words[w][2]);
+  }
+  if (row.C == 1) return;
+  uint64_t* word = sm.mine[row.told & 7];
+  ++row.told;
+  if (threadIdx.x == 0) {
+    word[0] = a;
+    word[1] = b;
+    word[2] = c;
+  }
+  row.sync();
+  const bool on = lane < row.C;
+  a = warp_sum(on ? row.read(word, lane) : 0);
+  b = warp_sum(on ? row.read(word + 1, lane) : 0);
+  c = on ? row.read(word + 2, lane) : 0;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) c = join(c, __shfl_xor_sync(0xffffffffu, c, o));
 }
 
 // The cluster's histogram from its blocks', into count_all and mass_all.  Blocks fill
@@ -311,9 +359,11 @@ __device__ __forceinline__ void join_counts(Row& row) {
   Shared& sm = *row.sm;
   row.sync();
   for (int i = threadIdx.x; i < kBuckets; i += kThreads) {
-    uint32_t n = row.C > 1 ? 0u : sm.count[row.turn][i];
-    if (row.C > 1)
-      for (int c = 0; c < row.C; ++c) n += row.read(&sm.count[row.turn][i], c);
+    uint32_t v[kMostBlocks], n = 0;             // (all blocks' at once)
+#pragma unroll
+    for (int c = 0; c < kMostBlocks; ++c) v[c] = c < row.C ? row.read(&sm.count[row.turn][i], c) : 0u;
+#pragma unroll
+    for (int c = 0; c < kMostBlocks; ++c) n += v[c];
     sm.count_all[i] = n;
     sm.mass_all[i] = 0;
   }
@@ -378,7 +428,7 @@ __device__ __forceinline__ Cut find_cut(Row& row, const Weights& wt, const uint8
   uint64_t lo = 0, hi = 0;                      // as largest of ~key and of key
   each<T>(data, vecs, [&](float x, int) {
     if (x != -INFINITY && wt.bucket(x) == at.bucket) {
-      const uint32_t k = key_of(x);
+      const uint32_t k = key_of<T>(x);
       hi = max(hi, (uint64_t)k);
       lo = max(lo, (uint64_t)(~k));
     }
@@ -392,7 +442,7 @@ __device__ __forceinline__ Cut find_cut(Row& row, const Weights& wt, const uint8
     const int shift = bits > 10 ? bits - 10 : 0;
     clear_histogram(row);
     each<T>(data, vecs, [&](float x, int) {
-      const uint32_t k = key_of(x);
+      const uint32_t k = key_of<T>(x);
       if (k >= low && k <= top) {
         const uint32_t b = (top - k) >> shift;
         atomicAdd(&sm.count[row.turn][b], 1u);
@@ -408,7 +458,7 @@ __device__ __forceinline__ Cut find_cut(Row& row, const Weights& wt, const uint8
     if (shift == 0) {
       Cut cut;
       cut.key = top;
-      const uint64_t w = wt.of(logit_of(top));
+      const uint64_t w = wt.of(logit_of<T>(top));
       cut.ties = (uint32_t)(by_mass ? (need - mass + w - 1) / w : need - count);
       mass += cut.ties * w;
       return cut;
@@ -516,7 +566,7 @@ __device__ __forceinline__ Cut narrow(Row& row, const Weights& wt, const uint8_t
     const uint32_t width = (1u << shift) - 1u;
     clear_counts(row);
     each<T>(data, vecs, [&](float x, int) {
-      const uint32_t k = key_of(x);
+      const uint32_t k = key_of<T>(x);
       if (k >= low && k <= top) atomicAdd(&sm.count[row.turn][(top - k) >> shift], 1u);
     });
     join_counts(row);
@@ -526,7 +576,7 @@ __device__ __forceinline__ Cut narrow(Row& row, const Weights& wt, const uint8_t
         const uint64_t n = sm.count_all[b];
         if (n == 0) continue;
         const uint32_t first = top - ((uint32_t)b << shift), last = first - low > width ? first - width : low;
-        const uint64_t w = wt.of(logit_of(upper ? first : last)), room = shift > 0 ? (w >> 30) + 1 : 0;
+        const uint64_t w = wt.of(logit_of<T>(upper ? first : last)), room = shift > 0 ? (w >> 30) + 1 : 0;
         sm.mass_all[b] = n * (upper ? w + room : w - min(w, room));
       }
       __syncthreads();
@@ -537,7 +587,7 @@ __device__ __forceinline__ Cut narrow(Row& row, const Weights& wt, const uint8_t
     if (shift == 0) {
       Cut cut;
       cut.key = top - (uint32_t)p.bucket;
-      const uint64_t w = wt.of(logit_of(cut.key));
+      const uint64_t w = wt.of(logit_of<T>(cut.key));
       cut.ties = (uint32_t)((need - p.mass + w - 1) / w);
       return cut;
     }
@@ -553,31 +603,27 @@ __device__ __forceinline__ Cut narrow(Row& row, const Weights& wt, const uint8_t
                    e_last = last_of(end);
     uint64_t m0 = 0, m1 = 0, m2 = 0;
     each<T>(data, vecs, [&](float x, int) {
-      const uint32_t k = key_of(x);
+      const uint32_t k = key_of<T>(x);
       if (k > top || k < m_last) return;
       const uint64_t w = wt.of(x);
       if (k > p_first) m0 += w;
       else if (k >= p_last) m1 += w;
       else m2 += w;
     });
-    m0 = cluster_sum(row, m0, nullptr);
+    cluster_words(row, m0, m1, m2, false);
     need = need > m0 ? need - m0 : 1;
     top = p_first;
     uint32_t to = p_last;
-    if (end > p.bucket) {
-      m1 = cluster_sum(row, m1, nullptr);
-      if (need > m1) {
-        need -= m1;
-        m2 = cluster_sum(row, m2, nullptr);
-        to = m_last;
-        if (mid > p.bucket && need <= m2) {
-          top = p_last - 1;
-        } else {
-          need = need > m2 ? need - m2 : 1;
-          if (m_last == low) return Cut{low, 0xffffffffu};            // (nothing is left: all of them)
-          top = m_last - 1;
-          to = e_last;
-        }
+    if (end > p.bucket && need > m1) {
+      need -= m1;
+      to = m_last;
+      if (mid > p.bucket && need <= m2) {
+        top = p_last - 1;
+      } else {
+        need = need > m2 ? need - m2 : 1;
+        if (m_last == low) return Cut{low, 0xffffffffu};              // (nothing is left: all of them)
+        top = m_last - 1;
+        to = e_last;
       }
     }
     low = max(low, to);
@@ -598,7 +644,7 @@ __device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uin
   each<T>(data, vecs, [&](float x, int e) {
     if (wt.z_of(x) * kPerZ < (float)(upto + 1)) {
       const uint32_t at = atomicAdd(&sm.listed, 1u);
-      sm.list_key[at] = key_of(x);
+      sm.list_key[at] = key_of<T>(x);
       sm.list_index[at] = (uint32_t)(index0 + e);
     }
   });
@@ -630,7 +676,7 @@ __device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uin
       const uint32_t o = sm.list_key[j];
       rank += o > key || (o == key && sm.list_index[j] < at) ? 1u : 0u;
     }
-    weight[rank] = wt.of(logit_of(key));
+    weight[rank] = wt.of(logit_of<T>(key));
     index[rank] = at;
     key_in_order[rank] = key;
   }
@@ -674,7 +720,7 @@ __device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uin
     uint64_t cum = 0;
     for (uint32_t j = 0; j < kept; ++j) cum += index[j] <= at ? weight[j] : 0;
     if (target < cum && target >= cum - weight[r])
-      write_token(wt, at, weight[r], sum_kept, wt.z_of(logit_of(key_in_order[r])) * 0.693147182f, token, logprob);
+      write_token(wt, at, weight[r], sum_kept, wt.z_of(logit_of<T>(key_in_order[r])) * 0.693147182f, token, logprob);
   }
 }
 
@@ -758,14 +804,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   const bool greedy = !(temp > 0.f);
   Weights wt;
   wt.small = temp > 0x1p90f ? 0x1p-90f : 1.f;
-  if (t == 0) {
-    // (one thread: fp64 is slow here; the maximum's barriers come before it is read)
-    const double c = greedy ? 0.0 : 1.4426950408889634074 / ((double)temp * (double)wt.small);
-    // (a T so small that the factor is no fp32 number: 0 times it has to be 0)
-    sm.factor[0] = c < 3e38 ? (float)c : 3e38f;
-    sm.factor[1] = c < 3e38 ? (float)(c - (double)(float)c) : 0.f;
+  {
+    // log2(e) / T in two parts, in fp32 alone (fp64 is slow here); a T so small that the factor is no fp32 number: 0
+    // times it has to be 0
+    constexpr float kHi = 1.44269502f, kLo = 1.92596303e-8f;
+    const float T1 = temp * wt.small;
+    wt.ch = greedy || T1 == INFINITY ? 0.f : fminf(__fdiv_rn(kHi, T1), 3e38f);
+    wt.cl = wt.ch == 0.f || wt.ch == 3e38f ? 0.f : __fdiv_rn(fmaf(-wt.ch, T1, kHi) + kLo, T1);
   }
-  M = logit_of((uint32_t)cluster_max(row, key_of(M)));
+  M = logit_of<T>((uint32_t)cluster_max(row, key_of<T>(M)));
   if (M == INFINITY) {
     // these share everything: 0 for them, nothing for the others
     for (int v = t; v < vecs; v += kThreads) {
@@ -784,8 +831,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   wt.M = M * wt.small;
   wt.q = a.q;
   wt.table = sm.table;
-  wt.ch = sm.factor[0];
-  wt.cl = sm.factor[1];
   const int32_t k = a.top_k ? __ldg(a.top_k + r) : 0;
   const float p = a.top_p ? __ldg(a.top_p + r) : 1.f;
   const float mp = a.min_p ? __ldg(a.min_p + r) : 0.f;
@@ -842,16 +887,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           if (by_p) {
             uint64_t kept = 0, unused, tie0;    // all that top-k keeps
             uint32_t ties = 0;
-            walk<T>(data, v0, v1, 1, [&](float x, int) { ties += key_of(x) == cut_k.key ? 1u : 0u; });
+            walk<T>(data, v0, v1, 1, [&](float x, int) { ties += key_of<T>(x) == cut_k.key ? 1u : 0u; });
             cluster_sum(row, ties, &tie0);
             walk<T>(data, v0, v1, 1, [&](float x, int) {
-              const uint32_t key = key_of(x);
+              const uint32_t key = key_of<T>(x);
               if (key > cut_k.key || (key == cut_k.key && tie0++ < cut_k.ties)) kept += wt.of(x);
             });
             kept = cluster_sum(row, kept, nullptr);
             clear_histogram(row);
             each<T>(data, vecs, [&](float x, int) {
-              if (key_of(x) >= cut_k.key) {
+              if (key_of<T>(x) >= cut_k.key) {
                 const uint64_t w = wt.of(x);
                 const int b = wt.bucket(x);
                 atomicAdd(&sm.count[row.turn][b], 1u);
@@ -880,19 +925,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             above += w;
             sum += w >= least ? w : 0;
           } else if (z < (float)(b.y + 1)) {
-            hi = max(hi, (uint64_t)key_of(x));
-            lo = max(lo, (uint64_t)(~key_of(x)));
+            hi = max(hi, (uint64_t)key_of<T>(x));
+            lo = max(lo, (uint64_t)(~key_of<T>(x)));
           }
         });
-        total = cluster_sum(row, total, nullptr);
+        uint64_t keys = hi << 32 | lo;
+        cluster_words(row, total, above, keys, true);
         if (few) {
           from_list<T>(row, wt, data, vecs, index0, b.y, 0xffffffffu, true, p, total, least, u, token, logprob);
           done = true;
         } else {
-          above = cluster_sum(row, above, nullptr);
           const uint64_t need = share_of(p, total);
-          top = (uint32_t)cluster_max(row, hi);
-          cut_p = narrow<T>(row, wt, data, vecs, top, ~(uint32_t)cluster_max(row, lo), need > above ? need - above : 1);
+          top = (uint32_t)(keys >> 32);
+          cut_p = narrow<T>(row, wt, data, vecs, top, ~(uint32_t)keys, need > above ? need - above : 1);
           have_sum = true;
         }
       }
@@ -906,11 +951,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       uint64_t tie0 = 0;                        // such tokens in front of the run
       if (ties != 0xffffffffu) {
         uint32_t n = 0;
-        walk<T>(data, v0, v1, 1, [&](float x, int) { n += key_of(x) == ck ? 1u : 0u; });
+        walk<T>(data, v0, v1, 1, [&](float x, int) { n += key_of<T>(x) == ck ? 1u : 0u; });
         cluster_sum(row, n, &tie0);
       }
       auto weight = [&](float x, uint64_t& tie) -> uint64_t {
-        const uint32_t key = key_of(x);
+        const uint32_t key = key_of<T>(x);
         if (key < ck) return 0;
         if (key == ck && tie++ >= ties) return 0;
         const uint64_t w = wt.of(x);
@@ -919,7 +964,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       uint64_t tie = tie0, before;
       if (have_sum)
         walk<T>(data, v0, v1, 1, [&](float x, int) {
-          if (key_of(x) <= top) sum += weight(x, tie);
+          if (key_of<T>(x) <= top) sum += weight(x, tie);
         });
       else if (ck == 0 && least == 1)
         walk<T>(data, v0, v1, 1, [&](float x, int) { sum += wt.of(x); });
@@ -938,7 +983,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         for (int e0 = b0; e0 < b1; e0 += 32) {
           const int e = e0 + lane;
           const float x = e < b1 ? element<T>(data, e) : -INFINITY;
-          const uint32_t tied = __ballot_sync(0xffffffffu, e < b1 && key_of(x) == ck);
+          const uint32_t tied = __ballot_sync(0xffffffffu, e < b1 && key_of<T>(x) == ck);
           uint64_t rank = seen + __popc(tied & ((1u << lane) - 1u));
           const uint64_t w = e < b1 ? weight(x, rank) : 0;
           const uint64_t upto = at + scan_warp(w);
@@ -965,7 +1010,7 @@ cudaError_t launch_t(SampleArgs a, int64_t n_rows, cudaStream_t st) {
   // blocks of a row: so many that a slice leaves room for a second block on the SM, and
   // that few rows use the device
   int C = 1;
-  while (C < 8 && ((vecs + C - 1) / C * 16 > 66 * 1024 || (n_rows * C < kv8_sm_count() && vecs / C > 2 * kThreads))) C *= 2;
+  while (C < kMostBlocks && ((vecs + C - 1) / C * 16 > 66 * 1024 || (n_rows * C < kv8_sm_count() && vecs / C > 2 * kThreads))) C *= 2;
   a.C = C;
   a.vecs = (int)((vecs + C - 1) / C);
   const size_t smem = sizeof(Shared) + (size_t)a.vecs * 16;
