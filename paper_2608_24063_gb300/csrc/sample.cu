@@ -650,14 +650,17 @@ __device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uin
   });
   row.sync();
   if (row.rank != 0) return;
-  uint32_t n = sm.listed;
-  for (int c = 1; c < row.C; ++c) {
-    const uint32_t m = row.read(&sm.listed, c);
-    for (uint32_t i = t; i < m; i += kThreads) {
-      sm.list_key[n + i] = row.read(&sm.list_key[i], c);
-      sm.list_index[n + i] = row.read(&sm.list_index[i], c);
+  // the others' lists behind this block's, a warp a block
+  const int lane = t & 31, from = t >> 5;
+  const uint32_t count = lane < row.C ? row.read(&sm.listed, lane) : 0u, ends = scan_warp(count);
+  const uint32_t n = __shfl_sync(0xffffffffu, ends, 31);
+  static_assert(kMostBlocks <= kWarps, "a warp for each block");
+  if (from > 0 && from < row.C) {
+    const uint32_t m = __shfl_sync(0xffffffffu, count, from), at = __shfl_sync(0xffffffffu, ends, from) - m;
+    for (uint32_t i = lane; i < m; i += 32) {
+      sm.list_key[at + i] = row.read(&sm.list_key[i], from);
+      sm.list_index[at + i] = row.read(&sm.list_index[i], from);
     }
-    n += m;
   }
   __syncthreads();
   // in order: a token's place is the number of those before it
