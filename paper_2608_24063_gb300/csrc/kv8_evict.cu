@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kSelThreads) kv8_evict_select_kernel(const __g
   __shared__ int hist[kBins];
   __shared__ int scan[2][kSelThreads / 32];
   __shared__ int err, found_bin, found_need, found_all, gap;
-  const int t = threadIdx.x, r = blockIdx.y, g = blockIdx.x;
+  const int t = threadIdx.x, r = blockIdx.y, g = blockIdx.x, shift = __ffs(c.page) - 1;      // (pages are powers of two)
   if (t == 0) err = VC_OK;
   __syncthreads();
   const int cap = s.max_pages * c.page;
@@ -98,12 +98,33 @@ __global__ void __launch_bounds__(kSelThreads) kv8_evict_select_kernel(const __g
   const int32_t* table = s.block_table + (int64_t)r * s.max_pages;
   auto fetch = [&](int i) {
     if (i < a.sink || i >= len - a.recent) return kInfKey;
-    const int p = __ldg(table + i / c.page);
-    return weight_key(__ldg(a.weights + ((int64_t)p * c.Hkv + g) * c.page + i % c.page));
+    const int p = __ldg(table + (i >> shift));
+    return weight_key(__ldg(a.weights + (((p * c.Hkv + g) << shift) + (i & (c.page - 1)))));
   };
   const bool held = len <= cached;
-  if (held)
-    for (int i = t; i < len; i += kSelThreads) cache[i] = fetch(i);
+  if (held) {
+    // eight tokens at a time: their pages, then their weights
+    constexpr int kAtOnce = 8;
+    for (int i0 = t; i0 < len; i0 += kAtOnce * kSelThreads) {
+      int p[kAtOnce];
+      float w[kAtOnce];
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) {
+        const int i = i0 + n * kSelThreads;
+        p[n] = i < len ? __ldg(table + (i >> shift)) : 0;
+      }
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) {
+        const int i = i0 + n * kSelThreads;
+        w[n] = i < len ? __ldg(a.weights + (((p[n] * c.Hkv + g) << shift) + (i & (c.page - 1)))) : 0.f;
+      }
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) {
+        const int i = i0 + n * kSelThreads;
+        if (i < len) cache[i] = i < a.sink || i >= len - a.recent ? kInfKey : weight_key(w[n]);
+      }
+    }
+  }
   auto key = [&](int i) { return held ? cache[i] : fetch(i); };
   // the keep-th largest key: digit by digit from the top
   uint32_t prefix = 0u, mask = 0u;
@@ -111,12 +132,12 @@ __global__ void __launch_bounds__(kSelThreads) kv8_evict_select_kernel(const __g
   bool all = need == 0;
   if (need == 0) prefix = 0xffffffffu;          // no key is that large
   for (int pass = 0; pass < 3 && !all; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
     for (int i = t; i < kBins; i += kSelThreads) hist[i] = 0;
     __syncthreads();
     for (int i = t; i < len; i += kSelThreads) {
       const uint32_t k = key(i);
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1);
+      if ((k & mask) == prefix) atomicAdd(&hist[(k >> low) & ((1u << bits) - 1u)], 1);
     }
     __syncthreads();
     // threads from the top bin down
@@ -139,8 +160,8 @@ __global__ void __launch_bounds__(kSelThreads) kv8_evict_select_kernel(const __g
       }
     }
     __syncthreads();
-    prefix |= (uint32_t)found_bin << shift;
-    mask |= ((1u << bits) - 1u) << shift;
+    prefix |= (uint32_t)found_bin << low;
+    mask |= ((1u << bits) - 1u) << low;
     need = found_need;
     all = found_all != 0;                       // every key under the prefix stays
     __syncthreads();
@@ -174,7 +195,9 @@ __global__ void __launch_bounds__(kSelThreads) kv8_evict_select_kernel(const __g
 // ---------------------------------------------------------------------------
 // what stays moves together
 
-constexpr int kMoveThreads = 256, kMoveBytes = 16384;   // codes of a block's step
+// 16 caches of up to 12544 tokens cut to 3136, 8 heads of 128, us of both kernels (cold): 256 threads 90,
+// 512 75, 1024 75; 32 KB of codes a step and 512 threads 87.
+constexpr int kMoveThreads = 512, kMoveBytes = 16384;   // codes of a block's step
 constexpr int kNV = kMoveBytes / 16 / kMoveThreads;     // 16-code vectors of a thread
 
 // The largest magnitude of sixteen codes, NaN left out.
@@ -192,9 +215,31 @@ __device__ __forceinline__ float largest_code(const uint4& w) {
   return fmaxf(__low2float(m), __high2float(m));
 }
 
+// Sixteen codes times f = 2^k, 2^-24 <= f <= 2^15, to nearest even.  In fp16: a product that is not exact there
+// is below 2^-20, which e4m3 rounds to 0 like anything below 2^-10.
+__device__ __forceinline__ uint4 scale_codes(const uint4& w, float f) {
+  const __half2 f2 = __float2half2_rn(f);
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t r[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t b = e4m3x2_to_f16x2(x[i] >> (16 * h));
+      const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&b), f2);
+      unsigned short o;
+      asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(o) : "r"(*reinterpret_cast<const uint32_t*>(&z)));
+      r[h] = o;
+    }
+    y[i] = r[0] | r[1] << 16;
+  }
+  return make_uint4(y[0], y[1], y[2], y[3]);
+}
+
 // Grid: clusters of C blocks, one for each unit: (request, head) x {K, V}.
 template <int D>
-__global__ void __launch_bounds__(kMoveThreads) kv8_evict_move_kernel(const __grid_constant__ vc_kv8 c,
+__global__ void __launch_bounds__(kMoveThreads, 2) kv8_evict_move_kernel(const __grid_constant__ vc_kv8 c,
                                                                       const __grid_constant__ vc_kv8_step s,
                                                                       const __grid_constant__ Kv8EvictArgs a, int C) {
   constexpr int VPR = D / 16, TS = kMoveBytes / D;      // vectors of a token, tokens of a step
@@ -216,7 +261,8 @@ __global__ void __launch_bounds__(kMoveThreads) kv8_evict_move_kernel(const __gr
     if (t == 0) *a.status = e;
   }
   const Kv8Unit un = a.units[unit];
-  const int first = un.gap / c.page * c.page;           // token from which pages are written
+  const int shift = __ffs(c.page) - 1;
+  const int first = un.gap & ~(c.page - 1);             // token from which pages are written
   if (first >= un.len) return;                          // (the whole cluster)
   const int steps = (un.len - first + TS - 1) / TS, waves = (steps + C - 1) / C;
   const int32_t* table = s.block_table + (int64_t)r * s.max_pages;
@@ -227,41 +273,63 @@ __global__ void __launch_bounds__(kMoveThreads) kv8_evict_move_kernel(const __gr
 
   // (page, head) slot of a token of this head: slot / page is the scale's index
   auto slot_of = [&](int token) {
-    const int p = __ldg(table + token / c.page);
-    return ((int64_t)p * c.Hkv + g) * c.page + token % c.page;
+    const int p = __ldg(table + (token >> shift));
+    return ((p * c.Hkv + g) << shift) + (token & (c.page - 1));      // (all slots of a pool: below 2^31)
   };
+  // A wave's loads hang on one another: kept tokens, their pages, codes.  Each is sent for a wave before the
+  // next one needs it.
   struct Wave {
     uint4 w[kNV];
     float scale[kNV], weight;
   };
+  struct Places {
+    int of[kNV], weight;                        // kept tokens, then their slots; of the token whose weight the thread moves
+  };
   Wave cur, nxt;
+  Places tokens, slots;
   const int part = t % VPR;
   auto token = [&](int wave, int i) { return first + (wave * C + rank) * TS + (t + i * kMoveThreads) / VPR; };
+  auto weight_token = [&](int wave) { return first + (wave * C + rank) * TS + t; };
+  auto moves_weight = [&](int wave) { return !isv && t < TS && weight_token(wave) < un.len; };
+  auto load_tokens = [&](int wave) {
+#pragma unroll
+    for (int i = 0; i < kNV; ++i)
+      if (token(wave, i) < un.len) tokens.of[i] = __ldg(kept + token(wave, i));
+    if (moves_weight(wave)) tokens.weight = __ldg(kept + weight_token(wave));
+  };
+  auto load_slots = [&](int wave) {
+#pragma unroll
+    for (int i = 0; i < kNV; ++i)
+      if (token(wave, i) < un.len) slots.of[i] = slot_of(tokens.of[i]);
+    if (moves_weight(wave)) slots.weight = slot_of(tokens.weight);
+  };
   auto load = [&](int wave, Wave& x) {
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-      const int to = token(wave, i);
-      if (to < un.len) {
-        const int64_t from = slot_of(__ldg(kept + to));
-        x.w[i] = __ldcg(reinterpret_cast<const uint4*>(codes + from * D) + part);
-        x.scale[i] = __ldcg(scales + from / c.page);
+    for (int i = 0; i < kNV; ++i)
+      if (token(wave, i) < un.len) {
+        x.w[i] = __ldcg(reinterpret_cast<const uint4*>(codes + (int64_t)slots.of[i] * D) + part);
+        x.scale[i] = __ldcg(scales + (slots.of[i] >> shift));
       }
-    }
-    const int to = first + (wave * C + rank) * TS + t;
-    if (!isv && t < TS && to < un.len) x.weight = __ldcg(a.weights + slot_of(__ldg(kept + to)));
+    if (moves_weight(wave)) x.weight = __ldcg(a.weights + slots.weight);
   };
+  load_tokens(0);
+  load_slots(0);
+  load_tokens(1);
   load(0, cur);
+  load_slots(1);
+  load_tokens(2);
   __syncthreads();                                      // amax is cleared
   for (int wave = 0; wave < waves; ++wave) {
-    if (wave + 1 < waves) load(wave + 1, nxt);
-    const int at0 = (wave * C + rank) * TS;
+    load(wave + 1, nxt);
+    load_slots(wave + 2);
+    load_tokens(wave + 3);
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
       const bool on = token(wave, i) < un.len;
       const float m = on ? largest_code(cur.w[i]) * cur.scale[i] : 0.f;
       const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
       // (a warp's tokens lie on one page)
-      if ((t & 31) == 0) atomicMax(&amax[wave & 1][(t + i * kMoveThreads) / VPR / c.page], top);
+      if ((t & 31) == 0) atomicMax(&amax[wave & 1][(t + i * kMoveThreads) / VPR >> shift], top);
     }
     __syncwarp();
     if (C > 1) tc::cluster_sync();
@@ -272,21 +340,17 @@ __global__ void __launch_bounds__(kMoveThreads) kv8_evict_move_kernel(const __gr
       const int to = token(wave, i);
       if (to < un.len) {
         const int slot = (t + i * kMoveThreads) / VPR;
-        const float now = pow2_scale(__uint_as_float(amax[wave & 1][slot / c.page]));
+        const float now = pow2_scale(__uint_as_float(amax[wave & 1][slot >> shift]));
         // a token of zeros may have any scale: a factor past e4m3's range is not needed
         const float f = fminf(cur.scale[i] * pow2_inverse(now), 0x1p20f);
         uint4 y = cur.w[i];
-        if (f != 1.f) {
-          float v[16];
-          decode16(y, v);
-          y = encode16<false>(v, f, 448.f);
-        }
-        const int64_t dst = slot_of(to);
-        reinterpret_cast<uint4*>(codes + dst * D)[part] = y;
-        if (part == 0 && to % c.page == 0) scales[dst / c.page] = now;
+        if (f != 1.f) y = f <= 0x1p15f ? scale_codes(y, fmaxf(f, 0x1p-24f)) : scale_codes(scale_codes(y, 0x1p8f), f * 0x1p-8f);
+        const int dst = slot_of(to);
+        reinterpret_cast<uint4*>(codes + (int64_t)dst * D)[part] = y;
+        if (part == 0 && (to & (c.page - 1)) == 0) scales[dst >> shift] = now;
       }
     }
-    if (!isv && t < TS && first + at0 + t < un.len) a.weights[slot_of(first + at0 + t)] = cur.weight;
+    if (moves_weight(wave)) a.weights[slot_of(weight_token(wave))] = cur.weight;
     __syncthreads();
     if (t < TS / 16) amax[wave & 1][t] = 0u;            // (used again two barriers on)
     cur = nxt;
@@ -298,8 +362,10 @@ cudaError_t launch_move(const vc_kv8& c, const vc_kv8_step& s, const Kv8EvictArg
   const int64_t units = (int64_t)s.n_req * c.Hkv * 2;
   const int64_t most = (int64_t)s.max_pages * c.page < a.max_keep ? (int64_t)s.max_pages * c.page : a.max_keep;
   const int64_t steps = (most * D + kMoveBytes - 1) / kMoveBytes;
+  // blocks of a unit: while there are SMs without one (two an SM: 93 us instead of 75 in the case above, whose
+  // 240 units fill the device; a wave's end is felt)
   int C = 1;
-  while (C < 8 && units * C < 2 * kv8_sm_count() && C < steps) C *= 2;
+  while (C < 8 && units * C < kv8_sm_count() && C < steps) C *= 2;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = (unsigned)C;

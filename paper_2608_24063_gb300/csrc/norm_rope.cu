@@ -193,27 +193,32 @@ __global__ void __launch_bounds__(kThreads) norm_mrope_grad_kernel(const __grid_
   for (int i = 0; i < 8; ++i) dx[i] = dy[i] = 0.f;
   const int first = isk ? (int)blockIdx.x - p.nq : (int)blockIdx.x;
   const int blocks = isk ? (int)gridDim.x - p.nq : p.nq;
+  // items of a group of rows: (row, head), GROUPS of them at once; the next one's values are in flight
+  const int dl = GROUPS / H, dh = GROUPS - dl * H, lr0 = grp / H, h0 = grp - lr0 * H;
+  Raw8<T> x, y, g, k;
+  auto load = [&](int64_t r0, int rows, int lr, int h) {
+    if (lr >= rows) return;
+    const T* xp = X + (r0 + lr) * xs + (int64_t)h * D;
+    const T* gp = G + (r0 + lr) * gs + (int64_t)h * D;
+    x.load(xp + sl.o0);
+    y.load(xp + sl.o1);
+    g.load(gp + sl.o0);
+    k.load(gp + sl.o1);
+  };
   for (int64_t r0 = (int64_t)first * RB; r0 < a.n_rows; r0 += (int64_t)blocks * RB) {
+    const int rows = (int)(a.n_rows - r0 < RB ? a.n_rows - r0 : RB);
+    load(r0, rows, lr0, h0);
     __syncthreads();                            // the angles before are read
     for (int i = t; i < RB * HALF; i += kThreads)
       if (i % HALF < a.half && r0 + i / HALF < a.n_rows) cs[i / HALF][i % HALF] = angle(a, i % HALF, r0 + i / HALF);
     __syncthreads();
-    const int rows = (int)(a.n_rows - r0 < RB ? a.n_rows - r0 : RB);
-    const int items = rows * H;
-    for (int i0 = 0; i0 < items; i0 += GROUPS) {
-      const int item = i0 + grp;
-      const bool on = item < items;
-      const int lr = on ? item / H : 0, h = on ? item - lr * H : 0;
-      const int64_t row = r0 + lr;
-      float xa[8], ya[8], ga[8], gb[8], c[8], s[8];
-      Raw8<T> x, y, g, k;
-      const T* xp = X + row * xs + (int64_t)h * D;
-      const T* gp = G + row * gs + (int64_t)h * D;
+    int lr = lr0, h = h0;
+    for (int left = rows * H; left > 0; left -= GROUPS) {     // (the same for the block: shuffles need whole warps)
+      const bool on = lr < rows;
+      const int row_of = on ? lr : 0;
+      T* dst = O + (r0 + lr) * os + (int64_t)h * D;
+      float xa[8], ya[8], ga[8], gb[8];
       if (on) {
-        x.load(xp + sl.o0);
-        y.load(xp + sl.o1);
-        g.load(gp + sl.o0);
-        k.load(gp + sl.o1);
         x.get(xa);
         y.get(ya);
         g.get(ga);
@@ -222,11 +227,18 @@ __global__ void __launch_bounds__(kThreads) norm_mrope_grad_kernel(const __grid_
 #pragma unroll
         for (int i = 0; i < 8; ++i) xa[i] = ya[i] = ga[i] = gb[i] = 0.f;
       }
+      lr += dl;
+      h += dh;
+      if (h >= H) {
+        h -= H;
+        ++lr;
+      }
+      load(r0, rows, lr, h);
       if (sl.turns) {
-        float u[8], v[8];
+        float c[8], s[8], u[8], v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float2 w = cs[lr][slot * 8 + i];
+          const float2 w = cs[row_of][slot * 8 + i];
           c[i] = w.x;
           s[i] = w.y;                           // (the table holds -sin: R^T)
         }
@@ -258,7 +270,6 @@ __global__ void __launch_bounds__(kThreads) norm_mrope_grad_kernel(const __grid_
           xa[i] = rr * (ga[i] - xa[i] * m);
           ya[i] = rr * (gb[i] - ya[i] * m);
         }
-        T* dst = O + row * os + (int64_t)h * D;
         store8(dst + sl.o0, xa);
         store8(dst + sl.o1, ya);
       }
