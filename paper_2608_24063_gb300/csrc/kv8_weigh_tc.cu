@@ -33,6 +33,14 @@
 // and the two cancel.  Other roundings go either way and average out over a token's rows.
 // A tile's terms are added in eight partial sums, tiles with a compensated sum, so 16384
 // rows cost no more bits than 16.
+//
+// 2048 rows over 32768 tokens, 64 / 8 heads of 128 (1.07 TFLOP, 4.3 G exponentials): 1.00 ms, 1.07
+// PFLOP/s, 56% of the cuBLAS rate; at the 1.5 GHz that the card holds under it a product takes 1740
+// clocks: its MMAs 1024, its exponentials 1190 (32 a clock would be 1024; measured alone).
+// Without exponentials 0.90 ms, without MMAs 0.99, with a quarter of the epilogue 0.66.  Eight
+// epilogue warps 1.05 ms; two groups of eight that take products in turn 1.14, four with
+// buffers of 128 columns 1.10; all of a warp's columns loaded at once 1.06.  One fp32 step
+// holds 128 rows in two parts.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_sched.cuh"
@@ -329,11 +337,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
     // ---- loaders
     const int t = threadIdx.x - 32 * kLoadWarp0;
     if (!F32) prefetch_tmap(&tmQ);
-    // 16 codes of a token a thread at a time, kBatch of them in flight
-    constexpr int VPR = D / 16, kVecs = kGroup * VPR / kLoadThreads, kBatch = 8;
-    static_assert(kVecs % kBatch == 0 || kVecs < 2 * kBatch, "whole batches");
-    constexpr int kB = kVecs % kBatch == 0 ? kBatch : kVecs / 2;
-    static_assert(kVecs % kB == 0, "whole batches");
+    // 16 codes of a token a thread at a time, kB of them in flight
+    constexpr int VPR = D / 16, kVecs = kGroup * VPR / kLoadThreads, kB = 12;
+    static_assert(kVecs * kLoadThreads == kGroup * VPR && kVecs % kB == 0, "whole batches");
     uint4 codes[kB];
     auto fetch = [&](int batch) {
       int pid[kB];
@@ -359,8 +365,46 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
     const float* lp[NL];
     float lv[NL];
     int issued = 0;                             // steps whose copies were sent
+    auto send_rows = [&](int row, int st) {     // bf16: a step's rows, by one thread
+      issued = step + 1;
+      if (t == 0) {
+        mbar_arrive_expect_tx(&sm.q_full[st], (uint32_t)(RB * G * D * 2));
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x)
+          tma_load_3d(sm.q[st] + x * N * 128, &tmQ, x * 64, w.u.g * G, row, &sm.q_full[st]);
+      }
+      __syncwarp();
+    };
     do {
-      fetch(0);                                 // (under the end of the unit before)
+      // under the end of the unit before: half of the codes, the first step's rows and their lse
+      fetch(0);
+      const Req8 q = w.u.q;
+      const int b0 = line.first_block(q, w.u.rt * kGroup);
+      const int dead = max(0, q.m - q.len);     // the surplus first rows are no tokens
+      if (!F32) {
+        ok = warp_wait(&sm.q_empty[step & 1], ((step >> 1) & 1) ^ 1, abort);
+        if (!ok) break;
+        send_rows(q.row0 + (b0 + w.t0) * RB, step & 1);
+      }
+      auto fetch_lse = [&](int b) {
+#pragma unroll
+        for (int k = 0; k < NL; ++k) {
+          const int i = (b0 + b) * RB + li[k];
+          lv[k] = -INFINITY;
+          if (li[k] < RB && i >= dead && i < q.m) {
+            const float l = __ldg(lp[k] + (int64_t)(b0 + b) * RB * a.Hq);
+            lv[k] = -fmaf(l, a.lse_log2, l * a.lse_log2_lo);
+            if (lv[k] == INFINITY) lv[k] = -INFINITY;
+          }
+        }
+      };
+#pragma unroll
+      for (int k = 0; k < NL; ++k) {
+        const int x = t + k * kLoadThreads;
+        li[k] = x / G;
+        lp[k] = a.lse + (int64_t)(q.row0 + li[k]) * a.Hq + w.u.g * G + (x - li[k] * G);
+      }
+      fetch_lse(w.t0);
       ok = warp_wait(&sm.k_empty, (seg & 1) ^ 1, abort);
       if (!ok) break;
 #pragma unroll 1
@@ -383,42 +427,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
       }
       // (the issuer learns of it with the first step's rows, which this thread reports later)
       fence_proxy_async();
-      const Req8 q = w.u.q;
-      const int b0 = line.first_block(q, w.u.rt * kGroup);
-      const int dead = max(0, q.m - q.len);     // the surplus first rows are no tokens
-      auto fetch_lse = [&](int b) {
-#pragma unroll
-        for (int k = 0; k < NL; ++k) {
-          const int i = (b0 + b) * RB + li[k];
-          lv[k] = -INFINITY;
-          if (li[k] < RB && i >= dead && i < q.m) {
-            const float l = __ldg(lp[k] + (int64_t)(b0 + b) * RB * a.Hq);
-            lv[k] = -fmaf(l, a.lse_log2, l * a.lse_log2_lo);
-            if (lv[k] == INFINITY) lv[k] = -INFINITY;
-          }
-        }
-      };
-#pragma unroll
-      for (int k = 0; k < NL; ++k) {
-        const int x = t + k * kLoadThreads;
-        li[k] = x / G;
-        lp[k] = a.lse + (int64_t)(q.row0 + li[k]) * a.Hq + w.u.g * G + (x - li[k] * G);
-      }
-      fetch_lse(w.t0);
       for (int b = w.t0; ok && b < w.t1; ++b, ++step) {
         const int st = step & 1, i0 = (b0 + b) * RB;
-        ok = warp_wait(&sm.q_empty[st], ((step >> 1) & 1) ^ 1, abort);
-        if (!ok) break;
+        if (F32 || b > w.t0) {
+          ok = warp_wait(&sm.q_empty[st], ((step >> 1) & 1) ^ 1, abort);
+          if (!ok) break;
+        }
         uint8_t* dst = sm.q[st];
         if constexpr (!F32) {
-          issued = step + 1;
-          if (t == 0) {
-            mbar_arrive_expect_tx(&sm.q_full[st], (uint32_t)(RB * G * D * 2));
-#pragma unroll
-            for (int x = 0; x < D / 64; ++x)
-              tma_load_3d(dst + x * N * 128, &tmQ, x * 64, w.u.g * G, q.row0 + i0, &sm.q_full[st]);
-          }
-          __syncwarp();
+          if (b > w.t0) send_rows(q.row0 + i0, st);
           if (lane == 0) mbar_arrive(&sm.q_full[st]);   // (K, with a unit's first rows)
         }
         ok = warp_wait(&sm.l_empty[st], ((step >> 1) & 1) ^ 1, abort);
@@ -494,18 +511,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
     do {
       const int nt = tiles_of(), tok0 = w.u.rt * kGroup;
       const int b0 = line.first_block(w.u.q, tok0);
-      float fac[kTiles], acc[kTiles], low[kTiles];
+      float fac[kTiles], acc[kTiles], low[kTiles], old[kTiles];
       int64_t slot[kTiles];                     // of the thread's token, -1 if it has none
 #pragma unroll
       for (int kt = 0; kt < kTiles; ++kt) {
         const int x = kt * kKT + tok;
         slot[kt] = -1;
-        fac[kt] = acc[kt] = low[kt] = 0.f;
+        fac[kt] = acc[kt] = low[kt] = old[kt] = 0.f;
         if (x < w.u.kend) {
           const int p = load_page(s, c.n_pages, w.u.r, (tok0 + x) / c.page, err);
           if (p >= 0) {
             slot[kt] = ((int64_t)p * c.Hkv + w.u.g) * c.page + (tok0 + x) % c.page;
             fac[kt] = __ldg(c.K_scale + (int64_t)p * c.Hkv + w.u.g) * a.scale_log2;
+            // what the token had, unless it is one of the step's own: in the unit's first piece
+            if (quarter == 0 && w.t0 == 0 && tok0 + x < w.u.q.len - w.u.q.m) old[kt] = a.weights[slot[kt]];
           }
         }
       }
@@ -552,8 +571,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
           float v = acc[kt] - low[kt];
 #pragma unroll
           for (int x = 1; x < kParts; ++x) v += part[(x * kTiles + kt) * kKT + tok];
-          // what the token had, unless it is one of the step's own
-          if (slot[kt] >= 0 && w.t0 == 0 && tok0 + kt * kKT + tok < w.u.q.len - w.u.q.m) v += a.weights[slot[kt]];
+          v += old[kt];
           if (whole) {
             if (slot[kt] >= 0) a.weights[slot[kt]] = v;
           } else {

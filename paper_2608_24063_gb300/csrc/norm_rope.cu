@@ -12,6 +12,11 @@
 // sums over a head are three or two shuffles and the rest stays in registers, as in
 // rope.cu.
 //
+// 32768 rows of 72 heads of 128 in bf16 (1.21 GB): 209 us, 5.8 TB/s, 87% of a plain copy's rate (the
+// rotation alone: 198 us).  Gradient of 12544 rows of 32 heads (308 MB): 84 us, 3.7 TB/s, 55%: 16
+// warps an SM at 120 registers keep too little in flight, and more rows ahead of each thread
+// (89 us, cold, as without) or smaller blocks (103) do not help.  16 rows of 32 heads: a launch.
+//
 // Sums of squares that pass fp32's range are taken again of values times 2^-70: the
 // branch costs nothing where it is not taken.
 #include "kernels.h"

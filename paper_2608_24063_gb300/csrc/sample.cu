@@ -25,6 +25,12 @@
 //   - a larger top-k goes through histograms of counts and weights.
 // Then the kept weights of each thread's run of tokens are scanned, and the one warp that
 // holds the token looks through its run.
+//
+// 256 rows of 131072 in bf16, a fifth each greedy, all filters, none, and two of top-p alone with nuclei of
+// thousands (67 MB): 227 us, bound by the weights' arithmetic and the clusters' meetings, a plain read
+// 10 us.  64 rows of 50001 without filters 18 us, one row of 32000 with all of them 14 us, a chain of
+// eight steps between blocks.  In place of the cuts from counts, histograms of weights by 64-bit
+// atomics: 441, 31 and 52 us.
 #include "kernels.h"
 #include "kv8_sched.cuh"
 #include "profile.h"
@@ -965,10 +971,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         return w >= least ? w : 0;
       };
       uint64_t tie = tie0, before;
-      if (have_sum)
+      if (have_sum && top - ck < (uint32_t)kBuckets) {
+        // few different logits (of bf16 rows always): their weights from a table
+        for (uint32_t i = t; i <= top - ck; i += kThreads) {
+          const uint64_t w = wt.of(logit_of<T>(top - i));
+          sm.mass_all[i] = w >= least ? w : 0;
+        }
+        __syncthreads();
+        walk<T>(data, v0, v1, 1, [&](float x, int) {
+          const uint32_t key = key_of<T>(x);
+          if (key > top || key < ck || (key == ck && tie++ >= ties)) return;
+          sum += sm.mass_all[top - key];
+        });
+      } else if (have_sum) {
         walk<T>(data, v0, v1, 1, [&](float x, int) {
           if (key_of<T>(x) <= top) sum += weight(x, tie);
         });
+      }
       else if (ck == 0 && least == 1)
         walk<T>(data, v0, v1, 1, [&](float x, int) { sum += wt.of(x); });
       else

@@ -28,16 +28,18 @@ def run(segments, seed, mistake=None):
     def loader(me):
         step = 0
         for seg, (n, _) in enumerate(segments):
-            yield w("k_empty", k_empty, seg - 1)
-            need(not pipe or mistake, "K written under a product")
-            need(parts.get(seg - 1, EPILOGUE) == EPILOGUE, "K written while the quarters' sums lie there")
-            K[me] = seg                         # (reported with the first step's rows)
             for j in range(n):
                 st = step & 1
                 yield w("q_empty", q_empty[st], (step >> 1) - 1)
                 need(all(b[0] != "P" or b[2] != st for b in pipe), "query rows written under a product")
                 if me == 0:
                     flying.append(step)
+                if j == 0:
+                    # the first rows are on their way before the unit's K is
+                    yield w("k_empty", k_empty, seg - 1)
+                    need(not any(b[0] == "P" and b[3] < seg for b in pipe), "K written under a product")
+                    need(parts.get(seg - 1, EPILOGUE) == EPILOGUE, "K written while the quarters' sums lie there")
+                    K[me] = seg                 # (reported with the first step's rows)
                 q_full[st].arrive()
                 yield w("l_empty", l_empty[st], (step >> 1) - 1)
                 lse[st][me] = step
