@@ -19,8 +19,9 @@
 // multiplied first.
 //
 // Warps (672 threads):
-//   0-15   epilogue: warp w reads lanes 32 (w % 4) .., columns of quarter w / 4
-//   16-19  loaders: K tiles of the next unit, query rows of the next step, their lse
+//   0-15   a unit's K tiles (codes expanded), then the epilogue: warp w reads lanes
+//          32 (w % 4) .., columns of quarter w / 4
+//   16-19  loaders: query rows of the next step, their lse
 //   20     MMA issuer
 // Tensor memory: two buffers of kN columns, one product's epilogue under the next one's
 // MMAs.
@@ -79,7 +80,7 @@ struct alignas(1024) SmemW {
   uint8_t k[kTiles][C::KTILE];                  // [tile][64-column block][token][128 bytes], swizzled
   float neg_lse[2][C::N];                       // -lse log2(e) of the stage's rows; -inf for rows that add nothing
   float row_scale[2][C::F32 ? C::N : 1];        // power of two of an fp32 row
-  uint64_t q_full[2], q_empty[2], l_full[2], l_empty[2], k_empty, d_full[2], d_empty[2], done;
+  uint64_t q_full[2], q_empty[2], l_full[2], l_empty[2], k_full, d_full[2], d_empty[2], done;
   int64_t scan[kTcThreads / 32];
   Share share;
   uint32_t tmem_base;
@@ -256,14 +257,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sm.q_full[i], kLoadWarps + (F32 ? 0 : 1));     // bf16: the copies' bytes too
+      mbar_init(&sm.q_full[i], F32 ? kLoadWarps : 1);   // (bf16: the copies' bytes)
       mbar_init(&sm.q_empty[i], 1);
       mbar_init(&sm.l_full[i], kLoadWarps);
       mbar_init(&sm.l_empty[i], kEpiWarps);             // (apart from the rows: their copy does not wait for the epilogue)
       mbar_init(&sm.d_full[i], 1);
       mbar_init(&sm.d_empty[i], kEpiWarps);
     }
-    mbar_init(&sm.k_empty, kEpiWarps);                  // (their last product is done: so are all before it)
+    mbar_init(&sm.k_full, kEpiWarps);
     mbar_init(&sm.done, 1);
     sm.abort = 0;
     sm.err = VC_OK;
@@ -304,6 +305,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
     constexpr uint32_t idesc = F32 ? idesc_f16(128, N) : idesc_bf16_f32(128, N);
     const uint64_t qd = desc_sw128(smem_u32(sm.q)), kd = desc_sw128(smem_u32(sm.k));
     do {
+      ok = warp_wait(&sm.k_full, seg & 1, abort);
       const int nt = tiles_of();
       for (int j = w.t0; ok && j < w.t1; ++j, ++step) {
         const int st = step & 1;
@@ -337,28 +339,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
     // ---- loaders
     const int t = threadIdx.x - 32 * kLoadWarp0;
     if (!F32) prefetch_tmap(&tmQ);
-    // 16 codes of a token a thread at a time, kB of them in flight
-    constexpr int VPR = D / 16, kVecs = kGroup * VPR / kLoadThreads, kB = 12;
-    static_assert(kVecs * kLoadThreads == kGroup * VPR && kVecs % kB == 0, "whole batches");
-    uint4 codes[kB];
-    auto fetch = [&](int batch) {
-      int pid[kB];
-      const int tok0 = w.u.rt * kGroup;
-#pragma unroll
-      for (int i = 0; i < kB; ++i) {
-        const int tok = (t + (batch * kB + i) * kLoadThreads) / VPR;
-        pid[i] = tok < w.u.kend ? load_page(s, c.n_pages, w.u.r, (tok0 + tok) / c.page, err) : -1;
-      }
-#pragma unroll
-      for (int i = 0; i < kB; ++i) {
-        const int v = t + (batch * kB + i) * kLoadThreads, tok = tok0 + v / VPR;
-        codes[i] = make_uint4(0, 0, 0, 0);
-        if (pid[i] >= 0)
-          codes[i] = __ldg(reinterpret_cast<const uint4*>(
-                               static_cast<const uint8_t*>(c.K_codes) +
-                               (((int64_t)pid[i] * c.Hkv + w.u.g) * c.page + tok % c.page) * D) + v % VPR);
-      }
-    };
     // -lse of the columns t, t + 128 of a step: row and head do not change from step to step
     constexpr int NL = N / kLoadThreads;
     int li[NL];
@@ -376,16 +356,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
       __syncwarp();
     };
     do {
-      // under the end of the unit before: half of the codes, the first step's rows and their lse
-      fetch(0);
       const Req8 q = w.u.q;
       const int b0 = line.first_block(q, w.u.rt * kGroup);
       const int dead = max(0, q.m - q.len);     // the surplus first rows are no tokens
-      if (!F32) {
-        ok = warp_wait(&sm.q_empty[step & 1], ((step >> 1) & 1) ^ 1, abort);
-        if (!ok) break;
-        send_rows(q.row0 + (b0 + w.t0) * RB, step & 1);
-      }
       auto fetch_lse = [&](int b) {
 #pragma unroll
         for (int k = 0; k < NL; ++k) {
@@ -405,38 +378,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
         lp[k] = a.lse + (int64_t)(q.row0 + li[k]) * a.Hq + w.u.g * G + (x - li[k] * G);
       }
       fetch_lse(w.t0);
-      ok = warp_wait(&sm.k_empty, (seg & 1) ^ 1, abort);
-      if (!ok) break;
-#pragma unroll 1
-      for (int batch = 0; batch < kVecs / kB; ++batch) {
-        if (batch > 0) fetch(batch);
-#pragma unroll
-        for (int i = 0; i < kB; ++i) {
-          const int v = t + (batch * kB + i) * kLoadThreads, tok = v / VPR, part = v % VPR;
-          const uint32_t b[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
-          uint32_t y[8];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            y[2 * k] = F32 ? e4m3x2_to_f16x2(b[k]) : e4m3x2_to_bf16x2(b[k]);
-            y[2 * k + 1] = F32 ? e4m3x2_to_f16x2(b[k] >> 16) : e4m3x2_to_bf16x2(b[k] >> 16);
-          }
-          uint8_t* tile = sm.k[tok / kKT];
-          *reinterpret_cast<uint4*>(tile + piece16<kKT>(tok % kKT, 2 * part)) = make_uint4(y[0], y[1], y[2], y[3]);
-          *reinterpret_cast<uint4*>(tile + piece16<kKT>(tok % kKT, 2 * part + 1)) = make_uint4(y[4], y[5], y[6], y[7]);
-        }
-      }
-      // (the issuer learns of it with the first step's rows, which this thread reports later)
-      fence_proxy_async();
       for (int b = w.t0; ok && b < w.t1; ++b, ++step) {
         const int st = step & 1, i0 = (b0 + b) * RB;
-        if (F32 || b > w.t0) {
-          ok = warp_wait(&sm.q_empty[st], ((step >> 1) & 1) ^ 1, abort);
-          if (!ok) break;
-        }
+        // (only who fills the stage waits: another could find the barrier two phases on)
+        if (F32 || warp == kLoadWarp0) ok = warp_wait(&sm.q_empty[st], ((step >> 1) & 1) ^ 1, abort);
+        if (!ok) break;
         uint8_t* dst = sm.q[st];
         if constexpr (!F32) {
-          if (b > w.t0) send_rows(q.row0 + i0, st);
-          if (lane == 0) mbar_arrive(&sm.q_full[st]);   // (K, with a unit's first rows)
+          send_rows(q.row0 + i0, st);
         }
         ok = warp_wait(&sm.l_empty[st], ((step >> 1) & 1) ^ 1, abort);
         if (!ok) break;
@@ -511,6 +460,47 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
     do {
       const int nt = tiles_of(), tok0 = w.u.rt * kGroup;
       const int b0 = line.first_block(w.u.q, tok0);
+      {
+        // K tiles: the unit before is done with them once all of these warps are here.  16 codes of a token a
+        // thread at a time, kB of them in flight
+        constexpr int VPR = D / 16, kB = kGroup * VPR / (32 * kEpiWarps);
+        static_assert(kB * 32 * kEpiWarps == kGroup * VPR, "whole turns");
+        const int t = threadIdx.x;
+        int pid[kB];
+        uint4 codes[kB];
+#pragma unroll
+        for (int i = 0; i < kB; ++i) {
+          const int x = (t + i * 32 * kEpiWarps) / VPR;
+          pid[i] = x < w.u.kend ? load_page(s, c.n_pages, w.u.r, (tok0 + x) / c.page, err) : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kB; ++i) {
+          const int v = t + i * 32 * kEpiWarps, x = tok0 + v / VPR;
+          codes[i] = make_uint4(0, 0, 0, 0);
+          if (pid[i] >= 0)
+            codes[i] = __ldg(reinterpret_cast<const uint4*>(
+                                 static_cast<const uint8_t*>(c.K_codes) +
+                                 (((int64_t)pid[i] * c.Hkv + w.u.g) * c.page + x % c.page) * D) + v % VPR);
+        }
+        named_sync(1, 32 * kEpiWarps);
+#pragma unroll
+        for (int i = 0; i < kB; ++i) {
+          const int v = t + i * 32 * kEpiWarps, x = v / VPR, part = v % VPR;
+          const uint32_t b[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+          uint32_t y[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            y[2 * k] = F32 ? e4m3x2_to_f16x2(b[k]) : e4m3x2_to_bf16x2(b[k]);
+            y[2 * k + 1] = F32 ? e4m3x2_to_f16x2(b[k] >> 16) : e4m3x2_to_bf16x2(b[k] >> 16);
+          }
+          uint8_t* tile = sm.k[x / kKT];
+          *reinterpret_cast<uint4*>(tile + piece16<kKT>(x % kKT, 2 * part)) = make_uint4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<uint4*>(tile + piece16<kKT>(x % kKT, 2 * part + 1)) = make_uint4(y[4], y[5], y[6], y[7]);
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.k_full);
+      }
       float fac[kTiles], acc[kTiles], low[kTiles], old[kTiles];
       int64_t slot[kTiles];                     // of the thread's token, -1 if it has none
 #pragma unroll
@@ -598,7 +588,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.k_empty);
       ++seg;
     } while (w.next(line, s, err));
   }

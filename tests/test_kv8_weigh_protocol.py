@@ -13,14 +13,14 @@ LOADERS, EPILOGUE = 4, 16
 def run(segments, seed, mistake=None):
     """segments: (steps, K tiles) of each unit's piece."""
     rnd = random.Random(seed)
-    q_full, q_empty = [Bar(LOADERS + 1) for _ in range(2)], [Bar() for _ in range(2)]
+    q_full, q_empty = [Bar(2) for _ in range(2)], [Bar() for _ in range(2)]
     l_full, l_empty = [Bar(LOADERS) for _ in range(2)], [Bar(EPILOGUE) for _ in range(2)]
     d_full, d_empty = [Bar() for _ in range(2)], [Bar(EPILOGUE) for _ in range(2)]
-    k_empty = Bar(EPILOGUE)
-    K, Q, lse = [None] * LOADERS, [None, None], [[None] * LOADERS for _ in range(2)]
+    k_full = Bar(EPILOGUE)
+    K, Q, lse = [None] * EPILOGUE, [None, None], [[None] * LOADERS for _ in range(2)]
     D, pipe, sums, flying = [None, None], [], [], []
-    meet = Bar(EPILOGUE)                        # the epilogue warps at a segment's end
-    parts = {}
+    start, meet = Bar(EPILOGUE), Bar(EPILOGUE)                        # the epilogue warps at a segment's end
+    parts, wrote = {}, set()
 
     def w(name, bar, phase):
         return None if mistake == name else (bar, phase)
@@ -30,17 +30,12 @@ def run(segments, seed, mistake=None):
         for seg, (n, _) in enumerate(segments):
             for j in range(n):
                 st = step & 1
-                yield w("q_empty", q_empty[st], (step >> 1) - 1)
-                need(all(b[0] != "P" or b[2] != st for b in pipe), "query rows written under a product")
+                if me == 0 or mistake == "all wait":
+                    yield w("q_empty", q_empty[st], (step >> 1) - 1)
                 if me == 0:
+                    need(all(b[0] != "P" or b[2] != st for b in pipe), "query rows written under a product")
                     flying.append(step)
-                if j == 0:
-                    # the first rows are on their way before the unit's K is
-                    yield w("k_empty", k_empty, seg - 1)
-                    need(not any(b[0] == "P" and b[3] < seg for b in pipe), "K written under a product")
-                    need(parts.get(seg - 1, EPILOGUE) == EPILOGUE, "K written while the quarters' sums lie there")
-                    K[me] = seg                 # (reported with the first step's rows)
-                q_full[st].arrive()
+                    q_full[st].arrive()
                 yield w("l_empty", l_empty[st], (step >> 1) - 1)
                 lse[st][me] = step
                 l_full[st].arrive()
@@ -49,6 +44,7 @@ def run(segments, seed, mistake=None):
     def issuer():
         step = prod = 0
         for seg, (n, nt) in enumerate(segments):
+            yield w("k_full", k_full, seg)
             for j in range(n):
                 st = step & 1
                 yield w("q_full", q_full[st], step >> 1)
@@ -62,6 +58,12 @@ def run(segments, seed, mistake=None):
     def epilogue(me):
         step = prod = 0
         for seg, (n, nt) in enumerate(segments):
+            start.arrive()
+            yield w("start", start, seg)
+            need(not any(b[0] == "P" for b in pipe), "K written under a product")
+            need(parts.get(seg - 1, 4) == 4, "K written while the quarters' sums lie there")
+            K[me] = seg
+            k_full.arrive()
             for j in range(n):
                 st = step & 1
                 yield w("l_full", l_full[st], step >> 1)
@@ -77,10 +79,15 @@ def run(segments, seed, mistake=None):
                 l_empty[st].arrive()
                 step += 1
             parts[seg] = parts.get(seg, 0)
+            need(not any(b[0] == "P" for b in pipe), "sums written over K under a product")
+            wrote.add((seg, me))
             meet.arrive()
-            yield meet, seg
-            parts[seg] += 1
-            k_empty.arrive()
+            yield w("meet", meet, seg)
+            parts.setdefault(seg, 0)
+            if me < 4:                          # the quarter that adds the others' sums
+                need(all((seg, x) in wrote for x in range(4, EPILOGUE)), "sums read before they were written")
+                yield None
+                parts[seg] += 1
 
     def execute(busy):
         if not pipe:
@@ -90,7 +97,7 @@ def run(segments, seed, mistake=None):
             q_empty[b[1]].arrive()
             return True
         _, d, st, seg, step, kt = b
-        need(K == [seg] * LOADERS, "a product of another unit's K")
+        need(K == [seg] * EPILOGUE, "a product of another unit's K")
         need(Q[st] == step, "a product of another step's rows")
         D[d] = (seg, step, kt)
         d_full[d].arrive()
@@ -121,7 +128,7 @@ def test_protocol_holds():
         run(_segments(seed), seed)
 
 
-@pytest.mark.parametrize("mistake", ["k_empty", "q_empty", "q_full", "d_empty", "d_full", "l_empty", "l_full"])
+@pytest.mark.parametrize("mistake", ["k_full", "start", "q_empty", "q_full", "d_empty", "d_full", "l_empty", "l_full", "meet", "all wait"])
 def test_mistakes_are_caught(mistake):
     caught = 0
     for seed in range(60):
