@@ -80,10 +80,14 @@ int viscache_norm_mrope_grad(const vc_rope* rope, const int32_t* positions, int 
  * The pages of a call's requests must be different ones (a page of two requests
  * would be written by both): requests that share a prefix's pages are weighed
  * in calls of their own.
- * Scores as in viscache_kv8_attention (fp32 rows as two fp16 numbers), sums in
- * fp32 in an order that the call's sizes, lengths and the device's SMs decide:
- * the same call gives the same bits.  A key that is not finite makes its token's
- * weight NaN.
+ * Rows enter the products as in viscache_kv8_attention (fp32 rows as two fp16
+ * numbers); bf16 rows of calls of many rows (more than 64 of a KV head per request on
+ * average) as they are, so that their values' products with codes have to stay below
+ * 2^127 there, and count as 0 below 2^-126.  Scores as there below 2^22.  Sums in fp32
+ * in an order that the call's sizes, lengths and the device's SMs decide: the same
+ * call gives the same bits.  A key that is not finite makes its token's weight NaN.
+ * After VC_ERR_DEVICE_TIMEOUT (prunekv_get_status) clear the workspace before a
+ * captured call is replayed with it.
  * Workspace: viscache_kv8_workspace_size(n_rows, Hq, Hkv, d), as for the
  * attention; device checks and prunekv_get_status too.
  * Errors: VC_ERR_INVALID_ARG, VC_ERR_WORKSPACE, VC_ERR_CUDA, and

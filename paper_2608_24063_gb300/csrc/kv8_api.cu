@@ -145,9 +145,15 @@ Kernel kernel_of(const vc_kv8& c, const vc_kv8_step& s, int dtype, int32_t Hq) {
   return two ? Kernel::kTc2 : Kernel::kTc1;
 }
 
-// viscache_kv8_weigh on tcgen05: more packed rows of a KV head per request on average
-// than the mma.sync kernel's fragments hold.
-constexpr int64_t kWeighTcRows = 16;
+// viscache_kv8_weigh on tcgen05: more packed rows of a KV head per request on average than
+// this.  The mma.sync kernel reads a chunk's codes once and its rows 16 at a time; the
+// other expands each K tile once however many rows there are.  d = 128, 8 KV heads, us on
+// mma.sync / tcgen05 (cold):
+//   bf16, 64 requests of 4096 tokens, 24 rows 113 / 259, 48 rows 169 / 259, 128 rows 384 / 261
+//   8 of 8192 tokens, 48 rows 58 / 72, 128 rows 118 / 73; one of 8192, 48 rows 20 / 30, 128 rows 34 / 30
+//   fp32, 64 of 4096, 24 rows 160 / 228, 48 rows 267 / 231; 8 of 8192, 24 rows 51 / 63, 48 rows 81 / 63
+//   one of 8192, 24 rows 20 / 28, 48 rows 28 / 28
+constexpr int64_t kWeighTcRows = 64, kWeighTcRowsF32 = 32;
 
 bool valid_heads(int32_t Hq, int32_t Hkv) { return Hkv >= 1 && Hq >= Hkv && Hq <= 4096 && Hq % Hkv == 0; }
 
@@ -371,7 +377,8 @@ int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, 
   a.flags = reinterpret_cast<uint64_t*>(base + w.o_flags);
   a.part = reinterpret_cast<float*>(base + w.o_o);
   // (a step there holds all heads of a group: 128 fit in both types)
-  const bool many = (int64_t)step->n_rows * (Hq / cache->Hkv) > kWeighTcRows * step->n_req && Hq / cache->Hkv <= 128;
+  const bool many = (int64_t)step->n_rows * (Hq / cache->Hkv) > (dtype == VC_F32 ? kWeighTcRowsF32 : kWeighTcRows) * step->n_req &&
+                    Hq / cache->Hkv <= 128;
   return cuda_status(many ? launch_kv8_weigh_tc(*cache, *step, dtype, a, st)
                           : launch_kv8_weigh(*cache, *step, dtype, a, st));
 }

@@ -35,12 +35,14 @@
 // A tile's terms are added in eight partial sums, tiles with a compensated sum, so 16384
 // rows cost no more bits than 16.
 //
-// 2048 rows over 32768 tokens, 64 / 8 heads of 128 (1.07 TFLOP, 4.3 G exponentials): 1.00 ms, 1.07
-// PFLOP/s, 56% of the cuBLAS rate; at the 1.5 GHz that the card holds under it a product takes 1740
-// clocks: its MMAs 1024, its exponentials 1190 (32 a clock would be 1024; measured alone).
-// Without exponentials 0.90 ms, without MMAs 0.99, with a quarter of the epilogue 0.66.  Eight
-// epilogue warps 1.05 ms; two groups of eight that take products in turn 1.14, four with
-// buffers of 128 columns 1.10; all of a warp's columns loaded at once 1.06.  One fp32 step
+// 2048 rows over 32768 tokens, 64 / 8 heads of 128 (1.07 TFLOP, 4.3 G exponentials): 0.93 ms, 1.16
+// PFLOP/s, 61% of the cuBLAS rate.  Bound by the epilogue: a product's MMAs take 1024 clocks, its
+// exponentials 1190 (measured alone), all of it about 1600 at the 1.5 GHz that the card holds
+// under it.  At 1.00 ms, without exponentials 0.90, without MMAs 0.99, with a quarter of the
+// epilogue 0.66; eight epilogue warps 1.05; two groups of eight that take products in turn
+// 1.14, four with buffers of 128 columns 1.10; all of a warp's columns loaded at once 1.06 ms.
+// Few steps a unit: 64 requests of 128 rows over 4096 tokens 261 us, 7 us a unit, a chain of its
+// codes, products, sums and old weights (K expanded by the four loaders 353 us).  One fp32 step
 // holds 128 rows in two parts.
 #include "kernels.h"
 #include "kv8.cuh"

@@ -128,14 +128,29 @@ def test_many_rows(case, causal, dtype):
     Case(*case, dtype, causal).check()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", [([300, 90], [2, 1], 160, 1, 64, 16), ([200], [130], 128, 1, 64, 64), ([500], [70], 65, 1, 128, 32)],
+                         ids=str)
+def test_wide_groups(case, dtype):
+    # query heads of a group: more than a step of the many-rows kernel holds, as many as it holds, just over half
+    Case(*case, dtype).check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows", [16, 17, 33, 64, 65, 80])
+def test_rows_around_the_kernels_borders(rows, dtype):
+    Case([150, 333], [rows, rows], 1, 1, 128, 16, dtype).check()
+
+
 @pytest.mark.parametrize("causal", [True, False])
 def test_more_rows_than_tokens(causal):
     # the surplus first rows are no tokens: they add nothing, whatever their lse says
-    c = Case([3, 20], [6, 40], 4, 2, 64, 16, F32, causal)
-    c.check()
-    dead = ~np.isfinite(c.lse)
-    c.lse[dead] = -3.0
-    c.check()
+    for rows in ([6, 40], [90, 140]):
+        c = Case([3, 20], rows, 4, 2, 64, 16, F32, causal)
+        c.check()
+        dead = ~np.isfinite(c.lse)
+        c.lse[dead] = -3.0
+        c.check()
 
 
 def test_rows_that_see_nothing_add_nothing():
