@@ -13,9 +13,9 @@
 // rope.cu.
 //
 // 32768 rows of 72 heads of 128 in bf16 (1.21 GB): 209 us, 5.8 TB/s, 87% of a plain copy's rate (the
-// rotation alone: 198 us).  Gradient of 12544 rows of 32 heads (308 MB): 84 us, 3.7 TB/s, 55%: 16
-// warps an SM at 120 registers keep too little in flight, and more rows ahead of each thread
-// (89 us, cold, as without) or smaller blocks (103) do not help.  16 rows of 32 heads: a launch.
+// rotation alone: 198 us).  Gradient of 12544 rows of 32 heads (308 MB): 82 us, 3.8 TB/s, 57%: 16
+// warps an SM at 116 registers keep too little in flight; two rows ahead of each thread are no
+// faster, smaller blocks slower (cold 89 and 103 against 89).  16 rows of 32 heads: a launch.
 //
 // Sums of squares that pass fp32's range are taken again of values times 2^-70: the
 // branch costs nothing where it is not taken.
@@ -174,7 +174,7 @@ template <typename T, int D, bool ADJ>
 __global__ void __launch_bounds__(kThreads) norm_mrope_grad_kernel(const __grid_constant__ RopeArgs a,
                                                                    const __grid_constant__ NormRopeGrad p) {
   constexpr int SLOTS = D / 16, GROUPS = kThreads / SLOTS, HALF = D / 2, RB = kGradRows;
-  __shared__ float2 cs[RB][HALF];
+  __shared__ float2 cs[RB][HALF];                // frequency 8 slot + i at i * SLOTS + slot: no two slots on a bank
   __shared__ float sums[kThreads / 32][D];
   const int t = threadIdx.x, slot = t % SLOTS, grp = t / SLOTS;
   const bool isk = (int)blockIdx.x >= p.nq;
@@ -215,7 +215,8 @@ __global__ void __launch_bounds__(kThreads) norm_mrope_grad_kernel(const __grid_
     load(r0, rows, lr0, h0);
     __syncthreads();                            // the angles before are read
     for (int i = t; i < RB * HALF; i += kThreads)
-      if (i % HALF < a.half && r0 + i / HALF < a.n_rows) cs[i / HALF][i % HALF] = angle(a, i % HALF, r0 + i / HALF);
+      if (i % HALF < a.half && r0 + i / HALF < a.n_rows)
+        cs[i / HALF][i % 8 * SLOTS + i % HALF / 8] = angle(a, i % HALF, r0 + i / HALF);
     __syncthreads();
     int lr = lr0, h = h0;
     for (int left = rows * H; left > 0; left -= GROUPS) {     // (the same for the block: shuffles need whole warps)
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(kThreads) norm_mrope_grad_kernel(const __grid_
         float c[8], s[8], u[8], v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float2 w = cs[row_of][slot * 8 + i];
+          const float2 w = cs[row_of][i * SLOTS + slot];
           c[i] = w.x;
           s[i] = w.y;                           // (the table holds -sin: R^T)
         }
