@@ -9,6 +9,9 @@ layer's share of the visual tokens; its output goes into the cache that serves t
 lies ([Hkv][B_l][d], read in place), the text rows behind it.  Decoding replays one captured
 graph: rotate, append, attend in every layer, for all requests, with the lengths, the positions
 and the tokens on the device.  viscache_kv8_read gives a layer's rows back in 16 bits.
+
+With a budget the cache stops growing: each step's attention is added up with viscache_kv8_weigh
+and viscache_kv8_evict keeps the tokens of each layer and KV head that received most of it.
 """
 import os
 import sys
@@ -41,8 +44,8 @@ class Model:
         vc.viscache_mrope(self.rope, positions, q, k, q_out=q, k_out=k)
         return q, k, v
 
-    def attend(self, layer, x, q, cache, step, ws):
-        out = vc.viscache_kv8_attention(cache, step, q, ws=ws)
+    def attend(self, layer, x, q, cache, step, ws, lse=None):
+        out = vc.viscache_kv8_attention(cache, step, q, lse=lse, ws=ws)
         return x + out.view(x.shape[0], -1) @ self.w_o[layer]
 
     def pool(self, pages):
@@ -83,9 +86,9 @@ def prefill(m, x, positions):
 class Server:
     """Requests in the 8-bit cache of every layer, decoded together."""
 
-    def __init__(self, m, requests, retain=(1, 5), room=64):
-        """requests: (hidden rows, positions, visual tokens) of each."""
-        self.m, self.n = m, len(requests)
+    def __init__(self, m, requests, retain=(1, 5), room=64, budget=0):
+        """requests: (hidden rows, positions, visual tokens) of each; budget: the most tokens of a layer (0: all)."""
+        self.m, self.n, self.budget = m, len(requests), budget
         plans = [vc.viscache_plan_budgets(m.L, n, *retain)[0] for _, _, n in requests]
         text = [x.shape[0] - n for x, _, n in requests]
         self.lens = [[b[layer] + t for b, t in zip(plans, text)] for layer in range(m.L)]
@@ -107,6 +110,14 @@ class Server:
         self.steps = [m.step(self.table, [n + 1 for n in self.lens[layer]], [1] * self.n) for layer in range(m.L)]
         self.ws = m.workspace(self.n)
         self.graph = None
+        if budget:
+            # what every token of the prompt starts from: nothing yet
+            self.weights = [torch.zeros(sum(need), m.Hkv, m.page, device=m.device) for _ in range(m.L)]
+            self.lse = torch.empty(self.n, m.Hq, device=m.device)
+            self.keep = torch.full((self.n,), budget, dtype=torch.int32, device=m.device)
+            self.kept = torch.empty(self.n, m.Hkv, budget, dtype=torch.int32, device=m.device)
+            self.evict_ws = torch.empty(vc.viscache_kv8_evict_workspace_size(self.n, m.Hkv), dtype=torch.uint8,
+                                        device=m.device)
 
     def admit(self, r, kept, n, text, retain):
         """A prefilled request: its visual tokens compressed, then text, into the cache."""
@@ -134,8 +145,13 @@ class Server:
         for layer in range(m.L):
             q, k, v = m.qkv(layer, x, self.positions)
             vc.viscache_kv8_append(self.pools[layer], self.steps[layer], k, v, ws=self.ws)
-            x = m.attend(layer, x, q, self.pools[layer], self.steps[layer], self.ws)
-        self.x.copy_(x)                         # (a model would sample a token and look its row up)
+            cache, step = self.pools[layer], self.steps[layer]
+            x = m.attend(layer, x, q, cache, step, self.ws, self.lse if self.budget else None)
+            if self.budget:
+                vc.viscache_kv8_weigh(cache, step, q, self.lse, self.weights[layer], ws=self.ws)
+                vc.viscache_kv8_evict(cache, step, self.weights[layer], self.keep, self.budget, sink=4, recent=16,
+                                      kept=self.kept, new_lens=step.tensors[1], ws=self.evict_ws)
+        self.x.copy_(x)                         # (a model would draw a token with viscache_sample and look its row up)
         self.positions += 1
         for step in self.steps:
             step.tensors[1].add_(1)

@@ -509,7 +509,7 @@ __device__ __forceinline__ int2 share_buckets(Row& row, float p) {
   float2* word = reinterpret_cast<float2*>(sm.warp_mass);
   __syncthreads();
   if (lane == 31) word[warp] = make_float2(il, ih);
-  if (threadIdx.x == 0) sm.warp_count[0] = sm.warp_count[1] = kBuckets - 1;
+  if (threadIdx.x == 0) sm.warp_count[0] = sm.warp_count[1] = kBuckets - 2;      // (the last that counts anything)
   __syncthreads();
   float bl = il - ls, bh = ih - hs, tl = 0.f, th = 0.f;
   for (int w = 0; w < kWarps; ++w) {
@@ -717,7 +717,7 @@ __device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uin
       upto_sum[r] = before;
       // the first to reach top_p's share, and the first below min_p (at least one stays)
       if (by_p && from < need && need <= before) sm.found[0] = r + 1;
-      if (r > 0 && weight[r] < least && weight[r - 1] >= least) sm.found[1] = r;
+      if (r > 0 && weight[r] < least) atomicMin(reinterpret_cast<unsigned long long*>(&sm.found[1]), (unsigned long long)r);
     }
   }
   __syncthreads();

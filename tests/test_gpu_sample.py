@@ -130,6 +130,15 @@ def test_flat_rows_of_the_largest_vocabulary():
     _check(x, rng.random(4).tolist(), [1.0] * 4, k=[200000] * 4, p=[0.9] * 4)
 
 
+def test_tokens_at_the_end_of_what_is_counted():
+    # thousands of tokens 2^-63.97 of the best, where a weight is nothing: they are on no list
+    x = torch.full((4, 9000), -63.97 * math.log(2.0))
+    x[:, 17] = 0.0
+    x[:, 4000:4500] = -1.5
+    _check(x, [0.001, 0.3, 0.9, 0.999], [1.0] * 4, p=[0.99999, 0.9999999, 0.5, 0.99])
+    _check(x, [0.001, 0.3, 0.9, 0.999], [1.0] * 4, k=[1, 500, 501, 8000], p=[0.99999, 1.0, 0.5, 0.99])
+
+
 def test_the_share_of_each_token():
     # u walks over [0, 1): how often a token comes is its probability, to one step
     x = torch.tensor([[1.0, 0.0, -1.0, 2.0, 0.5]])
