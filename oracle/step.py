@@ -105,6 +105,7 @@ def sample(x, u: float, T: float, top_k: int = 0, top_p: float = 1.0, min_p: flo
         return -1, math.nan
     if not T > 0:
         return int(np.argmax(x)), 0.0
+    T = max(T, 2.0 ** -127)                                         # (no less counts)
     with np.errstate(invalid="ignore"):
         w = np.where(x == M, 1.0, np.exp((x - M) / T))
     w[(x == -np.inf) | ((M == np.inf) & (x != M))] = 0.0            # whatever T is

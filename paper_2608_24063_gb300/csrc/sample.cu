@@ -814,12 +814,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   Weights wt;
   wt.small = temp > 0x1p90f ? 0x1p-90f : 1.f;
   {
-    // log2(e) / T in two parts, in fp32 alone (fp64 is slow here); a T so small that the factor is no fp32 number: 0
-    // times it has to be 0
+    // log2(e) / T in two parts, in fp32 alone (fp64 is slow here); T no less than 2^-127, so that it is an fp32 number
     constexpr float kHi = 1.44269502f, kLo = 1.92596303e-8f;
-    const float T1 = temp * wt.small;
-    wt.ch = greedy || T1 == INFINITY ? 0.f : fminf(__fdiv_rn(kHi, T1), 3e38f);
-    wt.cl = wt.ch == 0.f || wt.ch == 3e38f ? 0.f : __fdiv_rn(fmaf(-wt.ch, T1, kHi) + kLo, T1);
+    const float T1 = fmaxf(temp, 0x1p-127f) * wt.small;
+    wt.ch = greedy || T1 == INFINITY ? 0.f : __fdiv_rn(kHi, T1);
+    wt.cl = wt.ch == 0.f ? 0.f : __fdiv_rn(fmaf(-wt.ch, T1, kHi) + kLo, T1);
   }
   M = logit_of<T>((uint32_t)cluster_max(row, key_of<T>(M)));
   if (M == INFINITY) {

@@ -139,6 +139,15 @@ def test_tokens_at_the_end_of_what_is_counted():
     _check(x, [0.001, 0.3, 0.9, 0.999], [1.0] * 4, k=[1, 500, 501, 8000], p=[0.99999, 1.0, 0.5, 0.99])
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_temperatures_below_the_least(dtype):
+    # a positive temperature below 2^-127 counts as 2^-127: logits of that size tell them apart
+    x = (torch.randn(12, 300, dtype=torch.float64, generator=torch.Generator().manual_seed(6)) * 1e-38).to(dtype)
+    T = [1e-45, 1e-42, 1e-39, 4e-39, 5.8e-39, 2.0 ** -127, 6e-39, 1e-38, 1e-37, 1e-45, 1e-40, 2.0 ** -126]
+    _check(x, [(i + 0.5) / 12 for i in range(12)], T)
+    _check(x, [(i + 0.5) / 12 for i in range(12)], T, p=[0.8] * 12)
+
+
 def test_the_share_of_each_token():
     # u walks over [0, 1): how often a token comes is its probability, to one step
     x = torch.tensor([[1.0, 0.0, -1.0, 2.0, 0.5]])
