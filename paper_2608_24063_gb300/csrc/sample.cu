@@ -11,13 +11,14 @@
 // wrong, and rows have up to 262144 borders, so weights are computed to about 38 bits
 // (pairs of fp32 numbers, a table of 2^(-i/64) and a polynomial of degree 4) and added as
 // 64-bit whole numbers: exact in any order, so neither atomics nor the split over blocks
-// change a result.  Such a weight costs some forty instructions, and what bounds large
-// batches is that arithmetic, so it is done as rarely as the cuts allow:
+// change a result.  Such a weight costs some sixty instructions, and what bounds large
+// batches is that arithmetic, so it is done as rarely as the cuts allow, and for bf16 logits
+// once for each value where there are many of them:
 //   - without filters once for each token;
 //   - with filters, the tokens are counted by buckets of 1/16 in z first (no weight).  What
 //     top-k keeps, and where top-p's cut can lie (a bucket's weights differ by 4.4%), follows
-//     from the counts.  If that is kMostListed tokens or fewer, they are listed, one block orders
-//     them by counting and does the rest on the list; for top-p alone the sum of all
+//     from the counts.  If that is kMostListed tokens or fewer, they are listed, one block puts
+//     them in order and does the rest on the list; for top-p alone the sum of all
 //     weights is taken once;
 //   - a larger nucleus: the sums of all weights and of those in buckets before the cut's
 //     are taken in one pass, by runs of tokens, and the cut is narrowed by counts of ever finer
@@ -27,10 +28,12 @@
 // holds the token looks through its run.
 //
 // 256 rows of 131072 in bf16, a fifth each greedy, all filters, none, and two of top-p alone with nuclei of
-// thousands (67 MB): 227 us, bound by the weights' arithmetic and the clusters' meetings, a plain read
-// 10 us.  64 rows of 50001 without filters 18 us, one row of 32000 with all of them 14 us, a chain of
+// thousands (67 MB): 138 us, bound by the passes' instructions and the clusters' meetings, a plain read
+// 10 us.  64 rows of 50001 without filters 18 us, one row of 32000 with all of them 13 us, a chain of
 // eight steps between blocks.  In place of the cuts from counts, histograms of weights by 64-bit
 // atomics: 441, 31 and 52 us.
+#include <cstddef>
+
 #include "kernels.h"
 #include "kv8_sched.cuh"
 #include "profile.h"
@@ -47,7 +50,15 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kBuckets = 1024;
 constexpr float kPerZ = 16.f;                   // buckets of 1 in z: z < 64
 constexpr int kTableBits = 48;
+constexpr int kCopies = 8;                      // of the table (one: 3 to 6% slower, lanes wait for one another's banks)
+// Vectors of a slice from which the weights of bf16 logits are taken from a table.  Without filters, with it and
+// without, us: 500 vectors (a row of 32000) 14.4 and 14.4, 1000 (64 rows of 32000) 16.7 and 18.8, 4096 (64 of
+// 131072) 27.3 and 39.3; with top_p the last 61 and 74.
+constexpr int kTableFrom = 512;
 constexpr int kMostListed = 1024;
+// Lists up to here are put in order by counting, longer ones by a sort.  A row of 32000, us: 10 tokens 14.5 and 16.5,
+// 100 16.7 and 18.8, 200 18.5 and 20.8, 256 20.9 and 21.0, 400 28.7 and 22.2.
+constexpr uint32_t kFew = 192;
 constexpr int kMostBlocks = 8;                  // of a row
 
 // 2^(48 - i / 64), rounded
@@ -80,7 +91,7 @@ struct Weights {
   float M, ch, cl;                              // the maximum times `small`; log2(e) / (T small) = ch + cl
   float small;                                  // 1; 2^-90 where T is past 2^90: then M - x stays in range
   int q;                                        // a weight of 1 is 2^q
-  const Power* table;
+  const Power* table;                           // the lane's copy
 
   __device__ __forceinline__ uint64_t one() const { return (uint64_t)1 << q; }
   // z to fp32, never decreasing as x falls; infinite (or NaN, of an infinite T) for -inf
@@ -95,7 +106,7 @@ struct Weights {
     const float t = fmaf(zh, 64.f, kMagic);
     const float g = fmaf(t - kMagic, -1.f / 64.f, zh);          // exact, |g| <= 1/128
     const int j = __float_as_int(t) - kMagicBits;
-    const Power power = table[j & 63];
+    const Power power = table[(j & 63) * kCopies];
     // 2^-(g + zl) = e^-y, y = yh + yl
     constexpr float kLn2 = 0.693147182f, kLn2Lo = -1.904654323e-9f;
     const float yh = g * kLn2;
@@ -128,7 +139,7 @@ __device__ __forceinline__ float logit_of(uint32_t k) {
 
 // What a row's blocks share.
 struct alignas(16) Shared {
-  Power table[64];
+  Power table[64 * kCopies];
   uint64_t mass[2][kBuckets], mass_all[kBuckets];       // the block's, by turn; the cluster's
   uint32_t count[2][kBuckets], count_all[kBuckets];
   uint64_t warp_mass[kWarps];
@@ -136,8 +147,7 @@ struct alignas(16) Shared {
   uint64_t words[kWarps][3];
   uint64_t mine[8][4];                                  // what the block tells the others, by turn
   uint64_t found[4];
-  uint32_t listed;                                      // the block's tokens on the list
-  uint32_t list_key[kMostListed], list_index[kMostListed];
+  uint32_t listed;                                      // the block's tokens on the list (in mass[1])
 };
 
 static_assert(sizeof(Shared) % 16 == 0, "the slice behind it is read in vectors");
@@ -645,13 +655,13 @@ __device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uin
                                           float u, int32_t* token, float* logprob) {
   Shared& sm = *row.sm;
   const int t = threadIdx.x;
+  // words of key and ~index: the block's, then all in order
+  uint64_t *list = sm.mass[1], *order = sm.mass[0];
   if (t == 0) sm.listed = 0;
   __syncthreads();
   each<T>(data, vecs, [&](float x, int e) {
     if (wt.z_of(x) * kPerZ < (float)(upto + 1)) {
-      const uint32_t at = atomicAdd(&sm.listed, 1u);
-      sm.list_key[at] = key_of<T>(x);
-      sm.list_index[at] = (uint32_t)(index0 + e);
+      list[atomicAdd(&sm.listed, 1u)] = (uint64_t)key_of<T>(x) << 32 | (uint32_t)~(index0 + e);
     }
   });
   row.sync();
@@ -663,44 +673,59 @@ __device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uin
   static_assert(kMostBlocks <= kWarps, "a warp for each block");
   if (from > 0 && from < row.C) {
     const uint32_t m = __shfl_sync(0xffffffffu, count, from), at = __shfl_sync(0xffffffffu, ends, from) - m;
-    for (uint32_t i = lane; i < m; i += 32) {
-      sm.list_key[at + i] = row.read(&sm.list_key[i], from);
-      sm.list_index[at + i] = row.read(&sm.list_index[i], from);
-    }
+    for (uint32_t i = lane; i < m; i += 32) order[at + i] = row.read(&list[i], from);
   }
-  __syncthreads();
-  // in order: a token's place is the number of those before it
-  uint64_t* weight = sm.mass[0];
-  uint64_t* upto_sum = sm.mass[1];
-  uint32_t *index = sm.count[0], *key_in_order = sm.count[1];
+  const uint32_t own = __shfl_sync(0xffffffffu, count, 0);
   constexpr int per = kMostListed / kThreads;
-  static_assert(kMostListed <= kBuckets, "the histograms' words hold the list in order");
+  static_assert(kMostListed <= kBuckets && per == 2, "the histograms' words hold the list, a thread a pair of it");
 #pragma unroll
   for (int i = 0; i < per; ++i) {
-    const uint32_t me = t + i * kThreads;
-    if (me >= n) break;
-    const uint32_t key = sm.list_key[me], at = sm.list_index[me];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) {
-      const uint32_t o = sm.list_key[j];
-      rank += o > key || (o == key && sm.list_index[j] < at) ? 1u : 0u;
-    }
-    weight[rank] = wt.of(logit_of<T>(key));
-    index[rank] = at;
-    key_in_order[rank] = key;
+    const uint32_t e = t + i * kThreads;
+    if (e < own) order[e] = list[e];
+    else if (e >= n) order[e] = 0;
   }
   __syncthreads();
+  uint64_t* upto_sum = sm.mass[1];
+  const bool few = n <= kFew;
+  if (few) {
+    // (a token's place is the number of those before it)
+    const uint64_t me = order[t];
+    uint32_t place = 0;
+    if (t < (int)n)
+      for (uint32_t j = 0; j < n; ++j) place += order[j] > me ? 1u : 0u;
+    __syncthreads();
+    if (t < (int)n) order[place] = me;
+    __syncthreads();
+  } else {
+    // a bitonic sort, whose steps of 32 and less stay inside a warp's 64 words
+    const uint32_t most = 2u << (31 - __clz((int)(n - 1)));
+    for (uint32_t size = 2; size <= most; size *= 2) {
+      for (uint32_t d = size / 2; d > 0; d /= 2) {
+        if ((uint32_t)t < most / 2) {
+          const uint32_t e = 2 * t - (t & (d - 1));
+          const uint64_t x = order[e], y = order[e + d];
+          if ((x < y) == ((e & size) == 0)) {
+            order[e] = y;
+            order[e + d] = x;
+          }
+        }
+        if (d > 32 || (d == 1 && size >= 64)) __syncthreads();
+        else __syncwarp();
+      }
+    }
+  }
   const uint32_t nk = min(n, k);
   uint64_t mine[per], sum = 0;
 #pragma unroll
   for (int i = 0; i < per; ++i) {
     const uint32_t r = t * per + i;
-    mine[i] = r < nk ? weight[r] : 0;
+    mine[i] = r < nk ? wt.of(logit_of<T>((uint32_t)(order[r] >> 32))) : 0;
     sum += mine[i];
   }
   const uint64_t incl = scan_warp(sum);
   if ((t & 31) == 31) sm.warp_mass[t >> 5] = incl;
   if (t == 0) sm.found[0] = sm.found[1] = nk;
+  for (int i = t; i < kBuckets; i += kThreads) sm.mass_all[i] = 0;
   __syncthreads();
   uint64_t before = incl - sum, all = 0;
   for (int w = 0; w < kWarps; ++w) {
@@ -717,20 +742,55 @@ __device__ __forceinline__ void from_list(Row& row, const Weights& wt, const uin
       upto_sum[r] = before;
       // the first to reach top_p's share, and the first below min_p (at least one stays)
       if (by_p && from < need && need <= before) sm.found[0] = r + 1;
-      if (r > 0 && weight[r] < least) atomicMin(reinterpret_cast<unsigned long long*>(&sm.found[1]), (unsigned long long)r);
+      if (r > 0 && mine[i] < least) atomicMin(reinterpret_cast<unsigned long long*>(&sm.found[1]), (unsigned long long)r);
     }
   }
   __syncthreads();
   const uint32_t kept = (uint32_t)min(sm.found[0], sm.found[1]);
   const uint64_t sum_kept = upto_sum[kept - 1];
   const uint64_t target = target_of(u, sum_kept);
-  for (uint32_t r = t; r < kept; r += kThreads) {
-    const uint32_t at = index[r];
-    uint64_t cum = 0;
-    for (uint32_t j = 0; j < kept; ++j) cum += index[j] <= at ? weight[j] : 0;
-    if (target < cum && target >= cum - weight[r])
-      write_token(wt, at, weight[r], sum_kept, wt.z_of(logit_of<T>(key_in_order[r])) * 0.693147182f, token, logprob);
+  uint32_t at[per];
+#pragma unroll
+  for (int i = 0; i < per; ++i) {
+    const uint32_t r = t * per + i;
+    at[i] = r < kept ? ~(uint32_t)order[r] : 0xffffffffu;
   }
+  auto write = [&](int i) {
+    write_token(wt, at[i], mine[i], sum_kept, wt.z_of(logit_of<T>((uint32_t)(order[t * per + i] >> 32))) * 0.693147182f,
+                token, logprob);
+  };
+  if (few) {
+#pragma unroll
+    for (int i = 0; i < per; ++i) sm.mass_all[t * per + i] = mine[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < per; ++i) {
+      if (at[i] == 0xffffffffu) break;
+      uint64_t cum = 0;
+      for (uint32_t j = 0; j < kept; ++j) cum += ~(uint32_t)order[j] <= at[i] ? sm.mass_all[j] : 0;
+      if (target < cum && target >= cum - mine[i]) write(i);
+    }
+    return;
+  }
+  // first the 256 indexes that hold it, then it
+  static_assert(kSampleMaxVocab <= 256 * kBuckets, "a bucket for each 256 indexes");
+#pragma unroll
+  for (int i = 0; i < per; ++i)
+    if (at[i] != 0xffffffffu)
+      atomicAdd(reinterpret_cast<unsigned long long*>(&sm.mass_all[at[i] >> 8]), (unsigned long long)mine[i]);
+  __syncthreads();
+  Place block, one;
+  find_place(row, true, target + 1, block);
+  for (int i = t; i < kBuckets; i += kThreads) sm.mass_all[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < per; ++i)
+    if (at[i] != 0xffffffffu && (int)(at[i] >> 8) == block.bucket) sm.mass_all[at[i] & 255] = mine[i];
+  __syncthreads();
+  find_place(row, true, target + 1 - block.mass, one);
+#pragma unroll
+  for (int i = 0; i < per; ++i)
+    if (at[i] == (uint32_t)(block.bucket << 8 | one.bucket)) write(i);
 }
 
 template <typename T>
@@ -747,11 +807,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   row.told = 0;
   row.sm = &sm;
   const int r = (int)blockIdx.x / a.C;
-  if (t < 64) {
-    const uint64_t x = kPowers[t];
+  {
+    // a copy for each lane of a quarter warp, which is what loads 16 bytes at a time: on banks of its own
+    static_assert(kThreads == 64 * kCopies, "a thread for each");
+    const uint64_t x = kPowers[t / kCopies];
     sm.table[t] = {(float)(uint32_t)(x >> 25) * 0x1p-23f, (float)(uint32_t)(x & 0x1ffffffu) * 0x1p-48f,
                    (int64_t)x + ((int64_t)kMagicBits << 19) - ((int64_t)kMagicBits << 11)};
   }
+
+  // weights of bf16 logits by their bits, in the histograms' words while these are not in use: of each sign the
+  // kSigned magnitudes up to the largest that counts
+  constexpr int kSigned = 3 * kBuckets / 2, kNoTable = 1 << 24;
+  static_assert(offsetof(Shared, mass_all) == offsetof(Shared, mass) + sizeof(Shared::mass), "one table");
+  uint64_t* const by_bits = reinterpret_cast<uint64_t*>(smem + offsetof(Shared, mass));
+  int top_bits = kNoTable;
 
   // (1) the slice: vectors of 16 bytes from the row's first byte rounded down; what is not
   // the row's, and NaN, as -inf
@@ -838,12 +907,35 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   }
   wt.M = M * wt.small;
   wt.q = a.q;
-  wt.table = sm.table;
+  wt.table = sm.table + (t & (kCopies - 1));
   const int32_t k = a.top_k ? __ldg(a.top_k + r) : 0;
   const float p = a.top_p ? __ldg(a.top_p + r) : 1.f;
   const float mp = a.min_p ? __ldg(a.min_p + r) : 0.f;
   float u = __ldg(a.u + r);
   u = u > 0.f ? u : 0.f;
+
+  auto fill_table = [&]() {
+    if constexpr (sizeof(T) == 2) {
+      if (a.vecs < kTableFrom) return;
+      // (a logit 64 in z below the maximum has no weight, and one past the largest magnitude here is further below)
+      const float largest = wt.ch > 0.f && wt.small == 1.f ? fmaxf(fabsf(M), fabsf(M - __fdiv_rn(64.f, wt.ch))) : INFINITY;
+      top_bits = min((int)(__float_as_uint(largest) >> 16) + 1, 0x7f80);
+      for (int i = t; i < 2 * kSigned; i += kThreads) {
+        const int bits = top_bits - (i < kSigned ? i : i - kSigned);
+        const float x = __uint_as_float((uint32_t)max(bits, 0) << 16 | (i < kSigned ? 0u : 0x80000000u));
+        by_bits[i] = x <= M ? wt.of(x) : 0;
+      }
+      __syncthreads();
+    }
+  };
+  auto weight_of = [&](float x) -> uint64_t {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t b = __float_as_uint(x);
+      const int i = top_bits - (int)(b >> 16 & 0x7fffu);
+      if (i < kSigned) return i < 0 ? 0 : by_bits[i + (b >> 31 ? kSigned : 0)];
+    }
+    return wt.of(x);
+  };
 
   // the cuts
   uint64_t least = 1;                           // weights below it are not kept
@@ -919,25 +1011,29 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
       } else if (by_p) {
         const int2 b = share_buckets(row, p);
-        uint64_t n = 0, total = 0, above = 0, hi = 0, lo = 0;
+        uint64_t n = 0, total = 0, above = 0;
+        uint32_t hi = 0, lo = 0;                // the largest key and ~key
         for (int i = t; i <= b.y; i += kThreads) n += sm.count_all[i];
         n = block_sum(sm, n);
         const bool few = n <= kMostListed;
         // all weights, those before the cut's buckets, and the keys of those buckets
+        const float z0 = few ? -1.f : (float)b.x, z1 = few ? -1.f : (float)(b.y + 1);
+        const bool all = least == 1;
+        fill_table();
         walk<T>(data, v0, v1, 1, [&](float x, int) {
-          const uint64_t w = wt.of(x);
-          total += w;
-          if (few || w == 0) return;
+          const uint64_t w = weight_of(x);
           const float z = wt.z_of(x) * kPerZ;
-          if (z < (float)b.x) {
+          total += w;
+          if (z < z0) {
             above += w;
-            sum += w >= least ? w : 0;
-          } else if (z < (float)(b.y + 1)) {
-            hi = max(hi, (uint64_t)key_of<T>(x));
-            lo = max(lo, (uint64_t)(~key_of<T>(x)));
+            if (!all && w >= least) sum += w;
+          } else if (z < z1) {
+            hi = max(hi, key_of<T>(x));
+            lo = max(lo, ~key_of<T>(x));
           }
         });
-        uint64_t keys = hi << 32 | lo;
+        if (all) sum = above;
+        uint64_t keys = (uint64_t)hi << 32 | lo;
         cluster_words(row, total, above, keys, true);
         if (few) {
           from_list<T>(row, wt, data, vecs, index0, b.y, 0xffffffffu, true, p, total, least, u, token, logprob);
@@ -987,8 +1083,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           if (key_of<T>(x) <= top) sum += weight(x, tie);
         });
       }
-      else if (ck == 0 && least == 1)
-        walk<T>(data, v0, v1, 1, [&](float x, int) { sum += wt.of(x); });
+      else if (ck == 0) {
+        fill_table();
+        walk<T>(data, v0, v1, 1, [&](float x, int) {
+          const uint64_t w = weight_of(x);
+          sum += w >= least ? w : 0;
+        });
+      }
       else
         walk<T>(data, v0, v1, 1, [&](float x, int) { sum += weight(x, tie); });
       const uint64_t total = cluster_sum(row, sum, &before);

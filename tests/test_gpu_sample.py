@@ -140,6 +140,36 @@ def test_tokens_at_the_end_of_what_is_counted():
 
 
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [1500, 262144])
+def test_lists_of_every_length(vocab, dtype):
+    # what top-k keeps is put in order: lengths around each power of two, with ties, drawn at both ends and between
+    ks = [k for n in (2, 4, 32, 64, 128, 256, 512, 1024) for k in (n - 1, n, n + 1)]
+    u = np.random.default_rng(9).random(len(ks))
+    u[::5], u[1::5] = 0.0, 0.9999999
+    x = _logits(len(ks), vocab, dtype, 10, spread=1.0)
+    if dtype == F32:
+        x[::2] = (x[::2] * 16).round() / 16
+    _check(x, u.tolist(), [1.0, 8.0] * (len(ks) // 2), ks)
+    _check(x, u.tolist(), [1.0, 8.0] * (len(ks) // 2), ks, [0.97, 0.5, 0.9999] * (len(ks) // 3))
+
+
+@pytest.mark.parametrize("p", [None, 0.9])
+def test_long_rows_of_every_range(p):
+    # rows long enough for the weights of bf16 logits to be looked up: signs, ranges and temperatures of every kind
+    vocab, rng = 131072, np.random.default_rng(12)
+    base = rng.standard_normal(vocab)
+    rows = [base * 3, -np.abs(base) - 5, base * 1e-3, base * 1e-20, np.abs(base) * 100, base * 0 - 7, base * 1e30,
+            base * 0.01 + 50, base.copy(), base.copy(), base * 3 - 60, np.abs(base) * 1e-39, base * 3, base * 3]
+    rows[8][rng.random(vocab) < 0.9] = -math.inf
+    rows[9][rng.random(vocab) < 0.9] = float(torch.finfo(BF).min)
+    T = [1.0, 0.7, 1e-3, 3e-21, 40.0, 1.0, 1e30, 0.02, 1.3, 1.3, 2.0, 1e-39, 1e5, 1e38]
+    x = torch.from_numpy(np.stack(rows)).to(BF)
+    n = len(rows)
+    _check(x, rng.random(n).tolist(), T, None, None if p is None else [p] * n)
+    _check(x, rng.random(n).tolist(), T, None, None if p is None else [p] * n, [1e-5] * n)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 def test_temperatures_below_the_least(dtype):
     # a positive temperature below 2^-127 counts as 2^-127: logits of that size tell them apart
     x = (torch.randn(12, 300, dtype=torch.float64, generator=torch.Generator().manual_seed(6)) * 1e-38).to(dtype)
