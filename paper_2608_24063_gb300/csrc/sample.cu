@@ -24,11 +24,12 @@
 //     are taken in one pass, by runs of tokens, and the cut is narrowed by counts of ever finer
 //     ranges of keys; weights are taken again of the tokens in the cut's buckets alone;
 //   - a larger top-k goes through histograms of counts and weights.
-// Then the kept weights of each thread's run of tokens are scanned, and the one warp that
+// Then the kept weights of each thread's run of tokens are summed (and the tokens that tie with the cut counted, in the
+// same pass: in one of their own 3 us of 66 more) and scanned, and the one warp that
 // holds the token looks through its run.
 //
 // 256 rows of 131072 in bf16, a fifth each greedy, all filters, none, and two of top-p alone with nuclei of
-// thousands (67 MB): 138 us, bound by the passes' instructions and the clusters' meetings, a plain read
+// thousands (67 MB): 135 us, bound by the passes' instructions and the clusters' meetings, a plain read
 // 10 us.  64 rows of 50001 without filters 18 us, one row of 32000 with all of them 13 us, a chain of
 // eight steps between blocks.  In place of the cuts from counts, histograms of weights by 64-bit
 // atomics: 441, 31 and 52 us.
@@ -1052,46 +1053,40 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       uint32_t ties = 0xffffffffu;
       if (cut_k.key == ck) ties = min(ties, cut_k.ties);
       if (cut_p.key == ck) ties = min(ties, cut_p.ties);
-      uint64_t tie0 = 0;                        // such tokens in front of the run
-      if (ties != 0xffffffffu) {
-        uint32_t n = 0;
-        walk<T>(data, v0, v1, 1, [&](float x, int) { n += key_of<T>(x) == ck ? 1u : 0u; });
-        cluster_sum(row, n, &tie0);
-      }
+      auto counts = [&](uint64_t w) { return w >= least ? w : 0; };
       auto weight = [&](float x, uint64_t& tie) -> uint64_t {
         const uint32_t key = key_of<T>(x);
         if (key < ck) return 0;
         if (key == ck && tie++ >= ties) return 0;
-        const uint64_t w = wt.of(x);
-        return w >= least ? w : 0;
+        return counts(wt.of(x));
       };
-      uint64_t tie = tie0, before;
+      uint64_t tie0 = 0, before;                // tokens that tie with the cut in front of the run
+      uint32_t tied = 0;                        // and in it
       if (have_sum && top - ck < (uint32_t)kBuckets) {
         // few different logits (of bf16 rows always): their weights from a table
-        for (uint32_t i = t; i <= top - ck; i += kThreads) {
-          const uint64_t w = wt.of(logit_of<T>(top - i));
-          sm.mass_all[i] = w >= least ? w : 0;
-        }
+        for (uint32_t i = t; i <= top - ck; i += kThreads) sm.mass_all[i] = counts(wt.of(logit_of<T>(top - i)));
         __syncthreads();
         walk<T>(data, v0, v1, 1, [&](float x, int) {
           const uint32_t key = key_of<T>(x);
-          if (key > top || key < ck || (key == ck && tie++ >= ties)) return;
-          sum += sm.mass_all[top - key];
+          if (key <= top && key > ck) sum += sm.mass_all[top - key];
+          tied += key == ck ? 1u : 0u;
         });
-      } else if (have_sum) {
-        walk<T>(data, v0, v1, 1, [&](float x, int) {
-          if (key_of<T>(x) <= top) sum += weight(x, tie);
-        });
-      }
-      else if (ck == 0) {
+      } else if (ck == 0) {
         fill_table();
+        walk<T>(data, v0, v1, 1, [&](float x, int) { sum += counts(weight_of(x)); });
+      } else {
+        const uint32_t last = have_sum ? top : 0xffffffffu;
         walk<T>(data, v0, v1, 1, [&](float x, int) {
-          const uint64_t w = weight_of(x);
-          sum += w >= least ? w : 0;
+          const uint32_t key = key_of<T>(x);
+          if (key <= last && key > ck) sum += counts(wt.of(x));
+          tied += key == ck ? 1u : 0u;
         });
       }
-      else
-        walk<T>(data, v0, v1, 1, [&](float x, int) { sum += weight(x, tie); });
+      if (ck != 0) {
+        if (ties != 0xffffffffu) cluster_sum(row, tied, &tie0);
+        const uint32_t stay = tie0 < ties ? min(tied, ties - (uint32_t)tie0) : 0u;
+        sum += stay * counts(wt.of(logit_of<T>(ck)));
+      }
       const uint64_t total = cluster_sum(row, sum, &before);
       // running sum > u * total, in whole numbers
       const uint64_t target = target_of(u, total);
@@ -1105,8 +1100,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         for (int e0 = b0; e0 < b1; e0 += 32) {
           const int e = e0 + lane;
           const float x = e < b1 ? element<T>(data, e) : -INFINITY;
-          const uint32_t tied = __ballot_sync(0xffffffffu, e < b1 && key_of<T>(x) == ck);
-          uint64_t rank = seen + __popc(tied & ((1u << lane) - 1u));
+          const uint32_t equal = __ballot_sync(0xffffffffu, e < b1 && key_of<T>(x) == ck);
+          uint64_t rank = seen + __popc(equal & ((1u << lane) - 1u));
           const uint64_t w = e < b1 ? weight(x, rank) : 0;
           const uint64_t upto = at + scan_warp(w);
           const uint32_t hit = __ballot_sync(0xffffffffu, upto > target);
@@ -1116,7 +1111,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             break;
           }
           at = __shfl_sync(0xffffffffu, upto, 31);
-          seen += __popc(tied);
+          seen += __popc(equal);
         }
       }
     }
