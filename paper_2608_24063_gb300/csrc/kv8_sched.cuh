@@ -4,7 +4,7 @@
 // request's group of query heads (row rho = i * G + j is query head j of the
 // group at the request's row i) over the tiles of KT keys that any of them
 // sees, at least one tile.  The units' tiles, in order of request, row tile,
-// KV head, form one line of T tiles; block i of N takes tiles
+// KV head, form one line (kv8_line.cuh) of T tiles; block i of N takes tiles
 // of it in turn, T / N of them and one more for the first T % N blocks.  So every
 // block has the same number of tiles whatever the lengths are, a long unit is split over blocks, and a
 // block's piece of a unit is a "segment".  A segment that is not a whole unit
@@ -24,6 +24,7 @@
 
 #include "kernels.h"
 #include "kv8.cuh"
+#include "kv8_line.cuh"
 
 namespace vc {
 
@@ -39,75 +40,6 @@ namespace kv8 {
 // What a segment's end costs, in tiles: measured on the few-rows kernel (the figures
 // above), taken for the others too, whose tiles and ends both take longer.
 constexpr int kEndTiles = 16;
-
-// Place in the line: a unit and the request's numbers.
-struct Unit {
-  int r, rt, g;          // request, row tile, KV head
-  Req8 q;
-  int tiles;             // key tiles of the unit
-  int kend;              // keys its rows see (0 .. q.len)
-};
-
-template <int MT, int KT>
-struct Line {
-  int Hkv, G, page, causal;
-
-  __device__ __forceinline__ int row_tiles(const Req8& q) const { return (q.m * G + MT - 1) / MT; }
-  // keys that the rows of row tile rt see together
-  __device__ __forceinline__ int keys(const Req8& q, int rt) const {
-    if (!causal) return q.len;
-    const int last = min(q.m - 1, ((rt + 1) * MT - 1) / G);
-    return min(q.len, max(0, q.len - q.m + last + 1));
-  }
-  __device__ __forceinline__ int tiles(int kend) const { return max(1, (kend + KT - 1) / KT); }
-  // tiles of a request's units for one KV head
-  __device__ __forceinline__ int64_t request_tiles(const Req8& q) const {
-    const int n = row_tiles(q);
-    if (!causal) return (int64_t)n * tiles(q.len);
-    int64_t sum = 0;
-    for (int rt = 0; rt < n; ++rt) sum += tiles(keys(q, rt));
-    return sum;
-  }
-  __device__ __forceinline__ void set(Unit& u) const {
-    u.kend = keys(u.q, u.rt);
-    u.tiles = tiles(u.kend);
-  }
-  // the next unit (there is one)
-  __device__ __forceinline__ void next(const vc_kv8_step& s, Unit& u, int32_t* status) const {
-    if (++u.g < Hkv) return;
-    u.g = 0;
-    if (++u.rt >= row_tiles(u.q)) {
-      u.rt = 0;
-      do {
-        ++u.r;
-        u.q = load_req(s, page, u.r, status);
-      } while (u.q.m == 0 && u.r + 1 < s.n_req);
-    }
-    set(u);
-  }
-};
-
-// a / b, in 32 bits where that holds it (the division of a few microseconds'
-// call is felt)
-__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
-  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
-// A block's share of the line.
-struct Share {
-  int64_t begin, end;      // the block's range of the line
-  int64_t per;             // tiles of a block, T / N
-  int more;                // the first T % N blocks have one more
-  int64_t tile0;           // the first unit's first tile on the line
-  Unit u;                  // the first unit
-  int pieces, piece;       // above 0: the block has this piece of that unit and no more
-
-  // the block that holds tile x of the line
-  __device__ __forceinline__ int block_of(int64_t x) const {
-    const int64_t y = x - more * (per + 1);
-    return y < 0 ? (int)divide(x, per + 1) : more + (int)divide(y, per);
-  }
-};
 
 // A split unit's pieces meet in the workspace without counters that would have
 // to be cleared: a block that has stored its piece sets the piece's flag to the
@@ -143,49 +75,6 @@ __device__ __forceinline__ void store_status(const Kv8AttnArgs& a, int32_t err) 
   }
 }
 
-// A role's walk over the block's segments.  Positions are relative to the
-// share's begin (a share is below 2^31 tiles: the host refuses longer lines).
-struct Walk {
-  Unit u;                // the segment's unit
-  int t0, t1;            // its tiles of the unit
-  int left;              // tiles of the share from t0 on
-  int rel;               // the unit's first tile, from the share's begin
-
-  __device__ __forceinline__ void start(const Share& sh) {
-    u = sh.u;
-    if (sh.pieces > 0) {
-      rel = 0;
-      t0 = u.tiles * sh.piece / sh.pieces;
-      t1 = u.tiles * (sh.piece + 1) / sh.pieces;
-      left = t1 - t0;
-      return;
-    }
-    left = (int)(sh.end - sh.begin);
-    rel = (int)(sh.tile0 - sh.begin);
-    t0 = -rel;
-    t1 = left < u.tiles - t0 ? t0 + left : u.tiles;
-  }
-  __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == u.tiles; }
-  // the next segment; false at the share's end
-  template <typename L>
-  __device__ __forceinline__ bool next(const L& line, const vc_kv8_step& s, int32_t* status) {
-    left -= t1 - t0;
-    if (left <= 0) return false;
-    rel += u.tiles;
-    line.next(s, u, status);
-    t0 = 0;
-    t1 = left < u.tiles ? left : u.tiles;
-    return true;
-  }
-  // the blocks that hold the unit's first and last tile
-  __device__ __forceinline__ int first_block(const Share& sh) const {
-    return sh.pieces > 0 ? (int)blockIdx.x - sh.piece : sh.block_of(sh.begin + rel);
-  }
-  __device__ __forceinline__ int last_block(const Share& sh) const {
-    return sh.pieces > 0 ? (int)blockIdx.x - sh.piece + sh.pieces - 1 : sh.block_of(sh.begin + rel + u.tiles - 1);
-  }
-};
-
 template <typename Int>
 __device__ __forceinline__ Int scan_warp(Int x) {
 #pragma unroll
@@ -194,35 +83,6 @@ __device__ __forceinline__ Int scan_warp(Int x) {
     if ((int)(threadIdx.x & 31) >= o) x += y;
   }
   return x;
-}
-
-// The block's range of a line of T tiles.
-__device__ __forceinline__ void set_range(Share& sh, int64_t T) {
-  const int N = (int)(T < (int64_t)gridDim.x ? T : (int64_t)gridDim.x);
-  const int i = blockIdx.x;
-  sh.per = N > 0 ? divide(T, N) : 0;
-  sh.more = (int)(T - sh.per * N);
-  sh.begin = i < N ? i * sh.per + min(i, sh.more) : 0;
-  sh.end = i < N ? sh.begin + sh.per + (i < sh.more ? 1 : 0) : 0;
-}
-
-// Finds the tile `begin` within request r, whose first tile is `at`.
-template <typename L>
-__device__ __forceinline__ void set_first(const L& line, Share& sh, int64_t begin, int64_t at, int r,
-                                          const Req8& q) {
-  Unit u;
-  u.r = r;
-  u.rt = 0;
-  u.q = q;
-  for (;; ++u.rt) {
-    line.set(u);
-    const int64_t row = (int64_t)line.Hkv * u.tiles;
-    if (begin < at + row) break;
-    at += row;
-  }
-  u.g = (int)divide(begin - at, u.tiles);
-  sh.tile0 = at + (int64_t)u.g * u.tiles;
-  sh.u = u;
 }
 
 // Computes the block's share with all of the block's NT threads; `sh` and
@@ -273,6 +133,11 @@ __device__ __forceinline__ void find_share(const L& line, const vc_kv8_step& s, 
             line.set(u);
             k = (u.tiles + per - 1) / per;
             if (at < line.Hkv * k) break;
+            if (u.rt + 1 >= rts) {              // (as in set_first)
+              set_status(status, VC_ERR_DEVICE_INDEX);
+              at = line.Hkv * k - 1;
+              break;
+            }
             at -= line.Hkv * k;
           }
           u.g = at / k;
@@ -292,7 +157,7 @@ __device__ __forceinline__ void find_share(const L& line, const vc_kv8_step& s, 
           sh.more = x.more;
           sh.pieces = 0;
         }
-        if (x.begin < x.end && x.begin >= upto - w && x.begin < upto) set_first(line, sh, x.begin, upto - w, lane, q);
+        if (x.begin < x.end && x.begin >= upto - w && x.begin < upto) set_first(line, sh, x.begin, upto - w, lane, q, status);
       }
     }
     __syncthreads();
@@ -325,7 +190,7 @@ __device__ __forceinline__ void find_share(const L& line, const vc_kv8_step& s, 
       const Req8 q = load_req(s, line.page, r, status);
       const int64_t w = line.Hkv * line.request_tiles(q);
       if (x.begin < at + w) {
-        set_first(line, sh, x.begin, at, r, q);
+        set_first(line, sh, x.begin, at, r, q, status);
         break;
       }
       at += w;

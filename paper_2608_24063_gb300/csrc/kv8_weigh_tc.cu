@@ -90,46 +90,6 @@ struct alignas(1024) SmemW {
   int32_t err;
 };
 
-// The line of steps: a unit's "row tile" is its group of K tiles, its "tiles" are the
-// steps, RB = N / G request rows of all G heads of a group, that see any of it.
-template <int N>
-struct Steps {
-  int Hkv, RB, page, causal;
-
-  __device__ __forceinline__ int row_tiles(const Req8& q) const { return q.m > 0 ? (q.len + kGroup - 1) / kGroup : 0; }
-  __device__ __forceinline__ int blocks(const Req8& q) const { return (q.m + RB - 1) / RB; }
-  // the first step with a row that sees token t
-  __device__ __forceinline__ int first_block(const Req8& q, int t) const {
-    return causal ? max(0, t - (q.len - q.m)) / RB : 0;
-  }
-  __device__ __forceinline__ int keys(const Req8& q, int rt) const { return blocks(q) - first_block(q, rt * kGroup); }
-  __device__ __forceinline__ int tiles(int steps) const { return steps; }
-  __device__ __forceinline__ int64_t request_tiles(const Req8& q) const {
-    const int n = row_tiles(q);
-    // groups that start before the step's own tokens are seen by every row
-    const int full = causal ? min(n, max(0, q.len - q.m) / kGroup + 1) : n;
-    int64_t sum = (int64_t)full * blocks(q);
-    for (int rt = full; rt < n; ++rt) sum += keys(q, rt);
-    return sum;
-  }
-  __device__ __forceinline__ void set(Unit& u) const {
-    u.kend = min(u.q.len - u.rt * kGroup, kGroup);      // tokens of the group
-    u.tiles = keys(u.q, u.rt);
-  }
-  __device__ __forceinline__ void next(const vc_kv8_step& s, Unit& u, int32_t* status) const {
-    if (++u.g < Hkv) return;
-    u.g = 0;
-    if (++u.rt >= row_tiles(u.q)) {
-      u.rt = 0;
-      do {
-        ++u.r;
-        u.q = load_req(s, page, u.r, status);
-      } while (row_tiles(u.q) == 0 && u.r + 1 < s.n_req);
-    }
-    set(u);
-  }
-};
-
 // 3-D tile load: box at (x = element, y = head, z = row) -> smem, completes on bar.
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z,
                                             uint64_t* bar) {
@@ -245,7 +205,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
   SmemW<T, D>& sm = *reinterpret_cast<SmemW<T, D>*>(smem_weigh);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int G = a.Hq / c.Hkv, RB = N / G;       // (the host sends G <= N)
-  const Steps<N> line{c.Hkv, RB, c.page, a.causal};
+  const Steps<N, kGroup> line{c.Hkv, RB, c.page, a.causal};
   auto report = [&](int32_t err) {
     a.block_status[blockIdx.x] = err;
     if (blockIdx.x == 0) {
