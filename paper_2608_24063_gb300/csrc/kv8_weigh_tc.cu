@@ -327,9 +327,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kv8_weigh_tc_kernel(const __gri
           const int i = (b0 + b) * RB + li[k];
           lv[k] = -INFINITY;
           if (li[k] < RB && i >= dead && i < q.m) {
+            // (an infinite lse, which adds nothing, stays out of the product: its second factor may be negative or 0)
             const float l = __ldg(lp[k] + (int64_t)(b0 + b) * RB * a.Hq);
-            lv[k] = -fmaf(l, a.lse_log2, l * a.lse_log2_lo);
-            if (lv[k] == INFINITY) lv[k] = -INFINITY;
+            if (fabsf(l) != INFINITY) lv[k] = -fmaf(l, a.lse_log2, l * a.lse_log2_lo);
           }
         }
       };
