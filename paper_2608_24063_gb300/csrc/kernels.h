@@ -177,11 +177,6 @@ struct NormRopeGrad {
   float eps;
   int32_t nq;                          // blocks of query heads, the first
 };
-constexpr int kNormGradBlocks = 304;   // blocks of the gradient at most, two for each of 152 SMs
-struct NormGradGrid {
-  int nq, nk;
-};
-NormGradGrid norm_grad_grid(int64_t n_rows, int32_t Hq, int32_t Hkv);
 cudaError_t launch_norm_mrope_grad(const RopeArgs& a, NormRopeGrad& p, int dtype, int d, bool adjacent, float* dwq,
                                    float* dwk, cudaStream_t st);
 

@@ -8,6 +8,7 @@
 
 #include "api_util.h"
 #include "kernels.h"
+#include "norm_grid.h"
 #include "viscache_step.h"
 
 namespace vc {

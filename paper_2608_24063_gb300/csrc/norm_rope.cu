@@ -20,6 +20,7 @@
 // Sums of squares that pass fp32's range are taken again of values times 2^-70: the
 // branch costs nothing where it is not taken.
 #include "kernels.h"
+#include "norm_grid.h"
 #include "profile.h"
 #include "rope.cuh"
 #include "vc_common.cuh"
@@ -169,7 +170,6 @@ __global__ void __launch_bounds__(kThreads) norm_mrope_kernel(const __grid_const
 // thread sums one weight's gradient (16 channels of its slot) in registers; a block
 // walks over groups of RB rows, whose angles it computes once.  The block's sums go
 // to the workspace, one row of D a block.
-constexpr int kGradRows = 16;
 template <typename T, int D, bool ADJ>
 __global__ void __launch_bounds__(kThreads) norm_mrope_grad_kernel(const __grid_constant__ RopeArgs a,
                                                                    const __grid_constant__ NormRopeGrad p) {
@@ -351,22 +351,6 @@ cudaError_t grad_t(const RopeArgs& a, NormRopeGrad& p, float* dwq, float* dwk, c
 }
 
 }  // namespace
-
-// Blocks of query and of key heads: by what a group of rows costs, its heads in turns of 32
-// and kGroupTurns more for its angles and its first loads; no more than there are groups.
-// 12544 rows of 28 + 4 heads of 128, us: by the heads alone 120, so 89.
-constexpr int kGroupTurns = 3;
-NormGradGrid norm_grad_grid(int64_t n_rows, int32_t Hq, int32_t Hkv) {
-  const int64_t groups = (n_rows + kGradRows - 1) / kGradRows;
-  auto cost = [](int64_t H) { return H > 0 ? (H * kGradRows + 31) / 32 + kGroupTurns : (int64_t)0; };
-  const int64_t cq = cost(Hq), ck = cost(Hkv);
-  int64_t nk = (kNormGradBlocks * ck + cq + ck - 1) / (cq + ck), nq = kNormGradBlocks - nk;
-  if (Hq > 0 && nq < 1) nq = 1;
-  NormGradGrid g;
-  g.nq = (int)(Hq > 0 ? (nq < groups ? nq : groups) : 0);
-  g.nk = (int)(nk < groups ? nk : groups);
-  return g;
-}
 
 #define VC_DISPATCH(F, ...)                                                                       \
   (dtype == VC_BF16 ? (d == 128 ? (adjacent ? F<__nv_bfloat16, 128, true>(__VA_ARGS__)            \
