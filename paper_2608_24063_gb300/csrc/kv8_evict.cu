@@ -100,6 +100,10 @@ __global__ void __launch_bounds__(kSelThreads) kv8_evict_select_kernel(const __g
     if (t == 0) a.units[unit] = {kNoGap, len, bad ? VC_ERR_DEVICE_INDEX : err, 0};
     return;
   }
+  if (keep == 0) {                              // nothing to choose
+    if (t == 0) a.units[unit] = {0, 0, err, 0};
+    return;
+  }
   const int32_t* table = s.block_table + (int64_t)r * s.max_pages;
   auto fetch = [&](int i) {
     if (i < a.sink || i >= len - a.recent) return kInfKey;
@@ -130,12 +134,11 @@ __global__ void __launch_bounds__(kSelThreads) kv8_evict_select_kernel(const __g
       }
     }
   }
-  auto key = [&](int i) { return held ? cache[i] : fetch(i); };
+  auto key = [&](int i) { return held ? cache[i] : fetch(i); };      // (of other threads' too: past a barrier)
   // the keep-th largest key: digit by digit from the top
   uint32_t prefix = 0u, mask = 0u;
   int need = keep;                              // how many of the keys under the prefix stay
-  bool all = need == 0;
-  if (need == 0) prefix = 0xffffffffu;          // no key is that large
+  bool all = false;
   for (int pass = 0; pass < 3 && !all; ++pass) {
     const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
     for (int i = t; i < kBins; i += kSelThreads) hist[i] = 0;
