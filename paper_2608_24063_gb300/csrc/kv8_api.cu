@@ -156,6 +156,14 @@ Kernel kernel_of(const vc_kv8& c, const vc_kv8_step& s, int dtype, int32_t Hq) {
 //   one of 8192, 24 rows 20 / 28, 48 rows 28 / 28
 constexpr int64_t kWeighTcRows = 64, kWeighTcRowsF32 = 32;
 
+// What the tensor cores cut off a score, on average, in 2^-24 of it ([kernel: few rows, many][bf16, fp32][d = 64,
+// 128]): a product's fp32 sum is cut, not rounded, at each of its steps of 16 dimensions, fp32 rows have twice as many,
+// and bf16 rows have fewer bits to lose.  Measured at scores of 15 and 38 (sums of the weights against 64 bits, 8
+// requests of 256 rows and 64 of 2, 1024 tokens; normal and uniform values, rows and pages of different size, outlier
+// channels, rows along a key), by data: few rows .2-.6, .4-1.5 | 2.1-3.2, 3.7-5.4; many .15-.6, .4-1.2 | .9-1.3, 1.4-2.4.
+// The factors are set off by the middle; what is left is of the size of fp32's rounding of a score.
+constexpr double kWeighCut[2][2][2] = {{{0.35, 0.8}, {2.4, 4.3}}, {{0.35, 0.75}, {1.1, 1.8}}};
+
 bool valid_heads(int32_t Hq, int32_t Hkv) { return Hkv >= 1 && Hq >= Hkv && Hq <= 4096 && Hq % Hkv == 0; }
 
 // The attention's line of key tiles (units of 8 rows at least): a block's share is
@@ -365,11 +373,15 @@ int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, 
   a.weights = weights;
   a.Hq = Hq;
   a.causal = causal != 0;
+  // (a step there holds all heads of a group: 128 fit in both types)
+  const bool many = (int64_t)step->n_rows * (Hq / cache->Hkv) > (dtype == VC_F32 ? kWeighTcRowsF32 : kWeighTcRows) * step->n_req &&
+                    Hq / cache->Hkv <= 128;
   const double exact = scale == 0.f ? 1.0 / sqrt((double)cache->d) : (double)scale;
-  a.scale = (float)exact;
-  constexpr double kLog2eExact = 1.4426950408889634074, kCut = 0.7213 * 0x1p-24;
+  const double cut = kWeighCut[many][dtype == VC_F32][cache->d == 128] * 0x1p-24;
+  a.scale = (float)fmin(exact * (1.0 + cut), 3.4028234663852886e38);
+  constexpr double kLog2eExact = 1.4426950408889634074;
   a.scale_log2 = (float)(exact * kLog2eExact);
-  const double factor = exact > 0.0 ? (double)a.scale_log2 / exact * (1.0 - kCut) : kLog2eExact;
+  const double factor = exact > 0.0 ? (double)a.scale_log2 / exact * (1.0 - cut) : kLog2eExact;
   a.lse_log2 = (float)factor;
   a.lse_log2_lo = (float)(factor - (double)a.lse_log2);
   a.status = reinterpret_cast<int32_t*>(base);
@@ -377,9 +389,6 @@ int viscache_kv8_weigh(const vc_kv8* cache, const vc_kv8_step* step, int dtype, 
   a.token = next_token();
   a.flags = reinterpret_cast<uint64_t*>(base + w.o_flags);
   a.part = reinterpret_cast<float*>(base + w.o_o);
-  // (a step there holds all heads of a group: 128 fit in both types)
-  const bool many = (int64_t)step->n_rows * (Hq / cache->Hkv) > (dtype == VC_F32 ? kWeighTcRowsF32 : kWeighTcRows) * step->n_req &&
-                    Hq / cache->Hkv <= 128;
   return cuda_status(many ? launch_kv8_weigh_tc(*cache, *step, dtype, a, st)
                           : launch_kv8_weigh(*cache, *step, dtype, a, st));
 }
