@@ -26,7 +26,8 @@ __device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t packe
 
 // The warp's query fragments, normalised (lane (gid, tig): row 8 n + gid of the
 // unit, dimensions tig * D/4 ...), and the power of two of rows 8 n + 2 tig, + 1.
-template <typename T, int D, int NQ, int NP>
+// TOKENS: rows that are no tokens (more rows than tokens) count as 0.
+template <typename T, int D, int NQ, int NP, bool TOKENS = false>
 __device__ __forceinline__ void load_q(const T* q, int64_t q_stride, const Unit& u, int G,
                                        uint32_t (&f)[NP][NQ][D / 16][2], float (&qs)[NQ][2]) {
   constexpr int DPT = D / 4;                    // dimensions of a thread
@@ -36,7 +37,7 @@ __device__ __forceinline__ void load_q(const T* q, int64_t q_stride, const Unit&
     const int rho = u.rt * 8 * NQ + 8 * n + gid;
     float x[DPT];
     float amax = 0.f;
-    if (rho < u.q.m * G) {
+    if (rho < u.q.m * G && (!TOKENS || rho >= (u.q.m - u.q.len) * G)) {
       const int i = rho / G, j = rho - i * G;
       const T* src = q + (int64_t)(u.q.row0 + i) * q_stride + (int64_t)(u.g * G + j) * D + tig * DPT;
 #pragma unroll

@@ -165,17 +165,16 @@ kv8_weigh_kernel(const __grid_constant__ vc_kv8 c, const __grid_constant__ vc_kv
       u.q = q;
       u.g = cur.g;
       u.rt = rt;
-      load_q<T, D, NQ, NP>(static_cast<const T*>(a.q), a.q_stride, u, G, qf, qs);
+      // (rows that are no tokens count as 0: theirs may hold anything, and not causal nothing masks them)
+      load_q<T, D, NQ, NP, true>(static_cast<const T*>(a.q), a.q_stride, u, G, qf, qs);
       const int base = q.len - q.m + 1, r0 = rt * MT;
-      // tokens that row i sees: rows that are no tokens see none, causal or not, whatever their queries hold
-      auto limit = [&](int i) { return a.causal || base + i <= 0 ? base + i : 0x7fffffff; };
-      lim_min = limit(r0 / G);
+      lim_min = a.causal ? base + r0 / G : 0x7fffffff;
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int rho = r0 + 8 * n + 2 * tig + h, i = rho / G;
-          lim[n][h] = limit(i);
+          lim[n][h] = a.causal ? base + i : 0x7fffffff;
           // rows that are none, see nothing or are no tokens add exp(-inf)
           float l = INFINITY;
           if (i < q.m && base + i > 0) {
