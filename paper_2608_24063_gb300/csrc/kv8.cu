@@ -97,6 +97,8 @@ struct UnitCfg {
   static_assert(NV * THREADS == VECS, "whole vectors");
 };
 
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+
 // Sixteen values as they lie in memory.
 template <typename T>
 struct Raw16 {
@@ -171,6 +173,36 @@ __device__ __forceinline__ void store16(float* p, const float (&v)[16]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+
+// Sixteen values times `inv` as codes; with CHECK what is not finite becomes NaN and
+// products stop at `top`.
+template <bool CHECK>
+__device__ __forceinline__ uint4 encode16(const float (&v)[16], float inv, float top) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float y = v[4 * i + k];
+      if constexpr (CHECK) x[k] = finite(y) ? fminf(fmaxf(y * inv, -top), top) : __uint_as_float(0x7fffffffu);
+      else x[k] = y * inv;
+    }
+    w[i] = f32x2_to_e4m3x2(x[0], x[1]) | f32x2_to_e4m3x2(x[2], x[3]) << 16;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ void decode16(const uint4& c, float (&v)[16]) {
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t h = e4m3x2_to_f16x2(w[i >> 1] >> (16 * (i & 1)));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    v[2 * i] = f.x;
+    v[2 * i + 1] = f.y;
+  }
 }
 
 // Block 0 checks every request and every page that the step touches, and stores

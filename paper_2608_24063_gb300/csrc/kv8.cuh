@@ -87,38 +87,6 @@ __device__ __forceinline__ float scale_log2(float s) { return fmaxf((float)(int)
 __device__ __forceinline__ float pow2_bits(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 __device__ __forceinline__ float2 pow2_factors(int e) { return make_float2(pow2_bits(e >> 1), pow2_bits(e - (e >> 1))); }
 
-__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
-
-// Sixteen values times `inv` as codes; with CHECK what is not finite becomes NaN and
-// products stop at `top`.
-template <bool CHECK>
-__device__ __forceinline__ uint4 encode16(const float (&v)[16], float inv, float top) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float y = v[4 * i + k];
-      if constexpr (CHECK) x[k] = finite(y) ? fminf(fmaxf(y * inv, -top), top) : __uint_as_float(0x7fffffffu);
-      else x[k] = y * inv;
-    }
-    w[i] = f32x2_to_e4m3x2(x[0], x[1]) | f32x2_to_e4m3x2(x[2], x[3]) << 16;
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-__device__ __forceinline__ void decode16(const uint4& c, float (&v)[16]) {
-  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t h = e4m3x2_to_f16x2(w[i >> 1] >> (16 * (i & 1)));
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    v[2 * i] = f.x;
-    v[2 * i + 1] = f.y;
-  }
-}
-
 // A value that is NaN spoils the sums of rows that see it and no others.  A product
 // takes 0 * NaN for a row that does not, so where a tile has tokens that some of the
 // unit's rows do not see, NaN codes of V count as 0 and the first such token is
