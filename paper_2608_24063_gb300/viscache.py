@@ -901,7 +901,7 @@ def viscache_kv8_evict(cache: Kv8Cache, step: Kv8Step, weights: torch.Tensor, ke
     the step's seq_lens."""
     fn = "viscache_kv8_evict"
     dev, n = _current_device(), step.c.n_req
-    if cache.index != dev or step.index != dev:
+    if cache.index != dev or step.index != dev or max_keep < 1:
         raise VisCacheError(fn, VC_ERR_INVALID_ARG)
     if kept is None:
         kept = _empty((n, cache.Hkv, max_keep), torch.int32, cache.device, stream)

@@ -51,3 +51,13 @@ def test_nothing_stays(lens, page):
         assert vc.prunekv_get_status(ws) == vc.VC_OK
         assert new_lens.tolist() == [0] * n and (kept == -7).all()
         assert all(torch.equal(x, y) for x, y in zip(before, (*codes, *scales, weights)))
+
+
+def test_binding_refuses_no_room_for_the_list():
+    codes = torch.zeros(2, 1, 16, 64, dtype=torch.uint8, device=DEV)
+    cache = vc.Kv8Cache(codes, codes.clone(), torch.ones(2, 1, device=DEV), torch.ones(2, 1, device=DEV))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    step = vc.Kv8Step(i32([[0, 1]]), i32([20]), i32([0, 1]), 1)
+    for max_keep in (0, -1):
+        with pytest.raises(vc.VisCacheError):
+            vc.viscache_kv8_evict(cache, step, torch.zeros(2, 1, 16, device=DEV), i32([0]), max_keep)
