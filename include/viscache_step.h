@@ -74,7 +74,8 @@ int viscache_norm_mrope_grad(const vc_rope* rope, const int32_t* positions, int 
  * `scale` mean what they mean in viscache_kv8_attention, whose `lse` this call
  * reads; it is called after the rows have been appended and attended.
  *   lse       device fp32 [n_rows][Hq].  A row whose lse is -inf (one that sees
- *             no token) adds nothing
+ *             no token) adds nothing; a row that is no token (more rows than
+ *             tokens) adds nothing whatever its queries and its lse hold
  *   weights   device fp32 [n_pages][Hkv][page], a number for every slot of the
  *             pool; 16-byte aligned.  Slots past seq_lens are left as they were.
  * The pages of a call's requests must be different ones (a page of two requests
@@ -85,7 +86,9 @@ int viscache_norm_mrope_grad(const vc_rope* rope, const int32_t* positions, int 
  * average) as they are, so that their values' products with codes have to stay below
  * 2^127 there, and count as 0 below 2^-126.  Scores as there below 2^22.  Sums in fp32
  * in an order that the call's sizes, lengths and the device's SMs decide: the same
- * call gives the same bits.  A key that is not finite makes its token's weight NaN.
+ * call gives the same bits.  A key that is not finite makes its token's weight NaN; the
+ * attention's lse of a row that sees it is NaN, and a row with such an lse makes the
+ * weights of all tokens that it sees NaN, which they then stay.
  * After VC_ERR_DEVICE_TIMEOUT (prunekv_get_status) clear the workspace before a
  * captured call is replayed with it.
  * Workspace: viscache_kv8_workspace_size(n_rows, Hq, Hkv, d), as for the

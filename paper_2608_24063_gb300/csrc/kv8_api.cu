@@ -148,8 +148,10 @@ Kernel kernel_of(const vc_kv8& c, const vc_kv8_step& s, int dtype, int32_t Hq) {
 
 // viscache_kv8_weigh on tcgen05: more packed rows of a KV head per request on average than
 // this.  The mma.sync kernel reads a chunk's codes once and its rows 16 at a time; the
-// other expands each K tile once however many rows there are.  d = 128, 8 KV heads, us on
-// mma.sync / tcgen05 (cold):
+// other expands each K tile once however many rows there are.  The average, because rows are
+// on the device: a long request among short ones takes the mma.sync kernel, whose shares count
+// chunks and not rows (64 requests of 4096 tokens, one of 256 rows and 63 of one: 6.3 ms).
+// d = 128, 8 KV heads, lengths drawn up to those given, us on mma.sync / tcgen05 (cold):
 //   bf16, 64 requests of 4096 tokens, 24 rows 113 / 259, 48 rows 169 / 259, 128 rows 384 / 261
 //   8 of 8192 tokens, 48 rows 58 / 72, 128 rows 118 / 73; one of 8192, 48 rows 20 / 30, 128 rows 34 / 30
 //   fp32, 64 of 4096, 24 rows 160 / 228, 48 rows 267 / 231; 8 of 8192, 24 rows 51 / 63, 48 rows 81 / 63

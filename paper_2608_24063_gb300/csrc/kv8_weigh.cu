@@ -12,16 +12,20 @@
 // codes become fragments); the queries' fragments stay in registers while the head lasts.
 //
 // Numbers: query rows as in kv8_attn.cu (powers of two, one fp16 part of bf16 rows,
-// two of fp32 rows); the exponent is (product * scale - lse) * log2(e): product times
-// the powers of two is exact, the subtraction is one fused multiply-add, so a large
-// lse costs no bits.
+// two of fp32 rows, 22 bits); the exponent is (product * scale - lse) * log2(e): product
+// times the powers of two is exact, the subtraction is one fused multiply-add, so a large
+// lse costs no bits.  The tensor cores cut a product's fp32 sums off; the scale is larger
+// by what that is on average (kWeighCut, kv8_api.cu: fp32 rows of 128, whose weights at
+// scores of 15 were short by 4.0e-6, are off by 1e-7 to 7e-7 on average).
 //
 // 32 requests of up to 32768 tokens, 64 / 8 heads of 128 (718 MB): 117 us, 6.1 TB/s, 92% of a plain
 // copy's rate (138 us from cold memory).  6 x 5 fp32 rows over 3136 tokens: 8 us, a launch, the
 // lengths, a page, a chunk.
 //
 // Requests of more rows than the fragments hold run over their rows 16 at a time for
-// each chunk; many rows belong to kv8_weigh_tc.cu.
+// each chunk, which a warp's share does not count: one request of 256 rows among 63 of
+// one, 4096 tokens each, takes 6.3 ms, all of one row 70 us.  Many rows belong to
+// kv8_weigh_tc.cu.
 #include "kernels.h"
 #include "kv8.cuh"
 #include "kv8_mma.cuh"
@@ -326,7 +330,7 @@ cudaError_t launch_c(const vc_kv8& c, const vc_kv8_step& s, const Kv8WeighArgs& 
 template <typename T, int D>
 cudaError_t launch_q(const vc_kv8& c, const vc_kv8_step& s, const Kv8WeighArgs& a, cudaStream_t st) {
   // Fragments of 8 query rows where the requests have no more on average, of bf16 calls; else of 16.  Us with 8 / with
-  // 16, cold: 64 requests of 4096 tokens, 16 rows 94 / 50, 24 rows 127 / 113, 128 rows 529 / 384; 8 rows of fp32 52 / 80;
+  // 16, cold: 64 requests of up to 4096 tokens, 16 rows 94 / 50, 24 rows 127 / 113, 128 rows 529 / 384; 8 rows of fp32 52 / 80;
   // fp32 24 rows 160 / 180, 48 rows 267 / 286 (the larger ones spill)
   const int64_t rows = (int64_t)s.n_rows * (a.Hq / c.Hkv);
   return rows <= 8 * (int64_t)s.n_req ? launch_c<T, D, 1>(c, s, a, st) : launch_c<T, D, 2>(c, s, a, st);

@@ -27,21 +27,26 @@
 // MMAs.
 //
 // Numbers: the exponent is one fused multiply-add, product * (scale log2(e)) - lse log2(e),
-// with factors that agree: the first is off by its rounding and by what the tensor cores
-// cut off a sum (half a unit of fp32's last place on average, 0.72 * 2^-24 of a sum whose
-// mantissa is spread as such sums are; scores of 12 came out short by 6.8e-7), so lse's
+// with factors that agree: the first is off by its rounding (2^-24 at most) and by what the
+// tensor cores cut off a sum (kWeighCut, kv8_api.cu, by type and head size), so lse's
 // factor, in two parts, is off by the same: a term that counts has a score near its lse,
-// and the two cancel.  Other roundings go either way and average out over a token's rows.
+// and the two cancel.  What is left of the cut on average, at scores of 15: 2 to 5e-7 either
+// way by the data (-15e-7 to 5e-7 with one constant for all); flat rows, whose scores lie far
+// below their lse, are off by the first factor's rounding times that distance (4e-7 at 7).
+// Other roundings go either way and average out over a token's rows.
 // A tile's terms are added in eight partial sums, tiles with a compensated sum, so 16384
 // rows cost no more bits than 16.
 //
 // 2048 rows over 32768 tokens, 64 / 8 heads of 128 (1.07 TFLOP, 4.3 G exponentials): 0.93 ms, 1.16
-// PFLOP/s, 61% of the cuBLAS rate.  Bound by the epilogue: a product's MMAs take 1024 clocks, its
-// exponentials 1190 (measured alone), all of it about 1600 at the 1.5 GHz that the card holds
-// under it.  At 1.00 ms, without exponentials 0.90, without MMAs 0.99, with a quarter of the
-// epilogue 0.66; eight epilogue warps 1.05; two groups of eight that take products in turn
+// PFLOP/s, 61% of the cuBLAS rate.  Bound by the epilogue, of which the exponentials are the
+// smaller part: at 1.00 ms it took 0.90 without them, 0.99 without MMAs, 0.66 with a quarter of
+// the epilogue (loads from tensor memory, of lse, multiply-adds, sums, exponentials).  A product's
+// MMAs take 1024 clocks, its exponentials 1190 (alone), all of it about 1600 at the 1.5 GHz that
+// the card holds under it; the tensor pipe, the special functions and the issue of instructions
+// are half busy each.  Eight epilogue warps 1.05; two groups of eight that take products in turn
 // 1.14, four with buffers of 128 columns 1.10; all of a warp's columns loaded at once 1.06 ms.
-// Few steps a unit: 64 requests of 128 rows over 4096 tokens 261 us, 7 us a unit, a chain of its
+// fp32 rows, the same chunk: 3.55 ms, two products a part and rows brought by four warps.
+// Few steps a unit: 64 requests of 128 rows over up to 4096 tokens 261 us, 7 us a unit, a chain of its
 // codes, products, sums and old weights (K expanded by the four loaders 353 us).  One fp32 step
 // holds 128 rows in two parts.
 #include "kernels.h"

@@ -14,7 +14,7 @@ struct NormGradGrid {
 
 // Blocks of query and of key heads: by what a group of rows costs, its heads in turns of 32
 // and kGroupTurns more for its angles and its first loads; no more than there are groups.
-// 12544 rows of 28 + 4 heads of 128, us: by the heads alone 120, so 89.
+// 12544 rows of 28 + 4 heads of 128, us (cold): by the heads alone 120, so 89.
 constexpr int kGroupTurns = 3;
 inline NormGradGrid norm_grad_grid(int64_t n_rows, int32_t Hq, int32_t Hkv) {
   const int64_t groups = (n_rows + kGradRows - 1) / kGradRows;
